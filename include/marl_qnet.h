@@ -58,7 +58,8 @@ extern "C" {
 #define MARL_ERR_BAD_DIM   -2   /* a size is <= 0 or outside the supported range */
 #define MARL_ERR_BAD_DTYPE -3   /* weight_dtype is not MARL_DTYPE_F32 / MARL_DTYPE_BF16 */
 #define MARL_ERR_MISMATCH  -4   /* n_weights != parameter count, or online/target differ */
-#define MARL_ERR_BAD_ARG   -5   /* epsilon or gamma outside [0,1] or not finite */
+#define MARL_ERR_BAD_ARG   -5   /* a scalar (epsilon, gamma, ...) outside its range or not finite, a misaligned
+                                   pointer, or arrays that may not be the same */
 #define MARL_ERR_DEVICE    -6   /* a HIP runtime call failed; see marl_last_device_error */
 #define MARL_ERR_NOMEM     -7   /* host or device allocation failed */
 
@@ -436,6 +437,135 @@ int marl_qnet_timing_read(marl_qnet *q, float *act_ms, int32_t *act_calls, float
  */
 int marl_probe_stream(const void *src, void *dst, size_t bytes, float *sink, void *hip_stream);
 int marl_probe_mfma(int32_t iters, float *sink, double *flops, void *hip_stream);
+
+/*
+ * Operators of a policy learner, beside the Q-network: a memory that is trained over whole sequences at once, the
+ * log probabilities its loss and its sampling need, and an update for weight matrices.  They have no handle: every
+ * call works on the current device, on arrays of the caller.  `dtype` is the element type of the arrays marked
+ * "elem" below (MARL_DTYPE_F32, _BF16, _F16); arithmetic, states and sums are fp32 (norms fp64) and each output is
+ * rounded once, to nearest even.  Rows with an ld_* argument lie that many elements apart, so that column blocks of a
+ * wider array can be passed; within a row elements are adjacent, and any element alignment is served (16-byte
+ * aligned rows are faster).  A workspace is 256-byte aligned device memory of at least the asked size that the
+ * caller owns; the calls allocate nothing, record no memory-set or copy nodes under graph capture, and give the same
+ * bits on every run.  Common errors: MARL_ERR_NULL, MARL_ERR_BAD_DTYPE, MARL_ERR_BAD_DIM (sizes, row strides, a
+ * workspace that is too small), MARL_ERR_BAD_ARG (scalars, a misaligned workspace, arrays that may not be the same).
+ */
+#define MARL_DTYPE_F16   2      /* element type of the policy operators only; networks refuse it */
+
+/*
+ * Gated linear recurrence over B sequences of T steps and C independent channels.  Per channel, with
+ *   rate = decay * log(1 + exp(lam)),  L = -rate * sigmoid(r),  a = exp(L),  beta = sqrt(1 - exp(2 L)):
+ *   h[t] = a h[t-1] + beta sigmoid(i) x        y[t] = h[t]
+ *   x, r, i    dev [B,T,C] elem, rows ld_x, ld_r, ld_i apart (row b T + t)
+ *   lam        dev [C] f32;  decay finite and positive
+ *   reset      dev [B,T] u8 or NULL   nonzero: a sequence starts at this step, a is 0 and beta 1
+ *   filled     dev [B,T] u8 or NULL   zero: padding; h passes unchanged, y is 0, and x, r, i, reset and the
+ *                                     upstream gradient of the row are not looked at, whatever they hold
+ *   h_first    dev [B,C] f32 or NULL (zero)   state before step 0
+ *   y          dev [B,T,C] elem, rows ld_y apart
+ *   h_last     dev [B,C] f32 or NULL  state after step T-1 (h_first if T is 0); may be h_first
+ *   workspace  afterwards holds the states that marl_linear_scan_grad starts from
+ * B, T and C may be 0 (C < 2^24, B T < 2^30).
+ */
+int marl_linear_scan_workspace_bytes(int32_t dtype, int32_t B, int32_t T, int32_t C, size_t *bytes);
+int marl_linear_scan(int32_t dtype, int32_t B, int32_t T, int32_t C, const void *x, int64_t ld_x, const void *r,
+                     int64_t ld_r, const void *i, int64_t ld_i, const float *lam, float decay, const uint8_t *reset,
+                     const uint8_t *filled, const float *h_first, void *y, int64_t ld_y, float *h_last,
+                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Backward pass of marl_linear_scan, which must have run with the same sizes, inputs and workspace before it (states
+ * are not read from y: they are computed again from the kept fp32 states, so that a 16-bit y costs no accuracy).
+ *   grad_y       dev [B,T,C] elem, rows ld_gy apart     dL/dy
+ *   grad_h_last  dev [B,C] f32 or NULL (zero)           dL/dh_last
+ *   grad_x, grad_r, grad_i   dev [B,T,C] elem, rows ld_gx, ld_gr, ld_gi apart, overwritten (0 in padding); none of
+ *                            them may be an input
+ *   grad_lam     dev [C] f32, overwritten: summed over all B and T in a fixed order
+ *   grad_h_first dev [B,C] f32 or NULL, overwritten; may be grad_h_last
+ */
+int marl_linear_scan_grad(int32_t dtype, int32_t B, int32_t T, int32_t C, const void *x, int64_t ld_x, const void *r,
+                          int64_t ld_r, const void *i, int64_t ld_i, const float *lam, float decay,
+                          const uint8_t *reset, const uint8_t *filled, const void *grad_y, int64_t ld_gy,
+                          const float *grad_h_last, void *workspace, size_t workspace_bytes, void *grad_x,
+                          int64_t ld_gx, void *grad_r, int64_t ld_gr, void *grad_i, int64_t ld_gi, float *grad_lam,
+                          float *grad_h_first, void *hip_stream);
+
+/*
+ * The same recurrence for one step of n sequences whose states are rows of a table (serving; the worker's step).
+ *   x, r, i   dev [n,C] elem, rows ld_x, ld_r, ld_i apart
+ *   slot      dev [n] i32 or NULL (0, 1, 2, ...)   row of each sequence; clamped into [0, slots); duplicates make
+ *                                                  the duplicated rows unspecified
+ *   reset     dev [n] u8 or NULL
+ *   h_in      dev [slots,C] f32     h_out dev [slots,C] f32, only the listed rows are written; may be h_in
+ *   y         dev [n,C] elem, rows ld_y apart
+ * n may be 0; slots >= 1, and without `slot` n <= slots.
+ */
+int marl_linear_step(int32_t dtype, int32_t n, int32_t C, const void *x, int64_t ld_x, const void *r, int64_t ld_r,
+                     const void *i, int64_t ld_i, const float *lam, float decay, const int32_t *slot, int32_t slots,
+                     const uint8_t *reset, const float *h_in, float *h_out, void *y, int64_t ld_y, void *hip_stream);
+
+/*
+ * Log probability of a given token (or action) in each of R rows of V logits, the entropy of the row and its K most
+ * likely tokens.  Over the available entries whose logit is above -infinity, z = scale * logit:
+ *   log_sum = log(sum exp z)   logp = z[token] - log_sum   entropy = -sum p log p, p = exp(z - log_sum)
+ *   logits   dev [R,V] elem, rows ld apart
+ *   token    dev [R] i32 or NULL        outside [0, V): logp is 0 and has no gradient.  Not available: logp is
+ *                                       -infinity and has no gradient
+ *   avail    dev u8 or NULL (all)       [R,V], rows ld_avail apart; ld_avail = 0: one [V] mask for all rows.
+ *                                       What stands in a masked place is not looked at, NaN included
+ *   scale    finite and positive
+ *   logp     dev [R] f32 or NULL        entropy, log_sum   dev [R] f32 or NULL
+ *   top_id   dev [R,K] i32, top_logp dev [R,K] f32   in descending order of the logit, ties to the lowest index; -1 and
+ *                                       -infinity where fewer are available.  Both NULL with K = 0; K <= 64
+ * A row with nothing available has logp 0, entropy 0, log_sum -infinity, and no gradient.  An available NaN or
+ * +infinity makes logp, entropy and log_sum of its row NaN, and its top entries unspecified indexes of the row.
+ * R may be 0; 1 <= V < 2^30, R < 2^31.
+ */
+int marl_log_prob_workspace_bytes(int32_t R, int32_t V, int32_t K, size_t *bytes);
+int marl_log_prob(int32_t dtype, int32_t R, int32_t V, const void *logits, int64_t ld, const int32_t *token,
+                  const uint8_t *avail, int64_t ld_avail, float scale, float *logp, float *entropy, float *log_sum,
+                  int32_t K, int32_t *top_id, float *top_logp, void *workspace, size_t workspace_bytes,
+                  void *hip_stream);
+
+/*
+ * Gradient of the logits, from the log_sum and entropy that marl_log_prob gave:
+ *   grad_logits[j] = scale * ( grad_logp (1[j = token] - p[j]) - grad_entropy p[j] (log p[j] + entropy) )
+ * and 0 in every place that is not available.
+ *   grad_logp dev [R] f32 or NULL (zero; token is then not needed), grad_entropy dev [R] f32 or NULL (zero; entropy is
+ *   then not needed), grad_logits dev [R,V] elem, rows ld_grad apart; may be logits (same ld)
+ */
+int marl_log_prob_grad(int32_t dtype, int32_t R, int32_t V, const void *logits, int64_t ld, const int32_t *token,
+                       const uint8_t *avail, int64_t ld_avail, float scale, const float *log_sum,
+                       const float *entropy, const float *grad_logp, const float *grad_entropy, void *grad_logits,
+                       int64_t ld_grad, void *hip_stream);
+
+/*
+ * Newton-Schulz iteration towards the orthogonal factor of L matrices [rows, cols]: with X the matrix or its
+ * transpose, whichever has no more rows than columns, X <- X / max(|X|_F, eps), then `steps` times
+ *   G = X X^T      X <- c0 X + (c1 G + c2 G G) X
+ * fp32 matrices keep 22 bits of every factor of the products; 16-bit ones keep 11 bits in the products and 22 in
+ * the term c0 X.
+ *   matrix  dev [L, rows, cols] elem     out dev [L, rows, cols] elem, may be matrix
+ *   coefficients host [3] f32 (finite);  steps 0 .. 64;  eps finite and positive
+ * L may be 0; rows, cols 1 .. 32768.
+ */
+int marl_muon_workspace_bytes(int32_t dtype, int32_t L, int32_t rows, int32_t cols, size_t *bytes);
+int marl_orthogonalize(int32_t dtype, int32_t L, int32_t rows, int32_t cols, const void *matrix, void *out,
+                       void *workspace, size_t workspace_bytes, int32_t steps, const float *coefficients, float eps,
+                       void *hip_stream);
+
+/*
+ * One update of L weight matrices by their orthogonalised momentum, NS as above:
+ *   momentum_out = beta momentum + grad        u = nesterov ? grad + beta momentum_out : momentum_out
+ *   weights_out  = (1 - lr weight_decay) weights - lr scale NS(u)
+ *   weights, grad   dev [L, rows, cols] elem    momentum dev [L, rows, cols] f32
+ *   weights_out, momentum_out may be weights, momentum (the update in place)
+ *   lr, beta, weight_decay, scale finite
+ */
+int marl_muon_step(int32_t dtype, int32_t L, int32_t rows, int32_t cols, const void *weights, const void *grad,
+                   const float *momentum, void *weights_out, float *momentum_out, void *workspace,
+                   size_t workspace_bytes, float lr, float beta, int32_t nesterov, float weight_decay, float scale,
+                   int32_t steps, const float *coefficients, float eps, void *hip_stream);
 
 /* Free the handle, its weights and scratch.  Synchronises the device.  NULL is allowed. */
 int marl_destroy(marl_qnet *q);

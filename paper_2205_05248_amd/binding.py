@@ -18,12 +18,17 @@ LIB_PATH = os.path.join(_HERE, "libmarl_qnet.so")
 MARL_DTYPE_F32 = 0
 MARL_DTYPE_BF16 = 1
 DTYPES = {"fp32": MARL_DTYPE_F32, "bf16": MARL_DTYPE_BF16}
+MARL_DTYPE_F16 = 2
+ELEMENTS = {"fp32": MARL_DTYPE_F32, "bf16": MARL_DTYPE_BF16, "fp16": MARL_DTYPE_F16}     # policy operators
 
 EXPORTS = ["marl_param_count", "marl_qnet_create", "marl_qnet_get_desc", "marl_act_step", "marl_act_step_indexed", "marl_unroll_td_indexed",
            "marl_unroll_td_double", "marl_qnet_grad_workspace_bytes", "marl_qnet_grad", "marl_qnet_grad_kept", "marl_unroll_td_keep", "marl_qnet_sgd_step", "marl_qnet_rmsprop_step", "marl_qnet_check_refresh_map",
            "marl_unroll_td", "marl_unroll_td_static", "marl_probe_stream", "marl_probe_mfma", "marl_qnet_reserve_unroll", "marl_destroy", "marl_strerror",
            "marl_last_device_error", "marl_qnet_set_timing", "marl_qnet_timing_read",
-           "marl_qnet_set_kernels", "marl_qnet_kernels_in_use", "marl_qnet_set_weights"]
+           "marl_qnet_set_kernels", "marl_qnet_kernels_in_use", "marl_qnet_set_weights",
+           "marl_linear_scan_workspace_bytes", "marl_linear_scan", "marl_linear_scan_grad", "marl_linear_step",
+           "marl_log_prob_workspace_bytes", "marl_log_prob", "marl_log_prob_grad",
+           "marl_muon_workspace_bytes", "marl_orthogonalize", "marl_muon_step"]
 # include/marl_mixer.h
 MIXER_EXPORTS = ["marl_mixer_param_count", "marl_mixer_create", "marl_mixer_destroy", "marl_mixer_td",
                  "marl_mixer_set_weights", "marl_mixer_grad_workspace_bytes", "marl_mixer_grad", "marl_mixer_sgd_step", "marl_mixer_rmsprop_step"]
@@ -134,6 +139,21 @@ def load():
         lib.marl_mixer_sgd_step.argtypes = [vp, vp, vp, f32, vp]
         lib.marl_mixer_td.restype = ctypes.c_int
         lib.marl_mixer_td.argtypes = [vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, vp]
+        i64, size, out = ctypes.c_int64, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+        for name, args in {
+                "marl_linear_scan_workspace_bytes": [i32, i32, i32, i32, out],
+                "marl_linear_scan": [i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, f32, vp, vp, vp, vp, i64, vp, vp, size, vp],
+                "marl_linear_scan_grad": [i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, f32, vp, vp, vp, i64, vp, vp, size,
+                                          vp, i64, vp, i64, vp, i64, vp, vp, vp],
+                "marl_linear_step": [i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, f32, vp, i32, vp, vp, vp, vp, i64, vp],
+                "marl_log_prob_workspace_bytes": [i32, i32, i32, out],
+                "marl_log_prob": [i32, i32, i32, vp, i64, vp, vp, i64, f32, vp, vp, vp, i32, vp, vp, vp, size, vp],
+                "marl_log_prob_grad": [i32, i32, i32, vp, i64, vp, vp, i64, f32, vp, vp, vp, vp, vp, i64, vp],
+                "marl_muon_workspace_bytes": [i32, i32, i32, i32, out],
+                "marl_orthogonalize": [i32, i32, i32, i32, vp, vp, vp, size, i32, vp, f32, vp],
+                "marl_muon_step": [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, size, f32, f32, i32, f32, f32, i32, vp, f32, vp]}.items():
+            getattr(lib, name).restype = ctypes.c_int
+            getattr(lib, name).argtypes = args
         _lib = lib
     return _lib
 
@@ -541,3 +561,201 @@ class Mixer:
             self.close()
         except Exception:
             pass
+
+
+# ------------------------------------------------------------------ policy operators (last part of include/marl_qnet.h)
+# Element arrays may be column blocks of a wider tensor: rows at one distance, adjacent elements within a row.
+_elements = None
+
+
+def _element(t, name):
+    """The dtype code of an element tensor."""
+    global _elements
+    if _elements is None:
+        if _torch is None:
+            _bind_torch()
+        _elements = {_torch.float32: MARL_DTYPE_F32, _torch.bfloat16: MARL_DTYPE_BF16, _torch.float16: MARL_DTYPE_F16}
+    code = _elements.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: expected a fp32, bf16 or fp16 tensor, got {t.dtype}")
+    return code
+
+
+def _rows(t, dtype, shape, name):
+    """Address and row distance of a device tensor [..., C] whose leading axes fold into one row index."""
+    ok = t.dtype is dtype and t.shape == shape and t.is_cuda and t.device.index == _torch.cuda.current_device()
+    if ok:
+        C, strides = shape[-1], t.stride()
+        if t.is_contiguous():
+            return t.data_ptr(), C
+        ok = C <= 1 or strides[-1] == 1
+        at = len(shape) - 2                                       # the innermost leading axis with more than one index
+        while at > 0 and shape[at] == 1:
+            at -= 1
+        ld = strides[at] if shape[at] > 1 else C
+        step = ld
+        for axis in range(at, -1, -1):
+            ok = ok and (shape[axis] == 1 or strides[axis] == step)
+            step *= shape[axis]
+        ok = ok and ld >= C
+    if not ok:
+        raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the current device with adjacent elements and "
+                         f"evenly spaced rows, got {t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
+    return t.data_ptr(), ld
+
+
+def _flat(t, dtype, shape, name, optional=False):
+    """Address of a contiguous tensor on the current device (`dtype`: a key of _dtypes)."""
+    address = _dev(t, dtype, shape, name, optional)
+    if t is not None and t.device.index != _torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, but the current device is {_torch.cuda.current_device()}")
+    return address
+
+
+def _workspace(t):
+    return (None, 0) if t is None or t.numel() == 0 else (_flat(t, "u8", (t.numel(),), "workspace"), t.numel())
+
+
+def _dtype_code(dtype):
+    if dtype not in ELEMENTS:
+        raise ValueError(f"dtype: expected one of {sorted(ELEMENTS)}, got {dtype!r}")
+    return ELEMENTS[dtype]
+
+
+def _bytes_of(entry, *args):
+    n = ctypes.c_size_t(0)
+    check(entry(*args, ctypes.byref(n)))
+    return int(n.value)
+
+
+def marl_linear_scan_workspace_bytes(dtype, B, T, C):
+    """dtype: "fp32", "bf16" or "fp16", the element type of the sequences."""
+    return _bytes_of(load().marl_linear_scan_workspace_bytes, _dtype_code(dtype), int(B), int(T), int(C))
+
+
+def marl_linear_scan(x, r, i, lam, decay, reset, filled, h_first, y, h_last, workspace):
+    """Gated linear recurrence over x, r, i [B,T,C]; reset, filled [B,T] u8, h_first [B,C], h_last [B,C] may be None."""
+    code = _element(x, "x")
+    B, T, C = x.shape
+    (px, lx), (pr, lr), (pi, li) = (_rows(t, x.dtype, (B, T, C), n) for t, n in ((x, "x"), (r, "r"), (i, "i")))
+    py, ly = _rows(y, x.dtype, (B, T, C), "y")
+    check(load().marl_linear_scan(
+        code, B, T, C, px, lx, pr, lr, pi, li, _flat(lam, "f32", (C,), "lam"), float(decay),
+        _flat(reset, "u8", (B, T), "reset", True), _flat(filled, "u8", (B, T), "filled", True),
+        _flat(h_first, "f32", (B, C), "h_first", True), py, ly, _flat(h_last, "f32", (B, C), "h_last", True), *_workspace(workspace),
+        _stream()))
+
+
+def marl_linear_scan_grad(x, r, i, lam, decay, reset, filled, grad_y, grad_h_last, workspace, grad_x, grad_r, grad_i, grad_lam,
+                          grad_h_first=None):
+    """workspace: as marl_linear_scan left it for the same inputs; grad_h_last, grad_h_first may be None."""
+    code = _element(x, "x")
+    B, T, C = x.shape
+    flat = []
+    for t, n in ((x, "x"), (r, "r"), (i, "i"), (grad_y, "grad_y"), (grad_x, "grad_x"), (grad_r, "grad_r"), (grad_i, "grad_i")):
+        flat.append(_rows(t, x.dtype, (B, T, C), n))
+    px, pr, pi, pg, gx, gr, gi = flat
+    check(load().marl_linear_scan_grad(
+        code, B, T, C, *px, *pr, *pi, _flat(lam, "f32", (C,), "lam"), float(decay), _flat(reset, "u8", (B, T), "reset", True),
+        _flat(filled, "u8", (B, T), "filled", True), *pg, _flat(grad_h_last, "f32", (B, C), "grad_h_last", True),
+        *_workspace(workspace), *gx, *gr, *gi, _flat(grad_lam, "f32", (C,), "grad_lam"),
+        _flat(grad_h_first, "f32", (B, C), "grad_h_first", True), _stream()))
+
+
+def marl_linear_step(x, r, i, lam, decay, slot, reset, h_in, h_out, y):
+    """One step of n sequences: x, r, i, y [n,C]; slot [n] i32 or None picks rows of h_in, h_out [slots,C] (may be the same)."""
+    code = _element(x, "x")
+    n, C = x.shape
+    slots = h_in.shape[0]
+    (px, lx), (pr, lr), (pi, li), (py, ly) = (_rows(t, x.dtype, (n, C), m) for t, m in ((x, "x"), (r, "r"), (i, "i"), (y, "y")))
+    check(load().marl_linear_step(
+        code, n, C, px, lx, pr, lr, pi, li, _flat(lam, "f32", (C,), "lam"), float(decay), _flat(slot, "i32", (n,), "slot", True), slots,
+        _flat(reset, "u8", (n,), "reset", True), _flat(h_in, "f32", (slots, C), "h_in"), _flat(h_out, "f32", (slots, C), "h_out"), py, ly,
+        _stream()))
+
+
+def marl_log_prob_workspace_bytes(R, V, K):
+    return _bytes_of(load().marl_log_prob_workspace_bytes, int(R), int(V), int(K))
+
+
+def _avail_of(avail, R, V):
+    """Address and row distance: [R,V], or [V] for all rows."""
+    if avail is None:
+        return None, 0
+    if avail.dim() == 1:
+        return _flat(avail, "u8", (V,), "avail"), 0
+    return _rows(avail, _dtypes["u8"], (R, V), "avail")
+
+
+def marl_log_prob(logits, token, avail, scale, logp, entropy, log_sum, top_id=None, top_logp=None, workspace=None):
+    """logits [R,V]; token [R] i32, avail [R,V] or [V] u8, and every output may be None; top_id [R,K] i32, top_logp [R,K]."""
+    code = _element(logits, "logits")
+    R, V = logits.shape
+    K = 0 if top_id is None else top_id.shape[1]
+    check(load().marl_log_prob(
+        code, R, V, *_rows(logits, logits.dtype, (R, V), "logits"), _flat(token, "i32", (R,), "token", True), *_avail_of(avail, R, V),
+        float(scale), _flat(logp, "f32", (R,), "logp", True), _flat(entropy, "f32", (R,), "entropy", True),
+        _flat(log_sum, "f32", (R,), "log_sum", True), K, _flat(top_id, "i32", (R, K), "top_id", True),
+        _flat(top_logp, "f32", (R, K), "top_logp", True), *_workspace(workspace), _stream()))
+
+
+def marl_log_prob_grad(logits, token, avail, scale, log_sum, entropy, grad_logp, grad_entropy, grad_logits):
+    """Gradient of the logits; grad_logp [R] and grad_entropy [R] may be None.  grad_logits may be logits."""
+    code = _element(logits, "logits")
+    R, V = logits.shape
+    check(load().marl_log_prob_grad(
+        code, R, V, *_rows(logits, logits.dtype, (R, V), "logits"), _flat(token, "i32", (R,), "token", True), *_avail_of(avail, R, V),
+        float(scale), _flat(log_sum, "f32", (R,), "log_sum"), _flat(entropy, "f32", (R,), "entropy", True),
+        _flat(grad_logp, "f32", (R,), "grad_logp", True), _flat(grad_entropy, "f32", (R,), "grad_entropy", True),
+        *_rows(grad_logits, logits.dtype, (R, V), "grad_logits"), _stream()))
+
+
+NS_STEPS, NS_COEFFICIENTS, NS_EPS = 5, (3.4445, -4.7750, 2.0315), 1e-7
+
+
+def marl_muon_workspace_bytes(dtype, L, rows, cols):
+    """dtype: "fp32", "bf16" or "fp16", the element type of the matrices."""
+    return _bytes_of(load().marl_muon_workspace_bytes, _dtype_code(dtype), int(L), int(rows), int(cols))
+
+
+def _matrices(t, shape, dtype, name):
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda or t.device.index != _torch.cuda.current_device():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, "
+                         f"got {t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
+    return t.data_ptr()
+
+
+def _batch_of(t):
+    if t.dim() not in (2, 3):
+        raise ValueError(f"expected one matrix or a batch of them, got shape {tuple(t.shape)}")
+    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
+
+
+def _coefficients(values):
+    if len(values) != 3:
+        raise ValueError(f"expected three coefficients, got {len(values)}")
+    return (ctypes.c_float * 3)(*values)
+
+
+def marl_orthogonalize(matrix, out, workspace, steps=NS_STEPS, coefficients=NS_COEFFICIENTS, eps=NS_EPS):
+    """Newton-Schulz iteration on matrix [rows,cols] or [L,rows,cols]; out may be matrix."""
+    code = _element(matrix, "matrix")
+    L, rows, cols = _batch_of(matrix)
+    check(load().marl_orthogonalize(
+        code, L, rows, cols, _matrices(matrix, matrix.shape, matrix.dtype, "matrix"), _matrices(out, matrix.shape, matrix.dtype, "out"),
+        *_workspace(workspace), int(steps), _coefficients(coefficients), float(eps), _stream()))
+
+
+def marl_muon_step(weights, grad, momentum, weights_out, momentum_out, workspace, lr, beta=0.95, nesterov=True, weight_decay=0.0,
+                   scale=1.0, steps=NS_STEPS, coefficients=NS_COEFFICIENTS, eps=NS_EPS):
+    """Momentum, orthogonalisation and weight update of [rows,cols] or [L,rows,cols] matrices; momentum in fp32.  weights_out and
+    momentum_out may be weights and momentum."""
+    code = _element(weights, "weights")
+    L, rows, cols = _batch_of(weights)
+    address = lambda t, name, dtype: _matrices(t, weights.shape, dtype, name)
+    f32 = _dtypes["f32"]
+    check(load().marl_muon_step(
+        code, L, rows, cols, address(weights, "weights", weights.dtype), address(grad, "grad", weights.dtype),
+        address(momentum, "momentum", f32), address(weights_out, "weights_out", weights.dtype), address(momentum_out, "momentum_out", f32),
+        *_workspace(workspace), float(lr), float(beta), int(bool(nesterov)), float(weight_decay), float(scale), int(steps),
+        _coefficients(coefficients), float(eps), _stream()))

@@ -838,7 +838,7 @@ const char *marl_strerror(int status)
     case MARL_ERR_BAD_DIM: return "a size is not positive or outside the supported range";
     case MARL_ERR_BAD_DTYPE: return "unknown weight dtype";
     case MARL_ERR_MISMATCH: return "weight count or network descriptions do not match";
-    case MARL_ERR_BAD_ARG: return "epsilon or gamma outside [0,1]";
+    case MARL_ERR_BAD_ARG: return "a scalar argument outside its range, a misaligned pointer, or arrays that may not be the same";
     case MARL_ERR_DEVICE: return "HIP runtime error";
     case MARL_ERR_NOMEM: return "out of memory";
     default: return "unknown status";

@@ -1,0 +1,254 @@
+"""The gated linear recurrence on the GPU against the 64-bit oracle.
+
+Tolerance.  A step's a and beta come out of a handful of fp32 operations, two to four half steps of 2^-24 each: below
+2^-21 of the value.  The inputs' retention (0.9 .. 0.999 at an eighth of the gate) lets about 250 steps add up, so
+a state is within 250 * 2^-21 = 1.2e-4 of the largest state, and so is every gradient of its own largest; the sum for
+lam within that of the sum of its terms' sizes.  16-bit outputs add half a step of their own.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import policy_oracle as orc
+from policy_util import DT, gen, host, near, randn
+from paper_2205_05248_amd import binding
+
+pytestmark = pytest.mark.gpu
+REL = 250 * 2.0 ** -21
+DECAY = 8.0
+
+
+def make(B, T, C, dtype, seed, reset=False, filled=False, first=True, layout="plain"):
+    """CPU tensors; layout: "plain", "fused" (column blocks of one tensor), "shifted" (blocks at an odd element)."""
+    g = gen(seed)
+    dt = DT[dtype]
+    s = dict(lam=torch.log(torch.expm1(-torch.log(0.9 + 0.099 * torch.rand(C, generator=g)))))
+    s["xri"] = randn(g, B, T, 3, C, dtype=dt)
+    s["reset"] = (torch.rand(B, T, generator=g) < 0.1).to(torch.uint8) if reset else None
+    if filled:
+        f = torch.rand(B, T, generator=g) < 0.8
+        f[-1] = B == 1                                          # a row without a step, if there are several
+        f[0, T // 2:] &= B > 2                                  # an early end
+        s["filled"] = f.to(torch.uint8)
+        s["xri"][~f] = float("nan")                             # what stands in padding does not matter
+    else:
+        s["filled"] = None
+    s["h_first"] = randn(g, B, C) if first else None
+    s["grad_y"] = randn(g, B, T, C, dtype=dt)
+    if filled:
+        s["grad_y"][~f] = float("inf")
+    s["grad_h_last"] = randn(g, B, C) if first else None
+    s["layout"] = layout
+    return s
+
+
+def on_gpu(s):
+    B, T, _, C = s["xri"].shape
+    xri = s["xri"].cuda()
+    if s["layout"] == "plain":
+        x, r, i = (xri[:, :, k].contiguous() for k in range(3))
+    else:
+        shift = 1 if s["layout"] == "shifted" else 0
+        wide = torch.zeros(B, T, 3 * C + 2 * shift, dtype=xri.dtype, device="cuda")
+        x, r, i = (wide[..., shift + k * C:shift + (k + 1) * C] for k in range(3))
+        for k, t in enumerate((x, r, i)):
+            t.copy_(xri[:, :, k])
+    d = {k: (s[k].cuda() if torch.is_tensor(s[k]) else None) for k in ("lam", "reset", "filled", "h_first", "grad_y", "grad_h_last")}
+    return dict(x=x, r=r, i=i, **d)
+
+
+def outputs(d):
+    B, T, C = d["x"].shape
+    dt, nan = d["x"].dtype, float("nan")
+    o = {k: torch.full((B, T, C), nan, dtype=dt, device="cuda") for k in ("y", "grad_x", "grad_r", "grad_i")}
+    o.update(h_last=torch.full((B, C), nan, device="cuda"), grad_lam=torch.full((C,), nan, device="cuda"),
+             grad_h_first=torch.full((B, C), nan, device="cuda"))
+    name = {v: k for k, v in DT.items()}[dt]
+    o["ws"] = torch.empty(binding.marl_linear_scan_workspace_bytes(name, B, T, C), dtype=torch.uint8, device="cuda").fill_(0xff)
+    return o
+
+
+def run(d, o):
+    binding.marl_linear_scan(d["x"], d["r"], d["i"], d["lam"], DECAY, d["reset"], d["filled"], d["h_first"], o["y"], o["h_last"], o["ws"])
+    binding.marl_linear_scan_grad(d["x"], d["r"], d["i"], d["lam"], DECAY, d["reset"], d["filled"], d["grad_y"], d["grad_h_last"], o["ws"],
+                                  o["grad_x"], o["grad_r"], o["grad_i"], o["grad_lam"], o["grad_h_first"])
+
+
+def check(s, o):
+    x, r, i = (host(s["xri"][:, :, k]) for k in range(3))
+    fill = host(s["filled"])
+    clean = (lambda v: v) if fill is None else (lambda v: np.where(fill[..., None] != 0, v, 0.0))
+    x, r, i, gy = clean(x), clean(r), clean(i), clean(host(s["grad_y"]))
+    args = (x, r, i, host(s["lam"]), DECAY, host(s["reset"]), fill, host(s["h_first"]))
+    y, last, _ = orc.linear_scan(*args)
+    gx, gr, gi, glam, gh = orc.linear_scan_grad(*args, gy, host(s["grad_h_last"]))
+    dt, f32 = s["xri"].dtype, torch.float32
+    near(o["y"], y, dt, REL, "y")
+    near(o["h_last"], last, f32, REL, "h_last")
+    near(o["grad_x"], gx, dt, REL, "grad_x")
+    near(o["grad_r"], gr, dt, REL, "grad_r")
+    near(o["grad_i"], gi, dt, REL, "grad_i")
+    near(o["grad_h_first"], gh, f32, REL, "grad_h_first")
+    rate, by_lam = orc.rates(host(s["lam"]), DECAY)
+    s_r = 1 / (1 + np.exp(-r))
+    sizes = (np.abs(gr) / (rate * (1 - s_r))).sum((0, 1)) * by_lam
+    near(o["grad_lam"], glam, f32, REL, "grad_lam", floor=sizes)
+
+
+SIZES = [(1, 1, 1), (3, 2, 5), (2, 17, 33), (1, 127, 64), (1, 128, 8), (2, 129, 130), (4, 33, 512), (1, 1000, 40), (40, 12, 64), (1, 2055, 100)]
+
+
+@pytest.mark.parametrize("B,T,C", SIZES)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_forward_and_backward(B, T, C, dtype):
+    k = SIZES.index((B, T, C))
+    s = make(B, T, C, dtype, 10 + k, reset=k % 2 == 1, filled=k % 3 == 2, first=k % 4 != 3, layout=("plain", "fused", "shifted")[k % 3])
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    check(s, o)
+
+
+@pytest.mark.parametrize("reset,filled", [(False, False), (True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("layout", ["plain", "shifted"])
+def test_masks_over_several_blocks(reset, filled, layout):
+    s = make(3, 700, 72, "bf16", 77, reset, filled, True, layout)
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    check(s, o)
+
+
+def test_no_step_at_all():
+    s = make(2, 0, 6, "fp32", 5)
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    assert torch.equal(o["h_last"], d["h_first"]) and torch.equal(o["grad_h_first"], d["grad_h_last"]) and not o["grad_lam"].any()
+
+
+def test_gates_at_their_ends():
+    """Gates that are shut, open or far out: no infinity from 1 / beta, no NaN."""
+    s = make(1, 40, 16, "fp32", 6)
+    s["xri"][0, ::3, 1] = -200.0                                   # a = 1, beta = 0
+    s["xri"][0, 1::3, 1] = 200.0
+    s["xri"][0, 5, 2], s["xri"][0, 9, 2] = -200.0, 200.0
+    s["lam"][3], s["lam"][4] = 60.0, -60.0
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    x, r, i = (host(s["xri"][:, :, k]) for k in range(3))
+    y, last, _ = orc.linear_scan(x, r, i, host(s["lam"]), DECAY, None, None, host(s["h_first"]))
+    near(o["y"], y, torch.float32, REL, "y")
+    near(o["h_last"], last, torch.float32, REL, "h_last")
+    for k in ("grad_x", "grad_r", "grad_i", "grad_lam", "grad_h_first"):
+        assert torch.isfinite(o[k]).all(), k
+
+
+def test_outputs_as_column_blocks_and_states_in_place():
+    s = make(2, 150, 24, "bf16", 8, reset=True)
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    wide = torch.full((2, 150, 5 * 24), 7.0, dtype=torch.bfloat16, device="cuda")
+    p = dict(o, y=wide[..., :24], grad_x=wide[..., 24:48], grad_r=wide[..., 48:72], grad_i=wide[..., 72:96], h_last=d["h_first"].clone(),
+             grad_h_first=d["grad_h_last"].clone(), grad_lam=torch.empty_like(o["grad_lam"]))
+    e = dict(d, h_first=p["h_last"], grad_h_last=p["grad_h_first"])
+    run(e, p)
+    torch.cuda.synchronize()
+    for k in ("y", "grad_x", "grad_r", "grad_i", "h_last", "grad_lam", "grad_h_first"):
+        assert torch.equal(o[k], p[k]), k
+    assert (wide[..., 96:] == 7).all()
+
+
+def test_same_bits_on_every_run_and_on_another_stream():
+    s = make(1, 5000, 96, "fp32", 9, reset=True)
+    d = on_gpu(s)
+    first = outputs(d)
+    run(d, first)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        o = outputs(d)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            run(d, o)
+        side.synchronize()
+        for k in first:
+            if k != "ws":
+                assert torch.equal(first[k], o[k]), k
+
+
+def test_replayed_from_a_graph():
+    s = make(2, 600, 128, "bf16", 11, reset=True, filled=True)
+    d = on_gpu(s)
+    d = {k: (None if v is None else v.clone()) for k, v in d.items()}
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(d, o)
+    for k in range(3):
+        d["x"].mul_(0.5)
+        want = outputs(d)
+        run(d, want)
+        for v in o:
+            if v != "ws":
+                o[v].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for v in o:
+            if v != "ws":
+                assert torch.equal(o[v], want[v]), (k, v)
+
+
+@pytest.mark.parametrize("n,C,slots,dtype", [(1, 1, 1, "fp32"), (24, 64, 24, "fp32"), (7, 33, 50, "bf16"), (130, 257, 200, "fp16"), (65, 2048, 65, "bf16")])
+@pytest.mark.parametrize("listed", [True, False])
+def test_single_steps(n, C, slots, dtype, listed):
+    g = gen(n + C)
+    s = make(1, n, C, dtype, n, layout="shifted" if C % 2 else "fused")
+    d = {k: (v[0] if k in "xri" else v) for k, v in on_gpu(s).items()}
+    slot = torch.randperm(slots, generator=g)[:n].to(torch.int32) if listed else None
+    reset = (torch.rand(n, generator=g) < 0.3).to(torch.uint8) if n > 1 else None
+    table = randn(g, slots, C)
+    dev = table.cuda()
+    y = torch.full((n, C), float("nan"), dtype=DT[dtype], device="cuda")
+    binding.marl_linear_step(d["x"], d["r"], d["i"], d["lam"], DECAY, None if slot is None else slot.cuda(), None if reset is None else reset.cuda(),
+                             dev, dev, y)
+    torch.cuda.synchronize()
+    x, r, i = (host(s["xri"][0, :, k]) for k in range(3))
+    want, after = orc.linear_step(x, r, i, host(s["lam"]), DECAY, host(slot), host(reset), host(table))
+    rel = 2.0 ** -20                                               # one step: a handful of operations
+    near(y, want, DT[dtype], rel, "y")
+    near(dev, after, torch.float32, rel, "h_out")
+    rest = torch.ones(slots, dtype=torch.bool)
+    rest[slot.long() if listed else torch.arange(n)] = False
+    assert torch.equal(dev.cpu()[rest], table[rest])
+
+
+def test_steps_follow_the_scan():
+    s = make(3, 9, 40, "fp32", 12)
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    h = d["h_first"].clone()
+    for t in range(9):
+        y = torch.empty(3, 40, device="cuda")
+        binding.marl_linear_step(d["x"][:, t], d["r"][:, t], d["i"][:, t], d["lam"], DECAY, None, None, h, h, y)
+        assert (y - o["y"][:, t]).abs().max() < REL
+    assert (h - o["h_last"]).abs().max() < REL
+
+
+def test_table_rows_out_of_range_are_clamped():
+    s = make(1, 2, 8, "fp32", 13)
+    d = {k: (v[0] if k in "xri" else v) for k, v in on_gpu(s).items()}
+    table, y = torch.ones(4, 8, device="cuda"), torch.empty(2, 8, device="cuda")
+    out = table.clone()
+    binding.marl_linear_step(d["x"], d["r"], d["i"], d["lam"], DECAY, torch.tensor([-5, 99], dtype=torch.int32, device="cuda"), None, table, out, y)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], y[0]) and torch.equal(out[3], y[1]) and (out[1:3] == 1).all()

@@ -1,0 +1,148 @@
+"""Newton-Schulz iteration and the update by an orthogonalised momentum on the GPU against the 64-bit oracle.
+
+Tolerance.  One step maps a singular value t to c0 t + c1 t^3 + c2 t^5, |coefficients| <= 4.8.  Products keep p bits of their
+factors (22 for fp32, 11 for 16-bit types, whose additive term c0 X keeps 22): an entry of G or of (P X) is a sum
+of rounded terms whose errors have random signs, 2^-p of the root of the sum of the squares of the terms, which is at most
+2^-p of the largest row's norm product, 1.2.  Singular directions differ by what later steps make of it: the polynomial's
+slope is at most 3.4445 and it is applied to errors of relative, not absolute size, so five steps of up to
+sum |c| = 10.3 times that error each, carried on by a slope that is at most 3.4445 only while the value itself grows by
+as much: 5 * 10.3 * 2^-p = 52 * 2^-p of the largest entry, twice for the two products.  fp32 adds the fp32 sums' own
+rounding, sqrt(K) 2^-24 over K <= 1024 terms, of the same weight: 2^-19.  So 104 * (2^-22 + 2^-19) = 2.3e-4 of the
+largest entry for fp32 and 104 * 2^-11 = 5.1e-2 for 16-bit types as the bound for any spectrum; random matrices stay
+far below it, which the mean below checks: errors of random signs leave a root mean square of a twentieth of the bound.
+That mean is not asked of matrices of low rank, where the rounding of X itself, 2^-24 of its entries, stands in directions
+that hold nothing else and five steps multiply by up to 3.4445^5 = 485 (the inputs' own rounding does the same).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import policy_oracle as orc
+from policy_util import DT, gen, host, near, randn
+from paper_2205_05248_amd import binding
+
+pytestmark = pytest.mark.gpu
+BOUND = {"fp32": 104 * (2.0 ** -22 + 2.0 ** -19), "bf16": 104 * 2.0 ** -11, "fp16": 104 * 2.0 ** -11}
+
+
+def gradient(g, L, rows, cols, dtype):
+    """A few strong directions over noise."""
+    q = min(rows, cols, 4)
+    return (torch.matmul(randn(g, L, rows, q), randn(g, L, q, cols)) + 0.5 * randn(g, L, rows, cols)).mul_(1e-2).to(DT[dtype])
+
+
+def workspace(dtype, L, rows, cols):
+    return torch.empty(binding.marl_muon_workspace_bytes(dtype, L, rows, cols), dtype=torch.uint8, device="cuda").fill_(0xff)
+
+
+def close(got, want, dtype, name):
+    near(got, want, DT[dtype], BOUND[dtype], name)
+    rms = np.sqrt(((host(got) - want) ** 2).mean()) / max(np.sqrt((want ** 2).mean()), 1e-300)
+    half = torch.finfo(DT[dtype]).eps / 2
+    assert rms <= BOUND[dtype] / 20 + half, (name, rms)
+
+
+SIZES = [(1, 1, 1), (2, 1, 50), (1, 7, 5), (3, 16, 16), (2, 64, 64), (2, 192, 64), (2, 64, 101), (1, 11, 64), (1, 128, 332), (2, 384, 128), (1, 129, 257),
+         (1, 200, 640), (1, 1000, 333), (5, 40, 128), (1, 512, 512)]
+
+
+@pytest.mark.parametrize("L,rows,cols", SIZES)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_orthogonalize(L, rows, cols, dtype):
+    m = gradient(gen(rows + cols), L, rows, cols, dtype)
+    dev, ws = m.cuda(), workspace(dtype, L, rows, cols)
+    out = torch.full_like(dev, float("nan"))
+    binding.marl_orthogonalize(dev, out, ws)
+    torch.cuda.synchronize()
+    close(out, orc.orthogonalize(host(m)), dtype, "out")
+    binding.marl_orthogonalize(dev, dev, ws)                       # in place, and the same bits again
+    torch.cuda.synchronize()
+    assert torch.equal(dev, out)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rank", [1, 3])
+def test_low_rank(dtype, rank):
+    g = gen(rank)
+    m = torch.matmul(randn(g, 96, rank), randn(g, rank, 160)).to(DT[dtype])
+    out = torch.empty_like(m, device="cuda")
+    binding.marl_orthogonalize(m.cuda(), out, workspace(dtype, 1, 96, 160))
+    torch.cuda.synchronize()
+    near(out, orc.orthogonalize(host(m)), DT[dtype], BOUND[dtype], "out")
+
+
+@pytest.mark.parametrize("steps,coefficients", [(0, (3.4445, -4.775, 2.0315)), (1, (1.5, -0.5, 0.0)), (2, (2.0, -1.5, 0.5)), (8, (1.875, -1.25, 0.375))])
+def test_steps_and_coefficients(steps, coefficients):
+    m = gradient(gen(steps), 2, 30, 70, "fp32")
+    out = torch.empty_like(m, device="cuda")
+    binding.marl_orthogonalize(m.cuda(), out, workspace("fp32", 2, 30, 70), steps, coefficients)
+    torch.cuda.synchronize()
+    near(out, orc.orthogonalize(host(m), steps, coefficients), torch.float32, BOUND["fp32"], "out")
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e25])
+@pytest.mark.parametrize("rows,cols", [(20, 30), (300, 200)])
+def test_the_norm_neither_overflows_nor_vanishes(size, rows, cols):
+    m = gradient(gen(4), 1, rows, cols, "fp32")
+    dev, out = (m * size).cuda(), torch.empty_like(m, device="cuda")
+    binding.marl_orthogonalize(dev, out, workspace("fp32", 1, rows, cols), eps=1e-37)
+    torch.cuda.synchronize()
+    near(out, orc.orthogonalize(host(m * size), eps=1e-37), torch.float32, BOUND["fp32"], "out")
+
+
+def test_zero_and_not_finite_matrices_stay_by_themselves():
+    m = gradient(gen(5), 4, 24, 40, "fp32")
+    clean, out, ws = torch.empty_like(m, device="cuda"), torch.empty_like(m, device="cuda"), workspace("fp32", 4, 24, 40)
+    binding.marl_orthogonalize(m.cuda(), clean, ws)
+    m[1] = 0.0
+    m[2, 3, 4] = float("inf")
+    binding.marl_orthogonalize(m.cuda(), out, ws)
+    torch.cuda.synchronize()
+    assert not out[1].any() and not torch.isfinite(out[2]).all()
+    assert torch.equal(out[0], clean[0]) and torch.equal(out[3], clean[3])
+
+
+@pytest.mark.parametrize("L,rows,cols", [(2, 192, 64), (1, 96, 400), (1, 300, 300)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_update(L, rows, cols, dtype, nesterov):
+    g = gen(rows)
+    w, grad, mom = randn(g, L, rows, cols, dtype=DT[dtype]), gradient(g, L, rows, cols, dtype), randn(g, L, rows, cols) * 0.1
+    kw = dict(lr=0.5, beta=0.9, nesterov=nesterov, weight_decay=0.1, scale=1.5)
+    ws = workspace(dtype, L, rows, cols)
+    dw, dm = w.cuda(), mom.cuda()
+    wo, mo = torch.empty_like(dw), torch.empty_like(dm)
+    binding.marl_muon_step(dw, grad.cuda(), dm, wo, mo, ws, **kw)
+    torch.cuda.synchronize()
+    want_w, want_m = orc.muon_step(host(w), host(grad), host(mom), **kw)
+    near(mo, want_m, torch.float32, 2.0 ** -23, "momentum")
+    step = np.abs(want_w - host(w) * 0.95).max()
+    near(wo, want_w, DT[dtype], BOUND[dtype], "weights", floor=step + np.abs(want_w).max() * 2.0 ** -16)
+    binding.marl_muon_step(dw, grad.cuda(), dm, dw, dm, ws, **kw)  # in place
+    torch.cuda.synchronize()
+    assert torch.equal(dw, wo) and torch.equal(dm, mo)
+
+
+@pytest.mark.parametrize("rows,cols", [(64, 64), (300, 520)])
+def test_replayed_from_a_graph_and_on_another_stream(rows, cols):
+    g = gen(6)
+    w, mom, grad = randn(g, rows, cols).cuda(), torch.zeros(rows, cols, device="cuda"), gradient(g, 1, rows, cols, "fp32")[0].cuda()
+    ws = workspace("fp32", 1, rows, cols)
+    go = lambda a, b, c: binding.marl_muon_step(a, grad, b, a, b, c, lr=0.02)
+    first = (w.clone(), mom.clone())
+    go(*first, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go(w, mom, ws)
+    want, side = (w.clone(), mom.clone()), torch.cuda.Stream()
+    ws2 = workspace("fp32", 1, rows, cols)
+    for k in range(4):
+        grad.mul_(-0.7)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            go(*want, ws2)
+        side.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(w, want[0]) and torch.equal(mom, want[1]), k
