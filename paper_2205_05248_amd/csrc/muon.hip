@@ -1,105 +1,112 @@
 // Newton-Schulz iteration X <- c0 X + (c1 G + c2 G G) X with G = X X^T on a batch of matrices, and the weight update by
-// an orthogonalised momentum.  fp32 tiles of 32 x 32 through shared memory, one thread per 2 x 2 results.
+// an orthogonalised momentum.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 
-#include "operator_types.h"
+#include "muon_product.h"
 
 namespace marl {
 namespace {
 
-constexpr int kTile = 32, kDepth = 32;
-
-// D = alpha A op(B) + beta C for matrices [M, K], [K, N] (or [N, K]: TRANSPOSED), dense, one batch member per blockIdx.z.
-template <bool TRANSPOSED>
-__global__ __launch_bounds__(256) void product_kernel(int M, int N, int K, const float *A, const float *B, const float *C, float *D,
-                                                      float alpha, float beta)
-{
-    __shared__ float a[kTile][kDepth + 1], b[kTile][kDepth + 1];
-    A += (size_t)blockIdx.z * M * K;
-    B += (size_t)blockIdx.z * K * N;
-    C += (size_t)blockIdx.z * M * N;
-    D += (size_t)blockIdx.z * M * N;
-    const int m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
-    const int tr = threadIdx.x / 16, tc = threadIdx.x % 16;
-    float acc[2][2] = {};
-    for (int k0 = 0; k0 < K; k0 += kDepth) {
-        for (int e = threadIdx.x; e < kTile * kDepth; e += 256) {
-            const int r = e / kDepth, k = e % kDepth;
-            a[r][k] = m0 + r < M && k0 + k < K ? A[(size_t)(m0 + r) * K + k0 + k] : 0.0f;
-            if constexpr (TRANSPOSED) b[r][k] = n0 + r < N && k0 + k < K ? B[(size_t)(n0 + r) * K + k0 + k] : 0.0f;
-            else b[k][r] = n0 + k < N && k0 + r < K ? B[(size_t)(k0 + r) * N + n0 + k] : 0.0f;
-        }
-        __syncthreads();
-        for (int k = 0; k < kDepth; ++k)
-            for (int i = 0; i < 2; ++i)
-                for (int j = 0; j < 2; ++j) acc[i][j] = fmaf(a[tr + 16 * i][k], b[tc + 16 * j][k], acc[i][j]);
-        __syncthreads();
-    }
-    for (int i = 0; i < 2; ++i)
-        for (int j = 0; j < 2; ++j) {
-            const int m = m0 + tr + 16 * i, n = n0 + tc + 16 * j;
-            if (m < M && n < N) D[(size_t)m * N + n] = alpha * acc[i][j] + (beta != 0.0f ? beta * C[(size_t)m * N + n] : 0.0f);
-        }
-}
-
 struct UpdateArgs {
-    int rows, cols;
-    bool tall;                 // X is the transpose
+    int rows, cols, rows_p, cols_p;    // as they are, and padded to multiples of 64
     const void *weights, *grad;
     const float *momentum;
     void *weights_out;
     float *momentum_out;
     float beta;
     int nesterov;
-    float keep, rate;          // weights_out = keep weights - rate X
-    float *X;
-    double *norm;              // [L] sum of squares
+    float keep, rate;                  // weights_out = keep weights - rate X
+    float eps;
+    double *part;                      // [L][kNormBlocks] sums of squares
+    _Float16 *Q, *Q_lo;                // planes in the matrix's own order; Q_lo, T_lo: PL = 1, may be NULL
+    _Float16 *T, *T_lo;                // and transposed
 };
 
-// X = the matrix (or its momentum) in fp32, and the sum of its squares: one workgroup per matrix.
+constexpr int kNormBlocks = 128;
+
 template <typename E>
-__global__ __launch_bounds__(1024) void start_kernel(UpdateArgs p)
+__device__ __forceinline__ float momentum_of(const UpdateArgs &p, size_t at)
 {
-    __shared__ double part[1024 / kWave];
-    const size_t n = (size_t)p.rows * p.cols, base = blockIdx.x * n;
+    const float g = to_f32(static_cast<const E *>(p.grad)[at]);
+    if (!p.momentum_out) return g;
+    const float m = p.momentum_out[at];
+    return p.nesterov ? fmaf(p.beta, m, g) : m;
+}
+
+// The new momentum, and the sum of squares of what is to be orthogonalised (fp64: squares of fp32 do not overflow there).
+template <typename E>
+__global__ __launch_bounds__(256) void momentum_kernel(UpdateArgs p)
+{
+    __shared__ double part[256 / kWave];
+    const size_t n = (size_t)p.rows * p.cols, base = blockIdx.y * n;
     double sum = 0.0;
-    for (size_t k = threadIdx.x; k < n; k += 1024) {
-        float u = to_f32(static_cast<const E *>(p.grad)[base + k]);
-        if (p.momentum) {
-            const float m = fmaf(p.beta, p.momentum[base + k], u);
-            p.momentum_out[base + k] = m;
-            u = p.nesterov ? fmaf(p.beta, m, u) : m;
-        }
-        const size_t r = k / p.cols, c = k % p.cols;
-        p.X[base + (p.tall ? c * p.rows + r : k)] = u;
+    for (size_t k = (size_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (size_t)kNormBlocks * 256) {
+        if (p.momentum) p.momentum_out[base + k] = fmaf(p.beta, p.momentum[base + k], to_f32(static_cast<const E *>(p.grad)[base + k]));
+        const float u = momentum_of<E>(p, base + k);
         sum += (double)u * u;
     }
     for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
     if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = 0.0;
-        for (int w = 0; w < 1024 / kWave; ++w) sum += part[w];
-        p.norm[blockIdx.x] = sum;
+    if (threadIdx.x == 0) p.part[(size_t)blockIdx.y * kNormBlocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// 1 / max(norm, eps), times the planes' scale, by the first wave's sum in fixed order.
+__device__ __forceinline__ double inverse_norm(const UpdateArgs &p, int batch)
+{
+    const double *part = p.part + (size_t)batch * kNormBlocks;
+    double sum = part[threadIdx.x % kWave] + part[threadIdx.x % kWave + kWave];
+    for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
+    return (double)kPlaneScale / fmax(sqrt(sum), (double)p.eps);
+}
+
+// X = u / max(|u|, eps) as planes, 64 x 64 entries a workgroup, in both orders; padding is zero.
+template <typename E, int PL>
+__global__ __launch_bounds__(256) void planes_kernel(UpdateArgs p)
+{
+    __shared__ float tile[64][65];
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+    const size_t n = (size_t)p.rows * p.cols, base = blockIdx.z * n, padded = (size_t)p.rows_p * p.cols_p * PL * blockIdx.z;
+    const double factor = inverse_norm(p, blockIdx.z);
+    for (int k = threadIdx.x; k < 64 * 64; k += 256) {
+        const int r = r0 + k / 64, c = c0 + k % 64;
+        tile[k / 64][k % 64] = r < p.rows && c < p.cols ? (float)(factor * momentum_of<E>(p, base + (size_t)r * p.cols + c)) : 0.0f;
+    }
+    __syncthreads();
+    auto put = [&](_Float16 *Q, _Float16 *Q_lo, size_t row, int ld, int c, const float *v) {
+        half8 h, l;
+        for (int e = 0; e < 8; ++e) {
+            h[e] = (_Float16)v[e];
+            l[e] = (_Float16)(v[e] - (float)h[e]);
+        }
+        _Float16 *to = Q + padded + row * ld * PL + plane_at<PL>(c);
+        *reinterpret_cast<half8 *>(to) = h;
+        if (PL == 2) *reinterpret_cast<half8 *>(to + 32) = l;
+        else if (Q_lo) *reinterpret_cast<half8 *>(Q_lo + padded + row * ld + c) = l;
+    };
+    for (int k = threadIdx.x; k < 64 * 8; k += 256) {
+        const int r = k / 8, c = k % 8 * 8;
+        float v[8], w[8];
+        for (int e = 0; e < 8; ++e) {
+            v[e] = tile[r][c + e];
+            w[e] = tile[c + e][r];
+        }
+        put(p.Q, p.Q_lo, (size_t)r0 + r, p.cols_p, c0 + c, v);
+        put(p.T, p.T_lo, (size_t)c0 + r, p.rows_p, r0 + c, w);
     }
 }
 
-__global__ __launch_bounds__(256) void scale_kernel(float *X, size_t n, const double *norm, float eps)
-{
-    const size_t k = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (k >= n) return;
-    X[blockIdx.y * n + k] = (float)(X[blockIdx.y * n + k] / fmax(sqrt(norm[blockIdx.y]), (double)eps));
-}
-
-template <typename E>
+template <typename E, int PL>
 __global__ __launch_bounds__(256) void finish_kernel(UpdateArgs p)
 {
     const size_t n = (size_t)p.rows * p.cols, k = (size_t)blockIdx.x * 256 + threadIdx.x, base = blockIdx.y * n;
     if (k >= n) return;
-    const size_t r = k / p.cols, c = k % p.cols;
-    const float x = p.X[base + (p.tall ? c * p.rows + r : k)];
+    const size_t r = k / p.cols, padded = (size_t)p.rows_p * p.cols_p * PL * blockIdx.y;
+    const int c = (int)(k % p.cols);
+    const size_t at = padded + r * p.cols_p * PL + plane_at<PL>(c);
+    const float x = ((float)p.Q[at] + (float)(PL == 2 ? p.Q[at + 32] : p.Q_lo[at])) * (1.0f / kPlaneScale);
     E *out = static_cast<E *>(p.weights_out) + base + k;
     *out = from_f32<E>(p.weights ? p.keep * to_f32(static_cast<const E *>(p.weights)[base + k]) - p.rate * x : x);
 }
@@ -108,51 +115,150 @@ bool sizes_ok(int L, int rows, int cols) { return L >= 0 && L <= 65535 && rows >
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
+// ---- which tiles a product takes
+struct Plan { int shape, splits; };                // shape: 0 of 256 x 256, 1 of 128 x 128, 2 of 64 x 64 results
+
+constexpr int kSide[3] = {256, 128, 64};
+
+int tiles_of(int shape, int Mp, int Np, bool symmetric)
+{
+    const int tm = (Mp + kSide[shape] - 1) / kSide[shape], tn = (Np + kSide[shape] - 1) / kSide[shape];
+    return symmetric ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+Plan plan_of(int L, int Mp, int Np, bool symmetric, int stages)
+{
+    Plan best{2, 1};
+    for (int shape = 0; shape < 3; ++shape)
+        if ((int64_t)tiles_of(shape, Mp, Np, symmetric) * L >= 128) { best.shape = shape; break; }
+    (void)stages;
+    return best;
+}
+
 struct Layout {
-    size_t x[2], g, p, norm, bytes;
+    int rows_p, cols_p, s, l, s_p, l_p, planes;
+    size_t x[2], t[2], x_lo[2], t_lo[2], g, p, part, bytes;
 };
 
-Layout layout_of(int L, int rows, int cols)
+Layout layout_of(int dtype, int L, int rows, int cols)
 {
-    const size_t s = rows < cols ? rows : cols, n = (size_t)rows * cols;
-    Layout l;
+    Layout y{};
+    auto pad = [](int v) { return (v + 63) / 64 * 64; };
+    y.rows_p = pad(rows); y.cols_p = pad(cols);
+    y.s = rows < cols ? rows : cols; y.l = rows < cols ? cols : rows;
+    y.s_p = pad(y.s); y.l_p = pad(y.l);
+    y.planes = dtype == MARL_DTYPE_BF16 ? 1 : 2;
+    const size_t n = (size_t)L * y.rows_p * y.cols_p * sizeof(_Float16), square = (size_t)L * y.s_p * y.s_p * sizeof(_Float16) * y.planes;
     size_t at = 0;
-    for (size_t &x : l.x) { x = at; at += up(L * n * sizeof(float)); }
-    l.g = at; at += up(L * s * s * sizeof(float));
-    l.p = at; at += up(L * s * s * sizeof(float));
-    l.norm = at; at += up(L * sizeof(double));
-    l.bytes = at;
-    return l;
+    auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
+    for (int k = 0; k < 2; ++k) {
+        y.x[k] = take(n * y.planes);
+        y.t[k] = take(n * y.planes);
+        y.x_lo[k] = y.planes == 1 ? take(n) : 0;
+        y.t_lo[k] = y.planes == 1 ? take(n) : 0;
+    }
+    y.g = take(square);
+    y.p = take(square);
+    y.part = take((size_t)L * kNormBlocks * sizeof(double));
+    y.bytes = at;
+    return y;
+}
+
+template <class S>
+int launch_product(Product p, int L, hipStream_t stream)
+{
+    static_assert(S::kLds <= 160 * 1024, "");
+    p.tiles_m = (p.Mp + S::TM - 1) / S::TM;
+    p.tiles_n = (p.Np + S::TN - 1) / S::TN;
+    p.tiles = p.symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+    if constexpr (S::kLds > 64 * 1024) {
+        for (const void *k : {reinterpret_cast<const void *>(product_kernel<S>), reinterpret_cast<const void *>(join_kernel<S>)}) {
+            const hipError_t err = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+            if (err != hipSuccess) return report_device_error(err, "hipFuncSetAttribute");
+        }
+    }
+    hipLaunchKernelGGL((product_kernel<S>), dim3((unsigned)(p.tiles * p.splits), (unsigned)L), dim3(S::kThreads), S::kLds, stream, p);
+    if (p.splits > 1) hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)p.tiles, (unsigned)L), dim3(S::kThreads), S::kLds, stream, p);
+    return MARL_OK;
+}
+
+template <int PL>
+int product(Product p, int L, hipStream_t stream)
+{
+    const Plan plan = plan_of(L, p.Mp, p.Np, p.symmetric, p.stages);
+    p.splits = plan.splits;
+    switch (plan.shape) {
+    case 0: return launch_product<TileShape<PL, 2, 4, 4, 2>>(p, L, stream);
+    case 1: return launch_product<TileShape<PL, 2, 2, 2, 2>>(p, L, stream);
+    default: return launch_product<TileShape<PL, 2, 2, 1, 1>>(p, L, stream);
+    }
+}
+
+template <typename E, int PL>
+int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, const float *coef, hipStream_t stream)
+{
+    auto at = [&](size_t offset) { return reinterpret_cast<_Float16 *>(workspace + offset); };
+    const bool tall = p.rows > p.cols;
+    _Float16 *X[2], *T[2], *X_lo[2], *T_lo[2];       // X [s][l] and its transpose
+    for (int k = 0; k < 2; ++k) {
+        X[k] = at(y.x[k]);
+        T[k] = at(y.t[k]);
+        X_lo[k] = PL == 1 ? at(y.x_lo[k]) : nullptr;
+        T_lo[k] = PL == 1 ? at(y.t_lo[k]) : nullptr;
+    }
+    p.rows_p = y.rows_p; p.cols_p = y.cols_p;
+    p.part = reinterpret_cast<double *>(workspace + y.part);
+    p.Q = tall ? T[0] : X[0]; p.Q_lo = tall ? T_lo[0] : X_lo[0];
+    p.T = tall ? X[0] : T[0]; p.T_lo = tall ? X_lo[0] : T_lo[0];
+    hipLaunchKernelGGL((momentum_kernel<E>), dim3(kNormBlocks, (unsigned)L), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((planes_kernel<E, PL>), dim3((unsigned)(y.cols_p / 64), (unsigned)(y.rows_p / 64), (unsigned)L), dim3(256), 0, stream, p);
+    const int64_t square = (int64_t)y.s_p * y.s_p * PL, whole = (int64_t)y.s_p * y.l_p * PL;
+    int now = 0;
+    for (int k = 0; k < steps; ++k) {
+        const bool last = k + 1 == steps;
+        Product g{};
+        g.A = g.B = X[now]; g.a_batch = g.b_batch = whole; g.lda = g.ldb = (int64_t)y.l_p * PL;
+        g.Mp = g.Np = y.s_p; g.stages = y.l_p * PL / 64;
+        g.alpha = 1.0f / kPlaneScale;
+        g.Dt = g.D = at(y.g); g.ldt = g.ldd = (int64_t)y.s_p * PL; g.t_batch = g.d_batch = square;
+        g.symmetric = 1;
+        int rc = product<PL>(g, L, stream);
+        if (rc) return rc;
+        Product q = g;
+        q.A = q.B = at(y.g); q.a_batch = q.b_batch = square; q.lda = q.ldb = (int64_t)y.s_p * PL;
+        q.stages = y.s_p * PL / 64;
+        q.alpha = coef[2] / kPlaneScale; q.beta = coef[1];
+        q.C = at(y.g);
+        q.Dt = q.D = at(y.p);
+        rc = product<PL>(q, L, stream);
+        if (rc) return rc;
+        Product x{};                                   // D [l][s] = X^T P, so D's transpose is the new X
+        x.A = T[now]; x.a_batch = whole; x.lda = (int64_t)y.s_p * PL;
+        x.B = at(y.p); x.b_batch = square; x.ldb = (int64_t)y.s_p * PL;
+        x.Mp = y.l_p; x.Np = y.s_p; x.stages = y.s_p * PL / 64;
+        x.alpha = 1.0f / kPlaneScale; x.beta = coef[0];
+        x.C = X[now]; x.C_lo = X_lo[now];
+        x.Dt = X[now ^ 1]; x.Dt_lo = X_lo[now ^ 1]; x.ldt = (int64_t)y.l_p * PL; x.t_batch = whole;
+        x.D = T[now ^ 1]; x.D_lo = last && tall ? T_lo[now ^ 1] : nullptr; x.ldd = (int64_t)y.s_p * PL; x.d_batch = whole;
+        rc = product<PL>(x, L, stream);
+        if (rc) return rc;
+        now ^= 1;
+    }
+    p.Q = tall ? T[now] : X[now]; p.Q_lo = tall ? T_lo[now] : X_lo[now];
+    const size_t n = (size_t)p.rows * p.cols;
+    hipLaunchKernelGGL((finish_kernel<E, PL>), dim3((unsigned)((n + 255) / 256), (unsigned)L), dim3(256), 0, stream, p);
+    return launched("orthogonalised update");
 }
 
 int newton_schulz(int dtype, int L, UpdateArgs p, char *workspace, int steps, const float *coef, float eps, hipStream_t stream)
 {
-    const Layout l = layout_of(L, p.rows, p.cols);
-    const int s = p.rows < p.cols ? p.rows : p.cols, len = p.rows < p.cols ? p.cols : p.rows;
-    const size_t n = (size_t)p.rows * p.cols;
-    float *X[2] = {reinterpret_cast<float *>(workspace + l.x[0]), reinterpret_cast<float *>(workspace + l.x[1])};
-    float *G = reinterpret_cast<float *>(workspace + l.g), *P = reinterpret_cast<float *>(workspace + l.p);
-    p.tall = p.rows > p.cols;
-    p.X = X[0];
-    p.norm = reinterpret_cast<double *>(workspace + l.norm);
-    const dim3 each((unsigned)((n + 255) / 256), (unsigned)L);
-    const unsigned ts = (unsigned)((s + kTile - 1) / kTile), tl = (unsigned)((len + kTile - 1) / kTile);
-    with_dtype(dtype, [&](auto e) {
-        hipLaunchKernelGGL((start_kernel<decltype(e)>), dim3((unsigned)L), dim3(1024), 0, stream, p);
-        return 0;
-    });
-    hipLaunchKernelGGL(scale_kernel, each, dim3(256), 0, stream, X[0], n, p.norm, eps);
-    for (int k = 0; k < steps; ++k) {
-        hipLaunchKernelGGL(product_kernel<true>, dim3(ts, ts, L), dim3(256), 0, stream, s, s, len, X[0], X[0], G, G, 1.0f, 0.0f);
-        hipLaunchKernelGGL(product_kernel<false>, dim3(ts, ts, L), dim3(256), 0, stream, s, s, s, G, G, G, P, coef[2], coef[1]);
-        hipLaunchKernelGGL(product_kernel<false>, dim3(tl, ts, L), dim3(256), 0, stream, s, len, s, P, X[0], X[0], X[1], 1.0f, coef[0]);
-        float *t = X[0]; X[0] = X[1]; X[1] = t;
+    p.eps = eps;
+    const Layout y = layout_of(dtype, L, p.rows, p.cols);
+    switch (dtype) {
+    case MARL_DTYPE_F32: return iterate<float, 2>(y, L, p, workspace, steps, coef, stream);
+    case MARL_DTYPE_BF16: return iterate<__bf16, 1>(y, L, p, workspace, steps, coef, stream);
+    default: return iterate<_Float16, 2>(y, L, p, workspace, steps, coef, stream);
     }
-    p.X = X[0];
-    return with_dtype(dtype, [&](auto e) {
-        hipLaunchKernelGGL((finish_kernel<decltype(e)>), each, dim3(256), 0, stream, p);
-        return launched("orthogonalised update");
-    });
 }
 
 int check(int dtype, int L, int rows, int cols, const void *workspace, size_t workspace_bytes, int steps, const float *coef, float eps)
@@ -163,7 +269,7 @@ int check(int dtype, int L, int rows, int cols, const void *workspace, size_t wo
     for (int k = 0; k < 3; ++k)
         if (!std::isfinite(coef[k])) return MARL_ERR_BAD_ARG;
     if (steps < 0 || steps > 64 || !std::isfinite(eps) || !(eps > 0.0f)) return MARL_ERR_BAD_ARG;
-    if (workspace_bytes < layout_of(L, rows, cols).bytes) return MARL_ERR_BAD_DIM;
+    if (workspace_bytes < layout_of(dtype, L, rows, cols).bytes) return MARL_ERR_BAD_DIM;
     if (!workspace && workspace_bytes) return MARL_ERR_NULL;
     return aligned_to(workspace, 256) ? MARL_OK : MARL_ERR_BAD_ARG;
 }
@@ -180,7 +286,7 @@ int marl_muon_workspace_bytes(int32_t dtype, int32_t L, int32_t rows, int32_t co
     if (!bytes) return MARL_ERR_NULL;
     if (!known_dtype(dtype)) return MARL_ERR_BAD_DTYPE;
     if (!sizes_ok(L, rows, cols)) return MARL_ERR_BAD_DIM;
-    *bytes = layout_of(L, rows, cols).bytes;
+    *bytes = layout_of(dtype, L, rows, cols).bytes;
     return MARL_OK;
 }
 

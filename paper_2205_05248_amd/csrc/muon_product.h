@@ -1,0 +1,301 @@
+// Products of the Newton-Schulz iteration on the fp16 matrix pipe.
+//
+// Every matrix of the iteration is kept as fp16 planes of its entries times 2^12: hi = fp16(v), lo = fp16(v - hi).  The scale
+// keeps lo above fp16's subnormals at the size that entries of large matrices have, and leaves room up to 16 (singular values
+// end near 1.2).  D = A B^T with both operands adjacent along the summed index, so that both are read the same way; G and P
+// are symmetric, and X is kept beside its transpose.
+//
+// PL = 2 (fp32 and fp16 matrices): each operand has both planes, a product is hi hi + hi lo + lo hi in fp32 accumulators; what is
+// left out, lo lo, is 2^-24 of a term.  Planes alternate in blocks of 32 of the summed index, [hi x 32][lo x 32].
+// PL = 1 (bf16 matrices): operands have the plane hi alone, 2^-12 of a term.  That is no rounding of X itself: X is carried
+// in the term c0 X with its plane lo, which lies in an array of its own.  Rounded X there would put noise into directions
+// in which X is small, and five steps would multiply it by up to 485; noise in P X and G is of the size of what it stands in.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "operator_types.h"
+
+namespace marl {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+constexpr float kPlaneScale = 4096.0f;
+
+// D[m, n] = alpha sum_k A[m, k] B[n, k] + beta C[m, n], m < Mp, n < Np (multiples of 64: the matrices are padded with zeros).
+// Strides and rows are in fp16 values; offset of (r, k) in planes: r ld + plane_at<PL>(k).
+struct Product {
+    const _Float16 *A, *B;
+    int64_t a_batch, b_batch;
+    int64_t lda, ldb;
+    int Mp, Np, stages;               // stages of 64 fp16 values of a row: 64 / PL of the summed index
+    float alpha, beta;
+    const _Float16 *C, *C_lo;         // [n][m], of scaled entries; C_lo: PL = 1 only.  Used with beta != 0
+    _Float16 *Dt, *Dt_lo;             // [n][m]
+    _Float16 *D, *D_lo;               // [m][n] or NULL
+    int64_t ldt, ldd, t_batch, d_batch;        // C, C_lo, Dt_lo lie as Dt; D_lo as D
+    int symmetric;                    // A is B: only tiles on and below the diagonal, D is the mirrored tile
+    int tiles_m, tiles_n, tiles;      // tiles: of one batch member
+    int splits;                       // parts of the sum, one workgroup each; > 1: accumulators go to `partial`
+    float *partial;                   // [batch][tiles][splits][16 MT NT / 4][threads] x 4
+};
+
+template <int PL>
+__host__ __device__ __forceinline__ int plane_at(int k) { return PL == 1 ? k : (k >> 5) * 64 + (k & 31); }
+
+template <int PL_, int WM_, int WN_, int MT_, int NT_>
+struct TileShape {
+    static constexpr int PL = PL_, WM = WM_, WN = WN_, MT = MT_, NT = NT_;
+    static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
+    static constexpr int TM = WM * MT * 32, TN = WN * NT * 32;
+    static constexpr int kStage = (TM + TN) * 128;                     // bytes: 64 fp16 values of every row
+    static constexpr int kWide = PL * 32 * (MT > NT ? MT : NT) + 8;    // a staged row of results, fp16 values
+    static constexpr int kStaging = 32 * kWide * 2;                    // bytes a wave
+    static constexpr int kLds = 2 * kStage > kWaves * kStaging ? 2 * kStage : kWaves * kStaging;
+    static constexpr int kQuads = 4 * MT * NT;                         // groups of four accumulators of a lane
+};
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
+
+// Tile (i, j) of a linear index.  Workgroups go round the eight dies in turn, so consecutive tiles are given to one die, and
+// they walk down strips eight tiles wide, so that what a die works on at a time shares its operands.
+__device__ __forceinline__ void tile_of(const Product &p, int id, int &i, int &j)
+{
+    if (p.symmetric) {
+        i = (int)((sqrtf(8.0f * (float)id + 1.0f) - 1.0f) * 0.5f);
+        while (i * (i + 1) / 2 > id) --i;
+        while ((i + 1) * (i + 2) / 2 <= id) ++i;
+        j = id - i * (i + 1) / 2;
+        return;
+    }
+    const int strip = id / (8 * p.tiles_m), first = strip * 8, width = min(8, p.tiles_n - first);
+    const int in = id - strip * 8 * p.tiles_m;
+    i = in / width;
+    j = first + in % width;
+}
+
+__device__ __forceinline__ int die_order(int id, int n)
+{
+    const int per = n / 8, rest = n % 8, die = id % 8;
+    return die * per + min(die, rest) + id / 8;
+}
+
+// What becomes of a tile's accumulators: result in fp16 planes, in both orders.
+template <class S>
+__device__ __forceinline__ void put_tile(const Product &p, int64_t batch, int m0, int n0, bool diagonal, floatx16 (&acc)[S::MT][S::NT], char *lds)
+{
+    constexpr int PL = S::PL, MT = S::MT, NT = S::NT;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int wm = m0 + (wave / S::WN) * MT * 32, wn = n0 + (wave % S::WN) * NT * 32;
+    const int col = lane & 31, high = lane >> 5;
+    _Float16 *stage = reinterpret_cast<_Float16 *>(lds + wave * S::kStaging);
+    auto wave_sync = [] {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    _Float16 *Dt = p.Dt + batch * p.t_batch, *D = p.D ? p.D + batch * p.d_batch : nullptr;
+    _Float16 *Dt_lo = p.Dt_lo ? p.Dt_lo + batch * p.t_batch : nullptr, *D_lo = p.D_lo ? p.D_lo + batch * p.d_batch : nullptr;
+    const _Float16 *C = p.C + batch * p.t_batch, *C_lo = p.C_lo ? p.C_lo + batch * p.t_batch : nullptr;
+#pragma unroll
+    for (int mb = 0; mb < MT; ++mb)
+#pragma unroll
+        for (int nb = 0; nb < NT; ++nb) {
+            __builtin_amdgcn_sched_barrier(0);                         // one block's loads at a time, or registers run out
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int m = wm + mb * 32 + 8 * q + 4 * high, n = wn + nb * 32 + col;
+                floatx4 c = {0, 0, 0, 0};
+                if (p.beta != 0.0f && m < p.Mp && n < p.Np) {
+                    const int64_t at = n * p.ldt + plane_at<PL>(m);
+                    const half4 h = *reinterpret_cast<const half4 *>(C + at);
+                    half4 l = {0, 0, 0, 0};
+                    if constexpr (PL == 2) l = *reinterpret_cast<const half4 *>(C + at + 32);
+                    else if (C_lo) l = *reinterpret_cast<const half4 *>(C_lo + at);
+                    for (int e = 0; e < 4; ++e) c[e] = (float)h[e] + (float)l[e];
+                }
+                for (int e = 0; e < 4; ++e) acc[mb][nb][4 * q + e] = p.alpha * acc[mb][nb][4 * q + e] + p.beta * c[e];
+            }
+        }
+    // rows n of the transpose, 32 at a time
+    const int passes = PL == 1 && (Dt_lo || D_lo) ? 2 : 1;             // PL = 1: the plane lo after the plane hi
+    for (int pass = 0; pass < passes; ++pass) {
+        _Float16 *T = pass ? Dt_lo : Dt;
+        if (T) {
+#pragma unroll
+            for (int nb = 0; nb < NT; ++nb) {
+                wave_sync();
+#pragma unroll
+                for (int mb = 0; mb < MT; ++mb) {
+                    asm volatile("" : "+v"(acc[mb][nb]));              // planes are formed where they are stored, not kept
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        half4 h, l;
+                        for (int e = 0; e < 4; ++e) {
+                            const float v = acc[mb][nb][4 * q + e];
+                            h[e] = (_Float16)v;
+                            l[e] = (_Float16)(v - (float)h[e]);
+                        }
+                        const int k = mb * 32 + 8 * q + 4 * high;
+                        *reinterpret_cast<half4 *>(stage + col * S::kWide + plane_at<PL>(k)) = pass ? l : h;
+                        if constexpr (PL == 2) *reinterpret_cast<half4 *>(stage + col * S::kWide + plane_at<PL>(k) + 32) = l;
+                    }
+                }
+                wave_sync();
+                constexpr int kChunks = MT * 4 * PL;                   // of eight values in a row
+                for (int c = lane; c < 32 * kChunks; c += kWave) {
+                    const int r = c / kChunks, k = c % kChunks * 8, n = wn + nb * 32 + r;
+                    if (n < p.Np && wm + k / PL < p.Mp)
+                        *reinterpret_cast<half8 *>(T + n * p.ldt + (int64_t)wm * PL + k) = *reinterpret_cast<const half8 *>(stage + r * S::kWide + k);
+                }
+            }
+        }
+        _Float16 *R = pass ? D_lo : D;
+        if (R && !diagonal) {
+#pragma unroll
+            for (int mb = 0; mb < MT; ++mb) {
+                wave_sync();
+#pragma unroll
+                for (int nb = 0; nb < NT; ++nb) {
+                    asm volatile("" : "+v"(acc[mb][nb]));
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float v = acc[mb][nb][e];
+                        const _Float16 h = (_Float16)v, l = (_Float16)(v - (float)h);
+                        const int r = 8 * (e / 4) + 4 * high + e % 4, k = nb * 32 + col;
+                        stage[r * S::kWide + plane_at<PL>(k)] = pass ? l : h;
+                        if constexpr (PL == 2) stage[r * S::kWide + plane_at<PL>(k) + 32] = l;
+                    }
+                }
+                wave_sync();
+                constexpr int kChunks = NT * 4 * PL;
+                for (int c = lane; c < 32 * kChunks; c += kWave) {
+                    const int r = c / kChunks, k = c % kChunks * 8, m = wm + mb * 32 + r;
+                    if (m < p.Mp && wn + k / PL < p.Np)
+                        *reinterpret_cast<half8 *>(R + m * p.ldd + (int64_t)wn * PL + k) = *reinterpret_cast<const half8 *>(stage + r * S::kWide + k);
+                }
+            }
+        }
+    }
+}
+
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    constexpr int PL = S::PL, MT = S::MT, NT = S::NT, TM = S::TM, TN = S::TN;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int units = p.tiles * p.splits;
+    const int unit = die_order(blockIdx.x, units), tile = unit % p.tiles, split = unit / p.tiles;
+    const int64_t batch = blockIdx.y;
+    int ti, tj;
+    tile_of(p, tile, ti, tj);
+    const int m0 = ti * TM, n0 = tj * TN;
+    const int k_begin = (int)((int64_t)split * p.stages / p.splits), k_end = (int)((int64_t)(split + 1) * p.stages / p.splits);
+
+    // A wave's load brings eight rows of 128 bytes; chunk c of row r goes to place c ^ (r & 7), so that lanes reading the same
+    // chunk of neighbouring rows meet different banks.  The place in shared memory is fixed by the lane, so the lane
+    // asks for the chunk that belongs there.
+    constexpr int kLoadsA = TM / 8 / S::kWaves, kLoadsB = TN / 8 / S::kWaves;
+    static_assert(kLoadsA * 8 * S::kWaves == TM && kLoadsB * 8 * S::kWaves == TN, "");
+    const int sub = lane >> 3, chunk = (lane & 7) ^ sub;
+    const _Float16 *from_a[kLoadsA], *from_b[kLoadsB];
+#pragma unroll
+    for (int q = 0; q < kLoadsA; ++q)
+        from_a[q] = p.A + batch * p.a_batch + (int64_t)min(m0 + (q * S::kWaves + wave) * 8 + sub, p.Mp - 1) * p.lda + chunk * 8;
+#pragma unroll
+    for (int q = 0; q < kLoadsB; ++q)
+        from_b[q] = p.B + batch * p.b_batch + (int64_t)min(n0 + (q * S::kWaves + wave) * 8 + sub, p.Np - 1) * p.ldb + chunk * 8;
+    auto load = [&](int k, int buffer) {
+        char *to = lds + buffer * S::kStage;
+#pragma unroll
+        for (int q = 0; q < kLoadsA; ++q)
+            __builtin_amdgcn_global_load_lds((global_void *)(from_a[q] + (int64_t)k * 64), (lds_void *)(to + (q * S::kWaves + wave) * 1024), 16, 0, 0);
+#pragma unroll
+        for (int q = 0; q < kLoadsB; ++q)
+            __builtin_amdgcn_global_load_lds((global_void *)(from_b[q] + (int64_t)k * 64), (lds_void *)(to + TM * 128 + (q * S::kWaves + wave) * 1024), 16, 0, 0);
+    };
+    floatx16 acc[MT][NT];
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
+
+    const int row = lane & 31, high = lane >> 5;
+    const char *read_a = lds + ((wave / S::WN) * MT * 32 + row) * 128, *read_b = lds + TM * 128 + ((wave % S::WN) * NT * 32 + row) * 128;
+    auto frag = [&](const char *base, int block, int c) {
+        return *reinterpret_cast<const half8 *>(base + block * 32 * 128 + ((c ^ (row & 7)) << 4));
+    };
+    load(k_begin, 0);
+    for (int k = k_begin; k < k_end; ++k) {
+        const int buffer = (k - k_begin) & 1;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // this wave's part of the stage has arrived
+        __syncthreads();                                               // everybody's has, and the other buffer is read
+        if (k + 1 < k_end) load(k + 1, buffer ^ 1);
+        const char *ra = read_a + buffer * S::kStage, *rb = read_b + buffer * S::kStage;
+#pragma unroll
+        for (int j = 0; j < 4 / PL; ++j) {
+            half8 a[PL][MT], b[PL][NT];
+#pragma unroll
+            for (int pl = 0; pl < PL; ++pl) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t) a[pl][t] = frag(ra, t, 4 * pl + 2 * j + high);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) b[pl][t] = frag(rb, t, 4 * pl + 2 * j + high);
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int u = 0; u < NT; ++u) {
+                    acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][t], b[0][u], acc[t][u], 0, 0, 0);
+                    if constexpr (PL == 2) {
+                        acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][t], b[1][u], acc[t][u], 0, 0, 0);
+                        acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1][t], b[0][u], acc[t][u], 0, 0, 0);
+                    }
+                }
+        }
+    }
+    if (p.splits > 1) {
+        floatx4 *to = reinterpret_cast<floatx4 *>(p.partial) + ((batch * p.tiles + tile) * p.splits + split) * (S::kQuads * S::kThreads) + threadIdx.x;
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+            for (int b = 0; b < NT; ++b)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    to[((a * NT + b) * 4 + q) * S::kThreads] = floatx4{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+        return;
+    }
+    __syncthreads();                                                   // the buffers become staging room
+    put_tile<S>(p, batch, m0, n0, p.symmetric && ti == tj, acc, lds);
+}
+
+// Sums the parts of a tile, in order, and finishes it.
+template <class S>
+__global__ __launch_bounds__(S::kThreads) void join_kernel(Product p)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int64_t batch = blockIdx.y;
+    const int tile = blockIdx.x;
+    int ti, tj;
+    tile_of(p, tile, ti, tj);
+    floatx16 acc[S::MT][S::NT];
+    const floatx4 *from = reinterpret_cast<const floatx4 *>(p.partial) + (batch * p.tiles + tile) * p.splits * (S::kQuads * S::kThreads) + threadIdx.x;
+#pragma unroll
+    for (int a = 0; a < S::MT; ++a)
+#pragma unroll
+        for (int b = 0; b < S::NT; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                floatx4 sum = {0, 0, 0, 0};
+                for (int s = 0; s < p.splits; ++s) sum += from[(s * S::kQuads + (a * S::NT + b) * 4 + q) * S::kThreads];
+                for (int e = 0; e < 4; ++e) acc[a][b][4 * q + e] = sum[e];
+            }
+    put_tile<S>(p, batch, ti * S::TM, tj * S::TN, p.symmetric && ti == tj, acc, lds);
+}
+
+}  // namespace marl

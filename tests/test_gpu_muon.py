@@ -61,6 +61,16 @@ def test_orthogonalize(L, rows, cols, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("L,rows,cols", [(32, 500, 450), (40, 260, 700)])
+def test_many_matrices_of_a_size_that_fills_the_large_tiles(dtype, L, rows, cols):
+    m = gradient(gen(L), L, rows, cols, dtype)
+    out = torch.empty_like(m, device="cuda")
+    binding.marl_orthogonalize(m.cuda(), out, workspace(dtype, L, rows, cols))
+    torch.cuda.synchronize()
+    close(out, orc.orthogonalize(host(m)), dtype, "out")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rank", [1, 3])
 def test_low_rank(dtype, rank):
     g = gen(rank)
