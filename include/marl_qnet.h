@@ -506,7 +506,7 @@ int marl_linear_step(int32_t dtype, int32_t n, int32_t C, const void *x, int64_t
 
 /*
  * Log probability of a given token (or action) in each of R rows of V logits, the entropy of the row and its K most
- * likely tokens.  Over the available entries whose logit is above -infinity, z = scale * logit:
+ * likely tokens.  Over the available entries, z = scale * logit (an entry whose z is -infinity has no probability):
  *   log_sum = log(sum exp z)   logp = z[token] - log_sum   entropy = -sum p log p, p = exp(z - log_sum)
  *   logits   dev [R,V] elem, rows ld apart
  *   token    dev [R] i32 or NULL        outside [0, V): logp is 0 and has no gradient.  Not available: logp is

@@ -1,8 +1,9 @@
 // Log probability of given tokens, entropy and most likely alternatives of rows of logits, and the logits' gradient.
-// One workgroup per row: one pass with a running maximum m, sum s = sum e^(z-m) and moment w = sum e^(z-m) (z-m), from which
-// log_sum = m + log s and entropy = log s - w / s.
+// One pass with a running maximum m, sum s = sum e^(z-m) and moment w = sum e^(z-m) (z-m), from which log_sum = m + log s and
+// entropy = log s - w / s.  Forward and backward are bound by the bytes of the logits.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "device_math.h"
@@ -30,6 +31,10 @@ struct LogProbArgs {
     const float *in_log_sum, *in_entropy, *grad_logp, *grad_entropy;
     void *grad_logits;
     int64_t ld_grad;
+    // long rows in parts
+    int parts, per;                    // parts of a row, chunks of a part
+    float *stats;                      // [R, parts, 4]
+    unsigned long long *keys;          // [R, parts, K]
 };
 
 // Running statistics of a set of z; m = -inf is the empty set.
@@ -37,117 +42,417 @@ struct Stats {
     float m, s, w;
 };
 
-// w of a set moved from maximum m to M >= m:  sum e^(z-M) (z-M) = e^(m-M) (w + (m-M) s).  Distances end at kFar, where
-// e^ is 0 in fp32: the distance of a type's lowest value would make the product 0 * infinity.
+// Distances end at kFar, where e^ is 0 in fp32: the distance of a type's lowest value would make the product 0 * infinity.
 constexpr float kFar = -200.0f;
+
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(kLog2e * v); }
 
 // The lowest finite value stays finite under a scale above one.
 __device__ __forceinline__ float scaled(float scale, float logit) { return fmaxf(scale * logit, -3.4028235e38f); }
 
+// w of a set moved from maximum m to M >= m:  sum e^(z-M) (z-M) = e^(m-M) (w + (m-M) s).  NaN in m stays.
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ Stats move_to(Stats a, float M)
+{
+    const float d = fmaxf(a.m - M, kFar), e = exp_of(d);
+    return {M, a.s * e, e * fmaf(d, a.s, a.w)};
+}
 __device__ __forceinline__ Stats join(Stats a, Stats b)
 {
-    const float M = fmaxf(a.m, b.m);
-    if (!(M > -kInf)) return {-kInf, a.s + b.s, 0.0f};          // (a NaN stays in s)
-    const float da = fmaxf(a.m - M, kFar), db = fmaxf(b.m - M, kFar);
-    const float ea = a.m > -kInf ? __expf(da) : 0.0f, eb = b.m > -kInf ? __expf(db) : 0.0f;
-    return {M, a.s * ea + b.s * eb, (a.m > -kInf ? ea * (a.w + da * a.s) : 0.0f) + (b.m > -kInf ? eb * (b.w + db * b.s) : 0.0f)};
+    const float M = max_nan(a.m, b.m);
+    a = move_to(a, M);
+    b = move_to(b, M);
+    return {M, a.s + b.s, a.w + b.w};
+}
+template <int LANES>
+__device__ __forceinline__ Stats join_lanes(Stats st)
+{
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) st = join(st, {__shfl_xor(st.m, d), __shfl_xor(st.s, d), __shfl_xor(st.w, d)});
+    return st;
+}
+
+// Takes in N logits, -inf where there is none.  A row's maximum settles after a few calls.
+template <int N>
+__device__ __forceinline__ void take(Stats &st, const float (&l)[N], float scale)
+{
+    float top = l[0];
+#pragma unroll
+    for (int k = 1; k < N; ++k) top = max_nan(top, l[k]);
+    const float M = max_nan(st.m, top == -kInf ? -kInf : top * scale);
+    if (!(M == st.m)) st = move_to(st, M);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        // nothing there: the distance ends at -1e30, whose exponential is 0.  NaN too, but then M is NaN, which is what counts.
+        const float d = fmaxf(fmaf(l[k], scale, -M), -1e30f), e = exp_of(d);
+        st.s += e;
+        st.w = fmaf(e, d, st.w);
+    }
+}
+
+// What a row's statistics and its token give.  A maximum of NaN or +infinity makes everything NaN.
+__device__ __forceinline__ void put_row(const LogProbArgs &p, int64_t row, Stats st, bool available, float logit, int token)
+{
+    const bool none = st.m == -kInf, bad = !(st.m < kInf);
+    const float nan = __builtin_nanf(""), log_s = logf(st.s);
+    if (p.log_sum) p.log_sum[row] = bad ? nan : none ? -kInf : st.m + log_s;
+    if (p.entropy) p.entropy[row] = bad ? nan : none ? 0.0f : log_s - st.w / st.s;
+    if (p.logp) {
+        float lp = 0.0f;
+        if (token >= 0 && token < p.V) lp = bad ? nan : none ? 0.0f : !available || logit == -kInf ? -kInf : fmaf(logit, p.scale, -st.m) - log_s;
+        else if (bad) lp = nan;
+        p.logp[row] = lp;
+    }
 }
 
 template <typename E>
-__global__ __launch_bounds__(kThreads) void log_prob_kernel(LogProbArgs p)
+__device__ __forceinline__ void finish_row(const LogProbArgs &p, int64_t row, Stats st)
 {
+    const int token = p.logp ? p.token[row] : -1;
+    const bool in = token >= 0 && token < p.V;
+    put_row(p, row, st, in && (!p.avail || p.avail[row * p.ld_avail + token]), in ? to_f32(static_cast<const E *>(p.logits)[row * p.ld + token]) : 0.0f, token);
+}
+
+// ---------------------------------------------------------------------------------- the K largest of what a wave holds
+// Keys order values, and equal values by lower index; 0 is nothing.
+typedef unsigned long long Key;
+
+__device__ __forceinline__ unsigned order_of(float v)
+{
+    const unsigned u = __float_as_uint(v + 0.0f);                      // -0 is 0
+    return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(Key key)
+{
+    const unsigned u = (unsigned)(key >> 32);
+    return __uint_as_float(u ^ (u >> 31 ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ Key key_of(unsigned order, unsigned index) { return order ? (Key)order << 32 | (unsigned)~index : 0; }
+__device__ __forceinline__ unsigned index_of(Key key) { return ~(unsigned)key; }
+
+__device__ __forceinline__ Key lane_key(Key key, int lane)
+{
+    return (Key)(unsigned)__builtin_amdgcn_readlane((int)(key >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)key, lane);
+}
+
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// out[0 .. K) = the K largest of 64 N entries in descending order, 0 behind the last.  The K-th largest of the lanes' own
+// largest bounds the K-th largest of all from below, and only K lanes have anything that reaches it: what reaches it goes to
+// `kept` (room for K N keys) and is ordered by counting.  For K = 20 of random values 24 of 2048 reach it.
+// RISING: a lane's indexes rise with j, so that of equal values it meets the first one first.
+template <int N, bool RISING, class OrderAt, class IndexAt>
+__device__ __forceinline__ void wave_top(OrderAt order, IndexAt index, int K, Key *kept, Key *out)
+{
+    const int lane = threadIdx.x % kWave;
+    Key mine = 0;
+    if constexpr (RISING) {
+        unsigned best = 0, at = 0;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (order(j) > best) { best = order(j); at = index(j); }
+        mine = key_of(best, at);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const Key key = key_of(order(j), index(j));
+            mine = key > mine ? key : mine;
+        }
+    }
+    int above = 0;
+    for (int l = 0; l < kWave; ++l) above += lane_key(mine, l) > mine;
+    const unsigned long long at_k = __ballot(above == K - 1 && mine);
+    const Key least = at_k ? lane_key(mine, __ffsll((long long)at_k) - 1) : 1;
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const Key key = key_of(order(j), index(j));
+        const unsigned long long pass = __ballot(key >= least);
+        if (pass) {
+            if (key >= least) kept[n + __popcll(pass & ((1ull << lane) - 1))] = key;
+            n += __popcll(pass);
+        }
+    }
+    wave_sync();
+    for (int c = lane; c < n; c += kWave) {
+        const Key key = kept[c];
+        int rank = 0;
+        for (int q = 0; q < n; ++q) rank += kept[q] > key;
+        if (rank < K) out[rank] = key;
+    }
+    for (int c = n + lane; c < K; c += kWave) out[c] = 0;
+    wave_sync();
+}
+
+__device__ __forceinline__ void put_top(const LogProbArgs &p, int64_t row, int k, Key key, Stats st, float log_s)
+{
+    p.top_id[row * p.K + k] = key ? (int)index_of(key) : -1;
+    p.top_logp[row * p.K + k] = key ? fmaf(value_of(key), p.scale, -st.m) - log_s : -kInf;
+}
+
+// ---------------------------------------------------------------------------------- reading
+// 16 bytes of a row at any element alignment, and as many mask bytes.
+template <typename E>
+struct Piece {
+    static constexpr int V = 16 / (int)sizeof(E);
+    typedef E Vec __attribute__((ext_vector_type(V)));
+    typedef Vec Loose __attribute__((aligned(sizeof(E))));
+    typedef uint8_t Bytes __attribute__((ext_vector_type(V)));
+    typedef Bytes LooseBytes __attribute__((aligned(1)));
+};
+
+// Entries j .. j + V of a row as fp32, -inf where masked or behind the end.
+template <typename E>
+__device__ __forceinline__ void read_piece(const E *l, const uint8_t *av, int j, int V, float *to)
+{
+    typedef Piece<E> P;
+    if (j + P::V <= V) {
+        const typename P::Vec v = *reinterpret_cast<const typename P::Loose *>(l + j);
+#pragma unroll
+        for (int k = 0; k < P::V; ++k) to[k] = to_f32(v[k]);
+        if (av) {
+            const typename P::Bytes m = *reinterpret_cast<const typename P::LooseBytes *>(av + j);
+#pragma unroll
+            for (int k = 0; k < P::V; ++k) to[k] = m[k] ? to[k] : -kInf;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < P::V; ++k) to[k] = j + k < V && (!av || av[j + k]) ? to_f32(l[j + k]) : -kInf;
+    }
+}
+
+// ---------------------------------------------------------------------------------- long rows
+constexpr int kHeld = 32;                              // logits of a lane at a time
+constexpr int kChunk = kThreads * kHeld;               // of a workgroup
+
+// A workgroup takes `per` chunks of a row; with one part per row it finishes the row, otherwise join_kernel does.  With
+// alternatives a part is one chunk, which stays in registers for wave_top.
+template <typename E, bool TOP>
+__global__ __launch_bounds__(kThreads) void long_rows_kernel(LogProbArgs p)
+{
+    constexpr int V = Piece<E>::V;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ Stats part[kThreads / kWave];
-    __shared__ float best_v[kThreads / kWave];
-    __shared__ int best_j[kThreads / kWave];
-    const int64_t row = blockIdx.x;
+    const int64_t row = blockIdx.x / p.parts;
+    const int piece = blockIdx.x % p.parts;
     const E *l = static_cast<const E *>(p.logits) + row * p.ld;
     const uint8_t *av = p.avail ? p.avail + row * p.ld_avail : nullptr;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t begin = (int64_t)piece * p.per * kChunk, end = begin + (int64_t)p.per * kChunk < p.V ? begin + (int64_t)p.per * kChunk : p.V;
     Stats st{-kInf, 0.0f, 0.0f};
-    for (int j = threadIdx.x; j < p.V; j += kThreads) {
-        if (av && !av[j]) continue;
-        const float v = to_f32(l[j]);
-        if (v == -kInf) continue;
-        st = join(st, {scaled(p.scale, v), 1.0f, 0.0f});
-        if (!(v < kInf)) st.s = __builtin_nanf("");             // NaN or +infinity: the row's values are NaN
+    float held[kHeld];
+    for (int64_t base = begin; base < end; base += kChunk) {
+#pragma unroll
+        for (int q = 0; q < kHeld / V; ++q) read_piece<E>(l, av, (int)base + (q * kThreads + (int)threadIdx.x) * V, p.V, held + q * V);
+        take(st, held, p.scale);
     }
-    for (int d = 1; d < kWave; d *= 2) st = join(st, {__shfl_xor(st.m, d), __shfl_xor(st.s, d), __shfl_xor(st.w, d)});
+    st = join_lanes<kWave>(st);
     if (lane == 0) part[wave] = st;
+    if constexpr (TOP) {
+        const int K = p.K;
+        Key *lists = reinterpret_cast<Key *>(lds), *kept = lists + (kThreads / kWave) * K + (size_t)wave * K * kHeld;
+        wave_top<kHeld, true>([&](int j) { return held[j] == -kInf ? 0u : order_of(held[j]); },
+                        [&](int j) { return (unsigned)((int)begin + (j / V * kThreads + (int)threadIdx.x) * V + j % V); }, K, kept, lists + wave * K);
+    }
     __syncthreads();
+    if (wave != 0) return;
     st = part[0];
+#pragma unroll
     for (int w = 1; w < kThreads / kWave; ++w) st = join(st, part[w]);
-    const bool none = st.s == 0.0f;
-    const float log_s = logf(st.s);
-    if (threadIdx.x == 0) {
-        if (p.log_sum) p.log_sum[row] = none ? -kInf : st.m + log_s;
-        if (p.entropy) p.entropy[row] = none ? 0.0f : log_s - st.w / st.s;
-        if (p.logp) {
-            const int tok = p.token ? p.token[row] : -1;
-            float lp = 0.0f;
-            if (!none && tok >= 0 && tok < p.V) {
-                const float v = to_f32(l[tok]);
-                lp = (av && !av[tok]) || v == -kInf ? -kInf : (scaled(p.scale, v) - st.m) - log_s;
-            }
-            p.logp[row] = lp;
+    if constexpr (TOP) {
+        const int K = p.K;
+        Key *lists = reinterpret_cast<Key *>(lds), *kept = lists + (kThreads / kWave) * K;
+        Key own[kThreads / kWave];
+#pragma unroll
+        for (int w = 0; w < kThreads / kWave; ++w) own[w] = lane < K ? lists[w * K + lane] : 0;
+        wave_sync();
+        wave_top<kThreads / kWave, false>([&](int j) { return (unsigned)(own[j] >> 32); }, [&](int j) { return index_of(own[j]); }, K, kept, lists);
+        if (lane < K) {
+            if (p.parts > 1) p.keys[((int64_t)row * p.parts + piece) * K + lane] = lists[lane];
+            else put_top(p, row, lane, lists[lane], st, logf(st.s));
         }
     }
-    // the K largest, one after the other: the largest among those that come after the last one in (value, index) order
-    float last_v = kInf;
-    int last_j = -1;
-    for (int k = 0; k < p.K; ++k) {
-        float v = -kInf;
-        int at = -1;
-        for (int j = threadIdx.x; j < p.V; j += kThreads) {
-            if (av && !av[j]) continue;
-            const float x = to_f32(l[j]);
-            if ((x < last_v || (x == last_v && j > last_j)) && x > v) { v = x; at = j; }
+    if (lane == 0) {
+        if (p.parts > 1) {
+            float *to = p.stats + ((int64_t)row * p.parts + piece) * 4;
+            to[0] = st.m; to[1] = st.s; to[2] = st.w;
+        } else {
+            finish_row<E>(p, row, st);
         }
-        for (int d = 1; d < kWave; d *= 2) {
-            const float ov = __shfl_xor(v, d);
-            const int oj = __shfl_xor(at, d);
-            if (oj >= 0 && (at < 0 || ov > v || (ov == v && oj < at))) { v = ov; at = oj; }
-        }
-        __syncthreads();
-        if (lane == 0) { best_v[wave] = v; best_j[wave] = at; }
-        __syncthreads();
-        v = -kInf;
-        at = -1;
-        for (int w = 0; w < kThreads / kWave; ++w)
-            if (best_j[w] >= 0 && (at < 0 || best_v[w] > v || (best_v[w] == v && best_j[w] < at))) { v = best_v[w]; at = best_j[w]; }
-        if (threadIdx.x == 0) {
-            p.top_id[row * p.K + k] = at;
-            p.top_logp[row * p.K + k] = at < 0 ? -kInf : (scaled(p.scale, v) - st.m) - log_s;
-        }
-        if (at < 0) { last_v = -kInf; last_j = p.V; }
-        else { last_v = v; last_j = at; }
     }
 }
 
+// A wave per row joins its parts.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void log_prob_grad_kernel(LogProbArgs p)
+__global__ __launch_bounds__(kWave) void join_kernel(LogProbArgs p)
 {
+    constexpr int N = 8;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x, K = p.K;
+    Stats st{-kInf, 0.0f, 0.0f};
+    for (int k = lane; k < p.parts; k += kWave) {
+        const float *from = p.stats + (row * p.parts + k) * 4;
+        st = join(st, {from[0], from[1], from[2]});
+    }
+    st = join_lanes<kWave>(st);
+    if (K > 0) {
+        Key *out = reinterpret_cast<Key *>(lds), *kept = out + K;
+        const Key *from = p.keys + row * p.parts * K;
+        const int64_t n = (int64_t)p.parts * K;
+        bool first = true;
+        for (int64_t base = 0; base < n; first = false) {              // the K best so far, and as many more as there is room for
+            Key own[N];
+            own[0] = first ? 0 : lane < K ? out[lane] : 0;
+#pragma unroll
+            for (int j = 1; j < N; ++j) {
+                const int64_t k = base + (int64_t)(j - 1) * kWave + lane;
+                own[j] = k < n ? from[k] : 0;
+            }
+            base += (N - 1) * kWave;
+            wave_sync();
+            wave_top<N, false>([&](int j) { return (unsigned)(own[j] >> 32); }, [&](int j) { return index_of(own[j]); }, K, kept, out);
+        }
+        if (lane < K) put_top(p, row, lane, out[lane], st, logf(st.s));
+    }
+    if (lane == 0) finish_row<E>(p, row, st);
+}
+
+// ---------------------------------------------------------------------------------- short rows
+// G lanes hold a row of at most G N logits; a wave takes 64 / G rows.
+template <typename E, int G, int N>
+__global__ __launch_bounds__(kThreads) void short_rows_kernel(LogProbArgs p)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, sub = lane % G;
+    const int64_t row = ((int64_t)blockIdx.x * (kThreads / kWave) + wave) * (kWave / G) + lane / G;
+    const bool there = row < p.R;
+    const E *l = static_cast<const E *>(p.logits) + (there ? row : 0) * p.ld;
+    const uint8_t *av = p.avail ? p.avail + (there ? row : 0) * p.ld_avail : nullptr;
+    float held[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int k = j * G + sub;
+        held[j] = there && k < p.V && (!av || av[k]) ? to_f32(l[k]) : -kInf;
+    }
+    Stats st{-kInf, 0.0f, 0.0f};
+    take(st, held, p.scale);
+    st = join_lanes<G>(st);
+    if (there && sub == 0) finish_row<E>(p, row, st);
+    if (p.K == 0) return;
+    const float log_s = logf(st.s);
+    if constexpr (G == kWave) {
+        if (!there) return;                                            // the whole wave
+        Key *out = reinterpret_cast<Key *>(lds) + (size_t)wave * p.K * (N + 1), *kept = out + p.K;
+        wave_top<N, true>([&](int j) { return held[j] == -kInf ? 0u : order_of(held[j]); }, [&](int j) { return (unsigned)(j * G + sub); }, p.K, kept, out);
+        if (lane < p.K) put_top(p, row, lane, out[lane], st, log_s);
+    } else {
+        Key last = ~(Key)0;
+        for (int k = 0; k < p.K; ++k) {                                // the largest below the last one
+            Key best = 0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const Key key = held[j] == -kInf ? 0 : key_of(order_of(held[j]), j * G + sub);
+                if (key < last && key > best) best = key;
+            }
+#pragma unroll
+            for (int d = 1; d < G; d *= 2) {
+                const Key other = (Key)(unsigned)__shfl_xor((int)(best >> 32), d) << 32 | (unsigned)__shfl_xor((int)(unsigned)best, d);
+                best = other > best ? other : best;
+            }
+            if (there && sub == 0) put_top(p, row, k, best, st, log_s);
+            last = best;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------- gradient
+struct RowGrad { float log_sum, ent, g_logp, g_ent; int token; };      // token: -1 without a gradient of its own; log_sum -inf: nothing there
+
+template <typename E>
+__device__ __forceinline__ RowGrad row_grad(const LogProbArgs &p, int64_t row)
+{
+    RowGrad g;
+    g.log_sum = p.in_log_sum[row];
+    const int tok = p.grad_logp ? p.token[row] : -1;
+    const bool has = tok >= 0 && tok < p.V && !(p.avail && !p.avail[row * p.ld_avail + tok]) &&
+                     to_f32(static_cast<const E *>(p.logits)[row * p.ld + tok]) != -kInf;
+    g.token = has ? tok : -1;
+    g.g_logp = has ? p.grad_logp[row] : 0.0f;
+    g.g_ent = p.grad_entropy ? p.grad_entropy[row] : 0.0f;
+    g.ent = p.grad_entropy ? p.in_entropy[row] : 0.0f;
+    return g;
+}
+
+__device__ __forceinline__ float grad_of(const RowGrad &g, float logit, int j, float scale)
+{
+    // p as the square of its root, which the hardware exponential does not flush where p is subnormal
+    const float lp = fmaxf(scaled(scale, logit) - g.log_sum, kFar), root = __builtin_amdgcn_exp2f(0.5f * kLog2e * lp);
+    const float v = scale * ((j == g.token ? g.g_logp : 0.0f) - root * (root * fmaf(g.g_ent, lp + g.ent, g.g_logp)));
+    return logit == -kInf || g.log_sum == -kInf ? 0.0f : v;
+}
+
+// A workgroup takes `per` chunks of a row (the whole row if it overwrites the logits: the token's is read before any is gone).
+template <typename E>
+__global__ __launch_bounds__(kThreads) void long_grad_kernel(LogProbArgs p)
+{
+    typedef Piece<E> P;
+    constexpr int V = P::V, kPieces = 4;
+    const int64_t row = blockIdx.x / p.parts;
+    const int piece = blockIdx.x % p.parts;
     const E *l = static_cast<const E *>(p.logits) + row * p.ld;
     const uint8_t *av = p.avail ? p.avail + row * p.ld_avail : nullptr;
     E *out = static_cast<E *>(p.grad_logits) + row * p.ld_grad;
-    const float log_sum = p.in_log_sum[row];
-    const bool none = log_sum == -kInf;
-    const int tok = p.grad_logp ? p.token[row] : -1;
-    const bool has = !none && tok >= 0 && tok < p.V && !(av && !av[tok]) && to_f32(l[tok]) != -kInf;
-    const float g_logp = has ? p.grad_logp[row] : 0.0f;
-    const float g_ent = p.grad_entropy ? p.grad_entropy[row] : 0.0f, ent = p.grad_entropy ? p.in_entropy[row] : 0.0f;
-    __syncthreads();                                            // the token's logit is read before it may be overwritten
-    for (int j = threadIdx.x; j < p.V; j += kThreads) {
-        float g = 0.0f;
-        if (!none && !(av && !av[j])) {
-            const float v = to_f32(l[j]);
-            if (v != -kInf) {
-                // p as the square of its root, which the hardware exponential does not flush where p is subnormal
-                const float lp = fmaxf(scaled(p.scale, v) - log_sum, kFar), root = __builtin_amdgcn_exp2f(0.5f * kLog2e * lp);
-                g = p.scale * ((has && j == tok ? g_logp : 0.0f) - root * (root * (g_logp + g_ent * (lp + ent))));
+    const RowGrad g = row_grad<E>(p, row);
+    __syncthreads();
+    constexpr int kStep = kThreads * V * kPieces;
+    const int64_t begin = (int64_t)piece * p.per * kStep, end = begin + (int64_t)p.per * kStep < p.V ? begin + (int64_t)p.per * kStep : p.V;
+    for (int64_t base = begin; base < end; base += kStep) {
+        float held[kPieces][V];
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) read_piece<E>(l, av, (int)base + (q * kThreads + (int)threadIdx.x) * V, p.V, held[q]);
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+            const int j = (int)base + (q * kThreads + (int)threadIdx.x) * V;
+            typename P::Vec v;
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = from_f32<E>(grad_of(g, held[q][k], j + k, p.scale));
+            if (j + V <= p.V) {
+                *reinterpret_cast<typename P::Loose *>(out + j) = v;
+            } else {
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (j + k < p.V) out[j + k] = v[k];
             }
         }
-        out[j] = from_f32<E>(g);
+    }
+}
+
+template <typename E, int G, int N>
+__global__ __launch_bounds__(kThreads) void short_grad_kernel(LogProbArgs p)
+{
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, sub = lane % G;
+    const int64_t row = ((int64_t)blockIdx.x * (kThreads / kWave) + wave) * (kWave / G) + lane / G;
+    if (row >= p.R) return;
+    const E *l = static_cast<const E *>(p.logits) + row * p.ld;
+    const uint8_t *av = p.avail ? p.avail + row * p.ld_avail : nullptr;
+    E *out = static_cast<E *>(p.grad_logits) + row * p.ld_grad;
+    const RowGrad g = row_grad<E>(p, row);
+    float held[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int k = j * G + sub;
+        held[j] = k < p.V && (!av || av[k]) ? to_f32(l[k]) : -kInf;
+    }
+    wave_sync();                                                       // all of the row is read before any of it is overwritten
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int k = j * G + sub;
+        if (k < p.V) out[k] = from_f32<E>(grad_of(g, held[j], k, p.scale));
     }
 }
 
@@ -160,7 +465,90 @@ int log_prob_check(int dtype, int R, int V, const void *logits, int64_t ld, cons
     return !logits && R > 0 ? MARL_ERR_NULL : MARL_OK;
 }
 
-size_t log_prob_workspace(int, int, int) { return 0; }
+// Rows up to this long are held by one wave or a part of it.
+constexpr int kShort = 2048;
+
+// Parts of a long row: with alternatives one per chunk; otherwise as many as fill the chip (eight workgroups on each of 256
+// compute units), not less than a chunk each.
+struct Cut { int parts, per; };
+Cut cut_of(int R, int V, int chunk, bool one_each)
+{
+    const int chunks = (V + chunk - 1) / chunk;
+    const int wanted = one_each ? chunks : (int)std::min<int64_t>(chunks, std::max<int64_t>(1, 2048 / std::max(R, 1)));
+    const int per = (chunks + wanted - 1) / wanted;
+    return {(chunks + per - 1) / per, per};
+}
+
+size_t log_prob_workspace(int R, int V, int K)
+{
+    if (V <= kShort) return 0;
+    const Cut cut = cut_of(R, V, kChunk, K > 0);
+    if (cut.parts == 1) return 0;
+    const size_t n = (size_t)R * cut.parts;
+    return ((n * 4 * sizeof(float) + 255) / 256 + (n * K * sizeof(Key) + 255) / 256) * 256;
+}
+
+template <typename E>
+int run_forward(LogProbArgs p, char *workspace, hipStream_t stream)
+{
+    if (p.V <= kShort) {
+        // lanes of a row: enough to hold it, few enough that short rows share a wave
+        auto go = [&](auto kernel, int G, int N) {
+            const int64_t rows = (int64_t)(kThreads / kWave) * (kWave / G);
+            const size_t lds = G == kWave ? (size_t)(kThreads / kWave) * p.K * (N + 1) * sizeof(Key) : 0;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((p.R + rows - 1) / rows)), dim3(kThreads), lds, stream, p);
+            return launched("log prob");
+        };
+        if (p.V <= 16) return go(short_rows_kernel<E, 4, 4>, 4, 4);
+        if (p.V <= 64) return go(short_rows_kernel<E, 8, 8>, 8, 8);
+        if (p.V <= 256) return go(short_rows_kernel<E, 16, 16>, 16, 16);
+        if (p.V <= 512) return go(short_rows_kernel<E, kWave, 8>, kWave, 8);
+        return go(short_rows_kernel<E, kWave, 32>, kWave, 32);
+    }
+    const Cut cut = cut_of(p.R, p.V, kChunk, p.K > 0);
+    p.parts = cut.parts;
+    p.per = cut.per;
+    if ((int64_t)p.R * p.parts >= ((int64_t)1 << 31)) return MARL_ERR_BAD_DIM;
+    p.stats = reinterpret_cast<float *>(workspace);
+    p.keys = reinterpret_cast<Key *>(workspace + ((size_t)p.R * p.parts * 4 * sizeof(float) + 255) / 256 * 256);
+    const dim3 grid((unsigned)(p.R * p.parts));
+    if (p.K > 0) {
+        const size_t lds = (size_t)(kThreads / kWave) * p.K * (kHeld + 1) * sizeof(Key);
+        if (lds > 64 * 1024) {
+            const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(long_rows_kernel<E, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (err != hipSuccess) return report_device_error(err, "hipFuncSetAttribute");
+        }
+        hipLaunchKernelGGL((long_rows_kernel<E, true>), grid, dim3(kThreads), lds, stream, p);
+    } else {
+        hipLaunchKernelGGL((long_rows_kernel<E, false>), grid, dim3(kThreads), 0, stream, p);
+    }
+    if (p.parts > 1) hipLaunchKernelGGL(join_kernel<E>, dim3((unsigned)p.R), dim3(kWave), (size_t)p.K * 9 * sizeof(Key), stream, p);
+    return launched("log prob");
+}
+
+template <typename E>
+int run_backward(LogProbArgs p, hipStream_t stream)
+{
+    if (p.V <= kShort) {
+        auto go = [&](auto kernel, int G) {
+            const int64_t rows = (int64_t)(kThreads / kWave) * (kWave / G);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((p.R + rows - 1) / rows)), dim3(kThreads), 0, stream, p);
+            return launched("log prob gradient");
+        };
+        if (p.V <= 16) return go(short_grad_kernel<E, 4, 4>, 4);
+        if (p.V <= 64) return go(short_grad_kernel<E, 8, 8>, 8);
+        if (p.V <= 256) return go(short_grad_kernel<E, 16, 16>, 16);
+        if (p.V <= 512) return go(short_grad_kernel<E, kWave, 8>, kWave);
+        return go(short_grad_kernel<E, kWave, 32>, kWave);
+    }
+    Cut cut = cut_of(p.R, p.V, kThreads * Piece<E>::V * 4, false);
+    if (p.grad_logits == p.logits) cut = {1, cut.parts * cut.per};
+    p.parts = cut.parts;
+    p.per = cut.per;
+    if ((int64_t)p.R * p.parts >= ((int64_t)1 << 31)) return MARL_ERR_BAD_DIM;
+    hipLaunchKernelGGL((long_grad_kernel<E>), dim3((unsigned)(p.R * p.parts)), dim3(kThreads), 0, stream, p);
+    return launched("log prob gradient");
+}
 
 }  // namespace
 }  // namespace marl
@@ -192,10 +580,7 @@ int marl_log_prob(int32_t dtype, int32_t R, int32_t V, const void *logits, int64
     p.R = R; p.V = V; p.K = K;
     p.logits = logits; p.ld = ld; p.token = token; p.avail = avail; p.ld_avail = ld_avail; p.scale = scale;
     p.logp = logp; p.entropy = entropy; p.log_sum = log_sum; p.top_id = top_id; p.top_logp = top_logp;
-    return with_dtype(dtype, [&](auto e) {
-        hipLaunchKernelGGL((log_prob_kernel<decltype(e)>), dim3((unsigned)R), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), p);
-        return launched("log prob");
-    });
+    return with_dtype(dtype, [&](auto e) { return run_forward<decltype(e)>(p, static_cast<char *>(workspace), static_cast<hipStream_t>(hip_stream)); });
 }
 
 int marl_log_prob_grad(int32_t dtype, int32_t R, int32_t V, const void *logits, int64_t ld, const int32_t *token,
@@ -214,10 +599,7 @@ int marl_log_prob_grad(int32_t dtype, int32_t R, int32_t V, const void *logits, 
     p.logits = logits; p.ld = ld; p.token = token; p.avail = avail; p.ld_avail = ld_avail; p.scale = scale;
     p.in_log_sum = log_sum; p.in_entropy = entropy; p.grad_logp = grad_logp; p.grad_entropy = grad_entropy;
     p.grad_logits = grad_logits; p.ld_grad = ld_grad;
-    return with_dtype(dtype, [&](auto e) {
-        hipLaunchKernelGGL((log_prob_grad_kernel<decltype(e)>), dim3((unsigned)R), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), p);
-        return launched("log prob gradient");
-    });
+    return with_dtype(dtype, [&](auto e) { return run_backward<decltype(e)>(p, static_cast<hipStream_t>(hip_stream)); });
 }
 
 }  // extern "C"
