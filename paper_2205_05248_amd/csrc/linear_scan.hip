@@ -11,29 +11,26 @@
 namespace marl {
 namespace {
 
-// The shape of the work.  A workgroup (a "unit") takes CT = 8 V channels, V of them 16 bytes of a row, over a span of
-// steps: eight lanes share a row, so a load instruction brings 128 bytes of each of eight rows, and a lane walks Tc steps
-// that follow one another.  Groups of eight lanes, then waves, then units follow one another in time.  What a
-// stretch of steps does to the state is h -> A h + H, and stretches compose; so a lane composes its own steps, eight groups
-// compose by lane exchange, the waves through shared memory, and units through memory (see look_back).  The inputs are read
-// once and stay in registers until the state at the unit's start is known.
-// Narrow and long units: the number of units of one sequence in flight, which is what look_back walks over, is small.
-template <typename E>
-struct Span {
-    static constexpr int V = 16 / (int)sizeof(E);
-    static constexpr int CT = 8 * V;
-};
+// The shape of the work.  A workgroup (a "unit") takes 64 channels over a span of steps.  A lane takes four bytes of a row
+// (V channels) and Tc steps that follow one another; lanes of one row lie side by side, and the wave holds V rows' worth of
+// lanes ("groups"), then waves, then units, which follow one another in time.  What a stretch of steps does to the
+// state is h -> A h + H, and stretches compose: a lane composes its own steps, the two groups of 16-bit types compose by lane
+// exchange, the waves through shared memory, and units through memory (see look_back).  The inputs are read once and stay
+// in registers until the state at the unit's start is known.
+// Narrow and long units: the number of units of one sequence in flight, which is what look_back walks over, is small.  Four
+// bytes a lane rather than sixteen: with eight channels a lane the lane exchanges were eight per element of the backward pass.
+constexpr int kChannels = 64;
+template <typename E> constexpr int kWide = 4 / (int)sizeof(E);            // V: channels of a lane, groups of a wave
+constexpr int kSteps = 16;                                                 // Tc forward
+template <typename E> constexpr int kStepsBack = 16 / kWide<E>;            // Tc backward: 16 elements, of which more is kept
 
-constexpr int kElements = 32, kElementsBack = 16;      // of a lane: V channels x Tc steps (the backward pass keeps more of each)
-constexpr int kMostWaves = 8;
-
-template <typename E> constexpr int steps_of_lane(bool back) { return (back ? kElementsBack : kElements) / Span<E>::V; }
-
-// Waves of a unit: enough for T, at most kMostWaves.
-inline int waves_for(int T, int lane_steps)
+// Most waves of a unit, and the waves that T needs.  The backward pass keeps seven values of each element: four waves of 168
+// registers, three units on a compute unit.
+constexpr int kMostWaves = 8, kMostWavesBack = 4;
+inline int waves_for(int T, int wave_steps, int most)
 {
     int w = 1;
-    while (w < kMostWaves && w * 8 * lane_steps < T) w *= 2;
+    while (w < most && w * wave_steps < T) w *= 2;
     return w;
 }
 
@@ -51,10 +48,10 @@ struct ScanArgs {
     void *y;
     int64_t ld_y;
     float *h_last;
-    float *states;                     // [B, kept, C] state before each `keep`-th step
-    int keep, kept;
+    float *states;                     // [B, kept, C] state before each 2^keep_log-th step
+    int keep_log, kept;
     unsigned *ticket;                  // order in which units begin
-    Word *words;                       // [units, sequences, CT]
+    Word *words;                       // [units, sequences, 64]
     // backward pass
     const void *grad_y;
     int64_t ld_gy;
@@ -79,71 +76,115 @@ __device__ __forceinline__ Sigmoid sigmoid2(float v)
     return {s, e * s};
 }
 
-// 1 - exp(y) for y <= 0.  Near 0 the difference would cancel: there the series, whose next term is below 2^-25.
-__device__ __forceinline__ float one_minus_exp(float y, float exp_y)
+// beta^2 = 1 - a^2 with a = exp(-x), x >= 0.  Near 0 the difference would cancel: there 2 a sinh(x) by its series, whose next
+// term is below 2^-26 of it.
+__device__ __forceinline__ float beta_square(float x, float a)
 {
-    float p = fmaf(y, 1.0f / 7.0f, 1.0f);
-    p = fmaf(y * (1.0f / 6.0f), p, 1.0f);
-    p = fmaf(y * 0.2f, p, 1.0f);
-    p = fmaf(y * 0.25f, p, 1.0f);
-    p = fmaf(y * (1.0f / 3.0f), p, 1.0f);
-    p = fmaf(y * 0.5f, p, 1.0f);
-    return y > -0.35f ? -y * p : 1.0f - exp_y;
+    const float q = x * x;
+    float p = fmaf(q, 1.0f / 5040.0f, 1.0f / 120.0f);
+    p = fmaf(q, p, 1.0f / 6.0f);
+    p = fmaf(q, p, 1.0f);
+    const float near = (a + a) * (x * p);
+    return x < 0.5f ? near : fmaf(-a, a, 1.0f);
 }
 
-struct Gates { Sigmoid sr, si; float a, inv_beta, beta; };
-__device__ __forceinline__ Gates gates_of(float r, float i, float rate)
+// What one step does forward: h -> a h + u.
+struct Step { float a, u; };
+__device__ __forceinline__ float amount_of(float x, float i) { return x * sigmoidf_fast(i); }
+__device__ __forceinline__ Step step_of(float x, float r, float i, float rate)
 {
-    Gates g;
-    g.sr = sigmoid2(r);
-    g.si = sigmoid2(i);
-    const float L = -rate * g.sr.s;
-    g.a = __builtin_amdgcn_exp2f(kLog2e * L);
-    const float om = one_minus_exp(2.0f * L, g.a * g.a);
-    g.inv_beta = __builtin_amdgcn_rsqf(fmaxf(om, 1e-30f));     // a gate that is shut has om = 0: beta 0, and no infinity
-    g.beta = om * g.inv_beta;
-    return g;
+    const float d = rate * sigmoidf_fast(r), a = __builtin_amdgcn_exp2f(-kLog2e * d);
+    return {a, __builtin_amdgcn_sqrtf(beta_square(d, a)) * amount_of(x, i)};
 }
 
-// 16 bytes of a row; entries beyond the last channel are zero and not stored.
-template <typename E, bool VEC>
+// And what its gradients need: dx = dh m, di = dh n, dL = a dh (h before - q), dr = -w s dL.
+struct StepBack { float a, u, q, m, n, s, w; };
+__device__ __forceinline__ StepBack step_back_of(float x, float r, float i, float rate, bool start)
+{
+    const Sigmoid sr = sigmoid2(r), si = sigmoid2(i);
+    const float d = rate * sr.s, a = __builtin_amdgcn_exp2f(-kLog2e * d), om = beta_square(d, a);
+    const float inv = __builtin_amdgcn_rsqf(fmaxf(om, 1e-30f));        // a gate that is shut has om = 0: beta 0, and no infinity
+    const float m = start ? si.s : om * inv * si.s, u = m * x;
+    return {start ? 0.0f : a, u, start ? 0.0f : a * inv * (si.s * x), m, u * si.c, sr.s, rate * sr.c};
+}
+
+// Four bytes of a row.  PAIRS: they lie at a multiple of four bytes and there is no odd channel at the end.
+// Held as one word: as a pair of 16-bit values the compiler gave each a register of its own wherever branches meet.
+template <typename E, bool PAIRS>
 struct Row {
-    static constexpr int V = Span<E>::V;
+    static constexpr int V = kWide<E>;
     typedef E Vec __attribute__((ext_vector_type(V)));
-    Vec v;
-    __device__ __forceinline__ void load(const void *base, int64_t at, int left)
+    uint32_t bits;
+    __device__ __forceinline__ float operator[](int k) const
     {
-        const E *p = static_cast<const E *>(base) + at;
-        if constexpr (VEC) {
-            v = *reinterpret_cast<const Vec *>(p);
-        } else {
+        uint32_t b = bits;
+        asm("" : "+v"(b));
+        return to_f32(__builtin_bit_cast(Vec, b)[k]);
+    }
+    __device__ __forceinline__ void set(const float (&f)[V])
+    {
+        Vec v;
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = k < left ? p[k] : (E)0.0f;
+        for (int k = 0; k < V; ++k) v[k] = from_f32<E>(f[k]);
+        bits = __builtin_bit_cast(uint32_t, v);
+    }
+};
+
+// A wave's rows of one array: the first one's address is the same for the wave, a lane adds its group's rows and its
+// channels, and a step adds a distance that is the same for all: no vector arithmetic per access.  reach: steps behind
+// the first that exist; loads of later ones read the last (and are dropped), stores are left out.
+template <typename E, bool PAIRS>
+struct Strip {
+    static constexpr int V = kWide<E>;
+    char *base;
+    int64_t step;                      // bytes
+    uint32_t lane;                     // bytes
+    int c;                             // element of the row
+    __device__ __forceinline__ Strip(const void *p, int64_t ld, int64_t row, int c0, int cl, int rows_down)
+        : base(static_cast<char *>(const_cast<void *>(p)) + (row * ld + c0) * (int)sizeof(E)), step(ld * (int)sizeof(E)),
+          lane((uint32_t)rows_down * (uint32_t)step + (uint32_t)cl * (uint32_t)sizeof(E)), c(cl) {}
+    __device__ __forceinline__ void load(Row<E, PAIRS> &r, int j, int left) const { read(r, base + j * step + lane, left); }
+    __device__ __forceinline__ void load_within(Row<E, PAIRS> &r, int t, int reach, int left) const
+    {
+        read(r, base + (int64_t)min(t, reach) * step + (uint32_t)c * (uint32_t)sizeof(E), left);
+    }
+    __device__ __forceinline__ void read(Row<E, PAIRS> &r, const char *at, int left) const
+    {
+        if constexpr (PAIRS) {
+            r.bits = *reinterpret_cast<const uint32_t *>(at);
+        } else {
+            typename Row<E, PAIRS>::Vec v;
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = k < left ? reinterpret_cast<const E *>(at)[k] : (E)0.0f;
+            r.bits = __builtin_bit_cast(uint32_t, v);
         }
     }
-    __device__ __forceinline__ void store(void *base, int64_t at, int left) const
+    __device__ __forceinline__ void store(const Row<E, PAIRS> &r, int j, int left) const
     {
-        E *p = static_cast<E *>(base) + at;
-        if constexpr (VEC) {
-            *reinterpret_cast<Vec *>(p) = v;
+        char *at = base + j * step + lane;
+        if constexpr (PAIRS) {
+            *reinterpret_cast<uint32_t *>(at) = r.bits;
         } else {
+            const typename Row<E, PAIRS>::Vec v = __builtin_bit_cast(typename Row<E, PAIRS>::Vec, r.bits);
 #pragma unroll
             for (int k = 0; k < V; ++k)
-                if (k < left) p[k] = v[k];
+                if (k < left) reinterpret_cast<E *>(at)[k] = v[k];
         }
     }
 };
 
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// What a step does to the state.  kPast: behind the last step; as padding, but nothing is stored.
-enum Kind { kPast, kPadding, kStart, kOrdinary };
-__device__ __forceinline__ Kind kind_of(const ScanArgs &p, int64_t b, int t)
+// Which of the N steps from t0 on (N <= 32, the same for the whole wave) exist, are filled, start a sequence: a bit each.
+struct Steps { unsigned exist, filled, start; };
+template <int N>
+__device__ __forceinline__ Steps steps_at(const ScanArgs &p, int64_t b, int t0)
 {
-    if (t >= p.T) return kPast;
-    const int64_t row = b * p.T + t;
-    if (p.filled && !p.filled[row]) return kPadding;
-    return p.reset && p.reset[row] ? kStart : kOrdinary;
+    const int lane = threadIdx.x % kWave, t = t0 + lane;
+    const bool exist = lane < N && t < p.T;
+    const int64_t row = b * p.T + (exist ? t : 0);
+    const bool filled = exist && (!p.filled || p.filled[row]), start = filled && p.reset && p.reset[row];
+    return {(unsigned)__ballot(exist), (unsigned)__ballot(filled), (unsigned)__ballot(start)};
 }
 
 __device__ __forceinline__ Word word_of(float A, float H)
@@ -159,7 +200,7 @@ __device__ __forceinline__ Word peek(const Word *at) { return __hip_atomic_load(
 // waits only for units whose tickets are lower, and they began before it: each wait ends.
 __device__ __forceinline__ float look_back(const Word *words, int before, int64_t stride, bool mine)
 {
-    constexpr int kAtOnce = 8;
+    constexpr int kAtOnce = 4;
     float A = 1.0f, H = 0.0f;
     bool open = mine;
     for (int k = before; k >= 0 && __any(open); k -= kAtOnce) {
@@ -196,92 +237,114 @@ __global__ __launch_bounds__(256) void scan_begin_kernel(Word *words, int64_t n_
 
 // Unit of a workgroup: sequences advance side by side, time outermost.
 struct Place { int seq, unit, b, c0; };
-template <typename E, bool CHAIN>
+template <bool CHAIN>
 __device__ __forceinline__ Place place_of(const ScanArgs &p, int *shared)
 {
     int id = blockIdx.x;
     if constexpr (CHAIN) {
         if (threadIdx.x == 0) *shared = (int)atomicAdd(p.ticket, 1u);
         lds_barrier();
-        id = *shared;
+        id = __builtin_amdgcn_readfirstlane(*shared);
     }
     const int seq = id % p.sequences;
-    return {seq, id / p.sequences, seq / p.tiles, seq % p.tiles * Span<E>::CT};
+    return {seq, id / p.sequences, seq / p.tiles, seq % p.tiles * kChannels};
 }
 
-template <typename E, bool VEC, int NW, bool CHAIN>
+template <typename E, bool PAIRS, int NW, bool CHAIN>
 __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
 {
-    constexpr int V = Span<E>::V, CT = Span<E>::CT, Tc = steps_of_lane<E>(false);
-    __shared__ float rate_s[CT], A_s[NW][CT], H_s[NW][CT], carry_s[NW][CT];
+    constexpr int V = kWide<E>, Tc = kSteps, kWaveSteps = V * Tc, kAll = (int)((1ull << kWaveSteps) - 1);
+    __shared__ float rate_s[kChannels], A_s[NW][kChannels], H_s[NW][kChannels], carry_s[NW][kChannels];
     __shared__ int id_s;
-    const Place at = place_of<E, CHAIN>(p, &id_s);
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, group = lane / 8, cl = lane % 8 * V;
-    const int c = at.c0 + cl, left = p.C - c, first = at.unit * (NW * 8 * Tc), t0 = first + (wave * 8 + group) * Tc;
-    Row<E, VEC> x[Tc], r[Tc], i[Tc];
-    Kind kind[Tc];
+    const Place at = place_of<CHAIN>(p, &id_s);
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / (kWave / V), cl = lane % (kWave / V) * V;
+    const int c = at.c0 + cl, left = p.C - c, first = at.unit * (NW * kWaveSteps), tw = first + wave * kWaveSteps;
+    const Steps steps = steps_at<kWaveSteps>(p, at.b, tw);
+    const unsigned exist = steps.exist >> (group * Tc), filled = steps.filled >> (group * Tc), start = steps.start >> (group * Tc);
+    const int64_t row0 = (int64_t)at.b * p.T + tw;
+    const int down = group * Tc;
+    Row<E, PAIRS> x[Tc], r[Tc], i[Tc];
+    if (steps.filled && left > 0) {
+        const Strip<E, PAIRS> sx(p.x, p.ld_x, row0, at.c0, cl, down), sr(p.r, p.ld_r, row0, at.c0, cl, down), si(p.i, p.ld_i, row0, at.c0, cl, down);
+        if (steps.exist == (unsigned)kAll) {
 #pragma unroll
-    for (int j = 0; j < Tc; ++j) {
-        kind[j] = left > 0 ? kind_of(p, at.b, t0 + j) : kPast;
-        if (kind[j] > kPadding) {
-            const int64_t row = (int64_t)at.b * p.T + t0 + j;
-            x[j].load(p.x, row * p.ld_x + c, left);
-            r[j].load(p.r, row * p.ld_r + c, left);
-            i[j].load(p.i, row * p.ld_i + c, left);
+            for (int j = 0; j < Tc; ++j) {
+                sr.load(r[j], j, left);
+                si.load(i[j], j, left);
+                sx.load(x[j], j, left);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < Tc; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                sr.load_within(r[j], down + j, p.T - 1 - tw, left);
+                si.load_within(i[j], down + j, p.T - 1 - tw, left);
+                sx.load_within(x[j], down + j, p.T - 1 - tw, left);
+            }
         }
     }
-    for (int k = threadIdx.x; k < CT; k += NW * kWave) rate_s[k] = at.c0 + k < p.C ? rate_of(p.lam[at.c0 + k], p.decay) : 0.0f;
+    for (int k = threadIdx.x; k < kChannels; k += NW * kWave) rate_s[k] = at.c0 + k < p.C ? rate_of(p.lam[at.c0 + k], p.decay) : 0.0f;
     lds_barrier();
     float a[Tc][V], u[Tc][V], A[V], H[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
+    if (steps.filled == (unsigned)kAll && steps.start == 0) {
 #pragma unroll
-    for (int j = 0; j < Tc; ++j) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            a[j][v] = 1.0f;
-            u[j][v] = 0.0f;
-        }
-        if (kind[j] > kPadding) {
+        for (int j = 0; j < Tc; ++j) {
+            __builtin_amdgcn_sched_barrier(0);         // a few steps at a time, or registers run out
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gates g = gates_of(to_f32(r[j].v[v]), to_f32(i[j].v[v]), rate_s[cl + v]);
-                const float in = g.si.s * to_f32(x[j].v[v]);
-                a[j][v] = kind[j] == kStart ? 0.0f : g.a;
-                u[j][v] = kind[j] == kStart ? in : g.beta * in;
-                H[v] = fmaf(a[j][v], H[v], u[j][v]);
-                A[v] *= a[j][v];
+                const Step s = step_of(x[j][v], r[j][v], i[j][v], rate_s[cl + v]);
+                a[j][v] = s.a;
+                u[j][v] = s.u;
+                H[v] = fmaf(s.a, H[v], s.u);
+                A[v] *= s.a;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < Tc; ++j) {
+            const bool live = filled >> j & 1, fresh = start >> j & 1;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                Step s = step_of(x[j][v], r[j][v], i[j][v], rate_s[cl + v]);
+                if (fresh) s = {0.0f, amount_of(x[j][v], i[j][v])};
+                if (!live) s = {1.0f, 0.0f};
+                a[j][v] = s.a;
+                u[j][v] = s.u;
+                H[v] = fmaf(s.a, H[v], s.u);
+                A[v] *= s.a;
             }
         }
     }
-    // what the groups before this one do: composed over the groups of the wave, then shifted by one
+    // what the group before this one does, and the wave
     float A_before[V], H_before[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-#pragma unroll
-        for (int d = 8; d < kWave; d *= 2) {
-            const float pA = __shfl_up(A[v], d), pH = __shfl_up(H[v], d);
-            if (lane >= d) {
+        A_before[v] = 1.0f;
+        H_before[v] = 0.0f;
+        if constexpr (V == 2) {
+            const float pA = __shfl_xor(A[v], 32), pH = __shfl_xor(H[v], 32);
+            if (group == 1) {
+                A_before[v] = pA;
+                H_before[v] = pH;
                 H[v] = fmaf(A[v], pH, H[v]);
                 A[v] *= pA;
             }
         }
-        A_before[v] = __shfl_up(A[v], 8);
-        H_before[v] = __shfl_up(H[v], 8);
-        if (lane < 8) { A_before[v] = 1.0f; H_before[v] = 0.0f; }
-        if (lane >= kWave - 8) { A_s[wave][cl + v] = A[v]; H_s[wave][cl + v] = H[v]; }
+        if (group == V - 1) { A_s[wave][cl + v] = A[v]; H_s[wave][cl + v] = H[v]; }
     }
     lds_barrier();
     if (wave == 0) {
         const int ch = at.c0 + lane;
-        const bool mine = lane < CT && ch < p.C;
+        const bool mine = ch < p.C;
         float Aw = 1.0f, Hw = 0.0f;
-        if (mine)
-            for (int w = 0; w < NW; ++w) { Hw = fmaf(A_s[w][lane], Hw, H_s[w][lane]); Aw *= A_s[w][lane]; }
+        for (int w = 0; w < NW; ++w) { Hw = fmaf(A_s[w][lane], Hw, H_s[w][lane]); Aw *= A_s[w][lane]; }
         float h = 0.0f;
         if constexpr (CHAIN) {
-            const int64_t stride = (int64_t)p.sequences * CT;
-            Word *own = p.words + (int64_t)at.seq * CT + lane;
+            const int64_t stride = (int64_t)p.sequences * kChannels;
+            Word *own = p.words + (int64_t)at.seq * kChannels + lane;
             if (at.unit > 0) {
                 if (mine) publish(own + at.unit * stride, Aw, Hw);
                 h = look_back(own, at.unit - 1, stride, mine);
@@ -292,134 +355,121 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
         } else if (mine && p.h_first) {
             h = p.h_first[(int64_t)at.b * p.C + ch];
         }
-        if (mine) {
-            for (int w = 0; w < NW; ++w) {
-                carry_s[w][lane] = h;
-                const int t = first + w * 8 * Tc;
-                if (t < p.T && t % p.keep == 0) p.states[((int64_t)at.b * p.kept + t / p.keep) * p.C + ch] = h;
-                h = fmaf(A_s[w][lane], h, H_s[w][lane]);
-            }
-            if (p.h_last && at.unit == p.units - 1) p.h_last[(int64_t)at.b * p.C + ch] = h;
+        for (int w = 0; w < NW; ++w) {
+            carry_s[w][lane] = h;
+            const int t = first + w * kWaveSteps;
+            if (mine && t < p.T && (t & ((1 << p.keep_log) - 1)) == 0) p.states[((int64_t)at.b * p.kept + (t >> p.keep_log)) * p.C + ch] = h;
+            h = fmaf(A_s[w][lane], h, H_s[w][lane]);
         }
+        if (mine && p.h_last && at.unit == p.units - 1) p.h_last[(int64_t)at.b * p.C + ch] = h;
     }
     lds_barrier();
     if (left <= 0) return;
+    const Strip<E, PAIRS> sy(p.y, p.ld_y, row0, at.c0, cl, down);
     float h[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = fmaf(A_before[v], carry_s[wave][cl + v], H_before[v]);
 #pragma unroll
     for (int j = 0; j < Tc; ++j) {
-        if (kind[j] == kPast) continue;
-        Row<E, VEC> y;
+        Row<E, PAIRS> y;
+        float out[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             h[v] = fmaf(a[j][v], h[v], u[j][v]);
-            y.v[v] = from_f32<E>(kind[j] == kPadding ? 0.0f : h[v]);
+            out[v] = filled >> j & 1 ? h[v] : 0.0f;
         }
-        y.store(p.y, ((int64_t)at.b * p.T + t0 + j) * p.ld_y + c, left);
+        y.set(out);
+        if (steps.exist == (unsigned)kAll || (exist >> j & 1)) sy.store(y, j, left);
     }
 }
 
 // Backward pass.  D[t] = a[t] dL/dh[t] is what reaches h[t-1]: D[t] = a[t] (grad_y[t] + D[t+1]), the same kind of chain
 // backwards in time.  h is formed again inside the unit from the state kept at its start.
-template <typename E, bool VEC, int NW, bool CHAIN>
-__global__ __launch_bounds__(NW * kWave) void scan_grad_kernel(ScanArgs p)
+template <typename E, bool PAIRS, int NW, bool CHAIN>
+__global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
 {
-    constexpr int V = Span<E>::V, CT = Span<E>::CT, Tc = steps_of_lane<E>(true);
-    __shared__ float rate_s[CT], A_s[NW][CT], H_s[NW][CT], R_s[NW][CT], carry_s[NW][CT], after_s[NW][CT];
+    constexpr int V = kWide<E>, Tc = kStepsBack<E>, kWaveSteps = V * Tc, kAll = (1 << kWaveSteps) - 1;
+    __shared__ float rate_s[kChannels], A_s[NW][kChannels], H_s[NW][kChannels], R_s[NW][kChannels], carry_s[NW][kChannels], after_s[NW][kChannels];
     __shared__ int id_s;
-    const Place at = place_of<E, CHAIN>(p, &id_s);
+    const Place at = place_of<CHAIN>(p, &id_s);
     const int unit = p.units - 1 - at.unit;                    // the last steps first
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, group = lane / 8, cl = lane % 8 * V;
-    const int c = at.c0 + cl, left = p.C - c, t0 = unit * (NW * 8 * Tc) + (wave * 8 + group) * Tc;
-    Row<E, VEC> x[Tc], r[Tc], i[Tc], g[Tc];
-    Kind kind[Tc];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / (kWave / V), cl = lane % (kWave / V) * V;
+    const int c = at.c0 + cl, left = p.C - c, tw = (unit * NW + wave) * kWaveSteps;
+    const Steps steps = steps_at<kWaveSteps>(p, at.b, tw);
+    const unsigned exist = steps.exist >> (group * Tc), filled = steps.filled >> (group * Tc), start = steps.start >> (group * Tc);
+    const int64_t row0 = (int64_t)at.b * p.T + tw;
+    const int down = group * Tc;
+    Row<E, PAIRS> x[Tc], r[Tc], i[Tc], g[Tc];
+    if (steps.filled && left > 0) {
+        const Strip<E, PAIRS> sx(p.x, p.ld_x, row0, at.c0, cl, down), sr(p.r, p.ld_r, row0, at.c0, cl, down), si(p.i, p.ld_i, row0, at.c0, cl, down),
+            sg(p.grad_y, p.ld_gy, row0, at.c0, cl, down);
+        if (steps.exist == (unsigned)kAll) {
 #pragma unroll
-    for (int j = 0; j < Tc; ++j) {
-        kind[j] = left > 0 ? kind_of(p, at.b, t0 + j) : kPast;
-        if (kind[j] > kPadding) {
-            const int64_t row = (int64_t)at.b * p.T + t0 + j;
-            r[j].load(p.r, row * p.ld_r + c, left);
-            i[j].load(p.i, row * p.ld_i + c, left);
-            x[j].load(p.x, row * p.ld_x + c, left);
-            g[j].load(p.grad_y, row * p.ld_gy + c, left);
-        }
-    }
-    for (int k = threadIdx.x; k < CT; k += NW * kWave) rate_s[k] = at.c0 + k < p.C ? rate_of(p.lam[at.c0 + k], p.decay) : 0.0f;
-    lds_barrier();
-    Gates gate[Tc][V];
-    float u[Tc][V], A[V], H[V], R[V];
+            for (int j = 0; j < Tc; ++j) {
+                sr.load(r[j], j, left);
+                si.load(i[j], j, left);
+                sx.load(x[j], j, left);
+                sg.load(g[j], j, left);
+            }
+        } else {
 #pragma unroll
-    for (int v = 0; v < V; ++v) { A[v] = 1.0f; H[v] = 0.0f; R[v] = 0.0f; }
-#pragma unroll
-    for (int j = 0; j < Tc; ++j) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            gate[j][v].a = 1.0f;
-            u[j][v] = 0.0f;
-        }
-        if (kind[j] > kPadding) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                Gates &q = gate[j][v];
-                q = gates_of(to_f32(r[j].v[v]), to_f32(i[j].v[v]), rate_s[cl + v]);
-                if (kind[j] == kStart) { q.a = 0.0f; q.beta = 1.0f; q.inv_beta = 0.0f; }
-                u[j][v] = q.beta * q.si.s * to_f32(x[j].v[v]);
-                H[v] = fmaf(q.a, H[v], u[j][v]);
-                A[v] *= q.a;
+            for (int j = 0; j < Tc; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                sr.load_within(r[j], down + j, p.T - 1 - tw, left);
+                si.load_within(i[j], down + j, p.T - 1 - tw, left);
+                sx.load_within(x[j], down + j, p.T - 1 - tw, left);
+                sg.load_within(g[j], down + j, p.T - 1 - tw, left);
             }
         }
+    }
+    for (int k = threadIdx.x; k < kChannels; k += NW * kWave) rate_s[k] = at.c0 + k < p.C ? rate_of(p.lam[at.c0 + k], p.decay) : 0.0f;
+    lds_barrier();
+    StepBack q[Tc][V];
+    float A[V], H[V], R[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) { A[v] = 1.0f; H[v] = 0.0f; R[v] = 0.0f; }
+    const bool plain = steps.filled == (unsigned)kAll && steps.start == 0;
+#pragma unroll
+    for (int j = 0; j < Tc; ++j) {
+        const bool live = plain || (filled >> j & 1), fresh = !plain && (start >> j & 1);
+        __builtin_amdgcn_sched_barrier(0);             // a few steps at a time, or registers run out
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            q[j][v] = step_back_of(x[j][v], r[j][v], i[j][v], rate_s[cl + v], fresh);
+            if (!live) q[j][v] = {1.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            H[v] = fmaf(q[j][v].a, H[v], q[j][v].u);
+            A[v] *= q[j][v].a;
+        }
+        if (!live) g[j].bits = 0;
     }
 #pragma unroll
     for (int j = Tc - 1; j >= 0; --j)
-        if (kind[j] > kPadding)
 #pragma unroll
-            for (int v = 0; v < V; ++v) R[v] = gate[j][v].a * (to_f32(g[j].v[v]) + R[v]);
+        for (int v = 0; v < V; ++v) R[v] = q[j][v].a * (g[j][v] + R[v]);
     float A_before[V], H_before[V], A_after[V], R_after[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        float Af = A[v], Ab = A[v];
-#pragma unroll
-        for (int d = 8; d < kWave; d *= 2) {
-            const float pA = __shfl_up(Af, d), pH = __shfl_up(H[v], d), nA = __shfl_down(Ab, d), nR = __shfl_down(R[v], d);
-            if (lane >= d) {
-                H[v] = fmaf(Af, pH, H[v]);
-                Af *= pA;
-            }
-            if (lane < kWave - d) {
-                R[v] = fmaf(Ab, nR, R[v]);
-                Ab *= nA;
-            }
+        A_before[v] = A_after[v] = 1.0f;
+        H_before[v] = R_after[v] = 0.0f;
+        if constexpr (V == 2) {
+            const float oA = __shfl_xor(A[v], 32), oH = __shfl_xor(H[v], 32), oR = __shfl_xor(R[v], 32);
+            if (group == 1) { A_before[v] = oA; H_before[v] = oH; H[v] = fmaf(A[v], oH, H[v]); }
+            else { A_after[v] = oA; R_after[v] = oR; R[v] = fmaf(A[v], oR, R[v]); }
+            A[v] *= oA;
         }
-        A_before[v] = __shfl_up(Af, 8);
-        H_before[v] = __shfl_up(H[v], 8);
-        A_after[v] = __shfl_down(Ab, 8);
-        R_after[v] = __shfl_down(R[v], 8);
-        if (lane < 8) { A_before[v] = 1.0f; H_before[v] = 0.0f; }
-        if (lane >= kWave - 8) {
-            A_after[v] = 1.0f;
-            R_after[v] = 0.0f;
-            A_s[wave][cl + v] = Af;
-            H_s[wave][cl + v] = H[v];
-        }
-        if (lane < 8) R_s[wave][cl + v] = R[v];
+        if (group == V - 1) { A_s[wave][cl + v] = A[v]; H_s[wave][cl + v] = H[v]; }
+        if (group == 0) R_s[wave][cl + v] = R[v];
     }
     lds_barrier();
     if (wave == 0) {
         const int ch = at.c0 + lane;
-        const bool mine = lane < CT && ch < p.C;
+        const bool mine = ch < p.C;
+        float h = mine && p.T > 0 ? p.states[((int64_t)at.b * p.kept + unit) * p.C + ch] : 0.0f;
         float D = 0.0f, Aw = 1.0f, Rw = 0.0f;
-        if (mine) {
-            float h = p.T > 0 ? p.states[((int64_t)at.b * p.kept + unit) * p.C + ch] : 0.0f;
-            for (int w = 0; w < NW; ++w) {
-                carry_s[w][lane] = h;
-                h = fmaf(A_s[w][lane], h, H_s[w][lane]);
-            }
-            for (int w = NW - 1; w >= 0; --w) { Rw = fmaf(A_s[w][lane], Rw, R_s[w][lane]); Aw *= A_s[w][lane]; }
-        }
+        for (int w = NW - 1; w >= 0; --w) { Rw = fmaf(A_s[w][lane], Rw, R_s[w][lane]); Aw *= A_s[w][lane]; }
         if constexpr (CHAIN) {
-            const int64_t stride = (int64_t)p.sequences * CT;
-            Word *own = p.words + (int64_t)at.seq * CT + lane;
+            const int64_t stride = (int64_t)p.sequences * kChannels;
+            Word *own = p.words + (int64_t)at.seq * kChannels + lane;
             if (at.unit > 0) {
                 if (mine) publish(own + at.unit * stride, Aw, Rw);
                 D = look_back(own, at.unit - 1, stride, mine);
@@ -430,65 +480,63 @@ __global__ __launch_bounds__(NW * kWave) void scan_grad_kernel(ScanArgs p)
         } else if (mine && p.grad_h_last) {
             D = p.grad_h_last[(int64_t)at.b * p.C + ch];
         }
-        if (mine) {
-            for (int w = NW - 1; w >= 0; --w) {
-                after_s[w][lane] = D;
-                D = fmaf(A_s[w][lane], D, R_s[w][lane]);
-            }
-            if (p.grad_h_first && unit == 0) p.grad_h_first[(int64_t)at.b * p.C + ch] = D;
+        for (int w = 0; w < NW; ++w) {
+            carry_s[w][lane] = h;
+            h = fmaf(A_s[w][lane], h, H_s[w][lane]);
         }
+        for (int w = NW - 1; w >= 0; --w) {
+            after_s[w][lane] = D;
+            D = fmaf(A_s[w][lane], D, R_s[w][lane]);
+        }
+        if (mine && p.grad_h_first && unit == 0) p.grad_h_first[(int64_t)at.b * p.C + ch] = D;
     }
     lds_barrier();
-    float sum[V], before[Tc][V];
+    const Strip<E, PAIRS> sgx(p.grad_x, p.ld_gx, row0, at.c0, cl, down), sgr(p.grad_r, p.ld_gr, row0, at.c0, cl, down),
+        sgi(p.grad_i, p.ld_gi, row0, at.c0, cl, down);
+    float sum[V], D[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         sum[v] = 0.0f;
+        D[v] = fmaf(A_after[v], after_s[wave][cl + v], R_after[v]);
         float h = fmaf(A_before[v], carry_s[wave][cl + v], H_before[v]);
 #pragma unroll
         for (int j = 0; j < Tc; ++j) {
-            before[j][v] = h;
-            h = fmaf(gate[j][v].a, h, u[j][v]);
+            q[j][v].q = h - q[j][v].q;
+            h = fmaf(q[j][v].a, h, q[j][v].u);
         }
     }
-    float D[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) D[v] = fmaf(A_after[v], after_s[wave][cl + v], R_after[v]);
 #pragma unroll
     for (int j = Tc - 1; j >= 0; --j) {
-        if (kind[j] == kPast) continue;
-        Row<E, VEC> gx, gr, gi;
+        Row<E, PAIRS> gx, gr, gi;
+        float dx[V], dr[V], di[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            float dx = 0.0f, dr = 0.0f, di = 0.0f;
-            if (kind[j] != kPadding) {
-                const Gates &q = gate[j][v];
-                const float xv = to_f32(x[j].v[v]), dh = to_f32(g[j].v[v]) + D[v], du = dh * q.beta;
-                dx = du * q.si.s;
-                di = dx * xv * q.si.c;
-                D[v] = q.a * dh;
-                const float dL = D[v] * (before[j][v] - q.si.s * xv * q.a * q.inv_beta);       // (a = 0 at a sequence's start)
-                const float part = q.sr.s * dL;
-                dr = -rate_s[cl + v] * q.sr.c * part;
-                sum[v] -= part;
-            }
-            gx.v[v] = from_f32<E>(dx);
-            gr.v[v] = from_f32<E>(dr);
-            gi.v[v] = from_f32<E>(di);
+            const StepBack &k = q[j][v];
+            const float dh = g[j][v] + D[v];
+            dx[v] = dh * k.m;
+            di[v] = dh * k.n;
+            D[v] = k.a * dh;
+            const float part = k.s * (D[v] * k.q);
+            dr[v] = -k.w * part;
+            sum[v] -= part;
         }
-        const int64_t row = (int64_t)at.b * p.T + t0 + j;
-        gx.store(p.grad_x, row * p.ld_gx + c, left);
-        gr.store(p.grad_r, row * p.ld_gr + c, left);
-        gi.store(p.grad_i, row * p.ld_gi + c, left);
+        gx.set(dx);
+        gr.set(dr);
+        gi.set(di);
+        if ((steps.exist == (unsigned)kAll || (exist >> j & 1)) && left > 0) {
+            sgx.store(gx, j, left);
+            sgr.store(gr, j, left);
+            sgi.store(gi, j, left);
+        }
     }
     // the unit's part of the sum for lam: groups, then waves, in order
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-#pragma unroll
-        for (int d = 8; d < kWave; d *= 2) sum[v] += __shfl_xor(sum[v], d);
-        if (lane < 8) H_s[wave][cl + v] = sum[v];
+        if constexpr (V == 2) sum[v] += __shfl_xor(sum[v], 32);
+        if (group == 0) H_s[wave][cl + v] = sum[v];
     }
     lds_barrier();
-    for (int k = threadIdx.x; k < CT; k += NW * kWave) {
+    for (int k = threadIdx.x; k < kChannels; k += NW * kWave) {
         if (at.c0 + k >= p.C) continue;
         float total = 0.0f;
         for (int w = 0; w < NW; ++w) total += H_s[w][k];
@@ -496,18 +544,21 @@ __global__ __launch_bounds__(NW * kWave) void scan_grad_kernel(ScanArgs p)
     }
 }
 
-// grad_lam[c] = decay sigmoid(lam[c]) * sum of the units' parts: 16 runs of each channel side by side, then together, in order.
+// grad_lam[c] = decay sigmoid(lam[c]) * sum of the units' parts: 64 runs of each of 16 channels side by side, then together,
+// in order.
 __global__ __launch_bounds__(1024) void scan_lam_kernel(ScanArgs p, int64_t parts)
 {
-    __shared__ float run[16][kWave];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+    __shared__ float run[64][16 + 1];
+    const int k = threadIdx.x % 16, part = threadIdx.x / 16, c = blockIdx.x * 16 + k;
     float sum = 0.0f;
-    if (c < p.C)
-        for (int64_t k = wave; k < parts; k += 16) sum += p.lam_part[k * p.C + c];
-    run[wave][lane] = sum;
+    if (c < p.C) {
+#pragma unroll 4
+        for (int64_t at = part; at < parts; at += 64) sum += p.lam_part[at * p.C + c];
+    }
+    run[part][k] = sum;
     __syncthreads();
-    if (wave != 0 || c >= p.C) return;
-    for (int w = 1; w < 16; ++w) sum += run[w][lane];
+    if (part != 0 || c >= p.C) return;
+    for (int w = 1; w < 64; ++w) sum += run[w][k];
     p.grad_lam[c] = sum * p.decay * sigmoid2(p.lam[c]).s;
 }
 
@@ -533,10 +584,9 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs p)
     const int64_t row = id / p.C;
     const int c = (int)(id % p.C);
     const int64_t at = (int64_t)(p.slot ? min(max(p.slot[row], 0), p.slots - 1) : (int)row) * p.C + c;
-    const Gates g = gates_of(to_f32(static_cast<const E *>(p.r)[row * p.ld_r + c]),
-                             to_f32(static_cast<const E *>(p.i)[row * p.ld_i + c]), rate_of(p.lam[c], p.decay));
-    const float in = g.si.s * to_f32(static_cast<const E *>(p.x)[row * p.ld_x + c]);
-    const float h = p.reset && p.reset[row] ? in : fmaf(g.a, p.h_in[at], g.beta * in);
+    const float x = to_f32(static_cast<const E *>(p.x)[row * p.ld_x + c]), i = to_f32(static_cast<const E *>(p.i)[row * p.ld_i + c]);
+    const Step s = step_of(x, to_f32(static_cast<const E *>(p.r)[row * p.ld_r + c]), i, rate_of(p.lam[c], p.decay));
+    const float h = p.reset && p.reset[row] ? amount_of(x, i) : fmaf(s.a, p.h_in[at], s.u);
     p.h_out[at] = h;
     static_cast<E *>(p.y)[row * p.ld_y + c] = from_f32<E>(h);
 }
@@ -555,19 +605,19 @@ struct ScanPlan {
 
 ScanPlan scan_plan(int dtype, int B, int T, int C)
 {
-    const int V = 16 / element_bytes(dtype), CT = 8 * V, lane = kElements / V, lane_back = kElementsBack / V;
+    const int V = 4 / element_bytes(dtype), steps = V * kSteps, steps_back = 16;
     ScanPlan s{};
-    s.waves = waves_for(T, lane);
-    s.waves_back = waves_for(T, lane_back);
-    auto units = [&](int steps) { return T > 0 ? (T + steps - 1) / steps : 1; };
-    s.units = units(s.waves * 8 * lane);
-    s.units_back = units(s.waves_back * 8 * lane_back);
-    s.tiles = (C + CT - 1) / CT;
+    s.waves = waves_for(T, steps, kMostWaves);
+    s.waves_back = waves_for(T, steps_back, kMostWavesBack);
+    auto units = [&](int span) { return T > 0 ? (T + span - 1) / span : 1; };
+    s.units = units(s.waves * steps);
+    s.units_back = units(s.waves_back * steps_back);
+    s.tiles = (C + kChannels - 1) / kChannels;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
     s.states = take((size_t)B * s.units_back * C * sizeof(float));
     s.aside = take((size_t)B * C * sizeof(float));
-    s.n_words = s.units_back > 1 ? (int64_t)s.units_back * B * s.tiles * CT : 0;       // never fewer units than forward
+    s.n_words = s.units_back > 1 ? (int64_t)s.units_back * B * s.tiles * kChannels : 0;       // never fewer units than forward
     s.words = take((size_t)s.n_words * sizeof(Word));
     s.ticket = take(sizeof(unsigned));
     s.lam_part = take((size_t)B * s.units_back * C * sizeof(float));
@@ -590,12 +640,12 @@ int scan_check(int dtype, int B, int T, int C, float decay, const void *workspac
 
 unsigned blocks_of(int64_t n) { return (unsigned)((n + 255) / 256); }
 
-// Rows can be read 16 bytes at a time: everything is a multiple of 16 bytes apart.
-bool rows_of_sixteen(int dtype, int C, std::initializer_list<const void *> pointers, std::initializer_list<int64_t> strides)
+// Rows can be read four bytes at a time.
+bool rows_of_pairs(int dtype, int C, std::initializer_list<const void *> pointers, std::initializer_list<int64_t> strides)
 {
-    const int V = 16 / element_bytes(dtype);
+    const int V = 4 / element_bytes(dtype);
     bool ok = C % V == 0;
-    for (const void *p : pointers) ok = ok && aligned_to(p, 16);
+    for (const void *p : pointers) ok = ok && aligned_to(p, 4);
     for (int64_t ld : strides) ok = ok && ld % V == 0;
     return ok;
 }
@@ -608,22 +658,22 @@ int with_waves(int waves, F &&f)
     case 1: return f(std::integral_constant<int, 1>{});
     case 2: return f(std::integral_constant<int, 2>{});
     case 4: return f(std::integral_constant<int, 4>{});
-    default: return f(std::integral_constant<int, kMostWaves>{});
+    default: return f(std::integral_constant<int, 8>{});
     }
 }
 
-template <bool BACK, typename E, bool VEC, int NW, bool CHAIN>
+template <bool BACK, typename E, bool PAIRS, int NW, bool CHAIN>
 int launch_scan(const ScanArgs &p, hipStream_t stream)
 {
     const dim3 grid((unsigned)(p.units * p.sequences)), block(NW * kWave);
-    if constexpr (BACK) hipLaunchKernelGGL((scan_grad_kernel<E, VEC, NW, CHAIN>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((scan_kernel<E, VEC, NW, CHAIN>), grid, block, 0, stream, p);
+    if constexpr (BACK) hipLaunchKernelGGL((scan_grad_kernel<E, PAIRS, NW, CHAIN>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((scan_kernel<E, PAIRS, NW, CHAIN>), grid, block, 0, stream, p);
     return launched(BACK ? "linear scan gradient" : "linear scan");
 }
 
 // One workgroup per unit; with more than one unit in a sequence they hand the state on.
 template <bool BACK>
-int run_scan(int dtype, ScanArgs p, const ScanPlan &s, char *workspace, bool vec, hipStream_t stream)
+int run_scan(int dtype, ScanArgs p, const ScanPlan &s, char *workspace, bool pairs, hipStream_t stream)
 {
     p.tiles = s.tiles;
     if ((int64_t)p.B * s.tiles * (BACK ? s.units_back : s.units) >= ((int64_t)1 << 31)) return MARL_ERR_BAD_DIM;
@@ -631,24 +681,25 @@ int run_scan(int dtype, ScanArgs p, const ScanPlan &s, char *workspace, bool vec
     p.units = BACK ? s.units_back : s.units;
     p.states = reinterpret_cast<float *>(workspace + s.states);
     p.kept = s.units_back;
-    p.keep = s.waves_back * 8 * kElementsBack / (16 / element_bytes(dtype));
+    p.keep_log = __builtin_ctz(s.waves_back * 16);
     p.lam_part = reinterpret_cast<float *>(workspace + s.lam_part);
     p.words = reinterpret_cast<Word *>(workspace + s.words);
     p.ticket = reinterpret_cast<unsigned *>(workspace + s.ticket);
     if (p.units > 1) {
         float *aside = reinterpret_cast<float *>(workspace + s.aside);
-        const int64_t n_states = (int64_t)p.B * p.C, n_words = (int64_t)p.units * p.sequences * 128 / element_bytes(dtype);
+        const int64_t n_states = (int64_t)p.B * p.C, n_words = (int64_t)p.units * p.sequences * kChannels;
         hipLaunchKernelGGL(scan_begin_kernel, dim3(blocks_of(n_words > n_states ? n_words : n_states)), dim3(256), 0, stream, p.words, n_words, p.ticket,
                            BACK ? p.grad_h_last : p.h_first, aside, n_states);
         (BACK ? p.grad_h_last : p.h_first) = aside;
+        constexpr int kMost = BACK ? kMostWavesBack : kMostWaves;
         return with_dtype(dtype, [&](auto e) {
-            return vec ? launch_scan<BACK, decltype(e), true, kMostWaves, true>(p, stream) : launch_scan<BACK, decltype(e), false, kMostWaves, true>(p, stream);
+            return pairs ? launch_scan<BACK, decltype(e), true, kMost, true>(p, stream) : launch_scan<BACK, decltype(e), false, kMost, true>(p, stream);
         });
     }
     return with_dtype(dtype, [&](auto e) {
         return with_waves(BACK ? s.waves_back : s.waves, [&](auto waves) {
-            return vec ? launch_scan<BACK, decltype(e), true, decltype(waves)::value, false>(p, stream)
-                       : launch_scan<BACK, decltype(e), false, decltype(waves)::value, false>(p, stream);
+            return pairs ? launch_scan<BACK, decltype(e), true, decltype(waves)::value, false>(p, stream)
+                         : launch_scan<BACK, decltype(e), false, decltype(waves)::value, false>(p, stream);
         });
     });
 }
@@ -685,8 +736,8 @@ int marl_linear_scan(int32_t dtype, int32_t B, int32_t T, int32_t C, const void 
     p.x = x; p.r = r; p.i = i; p.ld_x = ld_x; p.ld_r = ld_r; p.ld_i = ld_i;
     p.lam = lam; p.decay = decay; p.reset = reset; p.filled = filled; p.h_first = h_first;
     p.y = y; p.ld_y = ld_y; p.h_last = h_last;
-    const bool vec = rows_of_sixteen(dtype, C, {x, r, i, y}, {ld_x, ld_r, ld_i, ld_y});
-    return run_scan<false>(dtype, p, scan_plan(dtype, B, T, C), static_cast<char *>(workspace), vec, static_cast<hipStream_t>(hip_stream));
+    const bool pairs = rows_of_pairs(dtype, C, {x, r, i, y}, {ld_x, ld_r, ld_i, ld_y});
+    return run_scan<false>(dtype, p, scan_plan(dtype, B, T, C), static_cast<char *>(workspace), pairs, static_cast<hipStream_t>(hip_stream));
 }
 
 int marl_linear_scan_grad(int32_t dtype, int32_t B, int32_t T, int32_t C, const void *x, int64_t ld_x, const void *r,
@@ -717,12 +768,12 @@ int marl_linear_scan_grad(int32_t dtype, int32_t B, int32_t T, int32_t C, const 
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const ScanPlan s = scan_plan(dtype, B, T, C);
     if (B > 0) {
-        const bool vec = rows_of_sixteen(dtype, C, {x, r, i, grad_y, grad_x, grad_r, grad_i}, {ld_x, ld_r, ld_i, ld_gy, ld_gx, ld_gr, ld_gi});
-        const int status = run_scan<true>(dtype, p, s, static_cast<char *>(workspace), vec, stream);
+        const bool pairs = rows_of_pairs(dtype, C, {x, r, i, grad_y, grad_x, grad_r, grad_i}, {ld_x, ld_r, ld_i, ld_gy, ld_gx, ld_gr, ld_gi});
+        const int status = run_scan<true>(dtype, p, s, static_cast<char *>(workspace), pairs, stream);
         if (status) return status;
         p.lam_part = reinterpret_cast<float *>(static_cast<char *>(workspace) + s.lam_part);
     }
-    hipLaunchKernelGGL(scan_lam_kernel, dim3((unsigned)((C + kWave - 1) / kWave)), dim3(1024), 0, stream, p, (int64_t)B * s.units_back);
+    hipLaunchKernelGGL(scan_lam_kernel, dim3((unsigned)((C + 15) / 16)), dim3(1024), 0, stream, p, (int64_t)B * s.units_back);
     return launched("linear scan gradient");
 }
 
