@@ -62,9 +62,12 @@ struct ScanArgs {
     float *grad_lam, *grad_h_first;
 };
 
+// decay log(1 + e^lam).  The rounding of 1 + e is undone by the quotient (Kahan): log(u) e / (u - 1) with u = 1 + e as rounded.
 __device__ __forceinline__ float rate_of(float lam, float decay)
 {
-    return decay * (lam > 20.0f ? lam : log1pf(expf(lam)));      // (above 20 the difference is below half a step)
+    const float e = __builtin_amdgcn_exp2f(kLog2e * lam), u = 1.0f + e, d = u - 1.0f;
+    const float soft = d == 0.0f ? e : __builtin_amdgcn_logf(u) * 0.69314718f * (e * __builtin_amdgcn_rcpf(d));
+    return decay * (lam > 20.0f ? lam : soft);                 // (above 20 the difference is below half a step)
 }
 
 // sigmoid(v) and its complement, each to fp32 accuracy at both ends.
@@ -76,37 +79,44 @@ __device__ __forceinline__ Sigmoid sigmoid2(float v)
     return {s, e * s};
 }
 
-// beta^2 = 1 - a^2 with a = exp(-x), x >= 0.  Near 0 the difference would cancel: there 2 a sinh(x) by its series, whose next
-// term is below 2^-26 of it.
-__device__ __forceinline__ float beta_square(float x, float a)
+// The decay of a step: a = 2^e with e = -log2(e) rate sigmoid(r) <= 0, and beta^2 = 1 - a^2.  Near 0 the difference would cancel:
+// there -2 a sinh(e ln 2) by its series up to the seventh power, whose next term is below 2^-26 of it.  `rate2` is -log2(e) rate.
+// `start` is 0, or -200 where a sequence starts: then a is 0 and beta 1.
+struct Decay { float a, om; };
+__device__ __forceinline__ Decay decay_of(float s_r, float rate2, float start)
 {
-    const float q = x * x;
-    float p = fmaf(q, 1.0f / 5040.0f, 1.0f / 120.0f);
-    p = fmaf(q, p, 1.0f / 6.0f);
-    p = fmaf(q, p, 1.0f);
-    const float near = (a + a) * (x * p);
-    return x < 0.5f ? near : fmaf(-a, a, 1.0f);
+    constexpr double l = 0.69314718055994530942, l3 = l * l * l, l5 = l3 * l * l, l7 = l5 * l * l;
+    const float e = fmaf(rate2, s_r, start), a = __builtin_amdgcn_exp2f(e), q = e * e;
+    float p = fmaf(q, (float)(-2.0 * l7 / 5040.0), (float)(-2.0 * l5 / 120.0));
+    p = fmaf(q, p, (float)(-2.0 * l3 / 6.0));
+    p = fmaf(q, p, (float)(-2.0 * l));
+    const float near = a * (e * p), far = fmaf(-a, a, 1.0f);
+    return {a, e > -0.72f ? near : far};
 }
 
 // What one step does forward: h -> a h + u.
 struct Step { float a, u; };
-__device__ __forceinline__ float amount_of(float x, float i) { return x * sigmoidf_fast(i); }
-__device__ __forceinline__ Step step_of(float x, float r, float i, float rate)
+__device__ __forceinline__ Step step_of(float x, float r, float i, float rate2, float start)
 {
-    const float d = rate * sigmoidf_fast(r), a = __builtin_amdgcn_exp2f(-kLog2e * d);
-    return {a, __builtin_amdgcn_sqrtf(beta_square(d, a)) * amount_of(x, i)};
+    const Decay d = decay_of(sigmoidf_fast(r), rate2, start);
+    return {d.a, __builtin_amdgcn_sqrtf(d.om) * (x * sigmoidf_fast(i))};
 }
 
-// And what its gradients need: dx = dh m, di = dh n, dL = a dh (h before - q), dr = -w s dL.
-struct StepBack { float a, u, q, m, n, s, w; };
-__device__ __forceinline__ StepBack step_back_of(float x, float r, float i, float rate, bool start)
+// And what its gradients need: dx = dh m, di = dh n, dL = a dh (h before - q), dr = -rate (1 - s) s dL.
+struct StepBack { float a, u, q, m, n, s; };
+__device__ __forceinline__ StepBack step_back_of(float x, float r, float i, float rate2, float start)
 {
-    const Sigmoid sr = sigmoid2(r), si = sigmoid2(i);
-    const float d = rate * sr.s, a = __builtin_amdgcn_exp2f(-kLog2e * d), om = beta_square(d, a);
-    const float inv = __builtin_amdgcn_rsqf(fmaxf(om, 1e-30f));        // a gate that is shut has om = 0: beta 0, and no infinity
-    const float m = start ? si.s : om * inv * si.s, u = m * x;
-    return {start ? 0.0f : a, u, start ? 0.0f : a * inv * (si.s * x), m, u * si.c, sr.s, rate * sr.c};
+    const Sigmoid si = sigmoid2(i);
+    const float s_r = sigmoidf_fast(r);
+    const Decay d = decay_of(s_r, rate2, start);
+    const float inv = __builtin_amdgcn_rsqf(fmaxf(d.om, 1e-30f));      // a gate that is shut has om = 0: beta 0, and no infinity
+    const float beta = d.om * inv, in = si.s * x, u = beta * in;
+    return {d.a, u, d.a * inv * in, beta * si.s, u * si.c, s_r};
 }
+
+// All bits or none, after bit j of `bits`.
+__device__ __forceinline__ uint32_t all_of(unsigned bits, int j) { return (uint32_t)((int)(bits << (31 - j)) >> 31); }
+__device__ __forceinline__ float start_of(unsigned start, int j) { return __uint_as_float(all_of(start, j) & 0xc3480000u); }
 
 // Four bytes of a row.  PAIRS: they lie at a multiple of four bytes and there is no odd channel at the end.
 // Held as one word: as a pair of 16-bit values the compiler gave each a register of its own wherever branches meet.
@@ -115,11 +125,20 @@ struct Row {
     static constexpr int V = kWide<E>;
     typedef E Vec __attribute__((ext_vector_type(V)));
     uint32_t bits;
-    __device__ __forceinline__ float operator[](int k) const
+    __device__ __forceinline__ void get(float (&f)[V]) const
     {
         uint32_t b = bits;
         asm("" : "+v"(b));
-        return to_f32(__builtin_bit_cast(Vec, b)[k]);
+        const Vec v = __builtin_bit_cast(Vec, b);
+#pragma unroll
+        for (int k = 0; k < V; ++k) f[k] = to_f32(v[k]);
+    }
+    // Without m the row is zeros; a gate's row is -infinity, a gate that is shut: the step does nothing to the state.
+    __device__ __forceinline__ void keep(uint32_t m) { bits &= m; }
+    __device__ __forceinline__ void keep_or_shut(uint32_t m)
+    {
+        constexpr uint32_t shut = sizeof(E) == 4 ? 0xff800000u : std::is_same<E, __bf16>::value ? 0xff80ff80u : 0xfc00fc00u;
+        bits = (bits & m) | (shut & ~m);
     }
     __device__ __forceinline__ void set(const float (&f)[V])
     {
@@ -143,7 +162,12 @@ struct Strip {
     __device__ __forceinline__ Strip(const void *p, int64_t ld, int64_t row, int c0, int cl, int rows_down)
         : base(static_cast<char *>(const_cast<void *>(p)) + (row * ld + c0) * (int)sizeof(E)), step(ld * (int)sizeof(E)),
           lane((uint32_t)rows_down * (uint32_t)step + (uint32_t)cl * (uint32_t)sizeof(E)), c(cl) {}
-    __device__ __forceinline__ void load(Row<E, PAIRS> &r, int j, int left) const { read(r, base + j * step + lane, left); }
+    // the row in hand, and on to the next one (in turn: all rows' addresses at once do not fit the scalar registers)
+    __device__ __forceinline__ void load(Row<E, PAIRS> &r, int left)
+    {
+        read(r, base + lane, left);
+        base += step;
+    }
     __device__ __forceinline__ void load_within(Row<E, PAIRS> &r, int t, int reach, int left) const
     {
         read(r, base + (int64_t)min(t, reach) * step + (uint32_t)c * (uint32_t)sizeof(E), left);
@@ -159,9 +183,9 @@ struct Strip {
             r.bits = __builtin_bit_cast(uint32_t, v);
         }
     }
-    __device__ __forceinline__ void store(const Row<E, PAIRS> &r, int j, int left) const
+    __device__ __forceinline__ void store(const Row<E, PAIRS> &r, int left) const
     {
-        char *at = base + j * step + lane;
+        char *at = base + lane;
         if constexpr (PAIRS) {
             *reinterpret_cast<uint32_t *>(at) = r.bits;
         } else {
@@ -198,9 +222,9 @@ __device__ __forceinline__ Word peek(const Word *at) { return __hip_atomic_load(
 // for anything, and (0, h) of the state behind them when they know it; A = 0 says that nothing before matters.  Walking
 // backwards from unit `before` over whichever is there, `stride` words apart, until A = 0; the first unit publishes (0, h) alone.  A unit
 // waits only for units whose tickets are lower, and they began before it: each wait ends.
+template <int kAtOnce>
 __device__ __forceinline__ float look_back(const Word *words, int before, int64_t stride, bool mine)
 {
-    constexpr int kAtOnce = 4;
     float A = 1.0f, H = 0.0f;
     bool open = mine;
     for (int k = before; k >= 0 && __any(open); k -= kAtOnce) {
@@ -265,13 +289,14 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
     const int down = group * Tc;
     Row<E, PAIRS> x[Tc], r[Tc], i[Tc];
     if (steps.filled && left > 0) {
-        const Strip<E, PAIRS> sx(p.x, p.ld_x, row0, at.c0, cl, down), sr(p.r, p.ld_r, row0, at.c0, cl, down), si(p.i, p.ld_i, row0, at.c0, cl, down);
+        Strip<E, PAIRS> sx(p.x, p.ld_x, row0, at.c0, cl, down), sr(p.r, p.ld_r, row0, at.c0, cl, down), si(p.i, p.ld_i, row0, at.c0, cl, down);
         if (steps.exist == (unsigned)kAll) {
 #pragma unroll
             for (int j = 0; j < Tc; ++j) {
-                sr.load(r[j], j, left);
-                si.load(i[j], j, left);
-                sx.load(x[j], j, left);
+                __builtin_amdgcn_sched_barrier(0);
+                sr.load(r[j], left);
+                si.load(i[j], left);
+                sx.load(x[j], left);
             }
         } else {
 #pragma unroll
@@ -285,37 +310,36 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
     }
     for (int k = threadIdx.x; k < kChannels; k += NW * kWave) rate_s[k] = at.c0 + k < p.C ? rate_of(p.lam[at.c0 + k], p.decay) : 0.0f;
     lds_barrier();
+    float rate2[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) rate2[v] = -kLog2e * rate_s[cl + v];
     float a[Tc][V], u[Tc][V], A[V], H[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
-    if (steps.filled == (unsigned)kAll && steps.start == 0) {
+    if (steps.filled != (unsigned)kAll) {
 #pragma unroll
         for (int j = 0; j < Tc; ++j) {
-            __builtin_amdgcn_sched_barrier(0);         // a few steps at a time, or registers run out
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const Step s = step_of(x[j][v], r[j][v], i[j][v], rate_s[cl + v]);
-                a[j][v] = s.a;
-                u[j][v] = s.u;
-                H[v] = fmaf(s.a, H[v], s.u);
-                A[v] *= s.a;
-            }
+            const uint32_t m = all_of(filled, j);
+            x[j].keep(m);
+            i[j].keep(m);
+            r[j].keep_or_shut(m);
         }
-    } else {
+    }
 #pragma unroll
-        for (int j = 0; j < Tc; ++j) {
-            const bool live = filled >> j & 1, fresh = start >> j & 1;
-            __builtin_amdgcn_sched_barrier(0);
+    for (int j = 0; j < Tc; ++j) {
+        __builtin_amdgcn_sched_barrier(0);                             // a step at a time, or registers run out
+        const float begins = start_of(start, j);
+        float xv[V], rv[V], iv[V];
+        x[j].get(xv);
+        r[j].get(rv);
+        i[j].get(iv);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                Step s = step_of(x[j][v], r[j][v], i[j][v], rate_s[cl + v]);
-                if (fresh) s = {0.0f, amount_of(x[j][v], i[j][v])};
-                if (!live) s = {1.0f, 0.0f};
-                a[j][v] = s.a;
-                u[j][v] = s.u;
-                H[v] = fmaf(s.a, H[v], s.u);
-                A[v] *= s.a;
-            }
+        for (int v = 0; v < V; ++v) {
+            const Step s = step_of(xv[v], rv[v], iv[v], rate2[v], begins);
+            a[j][v] = s.a;
+            u[j][v] = s.u;
+            H[v] = fmaf(s.a, H[v], s.u);
+            A[v] *= s.a;
         }
     }
     // what the group before this one does, and the wave
@@ -347,7 +371,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
             Word *own = p.words + (int64_t)at.seq * kChannels + lane;
             if (at.unit > 0) {
                 if (mine) publish(own + at.unit * stride, Aw, Hw);
-                h = look_back(own, at.unit - 1, stride, mine);
+                h = look_back<4>(own, at.unit - 1, stride, mine);
             } else if (mine) {
                 h = p.h_first[(int64_t)at.b * p.C + ch];
             }
@@ -365,22 +389,29 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
     }
     lds_barrier();
     if (left <= 0) return;
-    const Strip<E, PAIRS> sy(p.y, p.ld_y, row0, at.c0, cl, down);
     float h[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = fmaf(A_before[v], carry_s[wave][cl + v], H_before[v]);
+    Strip<E, PAIRS> sy(p.y, p.ld_y, row0, at.c0, cl, down);
+    auto put = [&](auto whole) {                               // whole: every step exists and counts
 #pragma unroll
-    for (int j = 0; j < Tc; ++j) {
-        Row<E, PAIRS> y;
-        float out[V];
+        for (int j = 0; j < Tc; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
+            Row<E, PAIRS> y;
+            float out[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            h[v] = fmaf(a[j][v], h[v], u[j][v]);
-            out[v] = filled >> j & 1 ? h[v] : 0.0f;
+            for (int v = 0; v < V; ++v) {
+                h[v] = fmaf(a[j][v], h[v], u[j][v]);
+                out[v] = h[v];
+            }
+            y.set(out);
+            if (!whole) y.keep(all_of(filled, j));
+            if (whole || (exist >> j & 1)) sy.store(y, left);
+            sy.base += sy.step;
         }
-        y.set(out);
-        if (steps.exist == (unsigned)kAll || (exist >> j & 1)) sy.store(y, j, left);
-    }
+    };
+    if (steps.filled == (unsigned)kAll) put(std::true_type{});
+    else put(std::false_type{});
 }
 
 // Backward pass.  D[t] = a[t] dL/dh[t] is what reaches h[t-1]: D[t] = a[t] (grad_y[t] + D[t+1]), the same kind of chain
@@ -401,15 +432,16 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
     const int down = group * Tc;
     Row<E, PAIRS> x[Tc], r[Tc], i[Tc], g[Tc];
     if (steps.filled && left > 0) {
-        const Strip<E, PAIRS> sx(p.x, p.ld_x, row0, at.c0, cl, down), sr(p.r, p.ld_r, row0, at.c0, cl, down), si(p.i, p.ld_i, row0, at.c0, cl, down),
+        Strip<E, PAIRS> sx(p.x, p.ld_x, row0, at.c0, cl, down), sr(p.r, p.ld_r, row0, at.c0, cl, down), si(p.i, p.ld_i, row0, at.c0, cl, down),
             sg(p.grad_y, p.ld_gy, row0, at.c0, cl, down);
         if (steps.exist == (unsigned)kAll) {
 #pragma unroll
             for (int j = 0; j < Tc; ++j) {
-                sr.load(r[j], j, left);
-                si.load(i[j], j, left);
-                sx.load(x[j], j, left);
-                sg.load(g[j], j, left);
+                __builtin_amdgcn_sched_barrier(0);
+                sr.load(r[j], left);
+                si.load(i[j], left);
+                sx.load(x[j], left);
+                sg.load(g[j], left);
             }
         } else {
 #pragma unroll
@@ -424,28 +456,45 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
     }
     for (int k = threadIdx.x; k < kChannels; k += NW * kWave) rate_s[k] = at.c0 + k < p.C ? rate_of(p.lam[at.c0 + k], p.decay) : 0.0f;
     lds_barrier();
+    float rate[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) rate[v] = rate_s[cl + v];
     StepBack q[Tc][V];
     float A[V], H[V], R[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) { A[v] = 1.0f; H[v] = 0.0f; R[v] = 0.0f; }
-    const bool plain = steps.filled == (unsigned)kAll && steps.start == 0;
+    if (steps.filled != (unsigned)kAll) {
+#pragma unroll
+        for (int j = 0; j < Tc; ++j) {
+            const uint32_t m = all_of(filled, j);
+            x[j].keep(m);
+            i[j].keep(m);
+            g[j].keep(m);
+            r[j].keep_or_shut(m);
+        }
+    }
 #pragma unroll
     for (int j = 0; j < Tc; ++j) {
-        const bool live = plain || (filled >> j & 1), fresh = !plain && (start >> j & 1);
-        __builtin_amdgcn_sched_barrier(0);             // a few steps at a time, or registers run out
+        __builtin_amdgcn_sched_barrier(0);                             // a step at a time, or registers run out
+        const float begins = start_of(start, j);
+        float xv[V], rv[V], iv[V];
+        x[j].get(xv);
+        r[j].get(rv);
+        i[j].get(iv);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            q[j][v] = step_back_of(x[j][v], r[j][v], i[j][v], rate_s[cl + v], fresh);
-            if (!live) q[j][v] = {1.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            q[j][v] = step_back_of(xv[v], rv[v], iv[v], -kLog2e * rate[v], begins);
             H[v] = fmaf(q[j][v].a, H[v], q[j][v].u);
             A[v] *= q[j][v].a;
         }
-        if (!live) g[j].bits = 0;
     }
 #pragma unroll
-    for (int j = Tc - 1; j >= 0; --j)
+    for (int j = Tc - 1; j >= 0; --j) {
+        float gv[V];
+        g[j].get(gv);
 #pragma unroll
-        for (int v = 0; v < V; ++v) R[v] = q[j][v].a * (g[j][v] + R[v]);
+        for (int v = 0; v < V; ++v) R[v] = q[j][v].a * (gv[v] + R[v]);
+    }
     float A_before[V], H_before[V], A_after[V], R_after[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -466,13 +515,14 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
         const bool mine = ch < p.C;
         float h = mine && p.T > 0 ? p.states[((int64_t)at.b * p.kept + unit) * p.C + ch] : 0.0f;
         float D = 0.0f, Aw = 1.0f, Rw = 0.0f;
+#pragma unroll 1
         for (int w = NW - 1; w >= 0; --w) { Rw = fmaf(A_s[w][lane], Rw, R_s[w][lane]); Aw *= A_s[w][lane]; }
         if constexpr (CHAIN) {
             const int64_t stride = (int64_t)p.sequences * kChannels;
             Word *own = p.words + (int64_t)at.seq * kChannels + lane;
             if (at.unit > 0) {
                 if (mine) publish(own + at.unit * stride, Aw, Rw);
-                D = look_back(own, at.unit - 1, stride, mine);
+                D = look_back<1>(own, at.unit - 1, stride, mine);
             } else if (mine) {
                 D = p.grad_h_last[(int64_t)at.b * p.C + ch];
             }
@@ -480,10 +530,12 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
         } else if (mine && p.grad_h_last) {
             D = p.grad_h_last[(int64_t)at.b * p.C + ch];
         }
+#pragma unroll 1
         for (int w = 0; w < NW; ++w) {
             carry_s[w][lane] = h;
             h = fmaf(A_s[w][lane], h, H_s[w][lane]);
         }
+#pragma unroll 1
         for (int w = NW - 1; w >= 0; --w) {
             after_s[w][lane] = D;
             D = fmaf(A_s[w][lane], D, R_s[w][lane]);
@@ -491,8 +543,6 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
         if (mine && p.grad_h_first && unit == 0) p.grad_h_first[(int64_t)at.b * p.C + ch] = D;
     }
     lds_barrier();
-    const Strip<E, PAIRS> sgx(p.grad_x, p.ld_gx, row0, at.c0, cl, down), sgr(p.grad_r, p.ld_gr, row0, at.c0, cl, down),
-        sgi(p.grad_i, p.ld_gi, row0, at.c0, cl, down);
     float sum[V], D[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -505,30 +555,42 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
             h = fmaf(q[j][v].a, h, q[j][v].u);
         }
     }
+    const int64_t last = row0 + Tc - 1;                        // (of group 0)
+    Strip<E, PAIRS> sgx(p.grad_x, p.ld_gx, last, at.c0, cl, down), sgr(p.grad_r, p.ld_gr, last, at.c0, cl, down),
+        sgi(p.grad_i, p.ld_gi, last, at.c0, cl, down);
+    auto put = [&](auto whole) {                               // whole: every step exists and counts
 #pragma unroll
-    for (int j = Tc - 1; j >= 0; --j) {
-        Row<E, PAIRS> gx, gr, gi;
-        float dx[V], dr[V], di[V];
+        for (int j = Tc - 1; j >= 0; --j) {
+            __builtin_amdgcn_sched_barrier(0);
+            Row<E, PAIRS> gx, gr, gi;
+            float gv[V], dx[V], dr[V], di[V];
+            g[j].get(gv);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const StepBack &k = q[j][v];
-            const float dh = g[j][v] + D[v];
-            dx[v] = dh * k.m;
-            di[v] = dh * k.n;
-            D[v] = k.a * dh;
-            const float part = k.s * (D[v] * k.q);
-            dr[v] = -k.w * part;
-            sum[v] -= part;
+            for (int v = 0; v < V; ++v) {
+                const StepBack &k = q[j][v];
+                const float dh = gv[v] + D[v];
+                dx[v] = dh * k.m;
+                di[v] = dh * k.n;
+                D[v] = k.a * dh;
+                const float part = k.s * (D[v] * k.q);
+                dr[v] = -rate[v] * fmaf(-k.s, part, part);
+                sum[v] -= part;
+            }
+            gx.set(dx);
+            gr.set(dr);
+            gi.set(di);
+            if (left > 0 && (whole || (exist >> j & 1))) {
+                sgx.store(gx, left);
+                sgr.store(gr, left);
+                sgi.store(gi, left);
+            }
+            sgx.base -= sgx.step;
+            sgr.base -= sgr.step;
+            sgi.base -= sgi.step;
         }
-        gx.set(dx);
-        gr.set(dr);
-        gi.set(di);
-        if ((steps.exist == (unsigned)kAll || (exist >> j & 1)) && left > 0) {
-            sgx.store(gx, j, left);
-            sgr.store(gr, j, left);
-            sgi.store(gi, j, left);
-        }
-    }
+    };
+    if (steps.filled == (unsigned)kAll) put(std::true_type{});
+    else put(std::false_type{});
     // the unit's part of the sum for lam: groups, then waves, in order
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -585,8 +647,9 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs p)
     const int c = (int)(id % p.C);
     const int64_t at = (int64_t)(p.slot ? min(max(p.slot[row], 0), p.slots - 1) : (int)row) * p.C + c;
     const float x = to_f32(static_cast<const E *>(p.x)[row * p.ld_x + c]), i = to_f32(static_cast<const E *>(p.i)[row * p.ld_i + c]);
-    const Step s = step_of(x, to_f32(static_cast<const E *>(p.r)[row * p.ld_r + c]), i, rate_of(p.lam[c], p.decay));
-    const float h = p.reset && p.reset[row] ? amount_of(x, i) : fmaf(s.a, p.h_in[at], s.u);
+    const bool start = p.reset && p.reset[row];
+    const Step s = step_of(x, to_f32(static_cast<const E *>(p.r)[row * p.ld_r + c]), i, -kLog2e * rate_of(p.lam[c], p.decay), start ? -200.0f : 0.0f);
+    const float h = start ? s.u : fmaf(s.a, p.h_in[at], s.u);
     p.h_out[at] = h;
     static_cast<E *>(p.y)[row * p.ld_y + c] = from_f32<E>(h);
 }
