@@ -2,6 +2,7 @@
 // an orthogonalised momentum.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "muon_product.h"
@@ -19,12 +20,13 @@ struct UpdateArgs {
     int nesterov;
     float keep, rate;                  // weights_out = keep weights - rate X
     float eps;
-    double *part;                      // [L][kNormBlocks] sums of squares
+    double *part;                      // [L][kNormBlocks] sums of squares, `parts` of them in use
+    int parts;
     _Float16 *Q, *Q_lo;                // planes in the matrix's own order; Q_lo, T_lo: PL = 1, may be NULL
     _Float16 *T, *T_lo;                // and transposed
 };
 
-constexpr int kNormBlocks = 128;
+constexpr int kNormBlocks = 1024;                  // at most, workgroups of a matrix in the first pass
 
 template <typename E>
 __device__ __forceinline__ float momentum_of(const UpdateArgs &p, size_t at)
@@ -35,17 +37,60 @@ __device__ __forceinline__ float momentum_of(const UpdateArgs &p, size_t at)
     return p.nesterov ? fmaf(p.beta, m, g) : m;
 }
 
+// Four entries of a row at a time where they lie at a multiple of their size (FOURS), else one.
+template <typename T, bool FOURS>
+struct Entries {
+    static constexpr int N = FOURS ? 4 : 1;
+    typedef T Vec __attribute__((ext_vector_type(4)));
+    float v[N];
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (FOURS) {
+            const Vec w = *reinterpret_cast<const Vec *>(p);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = to_f32(w[k]);
+        } else {
+            v[0] = to_f32(*p);
+        }
+    }
+    __device__ __forceinline__ void store(T *p) const
+    {
+        if constexpr (FOURS) {
+            Vec w;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = from_f32<T>(v[k]);
+            *reinterpret_cast<Vec *>(p) = w;
+        } else {
+            *p = from_f32<T>(v[0]);
+        }
+    }
+};
+
 // The new momentum, and the sum of squares of what is to be orthogonalised (fp64: squares of fp32 do not overflow there).
-template <typename E>
+template <typename E, bool FOURS>
 __global__ __launch_bounds__(256) void momentum_kernel(UpdateArgs p)
 {
+    typedef Entries<E, FOURS> Grad;
+    constexpr int N = Grad::N;
     __shared__ double part[256 / kWave];
     const size_t n = (size_t)p.rows * p.cols, base = blockIdx.y * n;
     double sum = 0.0;
-    for (size_t k = (size_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (size_t)kNormBlocks * 256) {
-        if (p.momentum) p.momentum_out[base + k] = fmaf(p.beta, p.momentum[base + k], to_f32(static_cast<const E *>(p.grad)[base + k]));
-        const float u = momentum_of<E>(p, base + k);
-        sum += (double)u * u;
+#pragma unroll 4
+    for (size_t k = ((size_t)blockIdx.x * 256 + threadIdx.x) * N; k < n; k += (size_t)gridDim.x * 256 * N) {
+        Grad u;
+        u.load(static_cast<const E *>(p.grad) + base + k);
+        if (p.momentum) {
+            Entries<float, FOURS> m;
+            m.load(p.momentum + base + k);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                m.v[e] = fmaf(p.beta, m.v[e], u.v[e]);
+                u.v[e] = p.nesterov ? fmaf(p.beta, m.v[e], u.v[e]) : m.v[e];
+            }
+            m.store(p.momentum_out + base + k);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum += (double)u.v[e] * u.v[e];
     }
     for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
     if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = sum;
@@ -53,12 +98,16 @@ __global__ __launch_bounds__(256) void momentum_kernel(UpdateArgs p)
     if (threadIdx.x == 0) p.part[(size_t)blockIdx.y * kNormBlocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// 1 / max(norm, eps), times the planes' scale, by the first wave's sum in fixed order.
-__device__ __forceinline__ double inverse_norm(const UpdateArgs &p, int batch)
+// 1 / max(norm, eps), times the planes' scale: the parts in fixed order, by a workgroup of 256.
+__device__ __forceinline__ double inverse_norm(const UpdateArgs &p, int batch, double *shared)
 {
     const double *part = p.part + (size_t)batch * kNormBlocks;
-    double sum = part[threadIdx.x % kWave] + part[threadIdx.x % kWave + kWave];
+    double sum = 0.0;
+    for (int k = threadIdx.x; k < p.parts; k += 256) sum += part[k];
     for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
+    if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = sum;
+    __syncthreads();
+    sum = (shared[0] + shared[1]) + (shared[2] + shared[3]);
     return (double)kPlaneScale / fmax(sqrt(sum), (double)p.eps);
 }
 
@@ -69,7 +118,8 @@ __global__ __launch_bounds__(256) void planes_kernel(UpdateArgs p)
     __shared__ float tile[64][65];
     const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
     const size_t n = (size_t)p.rows * p.cols, base = blockIdx.z * n, padded = (size_t)p.rows_p * p.cols_p * PL * blockIdx.z;
-    const double factor = inverse_norm(p, blockIdx.z);
+    __shared__ double shared[256 / kWave];
+    const double factor = inverse_norm(p, blockIdx.z, shared);
     for (int k = threadIdx.x; k < 64 * 64; k += 256) {
         const int r = r0 + k / 64, c = c0 + k % 64;
         tile[k / 64][k % 64] = r < p.rows && c < p.cols ? (float)(factor * momentum_of<E>(p, base + (size_t)r * p.cols + c)) : 0.0f;
@@ -98,17 +148,26 @@ __global__ __launch_bounds__(256) void planes_kernel(UpdateArgs p)
     }
 }
 
-template <typename E, int PL>
+template <typename E, int PL, bool FOURS>
 __global__ __launch_bounds__(256) void finish_kernel(UpdateArgs p)
 {
-    const size_t n = (size_t)p.rows * p.cols, k = (size_t)blockIdx.x * 256 + threadIdx.x, base = blockIdx.y * n;
-    if (k >= n) return;
-    const size_t r = k / p.cols, padded = (size_t)p.rows_p * p.cols_p * PL * blockIdx.y;
-    const int c = (int)(k % p.cols);
-    const size_t at = padded + r * p.cols_p * PL + plane_at<PL>(c);
-    const float x = ((float)p.Q[at] + (float)(PL == 2 ? p.Q[at + 32] : p.Q_lo[at])) * (1.0f / kPlaneScale);
-    E *out = static_cast<E *>(p.weights_out) + base + k;
-    *out = from_f32<E>(p.weights ? p.keep * to_f32(static_cast<const E *>(p.weights)[base + k]) - p.rate * x : x);
+    constexpr int N = FOURS ? 4 : 1;
+    const size_t n = (size_t)p.rows * p.cols, base = blockIdx.y * n, padded = (size_t)p.rows_p * p.cols_p * PL * blockIdx.y;
+    for (size_t k = ((size_t)blockIdx.x * 256 + threadIdx.x) * N; k < n; k += (size_t)gridDim.x * 256 * N) {
+        const int r = (int)(k / p.cols), c = (int)(k % p.cols);        // FOURS: rows are multiples of four
+        const size_t at = padded + (size_t)r * p.cols_p * PL + plane_at<PL>(c);
+        Entries<_Float16, FOURS> h, l;
+        h.load(p.Q + at);
+        l.load(PL == 2 ? p.Q + at + 32 : p.Q_lo + at);
+        Entries<E, FOURS> w;
+        if (p.weights) w.load(static_cast<const E *>(p.weights) + base + k);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float x = (h.v[e] + l.v[e]) * (1.0f / kPlaneScale);
+            w.v[e] = p.weights ? p.keep * w.v[e] - p.rate * x : x;
+        }
+        w.store(static_cast<E *>(p.weights_out) + base + k);
+    }
 }
 
 bool sizes_ok(int L, int rows, int cols) { return L >= 0 && L <= 65535 && rows >= 1 && cols >= 1 && rows <= 32768 && cols <= 32768; }
@@ -210,7 +269,14 @@ int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, co
     p.part = reinterpret_cast<double *>(workspace + y.part);
     p.Q = tall ? T[0] : X[0]; p.Q_lo = tall ? T_lo[0] : X_lo[0];
     p.T = tall ? X[0] : T[0]; p.T_lo = tall ? X_lo[0] : T_lo[0];
-    hipLaunchKernelGGL((momentum_kernel<E>), dim3(kNormBlocks, (unsigned)L), dim3(256), 0, stream, p);
+    const size_t n = (size_t)p.rows * p.cols;
+    const bool fours = p.cols % 4 == 0 && aligned_to(p.grad, 4 * sizeof(E)) && aligned_to(p.weights, 4 * sizeof(E)) &&
+                       aligned_to(p.weights_out, 4 * sizeof(E)) && aligned_to(p.momentum, 16) && aligned_to(p.momentum_out, 16);
+    // four entries a thread and turn, four turns; the passes over the entries are bound by their bytes
+    const unsigned blocks = (unsigned)std::min<size_t>(kNormBlocks, (n + 256 * 16 - 1) / (256 * 16));
+    p.parts = (int)blocks;
+    if (fours) hipLaunchKernelGGL((momentum_kernel<E, true>), dim3(blocks, (unsigned)L), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((momentum_kernel<E, false>), dim3(blocks, (unsigned)L), dim3(256), 0, stream, p);
     hipLaunchKernelGGL((planes_kernel<E, PL>), dim3((unsigned)(y.cols_p / 64), (unsigned)(y.rows_p / 64), (unsigned)L), dim3(256), 0, stream, p);
     const int64_t square = (int64_t)y.s_p * y.s_p * PL, whole = (int64_t)y.s_p * y.l_p * PL;
     int now = 0;
@@ -245,8 +311,9 @@ int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, co
         now ^= 1;
     }
     p.Q = tall ? T[now] : X[now]; p.Q_lo = tall ? T_lo[now] : X_lo[now];
-    const size_t n = (size_t)p.rows * p.cols;
-    hipLaunchKernelGGL((finish_kernel<E, PL>), dim3((unsigned)((n + 255) / 256), (unsigned)L), dim3(256), 0, stream, p);
+    const dim3 each((unsigned)std::min<size_t>((n + 1023) / 1024, 4096), (unsigned)L);
+    if (fours) hipLaunchKernelGGL((finish_kernel<E, PL, true>), each, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((finish_kernel<E, PL, false>), each, dim3(256), 0, stream, p);
     return launched("orthogonalised update");
 }
 
