@@ -148,6 +148,7 @@ __global__ __launch_bounds__(256) void planes_kernel(UpdateArgs p)
     }
 }
 
+// The update by X as it started: no step at all.  (Otherwise the last product writes the matrix.)
 template <typename E, int PL, bool FOURS>
 __global__ __launch_bounds__(256) void finish_kernel(UpdateArgs p)
 {
@@ -196,7 +197,7 @@ Plan plan_of(int L, int Mp, int Np, bool symmetric, int stages)
 
 struct Layout {
     int rows_p, cols_p, s, l, s_p, l_p, planes;
-    size_t x[2], t[2], x_lo[2], t_lo[2], g, p, part, bytes;
+    size_t x[2], t[2], x_lo[2], g, p, part, bytes;
 };
 
 Layout layout_of(int dtype, int L, int rows, int cols)
@@ -214,7 +215,6 @@ Layout layout_of(int dtype, int L, int rows, int cols)
         y.x[k] = take(n * y.planes);
         y.t[k] = take(n * y.planes);
         y.x_lo[k] = y.planes == 1 ? take(n) : 0;
-        y.t_lo[k] = y.planes == 1 ? take(n) : 0;
     }
     y.g = take(square);
     y.p = take(square);
@@ -223,7 +223,7 @@ Layout layout_of(int dtype, int L, int rows, int cols)
     return y;
 }
 
-template <class S>
+template <class S, typename E>
 int launch_product(Product p, int L, hipStream_t stream)
 {
     static_assert(S::kLds <= 160 * 1024, "");
@@ -231,25 +231,25 @@ int launch_product(Product p, int L, hipStream_t stream)
     p.tiles_n = (p.Np + S::TN - 1) / S::TN;
     p.tiles = p.symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
     if constexpr (S::kLds > 64 * 1024) {
-        for (const void *k : {reinterpret_cast<const void *>(product_kernel<S>), reinterpret_cast<const void *>(join_kernel<S>)}) {
+        for (const void *k : {reinterpret_cast<const void *>(product_kernel<S, E>), reinterpret_cast<const void *>(join_kernel<S, E>)}) {
             const hipError_t err = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
             if (err != hipSuccess) return report_device_error(err, "hipFuncSetAttribute");
         }
     }
-    hipLaunchKernelGGL((product_kernel<S>), dim3((unsigned)(p.tiles * p.splits), (unsigned)L), dim3(S::kThreads), S::kLds, stream, p);
-    if (p.splits > 1) hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)p.tiles, (unsigned)L), dim3(S::kThreads), S::kLds, stream, p);
+    hipLaunchKernelGGL((product_kernel<S, E>), dim3((unsigned)(p.tiles * p.splits), (unsigned)L), dim3(S::kThreads), S::kLds, stream, p);
+    if (p.splits > 1) hipLaunchKernelGGL((join_kernel<S, E>), dim3((unsigned)p.tiles, (unsigned)L), dim3(S::kThreads), S::kLds, stream, p);
     return MARL_OK;
 }
 
-template <int PL>
+template <int PL, typename E>
 int product(Product p, int L, hipStream_t stream)
 {
     const Plan plan = plan_of(L, p.Mp, p.Np, p.symmetric, p.stages);
     p.splits = plan.splits;
     switch (plan.shape) {
-    case 0: return launch_product<TileShape<PL, 2, 4, 4, 2>>(p, L, stream);
-    case 1: return launch_product<TileShape<PL, 2, 2, 2, 2>>(p, L, stream);
-    default: return launch_product<TileShape<PL, 2, 2, 1, 1>>(p, L, stream);
+    case 0: return launch_product<TileShape<PL, 2, 4, 4, 2>, E>(p, L, stream);
+    case 1: return launch_product<TileShape<PL, 2, 2, 2, 2>, E>(p, L, stream);
+    default: return launch_product<TileShape<PL, 2, 2, 1, 1>, E>(p, L, stream);
     }
 }
 
@@ -258,17 +258,16 @@ int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, co
 {
     auto at = [&](size_t offset) { return reinterpret_cast<_Float16 *>(workspace + offset); };
     const bool tall = p.rows > p.cols;
-    _Float16 *X[2], *T[2], *X_lo[2], *T_lo[2];       // X [s][l] and its transpose
+    _Float16 *X[2], *T[2], *X_lo[2];                 // X [s][l] and its transpose
     for (int k = 0; k < 2; ++k) {
         X[k] = at(y.x[k]);
         T[k] = at(y.t[k]);
         X_lo[k] = PL == 1 ? at(y.x_lo[k]) : nullptr;
-        T_lo[k] = PL == 1 ? at(y.t_lo[k]) : nullptr;
     }
     p.rows_p = y.rows_p; p.cols_p = y.cols_p;
     p.part = reinterpret_cast<double *>(workspace + y.part);
-    p.Q = tall ? T[0] : X[0]; p.Q_lo = tall ? T_lo[0] : X_lo[0];
-    p.T = tall ? X[0] : T[0]; p.T_lo = tall ? X_lo[0] : T_lo[0];
+    p.Q = tall ? T[0] : X[0]; p.Q_lo = tall && steps > 0 ? nullptr : X_lo[0];      // (without a step it is finish_kernel that reads lo)
+    p.T = tall ? X[0] : T[0]; p.T_lo = tall && steps > 0 ? X_lo[0] : nullptr;
     const size_t n = (size_t)p.rows * p.cols;
     const bool fours = p.cols % 4 == 0 && aligned_to(p.grad, 4 * sizeof(E)) && aligned_to(p.weights, 4 * sizeof(E)) &&
                        aligned_to(p.weights_out, 4 * sizeof(E)) && aligned_to(p.momentum, 16) && aligned_to(p.momentum_out, 16);
@@ -281,14 +280,13 @@ int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, co
     const int64_t square = (int64_t)y.s_p * y.s_p * PL, whole = (int64_t)y.s_p * y.l_p * PL;
     int now = 0;
     for (int k = 0; k < steps; ++k) {
-        const bool last = k + 1 == steps;
         Product g{};
         g.A = g.B = X[now]; g.a_batch = g.b_batch = whole; g.lda = g.ldb = (int64_t)y.l_p * PL;
         g.Mp = g.Np = y.s_p; g.stages = y.l_p * PL / 64;
         g.alpha = 1.0f / kPlaneScale;
         g.Dt = g.D = at(y.g); g.ldt = g.ldd = (int64_t)y.s_p * PL; g.t_batch = g.d_batch = square;
         g.symmetric = 1;
-        int rc = product<PL>(g, L, stream);
+        int rc = product<PL, E>(g, L, stream);
         if (rc) return rc;
         Product q = g;
         q.A = q.B = at(y.g); q.a_batch = q.b_batch = square; q.lda = q.ldb = (int64_t)y.s_p * PL;
@@ -296,7 +294,7 @@ int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, co
         q.alpha = coef[2] / kPlaneScale; q.beta = coef[1];
         q.C = at(y.g);
         q.Dt = q.D = at(y.p);
-        rc = product<PL>(q, L, stream);
+        rc = product<PL, E>(q, L, stream);
         if (rc) return rc;
         Product x{};                                   // D [l][s] = X^T P, so D's transpose is the new X
         x.A = T[now]; x.a_batch = whole; x.lda = (int64_t)y.s_p * PL;
@@ -305,15 +303,20 @@ int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, co
         x.alpha = 1.0f / kPlaneScale; x.beta = coef[0];
         x.C = X[now]; x.C_lo = X_lo[now];
         x.Dt = X[now ^ 1]; x.Dt_lo = X_lo[now ^ 1]; x.ldt = (int64_t)y.l_p * PL; x.t_batch = whole;
-        x.D = T[now ^ 1]; x.D_lo = last && tall ? T_lo[now ^ 1] : nullptr; x.ldd = (int64_t)y.s_p * PL; x.d_batch = whole;
-        rc = product<PL>(x, L, stream);
+        x.D = T[now ^ 1]; x.ldd = (int64_t)y.s_p * PL; x.d_batch = whole;
+        if (k + 1 == steps) {
+            x.out = p.weights_out; x.weights = p.weights;
+            x.rows = p.rows; x.cols = p.cols; x.tall = tall; x.keep = p.keep; x.rate = p.rate;
+        }
+        rc = product<PL, E>(x, L, stream);
         if (rc) return rc;
         now ^= 1;
     }
-    p.Q = tall ? T[now] : X[now]; p.Q_lo = tall ? T_lo[now] : X_lo[now];
-    const dim3 each((unsigned)std::min<size_t>((n + 1023) / 1024, 4096), (unsigned)L);
-    if (fours) hipLaunchKernelGGL((finish_kernel<E, PL, true>), each, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((finish_kernel<E, PL, false>), each, dim3(256), 0, stream, p);
+    if (steps == 0) {
+        const dim3 each((unsigned)std::min<size_t>((n + 1023) / 1024, 4096), (unsigned)L);
+        if (fours) hipLaunchKernelGGL((finish_kernel<E, PL, true>), each, dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((finish_kernel<E, PL, false>), each, dim3(256), 0, stream, p);
+    }
     return launched("orthogonalised update");
 }
 

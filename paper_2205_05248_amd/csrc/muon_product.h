@@ -33,13 +33,18 @@ struct Product {
     int Mp, Np, stages;               // stages of 64 fp16 values of a row: 64 / PL of the summed index
     float alpha, beta;
     const _Float16 *C, *C_lo;         // [n][m], of scaled entries; C_lo: PL = 1 only.  Used with beta != 0
-    _Float16 *Dt, *Dt_lo;             // [n][m]
-    _Float16 *D, *D_lo;               // [m][n] or NULL
-    int64_t ldt, ldd, t_batch, d_batch;        // C, C_lo, Dt_lo lie as Dt; D_lo as D
+    _Float16 *Dt, *Dt_lo;             // [n][m]; Dt_lo: PL = 1, may be NULL
+    _Float16 *D;                      // [m][n] or NULL
+    int64_t ldt, ldd, t_batch, d_batch;        // C, C_lo, Dt_lo lie as Dt
     int symmetric;                    // A is B: only tiles on and below the diagonal, D is the mirrored tile
     int tiles_m, tiles_n, tiles;      // tiles: of one batch member
     int splits;                       // parts of the sum, one workgroup each; > 1: accumulators go to `partial`
     float *partial;                   // [batch][tiles][splits][16 MT NT / 4][threads] x 4
+    // The last product of an update writes the matrix itself, [rows][cols]: out = keep weights - rate D, or D without weights
+    void *out;                        // NULL: planes
+    const void *weights;
+    int rows, cols, tall;             // tall: rows are m, otherwise rows are n
+    float keep, rate;
 };
 
 template <int PL>
@@ -51,8 +56,8 @@ struct TileShape {
     static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
     static constexpr int TM = WM * MT * 32, TN = WN * NT * 32;
     static constexpr int kStage = (TM + TN) * 128;                     // bytes: 64 fp16 values of every row
-    static constexpr int kWide = PL * 32 * (MT > NT ? MT : NT) + 8;    // a staged row of results, fp16 values
-    static constexpr int kStaging = 32 * kWide * 2;                    // bytes a wave
+    static constexpr int kPitch = 32 * MT + 4;                         // a staged row of results, fp32 values
+    static constexpr int kStaging = 32 * kPitch * 4;                   // bytes a wave: 32 columns of its results
     static constexpr int kLds = 2 * kStage > kWaves * kStaging ? 2 * kStage : kWaves * kStaging;
     static constexpr int kQuads = 4 * MT * NT;                         // groups of four accumulators of a lane
 };
@@ -83,105 +88,117 @@ __device__ __forceinline__ int die_order(int id, int n)
     return die * per + min(die, rest) + id / 8;
 }
 
-// What becomes of a tile's accumulators: result in fp16 planes, in both orders.
-template <class S>
+__device__ __forceinline__ void wave_meets()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Eight results along a row as planes.
+template <int PL>
+__device__ __forceinline__ void put_planes(_Float16 *to, _Float16 *to_lo, const float (&v)[8])
+{
+    half8 h, l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        h[e] = (_Float16)v[e];
+        l[e] = (_Float16)(v[e] - (float)h[e]);
+    }
+    *reinterpret_cast<half8 *>(to) = h;
+    if (PL == 2) *reinterpret_cast<half8 *>(to + 32) = l;
+    else if (to_lo) *reinterpret_cast<half8 *>(to_lo) = l;
+}
+
+// Eight results along row r, from column c, of the matrix itself.
+template <typename E>
+__device__ __forceinline__ void put_out(const Product &p, int64_t batch, int r, int c, const float (&v)[8])
+{
+    if (r >= p.rows) return;
+    const int64_t at = (batch * p.rows + r) * p.cols + c;
+    const E *w = static_cast<const E *>(p.weights);
+    E *out = static_cast<E *>(p.out);
+    const float rate = p.rate * (1.0f / kPlaneScale);
+    auto one = [&](float x, float was) { return w ? p.keep * was - rate * x : x * (1.0f / kPlaneScale); };
+    typedef E Eight __attribute__((ext_vector_type(8), aligned(sizeof(E))));
+    if (c + 8 <= p.cols) {
+        Eight o, was;
+        if (w) was = *reinterpret_cast<const Eight *>(w + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = from_f32<E>(one(v[e], w ? to_f32((E)was[e]) : 0.0f));
+        *reinterpret_cast<Eight *>(out + at) = o;
+    } else {
+        for (int e = 0; e < 8; ++e)
+            if (c + e < p.cols) out[at + e] = from_f32<E>(one(v[e], w ? to_f32(w[at + e]) : 0.0f));
+    }
+}
+
+// What becomes of a tile's accumulators.  Through shared memory, 32 columns at a time and each wave for itself, so that memory is
+// read and written along rows: once in the order [n][m], where C is added, and once in the order [m][n].
+template <class S, typename E>
 __device__ __forceinline__ void put_tile(const Product &p, int64_t batch, int m0, int n0, bool diagonal, floatx16 (&acc)[S::MT][S::NT], char *lds)
 {
-    constexpr int PL = S::PL, MT = S::MT, NT = S::NT;
+    constexpr int PL = S::PL, MT = S::MT, NT = S::NT, kPitch = S::kPitch, kAlong = MT * 4;      // kAlong: eights of a row of m
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int wm = m0 + (wave / S::WN) * MT * 32, wn = n0 + (wave % S::WN) * NT * 32;
-    const int col = lane & 31, high = lane >> 5;
-    _Float16 *stage = reinterpret_cast<_Float16 *>(lds + wave * S::kStaging);
-    auto wave_sync = [] {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    };
-    _Float16 *Dt = p.Dt + batch * p.t_batch, *D = p.D ? p.D + batch * p.d_batch : nullptr;
-    _Float16 *Dt_lo = p.Dt_lo ? p.Dt_lo + batch * p.t_batch : nullptr, *D_lo = p.D_lo ? p.D_lo + batch * p.d_batch : nullptr;
+    float *stage = reinterpret_cast<float *>(lds + wave * S::kStaging);
     const _Float16 *C = p.C + batch * p.t_batch, *C_lo = p.C_lo ? p.C_lo + batch * p.t_batch : nullptr;
+    const bool transposed = p.out ? p.tall != 0 : p.D && !diagonal;
 #pragma unroll
-    for (int mb = 0; mb < MT; ++mb)
+    for (int nb = 0; nb < NT; ++nb) {
+        wave_meets();
 #pragma unroll
-        for (int nb = 0; nb < NT; ++nb) {
-            __builtin_amdgcn_sched_barrier(0);                         // one block's loads at a time, or registers run out
+        for (int mb = 0; mb < MT; ++mb)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int m = wm + mb * 32 + 8 * q + 4 * high, n = wn + nb * 32 + col;
-                floatx4 c = {0, 0, 0, 0};
-                if (p.beta != 0.0f && m < p.Mp && n < p.Np) {
-                    const int64_t at = n * p.ldt + plane_at<PL>(m);
-                    const half4 h = *reinterpret_cast<const half4 *>(C + at);
-                    half4 l = {0, 0, 0, 0};
-                    if constexpr (PL == 2) l = *reinterpret_cast<const half4 *>(C + at + 32);
-                    else if (C_lo) l = *reinterpret_cast<const half4 *>(C_lo + at);
-                    for (int e = 0; e < 4; ++e) c[e] = (float)h[e] + (float)l[e];
-                }
-                for (int e = 0; e < 4; ++e) acc[mb][nb][4 * q + e] = p.alpha * acc[mb][nb][4 * q + e] + p.beta * c[e];
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<floatx4 *>(stage + (lane & 31) * kPitch + mb * 32 + 8 * q + 4 * (lane >> 5)) =
+                    floatx4{acc[mb][nb][4 * q], acc[mb][nb][4 * q + 1], acc[mb][nb][4 * q + 2], acc[mb][nb][4 * q + 3]};
+        wave_meets();
+#pragma unroll 4
+        for (int k = lane; k < 32 * kAlong; k += kWave) {
+            const int col = k / kAlong, along = k % kAlong * 8, n = wn + nb * 32 + col, m = wm + along;
+            if (n >= p.Np || m >= p.Mp) continue;
+            float *at = stage + col * kPitch + along, v[8];
+            const int64_t lies = n * p.ldt + plane_at<PL>(m);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = p.alpha * at[e];
+            if (p.beta != 0.0f) {
+                const half8 h = *reinterpret_cast<const half8 *>(C + lies);
+                half8 l = {};
+                if constexpr (PL == 2) l = *reinterpret_cast<const half8 *>(C + lies + 32);
+                else if (C_lo) l = *reinterpret_cast<const half8 *>(C_lo + lies);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, (float)h[e] + (float)l[e], v[e]);
+            }
+            if (transposed) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) at[e] = v[e];
+            }
+            if (p.out) {
+                if (!p.tall) put_out<E>(p, batch, n, m, v);
+            } else {
+                put_planes<PL>(p.Dt + batch * p.t_batch + lies, p.Dt_lo ? p.Dt_lo + batch * p.t_batch + lies : nullptr, v);
             }
         }
-    // rows n of the transpose, 32 at a time
-    const int passes = PL == 1 && (Dt_lo || D_lo) ? 2 : 1;             // PL = 1: the plane lo after the plane hi
-    for (int pass = 0; pass < passes; ++pass) {
-        _Float16 *T = pass ? Dt_lo : Dt;
-        if (T) {
+        if (!transposed) continue;
+        wave_meets();
+#pragma unroll 2
+        for (int k = lane; k < 32 * MT * 4; k += kWave) {              // row k / 4, eight columns
+            const int row = k / 4, col = k % 4 * 8, m = wm + row, n = wn + nb * 32 + col;
+            if (n >= p.Np || m >= p.Mp) continue;
+            float v[8];
 #pragma unroll
-            for (int nb = 0; nb < NT; ++nb) {
-                wave_sync();
-#pragma unroll
-                for (int mb = 0; mb < MT; ++mb) {
-                    asm volatile("" : "+v"(acc[mb][nb]));              // planes are formed where they are stored, not kept
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        half4 h, l;
-                        for (int e = 0; e < 4; ++e) {
-                            const float v = acc[mb][nb][4 * q + e];
-                            h[e] = (_Float16)v;
-                            l[e] = (_Float16)(v - (float)h[e]);
-                        }
-                        const int k = mb * 32 + 8 * q + 4 * high;
-                        *reinterpret_cast<half4 *>(stage + col * S::kWide + plane_at<PL>(k)) = pass ? l : h;
-                        if constexpr (PL == 2) *reinterpret_cast<half4 *>(stage + col * S::kWide + plane_at<PL>(k) + 32) = l;
-                    }
-                }
-                wave_sync();
-                constexpr int kChunks = MT * 4 * PL;                   // of eight values in a row
-                for (int c = lane; c < 32 * kChunks; c += kWave) {
-                    const int r = c / kChunks, k = c % kChunks * 8, n = wn + nb * 32 + r;
-                    if (n < p.Np && wm + k / PL < p.Mp)
-                        *reinterpret_cast<half8 *>(T + n * p.ldt + (int64_t)wm * PL + k) = *reinterpret_cast<const half8 *>(stage + r * S::kWide + k);
-                }
-            }
-        }
-        _Float16 *R = pass ? D_lo : D;
-        if (R && !diagonal) {
-#pragma unroll
-            for (int mb = 0; mb < MT; ++mb) {
-                wave_sync();
-#pragma unroll
-                for (int nb = 0; nb < NT; ++nb) {
-                    asm volatile("" : "+v"(acc[mb][nb]));
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float v = acc[mb][nb][e];
-                        const _Float16 h = (_Float16)v, l = (_Float16)(v - (float)h);
-                        const int r = 8 * (e / 4) + 4 * high + e % 4, k = nb * 32 + col;
-                        stage[r * S::kWide + plane_at<PL>(k)] = pass ? l : h;
-                        if constexpr (PL == 2) stage[r * S::kWide + plane_at<PL>(k) + 32] = l;
-                    }
-                }
-                wave_sync();
-                constexpr int kChunks = NT * 4 * PL;
-                for (int c = lane; c < 32 * kChunks; c += kWave) {
-                    const int r = c / kChunks, k = c % kChunks * 8, m = wm + mb * 32 + r;
-                    if (m < p.Mp && wn + k / PL < p.Np)
-                        *reinterpret_cast<half8 *>(R + m * p.ldd + (int64_t)wn * PL + k) = *reinterpret_cast<const half8 *>(stage + r * S::kWide + k);
-                }
+            for (int e = 0; e < 8; ++e) v[e] = stage[(col + e) * kPitch + row];
+            if (p.out) {
+                put_out<E>(p, batch, m, n, v);
+            } else {
+                const int64_t lies = m * p.ldd + plane_at<PL>(n);
+                put_planes<PL>(p.D + batch * p.d_batch + lies, nullptr, v);
             }
         }
     }
 }
 
-template <class S>
+template <class S, typename E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -271,11 +288,11 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
         return;
     }
     __syncthreads();                                                   // the buffers become staging room
-    put_tile<S>(p, batch, m0, n0, p.symmetric && ti == tj, acc, lds);
+    put_tile<S, E>(p, batch, m0, n0, p.symmetric && ti == tj, acc, lds);
 }
 
 // Sums the parts of a tile, in order, and finishes it.
-template <class S>
+template <class S, typename E>
 __global__ __launch_bounds__(S::kThreads) void join_kernel(Product p)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -295,7 +312,7 @@ __global__ __launch_bounds__(S::kThreads) void join_kernel(Product p)
                 for (int s = 0; s < p.splits; ++s) sum += from[(s * S::kQuads + (a * S::NT + b) * 4 + q) * S::kThreads];
                 for (int e = 0; e < 4; ++e) acc[a][b][4 * q + e] = sum[e];
             }
-    put_tile<S>(p, batch, ti * S::TM, tj * S::TN, p.symmetric && ti == tj, acc, lds);
+    put_tile<S, E>(p, batch, ti * S::TM, tj * S::TN, p.symmetric && ti == tj, acc, lds);
 }
 
 }  // namespace marl
