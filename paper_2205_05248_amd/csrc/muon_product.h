@@ -13,6 +13,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "operator_types.h"
 
 namespace marl {
@@ -212,12 +214,12 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
     const int m0 = ti * TM, n0 = tj * TN;
     const int k_begin = (int)((int64_t)split * p.stages / p.splits), k_end = (int)((int64_t)(split + 1) * p.stages / p.splits);
 
-    // A wave's load brings eight rows of 128 bytes; chunk c of row r goes to place c ^ (r & 7), so that lanes reading the same
-    // chunk of neighbouring rows meet different banks.  The place in shared memory is fixed by the lane, so the lane
-    // asks for the chunk that belongs there.
+    // A wave's load brings eight rows of 128 bytes; chunk c of row r goes to place c ^ (r / 2 & 7), so that sixteen lanes reading the
+    // same chunk of neighbouring rows meet all 64 banks (with c ^ (r & 7) half of the cycles were conflicts).  The place in shared memory
+    // is fixed by the lane, so the lane asks for the chunk that belongs there.
     constexpr int kLoadsA = TM / 8 / S::kWaves, kLoadsB = TN / 8 / S::kWaves;
-    static_assert(kLoadsA * 8 * S::kWaves == TM && kLoadsB * 8 * S::kWaves == TN, "");
-    const int sub = lane >> 3, chunk = (lane & 7) ^ sub;
+    static_assert(kLoadsA * 8 * S::kWaves == TM && kLoadsB * 8 * S::kWaves == TN && S::kWaves % 2 == 0, "");
+    const int sub = lane >> 3, chunk = (lane & 7) ^ ((wave & 1) * 4 + sub / 2);
     const _Float16 *from_a[kLoadsA], *from_b[kLoadsB];
 #pragma unroll
     for (int q = 0; q < kLoadsA; ++q)
@@ -245,37 +247,80 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
     const int row = lane & 31, high = lane >> 5;
     const char *read_a = lds + ((wave / S::WN) * MT * 32 + row) * 128, *read_b = lds + TM * 128 + ((wave % S::WN) * NT * 32 + row) * 128;
     auto frag = [&](const char *base, int block, int c) {
-        return *reinterpret_cast<const half8 *>(base + block * 32 * 128 + ((c ^ (row & 7)) << 4));
+        return *reinterpret_cast<const half8 *>(base + block * 32 * 128 + ((c ^ (row / 2 & 7)) << 4));
     };
-    load(k_begin, 0);
-    for (int k = k_begin; k < k_end; ++k) {
-        const int buffer = (k - k_begin) & 1;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // this wave's part of the stage has arrived
-        __syncthreads();                                               // everybody's has, and the other buffer is read
-        if (k + 1 < k_end) load(k + 1, buffer ^ 1);
+    // Fragments are read one step (16 of the summed index) ahead of the products that take them, so that shared memory and the matrix
+    // pipe work at the same time; the first step of the next stage is read behind the barrier that stands before the last
+    // step's products.  By then the stage in hand has been read to its end, so its buffer takes the stage after the next.
+    constexpr int kInStage = 4 / PL;
+    half8 a[2][PL][MT], b[2][PL][NT];
+    auto read = [&](int set, int buffer, int j) {
         const char *ra = read_a + buffer * S::kStage, *rb = read_b + buffer * S::kStage;
 #pragma unroll
-        for (int j = 0; j < 4 / PL; ++j) {
-            half8 a[PL][MT], b[PL][NT];
+        for (int pl = 0; pl < PL; ++pl) {
 #pragma unroll
-            for (int pl = 0; pl < PL; ++pl) {
+            for (int t = 0; t < MT; ++t) a[set][pl][t] = frag(ra, t, 4 * pl + 2 * j + high);
 #pragma unroll
-                for (int t = 0; t < MT; ++t) a[pl][t] = frag(ra, t, 4 * pl + 2 * j + high);
+            for (int t = 0; t < NT; ++t) b[set][pl][t] = frag(rb, t, 4 * pl + 2 * j + high);
+        }
+    };
+    auto arrive = [&] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // this wave's part of a stage has arrived
+        __syncthreads();                                               // everybody's has
+    };
+    constexpr int kReads = PL * (MT + NT), kProducts = (PL == 2 ? 3 : 1) * MT * NT;
+    auto products = [&](int set) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) b[pl][t] = frag(rb, t, 4 * pl + 2 * j + high);
-            }
+        for (int part = 0; part < (PL == 2 ? 3 : 1); ++part)           // hi hi, hi lo, lo hi
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int u = 0; u < NT; ++u) {
-                    acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][t], b[0][u], acc[t][u], 0, 0, 0);
-                    if constexpr (PL == 2) {
-                        acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0][t], b[1][u], acc[t][u], 0, 0, 0);
-                        acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1][t], b[0][u], acc[t][u], 0, 0, 0);
-                    }
-                }
+                for (int u = 0; u < NT; ++u)
+                    acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[set][part == 2][t], b[set][part == 1][u], acc[t][u], 0, 0, 0);
+    };
+    // Products, then one read, in turn: reads in a row would hold up the products behind them until shared memory took them.  The
+    // loads of a stage come first (they write shared memory, so no read passes them), a product between them.
+    constexpr int kLoads = kLoadsA + kLoadsB, kBetween = PL == 2 ? 1 : 0;
+    auto in_turn = [&](auto loads) {
+        constexpr int kFirst = decltype(loads)::value ? kLoads : 0, kEach = (kProducts - kFirst * kBetween) / kReads > 0 ? (kProducts - kFirst * kBetween) / kReads : 1;
+#pragma unroll
+        for (int q = 0; q < kFirst; ++q) {
+            __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+            if (kBetween) __builtin_amdgcn_sched_group_barrier(0x008, kBetween, 0);
+        }
+#pragma unroll
+        for (int q = 0; q < kReads; ++q) {
+            __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kProducts, 0);
+    };
+    load(k_begin, 0);                                                  // (every part has a stage at least)
+    arrive();
+    load(min(k_begin + 1, k_end - 1), 1);
+    read(0, 0, 0);
+    int buffer = 0;
+    for (int k = k_begin; k + 1 < k_end; ++k, buffer ^= 1) {
+#pragma unroll
+        for (int j = 0; j < kInStage; ++j) {
+            if (j + 1 < kInStage) {
+                read((j + 1) & 1, buffer, j + 1);
+            } else {
+                arrive();
+                load(min(k + 2, k_end - 1), buffer);                   // (behind the last stage: once more, and not read)
+                read((j + 1) & 1, buffer ^ 1, 0);
+            }
+            products(j & 1);
+            if (j + 1 < kInStage) in_turn(std::false_type{});
+            else in_turn(std::true_type{});
         }
     }
+#pragma unroll
+    for (int j = 0; j < kInStage; ++j) {
+        if (j + 1 < kInStage) read((j + 1) & 1, buffer, j + 1);
+        products(j & 1);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                   // nothing may still be on its way into the buffers
     if (p.splits > 1) {
         floatx4 *to = reinterpret_cast<floatx4 *>(p.partial) + ((batch * p.tiles + tile) * p.splits + split) * (S::kQuads * S::kThreads) + threadIdx.x;
 #pragma unroll
