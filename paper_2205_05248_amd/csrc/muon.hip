@@ -247,9 +247,9 @@ int product(Product p, int L, hipStream_t stream)
     const Plan plan = plan_of(L, p.Mp, p.Np, p.symmetric, p.stages);
     p.splits = plan.splits;
     switch (plan.shape) {
-    case 0: return launch_product<TileShape<PL, 2, 4, 4, 2>, E>(p, L, stream);
-    case 1: return launch_product<TileShape<PL, 2, 2, 2, 2>, E>(p, L, stream);
-    default: return launch_product<TileShape<PL, 2, 2, 1, 1>, E>(p, L, stream);
+    case 0: return launch_product<TileShape<PL, 2, 4, 4, 2, 2>, E>(p, L, stream);
+    case 1: return launch_product<TileShape<PL, 2, 2, 2, 2, 4>, E>(p, L, stream);
+    default: return launch_product<TileShape<PL, 2, 2, 1, 1, 4>, E>(p, L, stream);
     }
 }
 

@@ -52,15 +52,15 @@ struct Product {
 template <int PL>
 __host__ __device__ __forceinline__ int plane_at(int k) { return PL == 1 ? k : (k >> 5) * 64 + (k & 31); }
 
-template <int PL_, int WM_, int WN_, int MT_, int NT_>
+template <int PL_, int WM_, int WN_, int MT_, int NT_, int BUFFERS_>
 struct TileShape {
-    static constexpr int PL = PL_, WM = WM_, WN = WN_, MT = MT_, NT = NT_;
+    static constexpr int PL = PL_, WM = WM_, WN = WN_, MT = MT_, NT = NT_, kBuffers = BUFFERS_;
     static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
     static constexpr int TM = WM * MT * 32, TN = WN * NT * 32;
     static constexpr int kStage = (TM + TN) * 128;                     // bytes: 64 fp16 values of every row
     static constexpr int kPitch = 32 * MT + 4;                         // a staged row of results, fp32 values
     static constexpr int kStaging = 32 * kPitch * 4;                   // bytes a wave: 32 columns of its results
-    static constexpr int kLds = 2 * kStage > kWaves * kStaging ? 2 * kStage : kWaves * kStaging;
+    static constexpr int kLds = kBuffers * kStage > kWaves * kStaging ? kBuffers * kStage : kWaves * kStaging;
     static constexpr int kQuads = 4 * MT * NT;                         // groups of four accumulators of a lane
 };
 
@@ -264,10 +264,10 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
             for (int t = 0; t < NT; ++t) b[set][pl][t] = frag(rb, t, 4 * pl + 2 * j + high);
         }
     };
-    auto arrive = [&] {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // this wave's part of a stage has arrived
-        __syncthreads();                                               // everybody's has
-    };
+    // The oldest stage on its way has arrived: this wave's part of it, then everybody's.  A wave's loads return in order, kLoads
+    // a stage; the later stages stay on their way.
+    constexpr int kLoads = kLoadsA + kLoadsB;
+    auto arrive = [&] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S::kBuffers - 2) * kLoads) : "memory"); };
     constexpr int kReads = PL * (MT + NT), kProducts = (PL == 2 ? 3 : 1) * MT * NT;
     auto products = [&](int set) {
 #pragma unroll
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
     };
     // Products, then one read, in turn: reads in a row would hold up the products behind them until shared memory took them.  The
     // loads of a stage come first (they write shared memory, so no read passes them), a product between them.
-    constexpr int kLoads = kLoadsA + kLoadsB, kBetween = PL == 2 ? 1 : 0;
+    constexpr int kBetween = PL == 2 ? 1 : 0;
     auto in_turn = [&](auto loads) {
         constexpr int kFirst = decltype(loads)::value ? kLoads : 0, kEach = (kProducts - kFirst * kBetween) / kReads > 0 ? (kProducts - kFirst * kBetween) / kReads : 1;
 #pragma unroll
@@ -295,25 +295,28 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
         }
         __builtin_amdgcn_sched_group_barrier(0x008, kProducts, 0);
     };
-    load(k_begin, 0);                                                  // (every part has a stage at least)
+#pragma unroll
+    for (int q = 0; q < S::kBuffers - 1; ++q) load(min(k_begin + q, k_end - 1), q);    // (every part has a stage at least)
     arrive();
-    load(min(k_begin + 1, k_end - 1), 1);
+    load(min(k_begin + S::kBuffers - 1, k_end - 1), S::kBuffers - 1);
     read(0, 0, 0);
     int buffer = 0;
-    for (int k = k_begin; k + 1 < k_end; ++k, buffer ^= 1) {
+    for (int k = k_begin; k + 1 < k_end; ++k) {
+        const int next = buffer + 1 == S::kBuffers ? 0 : buffer + 1;
 #pragma unroll
         for (int j = 0; j < kInStage; ++j) {
             if (j + 1 < kInStage) {
                 read((j + 1) & 1, buffer, j + 1);
             } else {
                 arrive();
-                load(min(k + 2, k_end - 1), buffer);                   // (behind the last stage: once more, and not read)
-                read((j + 1) & 1, buffer ^ 1, 0);
+                load(min(k + S::kBuffers, k_end - 1), buffer);         // (behind the last stage: once more, and not read)
+                read((j + 1) & 1, next, 0);
             }
             products(j & 1);
             if (j + 1 < kInStage) in_turn(std::false_type{});
             else in_turn(std::true_type{});
         }
+        buffer = next;
     }
 #pragma unroll
     for (int j = 0; j < kInStage; ++j) {
