@@ -5,7 +5,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "muon_product.h"
+#include "muon_small.h"
 
 namespace marl {
 namespace {
@@ -191,25 +191,27 @@ Plan plan_of(int L, int Mp, int Np, bool symmetric, int stages)
     Plan best{2, 1};
     for (int shape = 0; shape < 3; ++shape)
         if ((int64_t)tiles_of(shape, Mp, Np, symmetric) * L >= 128) { best.shape = shape; break; }
-    (void)stages;
+    const int64_t tiles = (int64_t)tiles_of(best.shape, Mp, Np, symmetric) * L;
+    if (symmetric && stages >= 64 && tiles < 256) best.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, stages / 16));
     return best;
 }
 
 struct Layout {
     int rows_p, cols_p, s, l, s_p, l_p, planes;
-    size_t x[2], t[2], x_lo[2], g, p, part, bytes;
+    size_t x[2], t[2], x_lo[2], g, p, part, partial, bytes;
 };
 
 Layout layout_of(int dtype, int L, int rows, int cols)
 {
     Layout y{};
+    if (small_fits(rows, cols)) { y.bytes = 256; return y; }   // shared memory alone; a size of zero would be a special case for callers
     auto pad = [](int v) { return (v + 63) / 64 * 64; };
     y.rows_p = pad(rows); y.cols_p = pad(cols);
     y.s = rows < cols ? rows : cols; y.l = rows < cols ? cols : rows;
     y.s_p = pad(y.s); y.l_p = pad(y.l);
     y.planes = dtype == MARL_DTYPE_BF16 ? 1 : 2;
     const size_t n = (size_t)L * y.rows_p * y.cols_p * sizeof(_Float16), square = (size_t)L * y.s_p * y.s_p * sizeof(_Float16) * y.planes;
-    size_t at = 0;
+    size_t at = 0, partial = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
     for (int k = 0; k < 2; ++k) {
         y.x[k] = take(n * y.planes);
@@ -219,6 +221,13 @@ Layout layout_of(int dtype, int L, int rows, int cols)
     y.g = take(square);
     y.p = take(square);
     y.part = take((size_t)L * kNormBlocks * sizeof(double));
+    const int stages_g = y.l_p * y.planes / 64, stages_p = y.s_p * y.planes / 64;
+    for (int stages : {stages_g, stages_p}) {
+        const Plan plan = plan_of(L, y.s_p, y.s_p, true, stages);
+        if (plan.splits > 1)
+            partial = std::max(partial, (size_t)L * tiles_of(plan.shape, y.s_p, y.s_p, true) * plan.splits * kSide[plan.shape] * kSide[plan.shape] * sizeof(float));
+    }
+    y.partial = take(partial);
     y.bytes = at;
     return y;
 }
@@ -248,7 +257,7 @@ int product(Product p, int L, hipStream_t stream)
     p.splits = plan.splits;
     switch (plan.shape) {
     case 0: return launch_product<TileShape<PL, 2, 4, 4, 2, 2>, E>(p, L, stream);
-    case 1: return launch_product<TileShape<PL, 2, 2, 2, 2, 4>, E>(p, L, stream);
+    case 1: return launch_product<TileShape<PL, 2, 2, 2, 2, 2>, E>(p, L, stream);
     default: return launch_product<TileShape<PL, 2, 2, 1, 1, 4>, E>(p, L, stream);
     }
 }
@@ -286,6 +295,7 @@ int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, co
         g.alpha = 1.0f / kPlaneScale;
         g.Dt = g.D = at(y.g); g.ldt = g.ldd = (int64_t)y.s_p * PL; g.t_batch = g.d_batch = square;
         g.symmetric = 1;
+        g.partial = reinterpret_cast<float *>(workspace + y.partial);
         int rc = product<PL, E>(g, L, stream);
         if (rc) return rc;
         Product q = g;
@@ -320,9 +330,22 @@ int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, co
     return launched("orthogonalised update");
 }
 
+template <typename E>
+int iterate_small(int L, const UpdateArgs &p, int steps, const float *coef, hipStream_t stream)
+{
+    const int bytes = small_shape(p.rows, p.cols).bytes;
+    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(small_kernel<E>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (err != hipSuccess) return report_device_error(err, "hipFuncSetAttribute");
+    const SmallArgs a{p.rows, p.cols, steps, p.nesterov, p.weights, p.grad, p.momentum, p.weights_out, p.momentum_out,
+                      p.beta, p.keep, p.rate, p.eps, coef[0], coef[1], coef[2]};
+    hipLaunchKernelGGL(small_kernel<E>, dim3((unsigned)L), dim3(kSmallThreads), bytes, stream, a);
+    return launched("orthogonalised update");
+}
+
 int newton_schulz(int dtype, int L, UpdateArgs p, char *workspace, int steps, const float *coef, float eps, hipStream_t stream)
 {
     p.eps = eps;
+    if (small_fits(p.rows, p.cols)) return with_dtype(dtype, [&](auto e) { return iterate_small<decltype(e)>(L, p, steps, coef, stream); });
     const Layout y = layout_of(dtype, L, p.rows, p.cols);
     switch (dtype) {
     case MARL_DTYPE_F32: return iterate<float, 2>(y, L, p, workspace, steps, coef, stream);

@@ -1,0 +1,196 @@
+// The whole Newton-Schulz iteration of a small matrix in one workgroup: X, its transpose, G and P stay in shared memory.
+// A product of such a matrix takes a microsecond and a launch costs more: three products a step and the two passes around them
+// were 18 launches and 83 us for two matrices of 192 x 64.  Tiles of 16 x 16, one per wave and turn, sixteen waves: the chain of
+// dependent matrix instructions, which is what bounds it, is as short as it gets.  Planes as in muon_product.h, two of every factor
+// whatever the type: the third of the instructions that one plane would save does not show.
+#pragma once
+#include "muon_product.h"
+
+namespace marl {
+
+// What a thread and a wave hold at most: entries of the matrix, tiles of X.  Both planes of X and of its transpose in 160 KB leave
+// no more than 20480 entries.
+constexpr int kSmallThreads = 1024, kSmallEntries = 20, kSmallTurns = 5;
+
+// Rows of planes in shared memory: 16 bytes more than a multiple of 128, so that sixteen rows meet all banks.
+__host__ __device__ __forceinline__ int small_row(int k) { return 2 * k + 8; }
+
+struct SmallShape {
+    int s, l;                          // short and long side, padded to multiples of 32
+    int x, t, g, p, bytes;             // offsets in fp16 values, and bytes of all
+};
+
+__host__ __device__ inline SmallShape small_shape(int rows, int cols)
+{
+    SmallShape y{};
+    const int s = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
+    y.s = (s + 31) / 32 * 32;
+    y.l = (l + 31) / 32 * 32;
+    y.x = 0;
+    y.t = y.x + y.s * small_row(y.l);
+    y.g = y.t + y.l * small_row(y.s);
+    y.p = y.g + y.s * small_row(y.s);
+    y.bytes = (y.p + y.s * small_row(y.s)) * 2;
+    return y;
+}
+
+inline bool small_fits(int rows, int cols)
+{
+    if ((int64_t)rows * cols > kSmallEntries * kSmallThreads) return false;
+    const SmallShape y = small_shape(rows, cols);
+    return y.bytes <= 159 * 1024 && (y.s / 16) * (y.l / 16) <= kSmallTurns * (kSmallThreads / kWave);
+}
+
+struct SmallArgs {
+    int rows, cols, steps, nesterov;
+    const void *weights, *grad;
+    const float *momentum;
+    void *weights_out;
+    float *momentum_out;
+    float beta, keep, rate, eps, c0, c1, c2;
+};
+
+template <typename E>
+__global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ double part[kSmallThreads / kWave];
+    _Float16 *planes = reinterpret_cast<_Float16 *>(lds);
+    const SmallShape y = small_shape(a.rows, a.cols);
+    const bool tall = a.rows > a.cols;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = a.rows * a.cols;
+    const size_t base = (size_t)blockIdx.x * n;
+    _Float16 *X = planes + y.x, *T = planes + y.t, *G = planes + y.g, *P = planes + y.p;
+    const int ldx = small_row(y.l), lds_s = small_row(y.s);
+
+    float u[kSmallEntries];                                // momentum, or the gradient alone
+    double sum = 0.0;
+#pragma unroll
+    for (int q = 0; q < kSmallEntries; ++q) {
+        const int k = threadIdx.x + q * kSmallThreads;
+        u[q] = k < n ? to_f32(static_cast<const E *>(a.grad)[base + k]) : 0.0f;
+    }
+    if (a.momentum) {
+        float m[kSmallEntries];
+#pragma unroll
+        for (int q = 0; q < kSmallEntries; ++q) {
+            const int k = threadIdx.x + q * kSmallThreads;
+            m[q] = k < n ? a.momentum[base + k] : 0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < kSmallEntries; ++q) {
+            const int k = threadIdx.x + q * kSmallThreads;
+            m[q] = fmaf(a.beta, m[q], u[q]);
+            if (k < n) a.momentum_out[base + k] = m[q];
+            u[q] = a.nesterov ? fmaf(a.beta, m[q], u[q]) : m[q];
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < kSmallEntries; ++q) sum += (double)u[q] * u[q];
+    for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
+    if (lane == 0) part[wave] = sum;
+    for (int k = threadIdx.x; k < y.g / 8; k += kSmallThreads) reinterpret_cast<half8 *>(planes)[k] = half8{};     // padding of X and T
+    __syncthreads();
+    sum = 0.0;
+    for (int w = 0; w < kSmallThreads / kWave; ++w) sum += part[w];
+    const double factor = (double)kPlaneScale / fmax(sqrt(sum), (double)a.eps);
+    auto put = [&](_Float16 *to, float v) {
+        const _Float16 h = (_Float16)v;
+        to[0] = h;
+        to[32] = (_Float16)(v - (float)h);
+    };
+    // n < 2^15: the reciprocal, rounded up, gives the row without a division
+    const unsigned per_row = (unsigned)(0xffffffffu / (unsigned)a.cols) + 1;
+    auto row_of = [&](int k) { return a.cols == 1 ? k : (int)__umulhi((unsigned)k, per_row); };
+#pragma unroll
+    for (int q = 0; q < kSmallEntries; ++q) {
+        const int k = threadIdx.x + q * kSmallThreads, r = row_of(k), c = k - r * a.cols;
+        if (k >= n) break;
+        const float v = (float)(factor * u[q]);
+        const int i = tall ? c : r, j = tall ? r : c;      // X[i][j]
+        put(X + i * ldx + plane_at<2>(j), v);
+        put(T + j * lds_s + plane_at<2>(i), v);
+    }
+    __syncthreads();
+
+    // 16 x 16 results of A B^T over K: rows 4 (lane / 16) + e of A, row lane % 16 of B
+    auto tile = [&](const _Float16 *A, int lda, int m0, const _Float16 *B, int ldb, int n0, int K) {
+        floatx4 acc = {0, 0, 0, 0}, cross = {0, 0, 0, 0};
+        const _Float16 *pa = A + (m0 + (lane & 15)) * lda + 8 * (lane >> 4), *pb = B + (n0 + (lane & 15)) * ldb + 8 * (lane >> 4);
+        for (int k = 0; k < K; k += 32) {
+            const half8 ah = *reinterpret_cast<const half8 *>(pa + 2 * k), al = *reinterpret_cast<const half8 *>(pa + 2 * k + 32);
+            const half8 bh = *reinterpret_cast<const half8 *>(pb + 2 * k), bl = *reinterpret_cast<const half8 *>(pb + 2 * k + 32);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, acc, 0, 0, 0);
+            cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, cross, 0, 0, 0);
+            cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, cross, 0, 0, 0);
+        }
+        return acc + cross;
+    };
+    auto put_along = [&](_Float16 *to, const floatx4 &v) {  // four entries along a row
+        half4 h, l;
+        for (int e = 0; e < 4; ++e) {
+            h[e] = (_Float16)v[e];
+            l[e] = (_Float16)(v[e] - (float)h[e]);
+        }
+        *reinterpret_cast<half4 *>(to) = h;
+        *reinterpret_cast<half4 *>(to + 32) = l;
+    };
+    const int ts = y.s / 16, waves = kSmallThreads / kWave;
+    const int m4 = 4 * (lane >> 4), nn = lane & 15;
+    // a symmetric matrix: written once, in the order in which a lane holds it
+    auto square = [&](const _Float16 *A, int lda, int K, _Float16 *D, float alpha, float beta) {
+        for (int k = wave; k < ts * ts; k += waves) {
+            const int m0 = k / ts * 16, n0 = k % ts * 16;
+            floatx4 v = tile(A, lda, m0, A, lda, n0, K) * alpha;
+            const int at = (n0 + nn) * lds_s + plane_at<2>(m0 + m4);
+            if (beta != 0.0f) {
+                const half4 h = *reinterpret_cast<const half4 *>(G + at), l = *reinterpret_cast<const half4 *>(G + at + 32);
+                for (int e = 0; e < 4; ++e) v[e] = fmaf(beta, (float)h[e] + (float)l[e], v[e]);
+            }
+            put_along(D + at, v);
+        }
+        __syncthreads();
+    };
+    for (int step = 0; step < a.steps; ++step) {
+        square(X, ldx, y.l, G, 1.0f / kPlaneScale, 0.0f);
+        square(G, lds_s, y.s, P, a.c2 / kPlaneScale, a.c1);
+        // D [l][s] = T P; all of it is formed before any of X is overwritten
+        floatx4 held[kSmallTurns];
+        const int tiles = ts * (y.l / 16);
+#pragma unroll
+        for (int q = 0; q < kSmallTurns; ++q) {
+            const int k = wave + q * waves, m0 = k / ts * 16, n0 = k % ts * 16;
+            if (k < tiles) {
+                held[q] = tile(T, lds_s, m0, P, lds_s, n0, y.s) * (1.0f / kPlaneScale);
+                const int at = (n0 + nn) * ldx + plane_at<2>(m0 + m4);
+                const half4 h = *reinterpret_cast<const half4 *>(X + at), l = *reinterpret_cast<const half4 *>(X + at + 32);
+                for (int e = 0; e < 4; ++e) held[q][e] = fmaf(a.c0, (float)h[e] + (float)l[e], held[q][e]);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kSmallTurns; ++q) {
+            const int k = wave + q * waves, m0 = k / ts * 16, n0 = k % ts * 16;
+            if (k < tiles) {
+                put_along(X + (n0 + nn) * ldx + plane_at<2>(m0 + m4), held[q]);
+                for (int e = 0; e < 4; ++e) put(T + (m0 + m4 + e) * lds_s + plane_at<2>(n0 + nn), held[q][e]);
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int q = 0; q < kSmallEntries; ++q) {
+        const int k = threadIdx.x + q * kSmallThreads;
+        u[q] = a.weights && k < n ? to_f32(static_cast<const E *>(a.weights)[base + k]) : 0.0f;
+    }
+#pragma unroll
+    for (int q = 0; q < kSmallEntries; ++q) {
+        const int k = threadIdx.x + q * kSmallThreads, r = row_of(k), c = k - r * a.cols;
+        if (k >= n) break;
+        const _Float16 *at = tall ? T + r * lds_s + plane_at<2>(c) : X + r * ldx + plane_at<2>(c);
+        const float x = ((float)at[0] + (float)at[32]) * (1.0f / kPlaneScale);
+        static_cast<E *>(a.weights_out)[base + k] = from_f32<E>(a.weights ? a.keep * u[q] - a.rate * x : x);
+    }
+}
+
+}  // namespace marl
