@@ -581,39 +581,45 @@ def _element(t, name):
     return code
 
 
-def _rows(t, dtype, shape, name):
-    """Address and row distance of a device tensor [..., C] whose leading axes fold into one row index."""
-    ok = t.dtype is dtype and t.shape == shape and t.is_cuda and t.device.index == _torch.cuda.current_device()
-    if ok:
+def _rows(t, dtype, shape, name, device):
+    """Address and row distance of a tensor [..., C] on `device` whose leading axes fold into one row index."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device:
         C, strides = shape[-1], t.stride()
+        if strides[-1] == 1 or C <= 1:
+            if len(shape) == 2:
+                ld = strides[0] if shape[0] > 1 else C
+                if ld >= C:
+                    return t.data_ptr(), ld
+            elif len(shape) == 3:
+                B, T = shape[0], shape[1]
+                ld = strides[1] if T > 1 else strides[0] if B > 1 else C
+                if ld >= C and (B == 1 or T <= 1 or strides[0] == ld * T):
+                    return t.data_ptr(), ld
         if t.is_contiguous():
             return t.data_ptr(), C
-        ok = C <= 1 or strides[-1] == 1
-        at = len(shape) - 2                                       # the innermost leading axis with more than one index
-        while at > 0 and shape[at] == 1:
-            at -= 1
-        ld = strides[at] if shape[at] > 1 else C
-        step = ld
-        for axis in range(at, -1, -1):
-            ok = ok and (shape[axis] == 1 or strides[axis] == step)
-            step *= shape[axis]
-        ok = ok and ld >= C
-    if not ok:
-        raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the current device with adjacent elements and "
-                         f"evenly spaced rows, got {t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
-    return t.data_ptr(), ld
+    raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the current device with adjacent elements and "
+                     f"evenly spaced rows, got {t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
 
 
-def _flat(t, dtype, shape, name, optional=False):
-    """Address of a contiguous tensor on the current device (`dtype`: a key of _dtypes)."""
-    address = _dev(t, dtype, shape, name, optional)
-    if t is not None and t.device.index != _torch.cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, but the current device is {_torch.cuda.current_device()}")
-    return address
+def _flat(t, dtype, shape, name, device, optional=False):
+    """Address of a contiguous tensor on `device` (dtype: a key of _dtypes)."""
+    if t is None and optional:
+        return None
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.dtype is not _dtypes[dtype] or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, "
+                         f"got {t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
+    return t.data_ptr()
 
 
-def _workspace(t):
-    return (None, 0) if t is None or t.numel() == 0 else (_flat(t, "u8", (t.numel(),), "workspace"), t.numel())
+def _current_device():
+    """Ordinal of the current device; -2, which is no tensor's, without one."""
+    return _torch._C._cuda_getDevice() if _torch.cuda.is_initialized() else _torch.cuda.current_device() if _torch.cuda.is_available() else -2
+
+
+def _workspace(t, device):
+    return (None, 0) if t is None or t.numel() == 0 else (_flat(t, "u8", (t.numel(),), "workspace", device), t.numel())
 
 
 def _dtype_code(dtype):
@@ -635,42 +641,42 @@ def marl_linear_scan_workspace_bytes(dtype, B, T, C):
 
 def marl_linear_scan(x, r, i, lam, decay, reset, filled, h_first, y, h_last, workspace):
     """Gated linear recurrence over x, r, i [B,T,C]; reset, filled [B,T] u8, h_first [B,C], h_last [B,C] may be None."""
-    code = _element(x, "x")
+    code, d = _element(x, "x"), _current_device()
     B, T, C = x.shape
-    (px, lx), (pr, lr), (pi, li) = (_rows(t, x.dtype, (B, T, C), n) for t, n in ((x, "x"), (r, "r"), (i, "i")))
-    py, ly = _rows(y, x.dtype, (B, T, C), "y")
+    (px, lx), (pr, lr), (pi, li) = (_rows(t, x.dtype, (B, T, C), n, d) for t, n in ((x, "x"), (r, "r"), (i, "i")))
+    py, ly = _rows(y, x.dtype, (B, T, C), "y", d)
     check(load().marl_linear_scan(
-        code, B, T, C, px, lx, pr, lr, pi, li, _flat(lam, "f32", (C,), "lam"), float(decay),
-        _flat(reset, "u8", (B, T), "reset", True), _flat(filled, "u8", (B, T), "filled", True),
-        _flat(h_first, "f32", (B, C), "h_first", True), py, ly, _flat(h_last, "f32", (B, C), "h_last", True), *_workspace(workspace),
+        code, B, T, C, px, lx, pr, lr, pi, li, _flat(lam, "f32", (C,), "lam", d), float(decay),
+        _flat(reset, "u8", (B, T), "reset", d, True), _flat(filled, "u8", (B, T), "filled", d, True),
+        _flat(h_first, "f32", (B, C), "h_first", d, True), py, ly, _flat(h_last, "f32", (B, C), "h_last", d, True), *_workspace(workspace, d),
         _stream()))
 
 
 def marl_linear_scan_grad(x, r, i, lam, decay, reset, filled, grad_y, grad_h_last, workspace, grad_x, grad_r, grad_i, grad_lam,
                           grad_h_first=None):
     """workspace: as marl_linear_scan left it for the same inputs; grad_h_last, grad_h_first may be None."""
-    code = _element(x, "x")
+    code, d = _element(x, "x"), _current_device()
     B, T, C = x.shape
     flat = []
     for t, n in ((x, "x"), (r, "r"), (i, "i"), (grad_y, "grad_y"), (grad_x, "grad_x"), (grad_r, "grad_r"), (grad_i, "grad_i")):
-        flat.append(_rows(t, x.dtype, (B, T, C), n))
+        flat.append(_rows(t, x.dtype, (B, T, C), n, d))
     px, pr, pi, pg, gx, gr, gi = flat
     check(load().marl_linear_scan_grad(
-        code, B, T, C, *px, *pr, *pi, _flat(lam, "f32", (C,), "lam"), float(decay), _flat(reset, "u8", (B, T), "reset", True),
-        _flat(filled, "u8", (B, T), "filled", True), *pg, _flat(grad_h_last, "f32", (B, C), "grad_h_last", True),
-        *_workspace(workspace), *gx, *gr, *gi, _flat(grad_lam, "f32", (C,), "grad_lam"),
-        _flat(grad_h_first, "f32", (B, C), "grad_h_first", True), _stream()))
+        code, B, T, C, *px, *pr, *pi, _flat(lam, "f32", (C,), "lam", d), float(decay), _flat(reset, "u8", (B, T), "reset", d, True),
+        _flat(filled, "u8", (B, T), "filled", d, True), *pg, _flat(grad_h_last, "f32", (B, C), "grad_h_last", d, True),
+        *_workspace(workspace, d), *gx, *gr, *gi, _flat(grad_lam, "f32", (C,), "grad_lam", d),
+        _flat(grad_h_first, "f32", (B, C), "grad_h_first", d, True), _stream()))
 
 
 def marl_linear_step(x, r, i, lam, decay, slot, reset, h_in, h_out, y):
     """One step of n sequences: x, r, i, y [n,C]; slot [n] i32 or None picks rows of h_in, h_out [slots,C] (may be the same)."""
-    code = _element(x, "x")
+    code, d = _element(x, "x"), _current_device()
     n, C = x.shape
     slots = h_in.shape[0]
-    (px, lx), (pr, lr), (pi, li), (py, ly) = (_rows(t, x.dtype, (n, C), m) for t, m in ((x, "x"), (r, "r"), (i, "i"), (y, "y")))
+    (px, lx), (pr, lr), (pi, li), (py, ly) = (_rows(t, x.dtype, (n, C), m, d) for t, m in ((x, "x"), (r, "r"), (i, "i"), (y, "y")))
     check(load().marl_linear_step(
-        code, n, C, px, lx, pr, lr, pi, li, _flat(lam, "f32", (C,), "lam"), float(decay), _flat(slot, "i32", (n,), "slot", True), slots,
-        _flat(reset, "u8", (n,), "reset", True), _flat(h_in, "f32", (slots, C), "h_in"), _flat(h_out, "f32", (slots, C), "h_out"), py, ly,
+        code, n, C, px, lx, pr, lr, pi, li, _flat(lam, "f32", (C,), "lam", d), float(decay), _flat(slot, "i32", (n,), "slot", d, True), slots,
+        _flat(reset, "u8", (n,), "reset", d, True), _flat(h_in, "f32", (slots, C), "h_in", d), _flat(h_out, "f32", (slots, C), "h_out", d), py, ly,
         _stream()))
 
 
@@ -678,36 +684,36 @@ def marl_log_prob_workspace_bytes(R, V, K):
     return _bytes_of(load().marl_log_prob_workspace_bytes, int(R), int(V), int(K))
 
 
-def _avail_of(avail, R, V):
+def _avail_of(avail, R, V, d):
     """Address and row distance: [R,V], or [V] for all rows."""
     if avail is None:
         return None, 0
     if avail.dim() == 1:
-        return _flat(avail, "u8", (V,), "avail"), 0
-    return _rows(avail, _dtypes["u8"], (R, V), "avail")
+        return _flat(avail, "u8", (V,), "avail", d), 0
+    return _rows(avail, _dtypes["u8"], (R, V), "avail", d)
 
 
 def marl_log_prob(logits, token, avail, scale, logp, entropy, log_sum, top_id=None, top_logp=None, workspace=None):
     """logits [R,V]; token [R] i32, avail [R,V] or [V] u8, and every output may be None; top_id [R,K] i32, top_logp [R,K]."""
-    code = _element(logits, "logits")
+    code, d = _element(logits, "logits"), _current_device()
     R, V = logits.shape
     K = 0 if top_id is None else top_id.shape[1]
     check(load().marl_log_prob(
-        code, R, V, *_rows(logits, logits.dtype, (R, V), "logits"), _flat(token, "i32", (R,), "token", True), *_avail_of(avail, R, V),
-        float(scale), _flat(logp, "f32", (R,), "logp", True), _flat(entropy, "f32", (R,), "entropy", True),
-        _flat(log_sum, "f32", (R,), "log_sum", True), K, _flat(top_id, "i32", (R, K), "top_id", True),
-        _flat(top_logp, "f32", (R, K), "top_logp", True), *_workspace(workspace), _stream()))
+        code, R, V, *_rows(logits, logits.dtype, (R, V), "logits", d), _flat(token, "i32", (R,), "token", d, True), *_avail_of(avail, R, V, d),
+        float(scale), _flat(logp, "f32", (R,), "logp", d, True), _flat(entropy, "f32", (R,), "entropy", d, True),
+        _flat(log_sum, "f32", (R,), "log_sum", d, True), K, _flat(top_id, "i32", (R, K), "top_id", d, True),
+        _flat(top_logp, "f32", (R, K), "top_logp", d, True), *_workspace(workspace, d), _stream()))
 
 
 def marl_log_prob_grad(logits, token, avail, scale, log_sum, entropy, grad_logp, grad_entropy, grad_logits):
     """Gradient of the logits; grad_logp [R] and grad_entropy [R] may be None.  grad_logits may be logits."""
-    code = _element(logits, "logits")
+    code, d = _element(logits, "logits"), _current_device()
     R, V = logits.shape
     check(load().marl_log_prob_grad(
-        code, R, V, *_rows(logits, logits.dtype, (R, V), "logits"), _flat(token, "i32", (R,), "token", True), *_avail_of(avail, R, V),
-        float(scale), _flat(log_sum, "f32", (R,), "log_sum"), _flat(entropy, "f32", (R,), "entropy", True),
-        _flat(grad_logp, "f32", (R,), "grad_logp", True), _flat(grad_entropy, "f32", (R,), "grad_entropy", True),
-        *_rows(grad_logits, logits.dtype, (R, V), "grad_logits"), _stream()))
+        code, R, V, *_rows(logits, logits.dtype, (R, V), "logits", d), _flat(token, "i32", (R,), "token", d, True), *_avail_of(avail, R, V, d),
+        float(scale), _flat(log_sum, "f32", (R,), "log_sum", d), _flat(entropy, "f32", (R,), "entropy", d, True),
+        _flat(grad_logp, "f32", (R,), "grad_logp", d, True), _flat(grad_entropy, "f32", (R,), "grad_entropy", d, True),
+        *_rows(grad_logits, logits.dtype, (R, V), "grad_logits", d), _stream()))
 
 
 NS_STEPS, NS_COEFFICIENTS, NS_EPS = 5, (3.4445, -4.7750, 2.0315), 1e-7
@@ -718,8 +724,8 @@ def marl_muon_workspace_bytes(dtype, L, rows, cols):
     return _bytes_of(load().marl_muon_workspace_bytes, _dtype_code(dtype), int(L), int(rows), int(cols))
 
 
-def _matrices(t, shape, dtype, name):
-    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda or t.device.index != _torch.cuda.current_device():
+def _matrices(t, shape, dtype, name, device):
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, "
                          f"got {t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
     return t.data_ptr()
@@ -739,23 +745,23 @@ def _coefficients(values):
 
 def marl_orthogonalize(matrix, out, workspace, steps=NS_STEPS, coefficients=NS_COEFFICIENTS, eps=NS_EPS):
     """Newton-Schulz iteration on matrix [rows,cols] or [L,rows,cols]; out may be matrix."""
-    code = _element(matrix, "matrix")
+    code, d = _element(matrix, "matrix"), _current_device()
     L, rows, cols = _batch_of(matrix)
     check(load().marl_orthogonalize(
-        code, L, rows, cols, _matrices(matrix, matrix.shape, matrix.dtype, "matrix"), _matrices(out, matrix.shape, matrix.dtype, "out"),
-        *_workspace(workspace), int(steps), _coefficients(coefficients), float(eps), _stream()))
+        code, L, rows, cols, _matrices(matrix, matrix.shape, matrix.dtype, "matrix", d), _matrices(out, matrix.shape, matrix.dtype, "out", d),
+        *_workspace(workspace, d), int(steps), _coefficients(coefficients), float(eps), _stream()))
 
 
 def marl_muon_step(weights, grad, momentum, weights_out, momentum_out, workspace, lr, beta=0.95, nesterov=True, weight_decay=0.0,
                    scale=1.0, steps=NS_STEPS, coefficients=NS_COEFFICIENTS, eps=NS_EPS):
     """Momentum, orthogonalisation and weight update of [rows,cols] or [L,rows,cols] matrices; momentum in fp32.  weights_out and
     momentum_out may be weights and momentum."""
-    code = _element(weights, "weights")
+    code, d = _element(weights, "weights"), _current_device()
     L, rows, cols = _batch_of(weights)
-    address = lambda t, name, dtype: _matrices(t, weights.shape, dtype, name)
+    address = lambda t, name, dtype: _matrices(t, weights.shape, dtype, name, d)
     f32 = _dtypes["f32"]
     check(load().marl_muon_step(
         code, L, rows, cols, address(weights, "weights", weights.dtype), address(grad, "grad", weights.dtype),
         address(momentum, "momentum", f32), address(weights_out, "weights_out", weights.dtype), address(momentum_out, "momentum_out", f32),
-        *_workspace(workspace), float(lr), float(beta), int(bool(nesterov)), float(weight_decay), float(scale), int(steps),
+        *_workspace(workspace, d), float(lr), float(beta), int(bool(nesterov)), float(weight_decay), float(scale), int(steps),
         _coefficients(coefficients), float(eps), _stream()))

@@ -38,7 +38,8 @@ inline bool small_fits(int rows, int cols)
 {
     if ((int64_t)rows * cols > kSmallEntries * kSmallThreads) return false;
     const SmallShape y = small_shape(rows, cols);
-    return y.bytes <= 159 * 1024 && (y.s / 16) * (y.l / 16) <= kSmallTurns * (kSmallThreads / kWave);
+    const int waves = kSmallThreads / kWave, ts = y.s / 16;
+    return y.bytes <= 159 * 1024 && ts <= waves && y.l / 16 <= kSmallTurns * (waves / ts);
 }
 
 struct SmallArgs {
@@ -113,18 +114,28 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
     }
     __syncthreads();
 
-    // 16 x 16 results of A B^T over K: rows 4 (lane / 16) + e of A, row lane % 16 of B
-    auto tile = [&](const _Float16 *A, int lda, int m0, const _Float16 *B, int ldb, int n0, int K) {
-        floatx4 acc = {0, 0, 0, 0}, cross = {0, 0, 0, 0};
+    // 16 x 16 results of A B^T over K: rows 4 (lane / 16) + e of A, row lane % 16 of B.  Of N tiles below one another, `down` rows
+    // of A apart, those there are: what bounds it is shared memory, and they share the reads of B.
+    auto tiles = [&](auto count, int there, const _Float16 *A, int lda, int m0, int down, const _Float16 *B, int ldb, int n0, int K, floatx4 *out) {
+        constexpr int N = decltype(count)::value;
+        floatx4 cross[N];
+#pragma unroll
+        for (int q = 0; q < N; ++q) out[q] = cross[q] = floatx4{0, 0, 0, 0};
         const _Float16 *pa = A + (m0 + (lane & 15)) * lda + 8 * (lane >> 4), *pb = B + (n0 + (lane & 15)) * ldb + 8 * (lane >> 4);
         for (int k = 0; k < K; k += 32) {
-            const half8 ah = *reinterpret_cast<const half8 *>(pa + 2 * k), al = *reinterpret_cast<const half8 *>(pa + 2 * k + 32);
             const half8 bh = *reinterpret_cast<const half8 *>(pb + 2 * k), bl = *reinterpret_cast<const half8 *>(pb + 2 * k + 32);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, acc, 0, 0, 0);
-            cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, cross, 0, 0, 0);
-            cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, cross, 0, 0, 0);
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                if (q < there) {
+                    const _Float16 *at = pa + q * down * lda + 2 * k;
+                    const half8 ah = *reinterpret_cast<const half8 *>(at), al = *reinterpret_cast<const half8 *>(at + 32);
+                    out[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, out[q], 0, 0, 0);
+                    cross[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, cross[q], 0, 0, 0);
+                    cross[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, cross[q], 0, 0, 0);
+                }
         }
-        return acc + cross;
+#pragma unroll
+        for (int q = 0; q < N; ++q) out[q] += cross[q];
     };
     auto put_along = [&](_Float16 *to, const floatx4 &v) {  // four entries along a row
         half4 h, l;
@@ -137,45 +148,49 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
     };
     const int ts = y.s / 16, waves = kSmallThreads / kWave;
     const int m4 = 4 * (lane >> 4), nn = lane & 15;
-    // a symmetric matrix: written once, in the order in which a lane holds it
+    // a symmetric matrix: tiles on and below the diagonal, and their mirror images
     auto square = [&](const _Float16 *A, int lda, int K, _Float16 *D, float alpha, float beta) {
-        for (int k = wave; k < ts * ts; k += waves) {
-            const int m0 = k / ts * 16, n0 = k % ts * 16;
-            floatx4 v = tile(A, lda, m0, A, lda, n0, K) * alpha;
+        for (int k = wave; k < ts * (ts + 1) / 2; k += waves) {
+            int i = 0;
+            while ((i + 1) * (i + 2) / 2 <= k) ++i;
+            const int m0 = i * 16, n0 = (k - i * (i + 1) / 2) * 16;
+            floatx4 v;
+            tiles(std::integral_constant<int, 1>{}, 1, A, lda, m0, 0, A, lda, n0, K, &v);
             const int at = (n0 + nn) * lds_s + plane_at<2>(m0 + m4);
+            v *= alpha;
             if (beta != 0.0f) {
                 const half4 h = *reinterpret_cast<const half4 *>(G + at), l = *reinterpret_cast<const half4 *>(G + at + 32);
                 for (int e = 0; e < 4; ++e) v[e] = fmaf(beta, (float)h[e] + (float)l[e], v[e]);
             }
             put_along(D + at, v);
+            if (m0 != n0)
+                for (int e = 0; e < 4; ++e) put(D + (m0 + m4 + e) * lds_s + plane_at<2>(n0 + nn), v[e]);
         }
         __syncthreads();
     };
+    // D [l][s] = T P: a wave has one column of tiles and every `side`-th row of them
+    const int side = waves / ts, n0 = wave % ts * 16, i0 = wave / ts, rows_of_tiles = y.l / 16;
+    const int there = i0 < side && i0 < rows_of_tiles ? (rows_of_tiles - i0 + side - 1) / side : 0;
     for (int step = 0; step < a.steps; ++step) {
         square(X, ldx, y.l, G, 1.0f / kPlaneScale, 0.0f);
         square(G, lds_s, y.s, P, a.c2 / kPlaneScale, a.c1);
-        // D [l][s] = T P; all of it is formed before any of X is overwritten
-        floatx4 held[kSmallTurns];
-        const int tiles = ts * (y.l / 16);
+        floatx4 held[kSmallTurns];                          // all of D is formed before any of X is overwritten
+        if (there) tiles(std::integral_constant<int, kSmallTurns>{}, there, T, lds_s, i0 * 16, side * 16, P, lds_s, n0, y.s, held);
 #pragma unroll
-        for (int q = 0; q < kSmallTurns; ++q) {
-            const int k = wave + q * waves, m0 = k / ts * 16, n0 = k % ts * 16;
-            if (k < tiles) {
-                held[q] = tile(T, lds_s, m0, P, lds_s, n0, y.s) * (1.0f / kPlaneScale);
-                const int at = (n0 + nn) * ldx + plane_at<2>(m0 + m4);
+        for (int q = 0; q < kSmallTurns; ++q)
+            if (q < there) {
+                const int at = (n0 + nn) * ldx + plane_at<2>((i0 + q * side) * 16 + m4);
                 const half4 h = *reinterpret_cast<const half4 *>(X + at), l = *reinterpret_cast<const half4 *>(X + at + 32);
-                for (int e = 0; e < 4; ++e) held[q][e] = fmaf(a.c0, (float)h[e] + (float)l[e], held[q][e]);
+                for (int e = 0; e < 4; ++e) held[q][e] = fmaf(a.c0, (float)h[e] + (float)l[e], held[q][e] * (1.0f / kPlaneScale));
             }
-        }
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < kSmallTurns; ++q) {
-            const int k = wave + q * waves, m0 = k / ts * 16, n0 = k % ts * 16;
-            if (k < tiles) {
+        for (int q = 0; q < kSmallTurns; ++q)
+            if (q < there) {
+                const int m0 = (i0 + q * side) * 16;
                 put_along(X + (n0 + nn) * ldx + plane_at<2>(m0 + m4), held[q]);
                 for (int e = 0; e < 4; ++e) put(T + (m0 + m4 + e) * lds_s + plane_at<2>(n0 + nn), held[q][e]);
             }
-        }
         __syncthreads();
     }
 #pragma unroll
