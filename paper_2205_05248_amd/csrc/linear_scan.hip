@@ -671,7 +671,7 @@ ScanPlan scan_plan(int dtype, int B, int T, int C)
     const int V = 4 / element_bytes(dtype), steps = V * kSteps, steps_back = 16;
     ScanPlan s{};
     s.waves = waves_for(T, steps, kMostWaves);
-    s.waves_back = waves_for(T, steps_back, kMostWavesBack);
+    s.waves_back = waves_for(T, steps_back, T <= kMostWaves * steps_back ? kMostWaves : kMostWavesBack);
     auto units = [&](int span) { return T > 0 ? (T + span - 1) / span : 1; };
     s.units = units(s.waves * steps);
     s.units_back = units(s.waves_back * steps_back);
