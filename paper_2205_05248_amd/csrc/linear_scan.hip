@@ -117,6 +117,11 @@ __device__ __forceinline__ StepBack step_back_of(float x, float r, float i, floa
 // All bits or none, after bit j of `bits`.
 __device__ __forceinline__ uint32_t all_of(unsigned bits, int j) { return (uint32_t)((int)(bits << (31 - j)) >> 31); }
 __device__ __forceinline__ float start_of(unsigned start, int j) { return __uint_as_float(all_of(start, j) & 0xc3480000u); }
+// v, or 0 where step j starts a sequence: a product with a = 0 would let an infinity or NaN of the sequence before through.
+__device__ __forceinline__ float unless_start(float v, unsigned start, int j) { return __uint_as_float(__float_as_uint(v) & ~all_of(start, j)); }
+// The same where stretches meet: what one does to the state, and what two do that follow one another.
+__device__ __forceinline__ float follow(float A, float h, float H) { return A == 0.0f ? H : fmaf(A, h, H); }
+__device__ __forceinline__ float both(float A, float B) { return A == 0.0f || B == 0.0f ? 0.0f : A * B; }
 
 // Four bytes of a row.  PAIRS: they lie at a multiple of four bytes and there is no odd channel at the end.
 // Held as one word: as a pair of 16-bit values the compiler gave each a register of its own wherever branches meet.
@@ -218,35 +223,46 @@ __device__ __forceinline__ Word word_of(float A, float H)
 __device__ __forceinline__ void publish(Word *at, float A, float H) { __hip_atomic_store(at, word_of(A, H), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ Word peek(const Word *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
+__device__ __forceinline__ float word_A(Word w) { return __uint_as_float((unsigned)(w >> 32) & 0x7fffffffu); }
+__device__ __forceinline__ float word_H(Word w) { return __uint_as_float((unsigned)w); }
+
 // The state at the start of a unit, a lane per channel.  Units publish (A, H) of their own steps at once, without waiting
 // for anything, and (0, h) of the state behind them when they know it; A = 0 says that nothing before matters.  Walking
-// backwards from unit `before` over whichever is there, `stride` words apart, until A = 0; the first unit publishes (0, h) alone.  A unit
-// waits only for units whose tickets are lower, and they began before it: each wait ends.
+// backwards from unit `before` over whichever is there, `stride` words apart, until A = 0; the first unit publishes (0, h) alone.
+// What was met is then applied in the order of time, one unit after the other, as each unit does for the state that it publishes:
+// the same sums in the same order whichever of the two words was there, so that timing does not change a bit.  The last of the
+// kDeep words that there is room for has to be (0, h).  A unit waits only for units whose tickets are lower, and they began before it:
+// each wait ends.
+constexpr int kDeep = 64;
 template <int kAtOnce>
-__device__ __forceinline__ float look_back(const Word *words, int before, int64_t stride, bool mine)
+__device__ __forceinline__ float look_back(const Word *words, int before, int64_t stride, bool mine, Word (*held)[kChannels])
 {
-    float A = 1.0f, H = 0.0f;
+    const int lane = threadIdx.x % kWave;
     bool open = mine;
+    int n = 0;
     for (int k = before; k >= 0 && __any(open); k -= kAtOnce) {
         Word w[kAtOnce];
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) w[j] = open && k - j >= 0 ? peek(words + (int64_t)(k - j) * stride) : 0;
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
-            if (k - j < 0) break;
-            while (__any(open && w[j] == 0)) {
+            if (k - j < 0 || !__any(open)) break;
+            const bool last = n == kDeep - 1;
+            while (__any(open && (w[j] == 0 || (last && word_A(w[j]) != 0.0f)))) {
                 __builtin_amdgcn_s_sleep(1);
-                if (open && w[j] == 0) w[j] = peek(words + (int64_t)(k - j) * stride);
+                if (open) w[j] = peek(words + (int64_t)(k - j) * stride);
             }
-            if (open) {
-                const float a = __uint_as_float((unsigned)(w[j] >> 32) & 0x7fffffffu);
-                H = fmaf(A, __uint_as_float((unsigned)w[j]), H);
-                A *= a;
-                open = a != 0.0f;
-            }
+            held[n++][lane] = open ? w[j] : 0;
+            open = open && word_A(w[j]) != 0.0f;
         }
     }
-    return H;
+    float h = 0.0f;
+#pragma unroll 4
+    while (n > 0) {
+        const Word w = held[--n][lane];
+        h = follow(word_A(w), h, word_H(w));
+    }
+    return h;
 }
 
 // Clears the words and the ticket and puts the first states aside (h_last may be h_first, and the last unit may be done with it
@@ -280,6 +296,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
     constexpr int V = kWide<E>, Tc = kSteps, kWaveSteps = V * Tc, kAll = (int)((1ull << kWaveSteps) - 1);
     __shared__ float rate_s[kChannels], A_s[NW][kChannels], H_s[NW][kChannels], carry_s[NW][kChannels];
     __shared__ int id_s;
+    __shared__ Word held_s[CHAIN ? kDeep : 1][kChannels];
     const Place at = place_of<CHAIN>(p, &id_s);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / (kWave / V), cl = lane % (kWave / V) * V;
     const int c = at.c0 + cl, left = p.C - c, first = at.unit * (NW * kWaveSteps), tw = first + wave * kWaveSteps;
@@ -338,14 +355,16 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
             const Step s = step_of(xv[v], rv[v], iv[v], rate2[v], begins);
             a[j][v] = s.a;
             u[j][v] = s.u;
-            H[v] = fmaf(s.a, H[v], s.u);
+            H[v] = fmaf(s.a, unless_start(H[v], start, j), s.u);
             A[v] *= s.a;
         }
     }
+    const bool cut = (start & ((1u << Tc) - 1)) != 0;          // nothing passes the lane's steps, whatever their other decays are
     // what the group before this one does, and the wave
     float A_before[V], H_before[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
+        A[v] = cut ? 0.0f : A[v];
         A_before[v] = 1.0f;
         H_before[v] = 0.0f;
         if constexpr (V == 2) {
@@ -353,8 +372,8 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
             if (group == 1) {
                 A_before[v] = pA;
                 H_before[v] = pH;
-                H[v] = fmaf(A[v], pH, H[v]);
-                A[v] *= pA;
+                H[v] = follow(A[v], pH, H[v]);
+                A[v] = both(A[v], pA);
             }
         }
         if (group == V - 1) { A_s[wave][cl + v] = A[v]; H_s[wave][cl + v] = H[v]; }
@@ -364,18 +383,18 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
         const int ch = at.c0 + lane;
         const bool mine = ch < p.C;
         float Aw = 1.0f, Hw = 0.0f;
-        for (int w = 0; w < NW; ++w) { Hw = fmaf(A_s[w][lane], Hw, H_s[w][lane]); Aw *= A_s[w][lane]; }
+        for (int w = 0; w < NW; ++w) { Hw = follow(A_s[w][lane], Hw, H_s[w][lane]); Aw = both(Aw, A_s[w][lane]); }
         float h = 0.0f;
         if constexpr (CHAIN) {
             const int64_t stride = (int64_t)p.sequences * kChannels;
             Word *own = p.words + (int64_t)at.seq * kChannels + lane;
             if (at.unit > 0) {
                 if (mine) publish(own + at.unit * stride, Aw, Hw);
-                h = look_back<4>(own, at.unit - 1, stride, mine);
+                h = look_back<4>(own, at.unit - 1, stride, mine, held_s);
             } else if (mine) {
                 h = p.h_first[(int64_t)at.b * p.C + ch];
             }
-            if (mine) publish(own + at.unit * stride, 0.0f, fmaf(Aw, h, Hw));
+            if (mine) publish(own + at.unit * stride, 0.0f, follow(Aw, h, Hw));
         } else if (mine && p.h_first) {
             h = p.h_first[(int64_t)at.b * p.C + ch];
         }
@@ -383,7 +402,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
             carry_s[w][lane] = h;
             const int t = first + w * kWaveSteps;
             if (mine && t < p.T && (t & ((1 << p.keep_log) - 1)) == 0) p.states[((int64_t)at.b * p.kept + (t >> p.keep_log)) * p.C + ch] = h;
-            h = fmaf(A_s[w][lane], h, H_s[w][lane]);
+            h = follow(A_s[w][lane], h, H_s[w][lane]);
         }
         if (mine && p.h_last && at.unit == p.units - 1) p.h_last[(int64_t)at.b * p.C + ch] = h;
     }
@@ -391,7 +410,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
     if (left <= 0) return;
     float h[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = fmaf(A_before[v], carry_s[wave][cl + v], H_before[v]);
+    for (int v = 0; v < V; ++v) h[v] = follow(A_before[v], carry_s[wave][cl + v], H_before[v]);
     Strip<E, PAIRS> sy(p.y, p.ld_y, row0, at.c0, cl, down);
     auto put = [&](auto whole) {                               // whole: every step exists and counts
 #pragma unroll
@@ -401,7 +420,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
             float out[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                h[v] = fmaf(a[j][v], h[v], u[j][v]);
+                h[v] = fmaf(a[j][v], unless_start(h[v], start, j), u[j][v]);
                 out[v] = h[v];
             }
             y.set(out);
@@ -422,6 +441,7 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
     constexpr int V = kWide<E>, Tc = kStepsBack<E>, kWaveSteps = V * Tc, kAll = (1 << kWaveSteps) - 1;
     __shared__ float rate_s[kChannels], A_s[NW][kChannels], H_s[NW][kChannels], R_s[NW][kChannels], carry_s[NW][kChannels], after_s[NW][kChannels];
     __shared__ int id_s;
+    __shared__ Word held_s[CHAIN ? kDeep : 1][kChannels];
     const Place at = place_of<CHAIN>(p, &id_s);
     const int unit = p.units - 1 - at.unit;                    // the last steps first
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / (kWave / V), cl = lane % (kWave / V) * V;
@@ -484,7 +504,7 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             q[j][v] = step_back_of(xv[v], rv[v], iv[v], -kLog2e * rate[v], begins);
-            H[v] = fmaf(q[j][v].a, H[v], q[j][v].u);
+            H[v] = fmaf(q[j][v].a, unless_start(H[v], start, j), q[j][v].u);
             A[v] *= q[j][v].a;
         }
     }
@@ -493,18 +513,20 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
         float gv[V];
         g[j].get(gv);
 #pragma unroll
-        for (int v = 0; v < V; ++v) R[v] = q[j][v].a * (gv[v] + R[v]);
+        for (int v = 0; v < V; ++v) R[v] = unless_start(q[j][v].a * (gv[v] + R[v]), start, j);
     }
+    const bool cut = (start & ((1u << Tc) - 1)) != 0;          // nothing passes the lane's steps, whatever their other decays are
     float A_before[V], H_before[V], A_after[V], R_after[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
+        A[v] = cut ? 0.0f : A[v];
         A_before[v] = A_after[v] = 1.0f;
         H_before[v] = R_after[v] = 0.0f;
         if constexpr (V == 2) {
             const float oA = __shfl_xor(A[v], 32), oH = __shfl_xor(H[v], 32), oR = __shfl_xor(R[v], 32);
-            if (group == 1) { A_before[v] = oA; H_before[v] = oH; H[v] = fmaf(A[v], oH, H[v]); }
-            else { A_after[v] = oA; R_after[v] = oR; R[v] = fmaf(A[v], oR, R[v]); }
-            A[v] *= oA;
+            if (group == 1) { A_before[v] = oA; H_before[v] = oH; H[v] = follow(A[v], oH, H[v]); }
+            else { A_after[v] = oA; R_after[v] = oR; R[v] = follow(A[v], oR, R[v]); }
+            A[v] = both(A[v], oA);
         }
         if (group == V - 1) { A_s[wave][cl + v] = A[v]; H_s[wave][cl + v] = H[v]; }
         if (group == 0) R_s[wave][cl + v] = R[v];
@@ -516,29 +538,29 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
         float h = mine && p.T > 0 ? p.states[((int64_t)at.b * p.kept + unit) * p.C + ch] : 0.0f;
         float D = 0.0f, Aw = 1.0f, Rw = 0.0f;
 #pragma unroll 1
-        for (int w = NW - 1; w >= 0; --w) { Rw = fmaf(A_s[w][lane], Rw, R_s[w][lane]); Aw *= A_s[w][lane]; }
+        for (int w = NW - 1; w >= 0; --w) { Rw = follow(A_s[w][lane], Rw, R_s[w][lane]); Aw = both(Aw, A_s[w][lane]); }
         if constexpr (CHAIN) {
             const int64_t stride = (int64_t)p.sequences * kChannels;
             Word *own = p.words + (int64_t)at.seq * kChannels + lane;
             if (at.unit > 0) {
                 if (mine) publish(own + at.unit * stride, Aw, Rw);
-                D = look_back<1>(own, at.unit - 1, stride, mine);
+                D = look_back<1>(own, at.unit - 1, stride, mine, held_s);
             } else if (mine) {
                 D = p.grad_h_last[(int64_t)at.b * p.C + ch];
             }
-            if (mine) publish(own + at.unit * stride, 0.0f, fmaf(Aw, D, Rw));
+            if (mine) publish(own + at.unit * stride, 0.0f, follow(Aw, D, Rw));
         } else if (mine && p.grad_h_last) {
             D = p.grad_h_last[(int64_t)at.b * p.C + ch];
         }
 #pragma unroll 1
         for (int w = 0; w < NW; ++w) {
             carry_s[w][lane] = h;
-            h = fmaf(A_s[w][lane], h, H_s[w][lane]);
+            h = follow(A_s[w][lane], h, H_s[w][lane]);
         }
 #pragma unroll 1
         for (int w = NW - 1; w >= 0; --w) {
             after_s[w][lane] = D;
-            D = fmaf(A_s[w][lane], D, R_s[w][lane]);
+            D = follow(A_s[w][lane], D, R_s[w][lane]);
         }
         if (mine && p.grad_h_first && unit == 0) p.grad_h_first[(int64_t)at.b * p.C + ch] = D;
     }
@@ -547,10 +569,11 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         sum[v] = 0.0f;
-        D[v] = fmaf(A_after[v], after_s[wave][cl + v], R_after[v]);
-        float h = fmaf(A_before[v], carry_s[wave][cl + v], H_before[v]);
+        D[v] = follow(A_after[v], after_s[wave][cl + v], R_after[v]);
+        float h = follow(A_before[v], carry_s[wave][cl + v], H_before[v]);
 #pragma unroll
         for (int j = 0; j < Tc; ++j) {
+            h = unless_start(h, start, j);
             q[j][v].q = h - q[j][v].q;
             h = fmaf(q[j][v].a, h, q[j][v].u);
         }
@@ -571,7 +594,7 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
                 const float dh = gv[v] + D[v];
                 dx[v] = dh * k.m;
                 di[v] = dh * k.n;
-                D[v] = k.a * dh;
+                D[v] = unless_start(k.a * dh, start, j);
                 const float part = k.s * (D[v] * k.q);
                 dr[v] = -rate[v] * fmaf(-k.s, part, part);
                 sum[v] -= part;

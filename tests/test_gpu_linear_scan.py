@@ -252,3 +252,54 @@ def test_table_rows_out_of_range_are_clamped():
     binding.marl_linear_step(d["x"], d["r"], d["i"], d["lam"], DECAY, torch.tensor([-5, 99], dtype=torch.int32, device="cuda"), None, table, out, y)
     torch.cuda.synchronize()
     assert torch.equal(out[0], y[0]) and torch.equal(out[3], y[1]) and (out[1:3] == 1).all()
+
+
+@pytest.mark.parametrize("T,C,dtype", [(30000, 64, "fp32"), (9000, 640, "bf16")])
+def test_same_bits_beside_other_work(T, C, dtype):
+    """When units begin and how long they take is not what decides about the order of a sum."""
+    s = make(1, T, C, dtype, 20)
+    d = on_gpu(s)
+    first = outputs(d)
+    run(d, first)
+    torch.cuda.synchronize()
+    side, big = torch.cuda.Stream(), torch.zeros(1 << 24, device="cuda")
+    for n in range(6):
+        o = outputs(d)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(2 * n):
+                big.add_(1.0)
+        run(d, o)
+        torch.cuda.synchronize()
+        for k in first:
+            if k != "ws":
+                assert torch.equal(first[k], o[k]), (n, k)
+
+
+@pytest.mark.parametrize("B,T,C", [(2, 9, 3), (1, 90, 70), (2, 700, 66)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_reset_lets_nothing_through(B, T, C, dtype, value):
+    """What a sequence holds, or its gradient, infinities and NaN too, reaches neither the next one nor the one before."""
+    s = make(B, T, C, dtype, 21)
+    cut = T // 3, 2 * T // 3                                       # three sequences a row; the middle one is spoiled
+    s["reset"] = torch.zeros(B, T, dtype=torch.uint8)
+    s["reset"][:, 0] = 1
+    s["reset"][:, cut[0]], s["reset"][:, cut[1]] = 1, 1
+    clean_in = on_gpu(s)
+    clean = outputs(clean_in)
+    run(clean_in, clean)
+    at = (cut[0] + cut[1]) // 2
+    s["xri"][0, at, 0, C // 2] = value
+    s["xri"][0, cut[0] + 1, 1, C - 1] = float("nan")               # a gate: the decay itself is NaN
+    s["grad_y"][0, at, 0] = value
+    s["h_first"][0, C // 2] = value                                # a table's row that was never written
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    for k in ("y", "grad_x", "grad_r", "grad_i"):
+        for part in (slice(0, cut[0]), slice(cut[1], T)):
+            assert torch.equal(o[k][:, part], clean[k][:, part]), (k, part)
+    assert torch.equal(o["h_last"], clean["h_last"]) and torch.equal(o["grad_h_first"], clean["grad_h_first"])
+    assert not torch.isfinite(o["y"][0, at, C // 2]) and torch.isnan(o["y"][0, at, C - 1])
