@@ -243,21 +243,21 @@ __device__ __forceinline__ float look_back(const Word *words, int before, int64_
     for (int k = before; k >= 0 && __any(open); k -= kAtOnce) {
         Word w[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) w[j] = open && k - j >= 0 ? peek(words + (int64_t)(k - j) * stride) : 0;
+        for (int j = 0; j < kAtOnce; ++j) w[j] = open && k - j >= 0 ? peek(words + (int64_t)(k - j) * stride + lane) : 0;
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             if (k - j < 0 || !__any(open)) break;
             const bool last = n == kDeep - 1;
             while (__any(open && (w[j] == 0 || (last && word_A(w[j]) != 0.0f)))) {
                 __builtin_amdgcn_s_sleep(1);
-                if (open) w[j] = peek(words + (int64_t)(k - j) * stride);
+                if (open) w[j] = peek(words + (int64_t)(k - j) * stride + lane);
             }
             held[n++][lane] = open ? w[j] : 0;
             open = open && word_A(w[j]) != 0.0f;
         }
     }
     float h = 0.0f;
-#pragma unroll 4
+#pragma unroll kAtOnce
     while (n > 0) {
         const Word w = held[--n][lane];
         h = follow(word_A(w), h, word_H(w));
@@ -387,14 +387,14 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
         float h = 0.0f;
         if constexpr (CHAIN) {
             const int64_t stride = (int64_t)p.sequences * kChannels;
-            Word *own = p.words + (int64_t)at.seq * kChannels + lane;
+            Word *own = p.words + (int64_t)at.seq * kChannels;
             if (at.unit > 0) {
-                if (mine) publish(own + at.unit * stride, Aw, Hw);
+                if (mine) publish(own + at.unit * stride + lane, Aw, Hw);
                 h = look_back<4>(own, at.unit - 1, stride, mine, held_s);
             } else if (mine) {
                 h = p.h_first[(int64_t)at.b * p.C + ch];
             }
-            if (mine) publish(own + at.unit * stride, 0.0f, follow(Aw, h, Hw));
+            if (mine) publish(own + at.unit * stride + lane, 0.0f, follow(Aw, h, Hw));
         } else if (mine && p.h_first) {
             h = p.h_first[(int64_t)at.b * p.C + ch];
         }
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = follow(A_before[v], carry_s[wave][cl + v], H_before[v]);
     Strip<E, PAIRS> sy(p.y, p.ld_y, row0, at.c0, cl, down);
-    auto put = [&](auto whole) {                               // whole: every step exists and counts
+    auto put = [&](auto whole) {                               // whole: every step exists and counts, and none starts a sequence
 #pragma unroll
         for (int j = 0; j < Tc; ++j) {
             __builtin_amdgcn_sched_barrier(0);
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
             float out[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                h[v] = fmaf(a[j][v], unless_start(h[v], start, j), u[j][v]);
+                h[v] = fmaf(a[j][v], whole ? h[v] : unless_start(h[v], start, j), u[j][v]);
                 out[v] = h[v];
             }
             y.set(out);
@@ -429,7 +429,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
             sy.base += sy.step;
         }
     };
-    if (steps.filled == (unsigned)kAll) put(std::true_type{});
+    if (steps.filled == (unsigned)kAll && !steps.start) put(std::true_type{});
     else put(std::false_type{});
 }
 
@@ -541,14 +541,14 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
         for (int w = NW - 1; w >= 0; --w) { Rw = follow(A_s[w][lane], Rw, R_s[w][lane]); Aw = both(Aw, A_s[w][lane]); }
         if constexpr (CHAIN) {
             const int64_t stride = (int64_t)p.sequences * kChannels;
-            Word *own = p.words + (int64_t)at.seq * kChannels + lane;
+            Word *own = p.words + (int64_t)at.seq * kChannels;
             if (at.unit > 0) {
-                if (mine) publish(own + at.unit * stride, Aw, Rw);
+                if (mine) publish(own + at.unit * stride + lane, Aw, Rw);
                 D = look_back<1>(own, at.unit - 1, stride, mine, held_s);
             } else if (mine) {
                 D = p.grad_h_last[(int64_t)at.b * p.C + ch];
             }
-            if (mine) publish(own + at.unit * stride, 0.0f, follow(Aw, D, Rw));
+            if (mine) publish(own + at.unit * stride + lane, 0.0f, follow(Aw, D, Rw));
         } else if (mine && p.grad_h_last) {
             D = p.grad_h_last[(int64_t)at.b * p.C + ch];
         }
@@ -581,7 +581,7 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
     const int64_t last = row0 + Tc - 1;                        // (of group 0)
     Strip<E, PAIRS> sgx(p.grad_x, p.ld_gx, last, at.c0, cl, down), sgr(p.grad_r, p.ld_gr, last, at.c0, cl, down),
         sgi(p.grad_i, p.ld_gi, last, at.c0, cl, down);
-    auto put = [&](auto whole) {                               // whole: every step exists and counts
+    auto put = [&](auto whole) {                               // whole: every step exists and counts, and none starts a sequence
 #pragma unroll
         for (int j = Tc - 1; j >= 0; --j) {
             __builtin_amdgcn_sched_barrier(0);
@@ -594,7 +594,7 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
                 const float dh = gv[v] + D[v];
                 dx[v] = dh * k.m;
                 di[v] = dh * k.n;
-                D[v] = unless_start(k.a * dh, start, j);
+                D[v] = whole ? k.a * dh : unless_start(k.a * dh, start, j);
                 const float part = k.s * (D[v] * k.q);
                 dr[v] = -rate[v] * fmaf(-k.s, part, part);
                 sum[v] -= part;
@@ -612,7 +612,7 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
             sgi.base -= sgi.step;
         }
     };
-    if (steps.filled == (unsigned)kAll) put(std::true_type{});
+    if (steps.filled == (unsigned)kAll && !steps.start) put(std::true_type{});
     else put(std::false_type{});
     // the unit's part of the sum for lam: groups, then waves, in order
 #pragma unroll
