@@ -176,9 +176,9 @@ bool sizes_ok(int L, int rows, int cols) { return L >= 0 && L <= 65535 && rows >
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 // ---- which tiles a product takes
-struct Plan { int shape, splits; };                // shape: 0 of 256 x 256, 1 of 128 x 128, 2 of 64 x 64 results
+struct Plan { int shape, splits; };                // shape: 0 of 256 x 256, 1 of 128 x 128, 2 of 64 x 64 results, 3 as 1 by two groups of waves
 
-constexpr int kSide[3] = {256, 128, 64};
+constexpr int kSide[4] = {256, 128, 64, 128};
 
 int tiles_of(int shape, int Mp, int Np, bool symmetric)
 {
@@ -188,11 +188,16 @@ int tiles_of(int shape, int Mp, int Np, bool symmetric)
 
 Plan plan_of(int L, int Mp, int Np, bool symmetric, int stages)
 {
+    // The largest tile of which half the compute units get one.  A G or P that still leaves compute units without one and is long
+    // enough to pay for a second pass over its sums (2048 x 8192 bf16, G: 70 us, 92 in one part) goes in parts.
     Plan best{2, 1};
     for (int shape = 0; shape < 3; ++shape)
         if ((int64_t)tiles_of(shape, Mp, Np, symmetric) * L >= 128) { best.shape = shape; break; }
     const int64_t tiles = (int64_t)tiles_of(best.shape, Mp, Np, symmetric) * L;
-    if (symmetric && stages >= 64 && tiles < 256) best.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, stages / 16));
+    if (symmetric && stages >= 128 && tiles < 256) best.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, stages / 16));
+    // One 128 x 128 tile on a compute unit: two groups of waves, each with half of the sum, keep it busier than one (2048 x 2048 fp32:
+    // 3 us less a G or P, 6 an X; with more tiles two workgroups do that, and this would cost 28 us of 2048 x 8192 bf16's X).
+    if (best.shape == 1 && best.splits == 1 && tiles <= 256) best.shape = 3;
     return best;
 }
 
@@ -246,7 +251,7 @@ int launch_product(Product p, int L, hipStream_t stream)
         }
     }
     hipLaunchKernelGGL((product_kernel<S, E>), dim3((unsigned)(p.tiles * p.splits), (unsigned)L), dim3(S::kThreads), S::kLds, stream, p);
-    if (p.splits > 1) hipLaunchKernelGGL((join_kernel<S, E>), dim3((unsigned)p.tiles, (unsigned)L), dim3(S::kThreads), S::kLds, stream, p);
+    if (p.splits > 1) hipLaunchKernelGGL((join_kernel<S, E>), dim3((unsigned)p.tiles, (unsigned)L), dim3(S::kTileThreads), S::kLds, stream, p);
     return MARL_OK;
 }
 
@@ -258,7 +263,8 @@ int product(Product p, int L, hipStream_t stream)
     switch (plan.shape) {
     case 0: return launch_product<TileShape<PL, 2, 4, 4, 2, 2>, E>(p, L, stream);
     case 1: return launch_product<TileShape<PL, 2, 2, 2, 2, 2>, E>(p, L, stream);
-    default: return launch_product<TileShape<PL, 2, 2, 1, 1, 4>, E>(p, L, stream);
+    case 2: return launch_product<TileShape<PL, 2, 2, 1, 1, 4>, E>(p, L, stream);
+    default: return launch_product<TileShape<PL, 2, 2, 2, 2, 2, 2>, E>(p, L, stream);
     }
 }
 

@@ -52,16 +52,20 @@ struct Product {
 template <int PL>
 __host__ __device__ __forceinline__ int plane_at(int k) { return PL == 1 ? k : (k >> 5) * 64 + (k & 31); }
 
-template <int PL_, int WM_, int WN_, int MT_, int NT_, int BUFFERS_>
+// KW groups of WM x WN waves take the stages of the sum in turn and put their results together at the end: where there are fewer tiles
+// than compute units, the time of a product is that of one workgroup's stages one after the other.
+template <int PL_, int WM_, int WN_, int MT_, int NT_, int BUFFERS_, int KW_ = 1>
 struct TileShape {
-    static constexpr int PL = PL_, WM = WM_, WN = WN_, MT = MT_, NT = NT_, kBuffers = BUFFERS_;
-    static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
+    static constexpr int PL = PL_, WM = WM_, WN = WN_, MT = MT_, NT = NT_, kBuffers = BUFFERS_, KW = KW_;
+    static constexpr int kWaves = WM * WN, kTileThreads = kWaves * kWave, kThreads = KW * kTileThreads;
     static constexpr int TM = WM * MT * 32, TN = WN * NT * 32;
     static constexpr int kStage = (TM + TN) * 128;                     // bytes: 64 fp16 values of every row
     static constexpr int kPitch = 32 * MT + 4;                         // a staged row of results, fp32 values
     static constexpr int kStaging = 32 * kPitch * 4;                   // bytes a wave: 32 columns of its results
-    static constexpr int kLds = kBuffers * kStage > kWaves * kStaging ? kBuffers * kStage : kWaves * kStaging;
     static constexpr int kQuads = 4 * MT * NT;                         // groups of four accumulators of a lane
+    static constexpr int kJoining = (KW - 1) * kQuads * kTileThreads * 16;                 // bytes: what the groups behind the first hand over
+    static constexpr int kMost = kWaves * kStaging > kJoining ? kWaves * kStaging : kJoining;
+    static constexpr int kLds = kBuffers * KW * kStage > kMost ? kBuffers * KW * kStage : kMost;
 };
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -205,7 +209,8 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     constexpr int PL = S::PL, MT = S::MT, NT = S::NT, TM = S::TM, TN = S::TN;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave % S::kWaves;
+    const int group = S::KW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / S::kTileThreads);
     const int units = p.tiles * p.splits;
     const int unit = die_order(blockIdx.x, units), tile = unit % p.tiles, split = unit / p.tiles;
     const int64_t batch = blockIdx.y;
@@ -227,8 +232,10 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
 #pragma unroll
     for (int q = 0; q < kLoadsB; ++q)
         from_b[q] = p.B + batch * p.b_batch + (int64_t)min(n0 + (q * S::kWaves + wave) * 8 + sub, p.Np - 1) * p.ldb + chunk * 8;
-    auto load = [&](int k, int buffer) {
-        char *to = lds + buffer * S::kStage;
+    const int turns = (k_end - k_begin + S::KW - 1) / S::KW;           // stages of a group; the last may be one behind the end
+    auto load = [&](int turn, int buffer) {
+        char *to = lds + (buffer * S::KW + group) * S::kStage;
+        const int k = min(k_begin + min(turn, turns - 1) * S::KW + group, k_end - 1);
 #pragma unroll
         for (int q = 0; q < kLoadsA; ++q)
             __builtin_amdgcn_global_load_lds((global_void *)(from_a[q] + (int64_t)k * 64), (lds_void *)(to + (q * S::kWaves + wave) * 1024), 16, 0, 0);
@@ -245,7 +252,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
             for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
 
     const int row = lane & 31, high = lane >> 5;
-    const char *read_a = lds + ((wave / S::WN) * MT * 32 + row) * 128, *read_b = lds + TM * 128 + ((wave % S::WN) * NT * 32 + row) * 128;
+    const char *read_a = lds + group * S::kStage + ((wave / S::WN) * MT * 32 + row) * 128, *read_b = lds + group * S::kStage + TM * 128 + ((wave % S::WN) * NT * 32 + row) * 128;
     auto frag = [&](const char *base, int block, int c) {
         return *reinterpret_cast<const half8 *>(base + block * 32 * 128 + ((c ^ (row / 2 & 7)) << 4));
     };
@@ -255,7 +262,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
     constexpr int kInStage = 4 / PL;
     half8 a[2][PL][MT], b[2][PL][NT];
     auto read = [&](int set, int buffer, int j) {
-        const char *ra = read_a + buffer * S::kStage, *rb = read_b + buffer * S::kStage;
+        const char *ra = read_a + buffer * (S::KW * S::kStage), *rb = read_b + buffer * (S::KW * S::kStage);
 #pragma unroll
         for (int pl = 0; pl < PL; ++pl) {
 #pragma unroll
@@ -296,12 +303,12 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
         __builtin_amdgcn_sched_group_barrier(0x008, kProducts, 0);
     };
 #pragma unroll
-    for (int q = 0; q < S::kBuffers - 1; ++q) load(min(k_begin + q, k_end - 1), q);    // (every part has a stage at least)
+    for (int q = 0; q < S::kBuffers - 1; ++q) load(q, q);              // (every part has a stage at least)
     arrive();
-    load(min(k_begin + S::kBuffers - 1, k_end - 1), S::kBuffers - 1);
+    load(S::kBuffers - 1, S::kBuffers - 1);
     read(0, 0, 0);
     int buffer = 0;
-    for (int k = k_begin; k + 1 < k_end; ++k) {
+    for (int turn = 0; turn + 1 < turns; ++turn) {
         const int next = buffer + 1 == S::kBuffers ? 0 : buffer + 1;
 #pragma unroll
         for (int j = 0; j < kInStage; ++j) {
@@ -309,7 +316,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
                 read((j + 1) & 1, buffer, j + 1);
             } else {
                 arrive();
-                load(min(k + S::kBuffers, k_end - 1), buffer);         // (behind the last stage: once more, and not read)
+                load(turn + S::kBuffers, buffer);                      // (behind the last stage: once more, and not read)
                 read((j + 1) & 1, next, 0);
             }
             products(j & 1);
@@ -318,30 +325,62 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
         }
         buffer = next;
     }
+    if (S::KW == 1 || k_begin + (turns - 1) * S::KW + group < k_end) {
 #pragma unroll
-    for (int j = 0; j < kInStage; ++j) {
-        if (j + 1 < kInStage) read((j + 1) & 1, buffer, j + 1);
-        products(j & 1);
+        for (int j = 0; j < kInStage; ++j) {
+            if (j + 1 < kInStage) read((j + 1) & 1, buffer, j + 1);
+            products(j & 1);
+        }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                   // nothing may still be on its way into the buffers
+    if constexpr (S::KW > 1) {                                         // the groups' sums, in order
+        __syncthreads();
+        floatx4 *to = reinterpret_cast<floatx4 *>(lds) + threadIdx.x % S::kTileThreads;
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+            for (int b = 0; b < NT; ++b)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int quad = (a * NT + b) * 4 + q;
+                    if (group > 0)
+                        to[((group - 1) * S::kQuads + quad) * S::kTileThreads] = floatx4{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+                }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int a = 0; a < MT; ++a)
+#pragma unroll
+                for (int b = 0; b < NT; ++b)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int g = 0; g < S::KW - 1; ++g) {
+                            const floatx4 more = to[(g * S::kQuads + (a * NT + b) * 4 + q) * S::kTileThreads];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[a][b][4 * q + e] += more[e];
+                        }
+        }
+    }
+    __syncthreads();                                                   // the buffers become staging room
+    if (group > 0) return;
     if (p.splits > 1) {
-        floatx4 *to = reinterpret_cast<floatx4 *>(p.partial) + ((batch * p.tiles + tile) * p.splits + split) * (S::kQuads * S::kThreads) + threadIdx.x;
+        floatx4 *to = reinterpret_cast<floatx4 *>(p.partial) + ((batch * p.tiles + tile) * p.splits + split) * (S::kQuads * S::kTileThreads) + threadIdx.x;
 #pragma unroll
         for (int a = 0; a < MT; ++a)
 #pragma unroll
             for (int b = 0; b < NT; ++b)
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    to[((a * NT + b) * 4 + q) * S::kThreads] = floatx4{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+                    to[((a * NT + b) * 4 + q) * S::kTileThreads] = floatx4{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
         return;
     }
-    __syncthreads();                                                   // the buffers become staging room
     put_tile<S, E>(p, batch, m0, n0, p.symmetric && ti == tj, acc, lds);
 }
 
 // Sums the parts of a tile, in order, and finishes it.
 template <class S, typename E>
-__global__ __launch_bounds__(S::kThreads) void join_kernel(Product p)
+__global__ __launch_bounds__(S::kTileThreads) void join_kernel(Product p)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int64_t batch = blockIdx.y;
@@ -349,7 +388,7 @@ __global__ __launch_bounds__(S::kThreads) void join_kernel(Product p)
     int ti, tj;
     tile_of(p, tile, ti, tj);
     floatx16 acc[S::MT][S::NT];
-    const floatx4 *from = reinterpret_cast<const floatx4 *>(p.partial) + (batch * p.tiles + tile) * p.splits * (S::kQuads * S::kThreads) + threadIdx.x;
+    const floatx4 *from = reinterpret_cast<const floatx4 *>(p.partial) + (batch * p.tiles + tile) * p.splits * (S::kQuads * S::kTileThreads) + threadIdx.x;
 #pragma unroll
     for (int a = 0; a < S::MT; ++a)
 #pragma unroll
@@ -357,7 +396,7 @@ __global__ __launch_bounds__(S::kThreads) void join_kernel(Product p)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 floatx4 sum = {0, 0, 0, 0};
-                for (int s = 0; s < p.splits; ++s) sum += from[(s * S::kQuads + (a * S::NT + b) * 4 + q) * S::kThreads];
+                for (int s = 0; s < p.splits; ++s) sum += from[(s * S::kQuads + (a * S::NT + b) * 4 + q) * S::kTileThreads];
                 for (int e = 0; e < 4; ++e) acc[a][b][4 * q + e] = sum[e];
             }
     put_tile<S, E>(p, batch, ti * S::TM, tj * S::TN, p.symmetric && ti == tj, acc, lds);
