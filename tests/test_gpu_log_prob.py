@@ -237,3 +237,28 @@ def test_replayed_from_a_graph_and_on_another_stream(R, V, K):
         torch.cuda.synchronize()
         for a, b in zip(got[:6], want[:6]):
             assert torch.equal(a, b), k
+
+
+@pytest.mark.parametrize("V", [8187, 8192, 8193, 16384, 18437])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shift", [0, 1, 3])
+@pytest.mark.parametrize("avail", ["none", "rows"])
+def test_long_rows_that_begin_anywhere(V, dtype, shift, avail):
+    """Ends of a row on either side of a workgroup's pieces, rows and outputs at differing alignments; nothing beside the row is
+    read into it or written."""
+    s = make(5, V, dtype, 12 + shift, avail)
+    R, ld = 5, V + 5
+    wide = torch.full((R, ld), 1e4, dtype=DT[dtype], device="cuda")    # what a read beside the row would find
+    logits = wide[:, shift:shift + V]
+    logits.copy_(s["logits"])
+    avail_t = None if s["avail"] is None else s["avail"].cuda()
+    token = s["token"].cuda()
+    o = {k: torch.empty(R, device="cuda") for k in ("logp", "entropy", "log_sum")}
+    ws = torch.empty(max(1, binding.marl_log_prob_workspace_bytes(R, V, 0)), dtype=torch.uint8, device="cuda")
+    out = torch.full((R, V + 2), 7.0, dtype=DT[dtype], device="cuda")
+    binding.marl_log_prob(logits, token, avail_t, 1.1, o["logp"], o["entropy"], o["log_sum"], workspace=ws)
+    binding.marl_log_prob_grad(logits, token, avail_t, 1.1, o["log_sum"], o["entropy"], s["grad_logp"].cuda(), s["grad_entropy"].cuda(), out[:, 1:V + 1])
+    torch.cuda.synchronize()
+    assert (out[:, 0] == 7).all() and (out[:, V + 1] == 7).all()
+    o["grad"] = out[:, 1:V + 1].contiguous()
+    check(s, o, 1.1, 0)
