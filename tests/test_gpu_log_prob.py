@@ -262,3 +262,33 @@ def test_long_rows_that_begin_anywhere(V, dtype, shift, avail):
     assert (out[:, 0] == 7).all() and (out[:, V + 1] == 7).all()
     o["grad"] = out[:, 1:V + 1].contiguous()
     check(s, o, 1.1, 0)
+
+
+@pytest.mark.parametrize("V", [1, 3, 16, 17, 40, 63, 64, 65, 200, 255, 256])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("avail", ["none", "rows", "shared"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_short_rows_without_gaps(V, dtype, avail, in_place):
+    """Full and partial waves, tensors that begin anywhere; nothing beside them is read into a row or written."""
+    for R, shift in ((1, 0), (67, 1), (129, 3)):
+        s = make(R, V, dtype, 13, avail)
+        whole = torch.full((R * V + 32,), 1e4, dtype=DT[dtype], device="cuda")
+        logits = whole[16 + shift:16 + shift + R * V].view(R, V)
+        logits.copy_(s["logits"])
+        avail_t = None
+        if s["avail"] is not None:
+            bytes_ = torch.zeros(s["avail"].numel() + 32, dtype=torch.uint8, device="cuda")
+            avail_t = bytes_[5 + shift:5 + shift + s["avail"].numel()].view(s["avail"].shape)
+            avail_t.copy_(s["avail"])
+        token = s["token"].cuda()
+        o = {k: torch.empty(R, device="cuda") for k in ("logp", "entropy", "log_sum")}
+        binding.marl_log_prob(logits, token, avail_t, 0.9, o["logp"], o["entropy"], o["log_sum"])
+        room = whole if in_place else torch.full((R * V + 32,), 1e4, dtype=DT[dtype], device="cuda")
+        lead = 16 + shift if in_place else 16
+        grad = room[lead:lead + R * V].view(R, V)
+        binding.marl_log_prob_grad(logits, token, avail_t, 0.9, o["log_sum"], o["entropy"], s["grad_logp"].cuda(), s["grad_entropy"].cuda(), grad)
+        torch.cuda.synchronize()
+        beside = torch.full((), 1e4, dtype=DT[dtype], device="cuda")
+        assert (room[:lead] == beside).all() and (room[lead + R * V:] == beside).all()
+        o["grad"] = grad.clone()
+        check(s, o, 0.9, 0)
