@@ -407,7 +407,9 @@ struct FlatRows {
     static constexpr int kMost = kWave * N;
     E entries[kStretch<E, kMost>];
     uint8_t mask[kStretch<uint8_t, kMost>];
-    __device__ __forceinline__ int read(const LogProbArgs &p, int64_t first, int64_t row, bool there, float (&held)[N])
+    // token: of the lane's row, or -1; its logit and whether it is available are left in `taken`
+    struct Taken { float logit; bool available; };
+    __device__ __forceinline__ Taken read(const LogProbArgs &p, int64_t first, int64_t row, bool there, int token, float (&held)[N])
     {
         const int sub = threadIdx.x % G, rows = (int)min((int64_t)(kWave / G), p.R - first);
         const int64_t at = first * p.V, total = (int64_t)p.R * p.V;
@@ -422,8 +424,11 @@ struct FlatRows {
             const bool is = there && k < p.V && (!p.avail || (own ? mask[skew_m + in + k] : p.avail[k]));
             held[j] = is ? to_f32(entries[skew + in + k]) : -kInf;
         }
+        const bool in_row = there && token >= 0 && token < p.V;
+        const Taken taken{in_row ? to_f32(entries[skew + in + token]) : -kInf,
+                          in_row && (!p.avail || (own ? mask[skew_m + in + token] : p.avail[token]))};
         wave_sync();
-        return skew;
+        return taken;
     }
 };
 
@@ -438,12 +443,16 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(LogProbArgs p)
     const E *l = static_cast<const E *>(p.logits) + (there ? row : 0) * p.ld;
     const uint8_t *av = p.avail ? p.avail + (there ? row : 0) * p.ld_avail : nullptr;
     float held[N];
+    const int token = there && p.logp ? p.token[row] : -1;
+    typename FlatRows<E, G, N>::Taken taken;
     if constexpr (FLAT) {
         __shared__ __attribute__((aligned(16))) FlatRows<E, G, N> rows[kThreads / kWave];
         const int64_t first = ((int64_t)blockIdx.x * (kThreads / kWave) + wave) * (kWave / G);
         if (first >= p.R) return;                                      // the whole wave
-        rows[wave].read(p, first, row, there, held);
+        taken = rows[wave].read(p, first, row, there, token, held);
     } else {
+        const bool in = token >= 0 && token < p.V;
+        taken = {in ? to_f32(l[token]) : -kInf, in && (!av || av[token])};
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const int k = j * G + sub;
@@ -453,7 +462,7 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(LogProbArgs p)
     Stats st{-kInf, 0.0f, 0.0f};
     take(st, held, p.scale);
     st = join_lanes<G>(st);
-    if (there && sub == 0) finish_row<E>(p, row, st);
+    if (there && sub == 0) put_row(p, row, st, taken.available, taken.logit, token);
     if (p.K == 0) return;
     const float log_s = logf(st.s);
     if constexpr (G == kWave) {
@@ -484,19 +493,29 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(LogProbArgs p)
 // ---------------------------------------------------------------------------------- gradient
 struct RowGrad { float log_sum, ent, g_logp, g_ent; int token; };      // token: -1 without a gradient of its own; log_sum -inf: nothing there
 
-template <typename E>
+// (every load at once, none waits for another)
 __device__ __forceinline__ RowGrad row_grad(const LogProbArgs &p, int64_t row)
 {
     RowGrad g;
     g.log_sum = p.in_log_sum[row];
-    const int tok = p.grad_logp ? p.token[row] : -1;
-    const bool has = tok >= 0 && tok < p.V && !(p.avail && !p.avail[row * p.ld_avail + tok]) &&
-                     to_f32(static_cast<const E *>(p.logits)[row * p.ld + tok]) != -kInf;
-    g.token = has ? tok : -1;
-    g.g_logp = has ? p.grad_logp[row] : 0.0f;
+    g.token = p.grad_logp ? p.token[row] : -1;
+    g.g_logp = p.grad_logp ? p.grad_logp[row] : 0.0f;
     g.g_ent = p.grad_entropy ? p.grad_entropy[row] : 0.0f;
     g.ent = p.grad_entropy ? p.in_entropy[row] : 0.0f;
     return g;
+}
+// A token that is outside the row, masked or without probability has no gradient.
+__device__ __forceinline__ void drop_token(RowGrad &g, bool available, float logit)
+{
+    const bool has = available && logit != -kInf;
+    g.token = has ? g.token : -1;
+    g.g_logp = has ? g.g_logp : 0.0f;
+}
+template <typename E>
+__device__ __forceinline__ void look_at_token(RowGrad &g, const E *l, const uint8_t *av, int V)
+{
+    const bool in = g.token >= 0 && g.token < V;
+    drop_token(g, in && (!av || av[g.token]), in ? to_f32(l[g.token]) : -kInf);
 }
 
 __device__ __forceinline__ float grad_of(const RowGrad &g, float logit, bool taken, float scale)
@@ -518,7 +537,8 @@ __global__ __launch_bounds__(kThreads, 8) void long_grad_kernel(LogProbArgs p)
     const E *l = static_cast<const E *>(p.logits) + row * p.ld;
     const uint8_t *av = p.avail ? p.avail + row * p.ld_avail : nullptr;
     E *out = static_cast<E *>(p.grad_logits) + row * p.ld_grad;
-    const RowGrad g = row_grad<E>(p, row);
+    RowGrad g = row_grad(p, row);
+    look_at_token(g, l, av, p.V);
     __syncthreads();
     const int skew = skew_of(l), n = p.V + skew, token = g.token + skew;           // entry j of the row is skew + j
     l -= skew;
@@ -564,11 +584,12 @@ __global__ __launch_bounds__(kThreads) void short_grad_kernel(LogProbArgs p)
     const E *l = static_cast<const E *>(p.logits) + own * p.ld;
     const uint8_t *av = p.avail ? p.avail + own * p.ld_avail : nullptr;
     E *out = static_cast<E *>(p.grad_logits) + own * p.ld_grad;
-    const RowGrad g = row_grad<E>(p, own);
+    RowGrad g = row_grad(p, own);
     float held[N];
     if constexpr (FLAT) {
         __shared__ __attribute__((aligned(16))) FlatRows<E, G, N> rows[kThreads / kWave];
-        rows[wave].read(p, first, row, there, held);
+        const auto taken = rows[wave].read(p, first, row, there, g.token, held);
+        drop_token(g, taken.available, taken.logit);
         const int count = (int)min((int64_t)(kWave / G), p.R - first) * p.V;
         const int skew = (int)((reinterpret_cast<uintptr_t>(static_cast<E *>(p.grad_logits) + first * p.V) & 15) / sizeof(E));
 #pragma unroll
@@ -579,6 +600,7 @@ __global__ __launch_bounds__(kThreads) void short_grad_kernel(LogProbArgs p)
         wave_sync();
         bring_back<E, kWave * N>(static_cast<E *>(p.grad_logits), first * p.V, count, skew, rows[wave].entries);
     } else {
+        look_at_token(g, l, av, p.V);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const int k = j * G + sub;
