@@ -548,7 +548,7 @@ int marl_log_prob_grad(int32_t dtype, int32_t R, int32_t V, const void *logits, 
  * coefficients under which singular values grow beyond that the result is not finite.
  *   matrix  dev [L, rows, cols] elem     out dev [L, rows, cols] elem, may be matrix
  *   coefficients host [3] f32 (finite);  steps 0 .. 64;  eps finite and positive
- * L may be 0; rows, cols 1 .. 32768.
+ * A NaN in a matrix makes all of its result NaN.  L may be 0; rows, cols 1 .. 32768.
  */
 int marl_muon_workspace_bytes(int32_t dtype, int32_t L, int32_t rows, int32_t cols, size_t *bytes);
 int marl_orthogonalize(int32_t dtype, int32_t L, int32_t rows, int32_t cols, const void *matrix, void *out,

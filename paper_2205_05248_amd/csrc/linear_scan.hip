@@ -290,6 +290,9 @@ __device__ __forceinline__ Place place_of(const ScanArgs &p, int *shared)
     return {seq, id / p.sequences, seq / p.tiles, seq % p.tiles * kChannels};
 }
 
+// Forward.  Every input is read once and y written once.  What bounds it is the vector unit next to memory: 35 instructions an element, six
+// of them transcendental.  40001 x 1024 bf16 takes 85 us (3.8 TB/s), 4 x 16384 x 2048 bf16 takes 241 us (4.5 TB/s; a large copy reaches
+// 5.25); 320 x 120 x 64 fp32, one unit a sequence, 11 us.
 template <typename E, bool PAIRS, int NW, bool CHAIN>
 __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
 {
@@ -434,7 +437,8 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
 }
 
 // Backward pass.  D[t] = a[t] dL/dh[t] is what reaches h[t-1]: D[t] = a[t] (grad_y[t] + D[t+1]), the same kind of chain
-// backwards in time.  h is formed again inside the unit from the state kept at its start.
+// backwards in time.  h is formed again inside the unit from the state kept at its start.  66 instructions an element and three waves
+// on a SIMD, which wait for memory more than half of the time: 4 x 16384 x 2048 bf16 takes 489 us (3.8 TB/s), 320 x 120 x 64 fp32 19 us.
 template <typename E, bool PAIRS, int NW, bool CHAIN>
 __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
 {
@@ -647,6 +651,7 @@ __global__ __launch_bounds__(1024) void scan_lam_kernel(ScanArgs p, int64_t part
     p.grad_lam[c] = sum * p.decay * sigmoid2(p.lam[c]).s;
 }
 
+// A single step: an entry a thread.  777 x 2048 bf16 takes 8 us (25 MB), 24 x 64 fp32 3 us: the launch is what it costs.
 struct StepArgs {
     int n, C, slots;
     const void *x, *r, *i;

@@ -280,7 +280,9 @@ constexpr int kHeld = 32;                              // logits of a lane at a 
 constexpr int kChunk = kThreads * kHeld;               // of a workgroup
 
 // A workgroup takes `per` chunks of a row; with one part per row it finishes the row, otherwise join_kernel does.  With
-// alternatives a part is one chunk, which stays in registers for wave_top.
+// alternatives a part is one chunk, which stays in registers for wave_top.  8191 x 50021 fp16: 160 us, 5.1 TB/s, 11 instructions a logit.
+// 16 x 131072 bf16 with twenty alternatives: 13 us, and 5.5 us for the join; 256 workgroups of one chunk each, so what it costs is
+// one chunk's chain of loads, ballots and counts.
 template <typename E, bool TOP>
 __global__ __launch_bounds__(kThreads) void long_rows_kernel(LogProbArgs p)
 {
@@ -386,7 +388,7 @@ __global__ __launch_bounds__(kWave) void join_kernel(LogProbArgs p)
 // ---------------------------------------------------------------------------------- short rows
 // Rows that follow one another without a gap (FLAT): a wave brings its 64 / G of them to shared memory as one stretch, 16 bytes a
 // lane, and the lanes of a row take their entries from there.  A row of forty alone is 32 bytes a load and lane group, and loads, not
-// bytes, were what bounded it: 409600 x 40 fp32 with a mask, forward 31 us and gradient 38 us.
+// bytes, bound it: with a load per row 409600 x 40 fp32 with a mask took 31 us forward and 38 us backward.
 // `at`, `count`: the wave's stretch of an array of `total`; returns where in `to` it begins.
 template <typename T, int MOST>
 __device__ __forceinline__ int bring(const T *from, int64_t total, int64_t at, int count, T *to)
@@ -468,7 +470,8 @@ struct FlatRows {
     }
 };
 
-// G lanes hold a row of at most G N logits; a wave takes 64 / G rows.
+// G lanes hold a row of at most G N logits; a wave takes 64 / G rows.  409600 x 40 fp32 with a mask: 24 us forward (3.5 TB/s, its
+// instructions bound it), 29 us backward (5 TB/s).
 template <typename E, int G, int N, bool FLAT>
 __global__ __launch_bounds__(kThreads) void short_rows_kernel(LogProbArgs p)
 {
@@ -561,6 +564,7 @@ __device__ __forceinline__ float grad_of(const RowGrad &g, float logit, bool tak
 }
 
 // A workgroup takes `per` chunks of a row (the whole row if it overwrites the logits: the token's is read before any is gone).
+// 8191 x 50021 fp16: 337 us, 4.9 TB/s, as a large copy.
 template <typename E>
 __global__ __launch_bounds__(kThreads, 8) void long_grad_kernel(LogProbArgs p)
 {

@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256) void momentum_kernel(UpdateArgs p)
     if (threadIdx.x == 0) p.part[(size_t)blockIdx.y * kNormBlocks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// 1 / max(norm, eps), times the planes' scale: the parts in fixed order, by a workgroup of 256.
+// 1 / max(norm, eps), times the planes' scale: the parts in fixed order, by a workgroup of 256.  A norm of NaN stays one.
 __device__ __forceinline__ double inverse_norm(const UpdateArgs &p, int batch, double *shared)
 {
     const double *part = p.part + (size_t)batch * kNormBlocks;
@@ -108,7 +108,8 @@ __device__ __forceinline__ double inverse_norm(const UpdateArgs &p, int batch, d
     if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = sum;
     __syncthreads();
     sum = (shared[0] + shared[1]) + (shared[2] + shared[3]);
-    return (double)kPlaneScale / fmax(sqrt(sum), (double)p.eps);
+    const double norm = sqrt(sum);
+    return (double)kPlaneScale / (norm < (double)p.eps ? (double)p.eps : norm);
 }
 
 // X = u / max(|u|, eps) as planes, 64 x 64 entries a workgroup, in both orders; padding is zero.
@@ -251,7 +252,7 @@ int launch_product(Product p, int L, hipStream_t stream)
         }
     }
     hipLaunchKernelGGL((product_kernel<S, E>), dim3((unsigned)(p.tiles * p.splits), (unsigned)L), dim3(S::kThreads), S::kLds, stream, p);
-    if (p.splits > 1) hipLaunchKernelGGL((join_kernel<S, E>), dim3((unsigned)p.tiles, (unsigned)L), dim3(S::kTileThreads), S::kLds, stream, p);
+    if (p.splits > 1) hipLaunchKernelGGL((join_kernel<S, E>), dim3((unsigned)p.tiles, (unsigned)L, S::NT * S::MT / kJoinBlocks<S>), dim3(S::kTileThreads), S::kWaves * S::staging(kJoinBlocks<S>), stream, p);
     return MARL_OK;
 }
 

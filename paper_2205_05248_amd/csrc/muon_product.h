@@ -60,8 +60,10 @@ struct TileShape {
     static constexpr int kWaves = WM * WN, kTileThreads = kWaves * kWave, kThreads = KW * kTileThreads;
     static constexpr int TM = WM * MT * 32, TN = WN * NT * 32;
     static constexpr int kStage = (TM + TN) * 128;                     // bytes: 64 fp16 values of every row
-    static constexpr int kPitch = 32 * MT + 4;                         // a staged row of results, fp32 values
-    static constexpr int kStaging = 32 * kPitch * 4;                   // bytes a wave: 32 columns of its results
+    // staging of MB blocks below one another: fp32 values of a row of results, and bytes a wave for 32 columns of them
+    static constexpr int pitch(int MB) { return 32 * MB + 4; }
+    static constexpr int staging(int MB) { return 32 * pitch(MB) * 4; }
+    static constexpr int kStaging = staging(MT);
     static constexpr int kQuads = 4 * MT * NT;                         // groups of four accumulators of a lane
     static constexpr int kJoining = (KW - 1) * kQuads * kTileThreads * 16;                 // bytes: what the groups behind the first hand over
     static constexpr int kMost = kWaves * kStaging > kJoining ? kWaves * kStaging : kJoining;
@@ -139,21 +141,22 @@ __device__ __forceinline__ void put_out(const Product &p, int64_t batch, int r, 
 }
 
 // What becomes of a tile's accumulators.  Through shared memory, 32 columns at a time and each wave for itself, so that memory is
-// read and written along rows: once in the order [n][m], where C is added, and once in the order [m][n].
-template <class S, typename E>
-__device__ __forceinline__ void put_tile(const Product &p, int64_t batch, int m0, int n0, bool diagonal, floatx16 (&acc)[S::MT][S::NT], char *lds)
+// read and written along rows: once in the order [n][m], where C is added, and once in the order [m][n].  MB x NB of
+// the wave's MT x NT blocks of 32 x 32, from (mb0, nb0) on.
+template <class S, typename E, int MB, int NB>
+__device__ __forceinline__ void put_tile(const Product &p, int64_t batch, int m0, int n0, int mb0, int nb0, bool diagonal, floatx16 (&acc)[MB][NB], char *lds)
 {
-    constexpr int PL = S::PL, MT = S::MT, NT = S::NT, kPitch = S::kPitch, kAlong = MT * 4;      // kAlong: eights of a row of m
+    constexpr int PL = S::PL, kPitch = S::pitch(MB), kAlong = MB * 4;               // kAlong: eights of a row of m
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int wm = m0 + (wave / S::WN) * MT * 32, wn = n0 + (wave % S::WN) * NT * 32;
-    float *stage = reinterpret_cast<float *>(lds + wave * S::kStaging);
+    const int wm = m0 + (wave / S::WN) * S::MT * 32 + mb0 * 32, wn = n0 + (wave % S::WN) * S::NT * 32 + nb0 * 32;
+    float *stage = reinterpret_cast<float *>(lds + wave * S::staging(MB));
     const _Float16 *C = p.C + batch * p.t_batch, *C_lo = p.C_lo ? p.C_lo + batch * p.t_batch : nullptr;
     const bool transposed = p.out ? p.tall != 0 : p.D && !diagonal;
 #pragma unroll
-    for (int nb = 0; nb < NT; ++nb) {
+    for (int nb = 0; nb < NB; ++nb) {
         wave_meets();
 #pragma unroll
-        for (int mb = 0; mb < MT; ++mb)
+        for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 *reinterpret_cast<floatx4 *>(stage + (lane & 31) * kPitch + mb * 32 + 8 * q + 4 * (lane >> 5)) =
@@ -188,7 +191,7 @@ __device__ __forceinline__ void put_tile(const Product &p, int64_t batch, int m0
         if (!transposed) continue;
         wave_meets();
 #pragma unroll 2
-        for (int k = lane; k < 32 * MT * 4; k += kWave) {              // row k / 4, eight columns
+        for (int k = lane; k < 32 * MB * 4; k += kWave) {              // row k / 4, eight columns
             const int row = k / 4, col = k % 4 * 8, m = wm + row, n = wn + nb * 32 + col;
             if (n >= p.Np || m >= p.Mp) continue;
             float v[8];
@@ -375,31 +378,40 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
                     to[((a * NT + b) * 4 + q) * S::kTileThreads] = floatx4{acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
         return;
     }
-    put_tile<S, E>(p, batch, m0, n0, p.symmetric && ti == tj, acc, lds);
+    put_tile<S, E, MT, NT>(p, batch, m0, n0, 0, 0, p.symmetric && ti == tj, acc, lds);
 }
 
-// Sums the parts of a tile, in order, and finishes it.
+// Sums the parts of a tile, in order, and finishes it.  A workgroup takes two of each wave's blocks, so that there are several for a tile:
+// the parts of a split product are few tiles, and one workgroup each left half of the chip and most of its memory idle.
+template <class S> constexpr int kJoinBlocks = S::MT < 2 ? S::MT : 2;
 template <class S, typename E>
 __global__ __launch_bounds__(S::kTileThreads) void join_kernel(Product p)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
+    constexpr int MT = kJoinBlocks<S>;
     const int64_t batch = blockIdx.y;
-    const int tile = blockIdx.x;
+    const int tile = blockIdx.x, nb = blockIdx.z % S::NT, mb = blockIdx.z / S::NT * MT;
     int ti, tj;
     tile_of(p, tile, ti, tj);
-    floatx16 acc[S::MT][S::NT];
     const floatx4 *from = reinterpret_cast<const floatx4 *>(p.partial) + (batch * p.tiles + tile) * p.splits * (S::kQuads * S::kTileThreads) + threadIdx.x;
+    floatx4 sum[MT][4];
 #pragma unroll
-    for (int a = 0; a < S::MT; ++a)
+    for (int a = 0; a < MT; ++a)
 #pragma unroll
-        for (int b = 0; b < S::NT; ++b)
+        for (int q = 0; q < 4; ++q) sum[a][q] = floatx4{0, 0, 0, 0};
+    for (int s = 0; s < p.splits; ++s)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                floatx4 sum = {0, 0, 0, 0};
-                for (int s = 0; s < p.splits; ++s) sum += from[(s * S::kQuads + (a * S::NT + b) * 4 + q) * S::kTileThreads];
-                for (int e = 0; e < 4; ++e) acc[a][b][4 * q + e] = sum[e];
-            }
-    put_tile<S, E>(p, batch, ti * S::TM, tj * S::TN, p.symmetric && ti == tj, acc, lds);
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[a][q] += from[(s * S::kQuads + ((mb + a) * S::NT + nb) * 4 + q) * S::kTileThreads];
+    floatx16 acc[MT][1];
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[a][0][4 * q + e] = sum[a][q][e];
+    put_tile<S, E, MT, 1>(p, batch, ti * S::TM, tj * S::TN, mb, nb, p.symmetric && ti == tj, acc, lds);
 }
 
 }  // namespace marl

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
     __syncthreads();
     sum = 0.0;
     for (int w = 0; w < kSmallThreads / kWave; ++w) sum += part[w];
-    const double factor = (double)kPlaneScale / fmax(sqrt(sum), (double)a.eps);
+    const double norm = sqrt(sum), factor = (double)kPlaneScale / (norm < (double)a.eps ? (double)a.eps : norm);         // (a norm of NaN stays one)
     auto put = [&](_Float16 *to, float v) {
         const _Float16 h = (_Float16)v;
         to[0] = h;

@@ -156,3 +156,14 @@ def test_replayed_from_a_graph_and_on_another_stream(rows, cols):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(w, want[0]) and torch.equal(mom, want[1]), k
+
+
+@pytest.mark.parametrize("rows,cols", [(24, 40), (200, 300)])
+@pytest.mark.parametrize("steps", [0, 1, 5])
+def test_a_nan_makes_all_of_its_matrix_nan(rows, cols, steps):
+    m = gradient(gen(7), 2, rows, cols, "fp32")
+    m[1, rows - 1, 3] = float("nan")
+    out = torch.zeros_like(m, device="cuda")
+    binding.marl_orthogonalize(m.cuda(), out, workspace("fp32", 2, rows, cols), steps)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[1]).all() and torch.isfinite(out[0]).all()
