@@ -729,6 +729,14 @@ int scan_check(int dtype, int B, int T, int C, float decay, const void *workspac
     return aligned_to(workspace, 256) ? MARL_OK : MARL_ERR_BAD_ARG;
 }
 
+// A lane's offset behind its wave's first row, sixteen rows at most, is held in 32 bits.
+bool rows_ok(int C, std::initializer_list<int64_t> strides)
+{
+    for (int64_t ld : strides)
+        if (ld < C || ld >= ((int64_t)1 << 27)) return false;
+    return true;
+}
+
 unsigned blocks_of(int64_t n) { return (unsigned)((n + 255) / 256); }
 
 // Rows can be read four bytes at a time.
@@ -820,7 +828,7 @@ int marl_linear_scan(int32_t dtype, int32_t B, int32_t T, int32_t C, const void 
     if (rc) return rc;
     if (B == 0 || C == 0) return MARL_OK;
     if (!lam || (T > 0 && (!x || !r || !i || !y))) return MARL_ERR_NULL;
-    if (ld_x < C || ld_r < C || ld_i < C || ld_y < C) return MARL_ERR_BAD_DIM;
+    if (!rows_ok(C, {ld_x, ld_r, ld_i, ld_y})) return MARL_ERR_BAD_DIM;
     if (T > 0 && (y == x || y == r || y == i)) return MARL_ERR_BAD_ARG;
     ScanArgs p{};
     p.B = B; p.T = T; p.C = C;
@@ -842,7 +850,7 @@ int marl_linear_scan_grad(int32_t dtype, int32_t B, int32_t T, int32_t C, const 
     if (rc) return rc;
     if (C == 0) return MARL_OK;
     if (!lam || !grad_lam || (B > 0 && T > 0 && (!x || !r || !i || !grad_y || !grad_x || !grad_r || !grad_i))) return MARL_ERR_NULL;
-    if (ld_x < C || ld_r < C || ld_i < C || ld_gy < C || ld_gx < C || ld_gr < C || ld_gi < C) return MARL_ERR_BAD_DIM;
+    if (!rows_ok(C, {ld_x, ld_r, ld_i, ld_gy, ld_gx, ld_gr, ld_gi})) return MARL_ERR_BAD_DIM;
     const void *in[4] = {x, r, i, grad_y}, *out[3] = {grad_x, grad_r, grad_i};
     for (int k = 0; k < 3; ++k) {
         for (const void *v : in)

@@ -225,3 +225,11 @@ def test_binding_refuses_tensors_of_the_wrong_kind():
         binding.marl_orthogonalize(torch.zeros(4), torch.zeros(4), None)
     with pytest.raises(ValueError):
         binding.marl_orthogonalize(torch.zeros(4, 4), torch.zeros(4, 4), None)
+
+
+@pytest.mark.parametrize("call", [_scan, _scan_grad])
+@pytest.mark.parametrize("name", ["ld_x", "ld_r", "ld_i"])
+def test_rows_of_the_scans_that_lie_too_far_apart_are_refused(lib, call, name):
+    """A lane's offset inside a wave's rows has 32 bits."""
+    assert call(lib, **{name: 1 << 27}) == DIM
+    assert call(lib, B=0, C=0, **{name: 1 << 27}) == 0
