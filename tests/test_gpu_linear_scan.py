@@ -303,3 +303,18 @@ def test_a_reset_lets_nothing_through(B, T, C, dtype, value):
             assert torch.equal(o[k][:, part], clean[k][:, part]), (k, part)
     assert torch.equal(o["h_last"], clean["h_last"]) and torch.equal(o["grad_h_first"], clean["grad_h_first"])
     assert not torch.isfinite(o["y"][0, at, C // 2]) and torch.isnan(o["y"][0, at, C - 1])
+
+
+def test_single_steps_of_more_rows_than_the_chip_holds_at_a_time():
+    n, C = 600, 4096
+    s = make(1, n, C, "bf16", 22, layout="fused")
+    d = {k: (v[0] if k in "xri" else v) for k, v in on_gpu(s).items()}
+    slot = torch.randperm(n + 50, generator=gen(22))[:n].to(torch.int32)
+    table = randn(gen(23), n + 50, C)
+    dev, y = table.cuda(), torch.empty(n, C, dtype=torch.bfloat16, device="cuda")
+    binding.marl_linear_step(d["x"], d["r"], d["i"], d["lam"], DECAY, slot.cuda(), None, dev, dev, y)
+    torch.cuda.synchronize()
+    x, r, i = (host(s["xri"][0, :, k]) for k in range(3))
+    want, after = orc.linear_step(x, r, i, host(s["lam"]), DECAY, host(slot), None, host(table))
+    near(y, want, torch.bfloat16, 2.0 ** -20, "y")
+    near(dev, after, torch.float32, 2.0 ** -20, "h_out")
