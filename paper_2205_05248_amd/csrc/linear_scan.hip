@@ -234,9 +234,8 @@ __device__ __forceinline__ float word_H(Word w) { return __uint_as_float((unsign
 // the same sums in the same order whichever of the two words was there, so that timing does not change a bit.  The last of the
 // kDeep words that there is room for has to be (0, h).  A unit waits only for units whose tickets are lower, and they began before it:
 // each wait ends.
-constexpr int kDeep = 64;
-template <int kAtOnce>
-__device__ __forceinline__ float look_back(const Word *words, int before, int64_t stride, bool mine, Word (*held)[kChannels])
+template <int kAtOnce, int kDeep>
+__device__ __forceinline__ float look_back(const Word *words, int before, int64_t stride, bool mine, Word (&held)[kDeep][kChannels])
 {
     const int lane = threadIdx.x % kWave;
     bool open = mine;
@@ -300,7 +299,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
     constexpr int V = kWide<E>, Tc = kSteps, kWaveSteps = V * Tc, kAll = (int)((1ull << kWaveSteps) - 1);
     __shared__ float rate_s[kChannels], A_s[NW][kChannels], H_s[NW][kChannels], carry_s[NW][kChannels];
     __shared__ int id_s;
-    __shared__ Word held_s[CHAIN ? kDeep : 1][kChannels];
+    __shared__ Word held_s[CHAIN ? 64 : 1][kChannels];
     const Place at = place_of<CHAIN>(p, &id_s);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / (kWave / V), cl = lane % (kWave / V) * V;
     const int c = at.c0 + cl, left = p.C - c, first = at.unit * (NW * kWaveSteps), tw = first + wave * kWaveSteps;
@@ -439,14 +438,15 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
 
 // Backward pass.  D[t] = a[t] dL/dh[t] is what reaches h[t-1]: D[t] = a[t] (grad_y[t] + D[t+1]), the same kind of chain
 // backwards in time.  h is formed again inside the unit from the state kept at its start.  66 instructions an element and three waves
-// on a SIMD, which wait for memory more than half of the time: 4 x 16384 x 2048 bf16 takes 489 us (3.8 TB/s), 320 x 120 x 64 fp32 19 us.
+// on a SIMD, which wait for memory more than half of the time: 4 x 16384 x 2048 bf16 takes 473 us (4.0 TB/s), 320 x 120 x 64 fp32 19 us.
 template <typename E, bool PAIRS, int NW, bool CHAIN>
 __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
 {
     constexpr int V = kWide<E>, Tc = kStepsBack<E>, kWaveSteps = V * Tc, kAll = (1 << kWaveSteps) - 1;
     __shared__ float rate_s[kChannels], A_s[NW][kChannels], H_s[NW][kChannels], R_s[NW][kChannels], carry_s[NW][kChannels], after_s[NW][kChannels];
     __shared__ int id_s;
-    __shared__ Word held_s[CHAIN ? kDeep : 1][kChannels];
+    __shared__ Word held_s[CHAIN ? 32 : 1][kChannels];          // (three units on a compute unit: 53 KB each)
+    __shared__ uint32_t grad_s[CHAIN ? Tc : 1][NW * kWave];    // grad_y during look_back, for whose registers four spilled (489 us, not 473)
     const Place at = place_of<CHAIN>(p, &id_s);
     const int unit = p.units - 1 - at.unit;                    // the last steps first
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / (kWave / V), cl = lane % (kWave / V) * V;
@@ -520,6 +520,10 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
 #pragma unroll
         for (int v = 0; v < V; ++v) R[v] = unless_start(q[j][v].a * (gv[v] + R[v]), start, j);
     }
+    if constexpr (CHAIN) {
+#pragma unroll
+        for (int j = 0; j < Tc; ++j) grad_s[j][threadIdx.x] = g[j].bits;
+    }
     const bool cut = (start & ((1u << Tc) - 1)) != 0;          // nothing passes the lane's steps, whatever their other decays are
     float A_before[V], H_before[V], A_after[V], R_after[V];
 #pragma unroll
@@ -587,9 +591,12 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
     Strip<E, PAIRS> sgx(p.grad_x, p.ld_gx, last, at.c0, cl, down), sgr(p.grad_r, p.ld_gr, last, at.c0, cl, down),
         sgi(p.grad_i, p.ld_gi, last, at.c0, cl, down);
     auto put = [&](auto whole) {                               // whole: every step exists and counts, and none starts a sequence
+        if constexpr (CHAIN) g[Tc - 1].bits = grad_s[Tc - 1][threadIdx.x];
 #pragma unroll
         for (int j = Tc - 1; j >= 0; --j) {
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (CHAIN)
+                if (j > 0) g[j - 1].bits = grad_s[j - 1][threadIdx.x];
             Row<E, PAIRS> gx, gr, gi;
             float gv[V], dx[V], dr[V], di[V];
             g[j].get(gv);
