@@ -118,11 +118,17 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
     // of A apart, those there are: what bounds it is shared memory, and they share the reads of B.
     auto tiles = [&](auto count, int there, const _Float16 *A, int lda, int m0, int down, const _Float16 *B, int ldb, int n0, int K, floatx4 *out) {
         constexpr int N = decltype(count)::value;
-        floatx4 cross[N];
+        constexpr int kSpan = 64;                           // terms of a sum by themselves, as in muon_product.h (only G's are long)
+        floatx4 cross[N], total = {0, 0, 0, 0};
 #pragma unroll
         for (int q = 0; q < N; ++q) out[q] = cross[q] = floatx4{0, 0, 0, 0};
         const _Float16 *pa = A + (m0 + (lane & 15)) * lda + 8 * (lane >> 4), *pb = B + (n0 + (lane & 15)) * ldb + 8 * (lane >> 4);
         for (int k = 0; k < K; k += 32) {
+            if constexpr (N == 1)
+                if (k > 0 && k % kSpan == 0) {
+                    total += out[0];
+                    out[0] = floatx4{0, 0, 0, 0};
+                }
             const half8 bh = *reinterpret_cast<const half8 *>(pb + 2 * k), bl = *reinterpret_cast<const half8 *>(pb + 2 * k + 32);
 #pragma unroll
             for (int q = 0; q < N; ++q)
@@ -135,7 +141,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
                 }
         }
 #pragma unroll
-        for (int q = 0; q < N; ++q) out[q] += cross[q];
+        for (int q = 0; q < N; ++q) out[q] += total + cross[q];
     };
     auto put_along = [&](_Float16 *to, const floatx4 &v) {  // four entries along a row
         half4 h, l;

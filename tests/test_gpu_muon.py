@@ -167,3 +167,13 @@ def test_a_nan_makes_all_of_its_matrix_nan(rows, cols, steps):
     binding.marl_orthogonalize(m.cuda(), out, workspace("fp32", 2, rows, cols), steps)
     torch.cuda.synchronize()
     assert torch.isnan(out[1]).all() and torch.isfinite(out[0]).all()
+
+
+@pytest.mark.parametrize("L,rows,cols", [(2, 16, 1000), (1, 20, 4000), (1, 4000, 60), (1, 130, 5000)])
+@pytest.mark.parametrize("dtype", ["fp32", "fp16"])
+def test_few_rows_and_long_sums(L, rows, cols, dtype):
+    m = gradient(gen(9), L, rows, cols, dtype)
+    out = torch.empty_like(m, device="cuda")
+    binding.marl_orthogonalize(m.cuda(), out, workspace(dtype, L, rows, cols))
+    torch.cuda.synchronize()
+    close(out, orc.orthogonalize(host(m)), dtype, "out")
