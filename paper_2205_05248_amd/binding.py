@@ -618,6 +618,11 @@ def _current_device():
     return _torch._C._cuda_getDevice() if _torch.cuda.is_initialized() else _torch.cuda.current_device() if _torch.cuda.is_available() else -2
 
 
+def _stream_of(device):
+    """torch's current stream of the current device, whose ordinal is at hand."""
+    return _stream() if _raw_stream is None or device < 0 else _raw_stream(device)
+
+
 def _workspace(t, device):
     return (None, 0) if t is None or t.numel() == 0 else (_flat(t, "u8", (t.numel(),), "workspace", device), t.numel())
 
@@ -649,7 +654,7 @@ def marl_linear_scan(x, r, i, lam, decay, reset, filled, h_first, y, h_last, wor
         code, B, T, C, px, lx, pr, lr, pi, li, _flat(lam, "f32", (C,), "lam", d), float(decay),
         _flat(reset, "u8", (B, T), "reset", d, True), _flat(filled, "u8", (B, T), "filled", d, True),
         _flat(h_first, "f32", (B, C), "h_first", d, True), py, ly, _flat(h_last, "f32", (B, C), "h_last", d, True), *_workspace(workspace, d),
-        _stream()))
+        _stream_of(d)))
 
 
 def marl_linear_scan_grad(x, r, i, lam, decay, reset, filled, grad_y, grad_h_last, workspace, grad_x, grad_r, grad_i, grad_lam,
@@ -665,7 +670,7 @@ def marl_linear_scan_grad(x, r, i, lam, decay, reset, filled, grad_y, grad_h_las
         code, B, T, C, *px, *pr, *pi, _flat(lam, "f32", (C,), "lam", d), float(decay), _flat(reset, "u8", (B, T), "reset", d, True),
         _flat(filled, "u8", (B, T), "filled", d, True), *pg, _flat(grad_h_last, "f32", (B, C), "grad_h_last", d, True),
         *_workspace(workspace, d), *gx, *gr, *gi, _flat(grad_lam, "f32", (C,), "grad_lam", d),
-        _flat(grad_h_first, "f32", (B, C), "grad_h_first", d, True), _stream()))
+        _flat(grad_h_first, "f32", (B, C), "grad_h_first", d, True), _stream_of(d)))
 
 
 def marl_linear_step(x, r, i, lam, decay, slot, reset, h_in, h_out, y):
@@ -677,7 +682,7 @@ def marl_linear_step(x, r, i, lam, decay, slot, reset, h_in, h_out, y):
     check(load().marl_linear_step(
         code, n, C, px, lx, pr, lr, pi, li, _flat(lam, "f32", (C,), "lam", d), float(decay), _flat(slot, "i32", (n,), "slot", d, True), slots,
         _flat(reset, "u8", (n,), "reset", d, True), _flat(h_in, "f32", (slots, C), "h_in", d), _flat(h_out, "f32", (slots, C), "h_out", d), py, ly,
-        _stream()))
+        _stream_of(d)))
 
 
 def marl_log_prob_workspace_bytes(R, V, K):
@@ -702,7 +707,7 @@ def marl_log_prob(logits, token, avail, scale, logp, entropy, log_sum, top_id=No
         code, R, V, *_rows(logits, logits.dtype, (R, V), "logits", d), _flat(token, "i32", (R,), "token", d, True), *_avail_of(avail, R, V, d),
         float(scale), _flat(logp, "f32", (R,), "logp", d, True), _flat(entropy, "f32", (R,), "entropy", d, True),
         _flat(log_sum, "f32", (R,), "log_sum", d, True), K, _flat(top_id, "i32", (R, K), "top_id", d, True),
-        _flat(top_logp, "f32", (R, K), "top_logp", d, True), *_workspace(workspace, d), _stream()))
+        _flat(top_logp, "f32", (R, K), "top_logp", d, True), *_workspace(workspace, d), _stream_of(d)))
 
 
 def marl_log_prob_grad(logits, token, avail, scale, log_sum, entropy, grad_logp, grad_entropy, grad_logits):
@@ -713,7 +718,7 @@ def marl_log_prob_grad(logits, token, avail, scale, log_sum, entropy, grad_logp,
         code, R, V, *_rows(logits, logits.dtype, (R, V), "logits", d), _flat(token, "i32", (R,), "token", d, True), *_avail_of(avail, R, V, d),
         float(scale), _flat(log_sum, "f32", (R,), "log_sum", d), _flat(entropy, "f32", (R,), "entropy", d, True),
         _flat(grad_logp, "f32", (R,), "grad_logp", d, True), _flat(grad_entropy, "f32", (R,), "grad_entropy", d, True),
-        *_rows(grad_logits, logits.dtype, (R, V), "grad_logits", d), _stream()))
+        *_rows(grad_logits, logits.dtype, (R, V), "grad_logits", d), _stream_of(d)))
 
 
 NS_STEPS, NS_COEFFICIENTS, NS_EPS = 5, (3.4445, -4.7750, 2.0315), 1e-7
@@ -749,7 +754,7 @@ def marl_orthogonalize(matrix, out, workspace, steps=NS_STEPS, coefficients=NS_C
     L, rows, cols = _batch_of(matrix)
     check(load().marl_orthogonalize(
         code, L, rows, cols, _matrices(matrix, matrix.shape, matrix.dtype, "matrix", d), _matrices(out, matrix.shape, matrix.dtype, "out", d),
-        *_workspace(workspace, d), int(steps), _coefficients(coefficients), float(eps), _stream()))
+        *_workspace(workspace, d), int(steps), _coefficients(coefficients), float(eps), _stream_of(d)))
 
 
 def marl_muon_step(weights, grad, momentum, weights_out, momentum_out, workspace, lr, beta=0.95, nesterov=True, weight_decay=0.0,
@@ -764,4 +769,4 @@ def marl_muon_step(weights, grad, momentum, weights_out, momentum_out, workspace
         code, L, rows, cols, address(weights, "weights", weights.dtype), address(grad, "grad", weights.dtype),
         address(momentum, "momentum", f32), address(weights_out, "weights_out", weights.dtype), address(momentum_out, "momentum_out", f32),
         *_workspace(workspace, d), float(lr), float(beta), int(bool(nesterov)), float(weight_decay), float(scale), int(steps),
-        _coefficients(coefficients), float(eps), _stream()))
+        _coefficients(coefficients), float(eps), _stream_of(d)))
