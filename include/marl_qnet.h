@@ -465,7 +465,8 @@ int marl_probe_mfma(int32_t iters, float *sink, double *flops, void *hip_stream)
  *   y          dev [B,T,C] elem, rows ld_y apart
  *   h_last     dev [B,C] f32 or NULL  state after step T-1 (h_first if T is 0); may be h_first
  *   workspace  afterwards holds the states that marl_linear_scan_grad starts from
- * B, T and C may be 0 (C < 2^24, B T < 2^30, B C < 2^31); row distances are below 2^27, here and in the backward pass.
+ * B, T and C may be 0 (C < 2^24, B T < 2^30, B C < 2^31); row distances are at most 2^27 - 64, here and in the
+ * backward pass.
  */
 int marl_linear_scan_workspace_bytes(int32_t dtype, int32_t B, int32_t T, int32_t C, size_t *bytes);
 int marl_linear_scan(int32_t dtype, int32_t B, int32_t T, int32_t C, const void *x, int64_t ld_x, const void *r,

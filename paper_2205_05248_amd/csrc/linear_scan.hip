@@ -756,11 +756,14 @@ int scan_check(int dtype, int B, int T, int C, float decay, const void *workspac
     return aligned_to(workspace, 256) ? MARL_OK : MARL_ERR_BAD_ARG;
 }
 
-// A lane's offset behind its wave's first row, sixteen rows at most, is held in 32 bits.
+// A lane's offset behind its wave's first row is held in 32 bits (Strip::lane): sixteen rows of 16-bit elements down (fp32: none), and its
+// channel, less than kChannels to the right.
+constexpr int64_t kWidestRow = ((int64_t)1 << 27) - kChannels;
+static_assert((kSteps * kWidestRow + kChannels) * 2 <= ((int64_t)1 << 32), "");
 bool rows_ok(int C, std::initializer_list<int64_t> strides)
 {
     for (int64_t ld : strides)
-        if (ld < C || ld >= ((int64_t)1 << 27)) return false;
+        if (ld < C || ld > kWidestRow) return false;
     return true;
 }
 

@@ -233,3 +233,13 @@ def test_rows_of_the_scans_that_lie_too_far_apart_are_refused(lib, call, name):
     """A lane's offset inside a wave's rows has 32 bits."""
     assert call(lib, **{name: 1 << 27}) == DIM
     assert call(lib, B=0, C=0, **{name: 1 << 27}) == 0
+
+
+@pytest.mark.parametrize("call,names", [(_scan, ["ld_x", "ld_r", "ld_i", "ld_y"]), (_scan_grad, ["ld_x", "ld_r", "ld_i", "ld_gy", "ld_gx", "ld_gr", "ld_gi"])])
+@pytest.mark.parametrize("below", [1, 2, 3, 63])
+def test_the_widest_rows_leave_room_for_a_lanes_channel(lib, call, names, below):
+    """16 rows of 16-bit elements and the channel of a lane, up to 62, are one 32-bit offset: just below 2^27 elements it would wrap."""
+    worst = 16 * (2 ** 27 - 64) * 2 + 62 * 2 + 4
+    assert worst <= 2 ** 32 < 16 * (2 ** 27 - 1) * 2 + 62 * 2 + 4
+    for name in names:
+        assert call(lib, dtype=binding.MARL_DTYPE_BF16, **{name: 2 ** 27 - below}) == DIM, name
