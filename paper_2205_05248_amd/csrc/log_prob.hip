@@ -688,6 +688,14 @@ size_t log_prob_workspace(int R, int V, int K)
     return ((n * 4 * sizeof(float) + 255) / 256 + (n * K * sizeof(Key) + 255) / 256) * 256;
 }
 
+// Shared memory beyond 64 KB (from 63 alternatives on) has to be asked for.
+int make_room(void (*kernel)(LogProbArgs), size_t lds)
+{
+    if (lds <= 64 * 1024) return MARL_OK;
+    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    return err == hipSuccess ? MARL_OK : report_device_error(err, "hipFuncSetAttribute");
+}
+
 template <typename E>
 int run_forward(LogProbArgs p, char *workspace, hipStream_t stream)
 {
@@ -696,6 +704,7 @@ int run_forward(LogProbArgs p, char *workspace, hipStream_t stream)
         auto go = [&](auto kernel, int G, int N) {
             const int64_t rows = (int64_t)(kThreads / kWave) * (kWave / G);
             const size_t lds = G == kWave ? (size_t)(kThreads / kWave) * p.K * (N + 1) * sizeof(Key) : 0;
+            if (const int rc = make_room(kernel, lds)) return rc;
             hipLaunchKernelGGL(kernel, dim3((unsigned)((p.R + rows - 1) / rows)), dim3(kThreads), lds, stream, p);
             return launched("log prob");
         };
@@ -720,10 +729,7 @@ int run_forward(LogProbArgs p, char *workspace, hipStream_t stream)
     const dim3 grid((unsigned)(p.R * p.parts));
     if (p.K > 0) {
         const size_t lds = (size_t)(kThreads / kWave) * p.K * (kHeld + 1) * sizeof(Key);
-        if (lds > 64 * 1024) {
-            const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(long_rows_kernel<E, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            if (err != hipSuccess) return report_device_error(err, "hipFuncSetAttribute");
-        }
+        if (const int rc = make_room(long_rows_kernel<E, true>, lds)) return rc;
         hipLaunchKernelGGL((long_rows_kernel<E, true>), grid, dim3(kThreads), lds, stream, p);
     } else {
         hipLaunchKernelGGL((long_rows_kernel<E, false>), grid, dim3(kThreads), 0, stream, p);

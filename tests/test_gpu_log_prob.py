@@ -292,3 +292,13 @@ def test_short_rows_without_gaps(V, dtype, avail, in_place):
         assert (room[:lead] == beside).all() and (room[lead + R * V:] == beside).all()
         o["grad"] = grad.clone()
         check(s, o, 0.9, 0)
+
+
+
+@pytest.mark.parametrize("V", [513, 1000, 2048])
+@pytest.mark.parametrize("K", [62, 63, 64])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_most_alternatives_of_the_longest_short_rows(V, K, dtype):
+    """From 63 alternatives on, the room of a workgroup's four rows passes 64 KB of shared memory."""
+    s = make(9, V, dtype, 14, "rows")
+    check(s, run(s, 1.0, K, grad=False), 1.0, K)
