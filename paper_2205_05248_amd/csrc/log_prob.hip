@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "device_math.h"
 #include "operator_types.h"
@@ -24,6 +25,7 @@ struct LogProbArgs {
     const uint8_t *avail;
     int64_t ld_avail;
     float scale;
+    float lowest;                      // what is below it has a z of -infinity, and no probability
     float *logp, *entropy, *log_sum;
     int32_t *top_id;
     float *top_logp;
@@ -46,9 +48,6 @@ struct Stats {
 constexpr float kFar = -200.0f;
 
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(kLog2e * v); }
-
-// The lowest finite value stays finite under a scale above one.
-__device__ __forceinline__ float scaled(float scale, float logit) { return fmaxf(scale * logit, -3.4028235e38f); }
 
 // w of a set moved from maximum m to M >= m:  sum e^(z-M) (z-M) = e^(m-M) (w + (m-M) s).  NaN in m stays.
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
@@ -143,7 +142,7 @@ __device__ __forceinline__ void put_row(const LogProbArgs &p, int64_t row, Stats
     if (p.entropy) p.entropy[row] = bad ? nan : none ? 0.0f : log_s - st.w / st.s;
     if (p.logp) {
         float lp = 0.0f;
-        if (token >= 0 && token < p.V) lp = bad ? nan : none ? 0.0f : !available || logit == -kInf ? -kInf : (rounded(p.scale, logit) - st.m) - log_s;
+        if (token >= 0 && token < p.V) lp = bad ? nan : none ? 0.0f : !available || logit < p.lowest ? -kInf : (rounded(p.scale, logit) - st.m) - log_s;
         else if (bad) lp = nan;
         p.logp[row] = lp;
     }
@@ -318,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void long_rows_kernel(LogProbArgs p)
     if constexpr (TOP) {
         const int K = p.K;
         Key *lists = reinterpret_cast<Key *>(lds), *kept = lists + (kThreads / kWave) * K + (size_t)wave * K * kHeld;
-        wave_top<kHeld, true>([&](int j) { return held[j] == -kInf ? 0u : order_of(held[j]); },
+        wave_top<kHeld, true>([&](int j) { return held[j] < p.lowest ? 0u : order_of(held[j]); },
                         [&](int j) { return (unsigned)((int)begin + (j / V * kThreads + (int)threadIdx.x) * V + j % V); }, K, kept, lists + wave * K);
     }
     __syncthreads();
@@ -505,7 +504,7 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(LogProbArgs p)
     if constexpr (G == kWave) {
         if (!there) return;                                            // the whole wave
         Key *out = reinterpret_cast<Key *>(lds) + (size_t)wave * p.K * (N + 1), *kept = out + p.K;
-        wave_top<N, true>([&](int j) { return held[j] == -kInf ? 0u : order_of(held[j]); }, [&](int j) { return (unsigned)(j * G + sub); }, p.K, kept, out);
+        wave_top<N, true>([&](int j) { return held[j] < p.lowest ? 0u : order_of(held[j]); }, [&](int j) { return (unsigned)(j * G + sub); }, p.K, kept, out);
         if (lane < p.K) put_top(p, row, lane, out[lane], st, log_s);
     } else {
         Key last = ~(Key)0;
@@ -513,7 +512,7 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(LogProbArgs p)
             Key best = 0;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const Key key = held[j] == -kInf ? 0 : key_of(order_of(held[j]), j * G + sub);
+                const Key key = held[j] < p.lowest ? 0 : key_of(order_of(held[j]), j * G + sub);
                 if (key < last && key > best) best = key;
             }
 #pragma unroll
@@ -542,25 +541,25 @@ __device__ __forceinline__ RowGrad row_grad(const LogProbArgs &p, int64_t row)
     return g;
 }
 // A token that is outside the row, masked or without probability has no gradient.
-__device__ __forceinline__ void drop_token(RowGrad &g, bool available, float logit)
+__device__ __forceinline__ void drop_token(RowGrad &g, bool available, float logit, float lowest)
 {
-    const bool has = available && logit != -kInf;
+    const bool has = available && !(logit < lowest);
     g.token = has ? g.token : -1;
     g.g_logp = has ? g.g_logp : 0.0f;
 }
 template <typename E>
-__device__ __forceinline__ void look_at_token(RowGrad &g, const E *l, const uint8_t *av, int V)
+__device__ __forceinline__ void look_at_token(RowGrad &g, const E *l, const uint8_t *av, int V, float lowest)
 {
     const bool in = g.token >= 0 && g.token < V;
-    drop_token(g, in && (!av || av[g.token]), in ? to_f32(l[g.token]) : -kInf);
+    drop_token(g, in && (!av || av[g.token]), in ? to_f32(l[g.token]) : -kInf, lowest);
 }
 
-__device__ __forceinline__ float grad_of(const RowGrad &g, float logit, bool taken, float scale)
+__device__ __forceinline__ float grad_of(const RowGrad &g, float logit, bool taken, float scale, float lowest)
 {
     // p as the square of its root, which the hardware exponential does not flush where p is subnormal
-    const float lp = fmaxf(scaled(scale, logit) - g.log_sum, kFar), root = __builtin_amdgcn_exp2f(0.5f * kLog2e * lp);
+    const float lp = fmaxf(rounded(scale, logit) - g.log_sum, kFar), root = __builtin_amdgcn_exp2f(0.5f * kLog2e * lp);
     const float v = scale * ((taken ? g.g_logp : 0.0f) - root * (root * fmaf(g.g_ent, lp + g.ent, g.g_logp)));
-    return logit == -kInf || g.log_sum == -kInf ? 0.0f : v;
+    return logit < lowest || g.log_sum == -kInf ? 0.0f : v;
 }
 
 // A workgroup takes `per` chunks of a row (the whole row if it overwrites the logits: the token's is read before any is gone).
@@ -576,7 +575,7 @@ __global__ __launch_bounds__(kThreads, 8) void long_grad_kernel(LogProbArgs p)
     const uint8_t *av = p.avail ? p.avail + row * p.ld_avail : nullptr;
     E *out = static_cast<E *>(p.grad_logits) + row * p.ld_grad;
     RowGrad g = row_grad(p, row);
-    look_at_token(g, l, av, p.V);
+    look_at_token(g, l, av, p.V, p.lowest);
     __syncthreads();
     const int skew = skew_of(l), n = p.V + skew, token = g.token + skew;           // entry j of the row is skew + j
     l -= skew;
@@ -585,7 +584,7 @@ __global__ __launch_bounds__(kThreads, 8) void long_grad_kernel(LogProbArgs p)
     auto put = [&](const float *held, int j) {
         typename P::Vec v;
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[k] = from_f32<E>(grad_of(g, held[k], j + k == token, p.scale));
+        for (int k = 0; k < V; ++k) v[k] = from_f32<E>(grad_of(g, held[k], j + k == token, p.scale, p.lowest));
         if (j >= skew && j + V <= n) {
             *reinterpret_cast<typename P::Loose *>(out + j) = v;
         } else {
@@ -627,18 +626,18 @@ __global__ __launch_bounds__(kThreads) void short_grad_kernel(LogProbArgs p)
     if constexpr (FLAT) {
         __shared__ __attribute__((aligned(16))) FlatRows<E, G, N> rows[kThreads / kWave];
         const auto taken = rows[wave].read(p, first, row, there, g.token, held);
-        drop_token(g, taken.available, taken.logit);
+        drop_token(g, taken.available, taken.logit, p.lowest);
         const int count = (int)min((int64_t)(kWave / G), p.R - first) * p.V;
         const int skew = (int)((reinterpret_cast<uintptr_t>(static_cast<E *>(p.grad_logits) + first * p.V) & 15) / sizeof(E));
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const int k = j * G + sub;
-            if (there && k < p.V) rows[wave].entries[skew + (int)(row - first) * p.V + k] = from_f32<E>(grad_of(g, held[j], k == g.token, p.scale));
+            if (there && k < p.V) rows[wave].entries[skew + (int)(row - first) * p.V + k] = from_f32<E>(grad_of(g, held[j], k == g.token, p.scale, p.lowest));
         }
         wave_sync();
         bring_back<E, kWave * N>(static_cast<E *>(p.grad_logits), first * p.V, count, skew, rows[wave].entries);
     } else {
-        look_at_token(g, l, av, p.V);
+        look_at_token(g, l, av, p.V, p.lowest);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const int k = j * G + sub;
@@ -648,13 +647,24 @@ __global__ __launch_bounds__(kThreads) void short_grad_kernel(LogProbArgs p)
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const int k = j * G + sub;
-            if (there && k < p.V) out[k] = from_f32<E>(grad_of(g, held[j], k == g.token, p.scale));
+            if (there && k < p.V) out[k] = from_f32<E>(grad_of(g, held[j], k == g.token, p.scale, p.lowest));
         }
     }
 }
 
 // Rows without a gap between them, and masks too.
 bool rows_are_flat(const LogProbArgs &p) { return p.ld == p.V && (!p.avail || p.ld_avail == 0 || p.ld_avail == p.V); }
+
+// The lowest finite logit whose product with the scale, rounded to fp32, is finite.
+float lowest_of(float scale)
+{
+    const float least = std::numeric_limits<float>::lowest();
+    if (scale <= 1.0f) return least;
+    float v = least / scale;                                           // within a step of it
+    while (!std::isfinite(scale * v)) v = std::nextafter(v, 0.0f);
+    for (float w; std::isfinite(scale * (w = std::nextafter(v, least)));) v = w;
+    return v;
+}
 
 int log_prob_check(int dtype, int R, int V, const void *logits, int64_t ld, const uint8_t *avail, int64_t ld_avail, float scale)
 {
@@ -796,7 +806,7 @@ int marl_log_prob(int32_t dtype, int32_t R, int32_t V, const void *logits, int64
     if (!aligned_to(workspace, 256)) return MARL_ERR_BAD_ARG;
     LogProbArgs p{};
     p.R = R; p.V = V; p.K = K;
-    p.logits = logits; p.ld = ld; p.token = token; p.avail = avail; p.ld_avail = ld_avail; p.scale = scale;
+    p.logits = logits; p.ld = ld; p.token = token; p.avail = avail; p.ld_avail = ld_avail; p.scale = scale; p.lowest = lowest_of(scale);
     p.logp = logp; p.entropy = entropy; p.log_sum = log_sum; p.top_id = top_id; p.top_logp = top_logp;
     return with_dtype(dtype, [&](auto e) { return run_forward<decltype(e)>(p, static_cast<char *>(workspace), static_cast<hipStream_t>(hip_stream)); });
 }
@@ -814,7 +824,7 @@ int marl_log_prob_grad(int32_t dtype, int32_t R, int32_t V, const void *logits, 
     if (!log_sum || !grad_logits || (grad_logp && !token) || (grad_entropy && !entropy)) return MARL_ERR_NULL;
     LogProbArgs p{};
     p.R = R; p.V = V;
-    p.logits = logits; p.ld = ld; p.token = token; p.avail = avail; p.ld_avail = ld_avail; p.scale = scale;
+    p.logits = logits; p.ld = ld; p.token = token; p.avail = avail; p.ld_avail = ld_avail; p.scale = scale; p.lowest = lowest_of(scale);
     p.in_log_sum = log_sum; p.in_entropy = entropy; p.grad_logp = grad_logp; p.grad_entropy = grad_entropy;
     p.grad_logits = grad_logits; p.ld_grad = ld_grad;
     return with_dtype(dtype, [&](auto e) { return run_backward<decltype(e)>(p, static_cast<hipStream_t>(hip_stream)); });

@@ -302,3 +302,34 @@ def test_most_alternatives_of_the_longest_short_rows(V, K, dtype):
     """From 63 alternatives on, the room of a workgroup's four rows passes 64 KB of shared memory."""
     s = make(9, V, dtype, 14, "rows")
     check(s, run(s, 1.0, K, grad=False), 1.0, K)
+
+
+def low_scores(V):
+    """Rows that hold the type's lowest value, which a scale above one takes to -infinity."""
+    s = make(4, V, "fp32", 15)
+    low = torch.finfo(f32).min
+    s["logits"][0] = low                                           # nothing has a probability
+    s["logits"][1] = low
+    s["logits"][1, V // 2] = 1.0                                   # one entry has
+    s["token"][1] = V - 1                                          # and it is not the token
+    s["logits"][2, ::2] = low
+    s["token"][2] = 0
+    return s
+
+
+@pytest.mark.parametrize("V", [7, 40, 300, 900, 3000, 30000])
+@pytest.mark.parametrize("gap", [0, 5])
+def test_a_score_of_minus_infinity_has_no_probability_whatever_the_logit(V, gap):
+    """Forward, alternatives and gradient agree that what counts is scale * logit."""
+    K, scale = 4, 1.25
+    s = low_scores(V)
+    dead = s["logits"] == torch.finfo(f32).min
+    if gap:                                                        # rows that are read one by one
+        s["logits"] = torch.cat([s["logits"], torch.zeros(4, gap)], 1)
+    o = run(s, scale, K)
+    want = dict(s, logits=s["logits"].clone())
+    want["logits"][:, :V][dead] = -float("inf")                    # the same rows without those entries
+    check(want, o, scale, K)
+    assert o["logp"][0] == 0 and o["logp"][1] == -float("inf") and o["logp"][2] == -float("inf")
+    assert o["top_id"][0].eq(-1).all() and o["top_id"][1].tolist() == [V // 2, -1, -1, -1]
+    assert (o["top_logp"][0] == -float("inf")).all() and not o["grad"].cpu()[dead].any()
