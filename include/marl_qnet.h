@@ -531,7 +531,8 @@ int marl_log_prob(int32_t dtype, int32_t R, int32_t V, const void *logits, int64
 /*
  * Gradient of the logits, from the log_sum and entropy that marl_log_prob gave:
  *   grad_logits[j] = scale * ( grad_logp (1[j = token] - p[j]) - grad_entropy p[j] (log p[j] + entropy) )
- * and 0 in every place that is not available.
+ * and 0 in every place that is not available or has no probability.  A row whose log_sum is NaN has a gradient of NaN in
+ * all others.
  *   grad_logp dev [R] f32 or NULL (zero; token is then not needed), grad_entropy dev [R] f32 or NULL (zero; entropy is
  *   then not needed), grad_logits dev [R,V] elem, rows ld_grad apart; may be logits (same ld)
  */

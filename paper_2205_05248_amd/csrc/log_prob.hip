@@ -556,8 +556,8 @@ __device__ __forceinline__ void look_at_token(RowGrad &g, const E *l, const uint
 
 __device__ __forceinline__ float grad_of(const RowGrad &g, float logit, bool taken, float scale, float lowest)
 {
-    // p as the square of its root, which the hardware exponential does not flush where p is subnormal
-    const float lp = fmaxf(rounded(scale, logit) - g.log_sum, kFar), root = __builtin_amdgcn_exp2f(0.5f * kLog2e * lp);
+    // p as the square of its root, which the hardware exponential does not flush where p is subnormal; a log_sum of NaN stays one
+    const float lp = max_nan(rounded(scale, logit) - g.log_sum, kFar), root = __builtin_amdgcn_exp2f(0.5f * kLog2e * lp);
     const float v = scale * ((taken ? g.g_logp : 0.0f) - root * (root * fmaf(g.g_ent, lp + g.ent, g.g_logp)));
     return logit < lowest || g.log_sum == -kInf ? 0.0f : v;
 }

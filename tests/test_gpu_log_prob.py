@@ -333,3 +333,21 @@ def test_a_score_of_minus_infinity_has_no_probability_whatever_the_logit(V, gap)
     assert o["logp"][0] == 0 and o["logp"][1] == -float("inf") and o["logp"][2] == -float("inf")
     assert o["top_id"][0].eq(-1).all() and o["top_id"][1].tolist() == [V // 2, -1, -1, -1]
     assert (o["top_logp"][0] == -float("inf")).all() and not o["grad"].cpu()[dead].any()
+
+
+@pytest.mark.parametrize("V", [7, 40, 300, 900, 3000, 30000])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("parts", [("logp",), ("entropy",), ("logp", "entropy")])
+def test_the_gradient_of_a_row_that_is_not_finite_is_not_finite(V, value, parts):
+    """NaN in every place that is available, so that a check of the gradients sees it; masked places stay 0."""
+    for gap in (0, 5):
+        s = make(3, V, "fp32", 16, "rows", V + gap, V + gap)
+        s["avail"][1] = 1
+        s["avail"][1, 2] = 0
+        s["logits"][1] = 0.5
+        clean = run(s, 1.0, 0, parts=parts)
+        s["logits"][1, V - 2] = value
+        o = run(s, 1.0, 0, parts=parts)
+        here = s["avail"][1, :V] != 0
+        assert torch.isnan(o["grad"][1].cpu()[here]).all() and not o["grad"][1, 2]
+        assert torch.equal(o["grad"][::2], clean["grad"][::2])
