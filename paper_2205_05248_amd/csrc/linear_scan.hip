@@ -120,9 +120,13 @@ __device__ __forceinline__ uint32_t all_of(unsigned bits, int j) { return (uint3
 __device__ __forceinline__ float start_of(unsigned start, int j) { return __uint_as_float(all_of(start, j) & 0xc3480000u); }
 // v, or 0 where step j starts a sequence: a product with a = 0 would let an infinity or NaN of the sequence before through.
 __device__ __forceinline__ float unless_start(float v, unsigned start, int j) { return __uint_as_float(__float_as_uint(v) & ~all_of(start, j)); }
-// The same where stretches meet: what one does to the state, and what two do that follow one another.
+// The same where stretches meet: what one does to the state, and what two do that follow one another.  A = 0 says that a sequence starts in
+// the stretch, and nothing of before is left, infinity and NaN included.  A product of decays alone never says so: it ends at
+// the smallest normal number, which leaves less than 2^-26 of a state below 2^100, and through which what is not finite stays so.  (By its bits: a product is
+// not negative, and NaN lies above all.)
+__device__ __forceinline__ float decayed(float A) { return __uint_as_float(max(__float_as_uint(A), 0x00800000u)); }
 __device__ __forceinline__ float follow(float A, float h, float H) { return A == 0.0f ? H : fmaf(A, h, H); }
-__device__ __forceinline__ float both(float A, float B) { return A == 0.0f || B == 0.0f ? 0.0f : A * B; }
+__device__ __forceinline__ float both(float A, float B) { return A == 0.0f || B == 0.0f ? 0.0f : decayed(A * B); }
 
 // Four bytes of a row.  PAIRS: they lie at a multiple of four bytes and there is no odd channel at the end.
 // Held as one word: as a pair of 16-bit values the compiler gave each a register of its own wherever branches meet.
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
     float A_before[V], H_before[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        A[v] = cut ? 0.0f : A[v];
+        A[v] = cut ? 0.0f : decayed(A[v]);
         A_before[v] = 1.0f;
         H_before[v] = 0.0f;
         if constexpr (V == 2) {
@@ -528,7 +532,7 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
     float A_before[V], H_before[V], A_after[V], R_after[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        A[v] = cut ? 0.0f : A[v];
+        A[v] = cut ? 0.0f : decayed(A[v]);
         A_before[v] = A_after[v] = 1.0f;
         H_before[v] = R_after[v] = 0.0f;
         if constexpr (V == 2) {

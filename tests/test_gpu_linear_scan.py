@@ -318,3 +318,89 @@ def test_single_steps_of_more_rows_than_the_chip_holds_at_a_time():
     want, after = orc.linear_step(x, r, i, host(s["lam"]), DECAY, host(slot), None, host(table))
     near(y, want, torch.bfloat16, 2.0 ** -20, "y")
     near(dev, after, torch.float32, 2.0 ** -20, "h_out")
+
+
+def fast_channels(B, T, C, dtype, seed):
+    """Channels whose decays' product over a stretch of steps is far below the smallest fp32 number, without any reset."""
+    s = make(B, T, C, dtype, seed)
+    s["lam"] = torch.full((C,), 3.0)                               # half a gate keeps e^-12 of the state
+    s["lam"][C // 3] = 60.0                                        # and here nothing, to the last bit
+    return s
+
+
+def steps_from(s, value_of_h):
+    """The states of the same sequences, step by step."""
+    d = on_gpu(s)
+    B, T, C = d["x"].shape
+    h, states = value_of_h.clone(), []
+    for t in range(T):
+        y = torch.empty(B, C, dtype=d["x"].dtype, device="cuda")
+        binding.marl_linear_step(d["x"][:, t], d["r"][:, t], d["i"][:, t], d["lam"], DECAY, None, None, h, h, y)
+        states.append(h.clone())
+    return torch.stack(states, 1)
+
+
+@pytest.mark.parametrize("B,T,C", [(2, 9, 3), (1, 90, 70), (2, 700, 66)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("where", ["h_first", "x", "r"])
+def test_what_is_not_finite_stays_until_a_reset(B, T, C, dtype, value, where):
+    """However far the state decays: 0 times infinity or NaN is NaN, as step by step; and it stays in its channel and sequence."""
+    if where == "r":
+        value = float("nan")
+    s = fast_channels(B, T, C, dtype, 24)
+    clean_in = on_gpu(s)
+    clean = outputs(clean_in)
+    run(clean_in, clean)
+    t0, channels = (0 if where == "h_first" else T // 4), sorted({0, C // 3, C - 1})
+    for c in channels:
+        if where == "h_first":
+            s["h_first"][0, c] = value
+        else:
+            s["xri"][0, t0, "xri".index(where), c] = value
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    spoiled = torch.zeros(B, T, C, dtype=torch.bool, device="cuda")
+    spoiled[0, t0:, channels] = True
+    assert not torch.isfinite(o["y"][spoiled]).any() and not torch.isfinite(o["h_last"][0, channels]).any()
+    assert torch.equal(o["y"][~spoiled], clean["y"][~spoiled])
+    assert torch.equal(torch.isfinite(steps_from(s, d["h_first"])[:, -1]), torch.isfinite(o["h_last"]))
+    after = spoiled.clone()                                        # the gate's gradient has the state before the step as a factor
+    if where != "h_first":
+        after[0, t0] = False
+    assert not torch.isfinite(o["grad_r"][after]).any()
+    assert not torch.isfinite(o["grad_lam"][channels]).any()
+    others = [c for c in range(C) if c not in channels]
+    for k in ("grad_x", "grad_r", "grad_i"):
+        assert torch.equal(o[k][..., others], clean[k][..., others]), k
+    assert torch.equal(o["grad_lam"][others], clean["grad_lam"][others])
+
+
+@pytest.mark.parametrize("B,T,C", [(2, 9, 3), (1, 90, 70), (2, 700, 66)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("where", ["grad_h_last", "grad_y"])
+def test_a_gradient_that_is_not_finite_reaches_the_start(B, T, C, dtype, value, where):
+    s = fast_channels(B, T, C, dtype, 25)
+    clean_in = on_gpu(s)
+    clean = outputs(clean_in)
+    run(clean_in, clean)
+    t1, channels = (T - 1 if where == "grad_h_last" else 3 * T // 4), sorted({0, C // 3, C - 1})
+    for c in channels:
+        if where == "grad_h_last":
+            s["grad_h_last"][0, c] = value
+        else:
+            s["grad_y"][0, t1, c] = value
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    spoiled = torch.zeros(B, T, C, dtype=torch.bool, device="cuda")
+    spoiled[0, :t1 + 1, channels] = True
+    for k in ("grad_x", "grad_r", "grad_i"):
+        assert not torch.isfinite(o[k][spoiled]).any(), k
+        assert torch.equal(o[k][~spoiled], clean[k][~spoiled]), k
+    assert not torch.isfinite(o["grad_h_first"][0, channels]).any() and not torch.isfinite(o["grad_lam"][channels]).any()
+    assert torch.equal(o["y"], clean["y"])
