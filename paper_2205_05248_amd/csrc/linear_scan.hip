@@ -71,11 +71,11 @@ __device__ __forceinline__ float rate_of(float lam, float decay)
     return decay * (lam > 20.0f ? lam : soft);                 // (above 20 the difference is below half a step)
 }
 
-// sigmoid(v) and its complement, each to fp32 accuracy at both ends.
+// sigmoid(v) and its complement, each to fp32 accuracy at both ends.  NaN stays NaN.
 struct Sigmoid { float s, c; };
 __device__ __forceinline__ Sigmoid sigmoid2(float v)
 {
-    const float e = fminf(__builtin_amdgcn_exp2f(-kLog2e * v), 1e37f);
+    const float e = __builtin_elementwise_minimum(__builtin_amdgcn_exp2f(-kLog2e * v), 1e37f);
     const float s = __builtin_amdgcn_rcpf(1.0f + e);
     return {s, e * s};
 }

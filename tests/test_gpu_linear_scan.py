@@ -404,3 +404,18 @@ def test_a_gradient_that_is_not_finite_reaches_the_start(B, T, C, dtype, value, 
         assert torch.equal(o[k][~spoiled], clean[k][~spoiled]), k
     assert not torch.isfinite(o["grad_h_first"][0, channels]).any() and not torch.isfinite(o["grad_lam"][channels]).any()
     assert torch.equal(o["y"], clean["y"])
+
+
+@pytest.mark.parametrize("B,T,C", [(2, 9, 3), (1, 90, 70), (2, 700, 66)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_a_nan_of_the_input_gate_is_in_its_gradients(B, T, C, dtype):
+    s = make(B, T, C, dtype, 26)
+    t0 = T // 2
+    s["xri"][0, t0, 2, C - 1] = float("nan")
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    for k in ("y", "grad_x", "grad_i"):
+        assert torch.isnan(o[k][0, t0, C - 1]), k
+    assert torch.isnan(o["grad_r"][0, t0:, C - 1]).all() and torch.isnan(o["grad_lam"][C - 1])
