@@ -458,7 +458,7 @@ int marl_probe_mfma(int32_t iters, float *sink, double *flops, void *hip_stream)
  *   h[t] = a h[t-1] + beta sigmoid(i) x        y[t] = h[t]
  *   x, r, i    dev [B,T,C] elem, rows ld_x, ld_r, ld_i apart (row b T + t)
  *   lam        dev [C] f32;  decay finite and positive
- *   reset      dev [B,T] u8 or NULL   nonzero: a sequence starts at this step, a is 0 and beta 1
+ *   reset      dev [B,T] u8 or NULL   nonzero: a sequence starts at this step, a is 0 and beta 1 whatever r holds
  *   filled     dev [B,T] u8 or NULL   zero: padding; h passes unchanged, y is 0, and x, r, i, reset and the
  *                                     upstream gradient of the row are not looked at, whatever they hold
  *   h_first    dev [B,C] f32 or NULL (zero)   state before step 0

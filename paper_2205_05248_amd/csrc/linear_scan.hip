@@ -349,6 +349,10 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
             r[j].keep_or_shut(m);
         }
     }
+    if (steps.start) {                                         // a start has no decay of its own: its gate is not looked at
+#pragma unroll
+        for (int j = 0; j < Tc; ++j) r[j].keep(~all_of(start, j));
+    }
 #pragma unroll
     for (int j = 0; j < Tc; ++j) {
         __builtin_amdgcn_sched_barrier(0);                             // a step at a time, or registers run out
@@ -502,6 +506,10 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
             r[j].keep_or_shut(m);
         }
     }
+    if (steps.start) {                                         // a start has no decay of its own: its gate is not looked at
+#pragma unroll
+        for (int j = 0; j < Tc; ++j) r[j].keep(~all_of(start, j));
+    }
 #pragma unroll
     for (int j = 0; j < Tc; ++j) {
         __builtin_amdgcn_sched_barrier(0);                             // a step at a time, or registers run out
@@ -611,7 +619,7 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
                 dx[v] = dh * k.m;
                 di[v] = dh * k.n;
                 D[v] = whole ? k.a * dh : unless_start(k.a * dh, start, j);
-                const float part = k.s * (D[v] * k.q);
+                const float part = whole ? k.s * (D[v] * k.q) : unless_start(k.s * (D[v] * k.q), start, j);
                 dr[v] = -rate[v] * fmaf(-k.s, part, part);
                 sum[v] -= part;
             }
@@ -704,7 +712,7 @@ __global__ __launch_bounds__(256) void step_kernel(StepArgs p)
         Vec y;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const Step s = step_of(to_f32((E)x[v]), to_f32((E)r[v]), to_f32((E)i[v]), rate2[v], start ? -200.0f : 0.0f);
+            const Step s = step_of(to_f32((E)x[v]), start ? 0.0f : to_f32((E)r[v]), to_f32((E)i[v]), rate2[v], start ? -200.0f : 0.0f);
             h[v] = start ? s.u : fmaf(s.a, before[v], s.u);
             y[v] = from_f32<E>(h[v]);
         }

@@ -419,3 +419,64 @@ def test_a_nan_of_the_input_gate_is_in_its_gradients(B, T, C, dtype):
     for k in ("y", "grad_x", "grad_i"):
         assert torch.isnan(o[k][0, t0, C - 1]), k
     assert torch.isnan(o["grad_r"][0, t0:, C - 1]).all() and torch.isnan(o["grad_lam"][C - 1])
+
+
+@pytest.mark.parametrize("B,T,C", [(2, 9, 3), (1, 90, 70), (2, 700, 66)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_the_gate_of_a_step_that_starts_a_sequence_is_not_looked_at(B, T, C, dtype, value):
+    s = make(B, T, C, dtype, 27, reset=True, layout="shifted")
+    s["reset"][:, T // 2] = 1
+    start = s["reset"] != 0
+    outs = []
+    for v in (0.5, value):
+        s["xri"][:, :, 1][start] = v
+        d = on_gpu(s)
+        outs.append(outputs(d))
+        run(d, outs[-1])
+    torch.cuda.synchronize()
+    for k in outs[0]:
+        if k != "ws":
+            assert torch.equal(outs[0][k], outs[1][k]), k
+    assert not outs[1]["grad_r"].cpu()[start].any()
+    s["xri"][:, :, 1][start] = value
+    check(dict(s, xri=torch.where(torch.isfinite(s["xri"]), s["xri"], torch.full_like(s["xri"], 0.5))), outs[1])
+
+
+@pytest.mark.parametrize("C", [3, 64])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_the_gate_of_a_single_step_that_starts_a_sequence_is_not_looked_at(C, dtype, value):
+    s = make(1, 5, C, dtype, 28)
+    reset = torch.tensor([1, 0, 1, 0, 1], dtype=torch.uint8)
+    ys = []
+    for v in (0.5, value):
+        s["xri"][0, reset != 0, 1] = v
+        d = {k: (t[0].contiguous() if k in "xri" else t) for k, t in on_gpu(s).items()}
+        table, y = torch.full((5, C), 2.0, device="cuda"), torch.empty(5, C, dtype=DT[dtype], device="cuda")
+        table[0] = float("nan")
+        binding.marl_linear_step(d["x"], d["r"], d["i"], d["lam"], DECAY, None, reset.cuda(), table, table, y)
+        ys.append((y, table))
+    torch.cuda.synchronize()
+    assert torch.equal(ys[0][0], ys[1][0]) and torch.equal(ys[0][1], ys[1][1]) and torch.isfinite(ys[1][1]).all()
+
+
+@pytest.mark.parametrize("T", [9, 90, 700])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_an_infinite_input_of_a_sequence_of_one_step_leaves_the_decay_alone(T, dtype):
+    """grad_r of a step that starts a sequence is 0, and so is its part of grad_lam, whatever x is."""
+    s = make(1, T, 5, dtype, 29)
+    t0 = T // 2
+    s["reset"] = torch.zeros(1, T, dtype=torch.uint8)
+    s["reset"][:, t0:t0 + 2] = 1
+    clean_in = on_gpu(s)
+    clean = outputs(clean_in)
+    run(clean_in, clean)
+    s["xri"][0, t0, 0, 2] = float("inf")
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    for k in ("grad_r", "grad_lam", "grad_h_first", "grad_x", "h_last"):
+        assert torch.equal(o[k], clean[k]), k
+    assert not o["grad_r"][0, t0:t0 + 2].any() and torch.isinf(o["y"][0, t0, 2])
