@@ -118,7 +118,7 @@ __device__ __forceinline__ StepBack step_back_of(float x, float r, float i, floa
 // All bits or none, after bit j of `bits`.
 __device__ __forceinline__ uint32_t all_of(unsigned bits, int j) { return (uint32_t)((int)(bits << (31 - j)) >> 31); }
 __device__ __forceinline__ float start_of(unsigned start, int j) { return __uint_as_float(all_of(start, j) & 0xc3480000u); }
-// v, or 0 where step j starts a sequence: a product with a = 0 would let an infinity or NaN of the sequence before through.
+// v, or 0 at step j if its bit of `start` is set: a product with a = 0 would let an infinity or NaN of the sequence before through.
 __device__ __forceinline__ float unless_start(float v, unsigned start, int j) { return __uint_as_float(__float_as_uint(v) & ~all_of(start, j)); }
 // The same where stretches meet: what one does to the state, and what two do that follow one another.  A = 0 says that a sequence starts in
 // the stretch, and nothing of before is left, infinity and NaN included.  A product of decays alone never says so: it ends at
@@ -619,13 +619,19 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
                 dx[v] = dh * k.m;
                 di[v] = dh * k.n;
                 D[v] = whole ? k.a * dh : unless_start(k.a * dh, start, j);
-                const float part = whole ? k.s * (D[v] * k.q) : unless_start(k.s * (D[v] * k.q), start, j);
+                const float part = whole ? k.s * (D[v] * k.q) : unless_start(k.s * (D[v] * k.q), start | ~filled, j);
                 dr[v] = -rate[v] * fmaf(-k.s, part, part);
                 sum[v] -= part;
             }
             gx.set(dx);
             gr.set(dr);
             gi.set(di);
+            if (!whole) {                                      // padding: products with 0 would let an infinity or NaN that passes it show
+                const uint32_t m = all_of(filled, j);
+                gx.keep(m);
+                gr.keep(m);
+                gi.keep(m);
+            }
             if (left > 0 && (whole || (exist >> j & 1))) {
                 sgx.store(gx, left);
                 sgr.store(gr, left);

@@ -480,3 +480,29 @@ def test_an_infinite_input_of_a_sequence_of_one_step_leaves_the_decay_alone(T, d
     for k in ("grad_r", "grad_lam", "grad_h_first", "grad_x", "h_last"):
         assert torch.equal(o[k], clean[k]), k
     assert not o["grad_r"][0, t0:t0 + 2].any() and torch.isinf(o["y"][0, t0, 2])
+
+
+@pytest.mark.parametrize("B,T,C", [(2, 9, 3), (2, 90, 70), (2, 700, 66)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_padding_has_no_gradient_whatever_passes_through_it(B, T, C, dtype, value):
+    """A sequence without a step hands on what it is given, and adds nothing to grad_lam."""
+    s = make(B, T, C, dtype, 30, filled=True)
+    s["filled"][0] = 1
+    s["filled"][0, T // 3:T // 2] = 0
+    pad = s["filled"] == 0
+    s["xri"][~pad] = randn(gen(31), int((~pad).sum()), 3, C, dtype=DT[dtype])
+    s["grad_y"][~pad] = 1.0
+    clean_in = on_gpu(s)
+    clean = outputs(clean_in)
+    run(clean_in, clean)
+    s["h_first"][1, 0], s["grad_h_last"][1, C - 1] = value, value  # the row that is padding alone
+    s["grad_y"][0, T // 2, C - 1] = value                          # and what passes the padding inside a row
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    for k in ("y", "grad_x", "grad_r", "grad_i"):
+        assert not o[k].cpu()[pad].any(), k                        # (NaN counts as something)
+    assert torch.equal(o["grad_lam"][:C - 1], clean["grad_lam"][:C - 1])
+    assert not torch.isfinite(o["h_last"][1, 0]) and not torch.isfinite(o["grad_h_first"][1, C - 1])
