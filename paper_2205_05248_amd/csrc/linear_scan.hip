@@ -71,14 +71,15 @@ __device__ __forceinline__ float rate_of(float lam, float decay)
     return decay * (lam > 20.0f ? lam : soft);                 // (above 20 the difference is below half a step)
 }
 
-// sigmoid(v) and its complement, each to fp32 accuracy at both ends.  NaN stays NaN.
+// sigmoid(v) and its complement, each to fp32 accuracy at both ends, from e^-v, which ends where they are below fp32 anyway.  NaN stays NaN.
 struct Sigmoid { float s, c; };
-__device__ __forceinline__ Sigmoid sigmoid2(float v)
+__device__ __forceinline__ float odds_against(float v) { return __builtin_elementwise_minimum(__builtin_amdgcn_exp2f(-kLog2e * v), 1e37f); }
+__device__ __forceinline__ Sigmoid sigmoid_of_odds(float e)
 {
-    const float e = __builtin_elementwise_minimum(__builtin_amdgcn_exp2f(-kLog2e * v), 1e37f);
     const float s = __builtin_amdgcn_rcpf(1.0f + e);
     return {s, e * s};
 }
+__device__ __forceinline__ Sigmoid sigmoid2(float v) { return sigmoid_of_odds(odds_against(v)); }
 
 // The decay of a step: a = 2^e with e = -log2(e) rate sigmoid(r) <= 0, and beta^2 = 1 - a^2.  Near 0 the difference would cancel:
 // there -2 a sinh(e ln 2) by its series up to the seventh power, whose next term is below 2^-26 of it.  `rate2` is -log2(e) rate.
@@ -103,16 +104,18 @@ __device__ __forceinline__ Step step_of(float x, float r, float i, float rate2, 
     return {d.a, __builtin_amdgcn_sqrtf(d.om) * (x * sigmoidf_fast(i))};
 }
 
-// And what its gradients need: dx = dh m, di = dh n, dL = a dh (h before - q), dr = -rate (1 - s) s dL.
-struct StepBack { float a, u, q, m, n, s; };
+// And what its gradients need: dx = dh m, di = dh n, dL = a dh (h before - q), dr = -rate (1 - s) s dL.  odds: e^-r, from which both s and
+// 1 - s come (1 - s from s would cancel where the gate is open: at r = 10 two digits of it were left).
+struct StepBack { float a, u, q, m, n, odds; };
 __device__ __forceinline__ StepBack step_back_of(float x, float r, float i, float rate2, float start)
 {
     const Sigmoid si = sigmoid2(i);
-    const float s_r = sigmoidf_fast(r);
-    const Decay d = decay_of(s_r, rate2, start);
+    float odds = odds_against(r);
+    const Decay d = decay_of(sigmoid_of_odds(odds).s, rate2, start);
+    asm("" : "+v"(odds));                                              // s is formed again when it is wanted, or it is kept too, and registers spill
     const float inv = __builtin_amdgcn_rsqf(fmaxf(d.om, 1e-30f));      // a gate that is shut has om = 0: beta 0, and no infinity
     const float beta = d.om * inv, in = si.s * x, u = beta * in;
-    return {d.a, u, d.a * inv * in, beta * si.s, u * si.c, s_r};
+    return {d.a, u, d.a * inv * in, beta * si.s, u * si.c, odds};
 }
 
 // All bits or none, after bit j of `bits`.
@@ -619,8 +622,9 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
                 dx[v] = dh * k.m;
                 di[v] = dh * k.n;
                 D[v] = whole ? k.a * dh : unless_start(k.a * dh, start, j);
-                const float part = whole ? k.s * (D[v] * k.q) : unless_start(k.s * (D[v] * k.q), start | ~filled, j);
-                dr[v] = -rate[v] * fmaf(-k.s, part, part);
+                const Sigmoid sr = sigmoid_of_odds(k.odds);
+                const float part = whole ? sr.s * (D[v] * k.q) : unless_start(sr.s * (D[v] * k.q), start | ~filled, j);
+                dr[v] = -rate[v] * (sr.c * part);
                 sum[v] -= part;
             }
             gx.set(dx);

@@ -506,3 +506,39 @@ def test_padding_has_no_gradient_whatever_passes_through_it(B, T, C, dtype, valu
         assert not o[k].cpu()[pad].any(), k                        # (NaN counts as something)
     assert torch.equal(o["grad_lam"][:C - 1], clean["grad_lam"][:C - 1])
     assert not torch.isfinite(o["h_last"][1, 0]) and not torch.isfinite(o["grad_h_first"][1, C - 1])
+
+
+@pytest.mark.parametrize("T", [5, 60, 300])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_gradient_of_gates_that_are_almost_open_or_shut(T, dtype):
+    """Entry by entry: sigmoid(r) (1 - sigmoid(r)) keeps its digits at both ends.  The other factors of grad_r are within REL of their
+    largest values, and so is the product of the sizes (three factors of a few operations more)."""
+    C = 40
+    s = make(1, T, C, dtype, 32)
+    s["xri"][0, :, 1] = torch.linspace(-20, 20, T * C).view(C, T).t().to(DT[dtype])
+    s["lam"] = torch.linspace(-4, -1, C)
+    d = on_gpu(s)
+    o = outputs(d)
+    run(d, o)
+    torch.cuda.synchronize()
+    x, r, i = (host(s["xri"][:, :, k]) for k in range(3))
+    args = (x, r, i, host(s["lam"]), DECAY, None, None, host(s["h_first"]))
+    _, _, before = orc.linear_scan(*args)
+    want = orc.linear_scan_grad(*args, host(s["grad_y"]), host(s["grad_h_last"]))[1]
+    rate, _ = orc.rates(host(s["lam"]), DECAY)
+    e = np.exp(-np.abs(r))
+    s_r, slope = np.where(r > 0, 1 / (1 + e), e / (1 + e)), e / (1 + e) ** 2
+    a, beta = np.exp(-rate * s_r), np.sqrt(-np.expm1(-2 * rate * s_r))
+    q0 = np.abs(x) / (1 + np.exp(-i)) * a / beta
+    dh = adjoint(a, host(s["grad_y"]), host(s["grad_h_last"]))
+    sizes = rate * slope * (a * np.abs(dh).max() * (np.abs(before).max() + q0))
+    near(o["grad_r"], want, DT[dtype], 2 * REL, "grad_r", floor=sizes)
+
+
+def adjoint(a, grad_y, grad_h_last):
+    """dL/dh of every step."""
+    dh, out = grad_h_last, np.zeros(a.shape)
+    for t in range(a.shape[1] - 1, -1, -1):
+        out[:, t] = dh + grad_y[:, t]
+        dh = a[:, t] * out[:, t]
+    return out
