@@ -545,9 +545,9 @@ int marl_log_prob_grad(int32_t dtype, int32_t R, int32_t V, const void *logits, 
  * Newton-Schulz iteration towards the orthogonal factor of L matrices [rows, cols]: with X the matrix or its
  * transpose, whichever has no more rows than columns, X <- X / max(|X|_F, eps), then `steps` times
  *   G = X X^T      X <- c0 X + (c1 G + c2 G G) X
- * fp32 and fp16 matrices keep 22 bits of every factor of the products; bf16 ones keep 11 bits in the products and
- * 22 in the term c0 X, which leaves an error below a bf16 rounding.  Entries of X up to 16 are representable: with
- * coefficients under which singular values grow beyond that the result is not finite.
+ * Every factor of the products keeps 22 bits, whatever the type of the matrices, and sums are fp32.  Entries of X up to 16
+ * are representable: with coefficients under which singular values grow beyond that the result is not finite.
+ * Entries below 2^-15 are held to 2^-37, which shows in the result where the norm of a matrix is far below eps.
  *   matrix  dev [L, rows, cols] elem     out dev [L, rows, cols] elem, may be matrix
  *   coefficients host [3] f32 (finite);  steps 0 .. 64;  eps finite and positive
  * A NaN in a matrix makes all of its result NaN.  L may be 0; rows, cols 1 .. 32768.

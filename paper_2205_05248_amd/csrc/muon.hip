@@ -22,8 +22,8 @@ struct UpdateArgs {
     float eps;
     double *part;                      // [L][kNormBlocks] sums of squares, `parts` of them in use
     int parts;
-    _Float16 *Q, *Q_lo;                // planes in the matrix's own order; Q_lo, T_lo: PL = 1, may be NULL
-    _Float16 *T, *T_lo;                // and transposed
+    _Float16 *Q;                       // planes in the matrix's own order
+    _Float16 *T;                       // and transposed
 };
 
 constexpr int kNormBlocks = 1024;                  // at most, workgroups of a matrix in the first pass
@@ -113,12 +113,12 @@ __device__ __forceinline__ double inverse_norm(const UpdateArgs &p, int batch, d
 }
 
 // X = u / max(|u|, eps) as planes, 64 x 64 entries a workgroup, in both orders; padding is zero.
-template <typename E, int PL>
+template <typename E>
 __global__ __launch_bounds__(256) void planes_kernel(UpdateArgs p)
 {
     __shared__ float tile[64][65];
     const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-    const size_t n = (size_t)p.rows * p.cols, base = blockIdx.z * n, padded = (size_t)p.rows_p * p.cols_p * PL * blockIdx.z;
+    const size_t n = (size_t)p.rows * p.cols, base = blockIdx.z * n, padded = (size_t)p.rows_p * p.cols_p * 2 * blockIdx.z;
     __shared__ double shared[256 / kWave];
     const double factor = inverse_norm(p, blockIdx.z, shared);
     for (int k = threadIdx.x; k < 64 * 64; k += 256) {
@@ -126,16 +126,15 @@ __global__ __launch_bounds__(256) void planes_kernel(UpdateArgs p)
         tile[k / 64][k % 64] = r < p.rows && c < p.cols ? (float)(factor * momentum_of<E>(p, base + (size_t)r * p.cols + c)) : 0.0f;
     }
     __syncthreads();
-    auto put = [&](_Float16 *Q, _Float16 *Q_lo, size_t row, int ld, int c, const float *v) {
+    auto put = [&](_Float16 *Q, size_t row, int ld, int c, const float *v) {
         half8 h, l;
         for (int e = 0; e < 8; ++e) {
             h[e] = (_Float16)v[e];
             l[e] = (_Float16)(v[e] - (float)h[e]);
         }
-        _Float16 *to = Q + padded + row * ld * PL + plane_at<PL>(c);
+        _Float16 *to = Q + padded + row * ld * 2 + plane_at(c);
         *reinterpret_cast<half8 *>(to) = h;
-        if (PL == 2) *reinterpret_cast<half8 *>(to + 32) = l;
-        else if (Q_lo) *reinterpret_cast<half8 *>(Q_lo + padded + row * ld + c) = l;
+        *reinterpret_cast<half8 *>(to + 32) = l;
     };
     for (int k = threadIdx.x; k < 64 * 8; k += 256) {
         const int r = k / 8, c = k % 8 * 8;
@@ -144,23 +143,23 @@ __global__ __launch_bounds__(256) void planes_kernel(UpdateArgs p)
             v[e] = tile[r][c + e];
             w[e] = tile[c + e][r];
         }
-        put(p.Q, p.Q_lo, (size_t)r0 + r, p.cols_p, c0 + c, v);
-        put(p.T, p.T_lo, (size_t)c0 + r, p.rows_p, r0 + c, w);
+        put(p.Q, (size_t)r0 + r, p.cols_p, c0 + c, v);
+        put(p.T, (size_t)c0 + r, p.rows_p, r0 + c, w);
     }
 }
 
 // The update by X as it started: no step at all.  (Otherwise the last product writes the matrix.)
-template <typename E, int PL, bool FOURS>
+template <typename E, bool FOURS>
 __global__ __launch_bounds__(256) void finish_kernel(UpdateArgs p)
 {
     constexpr int N = FOURS ? 4 : 1;
-    const size_t n = (size_t)p.rows * p.cols, base = blockIdx.y * n, padded = (size_t)p.rows_p * p.cols_p * PL * blockIdx.y;
+    const size_t n = (size_t)p.rows * p.cols, base = blockIdx.y * n, padded = (size_t)p.rows_p * p.cols_p * 2 * blockIdx.y;
     for (size_t k = ((size_t)blockIdx.x * 256 + threadIdx.x) * N; k < n; k += (size_t)gridDim.x * 256 * N) {
         const int r = (int)(k / p.cols), c = (int)(k % p.cols);        // FOURS: rows are multiples of four
-        const size_t at = padded + (size_t)r * p.cols_p * PL + plane_at<PL>(c);
+        const size_t at = padded + (size_t)r * p.cols_p * 2 + plane_at(c);
         Entries<_Float16, FOURS> h, l;
         h.load(p.Q + at);
-        l.load(PL == 2 ? p.Q + at + 32 : p.Q_lo + at);
+        l.load(p.Q + at + 32);
         Entries<E, FOURS> w;
         if (p.weights) w.load(static_cast<const E *>(p.weights) + base + k);
 #pragma unroll
@@ -203,11 +202,11 @@ Plan plan_of(int L, int Mp, int Np, bool symmetric, int stages)
 }
 
 struct Layout {
-    int rows_p, cols_p, s, l, s_p, l_p, planes;
-    size_t x[2], t[2], x_lo[2], g, p, part, partial, bytes;
+    int rows_p, cols_p, s, l, s_p, l_p;
+    size_t x[2], t[2], g, p, part, partial, bytes;
 };
 
-Layout layout_of(int dtype, int L, int rows, int cols)
+Layout layout_of(int L, int rows, int cols)
 {
     Layout y{};
     if (small_fits(rows, cols)) { y.bytes = 256; return y; }   // shared memory alone; a size of zero would be a special case for callers
@@ -215,19 +214,17 @@ Layout layout_of(int dtype, int L, int rows, int cols)
     y.rows_p = pad(rows); y.cols_p = pad(cols);
     y.s = rows < cols ? rows : cols; y.l = rows < cols ? cols : rows;
     y.s_p = pad(y.s); y.l_p = pad(y.l);
-    y.planes = dtype == MARL_DTYPE_BF16 ? 1 : 2;
-    const size_t n = (size_t)L * y.rows_p * y.cols_p * sizeof(_Float16), square = (size_t)L * y.s_p * y.s_p * sizeof(_Float16) * y.planes;
+    const size_t n = (size_t)L * y.rows_p * y.cols_p * 2 * sizeof(_Float16), square = (size_t)L * y.s_p * y.s_p * 2 * sizeof(_Float16);
     size_t at = 0, partial = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
     for (int k = 0; k < 2; ++k) {
-        y.x[k] = take(n * y.planes);
-        y.t[k] = take(n * y.planes);
-        y.x_lo[k] = y.planes == 1 ? take(n) : 0;
+        y.x[k] = take(n);
+        y.t[k] = take(n);
     }
     y.g = take(square);
     y.p = take(square);
     y.part = take((size_t)L * kNormBlocks * sizeof(double));
-    const int stages_g = y.l_p * y.planes / 64, stages_p = y.s_p * y.planes / 64;
+    const int stages_g = y.l_p / 32, stages_p = y.s_p / 32;
     for (int stages : {stages_g, stages_p}) {
         const Plan plan = plan_of(L, y.s_p, y.s_p, true, stages);
         if (plan.splits > 1)
@@ -256,34 +253,33 @@ int launch_product(Product p, int L, hipStream_t stream)
     return MARL_OK;
 }
 
-template <int PL, typename E>
+template <typename E>
 int product(Product p, int L, hipStream_t stream)
 {
     const Plan plan = plan_of(L, p.Mp, p.Np, p.symmetric, p.stages);
     p.splits = plan.splits;
     switch (plan.shape) {
-    case 0: return launch_product<TileShape<PL, 2, 4, 4, 2, 2>, E>(p, L, stream);
-    case 1: return launch_product<TileShape<PL, 2, 2, 2, 2, 2>, E>(p, L, stream);
-    case 2: return launch_product<TileShape<PL, 2, 2, 1, 1, 4>, E>(p, L, stream);
-    default: return launch_product<TileShape<PL, 2, 2, 2, 2, 2, 2>, E>(p, L, stream);
+    case 0: return launch_product<TileShape<2, 4, 4, 2, 2>, E>(p, L, stream);
+    case 1: return launch_product<TileShape<2, 2, 2, 2, 2>, E>(p, L, stream);
+    case 2: return launch_product<TileShape<2, 2, 1, 1, 4>, E>(p, L, stream);
+    default: return launch_product<TileShape<2, 2, 2, 2, 2, 2>, E>(p, L, stream);
     }
 }
 
-template <typename E, int PL>
+template <typename E>
 int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, const float *coef, hipStream_t stream)
 {
     auto at = [&](size_t offset) { return reinterpret_cast<_Float16 *>(workspace + offset); };
     const bool tall = p.rows > p.cols;
-    _Float16 *X[2], *T[2], *X_lo[2];                 // X [s][l] and its transpose
+    _Float16 *X[2], *T[2];                           // X [s][l] and its transpose
     for (int k = 0; k < 2; ++k) {
         X[k] = at(y.x[k]);
         T[k] = at(y.t[k]);
-        X_lo[k] = PL == 1 ? at(y.x_lo[k]) : nullptr;
     }
     p.rows_p = y.rows_p; p.cols_p = y.cols_p;
     p.part = reinterpret_cast<double *>(workspace + y.part);
-    p.Q = tall ? T[0] : X[0]; p.Q_lo = tall && steps > 0 ? nullptr : X_lo[0];      // (without a step it is finish_kernel that reads lo)
-    p.T = tall ? X[0] : T[0]; p.T_lo = tall && steps > 0 ? X_lo[0] : nullptr;
+    p.Q = tall ? T[0] : X[0];
+    p.T = tall ? X[0] : T[0];
     const size_t n = (size_t)p.rows * p.cols;
     const bool fours = p.cols % 4 == 0 && aligned_to(p.grad, 4 * sizeof(E)) && aligned_to(p.weights, 4 * sizeof(E)) &&
                        aligned_to(p.weights_out, 4 * sizeof(E)) && aligned_to(p.momentum, 16) && aligned_to(p.momentum_out, 16);
@@ -292,47 +288,47 @@ int iterate(const Layout &y, int L, UpdateArgs p, char *workspace, int steps, co
     p.parts = (int)blocks;
     if (fours) hipLaunchKernelGGL((momentum_kernel<E, true>), dim3(blocks, (unsigned)L), dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((momentum_kernel<E, false>), dim3(blocks, (unsigned)L), dim3(256), 0, stream, p);
-    hipLaunchKernelGGL((planes_kernel<E, PL>), dim3((unsigned)(y.cols_p / 64), (unsigned)(y.rows_p / 64), (unsigned)L), dim3(256), 0, stream, p);
-    const int64_t square = (int64_t)y.s_p * y.s_p * PL, whole = (int64_t)y.s_p * y.l_p * PL;
+    hipLaunchKernelGGL((planes_kernel<E>), dim3((unsigned)(y.cols_p / 64), (unsigned)(y.rows_p / 64), (unsigned)L), dim3(256), 0, stream, p);
+    const int64_t square = (int64_t)y.s_p * y.s_p * 2, whole = (int64_t)y.s_p * y.l_p * 2;
     int now = 0;
     for (int k = 0; k < steps; ++k) {
         Product g{};
-        g.A = g.B = X[now]; g.a_batch = g.b_batch = whole; g.lda = g.ldb = (int64_t)y.l_p * PL;
-        g.Mp = g.Np = y.s_p; g.stages = y.l_p * PL / 64;
+        g.A = g.B = X[now]; g.a_batch = g.b_batch = whole; g.lda = g.ldb = (int64_t)y.l_p * 2;
+        g.Mp = g.Np = y.s_p; g.stages = y.l_p / 32;
         g.alpha = 1.0f / kPlaneScale;
-        g.Dt = g.D = at(y.g); g.ldt = g.ldd = (int64_t)y.s_p * PL; g.t_batch = g.d_batch = square;
+        g.Dt = g.D = at(y.g); g.ldt = g.ldd = (int64_t)y.s_p * 2; g.t_batch = g.d_batch = square;
         g.symmetric = 1;
         g.partial = reinterpret_cast<float *>(workspace + y.partial);
-        int rc = product<PL, E>(g, L, stream);
+        int rc = product<E>(g, L, stream);
         if (rc) return rc;
         Product q = g;
-        q.A = q.B = at(y.g); q.a_batch = q.b_batch = square; q.lda = q.ldb = (int64_t)y.s_p * PL;
-        q.stages = y.s_p * PL / 64;
+        q.A = q.B = at(y.g); q.a_batch = q.b_batch = square; q.lda = q.ldb = (int64_t)y.s_p * 2;
+        q.stages = y.s_p / 32;
         q.alpha = coef[2] / kPlaneScale; q.beta = coef[1];
         q.C = at(y.g);
         q.Dt = q.D = at(y.p);
-        rc = product<PL, E>(q, L, stream);
+        rc = product<E>(q, L, stream);
         if (rc) return rc;
         Product x{};                                   // D [l][s] = X^T P, so D's transpose is the new X
-        x.A = T[now]; x.a_batch = whole; x.lda = (int64_t)y.s_p * PL;
-        x.B = at(y.p); x.b_batch = square; x.ldb = (int64_t)y.s_p * PL;
-        x.Mp = y.l_p; x.Np = y.s_p; x.stages = y.s_p * PL / 64;
+        x.A = T[now]; x.a_batch = whole; x.lda = (int64_t)y.s_p * 2;
+        x.B = at(y.p); x.b_batch = square; x.ldb = (int64_t)y.s_p * 2;
+        x.Mp = y.l_p; x.Np = y.s_p; x.stages = y.s_p / 32;
         x.alpha = 1.0f / kPlaneScale; x.beta = coef[0];
-        x.C = X[now]; x.C_lo = X_lo[now];
-        x.Dt = X[now ^ 1]; x.Dt_lo = X_lo[now ^ 1]; x.ldt = (int64_t)y.l_p * PL; x.t_batch = whole;
-        x.D = T[now ^ 1]; x.ldd = (int64_t)y.s_p * PL; x.d_batch = whole;
+        x.C = X[now];
+        x.Dt = X[now ^ 1]; x.ldt = (int64_t)y.l_p * 2; x.t_batch = whole;
+        x.D = T[now ^ 1]; x.ldd = (int64_t)y.s_p * 2; x.d_batch = whole;
         if (k + 1 == steps) {
             x.out = p.weights_out; x.weights = p.weights;
             x.rows = p.rows; x.cols = p.cols; x.tall = tall; x.keep = p.keep; x.rate = p.rate;
         }
-        rc = product<PL, E>(x, L, stream);
+        rc = product<E>(x, L, stream);
         if (rc) return rc;
         now ^= 1;
     }
     if (steps == 0) {
         const dim3 each((unsigned)std::min<size_t>((n + 1023) / 1024, 4096), (unsigned)L);
-        if (fours) hipLaunchKernelGGL((finish_kernel<E, PL, true>), each, dim3(256), 0, stream, p);
-        else hipLaunchKernelGGL((finish_kernel<E, PL, false>), each, dim3(256), 0, stream, p);
+        if (fours) hipLaunchKernelGGL((finish_kernel<E, true>), each, dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((finish_kernel<E, false>), each, dim3(256), 0, stream, p);
     }
     return launched("orthogonalised update");
 }
@@ -353,12 +349,8 @@ int newton_schulz(int dtype, int L, UpdateArgs p, char *workspace, int steps, co
 {
     p.eps = eps;
     if (small_fits(p.rows, p.cols)) return with_dtype(dtype, [&](auto e) { return iterate_small<decltype(e)>(L, p, steps, coef, stream); });
-    const Layout y = layout_of(dtype, L, p.rows, p.cols);
-    switch (dtype) {
-    case MARL_DTYPE_F32: return iterate<float, 2>(y, L, p, workspace, steps, coef, stream);
-    case MARL_DTYPE_BF16: return iterate<__bf16, 1>(y, L, p, workspace, steps, coef, stream);
-    default: return iterate<_Float16, 2>(y, L, p, workspace, steps, coef, stream);
-    }
+    const Layout y = layout_of(L, p.rows, p.cols);
+    return with_dtype(dtype, [&](auto e) { return iterate<decltype(e)>(y, L, p, workspace, steps, coef, stream); });
 }
 
 int check(int dtype, int L, int rows, int cols, const void *workspace, size_t workspace_bytes, int steps, const float *coef, float eps)
@@ -369,7 +361,7 @@ int check(int dtype, int L, int rows, int cols, const void *workspace, size_t wo
     for (int k = 0; k < 3; ++k)
         if (!std::isfinite(coef[k])) return MARL_ERR_BAD_ARG;
     if (steps < 0 || steps > 64 || !std::isfinite(eps) || !(eps > 0.0f)) return MARL_ERR_BAD_ARG;
-    if (workspace_bytes < layout_of(dtype, L, rows, cols).bytes) return MARL_ERR_BAD_DIM;
+    if (workspace_bytes < layout_of(L, rows, cols).bytes) return MARL_ERR_BAD_DIM;
     if (!workspace && workspace_bytes) return MARL_ERR_NULL;
     return aligned_to(workspace, 256) ? MARL_OK : MARL_ERR_BAD_ARG;
 }
@@ -386,7 +378,7 @@ int marl_muon_workspace_bytes(int32_t dtype, int32_t L, int32_t rows, int32_t co
     if (!bytes) return MARL_ERR_NULL;
     if (!known_dtype(dtype)) return MARL_ERR_BAD_DTYPE;
     if (!sizes_ok(L, rows, cols)) return MARL_ERR_BAD_DIM;
-    *bytes = layout_of(dtype, L, rows, cols).bytes;
+    *bytes = layout_of(L, rows, cols).bytes;
     return MARL_OK;
 }
 

@@ -1,15 +1,13 @@
 // Products of the Newton-Schulz iteration on the fp16 matrix pipe.
 //
-// Every matrix of the iteration is kept as fp16 planes of its entries times 2^12: hi = fp16(v), lo = fp16(v - hi).  The scale
-// keeps lo above fp16's subnormals at the size that entries of large matrices have, and leaves room up to 16 (singular values
-// end near 1.2).  D = A B^T with both operands adjacent along the summed index, so that both are read the same way; G and P
-// are symmetric, and X is kept beside its transpose.
+// Every matrix of the iteration is kept as two fp16 planes of its entries times 2^12: hi = fp16(v), lo = fp16(v - hi), whatever the type of
+// the matrices.  The scale keeps lo above fp16's subnormals at the size that entries of large matrices have, and leaves room up
+// to 16 (singular values end near 1.2).  D = A B^T with both operands adjacent along the summed index, so that both are read the
+// same way; G and P are symmetric, and X is kept beside its transpose.
 //
-// PL = 2 (fp32 and fp16 matrices): each operand has both planes, a product is hi hi + hi lo + lo hi in fp32 accumulators; what is
-// left out, lo lo, is 2^-24 of a term.  Planes alternate in blocks of 32 of the summed index, [hi x 32][lo x 32].
-// PL = 1 (bf16 matrices): operands have the plane hi alone, 2^-12 of a term.  That is no rounding of X itself: X is carried
-// in the term c0 X with its plane lo, which lies in an array of its own.  Rounded X there would put noise into directions
-// in which X is small, and five steps would multiply it by up to 485; noise in P X and G is of the size of what it stands in.
+// A product is hi hi + hi lo + lo hi in fp32 accumulators; what is left out, lo lo, is 2^-22 of a term.  Planes alternate in blocks of 32
+// of the summed index, [hi x 32][lo x 32].  (One plane is not enough for bf16 matrices either: it leaves 1.2e-3 to 2.9e-3 of the result, where
+// its rounding to bf16 leaves 1.7e-3.)
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -27,17 +25,17 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 constexpr float kPlaneScale = 4096.0f;
 
 // D[m, n] = alpha sum_k A[m, k] B[n, k] + beta C[m, n], m < Mp, n < Np (multiples of 64: the matrices are padded with zeros).
-// Strides and rows are in fp16 values; offset of (r, k) in planes: r ld + plane_at<PL>(k).
+// Strides and rows are in fp16 values; offset of (r, k) in planes: r ld + plane_at(k).
 struct Product {
     const _Float16 *A, *B;
     int64_t a_batch, b_batch;
     int64_t lda, ldb;
-    int Mp, Np, stages;               // stages of 64 fp16 values of a row: 64 / PL of the summed index
+    int Mp, Np, stages;               // stages of 64 fp16 values of a row: 32 of the summed index
     float alpha, beta;
-    const _Float16 *C, *C_lo;         // [n][m], of scaled entries; C_lo: PL = 1 only.  Used with beta != 0
-    _Float16 *Dt, *Dt_lo;             // [n][m]; Dt_lo: PL = 1, may be NULL
+    const _Float16 *C;                // [n][m], of scaled entries; used with beta != 0
+    _Float16 *Dt;                     // [n][m]
     _Float16 *D;                      // [m][n] or NULL
-    int64_t ldt, ldd, t_batch, d_batch;        // C, C_lo, Dt_lo lie as Dt
+    int64_t ldt, ldd, t_batch, d_batch;        // C lies as Dt
     int symmetric;                    // A is B: only tiles on and below the diagonal, D is the mirrored tile
     int tiles_m, tiles_n, tiles;      // tiles: of one batch member
     int splits;                       // parts of the sum, one workgroup each; > 1: accumulators go to `partial`
@@ -49,14 +47,13 @@ struct Product {
     float keep, rate;
 };
 
-template <int PL>
-__host__ __device__ __forceinline__ int plane_at(int k) { return PL == 1 ? k : (k >> 5) * 64 + (k & 31); }
+__host__ __device__ __forceinline__ int plane_at(int k) { return (k >> 5) * 64 + (k & 31); }
 
 // KW groups of WM x WN waves take the stages of the sum in turn and put their results together at the end: where there are fewer tiles
 // than compute units, the time of a product is that of one workgroup's stages one after the other.
-template <int PL_, int WM_, int WN_, int MT_, int NT_, int BUFFERS_, int KW_ = 1>
+template <int WM_, int WN_, int MT_, int NT_, int BUFFERS_, int KW_ = 1>
 struct TileShape {
-    static constexpr int PL = PL_, WM = WM_, WN = WN_, MT = MT_, NT = NT_, kBuffers = BUFFERS_, KW = KW_;
+    static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, kBuffers = BUFFERS_, KW = KW_;
     static constexpr int kWaves = WM * WN, kTileThreads = kWaves * kWave, kThreads = KW * kTileThreads;
     static constexpr int TM = WM * MT * 32, TN = WN * NT * 32;
     static constexpr int kStage = (TM + TN) * 128;                     // bytes: 64 fp16 values of every row
@@ -103,8 +100,7 @@ __device__ __forceinline__ void wave_meets()
 }
 
 // Eight results along a row as planes.
-template <int PL>
-__device__ __forceinline__ void put_planes(_Float16 *to, _Float16 *to_lo, const float (&v)[8])
+__device__ __forceinline__ void put_planes(_Float16 *to, const float (&v)[8])
 {
     half8 h, l;
 #pragma unroll
@@ -113,8 +109,7 @@ __device__ __forceinline__ void put_planes(_Float16 *to, _Float16 *to_lo, const 
         l[e] = (_Float16)(v[e] - (float)h[e]);
     }
     *reinterpret_cast<half8 *>(to) = h;
-    if (PL == 2) *reinterpret_cast<half8 *>(to + 32) = l;
-    else if (to_lo) *reinterpret_cast<half8 *>(to_lo) = l;
+    *reinterpret_cast<half8 *>(to + 32) = l;
 }
 
 // Eight results along row r, from column c, of the matrix itself.
@@ -146,11 +141,11 @@ __device__ __forceinline__ void put_out(const Product &p, int64_t batch, int r, 
 template <class S, typename E, int MB, int NB>
 __device__ __forceinline__ void put_tile(const Product &p, int64_t batch, int m0, int n0, int mb0, int nb0, bool diagonal, floatx16 (&acc)[MB][NB], char *lds)
 {
-    constexpr int PL = S::PL, kPitch = S::pitch(MB), kAlong = MB * 4;               // kAlong: eights of a row of m
+    constexpr int kPitch = S::pitch(MB), kAlong = MB * 4;               // kAlong: eights of a row of m
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int wm = m0 + (wave / S::WN) * S::MT * 32 + mb0 * 32, wn = n0 + (wave % S::WN) * S::NT * 32 + nb0 * 32;
     float *stage = reinterpret_cast<float *>(lds + wave * S::staging(MB));
-    const _Float16 *C = p.C + batch * p.t_batch, *C_lo = p.C_lo ? p.C_lo + batch * p.t_batch : nullptr;
+    const _Float16 *C = p.C + batch * p.t_batch;
     const bool transposed = p.out ? p.tall != 0 : p.D && !diagonal;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -167,14 +162,11 @@ __device__ __forceinline__ void put_tile(const Product &p, int64_t batch, int m0
             const int col = k / kAlong, along = k % kAlong * 8, n = wn + nb * 32 + col, m = wm + along;
             if (n >= p.Np || m >= p.Mp) continue;
             float *at = stage + col * kPitch + along, v[8];
-            const int64_t lies = n * p.ldt + plane_at<PL>(m);
+            const int64_t lies = n * p.ldt + plane_at(m);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = p.alpha * at[e];
             if (p.beta != 0.0f) {
-                const half8 h = *reinterpret_cast<const half8 *>(C + lies);
-                half8 l = {};
-                if constexpr (PL == 2) l = *reinterpret_cast<const half8 *>(C + lies + 32);
-                else if (C_lo) l = *reinterpret_cast<const half8 *>(C_lo + lies);
+                const half8 h = *reinterpret_cast<const half8 *>(C + lies), l = *reinterpret_cast<const half8 *>(C + lies + 32);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = fmaf(p.beta, (float)h[e] + (float)l[e], v[e]);
             }
@@ -185,7 +177,7 @@ __device__ __forceinline__ void put_tile(const Product &p, int64_t batch, int m0
             if (p.out) {
                 if (!p.tall) put_out<E>(p, batch, n, m, v);
             } else {
-                put_planes<PL>(p.Dt + batch * p.t_batch + lies, p.Dt_lo ? p.Dt_lo + batch * p.t_batch + lies : nullptr, v);
+                put_planes(p.Dt + batch * p.t_batch + lies, v);
             }
         }
         if (!transposed) continue;
@@ -200,8 +192,8 @@ __device__ __forceinline__ void put_tile(const Product &p, int64_t batch, int m0
             if (p.out) {
                 put_out<E>(p, batch, m, n, v);
             } else {
-                const int64_t lies = m * p.ldd + plane_at<PL>(n);
-                put_planes<PL>(p.D + batch * p.d_batch + lies, nullptr, v);
+                const int64_t lies = m * p.ldd + plane_at(n);
+                put_planes(p.D + batch * p.d_batch + lies, v);
             }
         }
     }
@@ -211,7 +203,7 @@ template <class S, typename E>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    constexpr int PL = S::PL, MT = S::MT, NT = S::NT, TM = S::TM, TN = S::TN;
+    constexpr int MT = S::MT, NT = S::NT, TM = S::TM, TN = S::TN;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave % S::kWaves;
     const int group = S::KW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / S::kTileThreads);
     const int units = p.tiles * p.splits;
@@ -257,7 +249,7 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
     // A matrix instruction cuts its products off where the sum so far ends, so a long sum of squares, the diagonal of G, loses a part that grows
     // with its length.  Where there are registers for it, 256 terms are summed by themselves and added to the rest in fp32 (20 x 4000 fp32:
     // relative error 2.9e-6 in one sum, 1.4e-6 so; 1000 x 1000 1.7e-6 and 0.9e-6.  Three of 1000 x 333 take 177 us, not 170).
-    constexpr bool kBySpans = PL == 2 && MT * NT <= 4;
+    constexpr bool kBySpans = MT * NT <= 4;
     constexpr int kSpan = 8 / S::KW;                                   // stages
     floatx16 total[kBySpans ? MT : 1][kBySpans ? NT : 1];
     auto add_span = [&](bool first) {
@@ -282,12 +274,12 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
     // Fragments are read one step (16 of the summed index) ahead of the products that take them, so that shared memory and the matrix
     // pipe work at the same time; the first step of the next stage is read behind the barrier that stands before the last
     // step's products.  By then the stage in hand has been read to its end, so its buffer takes the stage after the next.
-    constexpr int kInStage = 4 / PL;
-    half8 a[2][PL][MT], b[2][PL][NT];
+    constexpr int kInStage = 2;
+    half8 a[2][2][MT], b[2][2][NT];
     auto read = [&](int set, int buffer, int j) {
         const char *ra = read_a + buffer * (S::KW * S::kStage), *rb = read_b + buffer * (S::KW * S::kStage);
 #pragma unroll
-        for (int pl = 0; pl < PL; ++pl) {
+        for (int pl = 0; pl < 2; ++pl) {
 #pragma unroll
             for (int t = 0; t < MT; ++t) a[set][pl][t] = frag(ra, t, 4 * pl + 2 * j + high);
 #pragma unroll
@@ -298,10 +290,10 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
     // a stage; the later stages stay on their way.
     constexpr int kLoads = kLoadsA + kLoadsB;
     auto arrive = [&] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S::kBuffers - 2) * kLoads) : "memory"); };
-    constexpr int kReads = PL * (MT + NT), kProducts = (PL == 2 ? 3 : 1) * MT * NT;
+    constexpr int kReads = 2 * (MT + NT), kProducts = 3 * MT * NT;
     auto products = [&](int set) {
 #pragma unroll
-        for (int part = 0; part < (PL == 2 ? 3 : 1); ++part)           // hi hi, hi lo, lo hi
+        for (int part = 0; part < 3; ++part)           // hi hi, hi lo, lo hi
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -310,13 +302,12 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
     };
     // Products, then one read, in turn: reads in a row would hold up the products behind them until shared memory took them.  The
     // loads of a stage come first (they write shared memory, so no read passes them), a product between them.
-    constexpr int kBetween = PL == 2 ? 1 : 0;
     auto in_turn = [&](auto loads) {
-        constexpr int kFirst = decltype(loads)::value ? kLoads : 0, kEach = (kProducts - kFirst * kBetween) / kReads > 0 ? (kProducts - kFirst * kBetween) / kReads : 1;
+        constexpr int kFirst = decltype(loads)::value ? kLoads : 0, kEach = (kProducts - kFirst) / kReads > 0 ? (kProducts - kFirst) / kReads : 1;
 #pragma unroll
         for (int q = 0; q < kFirst; ++q) {
             __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
-            if (kBetween) __builtin_amdgcn_sched_group_barrier(0x008, kBetween, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         }
 #pragma unroll
         for (int q = 0; q < kReads; ++q) {

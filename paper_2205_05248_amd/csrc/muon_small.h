@@ -1,8 +1,7 @@
 // The whole Newton-Schulz iteration of a small matrix in one workgroup: X, its transpose, G and P stay in shared memory.
 // A product of such a matrix takes a microsecond and a launch costs more: three products a step and the two passes around them
 // were 18 launches and 83 us for two matrices of 192 x 64.  Tiles of 16 x 16, one per wave and turn, sixteen waves: the chain of
-// dependent matrix instructions, which is what bounds it, is as short as it gets.  Planes as in muon_product.h, two of every factor
-// whatever the type: the third of the instructions that one plane would save does not show.
+// dependent matrix instructions, which is what bounds it, is as short as it gets.  Planes as in muon_product.h.
 #pragma once
 #include "muon_product.h"
 
@@ -109,8 +108,8 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
         if (k >= n) break;
         const float v = (float)(factor * u[q]);
         const int i = tall ? c : r, j = tall ? r : c;      // X[i][j]
-        put(X + i * ldx + plane_at<2>(j), v);
-        put(T + j * lds_s + plane_at<2>(i), v);
+        put(X + i * ldx + plane_at(j), v);
+        put(T + j * lds_s + plane_at(i), v);
     }
     __syncthreads();
 
@@ -162,7 +161,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
             const int m0 = i * 16, n0 = (k - i * (i + 1) / 2) * 16;
             floatx4 v;
             tiles(std::integral_constant<int, 1>{}, 1, A, lda, m0, 0, A, lda, n0, K, &v);
-            const int at = (n0 + nn) * lds_s + plane_at<2>(m0 + m4);
+            const int at = (n0 + nn) * lds_s + plane_at(m0 + m4);
             v *= alpha;
             if (beta != 0.0f) {
                 const half4 h = *reinterpret_cast<const half4 *>(G + at), l = *reinterpret_cast<const half4 *>(G + at + 32);
@@ -170,7 +169,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
             }
             put_along(D + at, v);
             if (m0 != n0)
-                for (int e = 0; e < 4; ++e) put(D + (m0 + m4 + e) * lds_s + plane_at<2>(n0 + nn), v[e]);
+                for (int e = 0; e < 4; ++e) put(D + (m0 + m4 + e) * lds_s + plane_at(n0 + nn), v[e]);
         }
         __syncthreads();
     };
@@ -185,7 +184,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
 #pragma unroll
         for (int q = 0; q < kSmallTurns; ++q)
             if (q < there) {
-                const int at = (n0 + nn) * ldx + plane_at<2>((i0 + q * side) * 16 + m4);
+                const int at = (n0 + nn) * ldx + plane_at((i0 + q * side) * 16 + m4);
                 const half4 h = *reinterpret_cast<const half4 *>(X + at), l = *reinterpret_cast<const half4 *>(X + at + 32);
                 for (int e = 0; e < 4; ++e) held[q][e] = fmaf(a.c0, (float)h[e] + (float)l[e], held[q][e] * (1.0f / kPlaneScale));
             }
@@ -194,8 +193,8 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
         for (int q = 0; q < kSmallTurns; ++q)
             if (q < there) {
                 const int m0 = (i0 + q * side) * 16;
-                put_along(X + (n0 + nn) * ldx + plane_at<2>(m0 + m4), held[q]);
-                for (int e = 0; e < 4; ++e) put(T + (m0 + m4 + e) * lds_s + plane_at<2>(n0 + nn), held[q][e]);
+                put_along(X + (n0 + nn) * ldx + plane_at(m0 + m4), held[q]);
+                for (int e = 0; e < 4; ++e) put(T + (m0 + m4 + e) * lds_s + plane_at(n0 + nn), held[q][e]);
             }
         __syncthreads();
     }
@@ -208,7 +207,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallArgs a)
     for (int q = 0; q < kSmallEntries; ++q) {
         const int k = threadIdx.x + q * kSmallThreads, r = row_of(k), c = k - r * a.cols;
         if (k >= n) break;
-        const _Float16 *at = tall ? T + r * lds_s + plane_at<2>(c) : X + r * ldx + plane_at<2>(c);
+        const _Float16 *at = tall ? T + r * lds_s + plane_at(c) : X + r * ldx + plane_at(c);
         const float x = ((float)at[0] + (float)at[32]) * (1.0f / kPlaneScale);
         static_cast<E *>(a.weights_out)[base + k] = from_f32<E>(a.weights ? a.keep * u[q] - a.rate * x : x);
     }

@@ -177,3 +177,56 @@ def test_few_rows_and_long_sums(L, rows, cols, dtype):
     binding.marl_orthogonalize(m.cuda(), out, workspace(dtype, L, rows, cols))
     torch.cuda.synchronize()
     close(out, orc.orthogonalize(host(m)), dtype, "out")
+
+
+# What two planes of every factor leave, for all types.  A plane pair is off by at most 2^-22 of its value, and the sums of three products
+# by as much again; signs are random, so that both products of a step carry sqrt(2) 2^-22 of the root mean square.  A step has coefficients
+# of 10.3 in all, and five steps of that size add up: 5 * 10.3 * sqrt(2) * 2^-22 = 1.7e-5 (one plane alone leaves 1.2e-3 to 2.9e-3).  Rounding to the
+# output's type moves w + d by no more than w by itself plus twice |d|.
+INSIDE = 5 * 10.3 * 2 ** 0.5 * 2.0 ** -22
+
+
+def close_to_rounding(got, want, dtype, name):
+    """got, want: torch, want in 64 bits on the GPU."""
+    err = (got.double() - want).square().mean().sqrt()
+    rounding = (want.to(DT[dtype]).double() - want).square().mean().sqrt()
+    size = want.square().mean().sqrt()
+    assert err <= rounding + 2 * INSIDE * size, (name, float(err / size), float(rounding / size))
+
+
+def newton_schulz_64(m, steps=5, coefficients=(3.4445, -4.7750, 2.0315)):
+    """One matrix at a time, in 64 bits on the GPU."""
+    out = []
+    for one in m.double():
+        X = one.t().contiguous() if one.shape[0] > one.shape[1] else one
+        X = X / X.norm()
+        for _ in range(steps):
+            G = X @ X.t()
+            X = coefficients[0] * X + (coefficients[1] * G + coefficients[2] * (G @ G)) @ X
+        out.append(X.t() if one.shape[0] > one.shape[1] else X)
+    return torch.stack(out)
+
+
+# The products of these run on tiles of each size; sums go in parts of a tile in the last five (4096 and longer sides with tiles for
+# more than half of the compute units but not for all), with parts of 64 x 64, 128 x 128 and 256 x 256 tiles.
+@pytest.mark.parametrize("L,rows,cols", [(4, 64, 48), (2, 200, 640), (1, 24, 4096), (1, 512, 512), (2, 1024, 1000), (1, 130, 5000), (1, 2000, 4100),
+                                         (4, 4099, 1000), (9, 1100, 4097), (1, 4096, 4100)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_all_that_is_lost_is_the_rounding_of_the_result(L, rows, cols, dtype):
+    m = gradient(gen(rows), L, rows, cols, dtype).cuda()
+    out = torch.empty_like(m)
+    binding.marl_orthogonalize(m, out, workspace(dtype, L, rows, cols))
+    close_to_rounding(out, newton_schulz_64(m), dtype, "out")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("L,rows,cols", [(2, 300, 520), (1, 2000, 4100)])
+def test_the_update_loses_no_more_than_its_rounding(L, rows, cols, dtype):
+    """Weights of zero: what is left is lr times the orthogonal factor, at its own precision."""
+    g = gen(rows + 1)
+    grad, mom = gradient(g, L, rows, cols, dtype).cuda(), (randn(g, L, rows, cols) * 1e-2).cuda()
+    w = torch.zeros_like(grad)
+    wo, mo = torch.empty_like(w), torch.empty_like(mom)
+    binding.marl_muon_step(w, grad, mom, wo, mo, workspace(dtype, L, rows, cols), lr=1.0, beta=0.9, scale=1.0)
+    momentum = 0.9 * mom.double() + grad.double()
+    close_to_rounding(wo, -newton_schulz_64(grad.double() + 0.9 * momentum), dtype, "weights")
