@@ -518,7 +518,7 @@ int marl_linear_step(int32_t dtype, int32_t n, int32_t C, const void *x, int64_t
  *   logp     dev [R] f32 or NULL        entropy, log_sum   dev [R] f32 or NULL
  *   top_id   dev [R,K] i32, top_logp dev [R,K] f32   in descending order of the logit, ties to the lowest index; -1 and
  *                                       -infinity where fewer are available.  Both NULL with K = 0; K <= 64
- * A row with nothing available has logp 0, entropy 0, log_sum -infinity, and no gradient.  An available NaN or
+ * A row with nothing available has logp 0, entropy 0, log_sum -infinity, and no gradient.  An available NaN or z of
  * +infinity makes logp, entropy and log_sum of its row NaN, and its top entries unspecified indexes of the row.
  * R may be 0; 1 <= V < 2^30, R < 2^31.
  */

@@ -18,7 +18,8 @@ namespace {
 // state is h -> A h + H, and stretches compose: a lane composes its own steps, the two groups of 16-bit types compose by lane
 // exchange, the waves through shared memory, and units through memory (see look_back).  The inputs are read once and stay
 // in registers until the state at the unit's start is known.
-// Narrow and long units: the number of units of one sequence in flight, which is what look_back walks over, is small.  Four
+// Narrow and long units: the number of units of one sequence in flight, which is what look_back walks over, is small.  Fewer than 64
+// channels leave lanes without work: 64 x 4000 steps fp32 take 114 us there and back with 16 channels, 179 us with 64.  Four
 // bytes a lane rather than sixteen: with eight channels a lane the lane exchanges were eight per element of the backward pass.
 constexpr int kChannels = 64;
 template <typename E> constexpr int kWide = 4 / (int)sizeof(E);            // V: channels of a lane, groups of a wave
@@ -297,9 +298,10 @@ __device__ __forceinline__ Place place_of(const ScanArgs &p, int *shared)
     return {seq, id / p.sequences, seq / p.tiles, seq % p.tiles * kChannels};
 }
 
-// Forward.  Every input is read once and y written once.  What bounds it is the vector unit next to memory: 35 instructions an element, six
-// of them transcendental.  40001 x 1024 bf16 takes 85 us (3.8 TB/s), 4 x 16384 x 2048 bf16 takes 241 us (4.5 TB/s; a large copy reaches
-// 5.25); 320 x 120 x 64 fp32, one unit a sequence, 11 us.
+// Forward.  Every input is read once and y written once.  34 instructions an element, six of them transcendental, but waves wait 53 to 55 %
+// of their cycles: a unit's loads all stand at its start, and what follows them is a chain through shared memory and the units before.
+// 40001 x 1024 bf16 takes 86 us with its small launch (3.8 TB/s), 4 x 16384 x 2048 bf16 225 us (4.8 TB/s; a large copy reaches 5.25); 320 x 120 x 64
+// fp32, one unit a sequence, 10 us.
 template <typename E, bool PAIRS, int NW, bool CHAIN>
 __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
 {
@@ -448,8 +450,8 @@ __global__ __launch_bounds__(NW * kWave, 4) void scan_kernel(ScanArgs p)
 }
 
 // Backward pass.  D[t] = a[t] dL/dh[t] is what reaches h[t-1]: D[t] = a[t] (grad_y[t] + D[t+1]), the same kind of chain
-// backwards in time.  h is formed again inside the unit from the state kept at its start.  66 instructions an element and three waves
-// on a SIMD, which wait for memory more than half of the time: 4 x 16384 x 2048 bf16 takes 473 us (4.0 TB/s), 320 x 120 x 64 fp32 19 us.
+// backwards in time.  h is formed again inside the unit from the state kept at its start.  69 instructions an element and three waves
+// on a SIMD, which wait 56 % of their cycles: 4 x 16384 x 2048 bf16 takes 457 us with its small launches (4.1 TB/s), 320 x 120 x 64 fp32 22 us.
 template <typename E, bool PAIRS, int NW, bool CHAIN>
 __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
 {
@@ -457,7 +459,7 @@ __global__ __launch_bounds__(NW * kWave, 3) void scan_grad_kernel(ScanArgs p)
     __shared__ float rate_s[kChannels], A_s[NW][kChannels], H_s[NW][kChannels], R_s[NW][kChannels], carry_s[NW][kChannels], after_s[NW][kChannels];
     __shared__ int id_s;
     __shared__ Word held_s[CHAIN ? 32 : 1][kChannels];          // (three units on a compute unit: 53 KB each)
-    __shared__ uint32_t grad_s[CHAIN ? Tc : 1][NW * kWave];    // grad_y during look_back, for whose registers four spilled (489 us, not 473)
+    __shared__ uint32_t grad_s[CHAIN ? Tc : 1][NW * kWave];    // grad_y during look_back, for whose registers four spilled otherwise
     const Place at = place_of<CHAIN>(p, &id_s);
     const int unit = p.units - 1 - at.unit;                    // the last steps first
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), group = lane / (kWave / V), cl = lane % (kWave / V) * V;

@@ -250,7 +250,7 @@ struct Piece {
 
 // How many entries a row begins behind a line of 128 bytes.  Pieces are counted from there, so that a wave reads and writes whole
 // lines: 8191 rows of 50021 in fp16 took 194 us forward and 364 us backward from where they begin, 165 and 364 us from a multiple of 16
-// bytes on, and take 160 and 337 us.
+// bytes on, and take 160 and 334 us.
 template <typename E>
 __device__ __forceinline__ int skew_of(const E *l) { return (int)((reinterpret_cast<uintptr_t>(l) & 127) / sizeof(E)); }
 
@@ -280,7 +280,7 @@ constexpr int kChunk = kThreads * kHeld;               // of a workgroup
 
 // A workgroup takes `per` chunks of a row; with one part per row it finishes the row, otherwise join_kernel does.  With
 // alternatives a part is one chunk, which stays in registers for wave_top.  8191 x 50021 fp16: 160 us, 5.1 TB/s, 11 instructions a logit.
-// 16 x 131072 bf16 with twenty alternatives: 13 us, and 5.5 us for the join; 256 workgroups of one chunk each, so what it costs is
+// 16 x 131072 bf16 with twenty alternatives: 13 us, and 6 us for the join; 256 workgroups of one chunk each, so what it costs is
 // one chunk's chain of loads, ballots and counts.
 template <typename E, bool TOP>
 __global__ __launch_bounds__(kThreads) void long_rows_kernel(LogProbArgs p)
@@ -470,7 +470,8 @@ struct FlatRows {
 };
 
 // G lanes hold a row of at most G N logits; a wave takes 64 / G rows.  409600 x 40 fp32 with a mask: 24 us forward (3.5 TB/s, its
-// instructions bound it), 29 us backward (5 TB/s).
+// instructions bound it), 29 us backward (5 TB/s).  20000 x 1000 fp32: 46 us both ways; bf16 72 us, for a lane reads an entry at a time.
+// Alternatives of rows up to 256 are found by a pass each: 20000 x 256 fp32 takes 7 us without, 12 with five, 58 with fifty.
 template <typename E, int G, int N, bool FLAT>
 __global__ __launch_bounds__(kThreads) void short_rows_kernel(LogProbArgs p)
 {
@@ -563,7 +564,7 @@ __device__ __forceinline__ float grad_of(const RowGrad &g, float logit, bool tak
 }
 
 // A workgroup takes `per` chunks of a row (the whole row if it overwrites the logits: the token's is read before any is gone).
-// 8191 x 50021 fp16: 337 us, 4.9 TB/s, as a large copy.
+// 8191 x 50021 fp16: 334 us, 4.9 TB/s; a large copy reaches 5.25.
 template <typename E>
 __global__ __launch_bounds__(kThreads, 8) void long_grad_kernel(LogProbArgs p)
 {

@@ -189,14 +189,14 @@ int tiles_of(int shape, int Mp, int Np, bool symmetric)
 Plan plan_of(int L, int Mp, int Np, bool symmetric, int stages)
 {
     // The largest tile of which half the compute units get one.  A G or P that still leaves compute units without one and is long
-    // enough to pay for a second pass over its sums (2048 x 8192 bf16, G: 70 us, 92 in one part) goes in parts.
+    // enough to pay for a second pass over its sums (2048 x 8192, G: 134 us, 179 in one part; 4096 x 4096, G and P: 236, 248) goes in parts.
     Plan best{2, 1};
     for (int shape = 0; shape < 3; ++shape)
         if ((int64_t)tiles_of(shape, Mp, Np, symmetric) * L >= 128) { best.shape = shape; break; }
     const int64_t tiles = (int64_t)tiles_of(best.shape, Mp, Np, symmetric) * L;
     if (symmetric && stages >= 128 && tiles < 256) best.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, stages / 16));
     // One 128 x 128 tile on a compute unit: two groups of waves, each with half of the sum, keep it busier than one (2048 x 2048 fp32:
-    // 3 us less a G or P, 6 an X; with more tiles two workgroups do that, and this would cost 28 us of 2048 x 8192 bf16's X).
+    // 3 us less a G or P, 6 an X; with more tiles two workgroups do that).
     if (best.shape == 1 && best.splits == 1 && tiles <= 256) best.shape = 3;
     return best;
 }

@@ -6,7 +6,7 @@
 // same way; G and P are symmetric, and X is kept beside its transpose.
 //
 // A product is hi hi + hi lo + lo hi in fp32 accumulators; what is left out, lo lo, is 2^-22 of a term.  Planes alternate in blocks of 32
-// of the summed index, [hi x 32][lo x 32].  (One plane is not enough for bf16 matrices either: it leaves 1.2e-3 to 2.9e-3 of the result, where
+// of the summed index, [hi x 32][lo x 32].  (One plane is not enough for bf16 matrices either: it leaves 1.2e-3 to 2.8e-3 of the result, where
 // its rounding to bf16 leaves 1.7e-3.)
 #pragma once
 #include <hip/hip_runtime.h>
@@ -248,7 +248,8 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product p)
 
     // A matrix instruction cuts its products off where the sum so far ends, so a long sum of squares, the diagonal of G, loses a part that grows
     // with its length.  Where there are registers for it, 256 terms are summed by themselves and added to the rest in fp32 (20 x 4000 fp32:
-    // relative error 2.9e-6 in one sum, 1.4e-6 so; 1000 x 1000 1.7e-6 and 0.9e-6.  Three of 1000 x 333 take 177 us, not 170).
+    // relative error 2.9e-6 in one sum, 1.4e-6 so; 1000 x 1000 1.7e-6 and 0.9e-6; fp32 products of an elementary form leave
+    // 1.15e-6 and 2.5e-6.  Three of 1000 x 333 take 4 % longer for it).
     constexpr bool kBySpans = MT * NT <= 4;
     constexpr int kSpan = 8 / S::KW;                                   // stages
     floatx16 total[kBySpans ? MT : 1][kBySpans ? NT : 1];
