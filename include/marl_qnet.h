@@ -570,6 +570,128 @@ int marl_muon_step(int32_t dtype, int32_t L, int32_t rows, int32_t cols, const v
                    size_t workspace_bytes, float lr, float beta, int32_t nesterov, float weight_decay, float scale,
                    int32_t steps, const float *coefficients, float eps, void *hip_stream);
 
+/*
+ * Gated delta rule over B sequences of T steps: a memory whose state is a matrix per head, which holds what it was last
+ * told about every direction of the key.  Hv value heads share Hk key heads (Hv a multiple of Hk; value head h reads
+ * key head h / (Hv / Hk)).  Per sequence and value head, with S [Dk,Dv] and S' its transpose:
+ *   a = exp(log_decay)      u = beta (v - a S[t-1]' k)      S[t] = a S[t-1] + k u'      o = scale S[t]' q
+ *   q, k       dev [B,T,Hk,Dk] elem, v dev [B,T,Hv,Dv] elem; rows (b T + t) ld_q, ld_k, ld_v apart, heads adjacent
+ *              within a row
+ *   log_decay  dev [B,T,Hv] f32        -infinity forgets everything, as reset does.  Finite values below -200 count as -200
+ *   beta       dev [B,T,Hv] f32
+ *   scale      finite
+ *   reset      dev [B,T] u8 or NULL    nonzero: a sequence starts at this step, a is 0 whatever log_decay holds
+ *   filled     dev [B,T] u8 or NULL    zero: padding; S passes unchanged, o is 0, and everything else of the row, its
+ *                                      upstream gradient included, is not looked at, whatever it holds
+ *   s_first    dev [B,Hv,Dk,Dv] f32 or NULL (zero)   state before step 0
+ *   o          dev [B,T,Hv,Dv] elem, rows ld_o apart; no input
+ *   s_last     dev [B,Hv,Dk,Dv] f32 or NULL          state after step T-1 (s_first if T is 0); may be s_first
+ *   keep       nonzero: the workspace afterwards holds what marl_delta_scan_grad starts from
+ * 1 <= Dk <= 128, 1 <= Dv <= 1024, 1 <= Hk <= Hv <= 1024.  B and T may be 0 (B Hv < 2^24, B T < 2^30); row distances are
+ * below 2^31.  The state stays bounded for keys of norm at most 1 with beta between 0 and 2 and log_decay at most 0;
+ * beyond that it grows as the formula says.  An infinity or NaN reaches no step before its own and none of another
+ * sequence.
+ */
+int marl_delta_scan_workspace_bytes(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_t Hv, int32_t Dk, int32_t Dv,
+                                    int32_t keep, size_t *bytes);
+int marl_delta_scan(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_t Hv, int32_t Dk, int32_t Dv, const void *q,
+                    int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v, const float *log_decay,
+                    const float *beta, float scale, const uint8_t *reset, const uint8_t *filled, const float *s_first,
+                    void *o, int64_t ld_o, float *s_last, int32_t keep, void *workspace, size_t workspace_bytes,
+                    void *hip_stream);
+
+/*
+ * Backward pass of marl_delta_scan, which must have run with keep and the same sizes, inputs and workspace before it.
+ *   grad_o       dev [B,T,Hv,Dv] elem, rows ld_go apart    dL/do
+ *   grad_s_last  dev [B,Hv,Dk,Dv] f32 or NULL (zero)       dL/ds_last
+ *   grad_q, grad_k   dev [B,T,Hk,Dk] elem, grad_v dev [B,T,Hv,Dv] elem, rows ld_gq, ld_gk, ld_gv apart, overwritten
+ *                (0 in padding); summed over the value heads of a key head in a fixed order; none may be an input
+ *   grad_log_decay, grad_beta   dev [B,T,Hv] f32, overwritten (0 in padding; that of log_decay is 0 where a is 0)
+ *   grad_s_first dev [B,Hv,Dk,Dv] f32 or NULL, overwritten; may be grad_s_last
+ */
+int marl_delta_scan_grad(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_t Hv, int32_t Dk, int32_t Dv,
+                         const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
+                         const float *log_decay, const float *beta, float scale, const uint8_t *reset,
+                         const uint8_t *filled, const void *grad_o, int64_t ld_go, const float *grad_s_last,
+                         void *workspace, size_t workspace_bytes, void *grad_q, int64_t ld_gq, void *grad_k,
+                         int64_t ld_gk, void *grad_v, int64_t ld_gv, float *grad_log_decay, float *grad_beta,
+                         float *grad_s_first, void *hip_stream);
+
+/*
+ * The delta rule for one step of n sequences whose states are rows of a table (serving; the worker's step).
+ *   q, k   dev [n,Hk,Dk] elem, v dev [n,Hv,Dv] elem, rows ld_q, ld_k, ld_v apart
+ *   log_decay, beta   dev [n,Hv] f32
+ *   slot   dev [n] i32 or NULL (0, 1, 2, ...)   row of each sequence; clamped into [0, slots); duplicates make the
+ *                                               duplicated rows unspecified
+ *   reset  dev [n] u8 or NULL
+ *   s_in   dev [slots,Hv,Dk,Dv] f32     s_out dev [slots,Hv,Dk,Dv] f32, only the listed rows are written; may be s_in
+ *   o      dev [n,Hv,Dv] elem, rows ld_o apart
+ * n may be 0; slots >= 1, and without `slot` n <= slots; n Hv < 2^24.
+ */
+int marl_delta_step(int32_t dtype, int32_t n, int32_t Hk, int32_t Hv, int32_t Dk, int32_t Dv, const void *q,
+                    int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v, const float *log_decay,
+                    const float *beta, float scale, const int32_t *slot, int32_t slots, const uint8_t *reset,
+                    const float *s_in, float *s_out, void *o, int64_t ld_o, void *hip_stream);
+
+/*
+ * Divergence of a student's R rows of V logits from K alternatives of a teacher, as marl_log_prob gives them.  Over the
+ * places that are available and have probability, q = softmax(scale * logit); p comes from the alternatives that are
+ * kept: those whose id is such a place (an id of -1, outside the row, or of a place without probability is left out).
+ *   tail zero:     p = softmax(top_value over the kept ones)
+ *                  loss = sum p (log p - log q)
+ *   tail nonzero:  p = exp(top_value), p_r = max(0, 1 - sum p) for all places that are not kept, whose probability is
+ *                  q_r;  loss = sum p (log p - log q) + p_r (log p_r - log q_r), without the last part where q_r is 0
+ *   logits     dev [R,V] elem, rows ld apart;   avail, scale   as in marl_log_prob
+ *   top_id     dev [R,K] i32, top_value dev [R,K] f32 (log probabilities; with tail zero any logits will do);
+ *              -infinity: no probability.  An id that is listed twice stands for both of its parts
+ *   loss       dev [R] f32
+ *   log_sum    dev [R] f32 or NULL     as in marl_log_prob
+ *   log_rest   dev [R] f32 or NULL     log q_r, -infinity if no place is left; written with tail nonzero only
+ * A row without any kept alternative has loss 0 and no gradient, and so has one with nothing available (log_sum and
+ * log_rest -infinity).  An available NaN or z of +infinity, or a kept value of NaN or +infinity, makes the row's loss NaN
+ * (the first two its log_sum and log_rest too).  1 <= K <= 64; R may be 0; 1 <= V < 2^30, R < 2^31.
+ */
+int marl_distill_workspace_bytes(int32_t R, int32_t V, int32_t K, size_t *bytes);
+int marl_distill(int32_t dtype, int32_t R, int32_t V, int32_t K, const void *logits, int64_t ld, const int32_t *top_id,
+                 const float *top_value, const uint8_t *avail, int64_t ld_avail, float scale, int32_t tail, float *loss,
+                 float *log_sum, float *log_rest, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gradient of the logits, from the log_sum and (with tail nonzero) the log_rest that marl_distill gave; W = sum p + p_r
+ * (p_r 0 with tail zero):
+ *   grad_logits[j] = scale grad_loss ( W q[j] - p[j] )          for a kept place (p summed if listed twice)
+ *                    scale grad_loss ( W - p_r / q_r ) q[j]     for any other
+ * and 0 in every place that is not available or has no probability, and in a row whose grad_loss is 0.  A row whose
+ * loss is NaN otherwise has a gradient of NaN in all others.
+ *   grad_loss dev [R] f32, grad_logits dev [R,V] elem, rows ld_grad apart; may be logits (same ld)
+ */
+int marl_distill_grad(int32_t dtype, int32_t R, int32_t V, int32_t K, const void *logits, int64_t ld,
+                      const int32_t *top_id, const float *top_value, const uint8_t *avail, int64_t ld_avail,
+                      float scale, int32_t tail, const float *log_sum, const float *log_rest, const float *grad_loss,
+                      void *grad_logits, int64_t ld_grad, void *hip_stream);
+
+/*
+ * Edit of R rows of V logits between the network and the sampling.  Per row, with c[j] the number of times that j was
+ * generated and `seen` for what stands in the prompt or was generated:
+ *   z = logit;   seen: z > 0 ? z / repetition : z * repetition;   z -= c > 0 ? presence : 0;   z -= frequency c
+ *   z += the biases listed for j, in their order;   not allowed: z = -infinity, whatever the logit holds
+ *   logits     dev [R,V] elem, rows ld apart      out dev [R,V] elem, rows ld_out apart; may be logits (same ld)
+ *   history    dev [R,L] i32 or NULL (L = 0), rows ld_history apart: the prompt, then what was generated; ids outside
+ *              [0, V) count for nothing
+ *   length     dev [R] i32 or NULL (L)      tokens of the row, clamped into [0, L]
+ *   prompt     dev [R] i32 or NULL (0)      how many of them are the prompt's, clamped into [0, length]
+ *   repetition, presence, frequency   dev [R] f32 or NULL (1, 0, 0); repetition positive
+ *   bias_id    dev [R,M] i32, bias_value dev [R,M] f32, or both NULL (M = 0); ids outside [0, V) are left out
+ *   allowed    dev i32 or NULL (all)        bit j % 32 of word j / 32; [R, ceil(V/32)], rows ld_allowed apart;
+ *              ld_allowed = 0: one row of words for all
+ * R may be 0; 1 <= V < 2^30, R < 2^24; 0 <= L < 2^24; 0 <= M <= 1024.
+ */
+int marl_penalize(int32_t dtype, int32_t R, int32_t V, const void *logits, int64_t ld, int32_t L,
+                  const int32_t *history, int64_t ld_history, const int32_t *length, const int32_t *prompt,
+                  const float *repetition, const float *presence, const float *frequency, int32_t M,
+                  const int32_t *bias_id, const float *bias_value, const int32_t *allowed, int64_t ld_allowed,
+                  void *out, int64_t ld_out, void *hip_stream);
+
 /* Free the handle, its weights and scratch.  Synchronises the device.  NULL is allowed. */
 int marl_destroy(marl_qnet *q);
 

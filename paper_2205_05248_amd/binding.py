@@ -28,7 +28,9 @@ EXPORTS = ["marl_param_count", "marl_qnet_create", "marl_qnet_get_desc", "marl_a
            "marl_qnet_set_kernels", "marl_qnet_kernels_in_use", "marl_qnet_set_weights",
            "marl_linear_scan_workspace_bytes", "marl_linear_scan", "marl_linear_scan_grad", "marl_linear_step",
            "marl_log_prob_workspace_bytes", "marl_log_prob", "marl_log_prob_grad",
-           "marl_muon_workspace_bytes", "marl_orthogonalize", "marl_muon_step"]
+           "marl_muon_workspace_bytes", "marl_orthogonalize", "marl_muon_step",
+           "marl_delta_scan_workspace_bytes", "marl_delta_scan", "marl_delta_scan_grad", "marl_delta_step",
+           "marl_distill_workspace_bytes", "marl_distill", "marl_distill_grad", "marl_penalize"]
 # include/marl_mixer.h
 MIXER_EXPORTS = ["marl_mixer_param_count", "marl_mixer_create", "marl_mixer_destroy", "marl_mixer_td",
                  "marl_mixer_set_weights", "marl_mixer_grad_workspace_bytes", "marl_mixer_grad", "marl_mixer_sgd_step", "marl_mixer_rmsprop_step"]
@@ -151,7 +153,17 @@ def load():
                 "marl_log_prob_grad": [i32, i32, i32, vp, i64, vp, vp, i64, f32, vp, vp, vp, vp, vp, i64, vp],
                 "marl_muon_workspace_bytes": [i32, i32, i32, i32, out],
                 "marl_orthogonalize": [i32, i32, i32, i32, vp, vp, vp, size, i32, vp, f32, vp],
-                "marl_muon_step": [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, size, f32, f32, i32, f32, f32, i32, vp, f32, vp]}.items():
+                "marl_muon_step": [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, size, f32, f32, i32, f32, f32, i32, vp, f32, vp],
+                "marl_delta_scan_workspace_bytes": [i32, i32, i32, i32, i32, i32, i32, i32, out],
+                "marl_delta_scan": [i32, i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, vp, vp, vp, i64, vp, i32, vp,
+                                    size, vp],
+                "marl_delta_scan_grad": [i32, i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, vp, vp, i64, vp, vp, size,
+                                         vp, i64, vp, i64, vp, i64, vp, vp, vp, vp],
+                "marl_delta_step": [i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, i32, vp, vp, vp, vp, i64, vp],
+                "marl_distill_workspace_bytes": [i32, i32, i32, out],
+                "marl_distill": [i32, i32, i32, i32, vp, i64, vp, vp, vp, i64, f32, i32, vp, vp, vp, vp, size, vp],
+                "marl_distill_grad": [i32, i32, i32, i32, vp, i64, vp, vp, vp, i64, f32, i32, vp, vp, vp, vp, i64, vp],
+                "marl_penalize": [i32, i32, i32, vp, i64, i32, vp, i64, vp, vp, vp, vp, vp, i32, vp, vp, vp, i64, vp, i64, vp]}.items():
             getattr(lib, name).restype = ctypes.c_int
             getattr(lib, name).argtypes = args
         _lib = lib
@@ -770,3 +782,127 @@ def marl_muon_step(weights, grad, momentum, weights_out, momentum_out, workspace
         address(momentum, "momentum", f32), address(weights_out, "weights_out", weights.dtype), address(momentum_out, "momentum_out", f32),
         *_workspace(workspace, d), float(lr), float(beta), int(bool(nesterov)), float(weight_decay), float(scale), int(steps),
         _coefficients(coefficients), float(eps), _stream_of(d)))
+
+
+def _heads(t, dtype, shape, name, device):
+    """Address and row distance of a tensor [..., H, D] on `device`: heads adjacent within a row, rows evenly spaced."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device:
+        H, D, strides = shape[-2], shape[-1], t.stride()
+        if (D <= 1 or strides[-1] == 1) and (H <= 1 or strides[-2] == D):
+            if len(shape) == 3:
+                ld = strides[0] if shape[0] > 1 else H * D
+                if ld >= H * D:
+                    return t.data_ptr(), ld
+            elif len(shape) == 4:
+                B, T = shape[0], shape[1]
+                ld = strides[1] if T > 1 else strides[0] if B > 1 else H * D
+                if ld >= H * D and (B == 1 or T <= 1 or strides[0] == ld * T):
+                    return t.data_ptr(), ld
+        if t.is_contiguous():
+            return t.data_ptr(), H * D
+    raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the current device with adjacent heads and "
+                     f"evenly spaced rows, got {t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
+
+
+def marl_delta_scan_workspace_bytes(dtype, B, T, Hk, Hv, Dk, Dv, keep=False):
+    """dtype: "fp32", "bf16" or "fp16", the element type of the sequences; keep: as in marl_delta_scan."""
+    return _bytes_of(load().marl_delta_scan_workspace_bytes, _dtype_code(dtype), int(B), int(T), int(Hk), int(Hv), int(Dk), int(Dv), int(bool(keep)))
+
+
+def marl_delta_scan(q, k, v, log_decay, beta, scale, reset, filled, s_first, o, s_last, workspace, keep=False):
+    """Gated delta rule over q, k [B,T,Hk,Dk] and v, o [B,T,Hv,Dv]; log_decay, beta [B,T,Hv]; reset, filled [B,T] u8 and s_first, s_last
+    [B,Hv,Dk,Dv] may be None.  keep: the workspace is left for marl_delta_scan_grad."""
+    code, d = _element(q, "q"), _current_device()
+    B, T, Hk, Dk = q.shape
+    Hv, Dv = v.shape[2:]
+    keys, values, state = (B, T, Hk, Dk), (B, T, Hv, Dv), (B, Hv, Dk, Dv)
+    check(load().marl_delta_scan(
+        code, B, T, Hk, Hv, Dk, Dv, *_heads(q, q.dtype, keys, "q", d), *_heads(k, q.dtype, keys, "k", d), *_heads(v, q.dtype, values, "v", d),
+        _flat(log_decay, "f32", (B, T, Hv), "log_decay", d), _flat(beta, "f32", (B, T, Hv), "beta", d), float(scale),
+        _flat(reset, "u8", (B, T), "reset", d, True), _flat(filled, "u8", (B, T), "filled", d, True), _flat(s_first, "f32", state, "s_first", d, True),
+        *_heads(o, q.dtype, values, "o", d), _flat(s_last, "f32", state, "s_last", d, True), int(bool(keep)), *_workspace(workspace, d), _stream_of(d)))
+
+
+def marl_delta_scan_grad(q, k, v, log_decay, beta, scale, reset, filled, grad_o, grad_s_last, workspace, grad_q, grad_k, grad_v, grad_log_decay,
+                         grad_beta, grad_s_first=None):
+    """workspace: as marl_delta_scan with keep left it for the same inputs; grad_s_last, grad_s_first may be None."""
+    code, d = _element(q, "q"), _current_device()
+    B, T, Hk, Dk = q.shape
+    Hv, Dv = v.shape[2:]
+    keys, values, gates, state = (B, T, Hk, Dk), (B, T, Hv, Dv), (B, T, Hv), (B, Hv, Dk, Dv)
+    heads = lambda t, shape, name: _heads(t, q.dtype, shape, name, d)
+    check(load().marl_delta_scan_grad(
+        code, B, T, Hk, Hv, Dk, Dv, *heads(q, keys, "q"), *heads(k, keys, "k"), *heads(v, values, "v"),
+        _flat(log_decay, "f32", gates, "log_decay", d), _flat(beta, "f32", gates, "beta", d), float(scale),
+        _flat(reset, "u8", (B, T), "reset", d, True), _flat(filled, "u8", (B, T), "filled", d, True), *heads(grad_o, values, "grad_o"),
+        _flat(grad_s_last, "f32", state, "grad_s_last", d, True), *_workspace(workspace, d), *heads(grad_q, keys, "grad_q"),
+        *heads(grad_k, keys, "grad_k"), *heads(grad_v, values, "grad_v"), _flat(grad_log_decay, "f32", gates, "grad_log_decay", d),
+        _flat(grad_beta, "f32", gates, "grad_beta", d), _flat(grad_s_first, "f32", state, "grad_s_first", d, True), _stream_of(d)))
+
+
+def marl_delta_step(q, k, v, log_decay, beta, scale, slot, reset, s_in, s_out, o):
+    """One step of n sequences: q, k [n,Hk,Dk], v, o [n,Hv,Dv], log_decay, beta [n,Hv]; slot [n] i32 or None picks rows of s_in, s_out
+    [slots,Hv,Dk,Dv] (may be the same)."""
+    code, d = _element(q, "q"), _current_device()
+    n, Hk, Dk = q.shape
+    Hv, Dv = v.shape[1:]
+    keys, values, slots = (n, Hk, Dk), (n, Hv, Dv), s_in.shape[0]
+    table = (slots, Hv, Dk, Dv)
+    check(load().marl_delta_step(
+        code, n, Hk, Hv, Dk, Dv, *_heads(q, q.dtype, keys, "q", d), *_heads(k, q.dtype, keys, "k", d), *_heads(v, q.dtype, values, "v", d),
+        _flat(log_decay, "f32", (n, Hv), "log_decay", d), _flat(beta, "f32", (n, Hv), "beta", d), float(scale), _flat(slot, "i32", (n,), "slot", d, True),
+        slots, _flat(reset, "u8", (n,), "reset", d, True), _flat(s_in, "f32", table, "s_in", d), _flat(s_out, "f32", table, "s_out", d),
+        *_heads(o, q.dtype, values, "o", d), _stream_of(d)))
+
+
+def marl_distill_workspace_bytes(R, V, K):
+    return _bytes_of(load().marl_distill_workspace_bytes, int(R), int(V), int(K))
+
+
+def marl_distill(logits, top_id, top_value, avail, scale, tail, loss, log_sum=None, log_rest=None, workspace=None):
+    """logits [R,V]; the teacher's top_id [R,K] i32 and top_value [R,K]; avail [R,V] or [V] u8 or None; tail: the teacher's probability beside its
+    alternatives counts; loss, log_sum, log_rest [R]."""
+    code, d = _element(logits, "logits"), _current_device()
+    R, V = logits.shape
+    K = top_id.shape[1]
+    check(load().marl_distill(
+        code, R, V, K, *_rows(logits, logits.dtype, (R, V), "logits", d), _flat(top_id, "i32", (R, K), "top_id", d),
+        _flat(top_value, "f32", (R, K), "top_value", d), *_avail_of(avail, R, V, d), float(scale), int(bool(tail)), _flat(loss, "f32", (R,), "loss", d),
+        _flat(log_sum, "f32", (R,), "log_sum", d, True), _flat(log_rest, "f32", (R,), "log_rest", d, True), *_workspace(workspace, d), _stream_of(d)))
+
+
+def marl_distill_grad(logits, top_id, top_value, avail, scale, tail, log_sum, log_rest, grad_loss, grad_logits):
+    """Gradient of the logits; log_rest may be None with tail false.  grad_logits may be logits."""
+    code, d = _element(logits, "logits"), _current_device()
+    R, V = logits.shape
+    K = top_id.shape[1]
+    check(load().marl_distill_grad(
+        code, R, V, K, *_rows(logits, logits.dtype, (R, V), "logits", d), _flat(top_id, "i32", (R, K), "top_id", d),
+        _flat(top_value, "f32", (R, K), "top_value", d), *_avail_of(avail, R, V, d), float(scale), int(bool(tail)),
+        _flat(log_sum, "f32", (R,), "log_sum", d), _flat(log_rest, "f32", (R,), "log_rest", d, True), _flat(grad_loss, "f32", (R,), "grad_loss", d),
+        *_rows(grad_logits, logits.dtype, (R, V), "grad_logits", d), _stream_of(d)))
+
+
+def _plain_rows(t, dtype, shape, name, device, optional=True):
+    """_rows for an argument that may be None."""
+    return (None, 0) if t is None and optional else _rows(t, _dtypes[dtype], shape, name, device)
+
+
+def marl_penalize(logits, history, length, prompt, repetition, presence, frequency, bias_id, bias_value, allowed, out):
+    """Penalties, biases and a grammar's mask on logits [R,V]; history [R,L] i32, length, prompt [R] i32, repetition, presence, frequency [R],
+    bias_id [R,M] i32, bias_value [R,M], allowed [R,ceil(V/32)] or [ceil(V/32)] i32 words of bits may be None.  out may be logits."""
+    code, d = _element(logits, "logits"), _current_device()
+    R, V = logits.shape
+    L = 0 if history is None else history.shape[1]
+    M = 0 if bias_id is None else bias_id.shape[1]
+    words = (V + 31) // 32
+    if allowed is not None and allowed.dim() == 1:
+        bits = _flat(allowed, "i32", (words,), "allowed", d), 0
+    else:
+        bits = _plain_rows(allowed, "i32", (R, words), "allowed", d)
+    per_row = lambda t, kind, name: _flat(t, kind, (R,), name, d, True)
+    check(load().marl_penalize(
+        code, R, V, *_rows(logits, logits.dtype, (R, V), "logits", d), L, *_plain_rows(history, "i32", (R, L), "history", d),
+        per_row(length, "i32", "length"), per_row(prompt, "i32", "prompt"), per_row(repetition, "f32", "repetition"),
+        per_row(presence, "f32", "presence"), per_row(frequency, "f32", "frequency"), M, _flat(bias_id, "i32", (R, M), "bias_id", d, True),
+        _flat(bias_value, "f32", (R, M), "bias_value", d, True), *bits, *_rows(out, logits.dtype, (R, V), "out", d), _stream_of(d)))

@@ -1,0 +1,150 @@
+"""Penalties, biases and grammar masks on the GPU against the 64-bit oracle.
+
+Tolerance.  Per place: the product or quotient with the repetition penalty, the presence penalty, frequency times count, and each bias round once, to
+2^-24 of the sums so far; with at most four biases on a place eight roundings of sums below S, the sum of all parts' sizes: 8 x 2^-24 S = 2^-21 S on top
+of half a step of the result's type.  A place that nothing touches is the logit itself, bit for bit.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import memory_oracle as orc
+from paper_2205_05248_amd import binding
+from policy_util import DT, gen, host, near, randn
+
+pytestmark = pytest.mark.gpu
+REL = 2.0 ** -21
+
+
+def make(R, V, L, M, dtype, seed, allowed="rows", ld=None):
+    g = gen(seed)
+    s = dict(V=V, logits=(randn(g, R, ld or V) * 3).to(DT[dtype]))
+    s["history"] = torch.randint(-1, V + 1, (R, L), generator=g).to(torch.int32) if L else None
+    if L:
+        few = torch.randint(0, V, (R, 3), generator=g)
+        again = few.gather(1, torch.randint(0, 3, (R, L), generator=g)).to(torch.int32)
+        s["history"] = torch.where(torch.rand(R, L, generator=g) < 0.5, again, s["history"])
+    s["length"] = torch.randint(-2, L + 3, (R,), generator=g).to(torch.int32)
+    s["prompt"] = torch.randint(-2, L + 3, (R,), generator=g).to(torch.int32)
+    s["repetition"], s["presence"], s["frequency"] = 1 + torch.rand(R, generator=g), torch.rand(R, generator=g), 0.3 * torch.rand(R, generator=g)
+    s["bias_id"] = torch.randint(-1, V + 1, (R, M), generator=g).to(torch.int32) if M else None
+    s["bias_value"] = randn(g, R, M) * 2 if M else None
+    words = (V + 31) // 32
+    shape = dict(rows=(R, words), shared=(words,), none=None)[allowed]
+    s["allowed"] = None if shape is None else torch.randint(-2 ** 31, 2 ** 31, shape, generator=g).to(torch.int32)
+    return s
+
+
+def run(s, in_place=False, **change):
+    V = s["V"]
+    d = {k: v.cuda() if torch.is_tensor(v) else v for k, v in {**s, **change}.items()}
+    logits = d["logits"][:, :V]
+    out = logits if in_place else torch.full((logits.shape[0], V), 7.0, dtype=logits.dtype, device="cuda")
+    binding.marl_penalize(logits, d["history"], d["length"], d["prompt"], d["repetition"], d["presence"], d["frequency"], d["bias_id"], d["bias_value"],
+                          d["allowed"], out)
+    torch.cuda.synchronize()
+    if in_place and d["logits"].shape[1] > V:
+        assert torch.equal(d["logits"][:, V:].cpu(), s["logits"][:, V:])
+    return out
+
+
+def check(s, out, **change):
+    a = {k: host(v) if torch.is_tensor(v) else v for k, v in {**s, **change}.items()}
+    names = ("history", "length", "prompt", "repetition", "presence", "frequency", "bias_id", "bias_value", "allowed")
+    logits = a["logits"][:, :s["V"]]
+    want = orc.penalize(logits, *(a[n] for n in names))
+    size = 2 * np.abs(logits) + 1.0 + (0.3 * a["history"].shape[1] if a["history"] is not None else 0) + (0 if a["bias_id"] is None else 4 * np.abs(a["bias_value"]).max(initial=0))
+    near(out, want, out.dtype, REL, "out", floor=size)
+    same = want == logits
+    assert np.array_equal(host(out)[same], logits[same])
+
+
+SIZES = [(1, 1, 0, 0), (2, 1, 5, 1), (24, 40, 120, 4), (5, 31, 7, 3), (5, 33, 64, 0), (3, 959, 300, 16), (3, 961, 300, 16), (4, 5000, 1000, 64), (2, 8161, 10, 2),
+         (2, 16384, 3000, 300), (3, 50021, 2000, 64), (1, 131072, 4096, 16)]
+
+
+@pytest.mark.parametrize("dtype,allowed", [("fp32", "rows"), ("bf16", "shared"), ("fp16", "none")])
+@pytest.mark.parametrize("size", SIZES)
+def test_penalize(size, dtype, allowed):
+    s = make(*size, dtype, sum(size), allowed)
+    check(s, run(s))
+
+
+@pytest.mark.parametrize("V", [40, 2000, 9001])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_wider_rows_and_in_place(V, in_place):
+    for dtype in ("fp32", "bf16"):
+        s = make(7, V, 50, 5, dtype, V, ld=V + 7)
+        check(s, run(s, in_place))
+
+
+@pytest.mark.parametrize("left_out", ["history", "length", "prompt", "repetition", "presence", "frequency", "bias_id", "allowed"])
+def test_optional_arguments(left_out):
+    s = make(6, 700, 80, 6, "fp32", 4)
+    change = {left_out: None}
+    if left_out == "bias_id":
+        change["bias_value"] = None
+    check(s, run(s, **change), **change)
+
+
+def test_a_token_many_times_and_a_bias_many_times():
+    s = make(2, 50, 70000, 1024, "fp32", 5, "none")
+    s["history"][:] = 3
+    s["history"][1, ::2] = 49
+    s["length"][:], s["prompt"][:] = 70000, 0
+    s["frequency"][:], s["bias_id"][:] = 2.0 ** -10, -1
+    s["bias_id"][:, 5::300] = 3
+    check(s, run(s))
+
+
+def test_history_and_bits_of_wider_arrays():
+    s = make(4, 300, 40, 0, "bf16", 6)
+    d = {k: v.cuda() if torch.is_tensor(v) else v for k, v in s.items()}
+    wide = torch.full((4, 60), 1, dtype=torch.int32, device="cuda")
+    wide[:, :40] = d["history"]
+    bits = torch.full((4, 20), -1, dtype=torch.int32, device="cuda")
+    bits[:, :10] = d["allowed"]
+    out = torch.empty(4, 300, dtype=torch.bfloat16, device="cuda")
+    binding.marl_penalize(d["logits"], wide[:, :40], d["length"], d["prompt"], d["repetition"], d["presence"], d["frequency"], None, None, bits[:, :10], out)
+    check(s, out)
+
+
+def test_what_is_not_finite_and_nothing_allowed():
+    """A masked place is not looked at; a row of which nothing is allowed is -infinity all along."""
+    s = make(3, 90, 20, 2, "fp32", 7)
+    s["logits"][:, 10], s["logits"][:, 20], s["logits"][:, 30] = float("nan"), float("inf"), -float("inf")
+    s["history"][:, 0] = 30
+    s["allowed"][1] = 0
+    out = host(run(s))
+    bits = (host(s["allowed"])[:, :, None] >> np.arange(32) & 1).reshape(3, -1)[:, :90] != 0
+    assert (out[~bits] == -np.inf).all()
+    assert np.isnan(out[:, 10][bits[:, 10]]).all() and (out[:, 20][bits[:, 20]] == np.inf).all() and (out[:, 30] == -np.inf).all()
+    with np.errstate(invalid="ignore"):
+        clean = {**s, "logits": torch.nan_to_num(s["logits"], 0.0, 0.0, 0.0)}
+    part = [j for j in range(90) if j not in (10, 20, 30)]
+    want = orc.penalize(host(clean["logits"]), *(host(s[n]) for n in ("history", "length", "prompt", "repetition", "presence", "frequency", "bias_id", "bias_value", "allowed")))
+    assert np.abs(out - want)[:, part][np.isfinite(want[:, part])].max() < 1e-4
+
+
+def test_penalties_before_log_probabilities_and_distillation():
+    """As a server uses them: the memory's step, a readout, the edit, and then log probabilities of what is left, which a student learns from."""
+    g = gen(8)
+    n, H, D, V, K = 6, 2, 16, 300, 8
+    table = torch.zeros(n, H, D, D, device="cuda")
+    q, k, v = ((randn(g, n, H, D) / 4).cuda() for _ in range(3))
+    o = torch.empty(n, H, D, device="cuda")
+    binding.marl_delta_step(q, k, v, torch.full((n, H), -0.1, device="cuda"), torch.full((n, H), 0.5, device="cuda"), 1.0, None, None, table, table, o)
+    logits = torch.matmul(o.flatten(1), randn(g, H * D, V).cuda() * 4).contiguous()
+    s = make(n, V, 30, 4, "fp32", 9)
+    s["logits"] = logits.cpu()
+    edited = run(s)
+    check(s, edited)
+    ids, values = torch.empty(n, K, dtype=torch.int32, device="cuda"), torch.empty(n, K, device="cuda")
+    log_sum = torch.empty(n, device="cuda")
+    binding.marl_log_prob(edited, None, None, 1.0, None, None, log_sum, ids, values, None)
+    allowed = (host(s["allowed"])[:, :, None] >> np.arange(32) & 1).reshape(n, -1)[:, :V] != 0
+    picked = host(ids)
+    assert all(allowed[r, j] for r in range(n) for j in picked[r] if j >= 0)
+    loss, own_sum, rest = (torch.empty(n, device="cuda") for _ in range(3))
+    binding.marl_distill(edited, ids, values, None, 1.0, True, loss, own_sum, rest, None)
+    assert torch.allclose(own_sum, log_sum, atol=2.0 ** -17) and float(loss.abs().max()) < 2.0 ** -15
