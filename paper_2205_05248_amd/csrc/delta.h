@@ -12,21 +12,32 @@
 // Factors f, t and E that are not 0 by their sequence are at least the smallest normal number: a state that is infinite or
 // NaN stays so however far it decays, and 0 says that a sequence starts in between, across which nothing is multiplied.
 #pragma once
+#include <type_traits>
+
 #include "operator_types.h"
 
 namespace marl {
 
 constexpr int kSteps = 64;                             // of a chunk
-constexpr int kCols = 16;                              // value columns of a workgroup on the way through the chunks
-constexpr int kDeltaThreads = 256;
+constexpr int kDeltaThreads = 256;                     // four waves; wave w has rows 16 w on of a chunk
 
 typedef float Acc __attribute__((ext_vector_type(4)));
+
+// Products run on the bf16 matrix pipe on sums of bf16 planes: a plane holds what the planes before it left, rounded to 8 bits, so that
+// three hold 24 and two 17 of a value's bits.  bf16 elements are one plane, fp16 two, fp32 three, all exactly.  States and what
+// leads to them or to a gradient in fp32 are kept in three; what ends in a 16-bit result alone in two, whose rounding, 2^-18, is 2^-6 of an
+// fp16 result's own.  Of the products of planes those are formed that are not below the smallest kept: six of three by three.  The fp32
+// matrix instructions would be 16 times slower, and fp16 planes, of which two would do, need every column scaled to their range.
+typedef __bf16 Frag __attribute__((ext_vector_type(8)));
+typedef __bf16 Four __attribute__((ext_vector_type(4)));
+template <typename E> constexpr int kExact = sizeof(E) == 4 ? 3 : std::is_same<E, _Float16>::value ? 2 : 1;
+template <typename E> constexpr int kFine = sizeof(E) == 4 ? 3 : 2;
 
 struct ChunkGates {
     double G[kSteps];
     float f[kSteps], t[kSteps], beta[kSteps];
     unsigned long long starts, live;                   // bit i: step i starts a sequence; is none of the padding
-    int bad;                                           // N or P hold an infinity or NaN
+    int bad;                                           // the rows of K or Q, N or P hold an infinity or NaN
     int pad[27];
 };
 static_assert(sizeof(ChunkGates) % 128 == 0, "records begin at lines");
@@ -49,12 +60,23 @@ struct DeltaArgs {
     void *grad_q, *grad_k, *grad_v;
     int64_t ld_gq, ld_gk, ld_gv;
     float *grad_log_decay, *grad_beta, *grad_s_first;
-    // workspace, one record per (b, value head, chunk)
-    ChunkGates *gates;
-    float *N, *P;                                      // [64,64]
+    // workspace.  Matrices in the order in which the matrix instructions take them: tiles of 16 rows by 32 columns, plane by plane, a lane's
+    // eight entries (row l % 16, columns l / 16 * 8 on) adjacent, so that a wave reads and writes 1 KB at a time.
+    Frag *K, *Q, *KT, *QT;                             // per (b, key head, chunk): rows, and transposed; QT null without keep
+    Frag *N, *P, *NT, *PT;                             // per (b, value head, chunk); NT and PT null without keep
+    ChunkGates *gates;                                 // per (b, value head, chunk), as all that follow
     float *S, *M;                                      // [Dk,Dv] before the chunk, [64,Dv]; null without keep
     float *D, *Y;                                      // [Dk,Dv] adjoint behind the chunk, [64,Dv]
 };
+
+// Fragments of one matrix: of the keys of a chunk (padded to DK), and of N and its kind.
+constexpr int key_frags(int DK, int planes) { return kSteps / 16 * (DK / 32) * planes * kWave; }
+constexpr int square_frags(int planes) { return kSteps / 16 * 2 * planes * kWave; }
+// The lane's fragment of tile (16 rows), step (32 columns) and plane.
+__device__ __forceinline__ int frag_at(int tile, int step, int plane, int steps, int planes)
+{
+    return ((tile * steps + step) * planes + plane) * kWave + (int)threadIdx.x % kWave;
+}
 
 __device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }      // NaN stays
 __device__ __forceinline__ float decay_of(double d) { return max_of(expf((float)d), 1.17549435e-38f); }
@@ -64,8 +86,77 @@ __device__ __forceinline__ int part_of(unsigned long long starts, int i) { retur
 __device__ __forceinline__ bool bit_of(unsigned long long bits, int i) { return bits >> i & 1; }
 // Whether step j hands anything to step i >= j.
 __device__ __forceinline__ bool joined(unsigned long long starts, int i, int j) { return part_of(starts, i) == part_of(starts, j); }
+// Steps of i's sequence up to and with i; from i on.
+__device__ __forceinline__ unsigned long long upto(unsigned long long starts, int i)
+{
+    const unsigned long long low = ~0ull >> (63 - i), before = starts & low;
+    return before ? low & ~0ull << (63 - __clzll((long long)before)) : low;
+}
+__device__ __forceinline__ unsigned long long from(unsigned long long starts, int i)
+{
+    const unsigned long long high = ~0ull << i, behind = starts & high & ~(1ull << i);
+    return behind ? high & (behind & -behind) - 1 : high;
+}
 
-// D = A B + C on 16 x 16 tiles in fp32: a(row, k), b(k, col) give one entry each; lane l holds rows l / 16 * 4 .. + 4 of column l % 16.
+// Planes of four values.
+template <int N>
+__device__ __forceinline__ void split(Acc v, Four (&out)[N])
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        out[n] = __builtin_convertvector(v, Four);
+        if (n + 1 < N) v -= __builtin_convertvector(out[n], Acc);
+    }
+}
+template <int N>
+__device__ __forceinline__ void split(const float *v, Frag (&out)[N])
+{
+    Four low[N], high[N];
+    split(Acc{v[0], v[1], v[2], v[3]}, low);
+    split(Acc{v[4], v[5], v[6], v[7]}, high);
+#pragma unroll
+    for (int n = 0; n < N; ++n) out[n] = __builtin_shufflevector(low[n], high[n], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// c + a b on a 16 x 32 by 32 x 16 tile, the smallest products first; ORDER: the largest sum of plane numbers that counts.  Lane l holds rows
+// l / 16 * 4 .. + 4 of column l % 16 of the result.
+template <int PA, int PB, int ORDER = (PA > PB ? PA : PB) - 1>
+__device__ __forceinline__ Acc multiply(const Frag (&a)[PA], const Frag (&b)[PB], Acc c)
+{
+#pragma unroll
+    for (int s = ORDER; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            if (s - i >= 0 && s - i < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[s - i], c, 0, 0, 0);
+    return c;
+}
+
+// The same over 64 columns k without the matrix pipe, for chunks that hold an infinity or NaN: only the k in pass[r] take part in the lane's
+// r-th row.  a: the matrix's fragments; b: the lane's column, planes `plane` apart.
+__device__ __noinline__ static Acc careful_multiply(Acc c, const Frag *a, int tile, int PA, const __bf16 *b, int PB, int plane, const unsigned long long *pass)
+{
+    const int group = threadIdx.x % kWave / 16;
+    for (int r = 0; r < 4; ++r) {
+        float v = c[r];
+        for (int k = 0; k < kSteps; ++k) {
+            if (!bit_of(pass[r], k)) continue;
+            float x = 0.0f, y = 0.0f;
+            for (int n = PA - 1; n >= 0; --n)
+                x += (float)reinterpret_cast<const __bf16 *>(a)[(((tile * 2 + k / 32) * PA + n) * kWave + group * 4 + r + k % 32 / 8 * 16) * 8 + k % 8];
+            for (int n = PB - 1; n >= 0; --n) y += (float)b[n * plane + k];
+            v = fmaf(x, y, v);
+        }
+        c[r] = v;
+    }
+    return c;
+}
+__device__ __forceinline__ bool all_finite(Acc a)
+{
+    const Acc z = a * 0.0f;
+    return (z[0] + z[1]) + (z[2] + z[3]) == 0.0f;
+}
+
+// D = A B + C on 16 x 16 tiles in fp32: a(row, k), b(k, col) give one entry each.
 template <class FA, class FB>
 __device__ __forceinline__ Acc product(int K, Acc c, FA &&a, FB &&b)
 {
@@ -73,7 +164,6 @@ __device__ __forceinline__ Acc product(int K, Acc c, FA &&a, FB &&b)
     for (int k = 0; k < K; k += 4) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a(at, k + group), b(k + group, at), c, 0, 0, 0);
     return c;
 }
-// The same without the matrix pipe, for chunks that hold an infinity or NaN: only entries of which pass(row, k) holds take part.
 template <class FA, class FB, class FP>
 __device__ __noinline__ Acc careful_product(int K, Acc c, FA &&a, FB &&b, FP &&pass)
 {
@@ -87,11 +177,6 @@ __device__ __noinline__ Acc careful_product(int K, Acc c, FA &&a, FB &&b, FP &&p
     }
     return c;
 }
-__device__ __forceinline__ bool all_finite(Acc a)
-{
-    const Acc z = a * 0.0f;
-    return (z[0] + z[1]) + (z[2] + z[3]) == 0.0f;
-}
 
 // Row of the elements of step t of sequence b and head h.
 template <typename E>
@@ -100,9 +185,53 @@ __device__ __forceinline__ const E *row_at(const void *base, int64_t ld, int64_t
     return static_cast<const E *>(base) + (b * T + t) * ld + (int64_t)h * D;
 }
 
+// NT adjacent columns of a row, 0 behind the last; and back.  16-byte alignment is not needed, nor any above the element's.
+template <typename E, int NT>
+__device__ __forceinline__ void read_columns(const E *row, int col, int D, float (&to)[NT])
+{
+    typedef E Vec __attribute__((ext_vector_type(NT)));
+    typedef Vec Loose __attribute__((aligned(sizeof(E))));
+    if (col + NT <= D) {
+        const Vec v = *reinterpret_cast<const Loose *>(row + col);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) to[n] = to_f32(v[n]);
+    } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) to[n] = col + n < D ? to_f32(row[col + n]) : 0.0f;
+    }
+}
+template <typename E, int NT>
+__device__ __forceinline__ void write_columns(E *row, int col, int D, const float (&from)[NT])
+{
+    typedef E Vec __attribute__((ext_vector_type(NT)));
+    typedef Vec Loose __attribute__((aligned(sizeof(E))));
+    if (col + NT <= D) {
+        Vec v;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) v[n] = from_f32<E>(from[n]);
+        *reinterpret_cast<Loose *>(row + col) = v;
+    } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            if (col + n < D) row[col + n] = from_f32<E>(from[n]);
+    }
+}
+
+// The head and the first column of a workgroup on its way through the chunks.  Workgroups go to the eight dies in turn: those of a head, which
+// read the same fragments, are given to one die.  head = -1: nothing to do.
+struct Place { int64_t head; int first; };
+__device__ __forceinline__ Place place_of(int64_t heads, int Dv, int columns)
+{
+    const int blocks = (Dv + columns - 1) / columns;
+    const int64_t all = heads * blocks, each = (all + 7) / 8, at = (int64_t)(blockIdx.x % 8) * each + blockIdx.x / 8;
+    return at < all && blockIdx.x / 8 < each ? Place{at / blocks, (int)(at % blocks) * columns} : Place{-1, 0};
+}
+inline unsigned places(int64_t heads, int Dv, int columns) { return (unsigned)((heads * ((Dv + columns - 1) / columns) + 7) / 8 * 8); }
+
 int delta_scan_launch(int dtype, const DeltaArgs &p, hipStream_t stream);
 int delta_grad_launch(int dtype, const DeltaArgs &p, hipStream_t stream);
 
+constexpr int padded_keys(int Dk) { return Dk <= 32 ? 32 : Dk <= 64 ? 64 : 128; }
 // Calls f with the padded key size as a constant.
 template <typename F>
 inline int with_keys(int Dk, F &&f)

@@ -9,128 +9,273 @@
 namespace marl {
 namespace {
 
-// The chunks of one head from the last to the first, for kCols value columns: D, Y and the gradient of v.  Wave w has rows 16 w
-// on of the chunk, and rows w DK / 4 on of the adjoint, which stays in its accumulators.
-template <typename E, int DK>
-__global__ __launch_bounds__(kDeltaThreads) void back_kernel(DeltaArgs p)
+// The chunks of one head from the last to the first, for 16 NT value columns as in the forward pass: D, Y and the gradient of v.  Wave w has
+// rows 16 w on of the chunk, and rows w DK / 4 on of the adjoint, which stays in its accumulators.
+template <typename E, int DK, int NT>
+__global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2 : 1) void back_kernel(DeltaArgs p)
 {
-    constexpr int LD = DK + 1, LS = DK + 1, LU = kSteps + 1;
+    constexpr int PE = kExact<E>, KS = DK / 32, LS = DK + 8, LU = kSteps + 8, C = 16 * NT;
     constexpr int kTiles = (DK + 63) / 64;
-    extern __shared__ __attribute__((aligned(16))) float lds[];
-    float *K = lds, *Q = K + kSteps * LD, *S = Q + kSteps * LD, *O = S + kCols * LS, *R = O + kCols * LU, *V = R + kCols * LU;
-    __shared__ ChunkGates gates;
-    __shared__ int not_finite[2];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    typedef __bf16 StatePlane[C][LS];
+    typedef __bf16 StepPlane[C][LU];
+    StatePlane *S = reinterpret_cast<StatePlane *>(lds);                           // [3], columns of the adjoint
+    // the upstream gradient of this chunk and of the next: [PE] as it is, [3] scaled by what of it reaches the state before
+    StepPlane *upstream = reinterpret_cast<StepPlane *>(lds + 3 * sizeof(StatePlane)), *R = upstream + 2 * (PE + 3), *V = R + 3;      // [3], [3]
+    __shared__ int not_finite[4];                      // upstream of even and odd chunks, beta dU, dV
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, at = lane % 16, group = lane / 16;
-    const int blocks = (p.Dv + kCols - 1) / kCols;
-    const int64_t head = blockIdx.x / blocks;
-    const int first = (int)(blockIdx.x % blocks) * kCols, col = first + at;
-    const int h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk);
-    const int64_t b = head / p.Hv;
-    const bool in = col < p.Dv;
-    Acc adj[kTiles];
-    auto key_row = [&](int tile, int r) { return (wave * kTiles + tile) * 16 + group * 4 + r; };
+    const Place place = place_of((int64_t)p.B * p.Hv, p.Dv, C);
+    if (place.head < 0) return;                        // the whole workgroup
+    const int64_t head = place.head, b = head / p.Hv;
+    const int col = place.first + at * NT, h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk);
+    const int64_t key_head = b * p.Hk + hk;
+    const bool has_state = wave * kTiles * 16 < DK;
+    Acc adj[kTiles][NT] = {};
+    if (p.grad_s_last && has_state)
 #pragma unroll
-    for (int tile = 0; tile < kTiles; ++tile)
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (wave * kTiles + tile) * 16 + group * 4 + r;
+                float v[NT] = {};
+                if (d < p.Dk) read_columns<float, NT>(p.grad_s_last + (head * p.Dk + d) * p.Dv, col, p.Dv, v);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) adj[tile][n][r] = v[n];
+            }
+    Frag k[KS][PE];
+    float go[4][NT];
+    Acc f_next, t_next, beta_next;
+    auto load_start = [&](int chunk) {
+        const Frag *K = p.K + (key_head * p.chunks + chunk) * key_frags(DK, PE);
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int n = 0; n < PE; ++n) k[s][n] = K[frag_at(wave, s, n, KS, PE)];
+        const ChunkGates &g = p.gates[head * p.chunks + chunk];
+        f_next = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
+        t_next = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
+        beta_next = *reinterpret_cast<const Acc *>(g.beta + wave * 16 + group * 4);
+#pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = key_row(tile, r);
-            adj[tile][r] = p.grad_s_last && in && d < p.Dk ? p.grad_s_last[(head * p.Dk + d) * p.Dv + col] : 0.0f;
+            const int t = chunk * kSteps + wave * 16 + group * 4 + r;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) go[r][n] = 0.0f;
+            if (t < p.T) read_columns<E, NT>(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), col, p.Dv, go[r]);
         }
+    };
+    auto adjoint_out = [&](float *to) {                // [Dk,Dv]
+#pragma unroll
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (wave * kTiles + tile) * 16 + group * 4 + r;
+                float v[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) v[n] = adj[tile][n][r];
+                if (d < p.Dk) write_columns<float, NT>(to + (int64_t)d * p.Dv, col, p.Dv, v);
+            }
+    };
+    auto share_adjoint = [&] {
+#pragma unroll
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                Four planes[3];
+                split(adj[tile][n], planes);
+#pragma unroll
+                for (int m = 0; m < 3; ++m) *reinterpret_cast<Four *>(&S[m][n * 16 + at][(wave * kTiles + tile) * 16 + group * 4]) = planes[m];
+            }
+    };
+    auto share_steps = [&](StepPlane *to, auto &planes, int n) {
+        constexpr int PLANES = sizeof(planes) / sizeof(Four);
+#pragma unroll
+        for (int m = 0; m < PLANES; ++m) *reinterpret_cast<Four *>(&to[m][n * 16 + at][wave * 16 + group * 4]) = planes[m];
+    };
+    auto share_upstream = [&](int chunk) {
+        const unsigned long long live = p.gates[head * p.chunks + chunk].live;
+        StepPlane *O = upstream + chunk % 2 * (PE + 3), *Of = O + PE;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            Acc o, of;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                o[r] = bit_of(live, wave * 16 + group * 4 + r) ? go[r][n] : 0.0f;
+                of[r] = f_next[r] == 0.0f ? 0.0f : p.scale * f_next[r] * o[r];
+            }
+            Four exact[PE], planes[3];
+            split(o, exact);
+            split(of, planes);
+            share_steps(O, exact, n);
+            share_steps(Of, planes, n);
+            if (!all_finite(o)) not_finite[chunk % 2] = 1;
+        }
+    };
+    if (threadIdx.x < 4) not_finite[threadIdx.x] = 0;
+    __syncthreads();
+    if (p.chunks > 0) {
+        load_start(p.chunks - 1);
+        share_upstream(p.chunks - 1);
+    }
+    if (has_state) share_adjoint();
+    __syncthreads();
     for (int chunk = p.chunks - 1; chunk >= 0; --chunk) {
         const int64_t record = head * p.chunks + chunk;
-        __syncthreads();
-        {
-            const int *from = reinterpret_cast<const int *>(p.gates + record);
-            int *to = reinterpret_cast<int *>(&gates);
-            for (int e = threadIdx.x; e < (int)(sizeof(ChunkGates) / 4); e += kDeltaThreads) to[e] = from[e];
-        }
-        if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
+        const ChunkGates &g = p.gates[record];
+        const unsigned long long starts = g.starts, live = g.live;
+        const float whole = g.f[kSteps - 1];
+        const bool bad = g.bad != 0, careful_o = bad || not_finite[chunk % 2];
+        const StepPlane *O = upstream + chunk % 2 * (PE + 3), *Of = O + PE;
+        // flags are taken back where all have read them and none sets them before the next barrier
+        if (threadIdx.x == 0) not_finite[(chunk + 1) % 2] = not_finite[3] = 0;
+        if (has_state) adjoint_out(p.D + record * p.Dk * p.Dv);
+        Frag nn[2][3], pp[2][3], kt[kTiles][2][PE], qt[kTiles][2][PE];
+        const Frag *N = p.NT + record * square_frags(3), *P = p.PT + record * square_frags(3);
+        const Frag *KT = p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE), *QT = p.QT + (key_head * p.chunks + chunk) * key_frags(DK, PE);
 #pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile)
-            for (int r = 0; r < 4; ++r) {
-                const int d = key_row(tile, r);
-                if (d < DK) S[at * LS + d] = adj[tile][r];
-                if (in && d < p.Dk) p.D[(record * p.Dk + d) * p.Dv + col] = adj[tile][r];
+        for (int s = 0; s < 2; ++s) {
+            if (s * 32 + 31 < wave * 16) continue;     // zeros
+#pragma unroll
+            for (int n = 0; n < 3; ++n) {
+                pp[s][n] = P[frag_at(wave, s, n, 2, 3)];
+                nn[s][n] = N[frag_at(wave, s, n, 2, 3)];
             }
-        __syncthreads();
-        const unsigned long long starts = gates.starts, alive = gates.live;
-        for (int e = threadIdx.x; e < kSteps * DK; e += kDeltaThreads) {
-            const int i = e / DK, d = e % DK;
-            const bool is = bit_of(alive, i) && d < p.Dk;
-            K[i * LD + d] = is ? to_f32(row_at<E>(p.k, p.ld_k, b, p.T, chunk * kSteps + i, hk, p.Dk)[d]) : 0.0f;
-            Q[i * LD + d] = is ? to_f32(row_at<E>(p.q, p.ld_q, b, p.T, chunk * kSteps + i, hk, p.Dk)[d]) : 0.0f;
         }
-        Acc go, scaled, y;
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r;
-            go[r] = bit_of(alive, i) && in ? to_f32(row_at<E>(p.grad_o, p.ld_go, b, p.T, chunk * kSteps + i, h, p.Dv)[col]) : 0.0f;
-            O[at * LU + i] = go[r];
-        }
-        if (!all_finite(go)) not_finite[0] = 1;
-        __syncthreads();
         // dU = P' dO + t K D
-        Acc kd = {};
-        kd = product(DK, kd, [&](int row, int k) { return K[(wave * 16 + row) * LD + k]; }, [&](int k, int c) { return S[c * LS + k]; });
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r;
-            const float t = gates.t[i];
-            y[r] = t == 0.0f || !bit_of(alive, i) ? 0.0f : t * kd[r];
+        const Acc f = f_next, t = t_next, beta = beta_next;
+        Acc y[NT] = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                Frag of_state[3];
+#pragma unroll
+                for (int m = 0; m < 3; ++m) of_state[m] = *reinterpret_cast<const Frag *>(&S[m][n * 16 + at][s * 32 + group * 8]);
+                y[n] = multiply<PE, 3>(k[s], of_state, y[n]);
+            }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[n][r] = t[r] == 0.0f || !bit_of(live, wave * 16 + group * 4 + r) ? 0.0f : t[r] * y[n][r];
+            if (careful_o) {
+                unsigned long long pass[4];
+                for (int r = 0; r < 4; ++r) {
+                    const int i = wave * 16 + group * 4 + r;
+                    pass[r] = bit_of(live, i) ? from(starts, i) & live : 0;
+                }
+                y[n] = careful_multiply(y[n], P, wave, 3, O[0][n * 16 + at], PE, C * LU, pass);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if (s * 32 + 31 < wave * 16) continue;
+                    Frag of_o[PE];
+#pragma unroll
+                    for (int x = 0; x < PE; ++x) of_o[x] = *reinterpret_cast<const Frag *>(&O[x][n * 16 + at][s * 32 + group * 8]);
+                    y[n] = multiply<3, PE>(pp[s], of_o, y[n]);
+                }
+            }
+            const Acc minus = -(beta * y[n]);
+            Four planes[3];
+            split(minus, planes);
+            share_steps(R, planes, n);
+            if (!all_finite(minus)) not_finite[2] = 1;
         }
-        const float *P = p.P + record * kSteps * kSteps + wave * 16, *N = p.N + record * kSteps * kSteps + wave * 16;
-        auto of_p = [&](int row, int k) { return P[k * kSteps + row]; };
-        auto of_o = [&](int k, int c) { return O[c * LU + k]; };
-        if (gates.bad || not_finite[0])
-            y = careful_product(kSteps, y, of_p, of_o, [&](int row, int k) {
-                const int i = wave * 16 + row;
-                return k >= i && bit_of(alive, i) && bit_of(alive, k) && joined(starts, k, i);
-            });
-        else y = product(kSteps - wave * 16, y, [&](int row, int k) { return of_p(row, wave * 16 + k); }, [&](int k, int c) { return of_o(wave * 16 + k, c); });
-        // Y = dU - N' (beta dU)
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r;
-            scaled[r] = bit_of(alive, i) ? gates.beta[i] * y[r] : 0.0f;
-            R[at * LU + i] = scaled[r];
-        }
-        if (!all_finite(scaled)) not_finite[1] = 1;
         __syncthreads();
-        auto of_n = [&](int row, int k) { return -N[k * kSteps + row]; };
-        auto of_r = [&](int k, int c) { return R[c * LU + k]; };
-        if (gates.bad || not_finite[1])
-            y = careful_product(kSteps, y, of_n, of_r, [&](int row, int k) {
-                const int i = wave * 16 + row;
-                return k > i && bit_of(alive, i) && bit_of(alive, k) && joined(starts, k, i);
-            });
-        else y = product(kSteps - wave * 16, y, [&](int row, int k) { return of_n(row, wave * 16 + k); }, [&](int k, int c) { return of_r(wave * 16 + k, c); });
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r, t = chunk * kSteps + i;
-            const float v = bit_of(alive, i) ? gates.beta[i] * y[r] : 0.0f;
-            const float f = gates.f[i];
-            V[at * LU + i] = f == 0.0f ? 0.0f : -f * v;
-            O[at * LU + i] = f == 0.0f ? 0.0f : p.scale * f * go[r];       // the wave's own rows, which others read before the barrier above
-            if (in) p.Y[(record * kSteps + i) * p.Dv + col] = bit_of(alive, i) ? y[r] : 0.0f;
-            if (t < p.T && in) const_cast<E *>(row_at<E>(p.grad_v, p.ld_gv, b, p.T, t, h, p.Dv))[col] = from_f32<E>(v);
+        // Y = dU - N' (beta dU), dV = beta Y
+        if (has_state)
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int n = 0; n < PE; ++n) {
+                        kt[tile][s][n] = KT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
+                        qt[tile][s][n] = QT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
+                    }
+        const bool careful_n = bad || not_finite[2];
+        Acc v[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (careful_n) {
+                unsigned long long pass[4];
+                for (int r = 0; r < 4; ++r) {
+                    const int i = wave * 16 + group * 4 + r;
+                    pass[r] = bit_of(live, i) ? from(starts, i) & live & ~(1ull << i) : 0;
+                }
+                y[n] = careful_multiply(y[n], N, wave, 3, R[0][n * 16 + at], 3, C * LU, pass);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if (s * 32 + 31 < wave * 16) continue;
+                    Frag of_r[3];
+#pragma unroll
+                    for (int x = 0; x < 3; ++x) of_r[x] = *reinterpret_cast<const Frag *>(&R[x][n * 16 + at][s * 32 + group * 8]);
+                    y[n] = multiply<3, 3>(nn[s], of_r, y[n]);
+                }
+            }
+            Acc back;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (!bit_of(live, wave * 16 + group * 4 + r)) y[n][r] = 0.0f;
+                v[n][r] = beta[r] * y[n][r];
+                back[r] = f[r] == 0.0f ? 0.0f : -f[r] * v[n][r];
+            }
+            Four planes[3];
+            split(back, planes);
+            share_steps(V, planes, n);
+            if (!all_finite(v[n])) not_finite[3] = 1;
         }
+        if (chunk > 0) load_start(chunk - 1);
         __syncthreads();
         // D <- f_63 D + (scale f Q)' dO - (f K)' dV
-        const float whole = gates.f[kSteps - 1];
+        if (has_state) {
 #pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile) {
-            for (int r = 0; r < 4; ++r) adj[tile][r] = whole == 0.0f ? 0.0f : whole * adj[tile][r];
-            const int d0 = (wave * kTiles + tile) * 16;
-            if (d0 < DK) {
-                adj[tile] = product(kSteps, adj[tile], [&](int row, int k) { return gates.f[k] == 0.0f ? 0.0f : Q[k * LD + d0 + row]; },
-                                    [&](int k, int c) { return O[c * LU + k]; });
-                adj[tile] = product(kSteps, adj[tile], [&](int row, int k) { return gates.f[k] == 0.0f ? 0.0f : K[k * LD + d0 + row]; },
-                                    [&](int k, int c) { return V[c * LU + k]; });
+            for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) adj[tile][n][r] = whole == 0.0f ? 0.0f : whole * adj[tile][n][r];
+            if (careful_o || not_finite[3]) {
+                unsigned long long pass[4];
+                for (int r = 0; r < 4; ++r) pass[r] = (starts ? (starts & -starts) - 1 : ~0ull) & live;
+                for (int tile = 0; tile < kTiles; ++tile)
+                    for (int n = 0; n < NT; ++n) {
+                        adj[tile][n] = careful_multiply(adj[tile][n], QT, wave * kTiles + tile, PE, Of[0][n * 16 + at], 3, C * LU, pass);
+                        adj[tile][n] = careful_multiply(adj[tile][n], KT, wave * kTiles + tile, PE, V[0][n * 16 + at], 3, C * LU, pass);
+                    }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        Frag of_o[3], of_v[3];
+#pragma unroll
+                        for (int x = 0; x < 3; ++x) {
+                            of_o[x] = *reinterpret_cast<const Frag *>(&Of[x][n * 16 + at][s * 32 + group * 8]);
+                            of_v[x] = *reinterpret_cast<const Frag *>(&V[x][n * 16 + at][s * 32 + group * 8]);
+                        }
+#pragma unroll
+                        for (int tile = 0; tile < kTiles; ++tile) {
+                            adj[tile][n] = multiply<PE, 3>(qt[tile][s], of_o, adj[tile][n]);
+                            adj[tile][n] = multiply<PE, 3>(kt[tile][s], of_v, adj[tile][n]);
+                        }
+                    }
             }
+            share_adjoint();
         }
-    }
-    if (p.grad_s_first)
 #pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile)
-            for (int r = 0; r < 4; ++r) {
-                const int d = key_row(tile, r);
-                if (in && d < p.Dk) p.grad_s_first[(head * p.Dk + d) * p.Dv + col] = adj[tile][r];
-            }
+        for (int r = 0; r < 4; ++r) {
+            const int i = wave * 16 + group * 4 + r, step = chunk * kSteps + i;
+            float x[NT], z[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x[n] = y[n][r], z[n] = bit_of(live, i) ? v[n][r] : 0.0f;
+            write_columns<float, NT>(p.Y + (record * kSteps + i) * p.Dv, col, p.Dv, x);
+            if (step < p.T) write_columns<E, NT>(const_cast<E *>(row_at<E>(p.grad_v, p.ld_gv, b, p.T, step, h, p.Dv)), col, p.Dv, z);
+        }
+        if (chunk > 0) share_upstream(chunk - 1);
+        if (threadIdx.x == 0) not_finite[2] = 0;
+        __syncthreads();
+    }
+    if (p.grad_s_first && has_state) adjoint_out(p.grad_s_first + head * p.Dk * p.Dv);
 }
 
 // Sum over the 16 lanes that hold a row.
@@ -149,8 +294,8 @@ template <typename E, int DK>
 __global__ __launch_bounds__(kDeltaThreads) void chunk_grad_kernel(DeltaArgs p)
 {
     constexpr int LD = DK + 1, LN = kSteps + 1, kTiles = DK / 16;
-    extern __shared__ __attribute__((aligned(16))) float lds[];
-    float *K = lds, *Q = K + kSteps * LD, *dN = Q + kSteps * LD, *dM = dN + kSteps * LN;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    float *K = reinterpret_cast<float *>(lds), *Q = K + kSteps * LD, *dN = Q + kSteps * LD, *dM = dN + kSteps * LN;
     __shared__ ChunkGates gates;
     __shared__ int not_finite;
     __shared__ float dG[kSteps], extra[kDeltaThreads / kWave], dbeta[kSteps];
@@ -312,18 +457,23 @@ __global__ __launch_bounds__(kDeltaThreads) void chunk_grad_kernel(DeltaArgs p)
         }
 }
 
+template <typename E, int DK, int NT>
+int run_back(const DeltaArgs &p, hipStream_t stream)
+{
+    const size_t lds = (size_t)16 * NT * (3 * (DK + 8) + (12 + 2 * kExact<E>) * (kSteps + 8)) * sizeof(__bf16);
+    if (const int rc = make_room_for(reinterpret_cast<const void *>(back_kernel<E, DK, NT>), lds)) return rc;
+    hipLaunchKernelGGL((back_kernel<E, DK, NT>), dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
+    return launched("delta scan gradient");
+}
+
 template <typename E, int DK>
 int run(const DeltaArgs &p, hipStream_t stream)
 {
-    size_t lds = (size_t)(2 * kSteps * (DK + 1) + kCols * (DK + 1) + 3 * kCols * (kSteps + 1)) * sizeof(float);
-    if (const int rc = make_room_for(reinterpret_cast<const void *>(back_kernel<E, DK>), lds)) return rc;
-    const int blocks = (p.Dv + kCols - 1) / kCols;
-    hipLaunchKernelGGL((back_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hv * blocks)), dim3(kDeltaThreads), lds, stream, p);
-    if (p.chunks > 0) {
-        lds = (size_t)(2 * kSteps * (DK + 1) + 2 * kSteps * (kSteps + 1)) * sizeof(float);
-        if (const int rc = make_room_for(reinterpret_cast<const void *>(chunk_grad_kernel<E, DK>), lds)) return rc;
-        hipLaunchKernelGGL((chunk_grad_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
-    }
+    const int rc = (int64_t)p.B * p.Hv * ((p.Dv + 31) / 32) >= 256 ? run_back<E, DK, 2>(p, stream) : run_back<E, DK, 1>(p, stream);
+    if (rc || p.chunks == 0) return rc;
+    const size_t lds = (size_t)(2 * kSteps * (DK + 1) + 2 * kSteps * (kSteps + 1)) * sizeof(float);
+    if (const int failed = make_room_for(reinterpret_cast<const void *>(chunk_grad_kernel<E, DK>), lds)) return failed;
+    hipLaunchKernelGGL((chunk_grad_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
     return launched("delta scan gradient");
 }
 

@@ -98,17 +98,26 @@ __global__ __launch_bounds__(kDeltaThreads) void step_kernel(StepArgs p)
 
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-struct Room { size_t gates, N, P, S, M, D, Y, all; };
-Room room_of(const DeltaArgs &p, bool keep)
+struct Room { size_t gates, K, Q, KT, QT, N, P, NT, PT, S, M, D, Y, all; };
+int planes_of(int dtype) { return dtype == MARL_DTYPE_F32 ? 3 : dtype == MARL_DTYPE_F16 ? 2 : 1; }
+Room room_of(int dtype, const DeltaArgs &p, bool keep)
 {
     const size_t records = (size_t)p.B * p.Hv * p.chunks, f = sizeof(float);
+    const size_t keys = (size_t)p.B * p.Hk * p.chunks * key_frags(padded_keys(p.Dk), planes_of(dtype)) * sizeof(Frag);
+    const size_t fine = records * square_frags(dtype == MARL_DTYPE_F32 ? 3 : 2) * sizeof(Frag), square = records * square_frags(3) * sizeof(Frag);
     Room r{};
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t here = at; at += up256(bytes); return here; };
     r.gates = take(records * sizeof(ChunkGates));
-    r.N = take(records * kSteps * kSteps * f);
-    r.P = take(records * kSteps * kSteps * f);
+    r.K = take(keys);
+    r.Q = take(keys);
+    r.KT = take(keys);
+    r.N = take(square);
+    r.P = take(fine);
     if (keep) {
+        r.QT = take(keys);
+        r.NT = take(square);
+        r.PT = take(square);
         r.S = take(records * p.Dk * p.Dv * f);
         r.M = take(records * kSteps * p.Dv * f);
         r.D = take(records * p.Dk * p.Dv * f);
@@ -117,17 +126,16 @@ Room room_of(const DeltaArgs &p, bool keep)
     r.all = at;
     return r;
 }
-void place(DeltaArgs &p, char *workspace, bool keep)
+void place(int dtype, DeltaArgs &p, char *workspace, bool keep)
 {
-    const Room r = room_of(p, keep);
+    const Room r = room_of(dtype, p, keep);
+    const auto frags = [&](size_t at) { return reinterpret_cast<Frag *>(workspace + at); };
+    const auto floats = [&](size_t at) { return reinterpret_cast<float *>(workspace + at); };
     p.gates = reinterpret_cast<ChunkGates *>(workspace + r.gates);
-    p.N = reinterpret_cast<float *>(workspace + r.N);
-    p.P = reinterpret_cast<float *>(workspace + r.P);
+    p.K = frags(r.K); p.Q = frags(r.Q); p.KT = frags(r.KT); p.N = frags(r.N); p.P = frags(r.P);
     if (!keep) return;
-    p.S = reinterpret_cast<float *>(workspace + r.S);
-    p.M = reinterpret_cast<float *>(workspace + r.M);
-    p.D = reinterpret_cast<float *>(workspace + r.D);
-    p.Y = reinterpret_cast<float *>(workspace + r.Y);
+    p.QT = frags(r.QT); p.NT = frags(r.NT); p.PT = frags(r.PT);
+    p.S = floats(r.S); p.M = floats(r.M); p.D = floats(r.D); p.Y = floats(r.Y);
 }
 
 constexpr int64_t kMostRow = (int64_t)1 << 31;
@@ -143,7 +151,7 @@ int sizes_check(int dtype, int B, int T, int Hk, int Hv, int Dk, int Dv)
     if (const int rc = heads_check(dtype, Hk, Hv, Dk, Dv)) return rc;
     if (B < 0 || T < 0 || (int64_t)B * Hv >= (1 << 24) || (int64_t)B * T >= (1 << 30)) return MARL_ERR_BAD_DIM;
     // grids: a workgroup per record, and one per head and sixteen columns
-    if ((int64_t)B * Hv * ((T + kSteps - 1) / kSteps) >= kMostRow || (int64_t)B * Hv * ((Dv + kCols - 1) / kCols) >= kMostRow) return MARL_ERR_BAD_DIM;
+    if ((int64_t)B * Hv * ((T + kSteps - 1) / kSteps) >= kMostRow || (int64_t)B * Hv * ((Dv + 15) / 16) >= kMostRow) return MARL_ERR_BAD_DIM;
     return MARL_OK;
 }
 bool row_fits(int64_t ld, int H, int D) { return ld >= (int64_t)H * D && ld < kMostRow; }
@@ -171,7 +179,7 @@ int marl_delta_scan_workspace_bytes(int32_t dtype, int32_t B, int32_t T, int32_t
 {
     if (!bytes) return MARL_ERR_NULL;
     if (const int rc = sizes_check(dtype, B, T, Hk, Hv, Dk, Dv)) return rc;
-    *bytes = room_of(args_of(B, T, Hk, Hv, Dk, Dv, nullptr, 0, nullptr, 0, nullptr, 0, nullptr, nullptr, 0, nullptr, nullptr), keep != 0).all;
+    *bytes = room_of(dtype, args_of(B, T, Hk, Hv, Dk, Dv, nullptr, 0, nullptr, 0, nullptr, 0, nullptr, nullptr, 0, nullptr, nullptr), keep != 0).all;
     return MARL_OK;
 }
 
@@ -184,7 +192,7 @@ int marl_delta_scan(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_t Hv,
     if (!std::isfinite(scale)) return MARL_ERR_BAD_ARG;
     if (B == 0) return MARL_OK;
     DeltaArgs p = args_of(B, T, Hk, Hv, Dk, Dv, q, ld_q, k, ld_k, v, ld_v, log_decay, beta, scale, reset, filled);
-    const size_t need = room_of(p, keep != 0).all;
+    const size_t need = room_of(dtype, p, keep != 0).all;
     if (T > 0) {
         if (!q || !k || !v || !log_decay || !beta || !o) return MARL_ERR_NULL;
         if (!row_fits(ld_q, Hk, Dk) || !row_fits(ld_k, Hk, Dk) || !row_fits(ld_v, Hv, Dv) || !row_fits(ld_o, Hv, Dv)) return MARL_ERR_BAD_DIM;
@@ -194,7 +202,7 @@ int marl_delta_scan(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_t Hv,
         if (!aligned_to(workspace, 256)) return MARL_ERR_BAD_ARG;
     }
     p.s_first = s_first; p.o = o; p.ld_o = ld_o; p.s_last = s_last;
-    place(p, static_cast<char *>(workspace), keep != 0);
+    place(dtype, p, static_cast<char *>(workspace), keep != 0);
     return delta_scan_launch(dtype, p, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -217,14 +225,14 @@ int marl_delta_scan_grad(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_
             for (const void *in : {q, k, v, grad_o})
                 if (out == in) return MARL_ERR_BAD_ARG;
         if (grad_q == grad_k || grad_q == grad_v || grad_k == grad_v) return MARL_ERR_BAD_ARG;
-        if (workspace_bytes < room_of(p, true).all) return MARL_ERR_BAD_DIM;
+        if (workspace_bytes < room_of(dtype, p, true).all) return MARL_ERR_BAD_DIM;
         if (!workspace) return MARL_ERR_NULL;
         if (!aligned_to(workspace, 256)) return MARL_ERR_BAD_ARG;
     }
     p.grad_o = grad_o; p.ld_go = ld_go; p.grad_s_last = grad_s_last;
     p.grad_q = grad_q; p.grad_k = grad_k; p.grad_v = grad_v; p.ld_gq = ld_gq; p.ld_gk = ld_gk; p.ld_gv = ld_gv;
     p.grad_log_decay = grad_log_decay; p.grad_beta = grad_beta; p.grad_s_first = grad_s_first;
-    place(p, static_cast<char *>(workspace), true);
+    place(dtype, p, static_cast<char *>(workspace), true);
     return delta_grad_launch(dtype, p, static_cast<hipStream_t>(hip_stream));
 }
 

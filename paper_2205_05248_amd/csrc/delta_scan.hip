@@ -2,7 +2,6 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <type_traits>
 
 #include "delta.h"
 
@@ -10,7 +9,7 @@ namespace marl {
 namespace {
 
 // Gates of a chunk, by one wave, a step a lane.
-__device__ __forceinline__ void gates_of(const DeltaArgs &p, int64_t b, int h, int chunk, ChunkGates &out)
+__device__ __forceinline__ void gates_of(const DeltaArgs &p, int64_t b, int h, int chunk, int bad, ChunkGates &out)
 {
     const int i = threadIdx.x % kWave, t = chunk * kSteps + i;
     const int64_t step = b * p.T + t;
@@ -19,262 +18,515 @@ __device__ __forceinline__ void gates_of(const DeltaArgs &p, int64_t b, int h, i
     const bool start = live && ((p.reset && p.reset[step]) || g == -__builtin_inff());
     g = start ? 0.0f : g < -200.0f ? -200.0f : g;
     const unsigned long long starts = __ballot(start);
-    const unsigned long long upto = starts << (63 - i);
-    const int first = upto ? i - __clzll((long long)upto) : 0;                     // of the lane's sequence
+    const unsigned long long so_far = starts << (63 - i);
+    const int first = so_far ? i - __clzll((long long)so_far) : 0;                 // of the lane's sequence
     double G = g;
     for (int d = 1; d < kWave; d *= 2) {
         const double before = __shfl_up(G, d);
         if (i - d >= first) G += before;
     }
-    const int part = __popcll(upto);
+    const int part = __popcll(so_far);
     const double G_end = __shfl(G, 63);
     const int part_end = __shfl(part, 63);
     out.G[i] = G;
     out.f[i] = part == 0 ? decay_of(G) : 0.0f;
     out.t[i] = part == part_end ? decay_of(G_end - G) : 0.0f;
     out.beta[i] = live ? p.beta[step * p.Hv + h] : 0.0f;
-    if (i == 0) out.starts = starts;
     const unsigned long long alive = __ballot(live);
-    if (i == 0) { out.live = alive; out.bad = 0; }
+    if (i == 0) { out.starts = starts; out.live = alive; out.bad = bad; }
 }
 
-// N and P of a chunk.  One workgroup; wave w has rows 16 w on.
+// Rows of a chunk as planes in shared memory, zeros in padding and behind Dk.
+template <typename E, int DK>
+struct KeyRows {
+    static constexpr int PE = kExact<E>, LD = DK + 8;
+    __bf16 at[PE][kSteps][LD];
+    // returns whether all of the lane's entries are finite
+    __device__ __forceinline__ bool fill(const DeltaArgs &p, const void *from, int64_t ld, int64_t b, int hk, int chunk, unsigned long long live)
+    {
+        typedef E Vec __attribute__((ext_vector_type(8)));
+        typedef Vec Loose __attribute__((aligned(sizeof(E))));
+        bool fine = true;
+        for (int e = threadIdx.x; e < kSteps * (DK / 8); e += kDeltaThreads) {
+            const int i = e / (DK / 8), d = e % (DK / 8) * 8;
+            float v[8] = {};
+            if (bit_of(live, i)) {
+                const E *row = row_at<E>(from, ld, b, p.T, chunk * kSteps + i, hk, p.Dk);
+                if (d + 8 <= p.Dk) {
+                    const Vec x = *reinterpret_cast<const Loose *>(row + d);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) v[c] = to_f32(x[c]);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) v[c] = d + c < p.Dk ? to_f32(row[d + c]) : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < 8; ++c) fine = fine && v[c] * 0.0f == 0.0f;
+            Frag planes[PE];
+            split(v, planes);
+#pragma unroll
+            for (int n = 0; n < PE; ++n) *reinterpret_cast<Frag *>(&at[n][i][d]) = planes[n];
+        }
+        return fine;
+    }
+    __device__ __forceinline__ void row_frag(int tile, int step, Frag (&to)[PE]) const
+    {
+        const int lane = threadIdx.x % kWave;
+#pragma unroll
+        for (int n = 0; n < PE; ++n) to[n] = *reinterpret_cast<const Frag *>(&at[n][tile * 16 + lane % 16][step * 32 + lane / 16 * 8]);
+    }
+    // wave w writes its rows, and every fourth tile of the transposed matrix
+    __device__ __forceinline__ void write(Frag *rows, Frag *turned) const
+    {
+        const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+#pragma unroll
+        for (int s = 0; s < DK / 32; ++s) {
+            Frag f[PE];
+            row_frag(wave, s, f);
+#pragma unroll
+            for (int n = 0; n < PE; ++n) rows[frag_at(wave, s, n, DK / 32, PE)] = f[n];
+        }
+        if (!turned) return;
+        for (int tile = wave; tile < DK / 16; tile += 4)
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int n = 0; n < PE; ++n) {
+                    Frag f;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) f[c] = at[n][s * 32 + lane / 16 * 8 + c][tile * 16 + lane % 16];
+                    turned[frag_at(tile, s, n, 2, PE)] = f;
+                }
+    }
+};
+
+// A 64 x 64 matrix in shared memory as fragments: a wave's rows, or the rows of its transpose; `steps`: which 32 columns hold anything.
+template <int PLANES, bool TURNED>
+__device__ __forceinline__ void write_square(const float *from, int ld, Frag *to)
+{
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, row = wave * 16 + lane % 16;
+    for (int s = 0; s < 2; ++s) {
+        if (TURNED ? s * 32 + 31 < wave * 16 : s * 32 > wave * 16 + 15) continue;  // on the other side of the diagonal
+        float v[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const int k = s * 32 + lane / 16 * 8 + c;
+            v[c] = TURNED ? from[k * ld + row] : from[row * ld + k];
+        }
+        Frag f[PLANES];
+        split(v, f);
+#pragma unroll
+        for (int n = 0; n < PLANES; ++n) to[frag_at(wave, s, n, 2, PLANES)] = f[n];
+    }
+}
+
+// A workgroup per key head and chunk: K and Q as fragments, and N and P of every value head that shares them.
 template <typename E, int DK>
 __global__ __launch_bounds__(kDeltaThreads) void chunk_kernel(DeltaArgs p)
 {
-    constexpr int LD = DK + 1, LN = kSteps + 1;
-    extern __shared__ __attribute__((aligned(16))) float lds[];
-    float *K = lds, *Q = K + kSteps * LD, *A = Q + kSteps * LD, *N = A + kSteps * LN;
+    constexpr int PE = kExact<E>, LN = kSteps + 1, kOrder = PE == 1 ? 0 : 2;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    auto &K = *reinterpret_cast<KeyRows<E, DK> *>(lds);
+    auto &Q = *reinterpret_cast<KeyRows<E, DK> *>(lds + sizeof(K));
+    float *A = reinterpret_cast<float *>(lds + 2 * sizeof(K)), *N = A + kSteps * LN;
     __shared__ ChunkGates gates;
-    __shared__ int bad;
-    const int64_t record = blockIdx.x;
-    const int chunk = (int)(record % p.chunks), h = (int)(record / p.chunks % p.Hv);
-    const int64_t b = record / p.chunks / p.Hv;
+    __shared__ int bad_rows, bad;
+    const int chunk = (int)(blockIdx.x % p.chunks), hk = (int)(blockIdx.x / p.chunks % p.Hk);
+    const int64_t b = blockIdx.x / p.chunks / p.Hk;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, at = lane % 16, group = lane / 16;
-    if (wave == 0) gates_of(p, b, h, chunk, gates);
-    if (threadIdx.x == 0) bad = 0;
-    __syncthreads();
-    const int hk = h / (p.Hv / p.Hk);
-    for (int e = threadIdx.x; e < kSteps * DK; e += kDeltaThreads) {
-        const int i = e / DK, d = e % DK;
-        const bool is = bit_of(gates.live, i) && d < p.Dk;
-        K[i * LD + d] = is ? to_f32(row_at<E>(p.k, p.ld_k, b, p.T, chunk * kSteps + i, hk, p.Dk)[d]) : 0.0f;
-        Q[i * LD + d] = is ? to_f32(row_at<E>(p.q, p.ld_q, b, p.T, chunk * kSteps + i, hk, p.Dk)[d]) : 0.0f;
-    }
-    for (int e = threadIdx.x; e < kSteps * LN; e += kDeltaThreads) A[e] = N[e] = 0.0f;
-    __syncthreads();
-    float *P_out = p.P + record * kSteps * kSteps;
-    bool fine = true;
-    for (int tile = 0; tile < 4; ++tile) {
-        Acc kk = {}, qk = {};
-        if (tile <= wave) {
-            auto keys = [&](int k, int col) { return K[(tile * 16 + col) * LD + k]; };
-            kk = product(DK, kk, [&](int row, int k) { return K[(wave * 16 + row) * LD + k]; }, keys);
-            qk = product(DK, qk, [&](int row, int k) { return Q[(wave * 16 + row) * LD + k]; }, keys);
-        }
-        const int j = tile * 16 + at;
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r;
-            const bool on = j <= i && bit_of(gates.live, i) && bit_of(gates.live, j) && joined(gates.starts, i, j);
-            const float e = on ? decay_of(gates.G[i] - gates.G[j]) : 0.0f;
-            const float a = on && j < i ? e * kk[r] : 0.0f, v = on ? p.scale * e * qk[r] : 0.0f;
-            A[i * LN + j] = a;
-            P_out[i * kSteps + j] = v;
-            fine = fine && (a + v) * 0.0f == 0.0f;
-        }
-    }
-    __syncthreads();
-    // blocks on the diagonal: N_i = A_i - sum_j A_ij beta_j N_j, a column a lane
+    if (threadIdx.x == 0) bad_rows = 0;
+    unsigned long long live;
     {
-        float n[16];
+        const int t = chunk * kSteps + lane;
+        live = __ballot(t < p.T && (!p.filled || p.filled[b * p.T + t]));
+    }
+    __syncthreads();
+    {
+        bool fine = K.fill(p, p.k, p.ld_k, b, hk, chunk, live);
+        fine = Q.fill(p, p.q, p.ld_q, b, hk, chunk, live) && fine;
+        if (!fine) bad_rows = 1;
+    }
+    __syncthreads();
+    K.write(p.K + (int64_t)blockIdx.x * key_frags(DK, PE), p.KT + (int64_t)blockIdx.x * key_frags(DK, PE));
+    Q.write(p.Q + (int64_t)blockIdx.x * key_frags(DK, PE), p.QT ? p.QT + (int64_t)blockIdx.x * key_frags(DK, PE) : nullptr);
+    Acc kk[4] = {}, qk[4] = {};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float v = A[(wave * 16 + i) * LN + wave * 16 + at];
+    for (int s = 0; s < DK / 32; ++s) {
+        Frag k[PE], q[PE];
+        K.row_frag(wave, s, k);
+        Q.row_frag(wave, s, q);
 #pragma unroll
-            for (int j = 0; j < i; ++j) v = fmaf(-A[(wave * 16 + i) * LN + wave * 16 + j] * gates.beta[wave * 16 + j], n[j], v);
-            n[i] = i > at ? v : 0.0f;
-            if (group == 0) N[(wave * 16 + i) * LN + wave * 16 + at] = n[i];
-            fine = fine && n[i] * 0.0f == 0.0f;
+        for (int tile = 0; tile < 4; ++tile) {
+            if (tile > wave) continue;
+            Frag other[PE];
+            K.row_frag(tile, s, other);
+            kk[tile] = multiply<PE, PE, kOrder>(k, other, kk[tile]);
+            qk[tile] = multiply<PE, PE, kOrder>(q, other, qk[tile]);
         }
     }
-    __syncthreads();
-    // block columns: N_ij = (I - N_ii beta) (A_ij - sum_m A_im beta_m N_mj), downwards
-    for (int i = wave + 1; i < 4; ++i) {
-        Acc c;
-        for (int r = 0; r < 4; ++r) c[r] = A[(i * 16 + group * 4 + r) * LN + wave * 16 + at];
-        c = product((i - wave) * 16, c, [&](int row, int k) { return -A[(i * 16 + row) * LN + wave * 16 + k] * gates.beta[wave * 16 + k]; },
-                    [&](int k, int col) { return N[(wave * 16 + k) * LN + wave * 16 + col]; });
-        for (int r = 0; r < 4; ++r) N[(i * 16 + group * 4 + r) * LN + wave * 16 + at] = c[r];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        c = product(16, c, [&](int row, int k) { return -N[(i * 16 + row) * LN + i * 16 + k] * gates.beta[i * 16 + k]; },
-                    [&](int k, int col) { return N[(i * 16 + k) * LN + wave * 16 + col]; });
-        __builtin_amdgcn_wave_barrier();
-        for (int r = 0; r < 4; ++r) N[(i * 16 + group * 4 + r) * LN + wave * 16 + at] = c[r];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        fine = fine && all_finite(c);
-    }
-    if (!fine) bad = 1;
-    __syncthreads();
-    if (bad && wave == 0) {                            // again without anything that is not one of the sequence's steps in between
-        for (int i = 0; i < kSteps; ++i) {
-            float v = 0.0f;
-            if (lane < i && joined(gates.starts, i, lane)) {
-                v = A[i * LN + lane];
-                for (int j = lane + 1; j < i; ++j)
-                    if (bit_of(gates.live, j)) v = fmaf(-A[i * LN + j] * gates.beta[j], N[j * LN + lane], v);
+    const int shared = p.Hv / p.Hk;
+    for (int member = 0; member < shared; ++member) {
+        const int h = hk * shared + member;
+        const int64_t record = (b * p.Hv + h) * p.chunks + chunk;
+        __syncthreads();
+        if (wave == 0) gates_of(p, b, h, chunk, 0, gates);
+        if (threadIdx.x == 0) bad = bad_rows;
+        __syncthreads();
+        const unsigned long long starts = gates.starts;
+        // P through the room of N, then A
+        bool fine = true;
+#pragma unroll
+        for (int tile = 0; tile < 4; ++tile) {
+            const int j = tile * 16 + at;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = wave * 16 + group * 4 + r;
+                const bool on = j <= i && bit_of(live, i) && bit_of(live, j) && joined(starts, i, j);
+                const float e = on ? decay_of(gates.G[i] - gates.G[j]) : 0.0f;
+                const float a = on && j < i ? e * kk[tile][r] : 0.0f, v = on ? p.scale * e * qk[tile][r] : 0.0f;
+                A[i * LN + j] = a;
+                N[i * LN + j] = v;
+                fine = fine && (a + v) * 0.0f == 0.0f;
             }
-            N[i * LN + lane] = v;
+        }
+        __syncthreads();
+        write_square<kFine<E>, false>(N, LN, p.P + record * square_frags(kFine<E>));
+        if (p.PT) write_square<3, true>(N, LN, p.PT + record * square_frags(3));
+        __syncthreads();
+        for (int e = threadIdx.x; e < kSteps * LN; e += kDeltaThreads) N[e] = 0.0f;
+        __syncthreads();
+        // blocks on the diagonal: N_i = A_i - sum_j A_ij beta_j N_j, a column a lane
+        {
+            float n[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float v = A[(wave * 16 + i) * LN + wave * 16 + at];
+#pragma unroll
+                for (int j = 0; j < i; ++j) v = fmaf(-A[(wave * 16 + i) * LN + wave * 16 + j] * gates.beta[wave * 16 + j], n[j], v);
+                n[i] = i > at ? v : 0.0f;
+                if (group == 0) N[(wave * 16 + i) * LN + wave * 16 + at] = n[i];
+                fine = fine && n[i] * 0.0f == 0.0f;
+            }
+        }
+        __syncthreads();
+        // block columns: N_ij = (I - N_ii beta) (A_ij - sum_m A_im beta_m N_mj), downwards
+        for (int i = wave + 1; i < 4; ++i) {
+            Acc c;
+            for (int r = 0; r < 4; ++r) c[r] = A[(i * 16 + group * 4 + r) * LN + wave * 16 + at];
+            c = product((i - wave) * 16, c, [&](int row, int k) { return -A[(i * 16 + row) * LN + wave * 16 + k] * gates.beta[wave * 16 + k]; },
+                        [&](int k, int col) { return N[(wave * 16 + k) * LN + wave * 16 + col]; });
+            for (int r = 0; r < 4; ++r) N[(i * 16 + group * 4 + r) * LN + wave * 16 + at] = c[r];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
+            c = product(16, c, [&](int row, int k) { return -N[(i * 16 + row) * LN + i * 16 + k] * gates.beta[i * 16 + k]; },
+                        [&](int k, int col) { return N[(i * 16 + k) * LN + wave * 16 + col]; });
+            __builtin_amdgcn_wave_barrier();
+            for (int r = 0; r < 4; ++r) N[(i * 16 + group * 4 + r) * LN + wave * 16 + at] = c[r];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            fine = fine && all_finite(c);
         }
+        if (!fine) bad = 1;
+        __syncthreads();
+        if (bad && wave == 0) {                        // again without anything that is not one of the sequence's steps in between
+            for (int i = 0; i < kSteps; ++i) {
+                float v = 0.0f;
+                if (lane < i && joined(starts, i, lane)) {
+                    v = A[i * LN + lane];
+                    for (int j = lane + 1; j < i; ++j)
+                        if (bit_of(live, j)) v = fmaf(-A[i * LN + j] * gates.beta[j], N[j * LN + lane], v);
+                }
+                N[i * LN + lane] = v;
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        if (threadIdx.x == 0) gates.bad = bad;
+        __syncthreads();
+        write_square<3, false>(N, LN, p.N + record * square_frags(3));
+        if (p.NT) write_square<3, true>(N, LN, p.NT + record * square_frags(3));
+        const int *from = reinterpret_cast<const int *>(&gates);
+        int *to = reinterpret_cast<int *>(p.gates + record);
+        for (int e = threadIdx.x; e < (int)(sizeof(ChunkGates) / 4); e += kDeltaThreads) to[e] = from[e];
     }
-    __syncthreads();
-    float *N_out = p.N + record * kSteps * kSteps;
-    for (int e = threadIdx.x; e < kSteps * kSteps; e += kDeltaThreads) N_out[e] = N[e / kSteps * LN + e % kSteps];
-    if (threadIdx.x == 0) gates.bad = bad;
-    __syncthreads();
-    const int *from = reinterpret_cast<const int *>(&gates);
-    int *to = reinterpret_cast<int *>(p.gates + record);
-    for (int e = threadIdx.x; e < (int)(sizeof(ChunkGates) / 4); e += kDeltaThreads) to[e] = from[e];
 }
 
-// The chunks of one head one after the other, for kCols value columns.  Wave w has rows 16 w on of the chunk, and rows
-// w DK / 4 on of the state, which stays in its accumulators.
-template <typename E, int DK>
-__global__ __launch_bounds__(kDeltaThreads) void scan_kernel(DeltaArgs p)
+// The chunks of one head one after the other, for 16 NT value columns: tile n of a lane's column l % 16 is column NT (l % 16) + n.  Wave w has
+// rows 16 w on of the chunk, and rows w DK / 4 on of the state, which stays in its accumulators; the others read it as planes from shared memory.
+// Loads are issued a phase ahead of their use, those for the start of a chunk in the middle of the one before.
+template <typename E, int DK, int NT>
+__global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2 : 1) void scan_kernel(DeltaArgs p)
 {
-    constexpr int LD = DK + 1, LS = DK + 1, LU = kSteps + 1;
+    constexpr int PE = kExact<E>, PF = kFine<E>, KS = DK / 32, LS = DK + 8, LU = kSteps + 8, C = 16 * NT;
     constexpr int kTiles = (DK + 63) / 64;             // of the state, for a wave; of DK = 32 two waves have one
-    extern __shared__ __attribute__((aligned(16))) float lds[];
-    float *K = lds, *Q = K + kSteps * LD, *S = Q + kSteps * LD, *R = S + kCols * LS, *U = R + kCols * LU, *Ue = U + kCols * LU;
-    __shared__ ChunkGates gates;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    typedef __bf16 StatePlane[C][LS];
+    typedef __bf16 StepPlane[C][LU];
+    StatePlane *S = reinterpret_cast<StatePlane *>(lds);                           // [3], columns of the state
+    StepPlane *R = reinterpret_cast<StepPlane *>(lds + 3 * sizeof(StatePlane)), *U = R + 3, *Ue = U + PF;      // [3], [PF], [3]
     __shared__ int not_finite[2];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, at = lane % 16, group = lane / 16;
-    const int blocks = (p.Dv + kCols - 1) / kCols;
-    const int64_t head = blockIdx.x / blocks;
-    const int first = (int)(blockIdx.x % blocks) * kCols, col = first + at;
-    const int h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk);
-    const int64_t b = head / p.Hv;
-    const bool in = col < p.Dv;
-    Acc state[kTiles];
-    auto key_row = [&](int tile, int r) { return (wave * kTiles + tile) * 16 + group * 4 + r; };
+    const Place place = place_of((int64_t)p.B * p.Hv, p.Dv, C);
+    if (place.head < 0) return;                        // the whole workgroup
+    const int64_t head = place.head, b = head / p.Hv;
+    const int col = place.first + at * NT, h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk);
+    const int64_t key_head = b * p.Hk + hk;
+    const bool has_state = wave * kTiles * 16 < DK;
+    Acc state[kTiles][NT] = {};
+    if (p.s_first && has_state)
 #pragma unroll
-    for (int tile = 0; tile < kTiles; ++tile)
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (wave * kTiles + tile) * 16 + group * 4 + r;
+                float v[NT] = {};
+                if (d < p.Dk) read_columns<float, NT>(p.s_first + (head * p.Dk + d) * p.Dv, col, p.Dv, v);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) state[tile][n][r] = v[n];
+            }
+    // for the start of a chunk
+    Frag k[KS][PE], q[KS][PE];
+    float v[4][NT];
+    Acc f_next, t_next, beta_next;
+    auto load_start = [&](int chunk) {
+        const Frag *K = p.K + (key_head * p.chunks + chunk) * key_frags(DK, PE), *Q = p.Q + (key_head * p.chunks + chunk) * key_frags(DK, PE);
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int n = 0; n < PE; ++n) {
+                k[s][n] = K[frag_at(wave, s, n, KS, PE)];
+                q[s][n] = Q[frag_at(wave, s, n, KS, PE)];
+            }
+        const ChunkGates &g = p.gates[head * p.chunks + chunk];
+        f_next = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
+        t_next = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
+        beta_next = *reinterpret_cast<const Acc *>(g.beta + wave * 16 + group * 4);
+#pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = key_row(tile, r);
-            state[tile][r] = p.s_first && in && d < p.Dk ? p.s_first[(head * p.Dk + d) * p.Dv + col] : 0.0f;
+            const int t = chunk * kSteps + wave * 16 + group * 4 + r;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) v[r][n] = 0.0f;
+            if (t < p.T) read_columns<E, NT>(row_at<E>(p.v, p.ld_v, b, p.T, t, h, p.Dv), col, p.Dv, v[r]);
         }
+    };
+    auto state_out = [&](float *to) {                  // [Dk,Dv]
+#pragma unroll
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (wave * kTiles + tile) * 16 + group * 4 + r;
+                float v[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) v[n] = state[tile][n][r];
+                if (d < p.Dk) write_columns<float, NT>(to + (int64_t)d * p.Dv, col, p.Dv, v);
+            }
+    };
+    auto share_state = [&] {
+#pragma unroll
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                Four planes[3];
+                split(state[tile][n], planes);
+#pragma unroll
+                for (int m = 0; m < 3; ++m) *reinterpret_cast<Four *>(&S[m][n * 16 + at][(wave * kTiles + tile) * 16 + group * 4]) = planes[m];
+            }
+    };
+    auto share_steps = [&](StepPlane *to, auto &planes, int n) {
+        constexpr int PLANES = sizeof(planes) / sizeof(Four);
+#pragma unroll
+        for (int m = 0; m < PLANES; ++m) *reinterpret_cast<Four *>(&to[m][n * 16 + at][wave * 16 + group * 4]) = planes[m];
+    };
+    if (p.chunks > 0) load_start(0);
+    if (has_state) share_state();
+    if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
+    __syncthreads();
     for (int chunk = 0; chunk < p.chunks; ++chunk) {
         const int64_t record = head * p.chunks + chunk;
-        __syncthreads();
-        {
-            const int *from = reinterpret_cast<const int *>(p.gates + record);
-            int *to = reinterpret_cast<int *>(&gates);
-            for (int e = threadIdx.x; e < (int)(sizeof(ChunkGates) / 4); e += kDeltaThreads) to[e] = from[e];
-        }
-        if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
+        const ChunkGates &g = p.gates[record];
+        const unsigned long long starts = g.starts, live = g.live;
+        const float whole = g.f[kSteps - 1];
+        const bool bad = g.bad != 0;
+        if (p.S && has_state) state_out(p.S + record * p.Dk * p.Dv);
+        Frag nn[2][3], pp[2][PF], kt[kTiles][2][PE];
+        const Frag *N = p.N + record * square_frags(3), *P = p.P + record * square_frags(PF);
+        const Frag *KT = p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE);
 #pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile)
-            for (int r = 0; r < 4; ++r) {
-                const int d = key_row(tile, r);
-                if (d < DK) S[at * LS + d] = state[tile][r];
-                if (p.S && in && d < p.Dk) p.S[(record * p.Dk + d) * p.Dv + col] = state[tile][r];
+        for (int s = 0; s < 2; ++s) {
+            if (s * 32 > wave * 16) continue;          // zeros
+#pragma unroll
+            for (int n = 0; n < 3; ++n) nn[s][n] = N[frag_at(wave, s, n, 2, 3)];
+#pragma unroll
+            for (int n = 0; n < PF; ++n) pp[s][n] = P[frag_at(wave, s, n, 2, PF)];
+        }
+        // R = V - f K S
+        Acc ks[NT] = {}, qs[NT] = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                Frag of_state[3], fine[PF];
+#pragma unroll
+                for (int m = 0; m < 3; ++m) of_state[m] = *reinterpret_cast<const Frag *>(&S[m][n * 16 + at][s * 32 + group * 8]);
+#pragma unroll
+                for (int m = 0; m < PF; ++m) fine[m] = of_state[m];
+                ks[n] = multiply<PE, 3>(k[s], of_state, ks[n]);
+                qs[n] = multiply<PE, PF>(q[s], fine, qs[n]);
             }
-        __syncthreads();
-        for (int e = threadIdx.x; e < kSteps * DK; e += kDeltaThreads) {
-            const int i = e / DK, d = e % DK;
-            const bool is = bit_of(gates.live, i) && d < p.Dk;
-            K[i * LD + d] = is ? to_f32(row_at<E>(p.k, p.ld_k, b, p.T, chunk * kSteps + i, hk, p.Dk)[d]) : 0.0f;
-            Q[i * LD + d] = is ? to_f32(row_at<E>(p.q, p.ld_q, b, p.T, chunk * kSteps + i, hk, p.Dk)[d]) : 0.0f;
-        }
-        __syncthreads();
-        auto of_state = [&](int k, int c) { return S[c * LS + k]; };
-        Acc ks = {}, qs = {};
-        ks = product(DK, ks, [&](int row, int k) { return K[(wave * 16 + row) * LD + k]; }, of_state);
-        qs = product(DK, qs, [&](int row, int k) { return Q[(wave * 16 + row) * LD + k]; }, of_state);
-        Acc m, scaled;
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r;
-            const bool live = bit_of(gates.live, i);
-            const float v = live && in ? to_f32(row_at<E>(p.v, p.ld_v, b, p.T, chunk * kSteps + i, h, p.Dv)[col]) : 0.0f;
-            const float f = gates.f[i];
-            m[r] = live ? f == 0.0f ? v : fmaf(-f, ks[r], v) : 0.0f;
-            scaled[r] = gates.beta[i] * m[r];
-            R[at * LU + i] = scaled[r];
-        }
-        if (!all_finite(scaled)) not_finite[0] = 1;
-        __syncthreads();
-        const unsigned long long starts = gates.starts, alive = gates.live;
-        const float *N = p.N + (record * kSteps + wave * 16) * kSteps, *P = p.P + (record * kSteps + wave * 16) * kSteps;
-        auto of_r = [&](int k, int c) { return R[c * LU + k]; };
-        auto of_n = [&](int row, int k) { return -N[row * kSteps + k]; };
-        if (gates.bad || not_finite[0])
-            m = careful_product(kSteps, m, of_n, of_r, [&](int row, int k) {
-                const int i = wave * 16 + row;
-                return k < i && bit_of(alive, i) && bit_of(alive, k) && joined(starts, i, k);
-            });
-        else m = product((wave + 1) * 16, m, of_n, of_r);
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r;
-            const float t = gates.t[i];
-            scaled[r] = gates.beta[i] * m[r];
-            U[at * LU + i] = scaled[r];
-            Ue[at * LU + i] = t == 0.0f ? 0.0f : t * scaled[r];
-            if (p.M && in) p.M[(record * kSteps + i) * p.Dv + col] = m[r];
-        }
-        if (!all_finite(scaled)) not_finite[1] = 1;
-        __syncthreads();
-        Acc o;
-        for (int r = 0; r < 4; ++r) {
-            const float f = gates.f[wave * 16 + group * 4 + r];
-            o[r] = f == 0.0f ? 0.0f : p.scale * f * qs[r];
-        }
-        auto of_u = [&](int k, int c) { return U[c * LU + k]; };
-        auto of_p = [&](int row, int k) { return P[row * kSteps + k]; };
-        if (gates.bad || not_finite[1])
-            o = careful_product(kSteps, o, of_p, of_u, [&](int row, int k) {
-                const int i = wave * 16 + row;
-                return k <= i && bit_of(alive, i) && bit_of(alive, k) && joined(starts, i, k);
-            });
-        else o = product((wave + 1) * 16, o, of_p, of_u);
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r, t = chunk * kSteps + i;
-            if (t < p.T && in) const_cast<E *>(row_at<E>(p.o, p.ld_o, b, p.T, t, h, p.Dv))[col] = from_f32<E>(bit_of(alive, i) ? o[r] : 0.0f);
-        }
-        const float whole = gates.f[kSteps - 1];
+        const Acc f = f_next, t = t_next, beta = beta_next;
+        Acc m[NT];
 #pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile) {
-            for (int r = 0; r < 4; ++r) state[tile][r] = whole == 0.0f ? 0.0f : whole * state[tile][r];
-            const int d0 = (wave * kTiles + tile) * 16;
-            if (d0 < DK)
-                state[tile] = product(kSteps, state[tile], [&](int row, int k) { return gates.t[k] == 0.0f ? 0.0f : K[k * LD + d0 + row]; },
-                                      [&](int k, int c) { return Ue[c * LU + k]; });
+        for (int n = 0; n < NT; ++n) {
+            Acc minus;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool on = bit_of(live, wave * 16 + group * 4 + r);
+                m[n][r] = !on ? 0.0f : f[r] == 0.0f ? v[r][n] : fmaf(-f[r], ks[n][r], v[r][n]);
+            }
+            minus = -(beta * m[n]);
+            Four planes[3];
+            split(minus, planes);
+            share_steps(R, planes, n);
+            if (!all_finite(minus)) not_finite[0] = 1;
         }
+        __syncthreads();
+        if (has_state)
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int n = 0; n < PE; ++n) kt[tile][s][n] = KT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
+        // M = R - N (beta R), U = beta M
+        const bool careful_n = bad || not_finite[0];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (careful_n) {
+                unsigned long long pass[4];
+                for (int r = 0; r < 4; ++r) {
+                    const int i = wave * 16 + group * 4 + r;
+                    pass[r] = bit_of(live, i) ? upto(starts, i) & live & ~(1ull << i) : 0;
+                }
+                m[n] = careful_multiply(m[n], N, wave, 3, R[0][n * 16 + at], 3, C * LU, pass);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if (s * 32 > wave * 16) continue;
+                    Frag of_r[3];
+#pragma unroll
+                    for (int x = 0; x < 3; ++x) of_r[x] = *reinterpret_cast<const Frag *>(&R[x][n * 16 + at][s * 32 + group * 8]);
+                    m[n] = multiply<3, 3>(nn[s], of_r, m[n]);
+                }
+            }
+            const Acc u = beta * m[n];
+            Acc to_end;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) to_end[r] = t[r] == 0.0f ? 0.0f : t[r] * u[r];
+            Four planes[PF], end_planes[3];
+            split(u, planes);
+            split(to_end, end_planes);
+            share_steps(U, planes, n);
+            share_steps(Ue, end_planes, n);
+            if (!all_finite(u)) not_finite[1] = 1;
+        }
+        if (p.M)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float x[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[n] = m[n][r];
+                write_columns<float, NT>(p.M + (record * kSteps + wave * 16 + group * 4 + r) * p.Dv, col, p.Dv, x);
+            }
+        if (chunk + 1 < p.chunks) load_start(chunk + 1);
+        __syncthreads();
+        // O = scale f Q S + P U
+        const bool careful_u = bad || not_finite[1];
+        Acc o[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[n][r] = f[r] == 0.0f ? 0.0f : p.scale * f[r] * qs[n][r];
+            if (careful_u) {
+                unsigned long long pass[4];
+                for (int r = 0; r < 4; ++r) {
+                    const int i = wave * 16 + group * 4 + r;
+                    pass[r] = bit_of(live, i) ? upto(starts, i) & live : 0;
+                }
+                o[n] = careful_multiply(o[n], P, wave, PF, U[0][n * 16 + at], PF, C * LU, pass);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if (s * 32 > wave * 16) continue;
+                    Frag of_u[PF];
+#pragma unroll
+                    for (int x = 0; x < PF; ++x) of_u[x] = *reinterpret_cast<const Frag *>(&U[x][n * 16 + at][s * 32 + group * 8]);
+                    o[n] = multiply<PF, PF>(pp[s], of_u, o[n]);
+                }
+            }
+        }
+        // S <- f_63 S + K' (t U)
+        if (has_state) {
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) state[tile][n][r] = whole == 0.0f ? 0.0f : whole * state[tile][n][r];
+            if (careful_u) {
+                unsigned long long pass[4];
+                for (int r = 0; r < 4; ++r) pass[r] = upto(starts, kSteps - 1) & live;
+                for (int tile = 0; tile < kTiles; ++tile)
+                    for (int n = 0; n < NT; ++n)
+                        state[tile][n] = careful_multiply(state[tile][n], KT, wave * kTiles + tile, PE, Ue[0][n * 16 + at], 3, C * LU, pass);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        Frag of_u[3];
+#pragma unroll
+                        for (int x = 0; x < 3; ++x) of_u[x] = *reinterpret_cast<const Frag *>(&Ue[x][n * 16 + at][s * 32 + group * 8]);
+#pragma unroll
+                        for (int tile = 0; tile < kTiles; ++tile) state[tile][n] = multiply<PE, 3>(kt[tile][s], of_u, state[tile][n]);
+                    }
+            }
+            share_state();
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = wave * 16 + group * 4 + r, step = chunk * kSteps + i;
+            float x[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x[n] = bit_of(live, i) ? o[n][r] : 0.0f;
+            if (step < p.T) write_columns<E, NT>(const_cast<E *>(row_at<E>(p.o, p.ld_o, b, p.T, step, h, p.Dv)), col, p.Dv, x);
+        }
+        if (threadIdx.x == 0) not_finite[0] = 0;       // read before the barrier above, written after the one below
+        __syncthreads();
+        if (threadIdx.x == 0) not_finite[1] = 0;
     }
-    if (p.s_last)
-#pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile)
-            for (int r = 0; r < 4; ++r) {
-                const int d = key_row(tile, r);
-                if (in && d < p.Dk) p.s_last[(head * p.Dk + d) * p.Dv + col] = state[tile][r];
-            }
+    if (p.s_last && has_state) state_out(p.s_last + head * p.Dk * p.Dv);
+}
+
+// Two tiles of columns a workgroup where that still fills the chip.
+template <typename E, int DK, int NT>
+int run_scan(const DeltaArgs &p, hipStream_t stream)
+{
+    const size_t lds = (size_t)16 * NT * (3 * (DK + 8) + (6 + kFine<E>) * (kSteps + 8)) * sizeof(__bf16);
+    if (const int rc = make_room_for(reinterpret_cast<const void *>(scan_kernel<E, DK, NT>), lds)) return rc;
+    hipLaunchKernelGGL((scan_kernel<E, DK, NT>), dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
+    return launched("delta scan");
 }
 
 template <typename E, int DK>
 int run(const DeltaArgs &p, hipStream_t stream)
 {
     if (p.chunks > 0) {
-        const size_t lds = (size_t)(2 * kSteps * (DK + 1) + 2 * kSteps * (kSteps + 1)) * sizeof(float);
+        const size_t lds = 2 * sizeof(KeyRows<E, DK>) + (size_t)2 * kSteps * (kSteps + 1) * sizeof(float);
         if (const int rc = make_room_for(reinterpret_cast<const void *>(chunk_kernel<E, DK>), lds)) return rc;
-        hipLaunchKernelGGL((chunk_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hv * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
+        hipLaunchKernelGGL((chunk_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
     }
-    const size_t lds = (size_t)(2 * kSteps * (DK + 1) + kCols * (DK + 1) + 3 * kCols * (kSteps + 1)) * sizeof(float);
-    if (const int rc = make_room_for(reinterpret_cast<const void *>(scan_kernel<E, DK>), lds)) return rc;
-    const int blocks = (p.Dv + kCols - 1) / kCols;
-    hipLaunchKernelGGL((scan_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hv * blocks)), dim3(kDeltaThreads), lds, stream, p);
-    return launched("delta scan");
+    if ((int64_t)p.B * p.Hv * ((p.Dv + 31) / 32) >= 256) return run_scan<E, DK, 2>(p, stream);
+    return run_scan<E, DK, 1>(p, stream);
 }
 
 }  // namespace
