@@ -65,9 +65,12 @@ struct DeltaArgs {
     Frag *K, *Q, *KT, *QT;                             // per (b, key head, chunk): rows, and transposed; QT null without keep
     Frag *N, *P, *NT, *PT;                             // per (b, value head, chunk); NT and PT null without keep
     ChunkGates *gates;                                 // per (b, value head, chunk), as all that follow
-    float *S, *M;                                      // [Dk,Dv] before the chunk, [64,Dv]; null without keep
-    float *D, *Y;                                      // [Dk,Dv] adjoint behind the chunk, [64,Dv]
+    // with keys and values padded, so that nothing asks where a row ends; null without keep
+    float *S, *M;                                      // [DK,DV] before the chunk, [64,DV]
+    float *D, *Y;                                      // [DK,DV] adjoint behind the chunk, [64,DV]
 };
+constexpr int padded_keys(int Dk) { return Dk <= 32 ? 32 : Dk <= 64 ? 64 : 128; }
+__host__ __device__ constexpr int padded_values(int Dv) { return (Dv + 31) / 32 * 32; }
 
 // Fragments of one matrix: of the keys of a chunk (padded to DK), and of N and its kind.
 constexpr int key_frags(int DK, int planes) { return kSteps / 16 * (DK / 32) * planes * kWave; }
@@ -133,11 +136,14 @@ __device__ __forceinline__ Acc multiply(const Frag (&a)[PA], const Frag (&b)[PB]
 
 // The same over 64 columns k without the matrix pipe, for chunks that hold an infinity or NaN: only the k in pass[r] take part in the lane's
 // r-th row.  a: the matrix's fragments; b: the lane's column, planes `plane` apart.
-__device__ __noinline__ static Acc careful_multiply(Acc c, const Frag *a, int tile, int PA, const __bf16 *b, int PB, int plane, const unsigned long long *pass)
+template <int PA, int PB>
+__device__ __forceinline__ Acc careful_multiply(Acc c, const Frag *a, int tile, const __bf16 *b, int plane, const unsigned long long (&pass)[4])
 {
     const int group = threadIdx.x % kWave / 16;
+#pragma unroll
     for (int r = 0; r < 4; ++r) {
         float v = c[r];
+#pragma unroll 1
         for (int k = 0; k < kSteps; ++k) {
             if (!bit_of(pass[r], k)) continue;
             float x = 0.0f, y = 0.0f;
@@ -164,20 +170,6 @@ __device__ __forceinline__ Acc product(int K, Acc c, FA &&a, FB &&b)
     for (int k = 0; k < K; k += 4) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a(at, k + group), b(k + group, at), c, 0, 0, 0);
     return c;
 }
-template <class FA, class FB, class FP>
-__device__ __noinline__ Acc careful_product(int K, Acc c, FA &&a, FB &&b, FP &&pass)
-{
-    const int lane = threadIdx.x % kWave, at = lane % 16, group = lane / 16;
-    for (int r = 0; r < 4; ++r) {
-        const int row = group * 4 + r;
-        float v = c[r];
-        for (int k = 0; k < K; ++k)
-            if (pass(row, k)) v = fmaf(a(row, k), b(k, at), v);
-        c[r] = v;
-    }
-    return c;
-}
-
 // Row of the elements of step t of sequence b and head h.
 template <typename E>
 __device__ __forceinline__ const E *row_at(const void *base, int64_t ld, int64_t b, int T, int t, int h, int D)
@@ -217,21 +209,22 @@ __device__ __forceinline__ void write_columns(E *row, int col, int D, const floa
     }
 }
 
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
+
 // The head and the first column of a workgroup on its way through the chunks.  Workgroups go to the eight dies in turn: those of a head, which
 // read the same fragments, are given to one die.  head = -1: nothing to do.
 struct Place { int64_t head; int first; };
 __device__ __forceinline__ Place place_of(int64_t heads, int Dv, int columns)
 {
-    const int blocks = (Dv + columns - 1) / columns;
+    const int blocks = padded_values(Dv) / columns;
     const int64_t all = heads * blocks, each = (all + 7) / 8, at = (int64_t)(blockIdx.x % 8) * each + blockIdx.x / 8;
     return at < all && blockIdx.x / 8 < each ? Place{at / blocks, (int)(at % blocks) * columns} : Place{-1, 0};
 }
-inline unsigned places(int64_t heads, int Dv, int columns) { return (unsigned)((heads * ((Dv + columns - 1) / columns) + 7) / 8 * 8); }
+inline unsigned places(int64_t heads, int Dv, int columns) { return (unsigned)((heads * (padded_values(Dv) / columns) + 7) / 8 * 8); }
 
 int delta_scan_launch(int dtype, const DeltaArgs &p, hipStream_t stream);
 int delta_grad_launch(int dtype, const DeltaArgs &p, hipStream_t stream);
 
-constexpr int padded_keys(int Dk) { return Dk <= 32 ? 32 : Dk <= 64 ? 64 : 128; }
 // Calls f with the padded key size as a constant.
 template <typename F>
 inline int with_keys(int Dk, F &&f)

@@ -23,7 +23,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
     // the upstream gradient of this chunk and of the next: [PE] as it is, [3] scaled by what of it reaches the state before
     StepPlane *upstream = reinterpret_cast<StepPlane *>(lds + 3 * sizeof(StatePlane)), *R = upstream + 2 * (PE + 3), *V = R + 3;      // [3], [3]
     __shared__ int not_finite[4];                      // upstream of even and odd chunks, beta dU, dV
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, at = lane % 16, group = lane / 16;
+    const int lane = threadIdx.x % kWave, wave = wave_index(), at = lane % 16, group = lane / 16;
     const Place place = place_of((int64_t)p.B * p.Hv, p.Dv, C);
     if (place.head < 0) return;                        // the whole workgroup
     const int64_t head = place.head, b = head / p.Hv;
@@ -62,6 +62,18 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
             for (int n = 0; n < NT; ++n) go[r][n] = 0.0f;
             if (t < p.T) read_columns<E, NT>(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), col, p.Dv, go[r]);
         }
+    };
+    const int DV = padded_values(p.Dv);
+    auto keep_adjoint = [&](float *to) {
+#pragma unroll
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float v[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) v[n] = adj[tile][n][r];
+                write_columns<float, NT>(to + ((wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
+            }
     };
     auto adjoint_out = [&](float *to) {                // [Dk,Dv]
 #pragma unroll
@@ -127,7 +139,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
         const StepPlane *O = upstream + chunk % 2 * (PE + 3), *Of = O + PE;
         // flags are taken back where all have read them and none sets them before the next barrier
         if (threadIdx.x == 0) not_finite[(chunk + 1) % 2] = not_finite[3] = 0;
-        if (has_state) adjoint_out(p.D + record * p.Dk * p.Dv);
+        if (has_state) keep_adjoint(p.D + record * DK * DV);
         Frag nn[2][3], pp[2][3], kt[kTiles][2][PE], qt[kTiles][2][PE];
         const Frag *N = p.NT + record * square_frags(3), *P = p.PT + record * square_frags(3);
         const Frag *KT = p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE), *QT = p.QT + (key_head * p.chunks + chunk) * key_frags(DK, PE);
@@ -162,7 +174,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
                     const int i = wave * 16 + group * 4 + r;
                     pass[r] = bit_of(live, i) ? from(starts, i) & live : 0;
                 }
-                y[n] = careful_multiply(y[n], P, wave, 3, O[0][n * 16 + at], PE, C * LU, pass);
+                y[n] = careful_multiply<3, PE>(y[n], P, wave, O[0][n * 16 + at], C * LU, pass);
             } else {
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
@@ -201,7 +213,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
                     const int i = wave * 16 + group * 4 + r;
                     pass[r] = bit_of(live, i) ? from(starts, i) & live & ~(1ull << i) : 0;
                 }
-                y[n] = careful_multiply(y[n], N, wave, 3, R[0][n * 16 + at], 3, C * LU, pass);
+                y[n] = careful_multiply<3, 3>(y[n], N, wave, R[0][n * 16 + at], C * LU, pass);
             } else {
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
@@ -237,10 +249,12 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
             if (careful_o || not_finite[3]) {
                 unsigned long long pass[4];
                 for (int r = 0; r < 4; ++r) pass[r] = (starts ? (starts & -starts) - 1 : ~0ull) & live;
+#pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        adj[tile][n] = careful_multiply(adj[tile][n], QT, wave * kTiles + tile, PE, Of[0][n * 16 + at], 3, C * LU, pass);
-                        adj[tile][n] = careful_multiply(adj[tile][n], KT, wave * kTiles + tile, PE, V[0][n * 16 + at], 3, C * LU, pass);
+                        adj[tile][n] = careful_multiply<PE, 3>(adj[tile][n], QT, wave * kTiles + tile, Of[0][n * 16 + at], C * LU, pass);
+                        adj[tile][n] = careful_multiply<PE, 3>(adj[tile][n], KT, wave * kTiles + tile, V[0][n * 16 + at], C * LU, pass);
                     }
             } else {
 #pragma unroll
@@ -268,7 +282,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
             float x[NT], z[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) x[n] = y[n][r], z[n] = bit_of(live, i) ? v[n][r] : 0.0f;
-            write_columns<float, NT>(p.Y + (record * kSteps + i) * p.Dv, col, p.Dv, x);
+            write_columns<float, NT>(p.Y + (record * kSteps + i) * DV, col, DV, x);
             if (step < p.T) write_columns<E, NT>(const_cast<E *>(row_at<E>(p.grad_v, p.ld_gv, b, p.T, step, h, p.Dv)), col, p.Dv, z);
         }
         if (chunk > 0) share_upstream(chunk - 1);
@@ -285,26 +299,91 @@ __device__ __forceinline__ float row_sum(float v)
     return v;
 }
 
-// Gradients of q, k, beta and the log decay of a chunk, the value heads of a key head one after the other.  Wave w has rows 16 w
-// on.  With dP = scale dO U', dA = -(dV) U' and their products with E, dN and dM:
-//   dq = dN K + scale f dO S'      dk = [dM K - f dV S'] + [dN' Q + dM' K + t U D']
-//   dG_i = q_i.dq_i + k_i.[first] - k_i.[second], to which the last step adds sum_j k_j.(t U D')_j + f_63 <D, S>;
-// the log decay's gradient is the sum of dG from its step to the end of its sequence.
-template <typename E, int DK>
-__global__ __launch_bounds__(kDeltaThreads) void chunk_grad_kernel(DeltaArgs p)
+// A chunk's steps as planes in shared memory, rows of 64 entries.
+constexpr int kRow = kSteps + 8;
+typedef __bf16 Plane[kSteps][kRow];
+
+template <int PLANES>
+__device__ __forceinline__ void put_row(Plane *to, int row, int col, const float *v)
 {
-    constexpr int LD = DK + 1, LN = kSteps + 1, kTiles = DK / 16;
+    Frag f[PLANES];
+    split(v, f);
+#pragma unroll
+    for (int n = 0; n < PLANES; ++n) *reinterpret_cast<Frag *>(&to[n][row][col]) = f[n];
+}
+template <int PLANES>
+__device__ __forceinline__ void get_frag(const Plane *from, int tile, int step, Frag (&to)[PLANES])
+{
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int n = 0; n < PLANES; ++n) to[n] = *reinterpret_cast<const Frag *>(&from[n][tile * 16 + lane % 16][step * 32 + lane / 16 * 8]);
+}
+
+// c + a b over 64 columns k for chunks that hold an infinity or NaN: only the k in pass[r] take part in the lane's r-th row.  a: rows of tile
+// `tile` in three planes; b: fragments of the transposed factor.
+template <int PB>
+__device__ __forceinline__ Acc careful_rows(Acc c, const Plane *a, int tile, const Frag *b, int b_tile, const unsigned long long (&pass)[4])
+{
+    const int lane = threadIdx.x % kWave, at = lane % 16, group = lane / 16;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int row = tile * 16 + group * 4 + r;
+        float v = c[r];
+#pragma unroll 1
+        for (int k = 0; k < kSteps; ++k) {
+            if (!bit_of(pass[r], k)) continue;
+            float x = 0.0f, y = 0.0f;
+            for (int n = 2; n >= 0; --n) x += (float)a[n][row][k];
+            for (int n = PB - 1; n >= 0; --n)
+                y += (float)reinterpret_cast<const __bf16 *>(b)[(((b_tile * 2 + k / 32) * PB + n) * kWave + at + k % 32 / 8 * 16) * 8 + k % 8];
+            v = fmaf(x, y, v);
+        }
+        c[r] = v;
+    }
+    return c;
+}
+
+// Gradients of q, k, beta and the log decay of a chunk, the value heads of a key head one after the other.  With dP = scale dO U',
+// dA = -(dV) U', their products dN and dM with E, and X = dM + dM':
+//   dq = dN K + scale f dO S'      dk = dN' Q + X K - f dV S' + t U D'
+//   dG_i = sum_j F_ij - sum_j F_ji + q_i.(scale f dO S')_i - k_i.(f dV S')_i - k_i.(t U D')_i      F_ij = dM_ij k_i.k_j + dN_ij q_i.k_j
+// to which the last step adds sum_j k_j.(t U D')_j + f_63 <D, S>; the log decay's gradient is the sum of dG from its step to the end of
+// its sequence.  Value columns come 64 at a time through shared memory.  Products with rows and columns of steps are split over the waves by
+// rows (16 w on), those with key columns by columns (w DK / 4 on), so that every entry of S and D is split into planes once.
+template <typename E, int DK>
+__global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs p)
+{
+    constexpr int PE = kExact<E>, KS = DK / 32, kTiles = (DK + 63) / 64, kOrder = PE == 1 ? 0 : 2;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    float *K = reinterpret_cast<float *>(lds), *Q = K + kSteps * LD, *dN = Q + kSteps * LD, *dM = dN + kSteps * LN;
+    Plane *U = reinterpret_cast<Plane *>(lds), *V = U + 3, *O = V + 3;             // [3], [3], [PE]
+    Plane *dN = U, *dNT = V, *X = U;                   // later in the same room, [3] each
     __shared__ ChunkGates gates;
     __shared__ int not_finite;
-    __shared__ float dG[kSteps], extra[kDeltaThreads / kWave], dbeta[kSteps];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, at = lane % 16, group = lane / 16;
-    const int chunk = (int)(blockIdx.x % p.chunks), hk = (int)(blockIdx.x / p.chunks % p.Hk);
+    __shared__ float rows_of[4][kSteps], columns_of[4][kSteps], flow[kSteps], extra[4], dbeta[kSteps];
+    const int lane = threadIdx.x % kWave;
+    int wave = wave_index(), at = lane % 16, group = lane / 16;
+    int nothing;
+    const int hk = (int)(blockIdx.x / p.chunks % p.Hk);
+    int chunk = (int)(blockIdx.x % p.chunks);
     const int64_t b = blockIdx.x / p.chunks / p.Hk;
-    const int shared = p.Hv / p.Hk;
-    Acc sum_q[kTiles] = {}, sum_k[kTiles] = {};
+    const int shared = p.Hv / p.Hk, DV = padded_values(p.Dv);
+    const bool has_keys = wave * kTiles * 16 < DK;
+    const Frag *K = p.K + (int64_t)blockIdx.x * key_frags(DK, PE), *Q = p.Q + (int64_t)blockIdx.x * key_frags(DK, PE);
+    const Frag *KT = p.KT + (int64_t)blockIdx.x * key_frags(DK, PE), *QT = p.QT + (int64_t)blockIdx.x * key_frags(DK, PE);
+    Acc sum_q[kTiles][4] = {}, sum_k[kTiles][4] = {};
+    unsigned long long alive = 0;
     for (int member = 0; member < shared; ++member) {
+        // else addresses, masks and the products of K and Q are formed before the loop, and 500 registers do not hold them
+        asm volatile("v_mov_b32 %0, 0" : "=v"(nothing));
+        at += nothing;
+        group += nothing;
+        nothing = __builtin_amdgcn_readfirstlane(nothing);
+        chunk += nothing;
+        wave += nothing;
+        K += nothing;
+        Q += nothing;
+        KT += nothing;
+        QT += nothing;
         const int h = hk * shared + member;
         const int64_t record = (b * p.Hv + h) * p.chunks + chunk;
         __syncthreads();
@@ -315,123 +394,234 @@ __global__ __launch_bounds__(kDeltaThreads) void chunk_grad_kernel(DeltaArgs p)
         }
         if (threadIdx.x == 0) not_finite = 0;
         __syncthreads();
-        const unsigned long long starts = gates.starts, alive = gates.live;
-        if (member == 0)
-            for (int e = threadIdx.x; e < kSteps * DK; e += kDeltaThreads) {
-                const int i = e / DK, d = e % DK;
-                const bool is = bit_of(alive, i) && d < p.Dk;
-                K[i * LD + d] = is ? to_f32(row_at<E>(p.k, p.ld_k, b, p.T, chunk * kSteps + i, hk, p.Dk)[d]) : 0.0f;
-                Q[i * LD + d] = is ? to_f32(row_at<E>(p.q, p.ld_q, b, p.T, chunk * kSteps + i, hk, p.Dk)[d]) : 0.0f;
-            }
-        const float *M = p.M + record * kSteps * p.Dv, *Y = p.Y + record * kSteps * p.Dv;
-        const float *S = p.S + record * p.Dk * p.Dv, *D = p.D + record * p.Dk * p.Dv;
-        auto grad_o = [&](int i, int c) {
-            return bit_of(alive, i) && c < p.Dv ? to_f32(row_at<E>(p.grad_o, p.ld_go, b, p.T, chunk * kSteps + i, h, p.Dv)[c]) : 0.0f;
-        };
-        auto grad_v = [&](int i, int c) { return bit_of(alive, i) && c < p.Dv ? gates.beta[i] * Y[i * p.Dv + c] : 0.0f; };
-        auto u = [&](int i, int c) { return bit_of(alive, i) && c < p.Dv ? gates.beta[i] * M[i * p.Dv + c] : 0.0f; };
-        auto mine = [&](int row) { return wave * 16 + row; };
-        bool fine = true;
-        for (int tile = 0; tile < 4; ++tile) {
-            Acc n = {}, m = {};
-            if (tile <= wave) {
-                auto of_u = [&](int k, int c) { return u(tile * 16 + c, k); };
-                n = product((p.Dv + 3) / 4 * 4, n, [&](int row, int k) { return grad_o(mine(row), k); }, of_u);
-                m = product((p.Dv + 3) / 4 * 4, m, [&](int row, int k) { return -grad_v(mine(row), k); }, of_u);
-            }
-            const int j = tile * 16 + at;
-            for (int r = 0; r < 4; ++r) {
-                const int i = mine(group * 4 + r);
-                const bool on = j <= i && bit_of(alive, i) && bit_of(alive, j) && joined(starts, i, j);
-                const float e = on ? decay_of(gates.G[i] - gates.G[j]) : 0.0f;
-                const float a = on ? p.scale * e * n[r] : 0.0f, c = on && j < i ? e * m[r] : 0.0f;
-                dN[i * LN + j] = a;
-                dM[i * LN + j] = c;
-                fine = fine && (a + c) * 0.0f == 0.0f;
-            }
-        }
-        for (int e = threadIdx.x; member == 0 && e < kSteps * DK; e += kDeltaThreads) fine = fine && (K[e / DK * LD + e % DK] + Q[e / DK * LD + e % DK]) * 0.0f == 0.0f;
-        if (!fine) not_finite = 1;
-        // dbeta = M.Y, four lanes a row
-        {
-            const int i = threadIdx.x / 4;
-            float v = 0.0f;
-            if (bit_of(alive, i))
-                for (int c = threadIdx.x % 4; c < p.Dv; c += 4) v = fmaf(M[i * p.Dv + c], Y[i * p.Dv + c], v);
-            v += __shfl_xor(v, 1);
-            v += __shfl_xor(v, 2);
-            if (threadIdx.x % 4 == 0) dbeta[i] = v;
-        }
-        __syncthreads();
-        const bool bad = gates.bad || not_finite;
-        Acc dq[kTiles], plus[kTiles], minus[kTiles];
-        float at_end = 0.0f, dot[4] = {};
+        const unsigned long long starts = gates.starts;
+        alive = gates.live;
+        const float *M = p.M + record * kSteps * DV, *Y = p.Y + record * kSteps * DV;
+        const float *S = p.S + record * DK * DV, *D = p.D + record * DK * DV;
+        Acc dp[4] = {}, da[4] = {}, far_q[kTiles][4] = {}, far_k[kTiles][4] = {}, end[kTiles][4] = {};
+        float dot_states = 0.0f, dot_beta = 0.0f;
+        for (int c0 = 0; c0 < p.Dv; c0 += kSteps) {
+            const int steps = min(2, (DV - c0) / 32);
+            // S and D of the wave's keys: loads go out before the wait for the staging
+            typedef float Eight __attribute__((ext_vector_type(8)));
+            Eight s[kTiles][2], d[kTiles][2];
 #pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile) {
-            const int d = tile * 16 + at, n = (p.Dv + 3) / 4 * 4;
-            auto of_s = [&](int k, int c) { return tile * 16 + c < p.Dk && k < p.Dv ? S[(tile * 16 + c) * p.Dv + k] : 0.0f; };
-            auto of_d = [&](int k, int c) { return tile * 16 + c < p.Dk && k < p.Dv ? D[(tile * 16 + c) * p.Dv + k] : 0.0f; };
-            Acc far_q = {}, far_k = {}, end = {};
-            far_q = product(n, far_q, [&](int row, int k) { return grad_o(mine(row), k); }, of_s);
-            far_k = product(n, far_k, [&](int row, int k) { return grad_v(mine(row), k); }, of_s);
-            end = product(n, end, [&](int row, int k) { return u(mine(row), k); }, of_d);
-            for (int r = 0; r < 4; ++r) {
-                const int i = mine(group * 4 + r);
-                const float f = gates.f[i], t = gates.t[i];
+            for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                for (int step = 0; step < 2; ++step) {
+                    if (!has_keys || step >= steps) continue;
+                    const int from = ((wave * kTiles + tile) * 16 + at) * DV + c0 + step * 32 + group * 8;
+                    s[tile][step] = *reinterpret_cast<const Eight *>(S + from);
+                    d[tile][step] = *reinterpret_cast<const Eight *>(D + from);
+                }
+            if (threadIdx.x % 4 < 2 * steps) {
+                const int i = threadIdx.x / 4, t = chunk * kSteps + i;
                 const bool live = bit_of(alive, i);
-                far_q[r] = f == 0.0f || !live ? 0.0f : p.scale * f * far_q[r];
-                far_k[r] = f == 0.0f || !live ? 0.0f : -f * far_k[r];
-                end[r] = t == 0.0f || !live ? 0.0f : t * end[r];
-                if (t != 0.0f && live) at_end = fmaf(K[i * LD + d], end[r], at_end);
+                const float beta = gates.beta[i];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int c = threadIdx.x % 4 * 16 + half * 8;
+                    const Eight m = *reinterpret_cast<const Eight *>(M + i * DV + c0 + c), y = *reinterpret_cast<const Eight *>(Y + i * DV + c0 + c);
+                    float u[8], v[8], o[8] = {};
+                    if (live) read_columns<E, 8>(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), c0 + c, p.Dv, o);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        dot_beta = live ? fmaf(m[e], y[e], dot_beta) : 0.0f;
+                        u[e] = live ? beta * m[e] : 0.0f;
+                        v[e] = live ? beta * y[e] : 0.0f;
+                    }
+                    put_row<3>(U, i, c, u);
+                    put_row<3>(V, i, c, v);
+                    put_row<PE>(O, i, c, o);
+                }
             }
-            auto of_k = [&](int k, int c) { return K[k * LD + tile * 16 + c]; };
-            auto of_q = [&](int k, int c) { return Q[k * LD + tile * 16 + c]; };
-            auto n_row = [&](int row, int k) { return dN[mine(row) * LN + k]; };
-            auto m_row = [&](int row, int k) { return dM[mine(row) * LN + k]; };
-            auto n_col = [&](int row, int k) { return dN[k * LN + mine(row)]; };
-            auto m_col = [&](int row, int k) { return dM[k * LN + mine(row)]; };
-            if (bad) {
-                auto before = [&](int row, int k) {
-                    const int i = mine(row);
-                    return k <= i && bit_of(alive, i) && bit_of(alive, k) && joined(starts, i, k);
-                };
-                auto behind = [&](int row, int k) {
-                    const int i = mine(row);
-                    return k >= i && bit_of(alive, i) && bit_of(alive, k) && joined(starts, k, i);
-                };
-                dq[tile] = careful_product(kSteps, far_q, n_row, of_k, before);
-                plus[tile] = careful_product(kSteps, far_k, m_row, of_k, before);
-                minus[tile] = careful_product(kSteps, end, n_col, of_q, behind);
-                minus[tile] = careful_product(kSteps, minus[tile], m_col, of_k, behind);
-            } else {
-                dq[tile] = product(kSteps, far_q, n_row, of_k);
-                plus[tile] = product(kSteps, far_k, m_row, of_k);
-                minus[tile] = product(kSteps, end, n_col, of_q);
-                minus[tile] = product(kSteps, minus[tile], m_col, of_k);
+            __syncthreads();
+#pragma unroll
+            for (int step = 0; step < 2; ++step) {
+                if (step >= steps) continue;
+                Frag o[PE], v[3];
+                get_frag(O, wave, step, o);
+                get_frag(V, wave, step, v);
+#pragma unroll
+                for (int tile = 0; tile < 4; ++tile) {
+                    if (tile > wave) continue;
+                    Frag u[3];
+                    get_frag(U, tile, step, u);
+                    dp[tile] = multiply<PE, 3>(o, u, dp[tile]);
+                    da[tile] = multiply<3, 3>(v, u, da[tile]);
+                }
+                if (!has_keys) continue;
+                Frag of_s[kTiles][3], of_d[kTiles][3];
+#pragma unroll
+                for (int tile = 0; tile < kTiles; ++tile) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dot_states = fmaf(s[tile][step][e], d[tile][step][e], dot_states);
+                    split(reinterpret_cast<const float *>(&s[tile][step]), of_s[tile]);
+                    split(reinterpret_cast<const float *>(&d[tile][step]), of_d[tile]);
+                }
+#pragma unroll
+                for (int row = 0; row < 4; ++row) {
+                    __builtin_amdgcn_sched_barrier(0); // (loads of all rows at once would not fit the registers)
+                    Frag u[3];
+                    get_frag(O, row, step, o);
+                    get_frag(V, row, step, v);
+                    get_frag(U, row, step, u);
+#pragma unroll
+                    for (int tile = 0; tile < kTiles; ++tile) {
+                        far_q[tile][row] = multiply<PE, 3>(o, of_s[tile], far_q[tile][row]);
+                        far_k[tile][row] = multiply<3, 3>(v, of_s[tile], far_k[tile][row]);
+                        end[tile][row] = multiply<3, 3>(u, of_d[tile], end[tile][row]);
+                    }
+                }
             }
-            for (int r = 0; r < 4; ++r) {
-                const int i = mine(group * 4 + r);
-                dot[r] = fmaf(Q[i * LD + d], dq[tile][r], fmaf(K[i * LD + d], plus[tile][r] - minus[tile][r], dot[r]));
-                sum_q[tile][r] += dq[tile][r];
-                sum_k[tile][r] += plus[tile][r] + minus[tile][r];
-            }
+            __syncthreads();
         }
-        for (int r = 0; r < 4; ++r) {
-            const float v = row_sum(dot[r]);
-            if (at == 0) dG[mine(group * 4 + r)] = v;
+        // what goes from step j to step i, and the row and column sums of F
+        Acc dm[4];
+        {
+            Acc kk[4] = {}, qk[4] = {};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                __builtin_amdgcn_sched_barrier(0);
+                Frag k[PE], q[PE];
+#pragma unroll
+                for (int n = 0; n < PE; ++n) k[n] = K[frag_at(wave, s, n, KS, PE)], q[n] = Q[frag_at(wave, s, n, KS, PE)];
+#pragma unroll
+                for (int tile = 0; tile < 4; ++tile) {
+                    if (tile > wave) continue;
+                    Frag other[PE];
+#pragma unroll
+                    for (int n = 0; n < PE; ++n) other[n] = K[frag_at(tile, s, n, KS, PE)];
+                    kk[tile] = multiply<PE, PE, kOrder>(k, other, kk[tile]);
+                    qk[tile] = multiply<PE, PE, kOrder>(q, other, qk[tile]);
+                }
+            }
+            float row_flow[4] = {};
+            bool fine = true;
+            unsigned long long before[4];              // steps that hand something to the lane's rows
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = wave * 16 + group * 4 + r;
+                before[r] = bit_of(alive, i) ? upto(starts, i) & alive : 0;
+            }
+#pragma unroll
+            for (int tile = 0; tile < 4; ++tile) {
+                const int j = tile * 16 + at;
+                Acc dn;
+                float column = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = wave * 16 + group * 4 + r;
+                    const bool on = tile <= wave && bit_of(before[r], j), below = on && j < i;
+                    const float e = decay_of(gates.G[i] - gates.G[j]), n = p.scale * e * dp[tile][r], m = -e * da[tile][r];
+                    dn[r] = on ? n : 0.0f;
+                    dm[tile][r] = below ? m : 0.0f;
+                    const float f = (on ? n * qk[tile][r] : 0.0f) + (below ? m * kk[tile][r] : 0.0f);
+                    row_flow[r] += f;
+                    column += f;
+                }
+                fine = fine && all_finite(dn) && all_finite(dm[tile]);
+                Four planes[3];
+                split(dn, planes);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) {
+                    *reinterpret_cast<Four *>(&dNT[n][j][wave * 16 + group * 4]) = planes[n];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) dN[n][wave * 16 + group * 4 + r][j] = planes[n][r];
+                }
+                column += __shfl_xor(column, 16);
+                column += __shfl_xor(column, 32);
+                if (group == 0) columns_of[wave][j] = column;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float v = row_sum(row_flow[r]);
+                if (at == 0) flow[wave * 16 + group * 4 + r] = v;
+            }
+            if (!fine) not_finite = 1;
+        }
+        {
+            dot_beta += __shfl_xor(dot_beta, 1);
+            dot_beta += __shfl_xor(dot_beta, 2);
+            if (threadIdx.x % 4 == 0) dbeta[threadIdx.x / 4] = dot_beta;
+        }
+        // the parts that come from and go to other chunks
+        float at_end = 0.0f;
+#pragma unroll
+        for (int row = 0; row < 4; ++row) {
+            __builtin_amdgcn_sched_barrier(0);
+            float dot[4] = {};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = row * 16 + group * 4 + r;
+                const int64_t step = b * p.T + min(chunk * kSteps + i, p.T - 1);
+                const bool live = bit_of(alive, i);
+                const float f = live ? gates.f[i] : 0.0f, t = live ? gates.t[i] : 0.0f;
+#pragma unroll
+                for (int tile = 0; tile < kTiles; ++tile) {
+                    if (!has_keys) continue;
+                    const int d = (wave * kTiles + tile) * 16 + at, from = hk * p.Dk + min(d, p.Dk - 1);
+                    const float k = to_f32(static_cast<const E *>(p.k)[step * p.ld_k + from]), q = to_f32(static_cast<const E *>(p.q)[step * p.ld_q + from]);
+                    const bool key = d < p.Dk;
+                    const float fq = p.scale * f * far_q[tile][row][r], fk = -f * far_k[tile][row][r], e = t * end[tile][row][r];
+                    const float to_later = t != 0.0f && key ? k * e : 0.0f;
+                    at_end += to_later;
+                    dot[r] += (f != 0.0f && key ? fmaf(q, fq, k * fk) : 0.0f) - to_later;
+                    sum_q[tile][row][r] += f != 0.0f ? fq : 0.0f;
+                    sum_k[tile][row][r] += (f != 0.0f ? fk : 0.0f) + (t != 0.0f ? e : 0.0f);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float v = row_sum(dot[r]);
+                if (at == 0) rows_of[wave][row * 16 + group * 4 + r] = v;
+            }
         }
         const float whole = gates.f[kSteps - 1];
-        if (whole != 0.0f) {
-            float v = 0.0f;
-            for (int e = threadIdx.x; e < p.Dk * p.Dv; e += kDeltaThreads) v = fmaf(D[e], S[e], v);
-            at_end = fmaf(whole, v, at_end);
-        }
+        if (whole != 0.0f) at_end = fmaf(whole, dot_states, at_end);
         for (int d = 1; d < kWave; d *= 2) at_end += __shfl_xor(at_end, d);
         if (lane == 0) extra[wave] = at_end;
         __syncthreads();
+        const bool bad = gates.bad || not_finite;
+        auto key_products = [&](const Plane *a, const Frag *keys, Acc (&sum)[kTiles][4], int which) {
+            if (!has_keys) return;
+#pragma unroll
+            for (int row = 0; row < 4; ++row) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (bad) {
+                    unsigned long long pass[4];
+                    int hidden = group;                // (the masks are formed here, not kept ready)
+                    asm volatile("" : "+v"(hidden));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int i = row * 16 + hidden * 4 + r;
+                        pass[r] = !bit_of(alive, i) ? 0 : (which == 0 ? upto(starts, i) : which == 1 ? from(starts, i) : upto(starts, i) | from(starts, i)) & alive;
+                    }
+#pragma unroll
+                    for (int tile = 0; tile < kTiles; ++tile) sum[tile][row] = careful_rows<PE>(sum[tile][row], a, row, keys, wave * kTiles + tile, pass);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        if (which == 0 ? s * 32 > row * 16 + 15 : which == 1 ? s * 32 + 31 < row * 16 : false) continue;       // zeros
+                        Frag of_a[3];
+                        get_frag(a, row, s, of_a);
+#pragma unroll
+                        for (int tile = 0; tile < kTiles; ++tile) {
+                            Frag key[PE];
+#pragma unroll
+                            for (int n = 0; n < PE; ++n) key[n] = keys[frag_at(wave * kTiles + tile, s, n, 2, PE)];
+                            sum[tile][row] = multiply<3, PE>(of_a, key, sum[tile][row]);
+                        }
+                    }
+                }
+            }
+        };
+        key_products(dN, KT, sum_q, 0);
+        key_products(dNT, QT, sum_k, 1);
         if (wave == 0) {
             const int i = lane, t = chunk * kSteps + i, part = part_of(starts, i);
-            float v = dG[i];
+            float v = flow[i] - ((columns_of[0][i] + columns_of[1][i]) + (columns_of[2][i] + columns_of[3][i]));
+            v += (rows_of[0][i] + rows_of[1][i]) + (rows_of[2][i] + rows_of[3][i]);
             if (i == kSteps - 1) v += (extra[0] + extra[1]) + (extra[2] + extra[3]);
             double s = v;
             for (int d = 1; d < kWave; d *= 2) {
@@ -445,16 +635,63 @@ __global__ __launch_bounds__(kDeltaThreads) void chunk_grad_kernel(DeltaArgs p)
                 p.grad_beta[to] = bit_of(alive, i) ? dbeta[i] : 0.0f;
             }
         }
-    }
+        __syncthreads();
+        // X takes the room of dN
 #pragma unroll
-    for (int tile = 0; tile < kTiles; ++tile)
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r, t = chunk * kSteps + i, d = tile * 16 + at;
-            if (t >= p.T || d >= p.Dk) continue;
-            const bool live = bit_of(gates.live, i);
-            const_cast<E *>(row_at<E>(p.grad_q, p.ld_gq, b, p.T, t, hk, p.Dk))[d] = from_f32<E>(live ? sum_q[tile][r] : 0.0f);
-            const_cast<E *>(row_at<E>(p.grad_k, p.ld_gk, b, p.T, t, hk, p.Dk))[d] = from_f32<E>(live ? sum_k[tile][r] : 0.0f);
+        for (int tile = 0; tile < 4; ++tile) {
+            if (tile > wave) continue;
+            Four planes[3];
+            split(dm[tile], planes);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) {
+                const int j = tile * 16 + at;
+                if (tile < wave) *reinterpret_cast<Four *>(&X[n][j][wave * 16 + group * 4]) = planes[n];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int i = wave * 16 + group * 4 + r;
+                    if (tile < wave) {
+                        X[n][i][j] = planes[n][r];
+                    } else if (j <= i) {               // 0 where j = i
+                        X[n][i][j] = planes[n][r];
+                        X[n][j][i] = planes[n][r];
+                    }
+                }
+            }
         }
+        __syncthreads();
+        key_products(X, KT, sum_k, 2);
+    }
+    // rows of the results through shared memory
+    typedef E Row[DK + 8];
+    Row *rows = reinterpret_cast<Row *>(lds);
+    typedef E Vec __attribute__((ext_vector_type(8)));
+    typedef Vec Loose __attribute__((aligned(sizeof(E))));
+    auto put = [&](Acc (&sum)[kTiles][4], void *to, int64_t ld) {
+        __syncthreads();
+        if (has_keys)
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                for (int row = 0; row < 4; ++row)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int i = row * 16 + group * 4 + r;
+                        rows[i][(wave * kTiles + tile) * 16 + at] = from_f32<E>(bit_of(alive, i) ? sum[tile][row][r] : 0.0f);
+                    }
+        __syncthreads();
+        for (int e = threadIdx.x; e < kSteps * (DK / 8); e += kDeltaThreads) {
+            const int i = e / (DK / 8), d = e % (DK / 8) * 8, t = chunk * kSteps + i;
+            if (t >= p.T || d >= p.Dk) continue;
+            E *out = const_cast<E *>(row_at<E>(to, ld, b, p.T, t, hk, p.Dk)) + d;
+            if (d + 8 <= p.Dk) {
+                *reinterpret_cast<Loose *>(out) = *reinterpret_cast<const Vec *>(&rows[i][d]);
+            } else {
+                for (int c = 0; d + c < p.Dk; ++c) out[c] = rows[i][d + c];
+            }
+        }
+    };
+    put(sum_q, p.grad_q, p.ld_gq);
+    put(sum_k, p.grad_k, p.ld_gk);
 }
 
 template <typename E, int DK, int NT>
@@ -471,7 +708,7 @@ int run(const DeltaArgs &p, hipStream_t stream)
 {
     const int rc = (int64_t)p.B * p.Hv * ((p.Dv + 31) / 32) >= 256 ? run_back<E, DK, 2>(p, stream) : run_back<E, DK, 1>(p, stream);
     if (rc || p.chunks == 0) return rc;
-    const size_t lds = (size_t)(2 * kSteps * (DK + 1) + 2 * kSteps * (kSteps + 1)) * sizeof(float);
+    const size_t lds = (6 + kExact<E>) * sizeof(Plane);            // (the results' rows, 64 of DK + 8, are less)
     if (const int failed = make_room_for(reinterpret_cast<const void *>(chunk_grad_kernel<E, DK>), lds)) return failed;
     hipLaunchKernelGGL((chunk_grad_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
     return launched("delta scan gradient");

@@ -118,10 +118,11 @@ Room room_of(int dtype, const DeltaArgs &p, bool keep)
         r.QT = take(keys);
         r.NT = take(square);
         r.PT = take(square);
-        r.S = take(records * p.Dk * p.Dv * f);
-        r.M = take(records * kSteps * p.Dv * f);
-        r.D = take(records * p.Dk * p.Dv * f);
-        r.Y = take(records * kSteps * p.Dv * f);
+        const size_t state = records * padded_keys(p.Dk) * padded_values(p.Dv) * f, steps = records * kSteps * padded_values(p.Dv) * f;
+        r.S = take(state);
+        r.M = take(steps);
+        r.D = take(state);
+        r.Y = take(steps);
     }
     r.all = at;
     return r;
@@ -151,7 +152,7 @@ int sizes_check(int dtype, int B, int T, int Hk, int Hv, int Dk, int Dv)
     if (const int rc = heads_check(dtype, Hk, Hv, Dk, Dv)) return rc;
     if (B < 0 || T < 0 || (int64_t)B * Hv >= (1 << 24) || (int64_t)B * T >= (1 << 30)) return MARL_ERR_BAD_DIM;
     // grids: a workgroup per record, and one per head and sixteen columns
-    if ((int64_t)B * Hv * ((T + kSteps - 1) / kSteps) >= kMostRow || (int64_t)B * Hv * ((Dv + 15) / 16) >= kMostRow) return MARL_ERR_BAD_DIM;
+    if ((int64_t)B * Hv * ((T + kSteps - 1) / kSteps) >= kMostRow || (int64_t)B * Hv * (padded_values(Dv) / 16) >= kMostRow - 8) return MARL_ERR_BAD_DIM;
     return MARL_OK;
 }
 bool row_fits(int64_t ld, int H, int D) { return ld >= (int64_t)H * D && ld < kMostRow; }

@@ -79,7 +79,7 @@ struct KeyRows {
     // wave w writes its rows, and every fourth tile of the transposed matrix
     __device__ __forceinline__ void write(Frag *rows, Frag *turned) const
     {
-        const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+        const int lane = threadIdx.x % kWave, wave = wave_index();
 #pragma unroll
         for (int s = 0; s < DK / 32; ++s) {
             Frag f[PE];
@@ -104,7 +104,7 @@ struct KeyRows {
 template <int PLANES, bool TURNED>
 __device__ __forceinline__ void write_square(const float *from, int ld, Frag *to)
 {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, row = wave * 16 + lane % 16;
+    const int lane = threadIdx.x % kWave, wave = wave_index(), row = wave * 16 + lane % 16;
     for (int s = 0; s < 2; ++s) {
         if (TURNED ? s * 32 + 31 < wave * 16 : s * 32 > wave * 16 + 15) continue;  // on the other side of the diagonal
         float v[8];
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kDeltaThreads) void chunk_kernel(DeltaArgs p)
     __shared__ int bad_rows, bad;
     const int chunk = (int)(blockIdx.x % p.chunks), hk = (int)(blockIdx.x / p.chunks % p.Hk);
     const int64_t b = blockIdx.x / p.chunks / p.Hk;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, at = lane % 16, group = lane / 16;
+    const int lane = threadIdx.x % kWave, wave = wave_index(), at = lane % 16, group = lane / 16;
     if (threadIdx.x == 0) bad_rows = 0;
     unsigned long long live;
     {
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
     StatePlane *S = reinterpret_cast<StatePlane *>(lds);                           // [3], columns of the state
     StepPlane *R = reinterpret_cast<StepPlane *>(lds + 3 * sizeof(StatePlane)), *U = R + 3, *Ue = U + PF;      // [3], [PF], [3]
     __shared__ int not_finite[2];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, at = lane % 16, group = lane / 16;
+    const int lane = threadIdx.x % kWave, wave = wave_index(), at = lane % 16, group = lane / 16;
     const Place place = place_of((int64_t)p.B * p.Hv, p.Dv, C);
     if (place.head < 0) return;                        // the whole workgroup
     const int64_t head = place.head, b = head / p.Hv;
@@ -309,6 +309,18 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
             if (t < p.T) read_columns<E, NT>(row_at<E>(p.v, p.ld_v, b, p.T, t, h, p.Dv), col, p.Dv, v[r]);
         }
     };
+    const int DV = padded_values(p.Dv);
+    auto keep_state = [&](float *to) {
+#pragma unroll
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float v[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) v[n] = state[tile][n][r];
+                write_columns<float, NT>(to + ((wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
+            }
+    };
     auto state_out = [&](float *to) {                  // [Dk,Dv]
 #pragma unroll
         for (int tile = 0; tile < kTiles; ++tile)
@@ -347,7 +359,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
         const unsigned long long starts = g.starts, live = g.live;
         const float whole = g.f[kSteps - 1];
         const bool bad = g.bad != 0;
-        if (p.S && has_state) state_out(p.S + record * p.Dk * p.Dv);
+        if (p.S && has_state) keep_state(p.S + record * DK * DV);
         Frag nn[2][3], pp[2][PF], kt[kTiles][2][PE];
         const Frag *N = p.N + record * square_frags(3), *P = p.P + record * square_frags(PF);
         const Frag *KT = p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE);
@@ -407,7 +419,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
                     const int i = wave * 16 + group * 4 + r;
                     pass[r] = bit_of(live, i) ? upto(starts, i) & live & ~(1ull << i) : 0;
                 }
-                m[n] = careful_multiply(m[n], N, wave, 3, R[0][n * 16 + at], 3, C * LU, pass);
+                m[n] = careful_multiply<3, 3>(m[n], N, wave, R[0][n * 16 + at], C * LU, pass);
             } else {
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
@@ -435,7 +447,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
                 float x[NT];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) x[n] = m[n][r];
-                write_columns<float, NT>(p.M + (record * kSteps + wave * 16 + group * 4 + r) * p.Dv, col, p.Dv, x);
+                write_columns<float, NT>(p.M + (record * kSteps + wave * 16 + group * 4 + r) * DV, col, DV, x);
             }
         if (chunk + 1 < p.chunks) load_start(chunk + 1);
         __syncthreads();
@@ -452,7 +464,7 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
                     const int i = wave * 16 + group * 4 + r;
                     pass[r] = bit_of(live, i) ? upto(starts, i) & live : 0;
                 }
-                o[n] = careful_multiply(o[n], P, wave, PF, U[0][n * 16 + at], PF, C * LU, pass);
+                o[n] = careful_multiply<PF, PF>(o[n], P, wave, U[0][n * 16 + at], C * LU, pass);
             } else {
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
@@ -475,9 +487,11 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
             if (careful_u) {
                 unsigned long long pass[4];
                 for (int r = 0; r < 4; ++r) pass[r] = upto(starts, kSteps - 1) & live;
+#pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        state[tile][n] = careful_multiply(state[tile][n], KT, wave * kTiles + tile, PE, Ue[0][n * 16 + at], 3, C * LU, pass);
+                        state[tile][n] = careful_multiply<PE, 3>(state[tile][n], KT, wave * kTiles + tile, Ue[0][n * 16 + at], C * LU, pass);
             } else {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
