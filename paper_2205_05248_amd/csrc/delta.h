@@ -35,10 +35,11 @@ template <typename E> constexpr int kFine = sizeof(E) == 4 ? 3 : 2;
 
 struct ChunkGates {
     double G[kSteps];
-    float f[kSteps], t[kSteps], beta[kSteps];
-    unsigned long long starts, live;                   // bit i: step i starts a sequence; is none of the padding
+    float f[kSteps], t[kSteps], beta[kSteps];          // t: -1 in padding
+    float whole;                                       // f of the last step
     int bad;                                           // the rows of K or Q, N or P hold an infinity or NaN
-    int pad[27];
+    unsigned long long starts, live;                   // bit i: step i starts a sequence; is none of the padding
+    int pad[26];
 };
 static_assert(sizeof(ChunkGates) % 128 == 0, "records begin at lines");
 
@@ -207,6 +208,15 @@ __device__ __forceinline__ void write_columns(E *row, int col, int D, const floa
         for (int n = 0; n < NT; ++n)
             if (col + n < D) row[col + n] = from_f32<E>(from[n]);
     }
+}
+
+// A 0 that the compiler does not know.  Added to an address that is the same for all lanes it keeps the load off the scalar unit, where a load
+// still under way delays every access to shared memory.
+__device__ __forceinline__ int hidden_zero()
+{
+    int zero;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(zero));
+    return zero;
 }
 
 __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }

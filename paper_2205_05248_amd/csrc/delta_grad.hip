@@ -9,13 +9,30 @@
 namespace marl {
 namespace {
 
-// The chunks of one head from the last to the first, for 16 NT value columns as in the forward pass: D, Y and the gradient of v.  Wave w has
-// rows 16 w on of the chunk, and rows w DK / 4 on of the adjoint, which stays in its accumulators.
+// What a chunk needs from memory on the way back.
 template <typename E, int DK, int NT>
-__global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2 : 1) void back_kernel(DeltaArgs p)
+struct BackLoads {
+    static constexpr int PE = kExact<E>, KS = DK / 32, kTiles = (DK + 63) / 64;
+    Frag k[KS][PE], n[2][3], p[2][3], kt[kTiles][2][PE], qt[kTiles][2][PE];
+    Acc f, t, beta;
+    float whole;
+    int bad;
+};
+// The upstream gradient of a chunk, and what scales it.
+template <int NT>
+struct Upstream {
+    float o[4][NT];
+    Acc f, t;
+};
+
+// The chunks of one head from the last to the first, for 16 NT value columns as in the forward pass: D, Y and the gradient of v.  Wave w has
+// rows 16 w on of the chunk, and rows w DK / 4 on of the adjoint, which stays in its accumulators.  AHEAD as in the forward pass.
+template <typename E, int DK, int NT, bool AHEAD>
+__global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
 {
+    typedef BackLoads<E, DK, NT> Loads;
     constexpr int PE = kExact<E>, KS = DK / 32, LS = DK + 8, LU = kSteps + 8, C = 16 * NT;
-    constexpr int kTiles = (DK + 63) / 64;
+    constexpr int kTiles = Loads::kTiles;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef __bf16 StatePlane[C][LS];
     typedef __bf16 StepPlane[C][LU];
@@ -23,11 +40,11 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
     // the upstream gradient of this chunk and of the next: [PE] as it is, [3] scaled by what of it reaches the state before
     StepPlane *upstream = reinterpret_cast<StepPlane *>(lds + 3 * sizeof(StatePlane)), *R = upstream + 2 * (PE + 3), *V = R + 3;      // [3], [3]
     __shared__ int not_finite[4];                      // upstream of even and odd chunks, beta dU, dV
-    const int lane = threadIdx.x % kWave, wave = wave_index(), at = lane % 16, group = lane / 16;
+    const int lane = threadIdx.x % kWave, wave = wave_index(), at = lane % 16, group = lane / 16, zero = hidden_zero();
     const Place place = place_of((int64_t)p.B * p.Hv, p.Dv, C);
     if (place.head < 0) return;                        // the whole workgroup
     const int64_t head = place.head, b = head / p.Hv;
-    const int col = place.first + at * NT, h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk);
+    const int col = place.first + at * NT, h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk), DV = padded_values(p.Dv);
     const int64_t key_head = b * p.Hk + hk;
     const bool has_state = wave * kTiles * 16 < DK;
     Acc adj[kTiles][NT] = {};
@@ -42,50 +59,49 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
 #pragma unroll
                 for (int n = 0; n < NT; ++n) adj[tile][n][r] = v[n];
             }
-    Frag k[KS][PE];
-    float go[4][NT];
-    Acc f_next, t_next, beta_next;
-    auto load_start = [&](int chunk) {
-        const Frag *K = p.K + (key_head * p.chunks + chunk) * key_frags(DK, PE);
+    auto load = [&](Loads &x, int chunk) {
+        const int64_t record = head * p.chunks + chunk, key_record = key_head * p.chunks + chunk;
+        const Frag *K = p.K + key_record * key_frags(DK, PE), *KT = p.KT + key_record * key_frags(DK, PE), *QT = p.QT + key_record * key_frags(DK, PE);
+        const Frag *N = p.NT + record * square_frags(3), *P = p.PT + record * square_frags(3);
+        const ChunkGates &g = p.gates[record];
+        x.f = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
+        x.t = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
+        x.beta = *reinterpret_cast<const Acc *>(g.beta + wave * 16 + group * 4);
+        x.whole = (&g.whole)[zero];
+        x.bad = (&g.bad)[zero];
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int n = 0; n < PE; ++n) k[s][n] = K[frag_at(wave, s, n, KS, PE)];
+            for (int n = 0; n < PE; ++n) x.k[s][n] = K[frag_at(wave, s, n, KS, PE)];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s * 32 + 31 < wave * 16) continue;     // zeros
+#pragma unroll
+            for (int n = 0; n < 3; ++n) {
+                x.p[s][n] = P[frag_at(wave, s, n, 2, 3)];
+                x.n[s][n] = N[frag_at(wave, s, n, 2, 3)];
+            }
+        }
+        if (has_state)
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int n = 0; n < PE; ++n) {
+                        x.kt[tile][s][n] = KT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
+                        x.qt[tile][s][n] = QT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
+                    }
+    };
+    auto load_upstream = [&](Upstream<NT> &x, int chunk) {
         const ChunkGates &g = p.gates[head * p.chunks + chunk];
-        f_next = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
-        t_next = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
-        beta_next = *reinterpret_cast<const Acc *>(g.beta + wave * 16 + group * 4);
+        x.f = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
+        x.t = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int t = chunk * kSteps + wave * 16 + group * 4 + r;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) go[r][n] = 0.0f;
-            if (t < p.T) read_columns<E, NT>(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), col, p.Dv, go[r]);
+            const int t = min(chunk * kSteps + wave * 16 + group * 4 + r, p.T - 1);
+            read_columns<E, NT>(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), col, p.Dv, x.o[r]);
         }
-    };
-    const int DV = padded_values(p.Dv);
-    auto keep_adjoint = [&](float *to) {
-#pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float v[NT];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) v[n] = adj[tile][n][r];
-                write_columns<float, NT>(to + ((wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
-            }
-    };
-    auto adjoint_out = [&](float *to) {                // [Dk,Dv]
-#pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = (wave * kTiles + tile) * 16 + group * 4 + r;
-                float v[NT];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) v[n] = adj[tile][n][r];
-                if (d < p.Dk) write_columns<float, NT>(to + (int64_t)d * p.Dv, col, p.Dv, v);
-            }
     };
     auto share_adjoint = [&] {
 #pragma unroll
@@ -103,16 +119,15 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
 #pragma unroll
         for (int m = 0; m < PLANES; ++m) *reinterpret_cast<Four *>(&to[m][n * 16 + at][wave * 16 + group * 4]) = planes[m];
     };
-    auto share_upstream = [&](int chunk) {
-        const unsigned long long live = p.gates[head * p.chunks + chunk].live;
+    auto share_upstream = [&](const Upstream<NT> &x, int chunk) {
         StepPlane *O = upstream + chunk % 2 * (PE + 3), *Of = O + PE;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             Acc o, of;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                o[r] = bit_of(live, wave * 16 + group * 4 + r) ? go[r][n] : 0.0f;
-                of[r] = f_next[r] == 0.0f ? 0.0f : p.scale * f_next[r] * o[r];
+                o[r] = x.t[r] < 0.0f ? 0.0f : x.o[r][n];
+                of[r] = x.f[r] == 0.0f ? 0.0f : p.scale * x.f[r] * o[r];
             }
             Four exact[PE], planes[3];
             split(o, exact);
@@ -122,38 +137,30 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
             if (!all_finite(o)) not_finite[chunk % 2] = 1;
         }
     };
-    if (threadIdx.x < 4) not_finite[threadIdx.x] = 0;
-    __syncthreads();
-    if (p.chunks > 0) {
-        load_start(p.chunks - 1);
-        share_upstream(p.chunks - 1);
-    }
-    if (has_state) share_adjoint();
-    __syncthreads();
-    for (int chunk = p.chunks - 1; chunk >= 0; --chunk) {
+    auto step = [&](int chunk, Loads &x, Loads &next) {
         const int64_t record = head * p.chunks + chunk;
-        const ChunkGates &g = p.gates[record];
-        const unsigned long long starts = g.starts, live = g.live;
-        const float whole = g.f[kSteps - 1];
-        const bool bad = g.bad != 0, careful_o = bad || not_finite[chunk % 2];
+        Upstream<NT> up;
+        if (!AHEAD) load(x, chunk);
+        if (chunk > 0) {
+            load_upstream(up, chunk - 1);
+            if (AHEAD) load(next, chunk - 1);
+        }
+        const Acc f = x.f, t = x.t, beta = x.beta;
         const StepPlane *O = upstream + chunk % 2 * (PE + 3), *Of = O + PE;
+        const bool bad = __builtin_amdgcn_readfirstlane(x.bad) != 0, careful_o = bad || not_finite[chunk % 2];
         // flags are taken back where all have read them and none sets them before the next barrier
         if (threadIdx.x == 0) not_finite[(chunk + 1) % 2] = not_finite[3] = 0;
-        if (has_state) keep_adjoint(p.D + record * DK * DV);
-        Frag nn[2][3], pp[2][3], kt[kTiles][2][PE], qt[kTiles][2][PE];
-        const Frag *N = p.NT + record * square_frags(3), *P = p.PT + record * square_frags(3);
-        const Frag *KT = p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE), *QT = p.QT + (key_head * p.chunks + chunk) * key_frags(DK, PE);
+        if (has_state)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (s * 32 + 31 < wave * 16) continue;     // zeros
+            for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
-            for (int n = 0; n < 3; ++n) {
-                pp[s][n] = P[frag_at(wave, s, n, 2, 3)];
-                nn[s][n] = N[frag_at(wave, s, n, 2, 3)];
-            }
-        }
+                for (int r = 0; r < 4; ++r) {
+                    float v[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) v[n] = adj[tile][n][r];
+                    write_columns<float, NT>(p.D + (record * DK + (wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
+                }
         // dU = P' dO + t K D
-        const Acc f = f_next, t = t_next, beta = beta_next;
         Acc y[NT] = {};
 #pragma unroll
         for (int s = 0; s < KS; ++s)
@@ -162,29 +169,37 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
                 Frag of_state[3];
 #pragma unroll
                 for (int m = 0; m < 3; ++m) of_state[m] = *reinterpret_cast<const Frag *>(&S[m][n * 16 + at][s * 32 + group * 8]);
-                y[n] = multiply<PE, 3>(k[s], of_state, y[n]);
+                y[n] = multiply<PE, 3>(x.k[s], of_state, y[n]);
             }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[n][r] = t[r] == 0.0f || !bit_of(live, wave * 16 + group * 4 + r) ? 0.0f : t[r] * y[n][r];
-            if (careful_o) {
-                unsigned long long pass[4];
-                for (int r = 0; r < 4; ++r) {
-                    const int i = wave * 16 + group * 4 + r;
-                    pass[r] = bit_of(live, i) ? from(starts, i) & live : 0;
-                }
-                y[n] = careful_multiply<3, PE>(y[n], P, wave, O[0][n * 16 + at], C * LU, pass);
-            } else {
+            for (int r = 0; r < 4; ++r) y[n][r] = t[r] > 0.0f || t[r] != t[r] ? t[r] * y[n][r] : 0.0f;
+        if (careful_o) {
+            const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
+            unsigned long long pass[4];
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    if (s * 32 + 31 < wave * 16) continue;
+            for (int r = 0; r < 4; ++r) {
+                const int i = wave * 16 + group * 4 + r;
+                pass[r] = bit_of(live, i) ? from(starts, i) & live : 0;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) y[n] = careful_multiply<3, PE>(y[n], p.PT + record * square_frags(3), wave, O[0][n * 16 + at], C * LU, pass);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (s * 32 + 31 < wave * 16) continue;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
                     Frag of_o[PE];
 #pragma unroll
-                    for (int x = 0; x < PE; ++x) of_o[x] = *reinterpret_cast<const Frag *>(&O[x][n * 16 + at][s * 32 + group * 8]);
-                    y[n] = multiply<3, PE>(pp[s], of_o, y[n]);
+                    for (int c = 0; c < PE; ++c) of_o[c] = *reinterpret_cast<const Frag *>(&O[c][n * 16 + at][s * 32 + group * 8]);
+                    y[n] = multiply<3, PE>(x.p[s], of_o, y[n]);
                 }
             }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
             const Acc minus = -(beta * y[n]);
             Four planes[3];
             split(minus, planes);
@@ -193,42 +208,37 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
         }
         __syncthreads();
         // Y = dU - N' (beta dU), dV = beta Y
-        if (has_state)
+        if (bad || not_finite[2]) {
+            const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
+            unsigned long long pass[4];
 #pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile)
+            for (int r = 0; r < 4; ++r) {
+                const int i = wave * 16 + group * 4 + r;
+                pass[r] = bit_of(live, i) ? from(starts, i) & live & ~(1ull << i) : 0;
+            }
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+            for (int n = 0; n < NT; ++n) y[n] = careful_multiply<3, 3>(y[n], p.NT + record * square_frags(3), wave, R[0][n * 16 + at], C * LU, pass);
+        } else {
 #pragma unroll
-                    for (int n = 0; n < PE; ++n) {
-                        kt[tile][s][n] = KT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
-                        qt[tile][s][n] = QT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
-                    }
-        const bool careful_n = bad || not_finite[2];
+            for (int s = 0; s < 2; ++s) {
+                if (s * 32 + 31 < wave * 16) continue;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    Frag of_r[3];
+#pragma unroll
+                    for (int c = 0; c < 3; ++c) of_r[c] = *reinterpret_cast<const Frag *>(&R[c][n * 16 + at][s * 32 + group * 8]);
+                    y[n] = multiply<3, 3>(x.n[s], of_r, y[n]);
+                }
+            }
+        }
         Acc v[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            if (careful_n) {
-                unsigned long long pass[4];
-                for (int r = 0; r < 4; ++r) {
-                    const int i = wave * 16 + group * 4 + r;
-                    pass[r] = bit_of(live, i) ? from(starts, i) & live & ~(1ull << i) : 0;
-                }
-                y[n] = careful_multiply<3, 3>(y[n], N, wave, R[0][n * 16 + at], C * LU, pass);
-            } else {
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    if (s * 32 + 31 < wave * 16) continue;
-                    Frag of_r[3];
-#pragma unroll
-                    for (int x = 0; x < 3; ++x) of_r[x] = *reinterpret_cast<const Frag *>(&R[x][n * 16 + at][s * 32 + group * 8]);
-                    y[n] = multiply<3, 3>(nn[s], of_r, y[n]);
-                }
-            }
             Acc back;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (!bit_of(live, wave * 16 + group * 4 + r)) y[n][r] = 0.0f;
-                v[n][r] = beta[r] * y[n][r];
+                y[n][r] = t[r] < 0.0f ? 0.0f : y[n][r];
+                v[n][r] = t[r] < 0.0f ? 0.0f : beta[r] * y[n][r];
                 back[r] = f[r] == 0.0f ? 0.0f : -f[r] * v[n][r];
             }
             Four planes[3];
@@ -236,7 +246,6 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
             share_steps(V, planes, n);
             if (!all_finite(v[n])) not_finite[3] = 1;
         }
-        if (chunk > 0) load_start(chunk - 1);
         __syncthreads();
         // D <- f_63 D + (scale f Q)' dO - (f K)' dV
         if (has_state) {
@@ -245,16 +254,19 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) adj[tile][n][r] = whole == 0.0f ? 0.0f : whole * adj[tile][n][r];
+                    for (int r = 0; r < 4; ++r) adj[tile][n][r] = x.whole == 0.0f ? 0.0f : x.whole * adj[tile][n][r];
             if (careful_o || not_finite[3]) {
+                const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
+                const int64_t key_record = key_head * p.chunks + chunk;
                 unsigned long long pass[4];
+#pragma unroll
                 for (int r = 0; r < 4; ++r) pass[r] = (starts ? (starts & -starts) - 1 : ~0ull) & live;
 #pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        adj[tile][n] = careful_multiply<PE, 3>(adj[tile][n], QT, wave * kTiles + tile, Of[0][n * 16 + at], C * LU, pass);
-                        adj[tile][n] = careful_multiply<PE, 3>(adj[tile][n], KT, wave * kTiles + tile, V[0][n * 16 + at], C * LU, pass);
+                        adj[tile][n] = careful_multiply<PE, 3>(adj[tile][n], p.QT + key_record * key_frags(DK, PE), wave * kTiles + tile, Of[0][n * 16 + at], C * LU, pass);
+                        adj[tile][n] = careful_multiply<PE, 3>(adj[tile][n], p.KT + key_record * key_frags(DK, PE), wave * kTiles + tile, V[0][n * 16 + at], C * LU, pass);
                     }
             } else {
 #pragma unroll
@@ -263,33 +275,58 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
                     for (int n = 0; n < NT; ++n) {
                         Frag of_o[3], of_v[3];
 #pragma unroll
-                        for (int x = 0; x < 3; ++x) {
-                            of_o[x] = *reinterpret_cast<const Frag *>(&Of[x][n * 16 + at][s * 32 + group * 8]);
-                            of_v[x] = *reinterpret_cast<const Frag *>(&V[x][n * 16 + at][s * 32 + group * 8]);
+                        for (int c = 0; c < 3; ++c) {
+                            of_o[c] = *reinterpret_cast<const Frag *>(&Of[c][n * 16 + at][s * 32 + group * 8]);
+                            of_v[c] = *reinterpret_cast<const Frag *>(&V[c][n * 16 + at][s * 32 + group * 8]);
                         }
 #pragma unroll
                         for (int tile = 0; tile < kTiles; ++tile) {
-                            adj[tile][n] = multiply<PE, 3>(qt[tile][s], of_o, adj[tile][n]);
-                            adj[tile][n] = multiply<PE, 3>(kt[tile][s], of_v, adj[tile][n]);
+                            adj[tile][n] = multiply<PE, 3>(x.qt[tile][s], of_o, adj[tile][n]);
+                            adj[tile][n] = multiply<PE, 3>(x.kt[tile][s], of_v, adj[tile][n]);
                         }
                     }
             }
             share_adjoint();
         }
+        if (chunk > 0) share_upstream(up, chunk - 1);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = wave * 16 + group * 4 + r, step = chunk * kSteps + i;
-            float x[NT], z[NT];
+            float c[NT], z[NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) x[n] = y[n][r], z[n] = bit_of(live, i) ? v[n][r] : 0.0f;
-            write_columns<float, NT>(p.Y + (record * kSteps + i) * DV, col, DV, x);
+            for (int n = 0; n < NT; ++n) c[n] = y[n][r], z[n] = v[n][r];
+            write_columns<float, NT>(p.Y + (record * kSteps + i) * DV, col, DV, c);
             if (step < p.T) write_columns<E, NT>(const_cast<E *>(row_at<E>(p.grad_v, p.ld_gv, b, p.T, step, h, p.Dv)), col, p.Dv, z);
         }
-        if (chunk > 0) share_upstream(chunk - 1);
         if (threadIdx.x == 0) not_finite[2] = 0;
         __syncthreads();
+    };
+    Loads even, odd;
+    if (threadIdx.x < 4) not_finite[threadIdx.x] = 0;
+    __syncthreads();
+    if (p.chunks > 0) {
+        Upstream<NT> up;
+        load_upstream(up, p.chunks - 1);
+        if (AHEAD) load(even, p.chunks - 1);
+        share_upstream(up, p.chunks - 1);
     }
-    if (p.grad_s_first && has_state) adjoint_out(p.grad_s_first + head * p.Dk * p.Dv);
+    if (has_state) share_adjoint();
+    __syncthreads();
+    for (int chunk = p.chunks - 1; chunk >= 0; chunk -= 2) {
+        step(chunk, even, odd);
+        if (chunk > 0) step(chunk - 1, odd, even);
+    }
+    if (p.grad_s_first && has_state)
+#pragma unroll
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (wave * kTiles + tile) * 16 + group * 4 + r;
+                float v[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) v[n] = adj[tile][n][r];
+                if (d < p.Dk) write_columns<float, NT>(p.grad_s_first + (head * p.Dk + d) * p.Dv, col, p.Dv, v);
+            }
 }
 
 // Sum over the 16 lanes that hold a row.
@@ -555,8 +592,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
             for (int r = 0; r < 4; ++r) {
                 const int i = row * 16 + group * 4 + r;
                 const int64_t step = b * p.T + min(chunk * kSteps + i, p.T - 1);
-                const bool live = bit_of(alive, i);
-                const float f = live ? gates.f[i] : 0.0f, t = live ? gates.t[i] : 0.0f;
+                const float f = bit_of(alive, i) ? gates.f[i] : 0.0f, t = bit_of(alive, i) ? gates.t[i] : 0.0f;
 #pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile) {
                     if (!has_keys) continue;
@@ -698,8 +734,9 @@ template <typename E, int DK, int NT>
 int run_back(const DeltaArgs &p, hipStream_t stream)
 {
     const size_t lds = (size_t)16 * NT * (3 * (DK + 8) + (12 + 2 * kExact<E>) * (kSteps + 8)) * sizeof(__bf16);
-    if (const int rc = make_room_for(reinterpret_cast<const void *>(back_kernel<E, DK, NT>), lds)) return rc;
-    hipLaunchKernelGGL((back_kernel<E, DK, NT>), dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
+    constexpr bool kAhead = kExact<E> * DK <= 256;     // else two chunks' loads do not fit the registers
+    if (const int rc = make_room_for(reinterpret_cast<const void *>(back_kernel<E, DK, NT, kAhead>), lds)) return rc;
+    hipLaunchKernelGGL((back_kernel<E, DK, NT, kAhead>), dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
     return launched("delta scan gradient");
 }
 

@@ -30,7 +30,8 @@ __device__ __forceinline__ void gates_of(const DeltaArgs &p, int64_t b, int h, i
     const int part_end = __shfl(part, 63);
     out.G[i] = G;
     out.f[i] = part == 0 ? decay_of(G) : 0.0f;
-    out.t[i] = part == part_end ? decay_of(G_end - G) : 0.0f;
+    out.t[i] = !live ? -1.0f : part == part_end ? decay_of(G_end - G) : 0.0f;
+    if (i == kSteps - 1) out.whole = out.f[i];
     out.beta[i] = live ? p.beta[step * p.Hv + h] : 0.0f;
     const unsigned long long alive = __ballot(live);
     if (i == 0) { out.starts = starts; out.live = alive; out.bad = bad; }
@@ -251,25 +252,37 @@ __global__ __launch_bounds__(kDeltaThreads) void chunk_kernel(DeltaArgs p)
     }
 }
 
+// What a chunk needs from memory.
+template <typename E, int DK, int NT>
+struct ScanLoads {
+    static constexpr int PE = kExact<E>, PF = kFine<E>, KS = DK / 32, kTiles = (DK + 63) / 64;
+    Frag k[KS][PE], q[KS][PE], n[2][3], p[2][PF], kt[kTiles][2][PE];
+    float v[4][NT];
+    Acc f, t, beta;
+    float whole;
+    int bad;
+};
+
 // The chunks of one head one after the other, for 16 NT value columns: tile n of a lane's column l % 16 is column NT (l % 16) + n.  Wave w has
 // rows 16 w on of the chunk, and rows w DK / 4 on of the state, which stays in its accumulators; the others read it as planes from shared memory.
-// Loads are issued a phase ahead of their use, those for the start of a chunk in the middle of the one before.
-template <typename E, int DK, int NT>
-__global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2 : 1) void scan_kernel(DeltaArgs p)
+// AHEAD: a chunk's loads go out a whole chunk before their use.
+template <typename E, int DK, int NT, bool AHEAD>
+__global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 {
+    typedef ScanLoads<E, DK, NT> Loads;
     constexpr int PE = kExact<E>, PF = kFine<E>, KS = DK / 32, LS = DK + 8, LU = kSteps + 8, C = 16 * NT;
-    constexpr int kTiles = (DK + 63) / 64;             // of the state, for a wave; of DK = 32 two waves have one
+    constexpr int kTiles = Loads::kTiles;              // of the state, for a wave; of DK = 32 two waves have one
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef __bf16 StatePlane[C][LS];
     typedef __bf16 StepPlane[C][LU];
     StatePlane *S = reinterpret_cast<StatePlane *>(lds);                           // [3], columns of the state
     StepPlane *R = reinterpret_cast<StepPlane *>(lds + 3 * sizeof(StatePlane)), *U = R + 3, *Ue = U + PF;      // [3], [PF], [3]
     __shared__ int not_finite[2];
-    const int lane = threadIdx.x % kWave, wave = wave_index(), at = lane % 16, group = lane / 16;
+    const int lane = threadIdx.x % kWave, wave = wave_index(), at = lane % 16, group = lane / 16, zero = hidden_zero();
     const Place place = place_of((int64_t)p.B * p.Hv, p.Dv, C);
     if (place.head < 0) return;                        // the whole workgroup
     const int64_t head = place.head, b = head / p.Hv;
-    const int col = place.first + at * NT, h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk);
+    const int col = place.first + at * NT, h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk), DV = padded_values(p.Dv);
     const int64_t key_head = b * p.Hk + hk;
     const bool has_state = wave * kTiles * 16 < DK;
     Acc state[kTiles][NT] = {};
@@ -284,54 +297,43 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
 #pragma unroll
                 for (int n = 0; n < NT; ++n) state[tile][n][r] = v[n];
             }
-    // for the start of a chunk
-    Frag k[KS][PE], q[KS][PE];
-    float v[4][NT];
-    Acc f_next, t_next, beta_next;
-    auto load_start = [&](int chunk) {
-        const Frag *K = p.K + (key_head * p.chunks + chunk) * key_frags(DK, PE), *Q = p.Q + (key_head * p.chunks + chunk) * key_frags(DK, PE);
+    auto load = [&](Loads &x, int chunk) {
+        const int64_t record = head * p.chunks + chunk, key_record = key_head * p.chunks + chunk;
+        const Frag *K = p.K + key_record * key_frags(DK, PE), *Q = p.Q + key_record * key_frags(DK, PE), *KT = p.KT + key_record * key_frags(DK, PE);
+        const Frag *N = p.N + record * square_frags(3), *P = p.P + record * square_frags(PF);
+        const ChunkGates &g = p.gates[record];
+        x.f = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
+        x.t = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
+        x.beta = *reinterpret_cast<const Acc *>(g.beta + wave * 16 + group * 4);
+        x.whole = (&g.whole)[zero];
+        x.bad = (&g.bad)[zero];
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int n = 0; n < PE; ++n) {
-                k[s][n] = K[frag_at(wave, s, n, KS, PE)];
-                q[s][n] = Q[frag_at(wave, s, n, KS, PE)];
+                x.k[s][n] = K[frag_at(wave, s, n, KS, PE)];
+                x.q[s][n] = Q[frag_at(wave, s, n, KS, PE)];
             }
-        const ChunkGates &g = p.gates[head * p.chunks + chunk];
-        f_next = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
-        t_next = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
-        beta_next = *reinterpret_cast<const Acc *>(g.beta + wave * 16 + group * 4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int t = chunk * kSteps + wave * 16 + group * 4 + r;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) v[r][n] = 0.0f;
-            if (t < p.T) read_columns<E, NT>(row_at<E>(p.v, p.ld_v, b, p.T, t, h, p.Dv), col, p.Dv, v[r]);
+            const int t = min(chunk * kSteps + wave * 16 + group * 4 + r, p.T - 1);
+            read_columns<E, NT>(row_at<E>(p.v, p.ld_v, b, p.T, t, h, p.Dv), col, p.Dv, x.v[r]);
         }
-    };
-    const int DV = padded_values(p.Dv);
-    auto keep_state = [&](float *to) {
 #pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile)
+        for (int s = 0; s < 2; ++s) {
+            if (s * 32 > wave * 16) continue;          // zeros
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float v[NT];
+            for (int n = 0; n < 3; ++n) x.n[s][n] = N[frag_at(wave, s, n, 2, 3)];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) v[n] = state[tile][n][r];
-                write_columns<float, NT>(to + ((wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
-            }
-    };
-    auto state_out = [&](float *to) {                  // [Dk,Dv]
+            for (int n = 0; n < PF; ++n) x.p[s][n] = P[frag_at(wave, s, n, 2, PF)];
+        }
+        if (has_state)
 #pragma unroll
-        for (int tile = 0; tile < kTiles; ++tile)
+            for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = (wave * kTiles + tile) * 16 + group * 4 + r;
-                float v[NT];
+                for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) v[n] = state[tile][n][r];
-                if (d < p.Dk) write_columns<float, NT>(to + (int64_t)d * p.Dv, col, p.Dv, v);
-            }
+                    for (int n = 0; n < PE; ++n) x.kt[tile][s][n] = KT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
     };
     auto share_state = [&] {
 #pragma unroll
@@ -349,28 +351,21 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
 #pragma unroll
         for (int m = 0; m < PLANES; ++m) *reinterpret_cast<Four *>(&to[m][n * 16 + at][wave * 16 + group * 4]) = planes[m];
     };
-    if (p.chunks > 0) load_start(0);
-    if (has_state) share_state();
-    if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
-    __syncthreads();
-    for (int chunk = 0; chunk < p.chunks; ++chunk) {
+    auto step = [&](int chunk, Loads &x, Loads &next) {
         const int64_t record = head * p.chunks + chunk;
-        const ChunkGates &g = p.gates[record];
-        const unsigned long long starts = g.starts, live = g.live;
-        const float whole = g.f[kSteps - 1];
-        const bool bad = g.bad != 0;
-        if (p.S && has_state) keep_state(p.S + record * DK * DV);
-        Frag nn[2][3], pp[2][PF], kt[kTiles][2][PE];
-        const Frag *N = p.N + record * square_frags(3), *P = p.P + record * square_frags(PF);
-        const Frag *KT = p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE);
+        if (!AHEAD) load(x, chunk);
+        else if (chunk + 1 < p.chunks) load(next, chunk + 1);
+        const Acc f = x.f, t = x.t, beta = x.beta;
+        if (p.S && has_state)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (s * 32 > wave * 16) continue;          // zeros
+            for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
-            for (int n = 0; n < 3; ++n) nn[s][n] = N[frag_at(wave, s, n, 2, 3)];
+                for (int r = 0; r < 4; ++r) {
+                    float v[NT];
 #pragma unroll
-            for (int n = 0; n < PF; ++n) pp[s][n] = P[frag_at(wave, s, n, 2, PF)];
-        }
+                    for (int n = 0; n < NT; ++n) v[n] = state[tile][n][r];
+                    write_columns<float, NT>(p.S + (record * DK + (wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
+                }
         // R = V - f K S
         Acc ks[NT] = {}, qs[NT] = {};
 #pragma unroll
@@ -382,58 +377,53 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
                 for (int m = 0; m < 3; ++m) of_state[m] = *reinterpret_cast<const Frag *>(&S[m][n * 16 + at][s * 32 + group * 8]);
 #pragma unroll
                 for (int m = 0; m < PF; ++m) fine[m] = of_state[m];
-                ks[n] = multiply<PE, 3>(k[s], of_state, ks[n]);
-                qs[n] = multiply<PE, PF>(q[s], fine, qs[n]);
+                ks[n] = multiply<PE, 3>(x.k[s], of_state, ks[n]);
+                qs[n] = multiply<PE, PF>(x.q[s], fine, qs[n]);
             }
-        const Acc f = f_next, t = t_next, beta = beta_next;
         Acc m[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            Acc minus;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const bool on = bit_of(live, wave * 16 + group * 4 + r);
-                m[n][r] = !on ? 0.0f : f[r] == 0.0f ? v[r][n] : fmaf(-f[r], ks[n][r], v[r][n]);
-            }
-            minus = -(beta * m[n]);
+            for (int r = 0; r < 4; ++r) m[n][r] = t[r] < 0.0f ? 0.0f : f[r] == 0.0f ? x.v[r][n] : fmaf(-f[r], ks[n][r], x.v[r][n]);
+            const Acc minus = -(beta * m[n]);
             Four planes[3];
             split(minus, planes);
             share_steps(R, planes, n);
             if (!all_finite(minus)) not_finite[0] = 1;
         }
         __syncthreads();
-        if (has_state)
-#pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile)
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int n = 0; n < PE; ++n) kt[tile][s][n] = KT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
         // M = R - N (beta R), U = beta M
+        const bool bad = __builtin_amdgcn_readfirstlane(x.bad) != 0;
         const bool careful_n = bad || not_finite[0];
+        if (careful_n) {
+            const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
+            unsigned long long pass[4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (careful_n) {
-                unsigned long long pass[4];
-                for (int r = 0; r < 4; ++r) {
-                    const int i = wave * 16 + group * 4 + r;
-                    pass[r] = bit_of(live, i) ? upto(starts, i) & live & ~(1ull << i) : 0;
-                }
-                m[n] = careful_multiply<3, 3>(m[n], N, wave, R[0][n * 16 + at], C * LU, pass);
-            } else {
+            for (int r = 0; r < 4; ++r) {
+                const int i = wave * 16 + group * 4 + r;
+                pass[r] = bit_of(live, i) ? upto(starts, i) & live & ~(1ull << i) : 0;
+            }
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    if (s * 32 > wave * 16) continue;
+            for (int n = 0; n < NT; ++n) m[n] = careful_multiply<3, 3>(m[n], p.N + record * square_frags(3), wave, R[0][n * 16 + at], C * LU, pass);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (s * 32 > wave * 16) continue;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
                     Frag of_r[3];
 #pragma unroll
-                    for (int x = 0; x < 3; ++x) of_r[x] = *reinterpret_cast<const Frag *>(&R[x][n * 16 + at][s * 32 + group * 8]);
-                    m[n] = multiply<3, 3>(nn[s], of_r, m[n]);
+                    for (int c = 0; c < 3; ++c) of_r[c] = *reinterpret_cast<const Frag *>(&R[c][n * 16 + at][s * 32 + group * 8]);
+                    m[n] = multiply<3, 3>(x.n[s], of_r, m[n]);
                 }
             }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
             const Acc u = beta * m[n];
             Acc to_end;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) to_end[r] = t[r] == 0.0f ? 0.0f : t[r] * u[r];
+            for (int r = 0; r < 4; ++r) to_end[r] = t[r] > 0.0f || t[r] != t[r] ? t[r] * u[r] : 0.0f;
             Four planes[PF], end_planes[3];
             split(u, planes);
             split(to_end, end_planes);
@@ -444,81 +434,101 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
         if (p.M)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                float x[NT];
+                float c[NT];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) x[n] = m[n][r];
-                write_columns<float, NT>(p.M + (record * kSteps + wave * 16 + group * 4 + r) * DV, col, DV, x);
+                for (int n = 0; n < NT; ++n) c[n] = m[n][r];
+                write_columns<float, NT>(p.M + (record * kSteps + wave * 16 + group * 4 + r) * DV, col, DV, c);
             }
-        if (chunk + 1 < p.chunks) load_start(chunk + 1);
         __syncthreads();
-        // O = scale f Q S + P U
-        const bool careful_u = bad || not_finite[1];
+        // O = scale f Q S + P U,  S <- f_63 S + K' (t U)
         Acc o[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < 4; ++r) o[n][r] = f[r] == 0.0f ? 0.0f : p.scale * f[r] * qs[n][r];
-            if (careful_u) {
-                unsigned long long pass[4];
-                for (int r = 0; r < 4; ++r) {
-                    const int i = wave * 16 + group * 4 + r;
-                    pass[r] = bit_of(live, i) ? upto(starts, i) & live : 0;
-                }
-                o[n] = careful_multiply<PF, PF>(o[n], P, wave, U[0][n * 16 + at], C * LU, pass);
-            } else {
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    if (s * 32 > wave * 16) continue;
-                    Frag of_u[PF];
+        for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
-                    for (int x = 0; x < PF; ++x) of_u[x] = *reinterpret_cast<const Frag *>(&U[x][n * 16 + at][s * 32 + group * 8]);
-                    o[n] = multiply<PF, PF>(pp[s], of_u, o[n]);
-                }
-            }
-        }
-        // S <- f_63 S + K' (t U)
-        if (has_state) {
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile)
+                for (int r = 0; r < 4; ++r) state[tile][n][r] = x.whole == 0.0f ? 0.0f : x.whole * state[tile][n][r];
+        if (bad || not_finite[1]) {
+            const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
+            unsigned long long pass[4];
+            if (has_state) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) state[tile][n][r] = whole == 0.0f ? 0.0f : whole * state[tile][n][r];
-            if (careful_u) {
-                unsigned long long pass[4];
                 for (int r = 0; r < 4; ++r) pass[r] = upto(starts, kSteps - 1) & live;
 #pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        state[tile][n] = careful_multiply<PE, 3>(state[tile][n], KT, wave * kTiles + tile, Ue[0][n * 16 + at], C * LU, pass);
-            } else {
+                        state[tile][n] = careful_multiply<PE, 3>(state[tile][n], p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE),
+                                                                 wave * kTiles + tile, Ue[0][n * 16 + at], C * LU, pass);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = wave * 16 + group * 4 + r;
+                pass[r] = bit_of(live, i) ? upto(starts, i) & live : 0;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n] = careful_multiply<PF, PF>(o[n], p.P + record * square_frags(PF), wave, U[0][n * 16 + at], C * LU, pass);
+        } else {
+            if (has_state)
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         Frag of_u[3];
 #pragma unroll
-                        for (int x = 0; x < 3; ++x) of_u[x] = *reinterpret_cast<const Frag *>(&Ue[x][n * 16 + at][s * 32 + group * 8]);
+                        for (int c = 0; c < 3; ++c) of_u[c] = *reinterpret_cast<const Frag *>(&Ue[c][n * 16 + at][s * 32 + group * 8]);
 #pragma unroll
-                        for (int tile = 0; tile < kTiles; ++tile) state[tile][n] = multiply<PE, 3>(kt[tile][s], of_u, state[tile][n]);
+                        for (int tile = 0; tile < kTiles; ++tile) state[tile][n] = multiply<PE, 3>(x.kt[tile][s], of_u, state[tile][n]);
                     }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (s * 32 > wave * 16) continue;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    Frag of_u[PF];
+#pragma unroll
+                    for (int c = 0; c < PF; ++c) of_u[c] = *reinterpret_cast<const Frag *>(&U[c][n * 16 + at][s * 32 + group * 8]);
+                    o[n] = multiply<PF, PF>(x.p[s], of_u, o[n]);
+                }
             }
-            share_state();
         }
+        if (has_state) share_state();
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r, step = chunk * kSteps + i;
-            float x[NT];
+            const int step = chunk * kSteps + wave * 16 + group * 4 + r;
+            float c[NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) x[n] = bit_of(live, i) ? o[n][r] : 0.0f;
-            if (step < p.T) write_columns<E, NT>(const_cast<E *>(row_at<E>(p.o, p.ld_o, b, p.T, step, h, p.Dv)), col, p.Dv, x);
+            for (int n = 0; n < NT; ++n) c[n] = t[r] < 0.0f ? 0.0f : o[n][r];
+            if (step < p.T) write_columns<E, NT>(const_cast<E *>(row_at<E>(p.o, p.ld_o, b, p.T, step, h, p.Dv)), col, p.Dv, c);
         }
         if (threadIdx.x == 0) not_finite[0] = 0;       // read before the barrier above, written after the one below
         __syncthreads();
         if (threadIdx.x == 0) not_finite[1] = 0;
+    };
+    Loads even, odd;
+    if (AHEAD && p.chunks > 0) load(even, 0);
+    if (has_state) share_state();
+    if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
+    __syncthreads();
+    for (int chunk = 0; chunk < p.chunks; chunk += 2) {
+        step(chunk, even, odd);
+        if (chunk + 1 < p.chunks) step(chunk + 1, odd, even);
     }
-    if (p.s_last && has_state) state_out(p.s_last + head * p.Dk * p.Dv);
+    if (p.s_last && has_state)
+#pragma unroll
+        for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (wave * kTiles + tile) * 16 + group * 4 + r;
+                float v[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) v[n] = state[tile][n][r];
+                if (d < p.Dk) write_columns<float, NT>(p.s_last + (head * p.Dk + d) * p.Dv, col, p.Dv, v);
+            }
 }
 
 // Two tiles of columns a workgroup where that still fills the chip.
@@ -526,8 +536,9 @@ template <typename E, int DK, int NT>
 int run_scan(const DeltaArgs &p, hipStream_t stream)
 {
     const size_t lds = (size_t)16 * NT * (3 * (DK + 8) + (6 + kFine<E>) * (kSteps + 8)) * sizeof(__bf16);
-    if (const int rc = make_room_for(reinterpret_cast<const void *>(scan_kernel<E, DK, NT>), lds)) return rc;
-    hipLaunchKernelGGL((scan_kernel<E, DK, NT>), dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
+    constexpr bool kAhead = kExact<E> * DK <= 256;     // else two chunks' loads do not fit the registers
+    if (const int rc = make_room_for(reinterpret_cast<const void *>(scan_kernel<E, DK, NT, kAhead>), lds)) return rc;
+    hipLaunchKernelGGL((scan_kernel<E, DK, NT, kAhead>), dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
     return launched("delta scan");
 }
 
