@@ -221,6 +221,21 @@ __device__ __forceinline__ int hidden_zero()
 
 __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
 
+// NT adjacent columns of a row as they lie in memory: loaded at once, whatever the row's end, and looked at later, so that the load can be on its way
+// meanwhile.  (With a conversion or a branch behind the load every row of the next chunk was waited for where it was asked for.)
+template <typename E, int NT>
+struct Columns {
+    typedef E Vec __attribute__((ext_vector_type(NT)));
+    typedef Vec Loose __attribute__((aligned(sizeof(E))));
+    Vec raw;
+    __device__ __forceinline__ void load(const E *row, int col, int D) { raw = *reinterpret_cast<const Loose *>(row + min(col, D - NT)); }      // D >= NT
+    __device__ __forceinline__ float at(int n, int col, int D) const
+    {
+        const float own = to_f32(raw[n]), last = to_f32(raw[NT - 1]);
+        return col + NT <= D ? own : col + n == D - 1 ? last : 0.0f;
+    }
+};
+
 // The head and the first column of a workgroup on its way through the chunks.  Workgroups go to the eight dies in turn: those of a head, which
 // read the same fragments, are given to one die.  head = -1: nothing to do.
 struct Place { int64_t head; int first; };

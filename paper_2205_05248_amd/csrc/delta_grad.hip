@@ -19,9 +19,9 @@ struct BackLoads {
     int bad;
 };
 // The upstream gradient of a chunk, and what scales it.
-template <int NT>
+template <typename E, int NT>
 struct Upstream {
-    float o[4][NT];
+    Columns<E, NT> o[4];
     Acc f, t;
 };
 
@@ -93,14 +93,14 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
                         x.qt[tile][s][n] = QT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
                     }
     };
-    auto load_upstream = [&](Upstream<NT> &x, int chunk) {
+    auto load_upstream = [&](Upstream<E, NT> &x, int chunk) {
         const ChunkGates &g = p.gates[head * p.chunks + chunk];
         x.f = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
         x.t = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int t = min(chunk * kSteps + wave * 16 + group * 4 + r, p.T - 1);
-            read_columns<E, NT>(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), col, p.Dv, x.o[r]);
+            x.o[r].load(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), col, p.Dv);
         }
     };
     auto share_adjoint = [&] {
@@ -119,14 +119,14 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
 #pragma unroll
         for (int m = 0; m < PLANES; ++m) *reinterpret_cast<Four *>(&to[m][n * 16 + at][wave * 16 + group * 4]) = planes[m];
     };
-    auto share_upstream = [&](const Upstream<NT> &x, int chunk) {
+    auto share_upstream = [&](const Upstream<E, NT> &x, int chunk) {
         StepPlane *O = upstream + chunk % 2 * (PE + 3), *Of = O + PE;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             Acc o, of;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                o[r] = x.t[r] < 0.0f ? 0.0f : x.o[r][n];
+                o[r] = x.t[r] < 0.0f ? 0.0f : x.o[r].at(n, col, p.Dv);
                 of[r] = x.f[r] == 0.0f ? 0.0f : p.scale * x.f[r] * o[r];
             }
             Four exact[PE], planes[3];
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
     };
     auto step = [&](int chunk, Loads &x, Loads &next) {
         const int64_t record = head * p.chunks + chunk;
-        Upstream<NT> up;
+        Upstream<E, NT> up;
         if (!AHEAD) load(x, chunk);
         if (chunk > 0) {
             load_upstream(up, chunk - 1);
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
     if (threadIdx.x < 4) not_finite[threadIdx.x] = 0;
     __syncthreads();
     if (p.chunks > 0) {
-        Upstream<NT> up;
+        Upstream<E, NT> up;
         load_upstream(up, p.chunks - 1);
         if (AHEAD) load(even, p.chunks - 1);
         share_upstream(up, p.chunks - 1);
@@ -743,7 +743,7 @@ int run_back(const DeltaArgs &p, hipStream_t stream)
 template <typename E, int DK>
 int run(const DeltaArgs &p, hipStream_t stream)
 {
-    const int rc = (int64_t)p.B * p.Hv * ((p.Dv + 31) / 32) >= 256 ? run_back<E, DK, 2>(p, stream) : run_back<E, DK, 1>(p, stream);
+    const int rc = p.Dv > 16 && (int64_t)p.B * p.Hv * ((p.Dv + 31) / 32) >= 256 ? run_back<E, DK, 2>(p, stream) : run_back<E, DK, 1>(p, stream);
     if (rc || p.chunks == 0) return rc;
     const size_t lds = (6 + kExact<E>) * sizeof(Plane);            // (the results' rows, 64 of DK + 8, are less)
     if (const int failed = make_room_for(reinterpret_cast<const void *>(chunk_grad_kernel<E, DK>), lds)) return failed;

@@ -257,7 +257,7 @@ template <typename E, int DK, int NT>
 struct ScanLoads {
     static constexpr int PE = kExact<E>, PF = kFine<E>, KS = DK / 32, kTiles = (DK + 63) / 64;
     Frag k[KS][PE], q[KS][PE], n[2][3], p[2][PF], kt[kTiles][2][PE];
-    float v[4][NT];
+    Columns<E, NT> v[4];
     Acc f, t, beta;
     float whole;
     int bad;
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int t = min(chunk * kSteps + wave * 16 + group * 4 + r, p.T - 1);
-            read_columns<E, NT>(row_at<E>(p.v, p.ld_v, b, p.T, t, h, p.Dv), col, p.Dv, x.v[r]);
+            x.v[r].load(row_at<E>(p.v, p.ld_v, b, p.T, t, h, p.Dv), col, p.Dv);
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -384,7 +384,10 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) m[n][r] = t[r] < 0.0f ? 0.0f : f[r] == 0.0f ? x.v[r][n] : fmaf(-f[r], ks[n][r], x.v[r][n]);
+            for (int r = 0; r < 4; ++r) {
+                const float v = x.v[r].at(n, col, p.Dv);
+                m[n][r] = t[r] < 0.0f ? 0.0f : f[r] == 0.0f ? v : fmaf(-f[r], ks[n][r], v);
+            }
             const Acc minus = -(beta * m[n]);
             Four planes[3];
             split(minus, planes);
@@ -550,7 +553,7 @@ int run(const DeltaArgs &p, hipStream_t stream)
         if (const int rc = make_room_for(reinterpret_cast<const void *>(chunk_kernel<E, DK>), lds)) return rc;
         hipLaunchKernelGGL((chunk_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
     }
-    if ((int64_t)p.B * p.Hv * ((p.Dv + 31) / 32) >= 256) return run_scan<E, DK, 2>(p, stream);
+    if (p.Dv > 16 && (int64_t)p.B * p.Hv * ((p.Dv + 31) / 32) >= 256) return run_scan<E, DK, 2>(p, stream);
     return run_scan<E, DK, 1>(p, stream);
 }
 
