@@ -588,7 +588,7 @@ int marl_muon_step(int32_t dtype, int32_t L, int32_t rows, int32_t cols, const v
  *   s_last     dev [B,Hv,Dk,Dv] f32 or NULL          state after step T-1 (s_first if T is 0); may be s_first
  *   keep       nonzero: the workspace afterwards holds what marl_delta_scan_grad starts from
  * 1 <= Dk <= 128, 1 <= Dv <= 1024, 1 <= Hk <= Hv <= 1024.  B and T may be 0 (B Hv < 2^24, B T < 2^30); row distances are
- * below 2^31.  The state stays bounded for keys of norm at most 1 with beta between 0 and 2 and log_decay at most 0;
+ * below 2^24.  The state stays bounded for keys of norm at most 1 with beta between 0 and 2 and log_decay at most 0;
  * beyond that it grows as the formula says.  An infinity or NaN reaches no step before its own and none of another
  * sequence.
  */

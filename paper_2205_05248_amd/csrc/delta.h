@@ -236,6 +236,48 @@ struct Columns {
     }
 };
 
+// Rows of a chunk's results, written without a branch: what lies behind the last step or column goes to an offset that the descriptor does not
+// cover.  (Behind a branch the compiler cannot count the stores under way, and waits for them with the next chunk's loads.)  Row distances are
+// below 2^24, so that 64 rows are covered by 32 bits.
+constexpr int kRawBuffer = 0x00020000;
+template <typename E, int NT>
+struct RowsOut {
+    __amdgpu_buffer_rsrc_t buffer;
+    unsigned ld;
+    int rows, Dv;
+    bool pairs;
+    __device__ __forceinline__ RowsOut(const DeltaArgs &p, void *base, int64_t ld_, int64_t b, int chunk, int h)
+        : ld((unsigned)ld_), rows(min(kSteps, p.T - chunk * kSteps)), Dv(p.Dv)
+    {
+        E *first = const_cast<E *>(row_at<E>(base, ld_, b, p.T, chunk * kSteps, h, Dv));
+        buffer = __builtin_amdgcn_make_buffer_rsrc(first, 0, (int)((ld * (unsigned)(rows - 1) + (unsigned)Dv) * (unsigned)sizeof(E)), kRawBuffer);
+        pairs = sizeof(E) == 4 ? Dv % 2 == 0 : Dv % 2 == 0 && ld % 2 == 0 && (reinterpret_cast<uintptr_t>(base) & 3) == 0;
+    }
+    __device__ __forceinline__ void put(int row, int col, const float (&v)[NT]) const
+    {
+        typedef unsigned U2 __attribute__((ext_vector_type(2)));
+        typedef E Vec __attribute__((ext_vector_type(NT)));
+        const unsigned at = (ld * (unsigned)row + (unsigned)col) * (unsigned)sizeof(E), none = 0xfffffff0u;
+        Vec w;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) w[n] = from_f32<E>(v[n]);
+        if constexpr (NT == 2) {
+            if (pairs) {
+                const unsigned to = row < rows && col < Dv ? at : none;
+                if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(U2, w), buffer, to, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, w), buffer, to, 0, 0);
+                return;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const unsigned to = row < rows && col + n < Dv ? at + n * (unsigned)sizeof(E) : none;
+            if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, (float)w[n]), buffer, to, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, (E)w[n]), buffer, to, 0, 0);
+        }
+    }
+};
+
 // The head and the first column of a workgroup on its way through the chunks.  Workgroups go to the eight dies in turn: those of a head, which
 // read the same fragments, are given to one die.  head = -1: nothing to do.
 struct Place { int64_t head; int first; };

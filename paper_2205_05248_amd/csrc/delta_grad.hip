@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
     const int64_t head = place.head, b = head / p.Hv;
     const int col = place.first + at * NT, h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk), DV = padded_values(p.Dv);
     const int64_t key_head = b * p.Hk + hk;
-    const bool has_state = wave * kTiles * 16 < DK;
+    const bool has_state = DK >= 64 || wave * 16 < DK;
     Acc adj[kTiles][NT] = {};
     if (p.grad_s_last && has_state)
 #pragma unroll
@@ -74,24 +74,22 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
 #pragma unroll
             for (int n = 0; n < PE; ++n) x.k[s][n] = K[frag_at(wave, s, n, KS, PE)];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (s * 32 + 31 < wave * 16) continue;     // zeros
+        for (int s = 0; s < 2; ++s) {                  // (what lies on the other side of the diagonal is never written, and not used)
 #pragma unroll
             for (int n = 0; n < 3; ++n) {
                 x.p[s][n] = P[frag_at(wave, s, n, 2, 3)];
                 x.n[s][n] = N[frag_at(wave, s, n, 2, 3)];
             }
         }
-        if (has_state)
 #pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile)
+        for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int n = 0; n < PE; ++n) {
-                        x.kt[tile][s][n] = KT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
-                        x.qt[tile][s][n] = QT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
-                    }
+                for (int n = 0; n < PE; ++n) {
+                    x.kt[tile][s][n] = KT[frag_at((wave * kTiles + tile) % (DK / 16), s, n, 2, PE)];
+                    x.qt[tile][s][n] = QT[frag_at((wave * kTiles + tile) % (DK / 16), s, n, 2, PE)];
+                }
     };
     auto load_upstream = [&](Upstream<E, NT> &x, int chunk) {
         const ChunkGates &g = p.gates[head * p.chunks + chunk];
@@ -141,10 +139,8 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
         const int64_t record = head * p.chunks + chunk;
         Upstream<E, NT> up;
         if (!AHEAD) load(x, chunk);
-        if (chunk > 0) {
-            load_upstream(up, chunk - 1);
-            if (AHEAD) load(next, chunk - 1);
-        }
+        load_upstream(up, max(chunk - 1, 0));
+        if (AHEAD) load(next, max(chunk - 1, 0));
         const Acc f = x.f, t = x.t, beta = x.beta;
         const StepPlane *O = upstream + chunk % 2 * (PE + 3), *Of = O + PE;
         const bool bad = __builtin_amdgcn_readfirstlane(x.bad) != 0, careful_o = bad || not_finite[chunk % 2];
@@ -289,14 +285,15 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
             share_adjoint();
         }
         if (chunk > 0) share_upstream(up, chunk - 1);
+        const RowsOut<E, NT> out(p, p.grad_v, p.ld_gv, b, chunk, h);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r, step = chunk * kSteps + i;
+            const int i = wave * 16 + group * 4 + r;
             float c[NT], z[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) c[n] = y[n][r], z[n] = v[n][r];
             write_columns<float, NT>(p.Y + (record * kSteps + i) * DV, col, DV, c);
-            if (step < p.T) write_columns<E, NT>(const_cast<E *>(row_at<E>(p.grad_v, p.ld_gv, b, p.T, step, h, p.Dv)), col, p.Dv, z);
+            out.put(i, col, z);
         }
         if (threadIdx.x == 0) not_finite[2] = 0;
         __syncthreads();

@@ -139,7 +139,7 @@ void place(int dtype, DeltaArgs &p, char *workspace, bool keep)
     p.S = floats(r.S); p.M = floats(r.M); p.D = floats(r.D); p.Y = floats(r.Y);
 }
 
-constexpr int64_t kMostRow = (int64_t)1 << 31;
+constexpr int64_t kMostRow = (int64_t)1 << 24, kMostGroups = (int64_t)1 << 31;
 
 int heads_check(int dtype, int Hk, int Hv, int Dk, int Dv)
 {
@@ -152,7 +152,7 @@ int sizes_check(int dtype, int B, int T, int Hk, int Hv, int Dk, int Dv)
     if (const int rc = heads_check(dtype, Hk, Hv, Dk, Dv)) return rc;
     if (B < 0 || T < 0 || (int64_t)B * Hv >= (1 << 24) || (int64_t)B * T >= (1 << 30)) return MARL_ERR_BAD_DIM;
     // grids: a workgroup per record, and one per head and sixteen columns
-    if ((int64_t)B * Hv * ((T + kSteps - 1) / kSteps) >= kMostRow || (int64_t)B * Hv * (padded_values(Dv) / 16) >= kMostRow - 8) return MARL_ERR_BAD_DIM;
+    if ((int64_t)B * Hv * ((T + kSteps - 1) / kSteps) >= kMostGroups || (int64_t)B * Hv * (padded_values(Dv) / 16) >= kMostGroups - 8) return MARL_ERR_BAD_DIM;
     return MARL_OK;
 }
 bool row_fits(int64_t ld, int H, int D) { return ld >= (int64_t)H * D && ld < kMostRow; }

@@ -265,8 +265,9 @@ struct ScanLoads {
 
 // The chunks of one head one after the other, for 16 NT value columns: tile n of a lane's column l % 16 is column NT (l % 16) + n.  Wave w has
 // rows 16 w on of the chunk, and rows w DK / 4 on of the state, which stays in its accumulators; the others read it as planes from shared memory.
-// AHEAD: a chunk's loads go out a whole chunk before their use.
-template <typename E, int DK, int NT, bool AHEAD>
+// AHEAD: a chunk's loads go out a whole chunk before their use, whether there is another chunk or not: behind a branch the compiler would wait
+// for them at the next wait of any kind.
+template <typename E, int DK, int NT, bool AHEAD, bool KEEP>
 __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 {
     typedef ScanLoads<E, DK, NT> Loads;
@@ -284,7 +285,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
     const int64_t head = place.head, b = head / p.Hv;
     const int col = place.first + at * NT, h = (int)(head % p.Hv), hk = h / (p.Hv / p.Hk), DV = padded_values(p.Dv);
     const int64_t key_head = b * p.Hk + hk;
-    const bool has_state = wave * kTiles * 16 < DK;
+    const bool has_state = DK >= 64 || wave * 16 < DK;
     Acc state[kTiles][NT] = {};
     if (p.s_first && has_state)
 #pragma unroll
@@ -320,20 +321,18 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
             x.v[r].load(row_at<E>(p.v, p.ld_v, b, p.T, t, h, p.Dv), col, p.Dv);
         }
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (s * 32 > wave * 16) continue;          // zeros
+        for (int s = 0; s < 2; ++s) {                  // (what lies on the other side of the diagonal is never written, and not used)
 #pragma unroll
             for (int n = 0; n < 3; ++n) x.n[s][n] = N[frag_at(wave, s, n, 2, 3)];
 #pragma unroll
             for (int n = 0; n < PF; ++n) x.p[s][n] = P[frag_at(wave, s, n, 2, PF)];
         }
-        if (has_state)
 #pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile)
+        for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int n = 0; n < PE; ++n) x.kt[tile][s][n] = KT[frag_at(wave * kTiles + tile, s, n, 2, PE)];
+                for (int n = 0; n < PE; ++n) x.kt[tile][s][n] = KT[frag_at((wave * kTiles + tile) % (DK / 16), s, n, 2, PE)];
     };
     auto share_state = [&] {
 #pragma unroll
@@ -354,9 +353,9 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
     auto step = [&](int chunk, Loads &x, Loads &next) {
         const int64_t record = head * p.chunks + chunk;
         if (!AHEAD) load(x, chunk);
-        else if (chunk + 1 < p.chunks) load(next, chunk + 1);
+        else load(next, min(chunk + 1, p.chunks - 1));
         const Acc f = x.f, t = x.t, beta = x.beta;
-        if (p.S && has_state)
+        if (KEEP && has_state)
 #pragma unroll
             for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
@@ -434,7 +433,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
             share_steps(Ue, end_planes, n);
             if (!all_finite(u)) not_finite[1] = 1;
         }
-        if (p.M)
+        if (KEEP)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float c[NT];
@@ -500,13 +499,13 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
             }
         }
         if (has_state) share_state();
+        const RowsOut<E, NT> out(p, p.o, p.ld_o, b, chunk, h);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int step = chunk * kSteps + wave * 16 + group * 4 + r;
             float c[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) c[n] = t[r] < 0.0f ? 0.0f : o[n][r];
-            if (step < p.T) write_columns<E, NT>(const_cast<E *>(row_at<E>(p.o, p.ld_o, b, p.T, step, h, p.Dv)), col, p.Dv, c);
+            out.put(wave * 16 + group * 4 + r, col, c);
         }
         if (threadIdx.x == 0) not_finite[0] = 0;       // read before the barrier above, written after the one below
         __syncthreads();
@@ -540,9 +539,12 @@ int run_scan(const DeltaArgs &p, hipStream_t stream)
 {
     const size_t lds = (size_t)16 * NT * (3 * (DK + 8) + (6 + kFine<E>) * (kSteps + 8)) * sizeof(__bf16);
     constexpr bool kAhead = kExact<E> * DK <= 256;     // else two chunks' loads do not fit the registers
-    if (const int rc = make_room_for(reinterpret_cast<const void *>(scan_kernel<E, DK, NT, kAhead>), lds)) return rc;
-    hipLaunchKernelGGL((scan_kernel<E, DK, NT, kAhead>), dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
-    return launched("delta scan");
+    const auto go = [&](auto kernel) {
+        if (const int rc = make_room_for(reinterpret_cast<const void *>(kernel), lds)) return rc;
+        hipLaunchKernelGGL(kernel, dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
+        return launched("delta scan");
+    };
+    return p.S ? go(scan_kernel<E, DK, NT, kAhead, true>) : go(scan_kernel<E, DK, NT, kAhead, false>);
 }
 
 template <typename E, int DK>
