@@ -102,14 +102,21 @@ __device__ __forceinline__ unsigned long long from(unsigned long long starts, in
     return behind ? high & (behind & -behind) - 1 : high;
 }
 
-// Planes of four values.
+// Planes of four values.  (Pairs: one instruction converts two.)
 template <int N>
 __device__ __forceinline__ void split(Acc v, Four (&out)[N])
 {
+    typedef __bf16 Two __attribute__((ext_vector_type(2)));
+    typedef float Pair __attribute__((ext_vector_type(2)));
+    Pair x{v[0], v[1]}, y{v[2], v[3]};
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        out[n] = __builtin_convertvector(v, Four);
-        if (n + 1 < N) v -= __builtin_convertvector(out[n], Acc);
+        const Two low = __builtin_convertvector(x, Two), high = __builtin_convertvector(y, Two);
+        out[n] = __builtin_shufflevector(low, high, 0, 1, 2, 3);
+        if (n + 1 < N) {
+            x -= __builtin_convertvector(low, Pair);
+            y -= __builtin_convertvector(high, Pair);
+        }
     }
 }
 template <int N>
@@ -133,6 +140,26 @@ __device__ __forceinline__ Acc multiply(const Frag (&a)[PA], const Frag (&b)[PB]
         for (int i = 0; i < PA; ++i)
             if (s - i >= 0 && s - i < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[s - i], c, 0, 0, 0);
     return c;
+}
+
+// The same with a sum of its own for the products of every size: none waits for another's, and small ones are not rounded to the size of large ones.
+template <int ORDER> struct Sums { Acc c[ORDER + 1] = {}; };
+template <int PA, int PB, int ORDER>
+__device__ __forceinline__ void multiply_into(Sums<ORDER> &sums, const Frag (&a)[PA], const Frag (&b)[PB])
+{
+#pragma unroll
+    for (int s = ORDER; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            if (s - i >= 0 && s - i < PB) sums.c[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[s - i], sums.c[s], 0, 0, 0);
+}
+template <int ORDER>
+__device__ __forceinline__ Acc total(const Sums<ORDER> &sums)
+{
+    Acc v = sums.c[ORDER];
+#pragma unroll
+    for (int s = ORDER - 1; s >= 0; --s) v += sums.c[s];
+    return v;
 }
 
 // The same over 64 columns k without the matrix pipe, for chunks that hold an infinity or NaN: only the k in pass[r] take part in the lane's

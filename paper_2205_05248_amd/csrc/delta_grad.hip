@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
                     write_columns<float, NT>(p.D + (record * DK + (wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
                 }
         // dU = P' dO + t K D
-        Acc y[NT] = {};
+        Sums<2> kd[NT];
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -165,12 +165,15 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
                 Frag of_state[3];
 #pragma unroll
                 for (int m = 0; m < 3; ++m) of_state[m] = *reinterpret_cast<const Frag *>(&S[m][n * 16 + at][s * 32 + group * 8]);
-                y[n] = multiply<PE, 3>(x.k[s], of_state, y[n]);
+                multiply_into(kd[n], x.k[s], of_state);
             }
+        Acc y[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+            const Acc of_k = total(kd[n]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[n][r] = t[r] > 0.0f || t[r] != t[r] ? t[r] * y[n][r] : 0.0f;
+            for (int r = 0; r < 4; ++r) y[n][r] = t[r] > 0.0f || t[r] != t[r] ? t[r] * of_k[r] : 0.0f;
+        }
         if (careful_o) {
             const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
             unsigned long long pass[4];
@@ -182,6 +185,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
 #pragma unroll
             for (int n = 0; n < NT; ++n) y[n] = careful_multiply<3, PE>(y[n], p.PT + record * square_frags(3), wave, O[0][n * 16 + at], C * LU, pass);
         } else {
+            Sums<2> po[NT];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if (s * 32 + 31 < wave * 16) continue;
@@ -190,9 +194,11 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
                     Frag of_o[PE];
 #pragma unroll
                     for (int c = 0; c < PE; ++c) of_o[c] = *reinterpret_cast<const Frag *>(&O[c][n * 16 + at][s * 32 + group * 8]);
-                    y[n] = multiply<3, PE>(x.p[s], of_o, y[n]);
+                    multiply_into(po[n], x.p[s], of_o);
                 }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) y[n] += total(po[n]);
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -215,6 +221,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
 #pragma unroll
             for (int n = 0; n < NT; ++n) y[n] = careful_multiply<3, 3>(y[n], p.NT + record * square_frags(3), wave, R[0][n * 16 + at], C * LU, pass);
         } else {
+            Sums<2> nr[NT];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if (s * 32 + 31 < wave * 16) continue;
@@ -223,9 +230,11 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
                     Frag of_r[3];
 #pragma unroll
                     for (int c = 0; c < 3; ++c) of_r[c] = *reinterpret_cast<const Frag *>(&R[c][n * 16 + at][s * 32 + group * 8]);
-                    y[n] = multiply<3, 3>(x.n[s], of_r, y[n]);
+                    multiply_into(nr[n], x.n[s], of_r);
                 }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) y[n] += total(nr[n]);
         }
         Acc v[NT];
 #pragma unroll
@@ -265,6 +274,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
                         adj[tile][n] = careful_multiply<PE, 3>(adj[tile][n], p.KT + key_record * key_frags(DK, PE), wave * kTiles + tile, V[0][n * 16 + at], C * LU, pass);
                     }
             } else {
+                Sums<2> of_keys[kTiles][NT];
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -277,10 +287,14 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
                         }
 #pragma unroll
                         for (int tile = 0; tile < kTiles; ++tile) {
-                            adj[tile][n] = multiply<PE, 3>(x.qt[tile][s], of_o, adj[tile][n]);
-                            adj[tile][n] = multiply<PE, 3>(x.kt[tile][s], of_v, adj[tile][n]);
+                            multiply_into(of_keys[tile][n], x.qt[tile][s], of_o);
+                            multiply_into(of_keys[tile][n], x.kt[tile][s], of_v);
                         }
                     }
+#pragma unroll
+                for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) adj[tile][n] += total(of_keys[tile][n]);
             }
             share_adjoint();
         }

@@ -366,7 +366,8 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
                     write_columns<float, NT>(p.S + (record * DK + (wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
                 }
         // R = V - f K S
-        Acc ks[NT] = {}, qs[NT] = {};
+        Sums<2> ks[NT];
+        Sums<PF - 1> qs[NT];
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -376,16 +377,17 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
                 for (int m = 0; m < 3; ++m) of_state[m] = *reinterpret_cast<const Frag *>(&S[m][n * 16 + at][s * 32 + group * 8]);
 #pragma unroll
                 for (int m = 0; m < PF; ++m) fine[m] = of_state[m];
-                ks[n] = multiply<PE, 3>(x.k[s], of_state, ks[n]);
-                qs[n] = multiply<PE, PF>(x.q[s], fine, qs[n]);
+                multiply_into(ks[n], x.k[s], of_state);
+                multiply_into(qs[n], x.q[s], fine);
             }
         Acc m[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+            const Acc of_k = total(ks[n]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float v = x.v[r].at(n, col, p.Dv);
-                m[n][r] = t[r] < 0.0f ? 0.0f : f[r] == 0.0f ? v : fmaf(-f[r], ks[n][r], v);
+                m[n][r] = t[r] < 0.0f ? 0.0f : f[r] == 0.0f ? v : fmaf(-f[r], of_k[r], v);
             }
             const Acc minus = -(beta * m[n]);
             Four planes[3];
@@ -408,6 +410,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 #pragma unroll
             for (int n = 0; n < NT; ++n) m[n] = careful_multiply<3, 3>(m[n], p.N + record * square_frags(3), wave, R[0][n * 16 + at], C * LU, pass);
         } else {
+            Sums<2> nr[NT];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if (s * 32 > wave * 16) continue;
@@ -416,9 +419,11 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
                     Frag of_r[3];
 #pragma unroll
                     for (int c = 0; c < 3; ++c) of_r[c] = *reinterpret_cast<const Frag *>(&R[c][n * 16 + at][s * 32 + group * 8]);
-                    m[n] = multiply<3, 3>(x.n[s], of_r, m[n]);
+                    multiply_into(nr[n], x.n[s], of_r);
                 }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) m[n] += total(nr[n]);
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -445,9 +450,11 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
         // O = scale f Q S + P U,  S <- f_63 S + K' (t U)
         Acc o[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+            const Acc of_q = total(qs[n]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[n][r] = f[r] == 0.0f ? 0.0f : p.scale * f[r] * qs[n][r];
+            for (int r = 0; r < 4; ++r) o[n][r] = f[r] == 0.0f ? 0.0f : p.scale * f[r] * of_q[r];
+        }
 #pragma unroll
         for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
@@ -475,7 +482,8 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 #pragma unroll
             for (int n = 0; n < NT; ++n) o[n] = careful_multiply<PF, PF>(o[n], p.P + record * square_frags(PF), wave, U[0][n * 16 + at], C * LU, pass);
         } else {
-            if (has_state)
+            if (has_state) {
+                Sums<2> ku[kTiles][NT];
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -484,8 +492,13 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 #pragma unroll
                         for (int c = 0; c < 3; ++c) of_u[c] = *reinterpret_cast<const Frag *>(&Ue[c][n * 16 + at][s * 32 + group * 8]);
 #pragma unroll
-                        for (int tile = 0; tile < kTiles; ++tile) state[tile][n] = multiply<PE, 3>(x.kt[tile][s], of_u, state[tile][n]);
+                        for (int tile = 0; tile < kTiles; ++tile) multiply_into(ku[tile][n], x.kt[tile][s], of_u);
                     }
+#pragma unroll
+                for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) state[tile][n] += total(ku[tile][n]);
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 if (s * 32 > wave * 16) continue;
