@@ -397,17 +397,20 @@ __device__ __forceinline__ Acc careful_rows(Acc c, const Plane *a, int tile, con
 //   dG_i = sum_j F_ij - sum_j F_ji + q_i.(scale f dO S')_i - k_i.(f dV S')_i - k_i.(t U D')_i      F_ij = dM_ij k_i.k_j + dN_ij q_i.k_j
 // to which the last step adds sum_j k_j.(t U D')_j + f_63 <D, S>; the log decay's gradient is the sum of dG from its step to the end of
 // its sequence.  Value columns come 64 at a time through shared memory.  Products with rows and columns of steps are split over the waves by
-// rows (16 w on), those with key columns by columns (w DK / 4 on), so that every entry of S and D is split into planes once.
+// rows, those with key columns by columns (16 w on), so that every entry of S and D is split into planes once.
+// Waves of a workgroup: with 128 keys eight, of which four form dP and four dA, else four that form both.
+constexpr int grad_waves(int DK) { return DK == 128 ? 8 : 4; }
+
 template <typename E, int DK>
-__global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs p)
+__global__ __launch_bounds__(grad_waves(DK) * kWave) void chunk_grad_kernel(DeltaArgs p)
 {
-    constexpr int PE = kExact<E>, KS = DK / 32, kTiles = (DK + 63) / 64, kOrder = PE == 1 ? 0 : 2;
+    constexpr int PE = kExact<E>, KS = DK / 32, kOrder = PE == 1 ? 0 : 2, kWaves = grad_waves(DK), kThreads = kWaves * kWave;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Plane *U = reinterpret_cast<Plane *>(lds), *V = U + 3, *O = V + 3;             // [3], [3], [PE]
     Plane *dN = U, *dNT = V, *X = U;                   // later in the same room, [3] each
     __shared__ ChunkGates gates;
     __shared__ int not_finite;
-    __shared__ float rows_of[4][kSteps], columns_of[4][kSteps], flow[kSteps], extra[4], dbeta[kSteps];
+    __shared__ float rows_of[kWaves][kSteps], columns_of[8][kSteps], flow[2][kSteps], extra[kWaves], dbeta[kSteps];
     const int lane = threadIdx.x % kWave;
     int wave = wave_index(), at = lane % 16, group = lane / 16;
     int nothing;
@@ -415,14 +418,14 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
     int chunk = (int)(blockIdx.x % p.chunks);
     const int64_t b = blockIdx.x / p.chunks / p.Hk;
     const int shared = p.Hv / p.Hk, DV = padded_values(p.Dv);
-    const bool has_keys = wave * kTiles * 16 < DK;
+    const bool has_keys = wave * 16 < DK;
     const Frag *K = p.K + (int64_t)blockIdx.x * key_frags(DK, PE), *Q = p.Q + (int64_t)blockIdx.x * key_frags(DK, PE);
     const Frag *KT = p.KT + (int64_t)blockIdx.x * key_frags(DK, PE), *QT = p.QT + (int64_t)blockIdx.x * key_frags(DK, PE);
-    Acc sum_q[kTiles][4] = {}, sum_k[kTiles][4] = {};
+    Acc sum_q[4] = {}, sum_k[4] = {};
     unsigned long long alive = 0;
     for (int member = 0; member < shared; ++member) {
         // else addresses, masks and the products of K and Q are formed before the loop, and 500 registers do not hold them
-        asm volatile("v_mov_b32 %0, 0" : "=v"(nothing));
+        nothing = hidden_zero();
         at += nothing;
         group += nothing;
         nothing = __builtin_amdgcn_readfirstlane(nothing);
@@ -438,7 +441,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
         {
             const int *from = reinterpret_cast<const int *>(p.gates + record);
             int *to = reinterpret_cast<int *>(&gates);
-            for (int e = threadIdx.x; e < (int)(sizeof(ChunkGates) / 4); e += kDeltaThreads) to[e] = from[e];
+            for (int e = threadIdx.x; e < (int)(sizeof(ChunkGates) / 4); e += kThreads) to[e] = from[e];
         }
         if (threadIdx.x == 0) not_finite = 0;
         __syncthreads();
@@ -446,29 +449,29 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
         alive = gates.live;
         const float *M = p.M + record * kSteps * DV, *Y = p.Y + record * kSteps * DV;
         const float *S = p.S + record * DK * DV, *D = p.D + record * DK * DV;
-        Acc dp[4] = {}, da[4] = {}, far_q[kTiles][4] = {}, far_k[kTiles][4] = {}, end[kTiles][4] = {};
+        Acc d_of[2][4] = {}, far_q[4] = {}, far_k[4] = {}, end[4] = {};            // d_of: dP, dA
         float dot_states = 0.0f, dot_beta = 0.0f;
         for (int c0 = 0; c0 < p.Dv; c0 += kSteps) {
             const int steps = min(2, (DV - c0) / 32);
             // S and D of the wave's keys: loads go out before the wait for the staging
             typedef float Eight __attribute__((ext_vector_type(8)));
-            Eight s[kTiles][2], d[kTiles][2];
+            Eight s[2], d[2];
 #pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile)
-#pragma unroll
-                for (int step = 0; step < 2; ++step) {
-                    if (!has_keys || step >= steps) continue;
-                    const int from = ((wave * kTiles + tile) * 16 + at) * DV + c0 + step * 32 + group * 8;
-                    s[tile][step] = *reinterpret_cast<const Eight *>(S + from);
-                    d[tile][step] = *reinterpret_cast<const Eight *>(D + from);
-                }
-            if (threadIdx.x % 4 < 2 * steps) {
-                const int i = threadIdx.x / 4, t = chunk * kSteps + i;
+            for (int step = 0; step < 2; ++step) {
+                if (!has_keys || step >= steps) continue;
+                const int from = (wave * 16 + at) * DV + c0 + step * 32 + group * 8;
+                s[step] = *reinterpret_cast<const Eight *>(S + from);
+                d[step] = *reinterpret_cast<const Eight *>(D + from);
+            }
+            {
+                constexpr int kPer = kThreads / kSteps, kHalves = 8 / kPer;        // threads of a row, and how often eight columns each
+                const int i = threadIdx.x / kPer, t = chunk * kSteps + i;
                 const bool live = bit_of(alive, i);
                 const float beta = gates.beta[i];
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int c = threadIdx.x % 4 * 16 + half * 8;
+                for (int half = 0; half < kHalves; ++half) {
+                    const int c = (threadIdx.x % kPer * kHalves + half) * 8;
+                    if (c >= 32 * steps) continue;
                     const Eight m = *reinterpret_cast<const Eight *>(M + i * DV + c0 + c), y = *reinterpret_cast<const Eight *>(Y + i * DV + c0 + c);
                     float u[8], v[8], o[8] = {};
                     if (live) read_columns<E, 8>(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), c0 + c, p.Dv, o);
@@ -487,142 +490,153 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
 #pragma unroll
             for (int step = 0; step < 2; ++step) {
                 if (step >= steps) continue;
-                Frag o[PE], v[3];
-                get_frag(O, wave, step, o);
-                get_frag(V, wave, step, v);
+                {
+                    const int row = wave % 4;
+                    Frag o[PE], v[3];
+                    if (kWaves == 4 || wave < 4) get_frag(O, row, step, o);
+                    if (kWaves == 4 || wave >= 4) get_frag(V, row, step, v);
 #pragma unroll
-                for (int tile = 0; tile < 4; ++tile) {
-                    if (tile > wave) continue;
-                    Frag u[3];
-                    get_frag(U, tile, step, u);
-                    dp[tile] = multiply<PE, 3>(o, u, dp[tile]);
-                    da[tile] = multiply<3, 3>(v, u, da[tile]);
+                    for (int tile = 0; tile < 4; ++tile) {
+                        if (tile > row) continue;
+                        Frag u[3];
+                        get_frag(U, tile, step, u);
+                        if (kWaves == 4 || wave < 4) d_of[0][tile] = multiply<PE, 3>(o, u, d_of[0][tile]);
+                        if (kWaves == 4) d_of[1][tile] = multiply<3, 3>(v, u, d_of[1][tile]);
+                        else if (wave >= 4) d_of[0][tile] = multiply<3, 3>(v, u, d_of[0][tile]);
+                    }
                 }
                 if (!has_keys) continue;
-                Frag of_s[kTiles][3], of_d[kTiles][3];
+                Frag of_s[3], of_d[3];
 #pragma unroll
-                for (int tile = 0; tile < kTiles; ++tile) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) dot_states = fmaf(s[tile][step][e], d[tile][step][e], dot_states);
-                    split(reinterpret_cast<const float *>(&s[tile][step]), of_s[tile]);
-                    split(reinterpret_cast<const float *>(&d[tile][step]), of_d[tile]);
-                }
+                for (int e = 0; e < 8; ++e) dot_states = fmaf(s[step][e], d[step][e], dot_states);
+                split(reinterpret_cast<const float *>(&s[step]), of_s);
+                split(reinterpret_cast<const float *>(&d[step]), of_d);
 #pragma unroll
                 for (int row = 0; row < 4; ++row) {
                     __builtin_amdgcn_sched_barrier(0); // (loads of all rows at once would not fit the registers)
-                    Frag u[3];
+                    Frag o[PE], v[3], u[3];
                     get_frag(O, row, step, o);
                     get_frag(V, row, step, v);
                     get_frag(U, row, step, u);
-#pragma unroll
-                    for (int tile = 0; tile < kTiles; ++tile) {
-                        far_q[tile][row] = multiply<PE, 3>(o, of_s[tile], far_q[tile][row]);
-                        far_k[tile][row] = multiply<3, 3>(v, of_s[tile], far_k[tile][row]);
-                        end[tile][row] = multiply<3, 3>(u, of_d[tile], end[tile][row]);
-                    }
+                    far_q[row] = multiply<PE, 3>(o, of_s, far_q[row]);
+                    far_k[row] = multiply<3, 3>(v, of_s, far_k[row]);
+                    end[row] = multiply<3, 3>(u, of_d, end[row]);
                 }
             }
             __syncthreads();
         }
         // what goes from step j to step i, and the row and column sums of F
         Acc dm[4];
-        {
-            Acc kk[4] = {}, qk[4] = {};
+        bool fine = true;
+        unsigned long long before[4];                  // steps that hand something to the lane's rows
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = wave % 4 * 16 + group * 4 + r;
+            before[r] = bit_of(alive, i) ? upto(starts, i) & alive : 0;
+        }
+        auto flows = [&](Acc (&of)[4], bool is_p) {    // of P, or of A
+            const int row = wave % 4;
+            Acc raw[4] = {};
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 __builtin_amdgcn_sched_barrier(0);
-                Frag k[PE], q[PE];
+                Frag mine[PE];
 #pragma unroll
-                for (int n = 0; n < PE; ++n) k[n] = K[frag_at(wave, s, n, KS, PE)], q[n] = Q[frag_at(wave, s, n, KS, PE)];
+                for (int n = 0; n < PE; ++n) mine[n] = (is_p ? Q : K)[frag_at(row, s, n, KS, PE)];
 #pragma unroll
                 for (int tile = 0; tile < 4; ++tile) {
-                    if (tile > wave) continue;
+                    if (tile > row) continue;
                     Frag other[PE];
 #pragma unroll
                     for (int n = 0; n < PE; ++n) other[n] = K[frag_at(tile, s, n, KS, PE)];
-                    kk[tile] = multiply<PE, PE, kOrder>(k, other, kk[tile]);
-                    qk[tile] = multiply<PE, PE, kOrder>(q, other, qk[tile]);
+                    raw[tile] = multiply<PE, PE, kOrder>(mine, other, raw[tile]);
                 }
             }
             float row_flow[4] = {};
-            bool fine = true;
-            unsigned long long before[4];              // steps that hand something to the lane's rows
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = wave * 16 + group * 4 + r;
-                before[r] = bit_of(alive, i) ? upto(starts, i) & alive : 0;
-            }
 #pragma unroll
             for (int tile = 0; tile < 4; ++tile) {
                 const int j = tile * 16 + at;
-                Acc dn;
+                Acc d;
                 float column = 0.0f;
+                if (tile <= row)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = wave * 16 + group * 4 + r;
-                    const bool on = tile <= wave && bit_of(before[r], j), below = on && j < i;
-                    const float e = decay_of(gates.G[i] - gates.G[j]), n = p.scale * e * dp[tile][r], m = -e * da[tile][r];
-                    dn[r] = on ? n : 0.0f;
-                    dm[tile][r] = below ? m : 0.0f;
-                    const float f = (on ? n * qk[tile][r] : 0.0f) + (below ? m * kk[tile][r] : 0.0f);
-                    row_flow[r] += f;
-                    column += f;
-                }
-                fine = fine && all_finite(dn) && all_finite(dm[tile]);
-                Four planes[3];
-                split(dn, planes);
+                    for (int r = 0; r < 4; ++r) {
+                        const int i = row * 16 + group * 4 + r;
+                        const bool on = bit_of(before[r], j) && (is_p || j < i);
+                        const float e = decay_of(gates.G[i] - gates.G[j]), v = (is_p ? p.scale : -1.0f) * e * of[tile][r];
+                        d[r] = on ? v : 0.0f;
+                        const float f = on ? v * raw[tile][r] : 0.0f;
+                        row_flow[r] += f;
+                        column += f;
+                    }
+                else d = Acc{};
+                fine = fine && all_finite(d);
+                if (is_p) {
+                    Four planes[3];
+                    split(d, planes);
 #pragma unroll
-                for (int n = 0; n < 3; ++n) {
-                    *reinterpret_cast<Four *>(&dNT[n][j][wave * 16 + group * 4]) = planes[n];
+                    for (int n = 0; n < 3; ++n) {
+                        *reinterpret_cast<Four *>(&dNT[n][j][row * 16 + group * 4]) = planes[n];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) dN[n][wave * 16 + group * 4 + r][j] = planes[n][r];
+                        for (int r = 0; r < 4; ++r) dN[n][row * 16 + group * 4 + r][j] = planes[n][r];
+                    }
+                } else {
+                    dm[tile] = d;
                 }
                 column += __shfl_xor(column, 16);
                 column += __shfl_xor(column, 32);
-                if (group == 0) columns_of[wave][j] = column;
+                if (group == 0) columns_of[(is_p ? 0 : 4) + row][j] = column;
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float v = row_sum(row_flow[r]);
-                if (at == 0) flow[wave * 16 + group * 4 + r] = v;
+                if (at == 0) flow[is_p ? 0 : 1][row * 16 + group * 4 + r] = v;
             }
-            if (!fine) not_finite = 1;
+        };
+        if constexpr (kWaves == 4) {
+            flows(d_of[0], true);
+            flows(d_of[1], false);
+        } else {
+            if (wave < 4) flows(d_of[0], true);
+            else flows(d_of[0], false);
         }
+        if (!fine) not_finite = 1;
         {
-            dot_beta += __shfl_xor(dot_beta, 1);
-            dot_beta += __shfl_xor(dot_beta, 2);
-            if (threadIdx.x % 4 == 0) dbeta[threadIdx.x / 4] = dot_beta;
+            constexpr int kPer = kThreads / kSteps;
+#pragma unroll
+            for (int d = 1; d < kPer; d *= 2) dot_beta += __shfl_xor(dot_beta, d);
+            if (threadIdx.x % kPer == 0) dbeta[threadIdx.x / kPer] = dot_beta;
         }
         // the parts that come from and go to other chunks
         float at_end = 0.0f;
+        if (has_keys) {
+            const int d = wave * 16 + at, from = hk * p.Dk + min(d, p.Dk - 1);
+            const bool key = d < p.Dk;
 #pragma unroll
-        for (int row = 0; row < 4; ++row) {
-            __builtin_amdgcn_sched_barrier(0);
-            float dot[4] = {};
+            for (int row = 0; row < 4; ++row) {
+                __builtin_amdgcn_sched_barrier(0);
+                float dot[4] = {};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = row * 16 + group * 4 + r;
-                const int64_t step = b * p.T + min(chunk * kSteps + i, p.T - 1);
-                const float f = bit_of(alive, i) ? gates.f[i] : 0.0f, t = bit_of(alive, i) ? gates.t[i] : 0.0f;
-#pragma unroll
-                for (int tile = 0; tile < kTiles; ++tile) {
-                    if (!has_keys) continue;
-                    const int d = (wave * kTiles + tile) * 16 + at, from = hk * p.Dk + min(d, p.Dk - 1);
+                for (int r = 0; r < 4; ++r) {
+                    const int i = row * 16 + group * 4 + r;
+                    const int64_t step = b * p.T + min(chunk * kSteps + i, p.T - 1);
+                    const float f = bit_of(alive, i) ? gates.f[i] : 0.0f, t = bit_of(alive, i) ? gates.t[i] : 0.0f;
                     const float k = to_f32(static_cast<const E *>(p.k)[step * p.ld_k + from]), q = to_f32(static_cast<const E *>(p.q)[step * p.ld_q + from]);
-                    const bool key = d < p.Dk;
-                    const float fq = p.scale * f * far_q[tile][row][r], fk = -f * far_k[tile][row][r], e = t * end[tile][row][r];
+                    const float fq = p.scale * f * far_q[row][r], fk = -f * far_k[row][r], e = t * end[row][r];
                     const float to_later = t != 0.0f && key ? k * e : 0.0f;
                     at_end += to_later;
-                    dot[r] += (f != 0.0f && key ? fmaf(q, fq, k * fk) : 0.0f) - to_later;
-                    sum_q[tile][row][r] += f != 0.0f ? fq : 0.0f;
-                    sum_k[tile][row][r] += (f != 0.0f ? fk : 0.0f) + (t != 0.0f ? e : 0.0f);
+                    dot[r] = (f != 0.0f && key ? fmaf(q, fq, k * fk) : 0.0f) - to_later;
+                    sum_q[row][r] += f != 0.0f ? fq : 0.0f;
+                    sum_k[row][r] += (f != 0.0f ? fk : 0.0f) + (t != 0.0f ? e : 0.0f);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float v = row_sum(dot[r]);
+                    if (at == 0) rows_of[wave][row * 16 + group * 4 + r] = v;
                 }
             }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float v = row_sum(dot[r]);
-                if (at == 0) rows_of[wave][row * 16 + group * 4 + r] = v;
-            }
+        } else {
+            rows_of[wave][lane] = 0.0f;
         }
         const float whole = gates.f[kSteps - 1];
         if (whole != 0.0f) at_end = fmaf(whole, dot_states, at_end);
@@ -630,8 +644,13 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
         if (lane == 0) extra[wave] = at_end;
         __syncthreads();
         const bool bad = gates.bad || not_finite;
-        auto key_products = [&](const Plane *a, const Frag *keys, Acc (&sum)[kTiles][4], int which) {
+        auto key_products = [&](const Plane *a, const Frag *keys, Acc (&sum)[4], int which) {
             if (!has_keys) return;
+            Frag key[2][PE];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int n = 0; n < PE; ++n) key[s][n] = keys[frag_at(wave, s, n, 2, PE)];
 #pragma unroll
             for (int row = 0; row < 4; ++row) {
                 __builtin_amdgcn_sched_barrier(0);
@@ -644,21 +663,14 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
                         const int i = row * 16 + hidden * 4 + r;
                         pass[r] = !bit_of(alive, i) ? 0 : (which == 0 ? upto(starts, i) : which == 1 ? from(starts, i) : upto(starts, i) | from(starts, i)) & alive;
                     }
-#pragma unroll
-                    for (int tile = 0; tile < kTiles; ++tile) sum[tile][row] = careful_rows<PE>(sum[tile][row], a, row, keys, wave * kTiles + tile, pass);
+                    sum[row] = careful_rows<PE>(sum[row], a, row, keys, wave, pass);
                 } else {
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         if (which == 0 ? s * 32 > row * 16 + 15 : which == 1 ? s * 32 + 31 < row * 16 : false) continue;       // zeros
                         Frag of_a[3];
                         get_frag(a, row, s, of_a);
-#pragma unroll
-                        for (int tile = 0; tile < kTiles; ++tile) {
-                            Frag key[PE];
-#pragma unroll
-                            for (int n = 0; n < PE; ++n) key[n] = keys[frag_at(wave * kTiles + tile, s, n, 2, PE)];
-                            sum[tile][row] = multiply<3, PE>(of_a, key, sum[tile][row]);
-                        }
+                        sum[row] = multiply<3, PE>(of_a, key[s], sum[row]);
                     }
                 }
             }
@@ -667,9 +679,11 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
         key_products(dNT, QT, sum_k, 1);
         if (wave == 0) {
             const int i = lane, t = chunk * kSteps + i, part = part_of(starts, i);
-            float v = flow[i] - ((columns_of[0][i] + columns_of[1][i]) + (columns_of[2][i] + columns_of[3][i]));
-            v += (rows_of[0][i] + rows_of[1][i]) + (rows_of[2][i] + rows_of[3][i]);
-            if (i == kSteps - 1) v += (extra[0] + extra[1]) + (extra[2] + extra[3]);
+            float v = flow[0][i] + flow[1][i];
+#pragma unroll
+            for (int w = 0; w < 8; ++w) v -= columns_of[w][i];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v += rows_of[w][i] + (i == kSteps - 1 ? extra[w] : 0.0f);
             double s = v;
             for (int d = 1; d < kWave; d *= 2) {
                 const double later = __shfl_down(s, d);
@@ -684,23 +698,26 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
         }
         __syncthreads();
         // X takes the room of dN
+        if (kWaves == 4 || wave >= 4) {
+            const int row = wave % 4;
 #pragma unroll
-        for (int tile = 0; tile < 4; ++tile) {
-            if (tile > wave) continue;
-            Four planes[3];
-            split(dm[tile], planes);
-#pragma unroll
-            for (int n = 0; n < 3; ++n) {
+            for (int tile = 0; tile < 4; ++tile) {
+                if (tile > row) continue;
+                Four planes[3];
+                split(dm[tile], planes);
                 const int j = tile * 16 + at;
-                if (tile < wave) *reinterpret_cast<Four *>(&X[n][j][wave * 16 + group * 4]) = planes[n];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int i = wave * 16 + group * 4 + r;
-                    if (tile < wave) {
-                        X[n][i][j] = planes[n][r];
-                    } else if (j <= i) {               // 0 where j = i
-                        X[n][i][j] = planes[n][r];
-                        X[n][j][i] = planes[n][r];
+                for (int n = 0; n < 3; ++n) {
+                    if (tile < row) *reinterpret_cast<Four *>(&X[n][j][row * 16 + group * 4]) = planes[n];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int i = row * 16 + group * 4 + r;
+                        if (tile < row) {
+                            X[n][i][j] = planes[n][r];
+                        } else if (j <= i) {           // 0 where j = i
+                            X[n][i][j] = planes[n][r];
+                            X[n][j][i] = planes[n][r];
+                        }
                     }
                 }
             }
@@ -713,20 +730,18 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void chunk_grad_kernel(DeltaArgs 
     Row *rows = reinterpret_cast<Row *>(lds);
     typedef E Vec __attribute__((ext_vector_type(8)));
     typedef Vec Loose __attribute__((aligned(sizeof(E))));
-    auto put = [&](Acc (&sum)[kTiles][4], void *to, int64_t ld) {
+    auto put = [&](Acc (&sum)[4], void *to, int64_t ld) {
         __syncthreads();
         if (has_keys)
 #pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile)
+            for (int row = 0; row < 4; ++row)
 #pragma unroll
-                for (int row = 0; row < 4; ++row)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int i = row * 16 + group * 4 + r;
-                        rows[i][(wave * kTiles + tile) * 16 + at] = from_f32<E>(bit_of(alive, i) ? sum[tile][row][r] : 0.0f);
-                    }
+                for (int r = 0; r < 4; ++r) {
+                    const int i = row * 16 + group * 4 + r;
+                    rows[i][wave * 16 + at] = from_f32<E>(bit_of(alive, i) ? sum[row][r] : 0.0f);
+                }
         __syncthreads();
-        for (int e = threadIdx.x; e < kSteps * (DK / 8); e += kDeltaThreads) {
+        for (int e = threadIdx.x; e < kSteps * (DK / 8); e += kThreads) {
             const int i = e / (DK / 8), d = e % (DK / 8) * 8, t = chunk * kSteps + i;
             if (t >= p.T || d >= p.Dk) continue;
             E *out = const_cast<E *>(row_at<E>(to, ld, b, p.T, t, hk, p.Dk)) + d;
@@ -758,7 +773,7 @@ int run(const DeltaArgs &p, hipStream_t stream)
     if (rc || p.chunks == 0) return rc;
     const size_t lds = (6 + kExact<E>) * sizeof(Plane);            // (the results' rows, 64 of DK + 8, are less)
     if (const int failed = make_room_for(reinterpret_cast<const void *>(chunk_grad_kernel<E, DK>), lds)) return failed;
-    hipLaunchKernelGGL((chunk_grad_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
+    hipLaunchKernelGGL((chunk_grad_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(grad_waves(DK) * kWave), lds, stream, p);
     return launched("delta scan gradient");
 }
 
