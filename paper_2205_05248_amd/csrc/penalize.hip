@@ -28,76 +28,120 @@ struct PenalizeArgs {
     int64_t ld_out;
 };
 
-constexpr unsigned kSeen = 0x80000000u, kBiased = 0x40000000u, kCount = 0x3fffffffu;
+// A place's word: how often it was generated (L < 2^24), whether it stood in the prompt, whether it has a bias.
+constexpr unsigned kPrompt = 0x80000000u, kBiased = 0x40000000u, kCount = 0x00ffffffu;
 
-// A place's word: whether it was seen, whether it has a bias, and how often it was generated (L < 2^24).
+// The biases of a piece, in their order.
+struct BiasList {
+    int n, at[kMostBiases];
+    float value[kMostBiases];
+};
+
+// The loads of the piece's logits and bits go out first; the history is counted while they are on their way.  777 rows of 50021 in fp16 with
+// histories of 4096 on average: see the entry point for times and pieces.
 template <typename E, int THREADS, int PIECE>
 __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
 {
     typedef Piece<E> P;
-    constexpr int V = P::V;
-    __shared__ __attribute__((aligned(16))) unsigned words[PIECE];
+    constexpr int V = P::V, kVectors = PIECE / THREADS / V, kBatch = 4;
+    typedef int Tokens __attribute__((ext_vector_type(4)));
+    typedef Tokens LooseTokens __attribute__((aligned(4)));
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    unsigned *words = reinterpret_cast<unsigned *>(lds);
+    BiasList &biases = *reinterpret_cast<BiasList *>(words + PIECE);
     const int64_t row = blockIdx.x / p.pieces;
     const int piece = blockIdx.x % p.pieces;
     const E *l = static_cast<const E *>(p.logits) + row * p.ld;
     E *out = static_cast<E *>(p.out) + row * p.ld_out;
     const int skew = skew_of(out);                                     // entry j of the row is skew + j
     const int n = p.V + skew, begin = piece * PIECE, end = min(begin + PIECE, n);
+    const int own = begin + (int)threadIdx.x * V;                      // vector q of the thread begins q THREADS V behind
+    l -= skew;
+    out -= skew;
+    typename P::Vec z_raw[kVectors];
+#pragma unroll
+    for (int q = 0; q < kVectors; ++q) {
+        const int j = own + q * THREADS * V;
+        if (j >= skew && j + V <= n) {
+            z_raw[q] = *reinterpret_cast<const typename P::Loose *>(l + j);
+        } else if (j < end) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) z_raw[q][k] = j + k >= skew && j + k < n ? l[j + k] : (E)0.0f;
+        }
+    }
+    unsigned bits[kVectors];
+    if (p.allowed) {
+        const uint32_t *allowed = p.allowed + row * p.ld_allowed;
+        const int last = (p.V - 1) / 32;
+#pragma unroll
+        for (int q = 0; q < kVectors; ++q) {
+            const int e = own + q * THREADS * V - skew, low = max(e, 0);
+            const uint64_t pair = (uint64_t)allowed[min(low / 32 + 1, last)] << 32 | allowed[min(low / 32, last)];
+            bits[q] = (unsigned)(pair >> (low % 32));
+            if (e < 0) bits[q] <<= min(-e, 31);                        // (before the row nothing is written)
+        }
+    }
     const int length = p.length ? min(max(p.length[row], 0), p.L) : p.L;
     const int prompt = p.prompt ? min(max(p.prompt[row], 0), length) : 0;
+    const float rho = p.repetition ? p.repetition[row] : 1.0f, presence = p.presence ? p.presence[row] : 0.0f;
+    const float frequency = p.frequency ? p.frequency[row] : 0.0f;
     const bool counts = length > 0 || p.M > 0;
     if (counts) {
         for (int w = threadIdx.x * 4; w < end - begin; w += THREADS * 4) *reinterpret_cast<uint4 *>(words + w) = make_uint4(0, 0, 0, 0);
         __syncthreads();
         const int32_t *history = p.history + row * p.ld_history;
-        for (int t = threadIdx.x; t < length; t += THREADS) {
-            const int id = history[t];
-            const int at = id + skew - begin;                          // no place of the piece if the id is none of the row
-            if (id >= 0 && id < p.V && at >= 0 && at < end - begin) {
-                atomicOr(&words[at], kSeen);
+        const int before = skew - begin;                               // place of an id in the piece, if it has one
+        auto count = [&](int t, int id) {
+            const int at = id + before;
+            if (id >= 0 && id < p.V && at >= 0 && at < end - begin && t < length) {
                 if (t >= prompt) atomicAdd(&words[at], 1u);
+                else atomicOr(&words[at], kPrompt);
             }
+        };
+        for (int base = 0; base < length; base += THREADS * 4 * kBatch) {
+            Tokens ids[kBatch];
+#pragma unroll
+            for (int q = 0; q < kBatch; ++q) {
+                const int t = base + (q * THREADS + (int)threadIdx.x) * 4;
+                if (t + 4 <= length) {
+                    ids[q] = *reinterpret_cast<const LooseTokens *>(history + t);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) ids[q][k] = t + k < length ? history[t + k] : -1;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < kBatch; ++q)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) count(base + (q * THREADS + (int)threadIdx.x) * 4 + k, ids[q][k]);
         }
-        for (int m = threadIdx.x; m < p.M; m += THREADS) {
-            const int id = p.bias_id[row * p.M + m];
-            const int at = id + skew - begin;
-            if (id >= 0 && id < p.V && at >= 0 && at < end - begin) atomicOr(&words[at], kBiased);
+        if (p.M > 0 && threadIdx.x < kWave) {                          // one wave keeps the order
+            int m = 0;
+            for (int base = 0; base < p.M; base += kWave) {
+                const int k = base + (int)threadIdx.x;
+                const int id = k < p.M ? p.bias_id[row * p.M + k] : -1, at = id + before;
+                const bool in = id >= 0 && id < p.V && at >= 0 && at < end - begin;
+                const unsigned long long all = __ballot(in);
+                if (in) {
+                    const int to = m + __popcll(all & ((1ull << threadIdx.x) - 1));
+                    biases.at[to] = at;
+                    biases.value[to] = p.bias_value[row * p.M + k];
+                    atomicOr(&words[at], kBiased);
+                }
+                m += __popcll(all);
+            }
+            if (threadIdx.x == 0) biases.n = m;
         }
         __syncthreads();
     }
-    const float rho = p.repetition ? p.repetition[row] : 1.0f, presence = p.presence ? p.presence[row] : 0.0f;
-    const float frequency = p.frequency ? p.frequency[row] : 0.0f;
-    const uint32_t *allowed = p.allowed ? p.allowed + row * p.ld_allowed : nullptr;
-    l -= skew;
-    out -= skew;
-    auto edit = [&](float z, unsigned word, int j) {
-        if (word & kSeen) z = z > 0.0f ? z / rho : z * rho;
-        const unsigned c = word & kCount;
-        if (c) z = (z - presence) - frequency * (float)c;
-        if (word & kBiased)
-            for (int m = 0; m < p.M; ++m)                              // in their order, whichever thread set the bit
-                if (p.bias_id[row * p.M + m] == j - skew) z += p.bias_value[row * p.M + m];
-        return z;
-    };
-    // bits of the V places from entry j - skew of the row on
-    auto bits_of = [&](int j) {
-        const int e = j - skew, last = (p.V - 1) / 32;
-        const int low = max(e, 0);
-        const uint64_t pair = (uint64_t)allowed[min(low / 32 + 1, last)] << 32 | allowed[min(low / 32, last)];
-        const unsigned bits = (unsigned)(pair >> (low % 32));
-        return e < 0 ? bits << min(-e, 31) : bits;                     // (before the row nothing is written)
-    };
-    for (int j = begin + (int)threadIdx.x * V; j < end; j += THREADS * V) {
-        const bool whole = j >= skew && j + V <= n;
+    const float inverse = 1.0f / rho;
+#pragma unroll
+    for (int q = 0; q < kVectors; ++q) {
+        const int j = own + q * THREADS * V;
+        if (j >= end) continue;
         float z[V];
-        if (whole) {
-            const typename P::Vec v = *reinterpret_cast<const typename P::Loose *>(l + j);
 #pragma unroll
-            for (int k = 0; k < V; ++k) z[k] = to_f32(v[k]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < V; ++k) z[k] = j + k >= skew && j + k < n ? to_f32(l[j + k]) : 0.0f;
-        }
+        for (int k = 0; k < V; ++k) z[k] = to_f32(z_raw[q][k]);
         if (counts) {
             unsigned w[V], any = 0;
 #pragma unroll
@@ -106,25 +150,37 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
                 w[k] = four.x; w[k + 1] = four.y; w[k + 2] = four.z; w[k + 3] = four.w;
                 any |= four.x | four.y | four.z | four.w;
             }
-            if (any)
+            if (any) {
 #pragma unroll
-                for (int k = 0; k < V; ++k)
-                    if (w[k] && j + k >= skew && j + k < n) z[k] = edit(z[k], w[k], j + k);
+                for (int k = 0; k < V; ++k) {
+                    // z / rho from its reciprocal, corrected by what is left over: as near as a division, which is four times as long
+                    const float guess = z[k] * inverse, divided = fmaf(fmaf(-guess, rho, z[k]), inverse, guess);
+                    const bool usual = fabsf(z[k]) < 1e30f && fabsf(z[k]) > 1e-30f;
+                    const float less = z[k] > 0.0f ? (usual ? divided : guess) : z[k] * rho;
+                    const unsigned c = w[k] & kCount;
+                    const float seen = w[k] & (kPrompt | kCount) ? less : z[k];
+                    z[k] = c ? (seen - presence) - frequency * (float)c : seen;
+                }
+                if (any & kBiased)
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        if (w[k] & kBiased)
+                            for (int m = 0; m < biases.n; ++m)
+                                if (biases.at[m] == j - begin + k) z[k] += biases.value[m];
+            }
         }
-        if (allowed) {
-            const unsigned bits = bits_of(j);
+        if (p.allowed)
 #pragma unroll
-            for (int k = 0; k < V; ++k) z[k] = bits >> k & 1 ? z[k] : -kInf;
-        }
-        if (whole) {
-            typename P::Vec v;
+            for (int k = 0; k < V; ++k) z[k] = bits[q] >> k & 1 ? z[k] : -kInf;
+        typename P::Vec v;
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = from_f32<E>(z[k]);
+        for (int k = 0; k < V; ++k) v[k] = from_f32<E>(z[k]);
+        if (j >= skew && j + V <= n) {
             *reinterpret_cast<typename P::Loose *>(out + j) = v;
         } else {
 #pragma unroll
             for (int k = 0; k < V; ++k)
-                if (j + k >= skew && j + k < n) out[j + k] = from_f32<E>(z[k]);
+                if (j + k >= skew && j + k < n) out[j + k] = v[k];
         }
     }
 }
@@ -156,16 +212,22 @@ int marl_penalize(int32_t dtype, int32_t R, int32_t V, const void *logits, int64
     p.allowed = reinterpret_cast<const uint32_t *>(allowed); p.ld_allowed = ld_allowed; p.out = out; p.ld_out = ld_out;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return with_dtype(dtype, [&](auto e) {
-        // pieces are counted from the line that the row's result begins in: up to 127 bytes before it
-        constexpr int kSmall = 1024, kLarge = 8192;
-        const bool small = V <= kSmall - 64;
-        const int piece = small ? kSmall : kLarge;
-        p.pieces = (int)(((int64_t)V + 63 + piece - 1) / piece);
-        if ((int64_t)R * p.pieces >= ((int64_t)1 << 31)) return (int)MARL_ERR_BAD_DIM;
-        const dim3 grid((unsigned)((int64_t)R * p.pieces));
-        if (small) hipLaunchKernelGGL((penalize_kernel<decltype(e), 64, kSmall>), grid, dim3(64), 0, stream, p);
-        else hipLaunchKernelGGL((penalize_kernel<decltype(e), 512, kLarge>), grid, dim3(512), 0, stream, p);
-        return launched("penalize");
+        // pieces are counted from the line that the row's result begins in: up to 127 bytes before it.  Every piece reads the history, so they
+        // are as large as shared memory allows two of at a time, unless that leaves too few for the chip
+        const auto go = [&](auto kernel, int threads, int piece) {
+            const size_t lds = piece * sizeof(unsigned) + (M > 0 ? sizeof(BiasList) : 0);
+            if (lds > 64 * 1024) {                     // more than that has to be asked for
+                const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+                if (err != hipSuccess) return report_device_error(err, "hipFuncSetAttribute");
+            }
+            p.pieces = (int)(((int64_t)V + 63 + piece - 1) / piece);
+            if ((int64_t)R * p.pieces >= ((int64_t)1 << 31)) return (int)MARL_ERR_BAD_DIM;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)R * p.pieces)), dim3(threads), lds, stream, p);
+            return launched("penalize");
+        };
+        if (V <= 1024 - 64) return go(penalize_kernel<decltype(e), 64, 1024>, 64, 1024);
+        if ((int64_t)R * V < (int64_t)512 * 8192) return go(penalize_kernel<decltype(e), 512, 8192>, 512, 8192);
+        return go(penalize_kernel<decltype(e), 1024, 16384>, 1024, 16384);
     });
 }
 
