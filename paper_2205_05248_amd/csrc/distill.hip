@@ -66,20 +66,33 @@ __device__ __forceinline__ RowSums row_sums(Sum kept, Sum rest)
 }
 
 // An alternative as a lane holds it.
-struct Kept { int id; float value, z; bool is; };
+struct Kept { int id; float value, z, logit; bool is; };
+// listed_at: what is listed, asked for before the row is there; kept_of: what the row, which may be in shared memory, says to it.
+__device__ __forceinline__ Kept listed_at(const DistillArgs &p, int64_t row, int k)
+{
+    Kept a{-1, -kInf, -kInf, -kInf, false};
+    if (k < p.K) {
+        a.id = p.top_id[row * p.K + k];
+        a.value = p.top_value[row * p.K + k];
+    }
+    return a;
+}
+template <typename E>
+__device__ __forceinline__ void kept_of(const DistillArgs &p, Kept &a, const E *l, const uint8_t *av)
+{
+    const bool in = a.id >= 0 && a.id < p.V;
+    a.id = in ? a.id : -1;
+    const bool available = in && (!av || av[a.id]);
+    a.logit = available ? to_f32(l[a.id]) : -kInf;
+    a.is = available && !(a.logit < p.lowest);
+    a.value = !a.is ? -kInf : a.value == kInf ? __builtin_nanf("") : a.value;
+    a.z = a.is ? rounded(p.scale, a.logit) : -kInf;
+}
 template <typename E>
 __device__ __forceinline__ Kept kept_at(const DistillArgs &p, const E *l, const uint8_t *av, int64_t row, int k)
 {
-    Kept a{-1, -kInf, -kInf, false};
-    if (k >= p.K) return a;
-    a.id = p.top_id[row * p.K + k];
-    if (a.id < 0 || a.id >= p.V) { a.id = -1; return a; }
-    const float logit = to_f32(l[a.id]);
-    a.is = (!av || av[a.id]) && !(logit < p.lowest);
-    if (!a.is) return a;
-    a.value = p.top_value[row * p.K + k];
-    if (a.value == kInf) a.value = __builtin_nanf("");
-    a.z = rounded(p.scale, logit);
+    Kept a = listed_at(p, row, k);
+    kept_of(p, a, l, av);
     return a;
 }
 
@@ -180,7 +193,7 @@ __device__ __forceinline__ void take(Sum &st, const float (&l)[N], float scale)
 }
 
 template <typename E>
-__global__ __launch_bounds__(kThreads) void long_rows_kernel(DistillArgs p)
+__global__ __launch_bounds__(kThreads, 8) void long_rows_kernel(DistillArgs p)
 {
     constexpr int V = Piece<E>::V;
     __shared__ Listed listed;
@@ -195,28 +208,30 @@ __global__ __launch_bounds__(kThreads) void long_rows_kernel(DistillArgs p)
     if (av) av -= skew;
     const int64_t begin = (int64_t)piece * p.per * kChunk, end = piece + 1 < p.parts ? begin + (int64_t)p.per * kChunk : n;
     listed.mark(p, row, skew, begin, end);
-    auto read = [&](int j, float *to) {
-        read_piece<E>(l, av, j, skew, n, to);
-        const unsigned out = listed.of<V>(j - (int)begin);
-        if (out)
-#pragma unroll
-            for (int k = 0; k < V; ++k) to[k] = out >> k & 1 ? -kInf : to[k];
-    };
     Sum st{-kInf, 0.0f};
     int64_t base = begin;
     for (; base + kChunk <= end; base += kChunk) {
         float held[kHeld];
+        unsigned out = 0;
 #pragma unroll
-        for (int q = 0; q < kHeld / V; ++q) read((int)base + (q * kThreads + (int)threadIdx.x) * V, held + q * V);
+        for (int q = 0; q < kHeld / V; ++q) {
+            const int j = (int)base + (q * kThreads + (int)threadIdx.x) * V;
+            read_piece<E>(l, av, j, skew, n, held + q * V);
+            out |= listed.of<V>(j - (int)begin) << (q * V);
+        }
+        if (out)                                       // (once for all pieces: a branch between their loads would wait for each)
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) held[k] = out >> k & 1 ? -kInf : held[k];
         take(st, held, p.scale);
     }
     for (; base + wave * (kWave * V) < end; base += kThreads * V) {    // what is left: a piece at a time, and no more than there are
         float some[V];
         const int j = (int)base + (int)threadIdx.x * V;
-        if (j < end) read(j, some);
-        else
+        read_piece<E>(l, av, j, skew, n, some);
+        const unsigned out = j < end ? listed.of<V>(j - (int)begin) : 0;
+        if (out)
 #pragma unroll
-            for (int k = 0; k < V; ++k) some[k] = -kInf;
+            for (int k = 0; k < V; ++k) some[k] = out >> k & 1 ? -kInf : some[k];
         take(st, some, p.scale);
     }
     st = join_wave(st);
@@ -353,7 +368,7 @@ __global__ __launch_bounds__(kThreads) void long_grad_kernel(DistillArgs p)
 }
 
 // ---------------------------------------------------------------------------------- short rows
-// G lanes hold a row of at most G N logits; lane `sub` of them looks at alternatives sub, sub + G, ...
+// G lanes hold a row of at most G N logits; lane `sub` of them looks at alternatives sub, sub + G, ..., of which the first stays with it.
 template <int G>
 struct ShortTeacher {
     Teacher t;
@@ -361,24 +376,28 @@ struct ShortTeacher {
     unsigned marked;                                   // of the lane's own entries j G + sub, bit j
 };
 template <typename E, int G>
-__device__ __forceinline__ ShortTeacher<G> short_teacher(const DistillArgs &p, const E *l, const uint8_t *av, int64_t row, bool there)
+__device__ __forceinline__ ShortTeacher<G> short_teacher(const DistillArgs &p, Kept &first, const E *l, const uint8_t *av, int64_t row, bool there)
 {
     const int lane = threadIdx.x % kWave, sub = lane % G;
     ShortTeacher<G> s{{-kInf, 0.0f, 0.0f}, 0.0f, 0};
-    for (int base = 0; base < p.K; base += G) {
-        const Kept a = there ? kept_at(p, l, av, row, base + sub) : Kept{-1, -kInf, -kInf, false};
+    if (!there) first.id = -1;
+    kept_of(p, first, l, av);
+    Kept a = first;
+    for (int base = 0;;) {
         for (int k = 0; k < G && base + k < p.K; ++k) {
             const int id = __shfl(a.id, lane - sub + k);
-            if (id >= 0 && id % G == sub) s.marked |= 1u << (id / G);
+            s.marked |= id >= 0 && id % G == sub ? 1u << (id / G) : 0u;
         }
         if (p.tail) {
             s.sum += a.is ? expf(a.value) : 0.0f;
         } else {
-            const float top = max_nan(s.t.top, a.is ? a.value : -kInf);
+            const float top = max_nan(s.t.top, a.value);
             if (!(top == s.t.top)) s.t.total *= s.t.top == -kInf ? 0.0f : expf(s.t.top - top);
             s.t.top = top;
             s.t.total += a.is && a.value != -kInf ? expf(a.value - top) : 0.0f;
         }
+        if ((base += G) >= p.K) break;
+        a = there ? kept_at(p, l, av, row, base + sub) : Kept{-1, -kInf, -kInf, -kInf, false};
     }
     if (p.tail) {
         s.sum = all_lanes<G>(s.sum, add);
@@ -392,6 +411,18 @@ __device__ __forceinline__ ShortTeacher<G> short_teacher(const DistillArgs &p, c
     return s;
 }
 
+// Where a row and its mask lie in the room that a wave's rows were brought to.
+template <typename E, int G, int N>
+__device__ __forceinline__ const E *row_in(const DistillArgs &p, const FlatRows<E, G, N> &rows, int64_t first, int64_t row)
+{
+    return rows.entries + (int)((reinterpret_cast<uintptr_t>(static_cast<const E *>(p.logits) + first * p.V) & 15) / sizeof(E)) + (int)(row - first) * p.V;
+}
+template <typename E, int G, int N>
+__device__ __forceinline__ const uint8_t *mask_in(const DistillArgs &p, const FlatRows<E, G, N> &rows, int64_t first, int64_t row)
+{
+    return !p.avail || p.ld_avail == 0 ? p.avail : rows.mask + (int)(reinterpret_cast<uintptr_t>(p.avail + first * p.V) & 15) + (int)(row - first) * p.V;
+}
+
 template <typename E, int G, int N, bool FLAT>
 __global__ __launch_bounds__(kThreads) void short_rows_kernel(DistillArgs p)
 {
@@ -399,12 +430,16 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(DistillArgs p)
     const int64_t first = ((int64_t)blockIdx.x * (kThreads / kWave) + wave) * (kWave / G), row = first + lane / G;
     if (first >= p.R) return;                                          // the whole wave
     const bool there = row < p.R;
-    const E *l = static_cast<const E *>(p.logits) + (there ? row : 0) * p.ld;
-    const uint8_t *av = p.avail ? p.avail + (there ? row : 0) * p.ld_avail : nullptr;
+    const int64_t own = there ? row : first;
+    const E *l = static_cast<const E *>(p.logits) + own * p.ld;
+    const uint8_t *av = p.avail ? p.avail + own * p.ld_avail : nullptr;
+    __shared__ __attribute__((aligned(16))) FlatRows<E, FLAT ? G : 1, FLAT ? N : 1> rows[FLAT ? kThreads / kWave : 1];
+    Kept listed = listed_at(p, own, sub);
     float held[N];
     if constexpr (FLAT) {
-        __shared__ __attribute__((aligned(16))) FlatRows<E, G, N> rows[kThreads / kWave];
         rows[wave].read(p, first, row, there, -1, held);
+        l = row_in(p, rows[wave], first, own);
+        av = mask_in(p, rows[wave], first, own);
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -412,7 +447,7 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(DistillArgs p)
             held[j] = there && k < p.V && (!av || av[k]) ? to_f32(l[k]) : -kInf;
         }
     }
-    const ShortTeacher<G> s = short_teacher<E, G>(p, l, av, row, there);
+    const ShortTeacher<G> s = short_teacher<E, G>(p, listed, l, av, own, there);
     float top_in = -kInf, top_out = -kInf;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -433,7 +468,7 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(DistillArgs p)
     const RowSums r = row_sums(kept, rest);
     float loss = 0.0f;
     for (int base = 0; base < p.K; base += G) {
-        const Kept a = there ? kept_at(p, l, av, row, base + sub) : Kept{-1, -kInf, -kInf, false};
+        const Kept a = base == 0 ? listed : there ? kept_at(p, l, av, own, base + sub) : Kept{-1, -kInf, -kInf, -kInf, false};
         const float prob = a.is ? probability(s.t, p.tail, a.value) : 0.0f;
         loss += part_of_loss(prob, p.tail ? a.value : (a.value - s.t.top) - s.t.log_total, (a.z - r.M) - r.log_s);
     }
@@ -453,9 +488,12 @@ __global__ __launch_bounds__(kThreads) void short_grad_kernel(DistillArgs p)
     const uint8_t *av = p.avail ? p.avail + own * p.ld_avail : nullptr;
     E *out = static_cast<E *>(p.grad_logits) + own * p.ld_grad;
     __shared__ __attribute__((aligned(16))) FlatRows<E, FLAT ? G : 1, FLAT ? N : 1> rows[FLAT ? kThreads / kWave : 1];
+    Kept listed = listed_at(p, own, sub);
     float held[N];
     if constexpr (FLAT) {
         rows[wave].read(p, first, row, there, -1, held);
+        l = row_in(p, rows[wave], first, own);
+        av = mask_in(p, rows[wave], first, own);
     } else {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -463,27 +501,37 @@ __global__ __launch_bounds__(kThreads) void short_grad_kernel(DistillArgs p)
             held[j] = there && k < p.V && (!av || av[k]) ? to_f32(l[k]) : -kInf;
         }
     }
-    const ShortTeacher<G> s = short_teacher<E, G>(p, l, av, own, there);
+    const ShortTeacher<G> s = short_teacher<E, G>(p, listed, l, av, own, there);
     const RowGrad g = row_grad(p, own, s.sum);
     constexpr int kRounds = kMostKept / G;                             // the kept ones' logits are read before any is overwritten
     int ids[kRounds];
     float grads[kRounds];
+    {                                                                  // listed twice: both parts
+        const float prob = listed.is ? probability(s.t, p.tail, listed.value) : 0.0f;
+        float sum = 0.0f;
+        for (int k = 0; k < G && k < p.K; ++k) {
+            const int id = __shfl(listed.id, lane - sub + k);
+            const float part = __shfl(prob, lane - sub + k);
+            sum += id == listed.id ? part : 0.0f;
+        }
+        ids[0] = listed.id;
+        grads[0] = sum;
+    }
 #pragma unroll
     for (int c = 0; c < kRounds; ++c) {
-        ids[c] = -1;
+        if (c > 0) ids[c] = -1;
         if (c * G >= p.K) continue;
-        const Kept a = there ? kept_at(p, l, av, own, c * G + sub) : Kept{-1, -kInf, -kInf, false};
-        if (a.id < 0) continue;
-        ids[c] = a.id;
-        grads[c] = 0.0f;
-        if (!a.is) continue;
-        float prob = 0.0f;
-        for (int k = 0; k < p.K; ++k)                                  // listed twice: both parts
-            if (p.top_id[own * p.K + k] == a.id) {
-                const float value = p.top_value[own * p.K + k];
-                prob += probability(s.t, p.tail, value == kInf ? __builtin_nanf("") : value);
-            }
-        grads[c] = kept_grad(g, to_f32(l[a.id]), prob, p.scale, p.lowest);
+        const Kept a = c == 0 ? listed : there ? kept_at(p, l, av, own, c * G + sub) : Kept{-1, -kInf, -kInf, -kInf, false};
+        if (c > 0) ids[c] = a.id, grads[c] = 0.0f;
+        if (p.K > G && a.is) {
+            grads[c] = 0.0f;
+            for (int k = 0; k < p.K; ++k)
+                if (p.top_id[own * p.K + k] == a.id) {
+                    const float value = p.top_value[own * p.K + k];
+                    grads[c] += probability(s.t, p.tail, value == kInf ? __builtin_nanf("") : value);
+                }
+        }
+        grads[c] = a.is ? kept_grad(g, a.logit, grads[c], p.scale, p.lowest) : 0.0f;
     }
     wave_sync();                                                       // all of the row is read before any of it is overwritten
     E *to = out;
@@ -499,7 +547,7 @@ __global__ __launch_bounds__(kThreads) void short_grad_kernel(DistillArgs p)
     }
 #pragma unroll
     for (int c = 0; c < kRounds; ++c)
-        if (there && ids[c] >= 0) to[ids[c]] = from_f32<E>(grads[c]);
+        if (c * G < p.K && there && ids[c] >= 0) to[ids[c]] = from_f32<E>(grads[c]);
     if constexpr (FLAT) {
         wave_sync();
         bring_back<E, kWave * N>(static_cast<E *>(p.grad_logits), first * p.V, (int)min((int64_t)(kWave / G), p.R - first) * p.V, skew, rows[wave].entries);
