@@ -136,15 +136,13 @@ __device__ __forceinline__ Teacher teacher_of(const Kept &a)
     return t;
 }
 
-// A wave finishes a row from the sum over the places that are not listed.
-template <typename E>
-__device__ __forceinline__ void finish_row(const DistillArgs &p, int64_t row, Sum rest)
+// A wave finishes a row from the sum over the places that are not listed and the alternatives that its lanes hold.
+__device__ __forceinline__ void finish_row(const DistillArgs &p, int64_t row, Sum rest, const Kept &a)
 {
-    const E *l = static_cast<const E *>(p.logits) + row * p.ld;
-    const Kept a = kept_at(p, l, p.avail ? p.avail + row * p.ld_avail : nullptr, row, threadIdx.x % kWave);
+    const bool met = met_before(a.id, p.K);            // (in all lanes: it reads them)
     Sum kept;
     kept.m = all_lanes<kWave>(a.z, max_nan);
-    kept.s = all_lanes<kWave>(a.is && !met_before(a.id, p.K) ? exp_of(a.z - kept.m) : 0.0f, add);
+    kept.s = all_lanes<kWave>(a.is && !met ? exp_of(a.z - kept.m) : 0.0f, add);
     const RowSums r = row_sums(kept, rest);
     const Teacher t = teacher_of(a);
     const float prob = a.is ? probability(t, p.tail, a.value) : 0.0f;
@@ -162,14 +160,13 @@ constexpr int kMostChunks = 16;                        // of a part: its places 
 // The listed places of a part of a row as bits, counted from `begin`.
 struct Listed {
     unsigned bits[kMostChunks * kChunk / 32];
-    // ids of entries of the row, which begins `skew` behind where places are counted from
-    __device__ __forceinline__ void mark(const DistillArgs &p, int64_t row, int skew, int64_t begin, int64_t end)
+    // id: the thread's alternative; the row begins `skew` behind where places are counted from
+    __device__ __forceinline__ void mark(const DistillArgs &p, int id, int skew, int64_t begin, int64_t end)
     {
         const int words = (int)((end - begin + 31) / 32);
         for (int w = threadIdx.x; w < words; w += kThreads) bits[w] = 0;
         __syncthreads();
         if ((int)threadIdx.x < p.K) {
-            const int id = p.top_id[row * p.K + threadIdx.x];
             const int64_t at = id + (int64_t)skew - begin;
             if (id >= 0 && id < p.V && at >= 0 && at < end - begin) atomicOr(&bits[at / 32], 1u << (at % 32));
         }
@@ -207,7 +204,7 @@ __global__ __launch_bounds__(kThreads, 8) void long_rows_kernel(DistillArgs p)
     l -= skew;
     if (av) av -= skew;
     const int64_t begin = (int64_t)piece * p.per * kChunk, end = piece + 1 < p.parts ? begin + (int64_t)p.per * kChunk : n;
-    listed.mark(p, row, skew, begin, end);
+    listed.mark(p, listed_at(p, row, threadIdx.x).id, skew, begin, end);
     Sum st{-kInf, 0.0f};
     int64_t base = begin;
     for (; base + kChunk <= end; base += kChunk) {
@@ -247,7 +244,7 @@ __global__ __launch_bounds__(kThreads, 8) void long_rows_kernel(DistillArgs p)
             to[0] = st.m; to[1] = st.s;
         }
     } else {
-        finish_row<E>(p, row, st);
+        finish_row(p, row, st, kept_at(p, l + skew, av ? av + skew : nullptr, row, lane));
     }
 }
 
@@ -256,12 +253,13 @@ template <typename E>
 __global__ __launch_bounds__(kWave) void join_kernel(DistillArgs p)
 {
     const int64_t row = blockIdx.x;
+    const Kept mine = kept_at(p, static_cast<const E *>(p.logits) + row * p.ld, p.avail ? p.avail + row * p.ld_avail : nullptr, row, threadIdx.x);
     Sum st{-kInf, 0.0f};
     for (int k = threadIdx.x; k < p.parts; k += kWave) {
         const float *from = p.stats + (row * p.parts + k) * 2;
         st = join(st, {from[0], from[1]});
     }
-    finish_row<E>(p, row, join_wave(st));
+    finish_row(p, row, join_wave(st), mine);
 }
 
 // What the gradient of a row needs: places that are not kept get C e^(z - base), kept ones W e^(z - log_sum) - p, all times `by`.
@@ -309,8 +307,8 @@ __global__ __launch_bounds__(kThreads) void long_grad_kernel(DistillArgs p)
     const E *l = static_cast<const E *>(p.logits) + row * p.ld;
     const uint8_t *av = p.avail ? p.avail + row * p.ld_avail : nullptr;
     E *out = static_cast<E *>(p.grad_logits) + row * p.ld_grad;
+    const Kept a = kept_at(p, l, av, row, threadIdx.x);
     if (threadIdx.x < kWave) {
-        const Kept a = kept_at(p, l, av, row, threadIdx.x);
         const Teacher t = teacher_of(a);
         const float prob = a.is ? probability(t, p.tail, a.value) : 0.0f, sum = all_lanes<kWave>(prob, add);
         ids[threadIdx.x] = a.is ? a.id : -1;
@@ -326,7 +324,7 @@ __global__ __launch_bounds__(kThreads) void long_grad_kernel(DistillArgs p)
     for (int64_t from = (int64_t)piece * span; from < stop; from += kMostChunks * kChunk) {
         const int64_t to = from + kMostChunks * kChunk < stop ? from + kMostChunks * kChunk : stop;
         __syncthreads();
-        listed.mark(p, row, skew, from, to);
+        listed.mark(p, a.id, skew, from, to);
         const RowGrad g = row_grad(p, row, total);
         auto put = [&](const float *held, int j) {
             typename P::Vec v;
