@@ -28,17 +28,17 @@ struct PenalizeArgs {
     int64_t ld_out;
 };
 
-// A place's word: how often it was generated (L < 2^24), whether it stood in the prompt, whether it has a bias.
+// A place's word: how often it was generated (L < 2^24), which bias it has, whether it has one, whether it stood in the prompt.
 constexpr unsigned kPrompt = 0x80000000u, kBiased = 0x40000000u, kCount = 0x00ffffffu;
+constexpr int kBiasShift = 24, kNumbered = 64;         // with more biases than that in a piece a place looks for its own
 
-// The biases of a piece, in their order.
+// The biases of a piece, in their order; where they are numbered, that of a place's first entry is the sum of all of its entries.
 struct BiasList {
-    int n, at[kMostBiases];
-    float value[kMostBiases];
+    int *n, *at;
+    float *value;                                      // [M] each
 };
 
-// The loads of the piece's logits and bits go out first; the history is counted while they are on their way.  777 rows of 50021 in fp16 with
-// histories of 4096 on average: see the entry point for times and pieces.
+// The loads of the piece's logits, bits, first tokens and biases go out first; the history is counted while they are on their way.
 template <typename E, int THREADS, int PIECE>
 __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
 {
@@ -48,9 +48,10 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
     typedef Tokens LooseTokens __attribute__((aligned(4)));
     extern __shared__ __attribute__((aligned(16))) char lds[];
     unsigned *words = reinterpret_cast<unsigned *>(lds);
-    BiasList &biases = *reinterpret_cast<BiasList *>(words + PIECE);
+    int *lists_at = reinterpret_cast<int *>(words + PIECE);
+    const BiasList biases{lists_at, lists_at + 1, reinterpret_cast<float *>(lists_at + 1 + p.M)};
     const int64_t row = blockIdx.x / p.pieces;
-    const int piece = blockIdx.x % p.pieces;
+    const int piece = blockIdx.x % p.pieces, lane = threadIdx.x % kWave;
     const E *l = static_cast<const E *>(p.logits) + row * p.ld;
     E *out = static_cast<E *>(p.out) + row * p.ld_out;
     const int skew = skew_of(out);                                     // entry j of the row is skew + j
@@ -71,15 +72,37 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
     }
     unsigned bits[kVectors];
     if (p.allowed) {
+        typedef uint64_t LooseWord __attribute__((aligned(4)));
         const uint32_t *allowed = p.allowed + row * p.ld_allowed;
         const int last = (p.V - 1) / 32;
 #pragma unroll
         for (int q = 0; q < kVectors; ++q) {
-            const int e = own + q * THREADS * V - skew, low = max(e, 0);
-            const uint64_t pair = (uint64_t)allowed[min(low / 32 + 1, last)] << 32 | allowed[min(low / 32, last)];
-            bits[q] = (unsigned)(pair >> (low % 32));
+            const int e = own + q * THREADS * V - skew, low = min(max(e, 0), p.V - 1), word = min(low / 32, max(last - 1, 0));
+            const uint64_t two = last > 0 ? *reinterpret_cast<const LooseWord *>(allowed + word) : allowed[0];
+            bits[q] = (unsigned)(two >> (low - word * 32));
             if (e < 0) bits[q] <<= min(-e, 31);                        // (before the row nothing is written)
         }
+    }
+    // the first tokens and biases too, whatever the row's length is
+    Tokens first[kBatch];
+    auto tokens_at = [&](Tokens &to, int t, int most) {
+        const int32_t *history = p.history + row * p.ld_history;
+        if (t + 4 <= most) {
+            to = *reinterpret_cast<const LooseTokens *>(history + t);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) to[k] = t + k < most ? history[t + k] : -1;
+        }
+    };
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+        if (q * THREADS * 4 < p.L) tokens_at(first[q], (q * THREADS + (int)threadIdx.x) * 4, p.L);
+    const bool lists = threadIdx.x >= THREADS - kWave;                 // the last wave, which has the fewest tokens
+    int bias_id = -1;
+    float bias_value = 0.0f;
+    if (lists && lane < p.M) {
+        bias_id = p.bias_id[row * p.M + lane];
+        bias_value = p.bias_value[row * p.M + lane];
     }
     const int length = p.length ? min(max(p.length[row], 0), p.L) : p.L;
     const int prompt = p.prompt ? min(max(p.prompt[row], 0), length) : 0;
@@ -89,48 +112,61 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
     if (counts) {
         for (int w = threadIdx.x * 4; w < end - begin; w += THREADS * 4) *reinterpret_cast<uint4 *>(words + w) = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        const int32_t *history = p.history + row * p.ld_history;
         const int before = skew - begin;                               // place of an id in the piece, if it has one
-        auto count = [&](int t, int id) {
+        auto place_of = [&](int id) {
             const int at = id + before;
-            if (id >= 0 && id < p.V && at >= 0 && at < end - begin && t < length) {
-                if (t >= prompt) atomicAdd(&words[at], 1u);
-                else atomicOr(&words[at], kPrompt);
-            }
+            return id >= 0 && id < p.V && at >= 0 && at < end - begin ? at : -1;
         };
-        for (int base = 0; base < length; base += THREADS * 4 * kBatch) {
-            Tokens ids[kBatch];
-#pragma unroll
-            for (int q = 0; q < kBatch; ++q) {
-                const int t = base + (q * THREADS + (int)threadIdx.x) * 4;
-                if (t + 4 <= length) {
-                    ids[q] = *reinterpret_cast<const LooseTokens *>(history + t);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) ids[q][k] = t + k < length ? history[t + k] : -1;
-                }
-            }
-#pragma unroll
-            for (int q = 0; q < kBatch; ++q)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) count(base + (q * THREADS + (int)threadIdx.x) * 4 + k, ids[q][k]);
-        }
-        if (p.M > 0 && threadIdx.x < kWave) {                          // one wave keeps the order
+        if (lists && p.M > 0) {
             int m = 0;
-            for (int base = 0; base < p.M; base += kWave) {
-                const int k = base + (int)threadIdx.x;
-                const int id = k < p.M ? p.bias_id[row * p.M + k] : -1, at = id + before;
-                const bool in = id >= 0 && id < p.V && at >= 0 && at < end - begin;
-                const unsigned long long all = __ballot(in);
-                if (in) {
-                    const int to = m + __popcll(all & ((1ull << threadIdx.x) - 1));
+            for (int base = 0; base < p.M; base += kWave) {            // one wave keeps the order
+                if (base > 0) {
+                    bias_id = base + lane < p.M ? p.bias_id[row * p.M + base + lane] : -1;
+                    bias_value = base + lane < p.M ? p.bias_value[row * p.M + base + lane] : 0.0f;
+                }
+                const int at = place_of(bias_id);
+                const unsigned long long all = __ballot(at >= 0);
+                if (at >= 0) {
+                    const int to = m + __popcll(all & ((1ull << lane) - 1));
                     biases.at[to] = at;
-                    biases.value[to] = p.bias_value[row * p.M + k];
-                    atomicOr(&words[at], kBiased);
+                    biases.value[to] = bias_value;
                 }
                 m += __popcll(all);
             }
-            if (threadIdx.x == 0) biases.n = m;
+            if (lane == 0) *biases.n = m;
+            wave_sync();
+            if (m <= kNumbered) {
+                const int at = lane < m ? biases.at[lane] : -1;
+                float sum = 0.0f;
+                bool leads = lane < m;
+                for (int k = 0; k < m; ++k) {
+                    const bool same = biases.at[k] == at;
+                    sum += same ? biases.value[k] : 0.0f;
+                    leads = leads && !(same && k < lane);
+                }
+                wave_sync();
+                if (leads) {
+                    biases.value[lane] = sum;
+                    atomicOr(&words[at], kBiased | (unsigned)lane << kBiasShift);
+                }
+            } else {
+                for (int k = lane; k < m; k += kWave) atomicOr(&words[biases.at[k]], kBiased);
+            }
+        }
+        for (int base = 0; base < length; base += THREADS * 4 * kBatch) {
+            if (base > 0)
+#pragma unroll
+                for (int q = 0; q < kBatch; ++q) tokens_at(first[q], base + (q * THREADS + (int)threadIdx.x) * 4, length);
+#pragma unroll
+            for (int q = 0; q < kBatch; ++q)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int t = base + (q * THREADS + (int)threadIdx.x) * 4 + k, at = place_of(first[q][k]);
+                    if (t < length && at >= 0) {
+                        if (t >= prompt) atomicAdd(&words[at], 1u);
+                        else atomicOr(&words[at], kPrompt);
+                    }
+                }
         }
         __syncthreads();
     }
@@ -164,9 +200,12 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
                 if (any & kBiased)
 #pragma unroll
                     for (int k = 0; k < V; ++k)
-                        if (w[k] & kBiased)
-                            for (int m = 0; m < biases.n; ++m)
-                                if (biases.at[m] == j - begin + k) z[k] += biases.value[m];
+                        if (w[k] & kBiased) {
+                            if (*biases.n <= kNumbered) z[k] += biases.value[w[k] >> kBiasShift & (kNumbered - 1)];
+                            else
+                                for (int m = 0; m < *biases.n; ++m)
+                                    if (biases.at[m] == j - begin + k) z[k] += biases.value[m];
+                        }
             }
         }
         if (p.allowed)
@@ -212,22 +251,19 @@ int marl_penalize(int32_t dtype, int32_t R, int32_t V, const void *logits, int64
     p.allowed = reinterpret_cast<const uint32_t *>(allowed); p.ld_allowed = ld_allowed; p.out = out; p.ld_out = ld_out;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     return with_dtype(dtype, [&](auto e) {
-        // pieces are counted from the line that the row's result begins in: up to 127 bytes before it.  Every piece reads the history, so they
-        // are as large as shared memory allows two of at a time, unless that leaves too few for the chip
+        // Pieces are counted from the line that the row's result begins in: up to 127 bytes before it.  Every piece reads the history, but with
+        // four of 8192 places on a compute unit some pass logits while others count: 777 rows of 50021 in fp16 with 4096 tokens on
+        // average, 64 biases and a mask take 65 us (25 without any of them, a copy 22), with pieces of 16384 and 1024 threads 82, with 4096
+        // and 256 threads 64.
         const auto go = [&](auto kernel, int threads, int piece) {
-            const size_t lds = piece * sizeof(unsigned) + (M > 0 ? sizeof(BiasList) : 0);
-            if (lds > 64 * 1024) {                     // more than that has to be asked for
-                const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-                if (err != hipSuccess) return report_device_error(err, "hipFuncSetAttribute");
-            }
+            const size_t lds = piece * sizeof(unsigned) + (1 + 2 * (size_t)M) * sizeof(int);       // 40 KB at most
             p.pieces = (int)(((int64_t)V + 63 + piece - 1) / piece);
             if ((int64_t)R * p.pieces >= ((int64_t)1 << 31)) return (int)MARL_ERR_BAD_DIM;
             hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)R * p.pieces)), dim3(threads), lds, stream, p);
             return launched("penalize");
         };
         if (V <= 1024 - 64) return go(penalize_kernel<decltype(e), 64, 1024>, 64, 1024);
-        if ((int64_t)R * V < (int64_t)512 * 8192) return go(penalize_kernel<decltype(e), 512, 8192>, 512, 8192);
-        return go(penalize_kernel<decltype(e), 1024, 16384>, 1024, 16384);
+        return go(penalize_kernel<decltype(e), 512, 8192>, 512, 8192);
     });
 }
 
