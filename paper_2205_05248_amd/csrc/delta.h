@@ -248,6 +248,21 @@ __device__ __forceinline__ int hidden_zero()
 
 __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
 
+// Reads of a record at an offset in bytes that fits 32 bits: uniform base, one register a lane.
+template <typename V>
+__device__ __forceinline__ V read_at(const void *base, unsigned offset) { return *reinterpret_cast<const V *>(static_cast<const char *>(base) + offset); }
+
+// The fragments of a matrix: the number of one is the same for all lanes of a wave and goes through a scalar register.
+struct FragReader {
+    __amdgpu_buffer_rsrc_t buffer;
+    __device__ __forceinline__ FragReader(const Frag *record) : buffer(__builtin_amdgcn_make_buffer_rsrc(const_cast<Frag *>(record), 0, -1, 0x00020000)) {}
+    __device__ __forceinline__ Frag at(int tile, int step, int plane, int steps, int planes) const
+    {
+        const int number = (tile * steps + step) * planes + plane;
+        return __builtin_bit_cast(Frag, __builtin_amdgcn_raw_buffer_load_b128(buffer, (int)threadIdx.x % kWave * 16, number * 1024, 0));
+    }
+};
+
 // NT adjacent columns of a row as they lie in memory: loaded at once, whatever the row's end, and looked at later, so that the load can be on its way
 // meanwhile.  (With a conversion or a branch behind the load every row of the next chunk was waited for where it was asked for.)
 template <typename E, int NT>
@@ -255,7 +270,8 @@ struct Columns {
     typedef E Vec __attribute__((ext_vector_type(NT)));
     typedef Vec Loose __attribute__((aligned(sizeof(E))));
     Vec raw;
-    __device__ __forceinline__ void load(const E *row, int col, int D) { raw = *reinterpret_cast<const Loose *>(row + min(col, D - NT)); }      // D >= NT
+    // offset: of the row's column min(col, D - NT), in bytes from `base`.  D >= NT: two tiles are taken of more than 16 columns only
+    __device__ __forceinline__ void load(const E *base, unsigned offset) { raw = read_at<Loose>(base, offset); }
     __device__ __forceinline__ float at(int n, int col, int D) const
     {
         const float own = to_f32(raw[n]), last = to_f32(raw[NT - 1]);
@@ -315,6 +331,9 @@ __device__ __forceinline__ Place place_of(int64_t heads, int Dv, int columns)
     return at < all && blockIdx.x / 8 < each ? Place{at / blocks, (int)(at % blocks) * columns} : Place{-1, 0};
 }
 inline unsigned places(int64_t heads, int Dv, int columns) { return (unsigned)((heads * (padded_values(Dv) / columns) + 7) / 8 * 8); }
+
+// Whether a workgroup takes two tiles of columns: where there are more than two columns a lane can hold, and workgroups for the whole chip.
+inline bool wide_columns(const DeltaArgs &p) { return p.Dv > 16 && (int64_t)p.B * p.Hv * (padded_values(p.Dv) / 32) >= 256; }
 
 int delta_scan_launch(int dtype, const DeltaArgs &p, hipStream_t stream);
 int delta_grad_launch(int dtype, const DeltaArgs &p, hipStream_t stream);

@@ -9,30 +9,13 @@
 namespace marl {
 namespace {
 
-// What a chunk needs from memory on the way back.
-template <typename E, int DK, int NT>
-struct BackLoads {
-    static constexpr int PE = kExact<E>, KS = DK / 32, kTiles = (DK + 63) / 64;
-    Frag k[KS][PE], n[2][3], p[2][3], kt[kTiles][2][PE], qt[kTiles][2][PE];
-    Acc f, t, beta;
-    float whole;
-    int bad;
-};
-// The upstream gradient of a chunk, and what scales it.
-template <typename E, int NT>
-struct Upstream {
-    Columns<E, NT> o[4];
-    Acc f, t;
-};
-
 // The chunks of one head from the last to the first, for 16 NT value columns as in the forward pass: D, Y and the gradient of v.  Wave w has
-// rows 16 w on of the chunk, and rows w DK / 4 on of the adjoint, which stays in its accumulators.  AHEAD as in the forward pass.
-template <typename E, int DK, int NT, bool AHEAD>
-__global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
+// rows 16 w on of the chunk, and rows w DK / 4 on of the adjoint, which stays in its accumulators.  Loads as in the forward pass.
+template <typename E, int DK, int NT>
+__global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2 : 1) void back_kernel(DeltaArgs p)
 {
-    typedef BackLoads<E, DK, NT> Loads;
     constexpr int PE = kExact<E>, KS = DK / 32, LS = DK + 8, LU = kSteps + 8, C = 16 * NT;
-    constexpr int kTiles = Loads::kTiles;
+    constexpr int kTiles = (DK + 63) / 64;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef __bf16 StatePlane[C][LS];
     typedef __bf16 StepPlane[C][LU];
@@ -59,47 +42,58 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) adj[tile][n][r] = v[n];
             }
-    auto load = [&](Loads &x, int chunk) {
-        const int64_t record = head * p.chunks + chunk, key_record = key_head * p.chunks + chunk;
-        const Frag *K = p.K + key_record * key_frags(DK, PE), *KT = p.KT + key_record * key_frags(DK, PE), *QT = p.QT + key_record * key_frags(DK, PE);
-        const Frag *N = p.NT + record * square_frags(3), *P = p.PT + record * square_frags(3);
-        const ChunkGates &g = p.gates[record];
-        x.f = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
-        x.t = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
-        x.beta = *reinterpret_cast<const Acc *>(g.beta + wave * 16 + group * 4);
-        x.whole = (&g.whole)[zero];
-        x.bad = (&g.bad)[zero];
+    Frag k[KS][PE], n_of[2][3], p_of[2][3], kt[kTiles][2][PE], qt[kTiles][2][PE];
+    Columns<E, NT> up[4];
+    Acc f_next, t_next, beta_next, f_up, t_up;
+    float whole_next;
+    int bad_next;
+    const unsigned of_row = (wave * 16 + group * 4) * 4u, row_bytes = (unsigned)p.ld_go * (unsigned)sizeof(E);
+    const unsigned first_o = (wave * 16 + group * 4) * row_bytes + (unsigned)min(col, p.Dv - NT) * (unsigned)sizeof(E);
+    auto load_start = [&](int chunk) {
+        const ChunkGates *g = p.gates + head * p.chunks + chunk;
+        const FragReader K(p.K + (key_head * p.chunks + chunk) * key_frags(DK, PE)), P(p.PT + (head * p.chunks + chunk) * square_frags(3));
+        f_next = read_at<Acc>(g->f, of_row);
+        t_next = read_at<Acc>(g->t, of_row);
+        beta_next = read_at<Acc>(g->beta, of_row);
+        whole_next = read_at<float>(&g->whole, (unsigned)zero);
+        bad_next = read_at<int>(&g->bad, (unsigned)zero);
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int n = 0; n < PE; ++n) x.k[s][n] = K[frag_at(wave, s, n, KS, PE)];
+            for (int n = 0; n < PE; ++n) k[s][n] = K.at(wave, s, n, KS, PE);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {                  // (what lies on the other side of the diagonal is never written, and not used)
+        for (int s = 0; s < 2; ++s)                    // (what lies on the other side of the diagonal is never written, and not used)
 #pragma unroll
-            for (int n = 0; n < 3; ++n) {
-                x.p[s][n] = P[frag_at(wave, s, n, 2, 3)];
-                x.n[s][n] = N[frag_at(wave, s, n, 2, 3)];
-            }
-        }
+            for (int n = 0; n < 3; ++n) p_of[s][n] = P.at(wave, s, n, 2, 3);
+    };
+    auto load_n = [&](int chunk) {
+        const FragReader N(p.NT + (head * p.chunks + chunk) * square_frags(3));
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int n = 0; n < 3; ++n) n_of[s][n] = N.at(wave, s, n, 2, 3);
+    };
+    auto load_end = [&](int chunk) {
+        const int64_t key_record = key_head * p.chunks + chunk;
+        const FragReader KT(p.KT + key_record * key_frags(DK, PE)), QT(p.QT + key_record * key_frags(DK, PE));
 #pragma unroll
         for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int n = 0; n < PE; ++n) {
-                    x.kt[tile][s][n] = KT[frag_at((wave * kTiles + tile) % (DK / 16), s, n, 2, PE)];
-                    x.qt[tile][s][n] = QT[frag_at((wave * kTiles + tile) % (DK / 16), s, n, 2, PE)];
+                    kt[tile][s][n] = KT.at((wave * kTiles + tile) % (DK / 16), s, n, 2, PE);
+                    qt[tile][s][n] = QT.at((wave * kTiles + tile) % (DK / 16), s, n, 2, PE);
                 }
     };
-    auto load_upstream = [&](Upstream<E, NT> &x, int chunk) {
-        const ChunkGates &g = p.gates[head * p.chunks + chunk];
-        x.f = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
-        x.t = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
+    auto load_upstream = [&](int chunk) {
+        const ChunkGates *g = p.gates + head * p.chunks + chunk;
+        f_up = read_at<Acc>(g->f, of_row);
+        t_up = read_at<Acc>(g->t, of_row);
+        const E *rows = row_at<E>(p.grad_o, p.ld_go, b, p.T, chunk * kSteps, h, p.Dv);
+        const int last = p.T - chunk * kSteps;         // rows behind it are not read: the first one is instead
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = min(chunk * kSteps + wave * 16 + group * 4 + r, p.T - 1);
-            x.o[r].load(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), col, p.Dv);
-        }
+        for (int r = 0; r < 4; ++r) up[r].load(rows, wave * 16 + group * 4 + r < last ? first_o + r * row_bytes : first_o - (wave * 16 + group * 4) * row_bytes);
     };
     auto share_adjoint = [&] {
 #pragma unroll
@@ -117,15 +111,20 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
 #pragma unroll
         for (int m = 0; m < PLANES; ++m) *reinterpret_cast<Four *>(&to[m][n * 16 + at][wave * 16 + group * 4]) = planes[m];
     };
-    auto share_upstream = [&](const Upstream<E, NT> &x, int chunk) {
+    auto steps_frag = [&](const StepPlane *from, int n, int s, auto &to) {
+        constexpr int PLANES = sizeof(to) / sizeof(Frag);
+#pragma unroll
+        for (int m = 0; m < PLANES; ++m) to[m] = *reinterpret_cast<const Frag *>(&from[m][n * 16 + at][s * 32 + group * 8]);
+    };
+    auto share_upstream = [&](int chunk) {
         StepPlane *O = upstream + chunk % 2 * (PE + 3), *Of = O + PE;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             Acc o, of;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                o[r] = x.t[r] < 0.0f ? 0.0f : x.o[r].at(n, col, p.Dv);
-                of[r] = x.f[r] == 0.0f ? 0.0f : p.scale * x.f[r] * o[r];
+                o[r] = t_up[r] < 0.0f ? 0.0f : up[r].at(n, col, p.Dv);
+                of[r] = f_up[r] == 0.0f ? 0.0f : p.scale * f_up[r] * o[r];
             }
             Four exact[PE], planes[3];
             split(o, exact);
@@ -135,28 +134,34 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
             if (!all_finite(o)) not_finite[chunk % 2] = 1;
         }
     };
-    auto step = [&](int chunk, Loads &x, Loads &next) {
+    if (threadIdx.x < 4) not_finite[threadIdx.x] = 0;
+    __syncthreads();
+    if (p.chunks > 0) {
+        load_upstream(p.chunks - 1);
+        load_start(p.chunks - 1);
+        load_n(p.chunks - 1);
+        load_end(p.chunks - 1);
+        share_upstream(p.chunks - 1);
+        load_upstream(max(p.chunks - 2, 0));
+    }
+    if (has_state) share_adjoint();
+    __syncthreads();
+    for (int chunk = p.chunks - 1; chunk >= 0; --chunk) {
         const int64_t record = head * p.chunks + chunk;
-        Upstream<E, NT> up;
-        if (!AHEAD) load(x, chunk);
-        load_upstream(up, max(chunk - 1, 0));
-        if (AHEAD) load(next, max(chunk - 1, 0));
-        const Acc f = x.f, t = x.t, beta = x.beta;
+        const int next = max(chunk - 1, 0);
+        const Acc f = f_next, t = t_next, beta = beta_next;
+        const float whole = whole_next;
         const StepPlane *O = upstream + chunk % 2 * (PE + 3), *Of = O + PE;
-        const bool bad = __builtin_amdgcn_readfirstlane(x.bad) != 0, careful_o = bad || not_finite[chunk % 2];
+        const bool bad = __builtin_amdgcn_readfirstlane(bad_next) != 0;
+        // dU = P' dO + t K D
+        Frag of_o[2][NT][PE];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) steps_frag(O, n, s, of_o[s][n]);
+        const bool careful_o = bad || not_finite[chunk % 2];
         // flags are taken back where all have read them and none sets them before the next barrier
         if (threadIdx.x == 0) not_finite[(chunk + 1) % 2] = not_finite[3] = 0;
-        if (has_state)
-#pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float v[NT];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) v[n] = adj[tile][n][r];
-                    write_columns<float, NT>(p.D + (record * DK + (wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
-                }
-        // dU = P' dO + t K D
         Sums<2> kd[NT];
 #pragma unroll
         for (int s = 0; s < KS; ++s)
@@ -165,7 +170,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
                 Frag of_state[3];
 #pragma unroll
                 for (int m = 0; m < 3; ++m) of_state[m] = *reinterpret_cast<const Frag *>(&S[m][n * 16 + at][s * 32 + group * 8]);
-                multiply_into(kd[n], x.k[s], of_state);
+                multiply_into(kd[n], k[s], of_state);
             }
         Acc y[NT];
 #pragma unroll
@@ -190,12 +195,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
             for (int s = 0; s < 2; ++s) {
                 if (s * 32 + 31 < wave * 16) continue;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    Frag of_o[PE];
-#pragma unroll
-                    for (int c = 0; c < PE; ++c) of_o[c] = *reinterpret_cast<const Frag *>(&O[c][n * 16 + at][s * 32 + group * 8]);
-                    multiply_into(po[n], x.p[s], of_o);
-                }
+                for (int n = 0; n < NT; ++n) multiply_into(po[n], p_of[s], of_o[s][n]);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) y[n] += total(po[n]);
@@ -208,8 +208,26 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
             share_steps(R, planes, n);
             if (!all_finite(minus)) not_finite[2] = 1;
         }
+        load_start(next);
+        if (has_state) {
+            float *to = p.D + record * DK * DV;
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float c[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) c[n] = adj[tile][n][r];
+                    write_columns<float, NT>(to, ((wave * kTiles + tile) * 16 + group * 4 + r) * DV + col, DK * DV, c);
+                }
+        }
         __syncthreads();
         // Y = dU - N' (beta dU), dV = beta Y
+        Frag of_r[2][NT][3];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) steps_frag(R, n, s, of_r[s][n]);
         if (bad || not_finite[2]) {
             const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
             unsigned long long pass[4];
@@ -226,12 +244,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
             for (int s = 0; s < 2; ++s) {
                 if (s * 32 + 31 < wave * 16) continue;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    Frag of_r[3];
-#pragma unroll
-                    for (int c = 0; c < 3; ++c) of_r[c] = *reinterpret_cast<const Frag *>(&R[c][n * 16 + at][s * 32 + group * 8]);
-                    multiply_into(nr[n], x.n[s], of_r);
-                }
+                for (int n = 0; n < NT; ++n) multiply_into(nr[n], n_of[s], of_r[s][n]);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) y[n] += total(nr[n]);
@@ -251,15 +264,37 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
             share_steps(V, planes, n);
             if (!all_finite(v[n])) not_finite[3] = 1;
         }
+        load_n(next);
+        {
+            const RowsOut<E, NT> out(p, p.grad_v, p.ld_gv, b, chunk, h);
+            float *to = p.Y + record * kSteps * DV;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = wave * 16 + group * 4 + r;
+                float c[NT], z[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) c[n] = y[n][r], z[n] = v[n][r];
+                write_columns<float, NT>(to, i * DV + col, kSteps * DV, c);
+                out.put(i, col, z);
+            }
+        }
         __syncthreads();
         // D <- f_63 D + (scale f Q)' dO - (f K)' dV
         if (has_state) {
+            Frag of_f[2][NT][3], of_v[2][NT][3];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    steps_frag(Of, n, s, of_f[s][n]);
+                    steps_frag(V, n, s, of_v[s][n]);
+                }
 #pragma unroll
             for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) adj[tile][n][r] = x.whole == 0.0f ? 0.0f : x.whole * adj[tile][n][r];
+                    for (int r = 0; r < 4; ++r) adj[tile][n][r] = whole == 0.0f ? 0.0f : whole * adj[tile][n][r];
             if (careful_o || not_finite[3]) {
                 const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
                 const int64_t key_record = key_head * p.chunks + chunk;
@@ -278,19 +313,12 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        Frag of_o[3], of_v[3];
-#pragma unroll
-                        for (int c = 0; c < 3; ++c) {
-                            of_o[c] = *reinterpret_cast<const Frag *>(&Of[c][n * 16 + at][s * 32 + group * 8]);
-                            of_v[c] = *reinterpret_cast<const Frag *>(&V[c][n * 16 + at][s * 32 + group * 8]);
-                        }
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int tile = 0; tile < kTiles; ++tile) {
-                            multiply_into(of_keys[tile][n], x.qt[tile][s], of_o);
-                            multiply_into(of_keys[tile][n], x.kt[tile][s], of_v);
+                            multiply_into(of_keys[tile][n], qt[tile][s], of_f[s][n]);
+                            multiply_into(of_keys[tile][n], kt[tile][s], of_v[s][n]);
                         }
-                    }
 #pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
@@ -298,34 +326,11 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void back_kernel(DeltaArgs p)
             }
             share_adjoint();
         }
-        if (chunk > 0) share_upstream(up, chunk - 1);
-        const RowsOut<E, NT> out(p, p.grad_v, p.ld_gv, b, chunk, h);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = wave * 16 + group * 4 + r;
-            float c[NT], z[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) c[n] = y[n][r], z[n] = v[n][r];
-            write_columns<float, NT>(p.Y + (record * kSteps + i) * DV, col, DV, c);
-            out.put(i, col, z);
-        }
+        load_end(next);
+        if (chunk > 0) share_upstream(chunk - 1);
+        load_upstream(max(chunk - 2, 0));
         if (threadIdx.x == 0) not_finite[2] = 0;
         __syncthreads();
-    };
-    Loads even, odd;
-    if (threadIdx.x < 4) not_finite[threadIdx.x] = 0;
-    __syncthreads();
-    if (p.chunks > 0) {
-        Upstream<E, NT> up;
-        load_upstream(up, p.chunks - 1);
-        if (AHEAD) load(even, p.chunks - 1);
-        share_upstream(up, p.chunks - 1);
-    }
-    if (has_state) share_adjoint();
-    __syncthreads();
-    for (int chunk = p.chunks - 1; chunk >= 0; chunk -= 2) {
-        step(chunk, even, odd);
-        if (chunk > 0) step(chunk - 1, odd, even);
     }
     if (p.grad_s_first && has_state)
 #pragma unroll
@@ -402,7 +407,7 @@ __device__ __forceinline__ Acc careful_rows(Acc c, const Plane *a, int tile, con
 constexpr int grad_waves(int DK) { return DK == 128 ? 8 : 4; }
 
 template <typename E, int DK>
-__global__ __launch_bounds__(grad_waves(DK) * kWave) void chunk_grad_kernel(DeltaArgs p)
+__global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(DeltaArgs p)
 {
     constexpr int PE = kExact<E>, KS = DK / 32, kOrder = PE == 1 ? 0 : 2, kWaves = grad_waves(DK), kThreads = kWaves * kWave;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -760,16 +765,15 @@ template <typename E, int DK, int NT>
 int run_back(const DeltaArgs &p, hipStream_t stream)
 {
     const size_t lds = (size_t)16 * NT * (3 * (DK + 8) + (12 + 2 * kExact<E>) * (kSteps + 8)) * sizeof(__bf16);
-    constexpr bool kAhead = kExact<E> * DK <= 256;     // else two chunks' loads do not fit the registers
-    if (const int rc = make_room_for(reinterpret_cast<const void *>(back_kernel<E, DK, NT, kAhead>), lds)) return rc;
-    hipLaunchKernelGGL((back_kernel<E, DK, NT, kAhead>), dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
+    if (const int rc = make_room_for(reinterpret_cast<const void *>(back_kernel<E, DK, NT>), lds)) return rc;
+    hipLaunchKernelGGL((back_kernel<E, DK, NT>), dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
     return launched("delta scan gradient");
 }
 
 template <typename E, int DK>
 int run(const DeltaArgs &p, hipStream_t stream)
 {
-    const int rc = p.Dv > 16 && (int64_t)p.B * p.Hv * ((p.Dv + 31) / 32) >= 256 ? run_back<E, DK, 2>(p, stream) : run_back<E, DK, 1>(p, stream);
+    const int rc = wide_columns(p) ? run_back<E, DK, 2>(p, stream) : run_back<E, DK, 1>(p, stream);
     if (rc || p.chunks == 0) return rc;
     const size_t lds = (6 + kExact<E>) * sizeof(Plane);            // (the results' rows, 64 of DK + 8, are less)
     if (const int failed = make_room_for(reinterpret_cast<const void *>(chunk_grad_kernel<E, DK>), lds)) return failed;

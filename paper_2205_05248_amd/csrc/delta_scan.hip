@@ -252,27 +252,15 @@ __global__ __launch_bounds__(kDeltaThreads) void chunk_kernel(DeltaArgs p)
     }
 }
 
-// What a chunk needs from memory.
-template <typename E, int DK, int NT>
-struct ScanLoads {
-    static constexpr int PE = kExact<E>, PF = kFine<E>, KS = DK / 32, kTiles = (DK + 63) / 64;
-    Frag k[KS][PE], q[KS][PE], n[2][3], p[2][PF], kt[kTiles][2][PE];
-    Columns<E, NT> v[4];
-    Acc f, t, beta;
-    float whole;
-    int bad;
-};
-
 // The chunks of one head one after the other, for 16 NT value columns: tile n of a lane's column l % 16 is column NT (l % 16) + n.  Wave w has
 // rows 16 w on of the chunk, and rows w DK / 4 on of the state, which stays in its accumulators; the others read it as planes from shared memory.
-// AHEAD: a chunk's loads go out a whole chunk before their use, whether there is another chunk or not: behind a branch the compiler would wait
-// for them at the next wait of any kind.
-template <typename E, int DK, int NT, bool AHEAD, bool KEEP>
-__global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
+// What a phase needs from memory is asked for where the same phase of the chunk before has used its registers, a whole chunk ahead, and
+// whether there is another chunk or not: behind a branch the compiler would wait for it at the next wait of any kind.
+template <typename E, int DK, int NT, bool KEEP>
+__global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 256 ? 2 : 1) void scan_kernel(DeltaArgs p)
 {
-    typedef ScanLoads<E, DK, NT> Loads;
     constexpr int PE = kExact<E>, PF = kFine<E>, KS = DK / 32, LS = DK + 8, LU = kSteps + 8, C = 16 * NT;
-    constexpr int kTiles = Loads::kTiles;              // of the state, for a wave; of DK = 32 two waves have one
+    constexpr int kTiles = (DK + 63) / 64;             // of the state, for a wave; of DK = 32 two waves have one
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef __bf16 StatePlane[C][LS];
     typedef __bf16 StepPlane[C][LU];
@@ -298,41 +286,52 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) state[tile][n][r] = v[n];
             }
-    auto load = [&](Loads &x, int chunk) {
-        const int64_t record = head * p.chunks + chunk, key_record = key_head * p.chunks + chunk;
-        const Frag *K = p.K + key_record * key_frags(DK, PE), *Q = p.Q + key_record * key_frags(DK, PE), *KT = p.KT + key_record * key_frags(DK, PE);
-        const Frag *N = p.N + record * square_frags(3), *P = p.P + record * square_frags(PF);
-        const ChunkGates &g = p.gates[record];
-        x.f = *reinterpret_cast<const Acc *>(g.f + wave * 16 + group * 4);
-        x.t = *reinterpret_cast<const Acc *>(g.t + wave * 16 + group * 4);
-        x.beta = *reinterpret_cast<const Acc *>(g.beta + wave * 16 + group * 4);
-        x.whole = (&g.whole)[zero];
-        x.bad = (&g.bad)[zero];
+    Frag k[KS][PE], q[KS][PE], n_of[2][3], p_of[2][PF], kt[kTiles][2][PE];
+    Columns<E, NT> v[4];
+    Acc f_next, t_next, beta_next;
+    float whole_next;
+    int bad_next;
+    const unsigned of_row = (wave * 16 + group * 4) * 4u, row_bytes = (unsigned)p.ld_v * (unsigned)sizeof(E);
+    const unsigned first_v = (wave * 16 + group * 4) * row_bytes + (unsigned)min(col, p.Dv - NT) * (unsigned)sizeof(E);
+    auto load_start = [&](int chunk) {
+        const ChunkGates *g = p.gates + head * p.chunks + chunk;
+        const FragReader K(p.K + (key_head * p.chunks + chunk) * key_frags(DK, PE)), Q(p.Q + (key_head * p.chunks + chunk) * key_frags(DK, PE));
+        f_next = read_at<Acc>(g->f, of_row);
+        t_next = read_at<Acc>(g->t, of_row);
+        beta_next = read_at<Acc>(g->beta, of_row);
+        whole_next = read_at<float>(&g->whole, (unsigned)zero);
+        bad_next = read_at<int>(&g->bad, (unsigned)zero);
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int n = 0; n < PE; ++n) {
-                x.k[s][n] = K[frag_at(wave, s, n, KS, PE)];
-                x.q[s][n] = Q[frag_at(wave, s, n, KS, PE)];
+                k[s][n] = K.at(wave, s, n, KS, PE);
+                q[s][n] = Q.at(wave, s, n, KS, PE);
             }
+        const E *rows = row_at<E>(p.v, p.ld_v, b, p.T, chunk * kSteps, h, p.Dv);
+        const int last = p.T - chunk * kSteps;         // rows behind it are not read: the first one is instead
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = min(chunk * kSteps + wave * 16 + group * 4 + r, p.T - 1);
-            x.v[r].load(row_at<E>(p.v, p.ld_v, b, p.T, t, h, p.Dv), col, p.Dv);
-        }
+        for (int r = 0; r < 4; ++r) v[r].load(rows, wave * 16 + group * 4 + r < last ? first_v + r * row_bytes : first_v - (wave * 16 + group * 4) * row_bytes);
+    };
+    auto load_n = [&](int chunk) {                     // (what lies on the other side of the diagonal is never written, and not used)
+        const FragReader N(p.N + (head * p.chunks + chunk) * square_frags(3));
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {                  // (what lies on the other side of the diagonal is never written, and not used)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int n = 0; n < 3; ++n) x.n[s][n] = N[frag_at(wave, s, n, 2, 3)];
-#pragma unroll
-            for (int n = 0; n < PF; ++n) x.p[s][n] = P[frag_at(wave, s, n, 2, PF)];
-        }
+            for (int n = 0; n < 3; ++n) n_of[s][n] = N.at(wave, s, n, 2, 3);
+    };
+    auto load_end = [&](int chunk) {
+        const FragReader P(p.P + (head * p.chunks + chunk) * square_frags(PF)), KT(p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE));
 #pragma unroll
         for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int n = 0; n < PE; ++n) x.kt[tile][s][n] = KT[frag_at((wave * kTiles + tile) % (DK / 16), s, n, 2, PE)];
+                for (int n = 0; n < PE; ++n) kt[tile][s][n] = KT.at((wave * kTiles + tile) % (DK / 16), s, n, 2, PE);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int n = 0; n < PF; ++n) p_of[s][n] = P.at(wave, s, n, 2, PF);
     };
     auto share_state = [&] {
 #pragma unroll
@@ -350,21 +349,25 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 #pragma unroll
         for (int m = 0; m < PLANES; ++m) *reinterpret_cast<Four *>(&to[m][n * 16 + at][wave * 16 + group * 4]) = planes[m];
     };
-    auto step = [&](int chunk, Loads &x, Loads &next) {
+    auto steps_frag = [&](const StepPlane *from, int n, int s, auto &to) {
+        constexpr int PLANES = sizeof(to) / sizeof(Frag);
+#pragma unroll
+        for (int m = 0; m < PLANES; ++m) to[m] = *reinterpret_cast<const Frag *>(&from[m][n * 16 + at][s * 32 + group * 8]);
+    };
+    if (p.chunks > 0) {
+        load_start(0);
+        load_n(0);
+        load_end(0);
+    }
+    if (has_state) share_state();
+    if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
+    __syncthreads();
+    for (int chunk = 0; chunk < p.chunks; ++chunk) {
         const int64_t record = head * p.chunks + chunk;
-        if (!AHEAD) load(x, chunk);
-        else load(next, min(chunk + 1, p.chunks - 1));
-        const Acc f = x.f, t = x.t, beta = x.beta;
-        if (KEEP && has_state)
-#pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float v[NT];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) v[n] = state[tile][n][r];
-                    write_columns<float, NT>(p.S + (record * DK + (wave * kTiles + tile) * 16 + group * 4 + r) * DV, col, DV, v);
-                }
+        const int next = min(chunk + 1, p.chunks - 1);
+        const Acc f = f_next, t = t_next, beta = beta_next;
+        const float whole = whole_next;
+        const bool bad = __builtin_amdgcn_readfirstlane(bad_next) != 0;
         // R = V - f K S
         Sums<2> ks[NT];
         Sums<PF - 1> qs[NT];
@@ -377,8 +380,8 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
                 for (int m = 0; m < 3; ++m) of_state[m] = *reinterpret_cast<const Frag *>(&S[m][n * 16 + at][s * 32 + group * 8]);
 #pragma unroll
                 for (int m = 0; m < PF; ++m) fine[m] = of_state[m];
-                multiply_into(ks[n], x.k[s], of_state);
-                multiply_into(qs[n], x.q[s], fine);
+                multiply_into(ks[n], k[s], of_state);
+                multiply_into(qs[n], q[s], fine);
             }
         Acc m[NT];
 #pragma unroll
@@ -386,8 +389,8 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
             const Acc of_k = total(ks[n]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float v = x.v[r].at(n, col, p.Dv);
-                m[n][r] = t[r] < 0.0f ? 0.0f : f[r] == 0.0f ? v : fmaf(-f[r], of_k[r], v);
+                const float value = v[r].at(n, col, p.Dv);
+                m[n][r] = t[r] < 0.0f ? 0.0f : f[r] == 0.0f ? value : fmaf(-f[r], of_k[r], value);
             }
             const Acc minus = -(beta * m[n]);
             Four planes[3];
@@ -395,11 +398,27 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
             share_steps(R, planes, n);
             if (!all_finite(minus)) not_finite[0] = 1;
         }
+        load_start(next);
+        if (KEEP && has_state) {
+            float *to = p.S + record * DK * DV;
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float c[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) c[n] = state[tile][n][r];
+                    write_columns<float, NT>(to, ((wave * kTiles + tile) * 16 + group * 4 + r) * DV + col, DK * DV, c);
+                }
+        }
         __syncthreads();
         // M = R - N (beta R), U = beta M
-        const bool bad = __builtin_amdgcn_readfirstlane(x.bad) != 0;
-        const bool careful_n = bad || not_finite[0];
-        if (careful_n) {
+        Frag of_r[2][NT][3];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) steps_frag(R, n, s, of_r[s][n]);
+        if (bad || not_finite[0]) {
             const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
             unsigned long long pass[4];
 #pragma unroll
@@ -415,12 +434,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
             for (int s = 0; s < 2; ++s) {
                 if (s * 32 > wave * 16) continue;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    Frag of_r[3];
-#pragma unroll
-                    for (int c = 0; c < 3; ++c) of_r[c] = *reinterpret_cast<const Frag *>(&R[c][n * 16 + at][s * 32 + group * 8]);
-                    multiply_into(nr[n], x.n[s], of_r);
-                }
+                for (int n = 0; n < NT; ++n) multiply_into(nr[n], n_of[s], of_r[s][n]);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) m[n] += total(nr[n]);
@@ -438,16 +452,28 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
             share_steps(Ue, end_planes, n);
             if (!all_finite(u)) not_finite[1] = 1;
         }
-        if (KEEP)
+        load_n(next);
+        if (KEEP) {
+            float *to = p.M + record * kSteps * DV;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float c[NT];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) c[n] = m[n][r];
-                write_columns<float, NT>(p.M + (record * kSteps + wave * 16 + group * 4 + r) * DV, col, DV, c);
+                write_columns<float, NT>(to, (wave * 16 + group * 4 + r) * DV + col, kSteps * DV, c);
             }
+        }
         __syncthreads();
         // O = scale f Q S + P U,  S <- f_63 S + K' (t U)
+        Frag of_e[2][NT][3], of_u[2][NT][PF];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) steps_frag(Ue, n, s, of_e[s][n]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) steps_frag(U, n, s, of_u[s][n]);
         Acc o[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -460,7 +486,7 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) state[tile][n][r] = x.whole == 0.0f ? 0.0f : x.whole * state[tile][n][r];
+                for (int r = 0; r < 4; ++r) state[tile][n][r] = whole == 0.0f ? 0.0f : whole * state[tile][n][r];
         if (bad || not_finite[1]) {
             const unsigned long long starts = p.gates[record].starts, live = p.gates[record].live;
             unsigned long long pass[4];
@@ -487,13 +513,9 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        Frag of_u[3];
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int c = 0; c < 3; ++c) of_u[c] = *reinterpret_cast<const Frag *>(&Ue[c][n * 16 + at][s * 32 + group * 8]);
-#pragma unroll
-                        for (int tile = 0; tile < kTiles; ++tile) multiply_into(ku[tile][n], x.kt[tile][s], of_u);
-                    }
+                        for (int tile = 0; tile < kTiles; ++tile) multiply_into(ku[tile][n], kt[tile][s], of_e[s][n]);
 #pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
@@ -503,14 +525,10 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
             for (int s = 0; s < 2; ++s) {
                 if (s * 32 > wave * 16) continue;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    Frag of_u[PF];
-#pragma unroll
-                    for (int c = 0; c < PF; ++c) of_u[c] = *reinterpret_cast<const Frag *>(&U[c][n * 16 + at][s * 32 + group * 8]);
-                    o[n] = multiply<PF, PF>(x.p[s], of_u, o[n]);
-                }
+                for (int n = 0; n < NT; ++n) o[n] = multiply<PF, PF>(p_of[s], of_u[s][n], o[n]);
             }
         }
+        load_end(next);
         if (has_state) share_state();
         const RowsOut<E, NT> out(p, p.o, p.ld_o, b, chunk, h);
 #pragma unroll
@@ -523,15 +541,6 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
         if (threadIdx.x == 0) not_finite[0] = 0;       // read before the barrier above, written after the one below
         __syncthreads();
         if (threadIdx.x == 0) not_finite[1] = 0;
-    };
-    Loads even, odd;
-    if (AHEAD && p.chunks > 0) load(even, 0);
-    if (has_state) share_state();
-    if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
-    __syncthreads();
-    for (int chunk = 0; chunk < p.chunks; chunk += 2) {
-        step(chunk, even, odd);
-        if (chunk + 1 < p.chunks) step(chunk + 1, odd, even);
     }
     if (p.s_last && has_state)
 #pragma unroll
@@ -546,18 +555,16 @@ __global__ __launch_bounds__(kDeltaThreads, 1) void scan_kernel(DeltaArgs p)
             }
 }
 
-// Two tiles of columns a workgroup where that still fills the chip.
 template <typename E, int DK, int NT>
 int run_scan(const DeltaArgs &p, hipStream_t stream)
 {
     const size_t lds = (size_t)16 * NT * (3 * (DK + 8) + (6 + kFine<E>) * (kSteps + 8)) * sizeof(__bf16);
-    constexpr bool kAhead = kExact<E> * DK <= 256;     // else two chunks' loads do not fit the registers
     const auto go = [&](auto kernel) {
         if (const int rc = make_room_for(reinterpret_cast<const void *>(kernel), lds)) return rc;
         hipLaunchKernelGGL(kernel, dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);
         return launched("delta scan");
     };
-    return p.S ? go(scan_kernel<E, DK, NT, kAhead, true>) : go(scan_kernel<E, DK, NT, kAhead, false>);
+    return p.S ? go(scan_kernel<E, DK, NT, true>) : go(scan_kernel<E, DK, NT, false>);
 }
 
 template <typename E, int DK>
@@ -568,8 +575,7 @@ int run(const DeltaArgs &p, hipStream_t stream)
         if (const int rc = make_room_for(reinterpret_cast<const void *>(chunk_kernel<E, DK>), lds)) return rc;
         hipLaunchKernelGGL((chunk_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
     }
-    if (p.Dv > 16 && (int64_t)p.B * p.Hv * ((p.Dv + 31) / 32) >= 256) return run_scan<E, DK, 2>(p, stream);
-    return run_scan<E, DK, 1>(p, stream);
+    return wide_columns(p) ? run_scan<E, DK, 2>(p, stream) : run_scan<E, DK, 1>(p, stream);
 }
 
 }  // namespace
