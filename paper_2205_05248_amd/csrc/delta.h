@@ -190,14 +190,19 @@ __device__ __forceinline__ bool all_finite(Acc a)
     return (z[0] + z[1]) + (z[2] + z[3]) == 0.0f;
 }
 
-// D = A B + C on 16 x 16 tiles in fp32: a(row, k), b(k, col) give one entry each.
+// c + a b on 16 x 16 tiles in fp32: a(row, k), b(k, col) give one entry each.  All entries are asked for before the first is used.
 template <class FA, class FB>
-__device__ __forceinline__ Acc product(int K, Acc c, FA &&a, FB &&b)
+__device__ __forceinline__ Acc product(Acc c, FA &&a, FB &&b)
 {
     const int lane = threadIdx.x % kWave, at = lane % 16, group = lane / 16;
-    for (int k = 0; k < K; k += 4) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a(at, k + group), b(k + group, at), c, 0, 0, 0);
+    float x[4], y[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) x[s] = a(at, s * 4 + group), y[s] = b(s * 4 + group, at);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], y[s], c, 0, 0, 0);
     return c;
 }
+
 // Row of the elements of step t of sequence b and head h.
 template <typename E>
 __device__ __forceinline__ const E *row_at(const void *base, int64_t ld, int64_t b, int T, int t, int h, int D)

@@ -1,6 +1,7 @@
 // Gated delta rule, backward: the way back through the chunks, then the gradients of every chunk side by side.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -352,20 +353,20 @@ __device__ __forceinline__ float row_sum(float v)
     return v;
 }
 
-// A chunk's steps as planes in shared memory, rows of 64 entries.
-constexpr int kRow = kSteps + 8;
-typedef __bf16 Plane[kSteps][kRow];
+// A chunk's steps as planes in shared memory, rows of COLUMNS entries.
+template <int COLUMNS> struct Rows { typedef __bf16 Plane[kSteps][COLUMNS + 8]; };
+typedef Rows<kSteps>::Plane Plane;
 
-template <int PLANES>
-__device__ __forceinline__ void put_row(Plane *to, int row, int col, const float *v)
+template <int PLANES, class PLANE>
+__device__ __forceinline__ void put_row(PLANE *to, int row, int col, const float *v)
 {
     Frag f[PLANES];
     split(v, f);
 #pragma unroll
     for (int n = 0; n < PLANES; ++n) *reinterpret_cast<Frag *>(&to[n][row][col]) = f[n];
 }
-template <int PLANES>
-__device__ __forceinline__ void get_frag(const Plane *from, int tile, int step, Frag (&to)[PLANES])
+template <int PLANES, class PLANE>
+__device__ __forceinline__ void get_frag(const PLANE *from, int tile, int step, Frag (&to)[PLANES])
 {
     const int lane = threadIdx.x % kWave;
 #pragma unroll
@@ -401,18 +402,21 @@ __device__ __forceinline__ Acc careful_rows(Acc c, const Plane *a, int tile, con
 //   dq = dN K + scale f dO S'      dk = dN' Q + X K - f dV S' + t U D'
 //   dG_i = sum_j F_ij - sum_j F_ji + q_i.(scale f dO S')_i - k_i.(f dV S')_i - k_i.(t U D')_i      F_ij = dM_ij k_i.k_j + dN_ij q_i.k_j
 // to which the last step adds sum_j k_j.(t U D')_j + f_63 <D, S>; the log decay's gradient is the sum of dG from its step to the end of
-// its sequence.  Value columns come 64 at a time through shared memory.  Products with rows and columns of steps are split over the waves by
+// its sequence.  Value columns come 32 or 64 at a time through shared memory.  Products with rows and columns of steps are split over the waves by
 // rows, those with key columns by columns (16 w on), so that every entry of S and D is split into planes once.
 // Waves of a workgroup: with 128 keys eight, of which four form dP and four dA, else four that form both.
 constexpr int grad_waves(int DK) { return DK == 128 ? 8 : 4; }
+constexpr int grad_columns(int DK) { return DK == 128 ? 64 : 32; }       // at a time: more do not fit the registers of four waves
 
 template <typename E, int DK>
 __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(DeltaArgs p)
 {
     constexpr int PE = kExact<E>, KS = DK / 32, kOrder = PE == 1 ? 0 : 2, kWaves = grad_waves(DK), kThreads = kWaves * kWave;
+    constexpr int CB = grad_columns(DK);
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    Plane *U = reinterpret_cast<Plane *>(lds), *V = U + 3, *O = V + 3;             // [3], [3], [PE]
-    Plane *dN = U, *dNT = V, *X = U;                   // later in the same room, [3] each
+    typedef typename Rows<CB>::Plane Block;
+    Block *U = reinterpret_cast<Block *>(lds), *V = U + 3, *O = V + 3;             // [3], [3], [PE]
+    Plane *dN = reinterpret_cast<Plane *>(lds), *dNT = dN + 3, *X = dN;            // later in the same room, [3] each
     __shared__ ChunkGates gates;
     __shared__ int not_finite;
     __shared__ float rows_of[kWaves][kSteps], columns_of[8][kSteps], flow[2][kSteps], extra[kWaves], dbeta[kSteps];
@@ -442,58 +446,75 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
         QT += nothing;
         const int h = hk * shared + member;
         const int64_t record = (b * p.Hv + h) * p.chunks + chunk;
-        __syncthreads();
-        {
-            const int *from = reinterpret_cast<const int *>(p.gates + record);
-            int *to = reinterpret_cast<int *>(&gates);
-            for (int e = threadIdx.x; e < (int)(sizeof(ChunkGates) / 4); e += kThreads) to[e] = from[e];
-        }
-        if (threadIdx.x == 0) not_finite = 0;
-        __syncthreads();
-        const unsigned long long starts = gates.starts;
-        alive = gates.live;
         const float *M = p.M + record * kSteps * DV, *Y = p.Y + record * kSteps * DV;
         const float *S = p.S + record * DK * DV, *D = p.D + record * DK * DV;
         Acc d_of[2][4] = {}, far_q[4] = {}, far_k[4] = {}, end[4] = {};            // d_of: dP, dA
         float dot_states = 0.0f, dot_beta = 0.0f;
-        for (int c0 = 0; c0 < p.Dv; c0 += kSteps) {
-            const int steps = min(2, (DV - c0) / 32);
-            // S and D of the wave's keys: loads go out before the wait for the staging
-            typedef float Eight __attribute__((ext_vector_type(8)));
-            Eight s[2], d[2];
+        // A block of columns: S and D of the wave's keys, and eight columns at a time of M, Y and dO of the thread's step.  All loads go out
+        // before any wait, those of the first block before the one for the gates.
+        typedef float Eight __attribute__((ext_vector_type(8)));
+        constexpr int kSteps32 = CB / 32, kPer = kThreads / kSteps, kHalves = CB / 8 / kPer;      // threads of a step, and how often eight columns each
+        static_assert(kHalves >= 1, "every thread has columns");
+        const int own = threadIdx.x / kPer;
+        Eight s[kSteps32], d[kSteps32], m[kHalves], y[kHalves];
+        float o[kHalves][8];
+        const E *grad_o = row_at<E>(p.grad_o, p.ld_go, b, p.T, min(chunk * kSteps + own, p.T - 1), h, p.Dv);
+        auto load = [&](int c0) {
 #pragma unroll
-            for (int step = 0; step < 2; ++step) {
-                if (!has_keys || step >= steps) continue;
-                const int from = (wave * 16 + at) * DV + c0 + step * 32 + group * 8;
+            for (int step = 0; step < kSteps32; ++step) {
+                const int from = (wave * 16 % DK + at) * DV + min(c0 + step * 32, DV - 32) + group * 8;
                 s[step] = *reinterpret_cast<const Eight *>(S + from);
                 d[step] = *reinterpret_cast<const Eight *>(D + from);
             }
+#pragma unroll
+            for (int half = 0; half < kHalves; ++half) {
+                const int c = c0 + (threadIdx.x % kPer * kHalves + half) * 8, from = own * DV + min(c, DV - 8);
+                m[half] = *reinterpret_cast<const Eight *>(M + from);
+                y[half] = *reinterpret_cast<const Eight *>(Y + from);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[half][e] = 0.0f;
+                read_columns<E, 8>(grad_o, c, p.Dv, o[half]);
+            }
+        };
+        constexpr int kWords = (int)(sizeof(ChunkGates) / 4), kTurns = (kWords + kThreads - 1) / kThreads;
+        int words[kTurns];
+#pragma unroll
+        for (int e = 0; e < kTurns; ++e) words[e] = reinterpret_cast<const int *>(p.gates + record)[min(e * kThreads + (int)threadIdx.x, kWords - 1)];
+        load(0);
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kTurns; ++e)
+            if (e * kThreads + (int)threadIdx.x < kWords) reinterpret_cast<int *>(&gates)[e * kThreads + threadIdx.x] = words[e];
+        if (threadIdx.x == 0) not_finite = 0;
+        __syncthreads();
+        const unsigned long long starts = gates.starts;
+        alive = gates.live;
+        for (int c0 = 0; c0 < p.Dv; c0 += CB) {
+            const int steps = min(kSteps32, (DV - c0) / 32);
+            if (c0 > 0) load(c0);
             {
-                constexpr int kPer = kThreads / kSteps, kHalves = 8 / kPer;        // threads of a row, and how often eight columns each
-                const int i = threadIdx.x / kPer, t = chunk * kSteps + i;
-                const bool live = bit_of(alive, i);
-                const float beta = gates.beta[i];
+                const bool live = bit_of(alive, own);
+                const float beta = gates.beta[own];
 #pragma unroll
                 for (int half = 0; half < kHalves; ++half) {
                     const int c = (threadIdx.x % kPer * kHalves + half) * 8;
-                    if (c >= 32 * steps) continue;
-                    const Eight m = *reinterpret_cast<const Eight *>(M + i * DV + c0 + c), y = *reinterpret_cast<const Eight *>(Y + i * DV + c0 + c);
-                    float u[8], v[8], o[8] = {};
-                    if (live) read_columns<E, 8>(row_at<E>(p.grad_o, p.ld_go, b, p.T, t, h, p.Dv), c0 + c, p.Dv, o);
+                    const bool in = live && c < 32 * steps;
+                    float u[8], v[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        dot_beta = live ? fmaf(m[e], y[e], dot_beta) : 0.0f;
-                        u[e] = live ? beta * m[e] : 0.0f;
-                        v[e] = live ? beta * y[e] : 0.0f;
+                        dot_beta = in ? fmaf(m[half][e], y[half][e], dot_beta) : dot_beta;
+                        u[e] = in ? beta * m[half][e] : 0.0f;
+                        v[e] = in ? beta * y[half][e] : 0.0f;
+                        o[half][e] = in ? o[half][e] : 0.0f;
                     }
-                    put_row<3>(U, i, c, u);
-                    put_row<3>(V, i, c, v);
-                    put_row<PE>(O, i, c, o);
+                    put_row<3>(U, own, c, u);
+                    put_row<3>(V, own, c, v);
+                    put_row<PE>(O, own, c, o[half]);
                 }
             }
             __syncthreads();
 #pragma unroll
-            for (int step = 0; step < 2; ++step) {
+            for (int step = 0; step < kSteps32; ++step) {
                 if (step >= steps) continue;
                 {
                     const int row = wave % 4;
@@ -544,16 +565,15 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
             Acc raw[4] = {};
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                __builtin_amdgcn_sched_barrier(0);
                 Frag mine[PE];
 #pragma unroll
-                for (int n = 0; n < PE; ++n) mine[n] = (is_p ? Q : K)[frag_at(row, s, n, KS, PE)];
+                for (int n = 0; n < PE; ++n) mine[n] = FragReader(is_p ? Q : K).at(row, s, n, KS, PE);
 #pragma unroll
                 for (int tile = 0; tile < 4; ++tile) {
                     if (tile > row) continue;
                     Frag other[PE];
 #pragma unroll
-                    for (int n = 0; n < PE; ++n) other[n] = K[frag_at(tile, s, n, KS, PE)];
+                    for (int n = 0; n < PE; ++n) other[n] = FragReader(K).at(tile, s, n, KS, PE);
                     raw[tile] = multiply<PE, PE, kOrder>(mine, other, raw[tile]);
                 }
             }
@@ -607,7 +627,6 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
         }
         if (!fine) not_finite = 1;
         {
-            constexpr int kPer = kThreads / kSteps;
 #pragma unroll
             for (int d = 1; d < kPer; d *= 2) dot_beta += __shfl_xor(dot_beta, d);
             if (threadIdx.x % kPer == 0) dbeta[threadIdx.x / kPer] = dot_beta;
@@ -617,16 +636,23 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
         if (has_keys) {
             const int d = wave * 16 + at, from = hk * p.Dk + min(d, p.Dk - 1);
             const bool key = d < p.Dk;
+            E k_of[4][4], q_of[4][4];
+#pragma unroll
+            for (int row = 0; row < 4; ++row)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t step = b * p.T + min(chunk * kSteps + row * 16 + group * 4 + r, p.T - 1);
+                    k_of[row][r] = static_cast<const E *>(p.k)[step * p.ld_k + from];
+                    q_of[row][r] = static_cast<const E *>(p.q)[step * p.ld_q + from];
+                }
 #pragma unroll
             for (int row = 0; row < 4; ++row) {
-                __builtin_amdgcn_sched_barrier(0);
                 float dot[4] = {};
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = row * 16 + group * 4 + r;
-                    const int64_t step = b * p.T + min(chunk * kSteps + i, p.T - 1);
                     const float f = bit_of(alive, i) ? gates.f[i] : 0.0f, t = bit_of(alive, i) ? gates.t[i] : 0.0f;
-                    const float k = to_f32(static_cast<const E *>(p.k)[step * p.ld_k + from]), q = to_f32(static_cast<const E *>(p.q)[step * p.ld_q + from]);
+                    const float k = to_f32(k_of[row][r]), q = to_f32(q_of[row][r]);
                     const float fq = p.scale * f * far_q[row][r], fk = -f * far_k[row][r], e = t * end[row][r];
                     const float to_later = t != 0.0f && key ? k * e : 0.0f;
                     at_end += to_later;
@@ -655,7 +681,7 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int n = 0; n < PE; ++n) key[s][n] = keys[frag_at(wave, s, n, 2, PE)];
+                for (int n = 0; n < PE; ++n) key[s][n] = FragReader(keys).at(wave, s, n, 2, PE);
 #pragma unroll
             for (int row = 0; row < 4; ++row) {
                 __builtin_amdgcn_sched_barrier(0);
@@ -775,7 +801,7 @@ int run(const DeltaArgs &p, hipStream_t stream)
 {
     const int rc = wide_columns(p) ? run_back<E, DK, 2>(p, stream) : run_back<E, DK, 1>(p, stream);
     if (rc || p.chunks == 0) return rc;
-    const size_t lds = (6 + kExact<E>) * sizeof(Plane);            // (the results' rows, 64 of DK + 8, are less)
+    const size_t lds = std::max((6 + kExact<E>) * sizeof(typename Rows<grad_columns(DK)>::Plane), 6 * sizeof(Plane));   // (the results' rows, 64 of DK + 8, are less)
     if (const int failed = make_room_for(reinterpret_cast<const void *>(chunk_grad_kernel<E, DK>), lds)) return failed;
     hipLaunchKernelGGL((chunk_grad_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(grad_waves(DK) * kWave), lds, stream, p);
     return launched("delta scan gradient");

@@ -8,34 +8,45 @@
 namespace marl {
 namespace {
 
-// Gates of a chunk, by one wave, a step a lane.
-__device__ __forceinline__ void gates_of(const DeltaArgs &p, int64_t b, int h, int chunk, int bad, ChunkGates &out)
-{
-    const int i = threadIdx.x % kWave, t = chunk * kSteps + i;
-    const int64_t step = b * p.T + t;
-    const bool live = t < p.T && (!p.filled || p.filled[step]);
-    float g = live ? p.log_decay[step * p.Hv + h] : 0.0f;
-    const bool start = live && ((p.reset && p.reset[step]) || g == -__builtin_inff());
-    g = start ? 0.0f : g < -200.0f ? -200.0f : g;
-    const unsigned long long starts = __ballot(start);
-    const unsigned long long so_far = starts << (63 - i);
-    const int first = so_far ? i - __clzll((long long)so_far) : 0;                 // of the lane's sequence
-    double G = g;
-    for (int d = 1; d < kWave; d *= 2) {
-        const double before = __shfl_up(G, d);
-        if (i - d >= first) G += before;
+// Gates of a chunk, by one wave, a step a lane.  asked: what they are made of, on its way; put: the gates.
+struct GateInputs {
+    float log_decay, beta;
+    bool live, reset;
+    __device__ __forceinline__ GateInputs(const DeltaArgs &p, int64_t b, int h, int chunk)
+    {
+        const int t = chunk * kSteps + (int)threadIdx.x % kWave;
+        const int64_t step = b * p.T + min(t, p.T - 1);
+        log_decay = p.log_decay[step * p.Hv + h];
+        beta = p.beta[step * p.Hv + h];
+        reset = p.reset && p.reset[step];
+        live = t < p.T && (!p.filled || p.filled[step]);
     }
-    const int part = __popcll(so_far);
-    const double G_end = __shfl(G, 63);
-    const int part_end = __shfl(part, 63);
-    out.G[i] = G;
-    out.f[i] = part == 0 ? decay_of(G) : 0.0f;
-    out.t[i] = !live ? -1.0f : part == part_end ? decay_of(G_end - G) : 0.0f;
-    if (i == kSteps - 1) out.whole = out.f[i];
-    out.beta[i] = live ? p.beta[step * p.Hv + h] : 0.0f;
-    const unsigned long long alive = __ballot(live);
-    if (i == 0) { out.starts = starts; out.live = alive; out.bad = bad; }
-}
+    __device__ __forceinline__ void put(ChunkGates &out) const
+    {
+        const int i = threadIdx.x % kWave;
+        float g = live ? log_decay : 0.0f;
+        const bool start = live && (reset || g == -__builtin_inff());
+        g = start ? 0.0f : g < -200.0f ? -200.0f : g;
+        const unsigned long long starts = __ballot(start), so_far = starts << (63 - i);
+        const int first = so_far ? i - __clzll((long long)so_far) : 0;             // of the lane's sequence
+        double G = g;
+        for (int d = 1; d < kWave; d *= 2) {
+            const double before = __shfl_up(G, d);
+            if (i - d >= first) G += before;
+        }
+        const int part = __popcll(so_far);
+        const double G_end = __shfl(G, 63);
+        const int part_end = __shfl(part, 63);
+        const float f = part == 0 ? decay_of(G) : 0.0f;
+        out.G[i] = G;
+        out.f[i] = f;
+        out.t[i] = !live ? -1.0f : part == part_end ? decay_of(G_end - G) : 0.0f;
+        out.beta[i] = live ? beta : 0.0f;
+        const unsigned long long alive = __ballot(live);
+        if (i == kSteps - 1) out.whole = f;
+        if (i == 0) { out.starts = starts; out.live = alive; out.bad = 0; }
+    }
+};
 
 // Rows of a chunk as planes in shared memory, zeros in padding and behind Dk.
 template <typename E, int DK>
@@ -121,35 +132,33 @@ __device__ __forceinline__ void write_square(const float *from, int ld, Frag *to
     }
 }
 
-// A workgroup per key head and chunk: K and Q as fragments, and N and P of every value head that shares them.
+// A workgroup per key head and chunk: K and Q as fragments, and N and P of every value head that shares them, four at a time.
 template <typename E, int DK>
-__global__ __launch_bounds__(kDeltaThreads) void chunk_kernel(DeltaArgs p)
+__global__ __launch_bounds__(kDeltaThreads, 2) void chunk_kernel(DeltaArgs p)
 {
     constexpr int PE = kExact<E>, LN = kSteps + 1, kOrder = PE == 1 ? 0 : 2;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     auto &K = *reinterpret_cast<KeyRows<E, DK> *>(lds);
     auto &Q = *reinterpret_cast<KeyRows<E, DK> *>(lds + sizeof(K));
     float *A = reinterpret_cast<float *>(lds + 2 * sizeof(K)), *N = A + kSteps * LN;
-    __shared__ ChunkGates gates;
+    __shared__ ChunkGates gates_of[4];
     __shared__ int bad_rows, bad;
     const int chunk = (int)(blockIdx.x % p.chunks), hk = (int)(blockIdx.x / p.chunks % p.Hk);
     const int64_t b = blockIdx.x / p.chunks / p.Hk;
     const int lane = threadIdx.x % kWave, wave = wave_index(), at = lane % 16, group = lane / 16;
+    const int shared = p.Hv / p.Hk;
     if (threadIdx.x == 0) bad_rows = 0;
     unsigned long long live;
     {
-        const int t = chunk * kSteps + lane;
-        live = __ballot(t < p.T && (!p.filled || p.filled[b * p.T + t]));
-    }
-    __syncthreads();
-    {
+        const GateInputs inputs(p, b, hk * shared + min(wave, shared - 1), chunk);
+        live = __ballot(inputs.live);
+        __syncthreads();
         bool fine = K.fill(p, p.k, p.ld_k, b, hk, chunk, live);
         fine = Q.fill(p, p.q, p.ld_q, b, hk, chunk, live) && fine;
         if (!fine) bad_rows = 1;
+        inputs.put(gates_of[wave]);
     }
     __syncthreads();
-    K.write(p.K + (int64_t)blockIdx.x * key_frags(DK, PE), p.KT + (int64_t)blockIdx.x * key_frags(DK, PE));
-    Q.write(p.Q + (int64_t)blockIdx.x * key_frags(DK, PE), p.QT ? p.QT + (int64_t)blockIdx.x * key_frags(DK, PE) : nullptr);
     Acc kk[4] = {}, qk[4] = {};
 #pragma unroll
     for (int s = 0; s < DK / 32; ++s) {
@@ -165,15 +174,24 @@ __global__ __launch_bounds__(kDeltaThreads) void chunk_kernel(DeltaArgs p)
             qk[tile] = multiply<PE, PE, kOrder>(q, other, qk[tile]);
         }
     }
-    const int shared = p.Hv / p.Hk;
     for (int member = 0; member < shared; ++member) {
-        const int h = hk * shared + member;
-        const int64_t record = (b * p.Hv + h) * p.chunks + chunk;
-        __syncthreads();
-        if (wave == 0) gates_of(p, b, h, chunk, 0, gates);
+        const int64_t record = (b * p.Hv + hk * shared + member) * p.chunks + chunk;
+        if (member > 0) {
+            if (member % 4 == 0) {
+                __syncthreads();
+                GateInputs(p, b, hk * shared + min(member + wave, shared - 1), chunk).put(gates_of[wave]);
+            }
+            __syncthreads();
+        }
+        ChunkGates &gates = gates_of[member % 4];
         if (threadIdx.x == 0) bad = bad_rows;
-        __syncthreads();
         const unsigned long long starts = gates.starts;
+        unsigned long long before[4];                  // steps that hand something to the lane's rows
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = wave * 16 + group * 4 + r;
+            before[r] = bit_of(live, i) ? upto(starts, i) & live : 0;
+        }
         // P through the room of N, then A
         bool fine = true;
 #pragma unroll
@@ -182,46 +200,62 @@ __global__ __launch_bounds__(kDeltaThreads) void chunk_kernel(DeltaArgs p)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int i = wave * 16 + group * 4 + r;
-                const bool on = j <= i && bit_of(live, i) && bit_of(live, j) && joined(starts, i, j);
-                const float e = on ? decay_of(gates.G[i] - gates.G[j]) : 0.0f;
-                const float a = on && j < i ? e * kk[tile][r] : 0.0f, v = on ? p.scale * e * qk[tile][r] : 0.0f;
+                float a = 0.0f, v = 0.0f;
+                if (tile <= wave) {
+                    const bool on = bit_of(before[r], j);
+                    const float e = decay_of(gates.G[i] - gates.G[j]);
+                    a = on && j < i ? e * kk[tile][r] : 0.0f;
+                    v = on ? p.scale * e * qk[tile][r] : 0.0f;
+                    fine = fine && (a + v) * 0.0f == 0.0f;
+                }
                 A[i * LN + j] = a;
                 N[i * LN + j] = v;
-                fine = fine && (a + v) * 0.0f == 0.0f;
             }
         }
         __syncthreads();
         write_square<kFine<E>, false>(N, LN, p.P + record * square_frags(kFine<E>));
         if (p.PT) write_square<3, true>(N, LN, p.PT + record * square_frags(3));
-        __syncthreads();
-        for (int e = threadIdx.x; e < kSteps * LN; e += kDeltaThreads) N[e] = 0.0f;
-        __syncthreads();
         // blocks on the diagonal: N_i = A_i - sum_j A_ij beta_j N_j, a column a lane
+        float n[16];
         {
-            float n[16];
+            const float *own = A + (wave * 16) * LN + wave * 16;
+            float column[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) column[i] = own[i * LN + at];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                float v = A[(wave * 16 + i) * LN + wave * 16 + at];
+                float v = column[i];
 #pragma unroll
-                for (int j = 0; j < i; ++j) v = fmaf(-A[(wave * 16 + i) * LN + wave * 16 + j] * gates.beta[wave * 16 + j], n[j], v);
-                n[i] = i > at ? v : 0.0f;
-                if (group == 0) N[(wave * 16 + i) * LN + wave * 16 + at] = n[i];
-                fine = fine && n[i] * 0.0f == 0.0f;
+                for (int j = 0; j < i; ++j) v = fmaf(-own[i * LN + j], n[j], v);
+                v = i > at ? v : 0.0f;
+                fine = fine && v * 0.0f == 0.0f;
+                n[i] = v * gates.beta[wave * 16 + i];
+                column[i] = v;
             }
+            __syncthreads();                           // P has been read
+            if (group == 0)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) N[(wave * 16 + i) * LN + wave * 16 + at] = column[i];
+            for (int e = lane; e < 16 * kSteps; e += kWave)                        // above the diagonal
+                if (e % kSteps >= wave * 16 + 16) N[(wave * 16 + e / kSteps) * LN + e % kSteps] = 0.0f;
         }
         __syncthreads();
         // block columns: N_ij = (I - N_ii beta) (A_ij - sum_m A_im beta_m N_mj), downwards
         for (int i = wave + 1; i < 4; ++i) {
             Acc c;
+#pragma unroll
             for (int r = 0; r < 4; ++r) c[r] = A[(i * 16 + group * 4 + r) * LN + wave * 16 + at];
-            c = product((i - wave) * 16, c, [&](int row, int k) { return -A[(i * 16 + row) * LN + wave * 16 + k] * gates.beta[wave * 16 + k]; },
-                        [&](int k, int col) { return N[(wave * 16 + k) * LN + wave * 16 + col]; });
+            for (int m = wave; m < i; ++m)
+                c = product(c, [&](int row, int k) { return -A[(i * 16 + row) * LN + m * 16 + k] * gates.beta[m * 16 + k]; },
+                            [&](int k, int col) { return N[(m * 16 + k) * LN + wave * 16 + col]; });
+#pragma unroll
             for (int r = 0; r < 4; ++r) N[(i * 16 + group * 4 + r) * LN + wave * 16 + at] = c[r];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            c = product(16, c, [&](int row, int k) { return -N[(i * 16 + row) * LN + i * 16 + k] * gates.beta[i * 16 + k]; },
+            c = product(c, [&](int row, int k) { return -N[(i * 16 + row) * LN + i * 16 + k] * gates.beta[i * 16 + k]; },
                         [&](int k, int col) { return N[(i * 16 + k) * LN + wave * 16 + col]; });
             __builtin_amdgcn_wave_barrier();
+#pragma unroll
             for (int r = 0; r < 4; ++r) N[(i * 16 + group * 4 + r) * LN + wave * 16 + at] = c[r];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -250,6 +284,8 @@ __global__ __launch_bounds__(kDeltaThreads) void chunk_kernel(DeltaArgs p)
         int *to = reinterpret_cast<int *>(p.gates + record);
         for (int e = threadIdx.x; e < (int)(sizeof(ChunkGates) / 4); e += kDeltaThreads) to[e] = from[e];
     }
+    K.write(p.K + (int64_t)blockIdx.x * key_frags(DK, PE), p.KT + (int64_t)blockIdx.x * key_frags(DK, PE));
+    Q.write(p.Q + (int64_t)blockIdx.x * key_frags(DK, PE), p.QT ? p.QT + (int64_t)blockIdx.x * key_frags(DK, PE) : nullptr);
 }
 
 // The chunks of one head one after the other, for 16 NT value columns: tile n of a lane's column l % 16 is column NT (l % 16) + n.  Wave w has
