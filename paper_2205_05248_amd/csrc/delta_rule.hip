@@ -52,7 +52,7 @@ __global__ __launch_bounds__(kDeltaThreads) void step_kernel(StepArgs p)
     for (int r = 0; r < kRowsHeld; ++r) {
         const int d = r * groups + y;
         if (r * groups >= p.Dk) break;
-        held[r] = in && d < p.Dk && !fresh ? __builtin_nontemporal_load(reinterpret_cast<const Vec *>(p.s_in + state + (int64_t)d * p.Dv)) : (Vec)0.0f;
+        held[r] = in && d < p.Dk && !fresh ? *reinterpret_cast<const Vec *>(p.s_in + state + (int64_t)d * p.Dv) : (Vec)0.0f;
         kd[r] = d < p.Dk ? to_f32(k[d]) : 0.0f;
         const float qd = d < p.Dk ? to_f32(q[d]) : 0.0f;
         if (d < p.Dk) {

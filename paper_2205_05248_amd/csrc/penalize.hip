@@ -215,7 +215,7 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = from_f32<E>(z[k]);
         if (j >= skew && j + V <= n) {
-            *reinterpret_cast<typename P::Loose *>(out + j) = v;
+            __builtin_nontemporal_store(v, reinterpret_cast<typename P::Loose *>(out + j));
         } else {
 #pragma unroll
             for (int k = 0; k < V; ++k)
