@@ -110,7 +110,8 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
     const float frequency = p.frequency ? p.frequency[row] : 0.0f;
     const bool counts = length > 0 || p.M > 0;
     if (counts) {
-        for (int w = threadIdx.x * 4; w < end - begin; w += THREADS * 4) *reinterpret_cast<uint4 *>(words + w) = make_uint4(0, 0, 0, 0);
+        // up to the end of the last vector, all of whose words are looked at
+        for (int w = threadIdx.x * 4; w < (end - begin + V - 1) / V * V; w += THREADS * 4) *reinterpret_cast<uint4 *>(words + w) = make_uint4(0, 0, 0, 0);
         __syncthreads();
         const int before = skew - begin;                               // place of an id in the piece, if it has one
         auto place_of = [&](int id) {

@@ -70,6 +70,18 @@ def test_penalize(size, dtype, allowed):
     check(s, run(s))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("V", [1, 3, 9, 10, 12, 41, 44, 970, 8195, 8196])
+def test_rows_that_end_inside_a_vector(V, dtype):
+    """With a history and no bias, after calls that left biases' marks behind in every compute unit's shared memory: words behind the row's end count for
+    nothing."""
+    for _ in range(2):
+        run(make(600, V + 16, 40, 64, dtype, 3 * V))
+    for seed in range(3):
+        s = make(300, V, 6, 0, dtype, V + seed, "none")
+        check(s, run(s))
+
+
 @pytest.mark.parametrize("V", [40, 2000, 9001])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_wider_rows_and_in_place(V, in_place):
