@@ -674,7 +674,7 @@ int marl_distill_grad(int32_t dtype, int32_t R, int32_t V, int32_t K, const void
  * Edit of R rows of V logits between the network and the sampling.  Per row, with c[j] the number of times that j was
  * generated and `seen` for what stands in the prompt or was generated:
  *   z = logit;   seen: z > 0 ? z / repetition : z * repetition;   z -= c > 0 ? presence : 0;   z -= frequency c
- *   z += the biases listed for j, in their order;   not allowed: z = -infinity, whatever the logit holds
+ *   z += the sum of the biases listed for j;   not allowed: z = -infinity, whatever the logit holds
  *   logits     dev [R,V] elem, rows ld apart      out dev [R,V] elem, rows ld_out apart; may be logits (same ld)
  *   history    dev [R,L] i32 or NULL (L = 0), rows ld_history apart: the prompt, then what was generated; ids outside
  *              [0, V) count for nothing

@@ -172,6 +172,7 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
         __syncthreads();
     }
     const float inverse = 1.0f / rho;
+    const bool divides = !(rho >= 1e-6f && rho <= 1e6f);               // the reciprocal or its products may leave the range of fp32
 #pragma unroll
     for (int q = 0; q < kVectors; ++q) {
         const int j = own + q * THREADS * V;
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
                     // z / rho from its reciprocal, corrected by what is left over: as near as a division, which is four times as long
                     const float guess = z[k] * inverse, divided = fmaf(fmaf(-guess, rho, z[k]), inverse, guess);
                     const bool usual = fabsf(z[k]) < 1e30f && fabsf(z[k]) > 1e-30f;
-                    const float less = z[k] > 0.0f ? (usual ? divided : guess) : z[k] * rho;
+                    const float less = z[k] > 0.0f ? (divides ? z[k] / rho : usual ? divided : guess) : z[k] * rho;
                     const unsigned c = w[k] & kCount;
                     const float seen = w[k] & (kPrompt | kCount) ? less : z[k];
                     z[k] = c ? (seen - presence) - frequency * (float)c : seen;
@@ -203,9 +204,11 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
                     for (int k = 0; k < V; ++k)
                         if (w[k] & kBiased) {
                             if (*biases.n <= kNumbered) z[k] += biases.value[w[k] >> kBiasShift & (kNumbered - 1)];
-                            else
-                                for (int m = 0; m < *biases.n; ++m)
-                                    if (biases.at[m] == j - begin + k) z[k] += biases.value[m];
+                            else {
+                                float sum = 0.0f;
+                                for (int m = 0; m < *biases.n; ++m) sum += biases.at[m] == j - begin + k ? biases.value[m] : 0.0f;
+                                z[k] += sum;
+                            }
                         }
             }
         }

@@ -82,6 +82,34 @@ def test_rows_that_end_inside_a_vector(V, dtype):
         check(s, run(s))
 
 
+def test_repetition_of_any_size():
+    """Quotients and products that leave the range of fp32 are infinite or 0 there, and no NaN; all others are as near as ever."""
+    rho = torch.tensor([1e-39, 1e-30, 1e-7, 2e-6, 5e5, 1e7, 1e30, 3e38, float("inf")])
+    s = make(9, 64, 30, 0, "fp32", 11, "none")
+    s["logits"] *= torch.tensor([1e-35, 1e-20, 1.0, 1e10]).repeat(16)
+    s["repetition"], s["presence"], s["frequency"], s["length"][:], s["prompt"][:] = rho, None, None, 30, 30
+    out = host(run(s))
+    with np.errstate(over="ignore", under="ignore"):
+        want = orc.penalize(host(s["logits"]), host(s["history"]), host(s["length"]), host(s["prompt"]), host(rho)).astype(np.float32).astype(np.float64)
+    assert not np.isnan(out).any()
+    large = np.abs(want) > 2.0 ** -100                                   # what is smaller may be flushed on the way
+    assert (np.isinf(out) == np.isinf(want)).all() and (np.sign(out) == np.sign(want))[large].all()
+    finite = large & np.isfinite(want)
+    # a product or quotient of its own: half a step, or with the reciprocal's rounding and the product's three of them
+    assert (np.abs(out - want)[finite] <= 3 * 2.0 ** -24 * np.abs(want)[finite]).all() and (np.abs(out)[~large] <= 2.0 ** -99).all()
+
+
+@pytest.mark.parametrize("count", [64, 65, 300])
+def test_biases_that_cancel(count):
+    """Their sum is formed on its own, however many a piece has: two large ones leave the logit its digits."""
+    s = make(2, 400, 0, count, "fp32", 12, "none")
+    s["bias_id"][:] = torch.arange(count).to(torch.int32)
+    s["bias_id"][:, -1] = 0
+    s["bias_value"][:, 0], s["bias_value"][:, -1] = 2.0 ** 30, -2.0 ** 30
+    check(s, run(s))
+    assert torch.equal(run(s)[:, 0].cpu(), s["logits"][:, 0])
+
+
 @pytest.mark.parametrize("V", [40, 2000, 9001])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_wider_rows_and_in_place(V, in_place):
