@@ -189,14 +189,23 @@ __global__ __launch_bounds__(THREADS) void penalize_kernel(PenalizeArgs p)
                 any |= four.x | four.y | four.z | four.w;
             }
             if (any) {
+                float less[V];
+                if (divides) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) less[k] = z[k] > 0.0f ? z[k] / rho : z[k] * rho;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        // z / rho from its reciprocal, corrected by what is left over: as near as a division, which is four times as long
+                        const float guess = z[k] * inverse, divided = fmaf(fmaf(-guess, rho, z[k]), inverse, guess);
+                        const bool usual = fabsf(z[k]) < 1e30f && fabsf(z[k]) > 1e-30f;
+                        less[k] = z[k] > 0.0f ? (usual ? divided : guess) : z[k] * rho;
+                    }
+                }
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
-                    // z / rho from its reciprocal, corrected by what is left over: as near as a division, which is four times as long
-                    const float guess = z[k] * inverse, divided = fmaf(fmaf(-guess, rho, z[k]), inverse, guess);
-                    const bool usual = fabsf(z[k]) < 1e30f && fabsf(z[k]) > 1e-30f;
-                    const float less = z[k] > 0.0f ? (divides ? z[k] / rho : usual ? divided : guess) : z[k] * rho;
                     const unsigned c = w[k] & kCount;
-                    const float seen = w[k] & (kPrompt | kCount) ? less : z[k];
+                    const float seen = w[k] & (kPrompt | kCount) ? less[k] : z[k];
                     z[k] = c ? (seen - presence) - frequency * (float)c : seen;
                 }
                 if (any & kBiased)
