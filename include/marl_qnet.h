@@ -587,10 +587,10 @@ int marl_muon_step(int32_t dtype, int32_t L, int32_t rows, int32_t cols, const v
  *   o          dev [B,T,Hv,Dv] elem, rows ld_o apart; no input
  *   s_last     dev [B,Hv,Dk,Dv] f32 or NULL          state after step T-1 (s_first if T is 0); may be s_first
  *   keep       nonzero: the workspace afterwards holds what marl_delta_scan_grad starts from
- * 1 <= Dk <= 128, 1 <= Dv <= 1024, 1 <= Hk <= Hv <= 1024.  B and T may be 0 (B Hv < 2^24, B T < 2^30); row distances are
- * below 2^24.  The state stays bounded for keys of norm at most 1 with beta between 0 and 2 and log_decay at most 0;
- * beyond that it grows as the formula says.  An infinity or NaN reaches no step before its own and none of another
- * sequence.
+ * 1 <= Dk <= 128, 1 <= Dv <= 1024, 1 <= Hk <= Hv <= 1024.  B and T may be 0; B T < 2^30, B Hv ceil(T / 64) and
+ * B Hv ceil(Dv / 32) < 2^23 - 4, row distances < 2^24.  The state stays bounded for keys of norm at most 1 with beta
+ * between 0 and 2 and log_decay at most 0; beyond that it grows as the formula says.  An infinity or NaN reaches no step
+ * before its own and none of another sequence.
  */
 int marl_delta_scan_workspace_bytes(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_t Hv, int32_t Dk, int32_t Dv,
                                     int32_t keep, size_t *bytes);
@@ -626,7 +626,7 @@ int marl_delta_scan_grad(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_
  *   reset  dev [n] u8 or NULL
  *   s_in   dev [slots,Hv,Dk,Dv] f32     s_out dev [slots,Hv,Dk,Dv] f32, only the listed rows are written; may be s_in
  *   o      dev [n,Hv,Dv] elem, rows ld_o apart
- * n may be 0; slots >= 1, and without `slot` n <= slots; n Hv < 2^24.
+ * n may be 0; slots >= 1, and without `slot` n <= slots; n Hv ceil(Dv / 32) < 2^24.
  */
 int marl_delta_step(int32_t dtype, int32_t n, int32_t Hk, int32_t Hv, int32_t Dk, int32_t Dv, const void *q,
                     int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v, const float *log_decay,
@@ -649,7 +649,8 @@ int marl_delta_step(int32_t dtype, int32_t n, int32_t Hk, int32_t Hv, int32_t Dk
  *   log_rest   dev [R] f32 or NULL     log q_r, -infinity if no place is left; written with tail nonzero only
  * A row without any kept alternative has loss 0 and no gradient, and so has one with nothing available (log_sum and
  * log_rest -infinity).  An available NaN or z of +infinity, or a kept value of NaN or +infinity, makes the row's loss NaN
- * (the first two its log_sum and log_rest too).  1 <= K <= 64; R may be 0; 1 <= V < 2^30, R < 2^31.
+ * (the first two its log_sum and log_rest too).  1 <= K <= 64; R may be 0; 1 <= V < 2^30, R < 2^24 (2^26 for V
+ * up to 2048).
  */
 int marl_distill_workspace_bytes(int32_t R, int32_t V, int32_t K, size_t *bytes);
 int marl_distill(int32_t dtype, int32_t R, int32_t V, int32_t K, const void *logits, int64_t ld, const int32_t *top_id,
@@ -684,7 +685,8 @@ int marl_distill_grad(int32_t dtype, int32_t R, int32_t V, int32_t K, const void
  *   bias_id    dev [R,M] i32, bias_value dev [R,M] f32, or both NULL (M = 0); ids outside [0, V) are left out
  *   allowed    dev i32 or NULL (all)        bit j % 32 of word j / 32; [R, ceil(V/32)], rows ld_allowed apart;
  *              ld_allowed = 0: one row of words for all
- * R may be 0; 1 <= V < 2^30, R < 2^24; 0 <= L < 2^24; 0 <= M <= 1024.
+ * R may be 0; 1 <= V < 2^30; R < 2^24, for V above 960 also R ceil((V + 63) / 8192) < 2^23; 0 <= L < 2^24;
+ * 0 <= M <= 1024.
  */
 int marl_penalize(int32_t dtype, int32_t R, int32_t V, const void *logits, int64_t ld, int32_t L,
                   const int32_t *history, int64_t ld_history, const int32_t *length, const int32_t *prompt,

@@ -139,7 +139,7 @@ void place(int dtype, DeltaArgs &p, char *workspace, bool keep)
     p.S = floats(r.S); p.M = floats(r.M); p.D = floats(r.D); p.Y = floats(r.Y);
 }
 
-constexpr int64_t kMostRow = (int64_t)1 << 24, kMostGroups = (int64_t)1 << 31;
+constexpr int64_t kMostRow = (int64_t)1 << 24;
 
 int heads_check(int dtype, int Hk, int Hv, int Dk, int Dv)
 {
@@ -151,8 +151,9 @@ int sizes_check(int dtype, int B, int T, int Hk, int Hv, int Dk, int Dv)
 {
     if (const int rc = heads_check(dtype, Hk, Hv, Dk, Dv)) return rc;
     if (B < 0 || T < 0 || (int64_t)B * Hv >= (1 << 24) || (int64_t)B * T >= (1 << 30)) return MARL_ERR_BAD_DIM;
-    // grids: a workgroup per record, and one per head and sixteen columns
-    if ((int64_t)B * Hv * ((T + kSteps - 1) / kSteps) >= kMostGroups || (int64_t)B * Hv * (padded_values(Dv) / 16) >= kMostGroups - 8) return MARL_ERR_BAD_DIM;
+    // a workgroup of up to 512 threads per record, and one of 256 per head and sixteen columns
+    const int64_t heads = (int64_t)B * Hv;
+    if (!fits_a_launch(heads * ((T + kSteps - 1) / kSteps), 512) || !fits_a_launch(heads * (padded_values(Dv) / 16) + 8, kDeltaThreads)) return MARL_ERR_BAD_DIM;
     return MARL_OK;
 }
 bool row_fits(int64_t ld, int H, int D) { return ld >= (int64_t)H * D && ld < kMostRow; }
@@ -242,7 +243,7 @@ int marl_delta_step(int32_t dtype, int32_t n, int32_t Hk, int32_t Hv, int32_t Dk
                     int32_t slots, const uint8_t *reset, const float *s_in, float *s_out, void *o, int64_t ld_o, void *hip_stream)
 {
     if (const int rc = heads_check(dtype, Hk, Hv, Dk, Dv)) return rc;
-    if (n < 0 || slots < 1 || (!slot && n > slots) || (int64_t)n * Hv >= (1 << 24)) return MARL_ERR_BAD_DIM;
+    if (n < 0 || slots < 1 || (!slot && n > slots) || !fits_a_launch((int64_t)n * Hv * (padded_values(Dv) / 32), kDeltaThreads)) return MARL_ERR_BAD_DIM;
     if (!std::isfinite(scale)) return MARL_ERR_BAD_ARG;
     if (n == 0) return MARL_OK;
     if (!q || !k || !v || !log_decay || !beta || !s_in || !s_out || !o) return MARL_ERR_NULL;

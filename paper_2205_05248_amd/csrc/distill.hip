@@ -564,6 +564,9 @@ Cut part_cut(int R, int V)
     return cut;
 }
 
+// A short row takes up to 64 lanes, a long one 256.
+bool rows_fit(int R, int V) { return V > kShort ? R < 1 << 24 : R < 1 << 26; }
+
 size_t distill_workspace(int R, int V)
 {
     if (V <= kShort) return 0;
@@ -595,7 +598,7 @@ int run_forward(DistillArgs p, hipStream_t stream)
     const Cut cut = part_cut(p.R, p.V);
     p.parts = cut.parts;
     p.per = cut.per;
-    if ((int64_t)p.R * p.parts >= ((int64_t)1 << 31)) return MARL_ERR_BAD_DIM;
+    if (!fits_a_launch((int64_t)p.R * p.parts, kThreads)) return MARL_ERR_BAD_DIM;
     hipLaunchKernelGGL(long_rows_kernel<E>, dim3((unsigned)(p.R * p.parts)), dim3(kThreads), 0, stream, p);
     if (p.parts > 1) hipLaunchKernelGGL(join_kernel<E>, dim3((unsigned)p.R), dim3(kWave), 0, stream, p);
     return launched("distill");
@@ -626,7 +629,7 @@ int run_backward(DistillArgs p, hipStream_t stream)
     if (p.grad_logits == p.logits) cut = {1, cut.parts * cut.per};
     p.parts = cut.parts;
     p.per = cut.per;
-    if ((int64_t)p.R * p.parts >= ((int64_t)1 << 31)) return MARL_ERR_BAD_DIM;
+    if (!fits_a_launch((int64_t)p.R * p.parts, kThreads)) return MARL_ERR_BAD_DIM;
     hipLaunchKernelGGL(long_grad_kernel<E>, dim3((unsigned)(p.R * p.parts)), dim3(kThreads), 0, stream, p);
     return launched("distill gradient");
 }
@@ -641,7 +644,7 @@ extern "C" {
 int marl_distill_workspace_bytes(int32_t R, int32_t V, int32_t K, size_t *bytes)
 {
     if (!bytes) return MARL_ERR_NULL;
-    if (R < 0 || V < 1 || V >= (1 << 30) || K < 1 || K > kMostKept) return MARL_ERR_BAD_DIM;
+    if (R < 0 || V < 1 || V >= (1 << 30) || K < 1 || K > kMostKept || !rows_fit(R, V)) return MARL_ERR_BAD_DIM;
     *bytes = distill_workspace(R, V);
     return MARL_OK;
 }
@@ -652,7 +655,7 @@ int marl_distill(int32_t dtype, int32_t R, int32_t V, int32_t K, const void *log
 {
     const int rc = logit_rows_check(dtype, R, V, logits, ld, avail, ld_avail, scale);
     if (rc) return rc;
-    if (K < 1 || K > kMostKept || workspace_bytes < distill_workspace(R, V)) return MARL_ERR_BAD_DIM;
+    if (K < 1 || K > kMostKept || !rows_fit(R, V) || workspace_bytes < distill_workspace(R, V)) return MARL_ERR_BAD_DIM;
     if (R == 0) return MARL_OK;
     if (!top_id || !top_value || !loss || (workspace_bytes && !workspace)) return MARL_ERR_NULL;
     if (!aligned_to(workspace, 256)) return MARL_ERR_BAD_ARG;
@@ -670,7 +673,7 @@ int marl_distill_grad(int32_t dtype, int32_t R, int32_t V, int32_t K, const void
 {
     const int rc = logit_rows_check(dtype, R, V, logits, ld, avail, ld_avail, scale);
     if (rc) return rc;
-    if (K < 1 || K > kMostKept || ld_grad < V) return MARL_ERR_BAD_DIM;
+    if (K < 1 || K > kMostKept || !rows_fit(R, V) || ld_grad < V) return MARL_ERR_BAD_DIM;
     if (grad_logits && grad_logits == logits && ld_grad != ld) return MARL_ERR_BAD_ARG;
     if (R == 0) return MARL_OK;
     if (!top_id || !top_value || !log_sum || (tail && !log_rest) || !grad_loss || !grad_logits) return MARL_ERR_NULL;

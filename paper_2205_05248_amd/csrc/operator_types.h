@@ -22,6 +22,9 @@ __host__ __device__ __forceinline__ int element_bytes(int dtype) { return dtype 
 
 inline bool known_dtype(int dtype) { return dtype == MARL_DTYPE_F32 || dtype == MARL_DTYPE_BF16 || dtype == MARL_DTYPE_F16; }
 
+// A launch has fewer than 2^32 threads.
+inline bool fits_a_launch(int64_t groups, int threads) { return groups * threads < (int64_t)1 << 32; }
+
 inline bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 // Calls f with a value of the element type of `dtype`.

@@ -271,7 +271,7 @@ int marl_penalize(int32_t dtype, int32_t R, int32_t V, const void *logits, int64
         const auto go = [&](auto kernel, int threads, int piece) {
             const size_t lds = piece * sizeof(unsigned) + (1 + 2 * (size_t)M) * sizeof(int);       // 40 KB at most
             p.pieces = (int)(((int64_t)V + 63 + piece - 1) / piece);
-            if ((int64_t)R * p.pieces >= ((int64_t)1 << 31)) return (int)MARL_ERR_BAD_DIM;
+            if (!fits_a_launch((int64_t)R * p.pieces, threads)) return (int)MARL_ERR_BAD_DIM;
             hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)R * p.pieces)), dim3(threads), lds, stream, p);
             return launched("penalize");
         };

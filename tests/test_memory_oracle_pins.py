@@ -178,6 +178,11 @@ REFUSED = [
     (_penalize, "BAD_DTYPE", dict(dtype=4)), (_penalize, "BAD_DIM", dict(V=0)), (_penalize, "BAD_DIM", dict(ld=39)), (_penalize, "BAD_DIM", dict(ld_out=39)),
     (_penalize, "BAD_DIM", dict(ld_history=2)), (_penalize, "BAD_DIM", dict(ld_allowed=1)), (_penalize, "BAD_DIM", dict(M=1025)),
     (_penalize, "BAD_DIM", dict(L=1 << 24)), (_penalize, "BAD_DIM", dict(R=1 << 24)), (_penalize, "BAD_ARG", dict(out=P, ld_out=48)),
+    (_scan, "BAD_DIM", dict(B=1 << 12, Hv=1024, ld_v=4096, ld_o=4096, T=128)), (_scan, "BAD_DIM", dict(B=1 << 12, T=1, Hv=1024, Dv=64, ld_v=1 << 16, ld_o=1 << 16)),
+    (_scan_grad, "BAD_DIM", dict(B=1 << 12, T=1, Hv=1024, Dv=64, ld_v=1 << 16, ld_go=1 << 16, ld_gv=1 << 16)),
+    (_step, "BAD_DIM", dict(n=1 << 13, slots=1 << 13, Hv=1024, Dv=64, ld_v=1 << 16, ld_o=1 << 16)),
+    (_distill, "BAD_DIM", dict(R=1 << 26)), (_distill, "BAD_DIM", dict(R=1 << 24, V=2049, ld=2049)), (_distill_grad, "BAD_DIM", dict(R=1 << 26)),
+    (_distill_grad, "BAD_DIM", dict(R=1 << 24, V=2049, ld=2049, ld_out=2049)), (_penalize, "BAD_DIM", dict(R=1 << 23, V=961, ld=961, ld_out=961, ld_allowed=31)),
     *[(_penalize, "NULL", {n: 0}) for n in ("logits", "history", "ids", "values", "out")],
 ]
 
