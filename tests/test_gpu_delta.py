@@ -153,6 +153,29 @@ def test_rows_of_wider_arrays(dtype):
     check(run(s, gap=5), wanted(s))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("Dv,gap", [(17, 0), (17, 5), (31, 0), (32, 1), (33, 2), (50, 3)])
+def test_two_columns_a_lane(Dv, gap, dtype):
+    """Heads enough for the whole chip: a lane has two value columns, the last of an odd number one; rows begin at odd elements too."""
+    s = make(32, 66, 4, 8, 12, Dv, dtype, 70 + Dv, *masks(32, 66, Dv, 0.05))
+    check(run(s, gap=gap), wanted(s))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("size", [(2, 70, 1, 9, 20, 12), (1, 65, 2, 10, 128, 40), (1, 130, 1, 5, 64, 90)])
+def test_many_heads_of_one_key(size, dtype):
+    s = make(*size, dtype, 80 + size[3], *masks(size[0], size[1], 9, 0.05, False))
+    check(run(s), wanted(s))
+
+
+def test_sequences_that_end_with_a_chunk():
+    for T in (63, 64, 65, 128):
+        s = make(3, T, 1, 2, 32, 32, "bf16", 90 + T)
+        s["reset"] = torch.zeros(3, T, dtype=torch.uint8)
+        s["reset"][0, -1], s["reset"][1, min(T - 1, 63)], s["reset"][2, min(T - 1, 64)] = 1, 1, 1
+        check(run(s), wanted(s))
+
+
 def test_forward_alone_and_without_states():
     s = make(2, 90, 1, 2, 16, 24, "bf16", 14, first=False)
     o = run(s, train=False, last=False)
