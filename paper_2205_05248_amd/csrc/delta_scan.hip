@@ -1,6 +1,7 @@
 // Gated delta rule, forward: the matrices of every chunk side by side, then the way through the chunks.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "delta.h"
@@ -134,13 +135,13 @@ __device__ __forceinline__ void write_square(const float *from, int ld, Frag *to
 
 // A workgroup per key head and chunk: K and Q as fragments, and N and P of every value head that shares them, four at a time.
 template <typename E, int DK>
-__global__ __launch_bounds__(kDeltaThreads, 2) void chunk_kernel(DeltaArgs p)
+__global__ __launch_bounds__(kDeltaThreads, 3) void chunk_kernel(DeltaArgs p)
 {
     constexpr int PE = kExact<E>, LN = kSteps + 1, kOrder = PE == 1 ? 0 : 2;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     auto &K = *reinterpret_cast<KeyRows<E, DK> *>(lds);
     auto &Q = *reinterpret_cast<KeyRows<E, DK> *>(lds + sizeof(K));
-    float *A = reinterpret_cast<float *>(lds + 2 * sizeof(K)), *N = A + kSteps * LN;
+    float *A = reinterpret_cast<float *>(lds), *N = A + kSteps * LN;
     __shared__ ChunkGates gates_of[4];
     __shared__ int bad_rows, bad;
     const int chunk = (int)(blockIdx.x % p.chunks), hk = (int)(blockIdx.x / p.chunks % p.Hk);
@@ -174,6 +175,9 @@ __global__ __launch_bounds__(kDeltaThreads, 2) void chunk_kernel(DeltaArgs p)
             qk[tile] = multiply<PE, PE, kOrder>(q, other, qk[tile]);
         }
     }
+    K.write(p.K + (int64_t)blockIdx.x * key_frags(DK, PE), p.KT + (int64_t)blockIdx.x * key_frags(DK, PE));
+    Q.write(p.Q + (int64_t)blockIdx.x * key_frags(DK, PE), p.QT ? p.QT + (int64_t)blockIdx.x * key_frags(DK, PE) : nullptr);
+    __syncthreads();                                   // A and N take the room of K and Q
     for (int member = 0; member < shared; ++member) {
         const int64_t record = (b * p.Hv + hk * shared + member) * p.chunks + chunk;
         if (member > 0) {
@@ -284,8 +288,6 @@ __global__ __launch_bounds__(kDeltaThreads, 2) void chunk_kernel(DeltaArgs p)
         int *to = reinterpret_cast<int *>(p.gates + record);
         for (int e = threadIdx.x; e < (int)(sizeof(ChunkGates) / 4); e += kDeltaThreads) to[e] = from[e];
     }
-    K.write(p.K + (int64_t)blockIdx.x * key_frags(DK, PE), p.KT + (int64_t)blockIdx.x * key_frags(DK, PE));
-    Q.write(p.Q + (int64_t)blockIdx.x * key_frags(DK, PE), p.QT ? p.QT + (int64_t)blockIdx.x * key_frags(DK, PE) : nullptr);
 }
 
 // The chunks of one head one after the other, for 16 NT value columns: tile n of a lane's column l % 16 is column NT (l % 16) + n.  Wave w has
@@ -607,7 +609,7 @@ template <typename E, int DK>
 int run(const DeltaArgs &p, hipStream_t stream)
 {
     if (p.chunks > 0) {
-        const size_t lds = 2 * sizeof(KeyRows<E, DK>) + (size_t)2 * kSteps * (kSteps + 1) * sizeof(float);
+        const size_t lds = std::max(2 * sizeof(KeyRows<E, DK>), (size_t)2 * kSteps * (kSteps + 1) * sizeof(float));
         if (const int rc = make_room_for(reinterpret_cast<const void *>(chunk_kernel<E, DK>), lds)) return rc;
         hipLaunchKernelGGL((chunk_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
     }
