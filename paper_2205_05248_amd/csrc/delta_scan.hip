@@ -134,7 +134,7 @@ __device__ __forceinline__ void write_square(const float *from, int ld, Frag *to
 }
 
 // A workgroup per key head and chunk: K and Q as fragments, and N and P of every value head that shares them, four at a time.  Bound by what it
-// writes, 26 to 49 KB for a head's squares and 4 or 8 matrices of its keys: 0.8 GB of 4 x 8192 x 16 heads x 128 x 128 bf16 with what the backward
+// writes, 31 to 74 KB for the squares of a head and three or four matrices of its keys: 0.8 GB of 4 x 8192 x 16 heads x 128 x 128 bf16 with what the backward
 // pass needs in 207 us, 4.0 TB/s (253 us with two workgroups a compute unit, which is what shared memory had room for before N and A took that of K
 // and Q; 222 with three; with 128 registers some 25 are spilled, which costs fp32 rows, three planes each, more than the fourth workgroup gives).
 template <typename E, int DK>
