@@ -337,8 +337,18 @@ __device__ __forceinline__ Place place_of(int64_t heads, int Dv, int columns)
 }
 inline unsigned places(int64_t heads, int Dv, int columns) { return (unsigned)((heads * (padded_values(Dv) / columns) + 7) / 8 * 8); }
 
-// Whether a workgroup takes two tiles of columns: where there are more than two columns a lane can hold, and workgroups for the whole chip.
-inline bool wide_columns(const DeltaArgs &p) { return p.Dv > 16 && (int64_t)p.B * p.Hv * (padded_values(p.Dv) / 32) >= 256; }
+// Whether a workgroup takes two tiles of columns: every fragment is read once for both, for half as many waves on a compute unit.  It needs more than
+// two columns a lane can hold, and workgroups for the whole chip: one a compute unit where the keys' planes fill a wave's registers anyway, else two.
+// 8 | 32 sequences of 512 steps, 16 heads, 64 columns (256 | 1024 workgroups of two tiles), us with one and two, forward with keep and backward:
+//   128 keys, bf16  47, 50 | 208, 186   70, 54 | 251, 194       64 keys, bf16  31, 36 | 161, 139   44, 41 | 163, 153
+//   128 keys, fp32 106, 79 | 381, 301  104, 81 | 391, 303       64 keys, fp32  52, 48 | 228, 200   74, 53 | 278, 199
+//    32 keys, bf16  28, 34 | 152, 114   34, 49 | 153, 137       32 keys, fp32  40, 49 | 195, 177   50, 102 | 191, 404
+// (backward with 32 keys two tiles spill, and are not taken.)
+template <typename E, int DK>
+inline bool wide_columns(const DeltaArgs &p)
+{
+    return p.Dv > 16 && (int64_t)p.B * p.Hv * (padded_values(p.Dv) / 32) >= (kExact<E> * DK >= 128 ? 256 : 512);
+}
 
 int delta_scan_launch(int dtype, const DeltaArgs &p, hipStream_t stream);
 int delta_grad_launch(int dtype, const DeltaArgs &p, hipStream_t stream);

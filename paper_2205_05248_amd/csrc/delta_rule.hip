@@ -28,6 +28,8 @@ constexpr int kRowsHeld = 16;                          // state rows of a thread
 // A workgroup has one sequence, one head and up to 32 vectors of V columns; `vectors` (a power of two) threads lie along the columns,
 // the others along the rows.  The state is read once, into registers: with k.S and q.S of the state before,
 //   u = beta (v - a k.S)      S <- a S + k u      o = scale (a q.S + (q.k) u).
+// Bound by the states' bytes: 201 x 16 x 128 x 128, 421 MB, in 87 us, 4.8 TB/s, as a large copy (105 us with stores through the caches, which
+// keep what no one reads again; loads past them too: 95).
 template <typename E, int V>
 __global__ __launch_bounds__(kDeltaThreads) void step_kernel(StepArgs p)
 {

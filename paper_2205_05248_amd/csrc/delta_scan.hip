@@ -297,8 +297,13 @@ __global__ __launch_bounds__(kDeltaThreads, kExact<E> == 1 ? 4 : 3) void chunk_k
 // rows 16 w on of the chunk, and rows w DK / 4 on of the state, which stays in its accumulators; the others read it as planes from shared memory.
 // What a phase needs from memory is asked for where the same phase of the chunk before has used its registers, a whole chunk ahead, and
 // whether there is another chunk or not: behind a branch the compiler would wait for it at the next wait of any kind.
+// Bound by the chain of a chunk: three barriers, between them products that wait for the splitting of what the other waves made, some 830 vector and
+// 90 matrix instructions a wave; at 128 keys and columns a chunk takes 2.2 us with 16 columns (20011 steps, 16 heads, bf16: 700 us, 128 workgroups on
+// 256 compute units) and 5.0 with 32 (4 x 8192, with keep: 644 us, waves wait 31 % of their cycles, the matrix pipe is busy for 12 %).  Everything at
+// hand a chunk ahead takes 1.4 times the registers that a third workgroup on a compute unit would leave: with 168 they spill, 88 -> 196 us of the 320 x
+// 120 batch with 4 heads of 16.
 template <typename E, int DK, int NT, bool KEEP>
-__global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 256 ? 2 : 1) void scan_kernel(DeltaArgs p)
+__global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : DK == 32) ? 2 : 1) void scan_kernel(DeltaArgs p)
 {
     constexpr int PE = kExact<E>, PF = kFine<E>, KS = DK / 32, LS = DK + 8, LU = kSteps + 8, C = 16 * NT;
     constexpr int kTiles = (DK + 63) / 64;             // of the state, for a wave; of DK = 32 two waves have one
@@ -616,7 +621,7 @@ int run(const DeltaArgs &p, hipStream_t stream)
         if (const int rc = make_room_for(reinterpret_cast<const void *>(chunk_kernel<E, DK>), lds)) return rc;
         hipLaunchKernelGGL((chunk_kernel<E, DK>), dim3((unsigned)((int64_t)p.B * p.Hk * p.chunks)), dim3(kDeltaThreads), lds, stream, p);
     }
-    return wide_columns(p) ? run_scan<E, DK, 2>(p, stream) : run_scan<E, DK, 1>(p, stream);
+    return wide_columns<E, DK>(p) ? run_scan<E, DK, 2>(p, stream) : run_scan<E, DK, 1>(p, stream);
 }
 
 }  // namespace

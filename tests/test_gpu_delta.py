@@ -157,8 +157,9 @@ def test_rows_of_wider_arrays(dtype):
 @pytest.mark.parametrize("Dv,gap", [(17, 0), (17, 5), (31, 0), (32, 1), (33, 2), (50, 3)])
 def test_two_columns_a_lane(Dv, gap, dtype):
     """Heads enough for the whole chip: a lane has two value columns, the last of an odd number one; rows begin at odd elements too."""
-    s = make(32, 66, 4, 8, 12, Dv, dtype, 70 + Dv, *masks(32, 66, Dv, 0.05))
-    check(run(s, gap=gap), wanted(s))
+    for Dk, B in ((12, 64), (40, 64), (70, 32)):
+        s = make(B, 66, 2, 8, Dk, Dv, dtype, 70 + Dv, *masks(B, 66, Dv, 0.05))
+        check(run(s, gap=gap), wanted(s))
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
