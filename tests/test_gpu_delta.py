@@ -310,6 +310,45 @@ def test_step_in_place_and_without_slots():
     near(table, want, f32, REL, "table")
 
 
+def test_rows_of_a_table_behind_32_bits():
+    """Entries behind 2^32 of a table, and rows of v and o as far apart as they may be."""
+    slots = (1 << 32) // (128 * 128) + 5
+    table = torch.empty(slots, 1, 128, 128, device="cuda")
+    s = make_step(3, 4, 1, 1, 128, 128, "bf16", 33)
+    s["slot"] = torch.tensor([0, 1, 3], dtype=torch.int32)
+    where = torch.tensor([slots - 1, 7, slots - 4], dtype=torch.int32)
+    others = torch.tensor([slots - 2, slots - 3, (slots - 1) % (1 << 18), 6, 8])
+    table[others.cuda()] = 7.0
+    table[where.long().cuda()] = s["s_in"][[0, 1, 3]].cuda()
+    o = torch.empty(3, 1, 128, dtype=torch.bfloat16, device="cuda")
+    d = [s[n].cuda() for n in ("q", "k", "v", "log_decay", "beta")]
+    binding.marl_delta_step(*d, s["scale"], where.cuda(), None, table, table, o)
+    a = {k: host(v) if torch.is_tensor(v) else v for k, v in s.items()}
+    want_o, want = orc.delta_step(a["q"], a["k"], a["v"], a["log_decay"], a["beta"], s["scale"], a["slot"], None, a["s_in"])
+    near(o, want_o, o.dtype, REL, "o")
+    near(table[where.long().cuda()], want[[0, 1, 3]], f32, REL, "table")
+    assert (table[others.cuda()] == 7.0).all()
+
+
+def test_rows_as_far_apart_as_they_may_be():
+    T, ld = 300, (1 << 24) - 1
+    s = make(1, T, 1, 1, 16, 20, "bf16", 34)
+    far = torch.empty(T * ld, dtype=torch.bfloat16, device="cuda")
+    rows = lambda first, n: far[first:].as_strided((1, T, 1, n), (T * ld, ld, n, 1))
+    v, o, grad_o, grad_v = rows(0, 20), rows(101, 20), rows(202, 20), rows(303, 20)
+    q, k, grad_q, grad_k = rows(404, 16), rows(505, 16), rows(606, 16), rows(707, 16)
+    for to, n in ((v, "v"), (grad_o, "grad_o"), (q, "q"), (k, "k")):
+        to.copy_(s[n])
+    d = {n: t.cuda() for n, t in s.items() if torch.is_tensor(t)}
+    out = dict(o=o, s_last=torch.empty_like(d["s_first"]), grad_q=grad_q, grad_k=grad_k, grad_v=grad_v, grad_log_decay=torch.empty(1, T, 1, device="cuda"),
+               grad_beta=torch.empty(1, T, 1, device="cuda"), grad_s_first=torch.empty_like(d["s_first"]))
+    ws = torch.empty(binding.marl_delta_scan_workspace_bytes("bf16", 1, T, 1, 1, 16, 20, True), dtype=torch.uint8, device="cuda")
+    binding.marl_delta_scan(q, k, v, d["log_decay"], d["beta"], s["scale"], None, None, d["s_first"], o, out["s_last"], ws, keep=True)
+    binding.marl_delta_scan_grad(q, k, v, d["log_decay"], d["beta"], s["scale"], None, None, grad_o, d["grad_s_last"], ws, grad_q, grad_k, grad_v,
+                                 out["grad_log_decay"], out["grad_beta"], out["grad_s_first"])
+    check(out, wanted(s))
+
+
 def test_step_forgets_what_is_not_finite():
     s = make_step(4, 4, 1, 1, 8, 8, "fp32", 31)
     s["reset"] = torch.tensor([1, 0, 0, 0], dtype=torch.uint8)

@@ -100,6 +100,19 @@ def test_wider_rows_and_in_place(V, K, in_place):
 
 
 @pytest.mark.parametrize("V", [40, 5000])
+def test_rows_behind_32_bits(V):
+    R, K, ld = 3, 6, (1 << 31) + 24
+    s = make(R, V, K, "fp16", V + 1)
+    far = torch.empty(2 * ld + V, dtype=torch.float16, device="cuda").as_strided((R, V), (ld, 1))
+    far.copy_(s["logits"])
+    ids, values, o = s["top_id"].cuda(), s["top_value"].cuda(), {k: torch.empty(R, device="cuda") for k in ("loss", "log_sum", "log_rest")}
+    ws = torch.empty(binding.marl_distill_workspace_bytes(R, V, K), dtype=torch.uint8, device="cuda")
+    binding.marl_distill(far, ids, values, None, 0.8, True, o["loss"], o["log_sum"], o["log_rest"], ws)
+    binding.marl_distill_grad(far, ids, values, None, 0.8, True, o["log_sum"], o["log_rest"], s["grad_loss"].cuda(), far)
+    check(s, {**o, "grad": far}, 0.8, True)
+
+
+@pytest.mark.parametrize("V", [40, 5000])
 def test_an_index_listed_twice_counts_twice(V):
     s = make(12, V, 6, "fp32", 5)
     s["top_id"][:, 3] = s["top_id"][:, 0]

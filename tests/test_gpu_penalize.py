@@ -137,6 +137,17 @@ def test_a_token_many_times_and_a_bias_many_times():
     check(s, run(s))
 
 
+def test_rows_behind_32_bits():
+    R, V, ld = 3, 5000, (1 << 31) + 24
+    s = make(R, V, 50, 4, "fp16", 13)
+    far = torch.empty(2 * ld + V, dtype=torch.float16, device="cuda").as_strided((R, V), (ld, 1))
+    far.copy_(s["logits"])
+    d = {k: v.cuda() if torch.is_tensor(v) else v for k, v in s.items()}
+    binding.marl_penalize(far, d["history"], d["length"], d["prompt"], d["repetition"], d["presence"], d["frequency"], d["bias_id"], d["bias_value"],
+                          d["allowed"], far)
+    check(s, far)
+
+
 def test_history_and_bits_of_wider_arrays():
     s = make(4, 300, 40, 0, "bf16", 6)
     d = {k: v.cuda() if torch.is_tensor(v) else v for k, v in s.items()}
