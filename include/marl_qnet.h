@@ -590,7 +590,7 @@ int marl_muon_step(int32_t dtype, int32_t L, int32_t rows, int32_t cols, const v
  * 1 <= Dk <= 128, 1 <= Dv <= 1024, 1 <= Hk <= Hv <= 1024.  B and T may be 0; B T < 2^30, B Hv ceil(T / 64) and
  * B Hv ceil(Dv / 32) < 2^23 - 4, row distances < 2^24.  The state stays bounded for keys of norm at most 1 with beta
  * between 0 and 2 and log_decay at most 0; beyond that it grows as the formula says.  An infinity or NaN reaches no step
- * before its own and none of another sequence.
+ * before its own and none of another sequence; fp32 values beyond 3.36e38 may come out as either.
  */
 int marl_delta_scan_workspace_bytes(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_t Hv, int32_t Dk, int32_t Dv,
                                     int32_t keep, size_t *bytes);

@@ -184,9 +184,11 @@ __device__ __forceinline__ Acc careful_multiply(Acc c, const Frag *a, int tile, 
     }
     return c;
 }
-__device__ __forceinline__ bool all_finite(Acc a)
+// What planes can hold: the first one of a value beyond 3.39e38 is rounded to infinity.  A NaN does not fit either.
+__device__ __forceinline__ bool fits_planes(float size) { return size < 3.36e38f; }
+__device__ __forceinline__ bool all_finite(Acc a)      // (and fit planes)
 {
-    const Acc z = a * 0.0f;
+    const Acc z = a * 1.0126f * 0.0f;
     return (z[0] + z[1]) + (z[2] + z[3]) == 0.0f;
 }
 

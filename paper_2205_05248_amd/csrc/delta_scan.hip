@@ -54,7 +54,7 @@ template <typename E, int DK>
 struct KeyRows {
     static constexpr int PE = kExact<E>, LD = DK + 8;
     __bf16 at[PE][kSteps][LD];
-    // returns whether all of the lane's entries are finite
+    // returns whether all of the lane's entries fit planes
     __device__ __forceinline__ bool fill(const DeltaArgs &p, const void *from, int64_t ld, int64_t b, int hk, int chunk, unsigned long long live)
     {
         typedef E Vec __attribute__((ext_vector_type(8)));
@@ -75,7 +75,7 @@ struct KeyRows {
                 }
             }
 #pragma unroll
-            for (int c = 0; c < 8; ++c) fine = fine && v[c] * 0.0f == 0.0f;
+            for (int c = 0; c < 8; ++c) fine = fine && fits_planes(fabsf(v[c]));
             Frag planes[PE];
             split(v, planes);
 #pragma unroll
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(kDeltaThreads, kExact<E> == 1 ? 4 : 3) void chunk_k
                     const float e = decay_of(gates.G[i] - gates.G[j]);
                     a = on && j < i ? e * kk[tile][r] : 0.0f;
                     v = on ? p.scale * e * qk[tile][r] : 0.0f;
-                    fine = fine && (a + v) * 0.0f == 0.0f;
+                    fine = fine && fits_planes(max_of(fabsf(a), fabsf(v)));
                 }
                 A[i * LN + j] = a;
                 N[i * LN + j] = v;
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(kDeltaThreads, kExact<E> == 1 ? 4 : 3) void chunk_k
 #pragma unroll
                 for (int j = 0; j < i; ++j) v = fmaf(-own[i * LN + j], n[j], v);
                 v = i > at ? v : 0.0f;
-                fine = fine && v * 0.0f == 0.0f;
+                fine = fine && fits_planes(fabsf(v));
                 n[i] = v * gates.beta[wave * 16 + i];
                 column[i] = v;
             }

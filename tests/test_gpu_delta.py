@@ -235,6 +235,31 @@ def test_what_is_not_finite_stays_in_its_sequence(what, value):
     assert np.array_equal(np.isfinite(host(o["s_last"])), np.isfinite(want["s_last"]))
 
 
+@pytest.mark.parametrize("what", ["v", "k", "q", "s_first"])
+def test_the_largest_numbers_stay_in_their_sequence(what):
+    """As what is not finite, although they are."""
+    B, T, H = 2, 150, 2
+    reset = torch.zeros(B, T, dtype=torch.uint8)
+    reset[0, 20] = reset[0, 45] = reset[0, 100] = 1
+    s = make(B, T, 1, H, 8, 16, "fp32", 20, reset=reset)
+    largest = torch.finfo(f32).max
+    if what == "s_first":
+        s["s_first"][0, 1, 2, 3] = -largest
+    elif what == "v":
+        s["v"][0, 30, 1, 3] = -largest
+    else:
+        s[what][0, 30, 0, 2] = largest
+    o = run(s)
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = wanted(s)
+    lo, at, hi = (0, 0, 20) if what == "s_first" else (20, 30, 45)
+    for name in ("o", "grad_q", "grad_k", "grad_v", "grad_log_decay", "grad_beta"):
+        outside = np.ones((B, T), bool)
+        outside[0, at if name == "o" else lo:hi] = False
+        g, w = host(o[name])[outside], want[name][outside]
+        assert np.abs(g - w).max() <= REL * np.abs(w).max(), name
+
+
 def test_the_same_bits_again():
     reset, filled = masks(3, 200, 4)
     s = make(3, 200, 2, 4, 32, 48, "bf16", 19, reset, filled)
