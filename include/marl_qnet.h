@@ -608,6 +608,7 @@ int marl_delta_scan(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_t Hv,
  *                (0 in padding); summed over the value heads of a key head in a fixed order; none may be an input
  *   grad_log_decay, grad_beta   dev [B,T,Hv] f32, overwritten (0 in padding; that of log_decay is 0 where a is 0)
  *   grad_s_first dev [B,Hv,Dk,Dv] f32 or NULL, overwritten; may be grad_s_last
+ * An infinity or NaN, of the upstream gradient too, reaches the gradients of no other sequence.
  */
 int marl_delta_scan_grad(int32_t dtype, int32_t B, int32_t T, int32_t Hk, int32_t Hv, int32_t Dk, int32_t Dv,
                          const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v,

@@ -235,6 +235,25 @@ def test_what_is_not_finite_stays_in_its_sequence(what, value):
     assert np.array_equal(np.isfinite(host(o["s_last"])), np.isfinite(want["s_last"]))
 
 
+@pytest.mark.parametrize("what", ["grad_o", "grad_s_last"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), torch.finfo(f32).max])
+def test_an_upstream_gradient_that_is_not_finite_stays_in_its_sequence(what, value):
+    B, T, H = 2, 150, 2
+    reset = torch.zeros(B, T, dtype=torch.uint8)
+    reset[0, 20] = reset[0, 45] = reset[0, 100] = 1
+    s = make(B, T, 1, H, 8, 16, "fp32", 21, reset=reset)
+    s[what][(0, 30, 1, 3) if what == "grad_o" else (0, 1, 2, 3)] = value
+    o = run(s)
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = wanted(s)
+    outside = np.ones((B, T), bool)
+    outside[0, slice(20, 45) if what == "grad_o" else slice(100, T)] = False
+    for name in ("grad_q", "grad_k", "grad_v", "grad_log_decay", "grad_beta"):
+        g, w = host(o[name])[outside], want[name][outside]
+        assert np.abs(g - w).max() <= REL * np.abs(w).max(), name
+    near(o["grad_s_first"], want["grad_s_first"], f32, REL, "grad_s_first")
+
+
 @pytest.mark.parametrize("what", ["v", "k", "q", "s_first"])
 def test_the_largest_numbers_stay_in_their_sequence(what):
     """As what is not finite, although they are."""
