@@ -24,14 +24,13 @@ constexpr int kDeltaThreads = 256;                     // four waves; wave w has
 typedef float Acc __attribute__((ext_vector_type(4)));
 
 // Products run on the bf16 matrix pipe on sums of bf16 planes: a plane holds what the planes before it left, rounded to 8 bits, so that
-// three hold 24 and two 17 of a value's bits.  bf16 elements are one plane, fp16 two, fp32 three, all exactly.  States and what
-// leads to them or to a gradient in fp32 are kept in three; what ends in a 16-bit result alone in two, whose rounding, 2^-18, is 2^-6 of an
-// fp16 result's own.  Of the products of planes those are formed that are not below the smallest kept: six of three by three.  The fp32
+// three hold 24 of a value's bits.  bf16 elements are one plane, fp16 two, fp32 three, all exactly.  States, matrices and steps are
+// three whatever the elements' type: a 16-bit result too can be what large numbers leave of each other.  Of the products of
+// planes those are formed that are not below the smallest kept: six of three by three.  The fp32
 // matrix instructions would be 16 times slower, and fp16 planes, of which two would do, need every column scaled to their range.
 typedef __bf16 Frag __attribute__((ext_vector_type(8)));
 typedef __bf16 Four __attribute__((ext_vector_type(4)));
 template <typename E> constexpr int kExact = sizeof(E) == 4 ? 3 : std::is_same<E, _Float16>::value ? 2 : 1;
-template <typename E> constexpr int kFine = sizeof(E) == 4 ? 3 : 2;
 
 struct ChunkGates {
     double G[kSteps];
@@ -340,16 +339,18 @@ __device__ __forceinline__ Place place_of(int64_t heads, int Dv, int columns)
 inline unsigned places(int64_t heads, int Dv, int columns) { return (unsigned)((heads * (padded_values(Dv) / columns) + 7) / 8 * 8); }
 
 // Whether a workgroup takes two tiles of columns: every fragment is read once for both, for half as many waves on a compute unit.  It needs more than
-// two columns a lane can hold, and workgroups for the whole chip: one a compute unit where the keys' planes fill a wave's registers anyway, else two.
+// two columns a lane can hold, and workgroups for the whole chip: one a compute unit where the keys' planes fill a wave's registers anyway, else two; where
+// one tile alone leaves no room for a second workgroup, half of them, for as soon as there are more tiles than compute units some have two in turn.
 // 8 | 32 sequences of 512 steps, 16 heads, 64 columns (256 | 1024 workgroups of two tiles), us with one and two, forward with keep and backward:
-//   128 keys, bf16  47, 50 | 208, 186   70, 54 | 251, 194       64 keys, bf16  31, 36 | 161, 139   44, 41 | 163, 153
-//   128 keys, fp32 106, 79 | 381, 301  104, 81 | 391, 303       64 keys, fp32  52, 48 | 228, 200   74, 53 | 278, 199
-//    32 keys, bf16  28, 34 | 152, 114   34, 49 | 153, 137       32 keys, fp32  40, 49 | 195, 177   50, 102 | 191, 404
+//   128 keys, bf16  60, 53 | 221, 206   70, 55 | 252, 204       64 keys, bf16  43, 38 | 169, 150   43, 42 | 161, 155
+//   128 keys, fp32 108, 79 | 387, 305  103, 82 | 390, 303       64 keys, fp32  63, 50 | 231, 202   74, 52 | 276, 200
+//    32 keys, bf16  38, 34 | 158, 123   34, 49 | 153, 137       32 keys, fp32  49, 59 | 191, 176   50, 102 | 191, 404
+// 3 sequences, 11 heads, 128 columns (132 workgroups of two tiles), 128 keys: bf16 35, 43 and 44, 45; fp16 61, 48 and 70, 53; fp32 73, 59 and 78, 64.
 // (backward with 32 keys two tiles spill, and are not taken.)
 template <typename E, int DK>
 inline bool wide_columns(const DeltaArgs &p)
 {
-    return p.Dv > 16 && (int64_t)p.B * p.Hv * (padded_values(p.Dv) / 32) >= (kExact<E> * DK >= 128 ? 256 : 512);
+    return p.Dv > 16 && (int64_t)p.B * p.Hv * (padded_values(p.Dv) / 32) >= (kExact<E> * DK >= 256 ? 129 : kExact<E> * DK >= 128 ? 256 : 512);
 }
 
 int delta_scan_launch(int dtype, const DeltaArgs &p, hipStream_t stream);

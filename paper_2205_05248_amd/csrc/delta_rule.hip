@@ -106,7 +106,7 @@ Room room_of(int dtype, const DeltaArgs &p, bool keep)
 {
     const size_t records = (size_t)p.B * p.Hv * p.chunks, f = sizeof(float);
     const size_t keys = (size_t)p.B * p.Hk * p.chunks * key_frags(padded_keys(p.Dk), planes_of(dtype)) * sizeof(Frag);
-    const size_t fine = records * square_frags(dtype == MARL_DTYPE_F32 ? 3 : 2) * sizeof(Frag), square = records * square_frags(3) * sizeof(Frag);
+    const size_t square = records * square_frags(3) * sizeof(Frag);
     Room r{};
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t here = at; at += up256(bytes); return here; };
@@ -115,7 +115,7 @@ Room room_of(int dtype, const DeltaArgs &p, bool keep)
     r.Q = take(keys);
     r.KT = take(keys);
     r.N = take(square);
-    r.P = take(fine);
+    r.P = take(square);
     if (keep) {
         r.QT = take(keys);
         r.NT = take(square);

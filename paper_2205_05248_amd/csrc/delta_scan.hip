@@ -220,7 +220,7 @@ __global__ __launch_bounds__(kDeltaThreads, kExact<E> == 1 ? 4 : 3) void chunk_k
             }
         }
         __syncthreads();
-        write_square<kFine<E>, false>(N, LN, p.P + record * square_frags(kFine<E>));
+        write_square<3, false>(N, LN, p.P + record * square_frags(3));
         if (p.PT) write_square<3, true>(N, LN, p.PT + record * square_frags(3));
         // blocks on the diagonal: N_i = A_i - sum_j A_ij beta_j N_j, a column a lane
         float n[16];
@@ -301,17 +301,17 @@ __global__ __launch_bounds__(kDeltaThreads, kExact<E> == 1 ? 4 : 3) void chunk_k
 // 90 matrix instructions a wave; at 128 keys and columns a chunk takes 2.2 us with 16 columns (20011 steps, 16 heads, bf16: 700 us, 128 workgroups on
 // 256 compute units) and 5.0 with 32 (4 x 8192, with keep: 644 us, waves wait 31 % of their cycles, the matrix pipe is busy for 12 %).  Everything at
 // hand a chunk ahead takes 1.4 times the registers that a third workgroup on a compute unit would leave: with 168 they spill, 88 -> 196 us of the 320 x
-// 120 batch with 4 heads of 16.
+// 120 batch with 4 heads of 16.  fp16 with 128 keys spills with 256 too, and has a compute unit for a workgroup: 450 -> 293 us of 4096 steps, 16 heads with keep.
 template <typename E, int DK, int NT, bool KEEP>
-__global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : DK == 32) ? 2 : 1) void scan_kernel(DeltaArgs p)
+__global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 192 : DK == 32) ? 2 : 1) void scan_kernel(DeltaArgs p)
 {
-    constexpr int PE = kExact<E>, PF = kFine<E>, KS = DK / 32, LS = DK + 8, LU = kSteps + 8, C = 16 * NT;
+    constexpr int PE = kExact<E>, KS = DK / 32, LS = DK + 8, LU = kSteps + 8, C = 16 * NT;
     constexpr int kTiles = (DK + 63) / 64;             // of the state, for a wave; of DK = 32 two waves have one
     extern __shared__ __attribute__((aligned(16))) char lds[];
     typedef __bf16 StatePlane[C][LS];
     typedef __bf16 StepPlane[C][LU];
     StatePlane *S = reinterpret_cast<StatePlane *>(lds);                           // [3], columns of the state
-    StepPlane *R = reinterpret_cast<StepPlane *>(lds + 3 * sizeof(StatePlane)), *U = R + 3, *Ue = U + PF;      // [3], [PF], [3]
+    StepPlane *R = reinterpret_cast<StepPlane *>(lds + 3 * sizeof(StatePlane)), *U = R + 3, *Ue = U + 3;       // [3] each
     __shared__ int not_finite[2];
     const int lane = threadIdx.x % kWave, wave = wave_index(), at = lane % 16, group = lane / 16, zero = hidden_zero();
     const Place place = place_of((int64_t)p.B * p.Hv, p.Dv, C);
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : D
 #pragma unroll
                 for (int n = 0; n < NT; ++n) state[tile][n][r] = v[n];
             }
-    Frag k[KS][PE], q[KS][PE], n_of[2][3], p_of[2][PF], kt[kTiles][2][PE];
+    Frag k[KS][PE], q[KS][PE], n_of[2][3], p_of[2][3], kt[kTiles][2][PE];
     Columns<E, NT> v[4];
     Acc f_next, t_next, beta_next;
     float whole_next;
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : D
             for (int n = 0; n < 3; ++n) n_of[s][n] = N.at(wave, s, n, 2, 3);
     };
     auto load_end = [&](int chunk) {
-        const FragReader P(p.P + (head * p.chunks + chunk) * square_frags(PF)), KT(p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE));
+        const FragReader P(p.P + (head * p.chunks + chunk) * square_frags(3)), KT(p.KT + (key_head * p.chunks + chunk) * key_frags(DK, PE));
 #pragma unroll
         for (int tile = 0; tile < kTiles; ++tile)
 #pragma unroll
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : D
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int n = 0; n < PF; ++n) p_of[s][n] = P.at(wave, s, n, 2, PF);
+            for (int n = 0; n < 3; ++n) p_of[s][n] = P.at(wave, s, n, 2, 3);
     };
     auto share_state = [&] {
 #pragma unroll
@@ -415,19 +415,16 @@ __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : D
         const float whole = whole_next;
         const bool bad = __builtin_amdgcn_readfirstlane(bad_next) != 0;
         // R = V - f K S
-        Sums<2> ks[NT];
-        Sums<PF - 1> qs[NT];
+        Sums<2> ks[NT], qs[NT];
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                Frag of_state[3], fine[PF];
+                Frag of_state[3];
 #pragma unroll
                 for (int m = 0; m < 3; ++m) of_state[m] = *reinterpret_cast<const Frag *>(&S[m][n * 16 + at][s * 32 + group * 8]);
-#pragma unroll
-                for (int m = 0; m < PF; ++m) fine[m] = of_state[m];
                 multiply_into(ks[n], k[s], of_state);
-                multiply_into(qs[n], q[s], fine);
+                multiply_into(qs[n], q[s], of_state);
             }
         Acc m[NT];
 #pragma unroll
@@ -491,7 +488,7 @@ __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : D
             Acc to_end;
 #pragma unroll
             for (int r = 0; r < 4; ++r) to_end[r] = t[r] > 0.0f || t[r] != t[r] ? t[r] * u[r] : 0.0f;
-            Four planes[PF], end_planes[3];
+            Four planes[3], end_planes[3];
             split(u, planes);
             split(to_end, end_planes);
             share_steps(U, planes, n);
@@ -511,7 +508,7 @@ __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : D
         }
         __syncthreads();
         // O = scale f Q S + P U,  S <- f_63 S + K' (t U)
-        Frag of_e[2][NT][3], of_u[2][NT][PF];
+        Frag of_e[2][NT][3], of_u[2][NT][3];
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -552,7 +549,7 @@ __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : D
                 pass[r] = bit_of(live, i) ? upto(starts, i) & live : 0;
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n) o[n] = careful_multiply<PF, PF>(o[n], p.P + record * square_frags(PF), wave, U[0][n * 16 + at], C * LU, pass);
+            for (int n = 0; n < NT; ++n) o[n] = careful_multiply<3, 3>(o[n], p.P + record * square_frags(3), wave, U[0][n * 16 + at], C * LU, pass);
         } else {
             if (has_state) {
                 Sums<2> ku[kTiles][NT];
@@ -571,7 +568,7 @@ __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : D
             for (int s = 0; s < 2; ++s) {
                 if (s * 32 > wave * 16) continue;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) o[n] = multiply<PF, PF>(p_of[s], of_u[s][n], o[n]);
+                for (int n = 0; n < NT; ++n) o[n] = multiply<3, 3>(p_of[s], of_u[s][n], o[n]);
             }
         }
         load_end(next);
@@ -604,7 +601,7 @@ __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 256 : D
 template <typename E, int DK, int NT>
 int run_scan(const DeltaArgs &p, hipStream_t stream)
 {
-    const size_t lds = (size_t)16 * NT * (3 * (DK + 8) + (6 + kFine<E>) * (kSteps + 8)) * sizeof(__bf16);
+    const size_t lds = (size_t)16 * NT * (3 * (DK + 8) + 9 * (kSteps + 8)) * sizeof(__bf16);
     const auto go = [&](auto kernel) {
         if (const int rc = make_room_for(reinterpret_cast<const void *>(kernel), lds)) return rc;
         hipLaunchKernelGGL(kernel, dim3(places((int64_t)p.B * p.Hv, p.Dv, 16 * NT)), dim3(kDeltaThreads), lds, stream, p);

@@ -1,0 +1,85 @@
+"""Digits that the memory and the distillation must not lose: small results of large numbers, gradients of strong decays, small remainders of a teacher, small
+gradients of long rows; and calls that run at the same time."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import memory_oracle as orc
+from paper_2205_05248_amd import binding
+from policy_util import DT, gen, host, near, randn
+
+pytestmark = pytest.mark.gpu
+f32 = torch.float32
+
+
+def room(n):
+    return torch.empty(max(n, 1), dtype=torch.uint8, device="cuda").fill_(0xff)
+
+
+def new(*shape, dtype=f32):
+    return torch.full(shape, float("nan"), dtype=dtype, device="cuda")
+
+
+class Scan:
+    """A batch on the device with all that its passes need; nothing waits before the caller does."""
+
+    def __init__(self, q, k, v, log_decay, beta, scale, s_first=None, grad_o=None, grad_s_last=None):
+        B, T, Hk, Dk = q.shape
+        Hv, Dv = v.shape[2:]
+        self.host = dict(q=q, k=k, v=v, log_decay=log_decay, beta=beta, s_first=s_first, grad_o=grad_o, grad_s_last=grad_s_last)
+        self.scale, dt, name = scale, q.dtype, {v: k for k, v in DT.items()}[q.dtype]
+        self.d = {n: None if t is None else t.cuda() for n, t in self.host.items()}
+        self.o, self.s_last = new(B, T, Hv, Dv, dtype=dt), new(B, Hv, Dk, Dv)
+        self.grads = [new(B, T, Hk, Dk, dtype=dt), new(B, T, Hk, Dk, dtype=dt), new(B, T, Hv, Dv, dtype=dt), new(B, T, Hv), new(B, T, Hv), new(B, Hv, Dk, Dv)]
+        self.train = grad_o is not None
+        self.ws = room(binding.marl_delta_scan_workspace_bytes(name, B, T, Hk, Hv, Dk, Dv, self.train))
+
+    def forward(self):
+        d = self.d
+        binding.marl_delta_scan(d["q"], d["k"], d["v"], d["log_decay"], d["beta"], self.scale, None, None, d["s_first"], self.o, self.s_last, self.ws, keep=self.train)
+
+    def backward(self):
+        d = self.d
+        binding.marl_delta_scan_grad(d["q"], d["k"], d["v"], d["log_decay"], d["beta"], self.scale, None, None, d["grad_o"], d["grad_s_last"], self.ws, *self.grads)
+
+    def wanted(self):
+        a = {n: None if t is None else host(t) for n, t in self.host.items()}
+        memory = (a["q"], a["k"], a["v"], a["log_decay"], a["beta"], self.scale, None, None, a["s_first"])
+        return orc.delta_scan(*memory)[0], orc.delta_scan_grad(*memory, a["grad_o"], a["grad_s_last"]) if self.train else None
+
+
+# ------------------------------------------------------------------------------------------------ results of 16-bit types
+@pytest.mark.parametrize("Dv", [16, 40])
+@pytest.mark.parametrize("Dk", [16, 64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_a_small_value_in_the_place_of_a_large_one(dtype, Dk, Dv):
+    """Keys are unit vectors, beta 1, no decay: an odd step puts 2^-12 of a number from 1 to 2 in the place of such a number and reads it back.  Its result is the
+    sum of at most four differences that are written within a chunk: three of them rounded to 2^-24, three additions of sums below 4 to 2^-23, and as much
+    again for the parts that the numbers are split into: 2^-20, which is 2^-8 of the result, on top of half a step of its type."""
+    B, T, g = 64, 128, gen(Dk + Dv)
+    at = (torch.arange(T // 2) % Dk).repeat_interleave(2).expand(B, T)
+    k = torch.nn.functional.one_hot(at, Dk)[:, :, None].to(DT[dtype])
+    v = (1 + 0.75 * torch.rand(B, T, 1, Dv, generator=g)) * torch.where(torch.rand(B, T, 1, Dv, generator=g) < 0.5, -1.0, 1.0)
+    v[:, 1::2] *= 2.0 ** -12
+    s = Scan(k, k, v.to(DT[dtype]), torch.zeros(B, T, 1), torch.ones(B, T, 1), 1.0)
+    s.forward()
+    got, want = s.o[:, 1::2], host(v.to(DT[dtype])[:, 1::2])
+    near(got, want, DT[dtype], 2.0 ** -8, "o", floor=np.abs(want))
+
+
+@pytest.mark.parametrize("Dv", [16, 40])
+@pytest.mark.parametrize("Dk", [16, 64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_a_small_sum_over_a_state(dtype, Dk, Dv):
+    """q reads two rows of the state that are each other's negative but for 2^-12 x of a number next to 1; nothing is written (beta 0) and nothing forgotten.  Rows
+    of the state are fp32 numbers below 2: four roundings of their size are 2^-21, 2^-9 of the result, on top of half a step of its type."""
+    B, g = 64, gen(7 * Dk + Dv)
+    first = torch.zeros(B, 1, Dk, Dv)
+    first[:, 0, 1] = 1 + 0.75 * torch.rand(B, Dv, generator=g)
+    first[:, 0, 9] = -first[:, 0, 1] + 2.0 ** -12 * (1 + torch.rand(B, Dv, generator=g))
+    q = torch.zeros(B, 3, 1, Dk)
+    q[..., 1] = q[..., 9] = 1.0
+    s = Scan(q.to(DT[dtype]), randn(g, B, 3, 1, Dk, dtype=DT[dtype]), randn(g, B, 3, 1, Dv, dtype=DT[dtype]), torch.zeros(B, 3, 1), torch.zeros(B, 3, 1), 1.0, first)
+    s.forward()
+    want = np.broadcast_to(host(first[:, :, 1]) + host(first[:, :, 9]), (B, 1, Dv))[:, None].repeat(3, 1)
+    near(s.o, want, DT[dtype], 2.0 ** -9, "o", floor=np.abs(want))
