@@ -347,11 +347,17 @@ __global__ __launch_bounds__(kDeltaThreads, NT == 1 && kExact<E> * DK <= 128 ? 2
             }
 }
 
-// Sum over the 16 lanes that hold a row.
+// Among the 16 lanes that hold a row: the value N lanes before, 0 before the first; the last one's; the sum.
+template <int CONTROL>
+__device__ __forceinline__ float of_row(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xf, 0xf, true)); }
+template <int N> __device__ __forceinline__ float lanes_before(float v) { return of_row<0x110 + N>(v); }
+__device__ __forceinline__ float last_lane(float v) { return of_row<0x15f>(v); }
 __device__ __forceinline__ float row_sum(float v)
 {
-    for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
-    return v;
+    v += of_row<0x128>(v);                             // rotations by 8, 4, 2 and 1
+    v += of_row<0x124>(v);
+    v += of_row<0x122>(v);
+    return v + of_row<0x121>(v);
 }
 
 // A chunk's steps as planes in shared memory, rows of COLUMNS entries.
@@ -401,9 +407,10 @@ __device__ __forceinline__ Acc careful_rows(Acc c, const Plane *a, int tile, con
 // Gradients of q, k, beta and the log decay of a chunk, the value heads of a key head one after the other.  With dP = scale dO U',
 // dA = -(dV) U', their products dN and dM with E, and X = dM + dM':
 //   dq = dN K + scale f dO S'      dk = dN' Q + X K - f dV S' + t U D'
-//   dG_i = sum_j F_ij - sum_j F_ji + q_i.(scale f dO S')_i - k_i.(f dV S')_i - k_i.(t U D')_i      F_ij = dM_ij k_i.k_j + dN_ij q_i.k_j
-// to which the last step adds sum_j k_j.(t U D')_j + f_63 <D, S>; the log decay's gradient is the sum of dG from its step to the end of
-// its sequence.  Value columns come 32 or 64 at a time through shared memory.  Products with rows and columns of steps are split over the waves by
+// The log decay of a step has a part in everything that is handed on across it, and its gradient is the sum of that:
+//   dg_i = sum_(m >= i > j) F_mj + sum_(m >= i) (q_m.(scale f dO S')_m - k_m.(f dV S')_m) + sum_(j < i) k_j.(t U D')_j + f_63 <D, S>
+// with F_mj = dM_mj k_m.k_j + dN_mj q_m.k_j.  (The differences of neighbours, sum_j F_ij - sum_j F_ji and so on, are cheaper to form, but hold what does not
+// cross i too, which has to cancel: at a decay of e^-12 a tenth of the gradient was rounding.)  Value columns come 32 or 64 at a time through shared memory.  Products with rows and columns of steps are split over the waves by
 // rows, those with key columns by columns (16 w on), so that every entry of S and D is split into planes once.
 // Waves of a workgroup: with 128 keys eight, of which four form dP and four dA, else four that form both (1.64 -> 1.21 ms of 4 x 8192 x 16 heads x 128 x
 // 128 bf16).  There it reads 2.8 GB and writes 0.4, and waits 65 % of its waves' cycles: a workgroup of 512 threads with 256 registers each fills a
@@ -422,7 +429,7 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
     Plane *dN = reinterpret_cast<Plane *>(lds), *dNT = dN + 3, *X = dN;            // later in the same room, [3] each
     __shared__ ChunkGates gates;
     __shared__ int not_finite;
-    __shared__ float rows_of[kWaves][kSteps], columns_of[8][kSteps], flow[2][kSteps], extra[kWaves], dbeta[kSteps];
+    __shared__ float far_of[kWaves][kSteps], later_of[kWaves][kSteps], crossing[8][kSteps], extra[kWaves], dbeta[kSteps];
     const int lane = threadIdx.x % kWave;
     int wave = wave_index(), at = lane % 16, group = lane / 16;
     int nothing;
@@ -554,7 +561,7 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
             }
             __syncthreads();
         }
-        // what goes from step j to step i, and the row and column sums of F
+        // what goes from step j to step i, and what of F crosses a step
         Acc dm[4];
         bool fine = true;
         unsigned long long before[4];                  // steps that hand something to the lane's rows
@@ -580,12 +587,12 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
                     raw[tile] = multiply<PE, PE, kOrder>(mine, other, raw[tile]);
                 }
             }
-            float row_flow[4] = {};
+            float left[4] = {};                        // sums of the rows in the tiles before
 #pragma unroll
             for (int tile = 0; tile < 4; ++tile) {
                 const int j = tile * 16 + at;
                 Acc d;
-                float column = 0.0f;
+                float across = 0.0f;                   // from before j to j or later
                 if (tile <= row)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
@@ -593,9 +600,14 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
                         const bool on = bit_of(before[r], j) && (is_p || j < i);
                         const float e = decay_of(gates.G[i] - gates.G[j]), v = (is_p ? p.scale : -1.0f) * e * of[tile][r];
                         d[r] = on ? v : 0.0f;
-                        const float f = on ? v * raw[tile][r] : 0.0f;
-                        row_flow[r] += f;
-                        column += f;
+                        float sum = on ? v * raw[tile][r] : 0.0f;
+                        sum += lanes_before<1>(sum);
+                        sum += lanes_before<2>(sum);
+                        sum += lanes_before<4>(sum);
+                        sum += lanes_before<8>(sum);
+                        const float before_j = left[r] + lanes_before<1>(sum);
+                        across += j <= i ? before_j : 0.0f;
+                        left[r] += last_lane(sum);
                     }
                 else d = Acc{};
                 fine = fine && all_finite(d);
@@ -611,14 +623,9 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
                 } else {
                     dm[tile] = d;
                 }
-                column += __shfl_xor(column, 16);
-                column += __shfl_xor(column, 32);
-                if (group == 0) columns_of[(is_p ? 0 : 4) + row][j] = column;
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float v = row_sum(row_flow[r]);
-                if (at == 0) flow[is_p ? 0 : 1][row * 16 + group * 4 + r] = v;
+                across += __shfl_xor(across, 16);
+                across += __shfl_xor(across, 32);
+                if (group == 0) crossing[(is_p ? 0 : 4) + row][j] = across;
             }
         };
         if constexpr (kWaves == 4) {
@@ -635,7 +642,6 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
             if (threadIdx.x % kPer == 0) dbeta[threadIdx.x / kPer] = dot_beta;
         }
         // the parts that come from and go to other chunks
-        float at_end = 0.0f;
         if (has_keys) {
             const int d = wave * 16 + at, from = hk * p.Dk + min(d, p.Dk - 1);
             const bool key = d < p.Dk;
@@ -650,32 +656,34 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
                 }
 #pragma unroll
             for (int row = 0; row < 4; ++row) {
-                float dot[4] = {};
+                float dot_far[4], dot_later[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = row * 16 + group * 4 + r;
                     const float f = bit_of(alive, i) ? gates.f[i] : 0.0f, t = bit_of(alive, i) ? gates.t[i] : 0.0f;
                     const float k = to_f32(k_of[row][r]), q = to_f32(q_of[row][r]);
                     const float fq = p.scale * f * far_q[row][r], fk = -f * far_k[row][r], e = t * end[row][r];
-                    const float to_later = t != 0.0f && key ? k * e : 0.0f;
-                    at_end += to_later;
-                    dot[r] = (f != 0.0f && key ? fmaf(q, fq, k * fk) : 0.0f) - to_later;
+                    dot_far[r] = f != 0.0f && key ? fmaf(q, fq, k * fk) : 0.0f;
+                    dot_later[r] = t != 0.0f && key ? k * e : 0.0f;
                     sum_q[row][r] += f != 0.0f ? fq : 0.0f;
                     sum_k[row][r] += (f != 0.0f ? fk : 0.0f) + (t != 0.0f ? e : 0.0f);
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float v = row_sum(dot[r]);
-                    if (at == 0) rows_of[wave][row * 16 + group * 4 + r] = v;
+                    const float far = row_sum(dot_far[r]), later = row_sum(dot_later[r]);
+                    if (at == 0) {
+                        far_of[wave][row * 16 + group * 4 + r] = far;
+                        later_of[wave][row * 16 + group * 4 + r] = later;
+                    }
                 }
             }
         } else {
-            rows_of[wave][lane] = 0.0f;
+            far_of[wave][lane] = later_of[wave][lane] = 0.0f;
         }
         const float whole = gates.f[kSteps - 1];
-        if (whole != 0.0f) at_end = fmaf(whole, dot_states, at_end);
-        for (int d = 1; d < kWave; d *= 2) at_end += __shfl_xor(at_end, d);
-        if (lane == 0) extra[wave] = at_end;
+        float through = whole != 0.0f ? whole * dot_states : 0.0f;
+        for (int d = 1; d < kWave; d *= 2) through += __shfl_xor(through, d);
+        if (lane == 0) extra[wave] = through;
         __syncthreads();
         const bool bad = gates.bad || not_finite;
         auto key_products = [&](const Plane *a, const Frag *keys, Acc (&sum)[4], int which) {
@@ -712,18 +720,24 @@ __global__ __launch_bounds__(grad_waves(DK) * kWave, 2) void chunk_grad_kernel(D
         key_products(dN, KT, sum_q, 0);
         key_products(dNT, QT, sum_k, 1);
         if (wave == 0) {
-            const int i = lane, t = chunk * kSteps + i, part = part_of(starts, i);
-            float v = flow[0][i] + flow[1][i];
+            // (parts of other sequences are 0: f behind the chunk's first start, t before its last)
+            const int i = lane, t = chunk * kSteps + i;
+            double far = 0.0, later = 0.0, s = 0.0;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) v -= columns_of[w][i];
+            for (int w = 0; w < 8; ++w) s += crossing[w][i];
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) v += rows_of[w][i] + (i == kSteps - 1 ? extra[w] : 0.0f);
-            double s = v;
-            for (int d = 1; d < kWave; d *= 2) {
-                const double later = __shfl_down(s, d);
-                const int its = __shfl_down(part, d);
-                if (i + d < kWave && its == part) s += later;
+            for (int w = 0; w < kWaves; ++w) {
+                far += far_of[w][i];
+                later += later_of[w][i];
+                s += extra[w];
             }
+            for (int d = 1; d < kWave; d *= 2) {
+                const double behind = __shfl_down(far, d), ahead = __shfl_up(later, d);
+                if (i + d < kWave) far += behind;
+                if (i >= d) later += ahead;
+            }
+            later = __shfl_up(later, 1);
+            s += far + (i > 0 ? later : 0.0);
             if (t < p.T) {
                 const int64_t to = (b * p.T + t) * p.Hv + h;
                 p.grad_log_decay[to] = bit_of(alive, i) && !bit_of(starts, i) ? (float)s : 0.0f;

@@ -83,3 +83,49 @@ def test_a_small_sum_over_a_state(dtype, Dk, Dv):
     s.forward()
     want = np.broadcast_to(host(first[:, :, 1]) + host(first[:, :, 9]), (B, 1, Dv))[:, None].repeat(3, 1)
     near(s.o, want, DT[dtype], 2.0 ** -9, "o", floor=np.abs(want))
+
+
+# ------------------------------------------------------------------------------------------------ gradients of strong decays
+# As in the tests of the delta rule: 2^-15 of the largest value for a single one, 2^-18 of the norm over all; here of the values that belong together, one
+# head's or those of its steps that forget.  A decay is off by a rounding of the sum of the log decays that it stands for, 2^-24 of at most 15 to 40: less.
+REL, NORM = 2.0 ** -15, 2.0 ** -18
+SIZES = [(2, 64, 1, 5, 16, 16, "fp32"), (1, 150, 5, 5, 24, 40, "fp32"), (1, 100, 1, 5, 128, 72, "fp32"), (2, 130, 1, 5, 64, 33, "bf16"), (1, 140, 5, 5, 128, 128, "bf16"),
+         (1, 70, 1, 5, 100, 20, "fp16")]
+
+
+def random_scan(B, T, Hk, Hv, Dk, Dv, dtype, seed, log_decay=None):
+    g = gen(seed)
+    unit = lambda t: (t / t.norm(dim=-1, keepdim=True)).to(DT[dtype])
+    values = lambda: randn(g, B, T, Hv, Dv, dtype=DT[dtype])
+    log_decay = -0.1 * torch.rand(B, T, Hv, generator=g) if log_decay is None else log_decay(torch.rand(B, T, Hv, generator=g))
+    return Scan(unit(randn(g, B, T, Hk, Dk)), unit(randn(g, B, T, Hk, Dk)), values(), log_decay, torch.rand(B, T, Hv, generator=g), Dk ** -0.5,
+                randn(g, B, Hv, Dk, Dv) * 0.5, values(), randn(g, B, Hv, Dk, Dv) * 0.5)
+
+
+def same_digits(got, want, name):
+    assert np.abs(got - want).max() <= REL * np.abs(want).max(), (name, np.abs(got - want).max() / np.abs(want).max())
+    assert np.linalg.norm(got - want) <= NORM * np.linalg.norm(want), (name, np.linalg.norm(got - want) / np.linalg.norm(want))
+
+
+@pytest.mark.parametrize("size", SIZES)
+def test_the_gradient_of_a_head_that_forgets_at_once(size):
+    """Every head has a decay of its own strength, and with it a gradient of its own size: down to e^-40 of the others'."""
+    strength = torch.tensor([0.5, 8.0, 12.0, 15.0, 40.0])
+    s = random_scan(*size, sum(size[:6]), lambda r: -strength * (0.9 + 0.1 * r))
+    s.forward()
+    s.backward()
+    got, want = host(s.grads[3]), s.wanted()[1][3]
+    for h in range(5):
+        same_digits(got[:, :, h], want[:, :, h], f"head {h}")
+
+
+@pytest.mark.parametrize("size", SIZES)
+def test_the_gradient_of_a_step_that_forgets(size):
+    """Strong decays between weak ones: their gradients are as small as what they leave of the state."""
+    hard = torch.arange(size[1]) % 5 == 3
+    s = random_scan(*size, 1 + sum(size[:6]), lambda r: torch.where(hard[None, :, None], -12.0 - r, -0.1 * r))
+    s.forward()
+    s.backward()
+    got, want = host(s.grads[3]), s.wanted()[1][3]
+    for name, steps in (("hard", hard.numpy()), ("soft", ~hard.numpy())):
+        same_digits(got[:, steps], want[:, steps], name)
