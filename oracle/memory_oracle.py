@@ -94,10 +94,11 @@ def delta_step(q, k, v, log_decay, beta, scale, slot, reset, s_in):
 
 
 def distill(logits, top_id, top_value, avail, scale, tail, grad_loss=None):
-    """dict of loss, log_sum, log_rest and, with grad_loss, grad."""
+    """dict of loss, log_sum, log_rest and, with grad_loss, grad and the sum of the sizes of its terms."""
     logits = np.asarray(logits, np.float64)
     R, V = logits.shape
-    out = dict(loss=np.zeros(R), log_sum=np.full(R, -np.inf), log_rest=np.full(R, -np.inf), grad=np.zeros((R, V)))
+    out = dict(loss=np.zeros(R), log_sum=np.full(R, -np.inf), log_rest=np.full(R, -np.inf), grad=np.zeros((R, V)),
+               grad_size=np.zeros((R, V)))
     for r in range(R):
         ok = np.ones(V, bool) if avail is None else (avail if avail.ndim == 1 else avail[r]) != 0
         ok = ok & ~(logits[r] == -np.inf)
@@ -132,10 +133,13 @@ def distill(logits, top_id, top_value, avail, scale, tail, grad_loss=None):
                 loss += left * (np.log(left) - out["log_rest"][r])
         out["loss"][r], out["log_sum"][r] = loss, log_sum
         if grad_loss is not None:
-            g = (mass + left) * q - target
+            g, size = (mass + left) * q - target, (mass + left) * q + target
             if left > 0:
-                g[others] -= left * np.exp(z[others] - log_sum - out["log_rest"][r])
+                part = left * np.exp(z[others] - log_sum - out["log_rest"][r])
+                g[others] -= part
+                size[others] += part
             out["grad"][r] = np.where(ok, scale * float(grad_loss[r]) * g, 0.0)
+            out["grad_size"][r] = np.where(ok, scale * abs(float(grad_loss[r])) * size, 0.0)
     return out
 
 

@@ -45,6 +45,17 @@ __device__ __forceinline__ Sum join_wave(Sum v)
     return v;
 }
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
+template <int LANES, int D = 1>
+__device__ __forceinline__ double sum_lanes(double v)
+{
+    if constexpr (D < LANES) {
+        const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+        const unsigned low = __float_as_uint(across<D>(__uint_as_float((unsigned)bits))), high = __float_as_uint(across<D>(__uint_as_float((unsigned)(bits >> 32))));
+        return sum_lanes<LANES, 2 * D>(v + __builtin_bit_cast(double, (uint64_t)high << 32 | low));
+    } else {
+        return v;
+    }
+}
 
 // What the two sums of a row give: of the kept places and of all others.
 struct RowSums {
@@ -98,23 +109,46 @@ __device__ __forceinline__ Kept kept_at(const DistillArgs &p, const E *l, const 
     return a;
 }
 
-// The teacher's side: log p of a value is value - top - log_total, p its exponential; `left` what it has for all other places.
+// The teacher's side: log p of a value is value - top - log_total, p its exponential.
 struct Teacher { float top, total, log_total; };
-__device__ __forceinline__ float probability(const Teacher &t, int tail, float value)
+// A constant in scalar registers where it is used: in vector registers, kept through the kernel, the twelve below leave room for five waves in place of seven on
+// rows of 1000 (50000 rows bf16, 20 alternatives: 100 -> 122 us).
+__device__ __forceinline__ double kept_scalar(double v)
 {
-    return tail ? expf(value) : t.total > 0.0f ? expf(value - t.top) / t.total : t.total == 0.0f ? 0.0f : __builtin_nanf("");
+    asm volatile("" : "+s"(v));
+    return v;
 }
+// p of an alternative whose value is its log probability, in 64 bits: what the teacher has for all other places is one minus the sum of these, of a sure teacher a
+// small number, for which its log probabilities have the digits and their exponentials in fp32 do not (of 1e-6 a twentieth was lost, of 2e-8 all).  e^v = 2^n e^r
+// with |r| <= log(2) / 2, whose series ends at r^11: the rest is below 2^-46.  (Half as long as the library's exponential, which needs no bounds; what is below them is 0 in
+// fp32, and above them infinite.)
+__device__ __forceinline__ double exact_part(const Kept &a)
+{
+    const float v = __builtin_elementwise_minimum(max_nan(a.value, -150.0f), 100.0f), n = __builtin_rintf(kLog2e * v);              // NaN stays
+    const double r = fma(-(double)n, 0.69314718055994530942, (double)v);
+    const double rr = r * r;
+    double factorial = 39916800, odd = 1 / factorial, even = 11 / factorial;       // 11!; two sums, neither waits for the other
+#pragma unroll
+    for (int i = 9; i > 0; i -= 2) {
+        factorial /= (i + 1) * (i + 2);
+        odd = fma(odd, rr, kept_scalar(1 / factorial));
+        even = fma(even, rr, kept_scalar(i / factorial));
+    }
+    return a.is ? __builtin_ldexp(fma(odd, r, even), (int)n) : 0.0;
+}
+__device__ __forceinline__ float left_of(double sum) { return sum >= 1.0 ? 0.0f : (float)(1.0 - sum); }                // NaN stays
+// The same of values that are any logits.
+__device__ __forceinline__ float share(const Teacher &t, const Kept &a)
+{
+    return !a.is ? 0.0f : t.total > 0.0f ? expf(a.value - t.top) / t.total : t.total == 0.0f ? 0.0f : __builtin_nanf("");
+}
+__device__ __forceinline__ float probability(const Teacher &t, int tail, const Kept &a) { return !tail ? share(t, a) : a.is ? expf(a.value) : 0.0f; }
 // p (log p - log q), 0 where p is.
 __device__ __forceinline__ float part_of_loss(float p, float log_p, float log_q) { return p == 0.0f ? 0.0f : p * (log_p - log_q); }
-__device__ __forceinline__ float left_of(float sum) { return sum >= 1.0f ? 0.0f : 1.0f - sum; }        // NaN stays
-
-__device__ __forceinline__ void put_row(const DistillArgs &p, int64_t row, const RowSums &r, float loss, float sum)
+__device__ __forceinline__ void put_row(const DistillArgs &p, int64_t row, const RowSums &r, float loss, float left)
 {
     const float nan = __builtin_nanf("");
-    if (p.tail && r.some_left) {
-        const float left = left_of(sum);
-        loss += part_of_loss(left, logf(left), r.log_rest);
-    }
+    if (p.tail && r.some_left) loss += part_of_loss(left, logf(left), r.log_rest);
     p.loss[row] = r.bad ? nan : r.none ? 0.0f : loss;
     if (p.log_sum) p.log_sum[row] = r.bad ? nan : r.none ? -kInf : r.M + r.log_s;
     if (p.tail && p.log_rest) p.log_rest[row] = r.bad ? nan : r.log_rest;
@@ -147,11 +181,12 @@ __device__ __forceinline__ void finish_row(const DistillArgs &p, int64_t row, Su
     kept.s = all_lanes<kWave>(a.is && !met ? exp_of(a.z - kept.m) : 0.0f, add);
     const RowSums r = row_sums(kept, rest);
     const Teacher t = teacher_of(a);
-    const float prob = a.is ? probability(t, p.tail, a.value) : 0.0f;
+    const double part = p.tail ? exact_part(a) : 0.0;
+    const float prob = p.tail ? (float)part : share(t, a);
     const float log_p = p.tail ? a.value : (a.value - t.top) - t.log_total;
     const float loss = all_lanes<kWave>(part_of_loss(prob, log_p, (a.z - r.M) - r.log_s), add);
-    const float sum = all_lanes<kWave>(prob, add);
-    if (threadIdx.x % kWave == 0) put_row(p, row, r, loss, sum);
+    const float left = p.tail ? left_of(sum_lanes<kWave>(part)) : 0.0f;
+    if (threadIdx.x % kWave == 0) put_row(p, row, r, loss, left);
 }
 
 // ---------------------------------------------------------------------------------- long rows
@@ -266,14 +301,14 @@ __global__ __launch_bounds__(kWave) void join_kernel(DistillArgs p)
 
 // What the gradient of a row needs: places that are not kept get C e^(z - base), kept ones W e^(z - log_sum) - p, all times `by`.
 struct RowGrad { float log_sum, base, W, C, by; };
-__device__ __forceinline__ RowGrad row_grad(const DistillArgs &p, int64_t row, float sum)
+__device__ __forceinline__ RowGrad row_grad(const DistillArgs &p, int64_t row, float sum, float left)
 {
     RowGrad g;
     g.log_sum = p.in_log_sum[row];
     g.by = p.scale * p.grad_loss[row];
     if (p.grad_loss[row] == 0.0f) g.by = 0.0f;
     const float log_rest = p.tail ? p.in_log_rest[row] : 0.0f;
-    const float left = p.tail && log_rest != -kInf ? left_of(sum) : 0.0f;
+    if (log_rest == -kInf) left = 0.0f;
     g.W = sum + left;
     // (W - left / q_r) q = (W q_r - left) (q / q_r): the quotient of two small numbers is formed in the exponent
     g.C = p.tail ? g.W * exp_of(log_rest) - left : g.W;
@@ -303,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void long_grad_kernel(DistillArgs p)
     constexpr int V = P::V, kPieces = 4, kStep = kThreads * V * kPieces;
     __shared__ Listed listed;
     __shared__ int ids[kMostKept];
-    __shared__ float probs[kMostKept], total;
+    __shared__ float probs[kMostKept], total, left;
     const int64_t row = blockIdx.x / p.parts;
     const int piece = blockIdx.x % p.parts;
     const E *l = static_cast<const E *>(p.logits) + row * p.ld;
@@ -312,10 +347,11 @@ __global__ __launch_bounds__(kThreads) void long_grad_kernel(DistillArgs p)
     const Kept a = kept_at(p, l, av, row, threadIdx.x);
     if (threadIdx.x < kWave) {
         const Teacher t = teacher_of(a);
-        const float prob = a.is ? probability(t, p.tail, a.value) : 0.0f, sum = all_lanes<kWave>(prob, add);
+        const double part = p.tail ? exact_part(a) : 0.0, parts = p.tail ? sum_lanes<kWave>(part) : 0.0;
+        const float prob = p.tail ? (float)part : share(t, a), sum = p.tail ? (float)parts : all_lanes<kWave>(prob, add);
         ids[threadIdx.x] = a.is ? a.id : -1;
         probs[threadIdx.x] = prob;
-        if (threadIdx.x == 0) total = sum;
+        if (threadIdx.x == 0) total = sum, left = p.tail ? left_of(parts) : 0.0f;
     }
     const int skew = skew_of(l), n = p.V + skew;                       // entry j of the row is skew + j
     const int64_t span = (int64_t)p.per * kStep;
@@ -327,7 +363,7 @@ __global__ __launch_bounds__(kThreads) void long_grad_kernel(DistillArgs p)
         const int64_t to = from + kMostChunks * kChunk < stop ? from + kMostChunks * kChunk : stop;
         __syncthreads();
         listed.mark(p, a.id, skew, from, to);
-        const RowGrad g = row_grad(p, row, total);
+        const RowGrad g = row_grad(p, row, total, left);
         auto put = [&](const float *held, int j) {
             typename P::Vec v;
             const unsigned marked = listed.of<V>(j - (int)from);
@@ -372,14 +408,15 @@ __global__ __launch_bounds__(kThreads) void long_grad_kernel(DistillArgs p)
 template <int G>
 struct ShortTeacher {
     Teacher t;
-    float sum;
+    float sum, left, first;                            // of all alternatives, of all other places, of the lane's first alternative
     unsigned marked;                                   // of the lane's own entries j G + sub, bit j
 };
 template <typename E, int G>
 __device__ __forceinline__ ShortTeacher<G> short_teacher(const DistillArgs &p, Kept &first, const E *l, const uint8_t *av, int64_t row, bool there)
 {
     const int lane = threadIdx.x % kWave, sub = lane % G;
-    ShortTeacher<G> s{{-kInf, 0.0f, 0.0f}, 0.0f, 0};
+    ShortTeacher<G> s{{-kInf, 0.0f, 0.0f}, 0.0f, 0.0f, 0.0f, 0};
+    double sum = 0.0;
     if (!there) first.id = -1;
     kept_of(p, first, l, av);
     Kept a = first;
@@ -389,7 +426,9 @@ __device__ __forceinline__ ShortTeacher<G> short_teacher(const DistillArgs &p, K
             s.marked |= id >= 0 && id % G == sub ? 1u << (id / G) : 0u;
         }
         if (p.tail) {
-            s.sum += a.is ? expf(a.value) : 0.0f;
+            const double part = exact_part(a);
+            if (base == 0) s.first = (float)part;
+            sum += part;
         } else {
             const float top = max_nan(s.t.top, a.value);
             if (!(top == s.t.top)) s.t.total *= s.t.top == -kInf ? 0.0f : expf(s.t.top - top);
@@ -400,13 +439,16 @@ __device__ __forceinline__ ShortTeacher<G> short_teacher(const DistillArgs &p, K
         a = there ? kept_at(p, l, av, row, base + sub) : Kept{-1, -kInf, -kInf, -kInf, false};
     }
     if (p.tail) {
-        s.sum = all_lanes<G>(s.sum, add);
+        sum = sum_lanes<G>(sum);
+        s.sum = (float)sum;
+        s.left = left_of(sum);
     } else {
         const float top = all_lanes<G>(s.t.top, max_nan);
         s.t.total = all_lanes<G>(s.t.top == -kInf ? 0.0f : s.t.total * expf(s.t.top - top), add);
         s.t.top = top;
         s.t.log_total = logf(s.t.total);
         s.sum = s.t.total == 0.0f ? 0.0f : s.t.total > 0.0f ? 1.0f : __builtin_nanf("");
+        s.first = share(s.t, first);
     }
     return s;
 }
@@ -469,11 +511,11 @@ __global__ __launch_bounds__(kThreads) void short_rows_kernel(DistillArgs p)
     float loss = 0.0f;
     for (int base = 0; base < p.K; base += G) {
         const Kept a = base == 0 ? listed : there ? kept_at(p, l, av, own, base + sub) : Kept{-1, -kInf, -kInf, -kInf, false};
-        const float prob = a.is ? probability(s.t, p.tail, a.value) : 0.0f;
+        const float prob = base == 0 ? s.first : probability(s.t, p.tail, a);
         loss += part_of_loss(prob, p.tail ? a.value : (a.value - s.t.top) - s.t.log_total, (a.z - r.M) - r.log_s);
     }
     loss = all_lanes<G>(loss, add);
-    if (there && sub == 0) put_row(p, row, r, loss, s.sum);
+    if (there && sub == 0) put_row(p, row, r, loss, s.left);
 }
 
 template <typename E, int G, int N, bool FLAT>
@@ -502,12 +544,12 @@ __global__ __launch_bounds__(kThreads) void short_grad_kernel(DistillArgs p)
         }
     }
     const ShortTeacher<G> s = short_teacher<E, G>(p, listed, l, av, own, there);
-    const RowGrad g = row_grad(p, own, s.sum);
+    const RowGrad g = row_grad(p, own, s.sum, s.left);
     constexpr int kRounds = kMostKept / G;                             // the kept ones' logits are read before any is overwritten
     int ids[kRounds];
     float grads[kRounds];
     {                                                                  // listed twice: both parts
-        const float prob = listed.is ? probability(s.t, p.tail, listed.value) : 0.0f;
+        const float prob = s.first;
         float sum = 0.0f;
         for (int k = 0; k < G && k < p.K; ++k) {
             const int id = __shfl(listed.id, lane - sub + k);
@@ -528,7 +570,7 @@ __global__ __launch_bounds__(kThreads) void short_grad_kernel(DistillArgs p)
             for (int k = 0; k < p.K; ++k)
                 if (p.top_id[own * p.K + k] == a.id) {
                     const float value = p.top_value[own * p.K + k];
-                    grads[c] += probability(s.t, p.tail, value == kInf ? __builtin_nanf("") : value);
+                    grads[c] += probability(s.t, p.tail, Kept{a.id, value == kInf ? __builtin_nanf("") : value, a.z, a.logit, true});
                 }
         }
         grads[c] = a.is ? kept_grad(g, a.logit, grads[c], p.scale, p.lowest) : 0.0f;

@@ -129,3 +129,42 @@ def test_the_gradient_of_a_step_that_forgets(size):
     got, want = host(s.grads[3]), s.wanted()[1][3]
     for name, steps in (("hard", hard.numpy()), ("soft", ~hard.numpy())):
         same_digits(got[:, steps], want[:, steps], name)
+
+
+# ------------------------------------------------------------------------------------------------ distillation
+# Gradients are compared with the sizes of their own terms, W q and p, or W q and p_r q / q_r.  An exponent is made of z (|z| <= 32, rounded: 2^-19), log_sum (1.25 x
+# 2^-18, as in the tests of the distillation), their difference (2^-20) and its product with log2 e (36 x 2^-24 at |z - log_sum| <= 25): 2.6 x 2^-18 of q.  q / q_r has
+# log_rest's 2.5 x 2^-18 on top, and q_r itself |log_rest| <= 25 times 2^-24: 5.7 x 2^-18 in all, where the remainder p_r is as exact as the alternatives are.
+TERMS = 5.7 * 2.0 ** -18
+
+
+def distill(s, scale, K):
+    R, V = s["logits"].shape
+    logits, ids, values = s["logits"].cuda(), s["top_id"].cuda(), s["top_value"].cuda()
+    avail = None if s.get("avail") is None else s["avail"].cuda()
+    loss, log_sum, rest, grad = new(R), new(R), new(R), new(R, V, dtype=logits.dtype)
+    tail = s["tail"]
+    binding.marl_distill(logits, ids, values, avail, scale, tail, loss, log_sum, rest if tail else None, room(binding.marl_distill_workspace_bytes(R, V, K)))
+    binding.marl_distill_grad(logits, ids, values, avail, scale, tail, log_sum, rest if tail else None, s["grad_loss"].cuda(), grad)
+    with np.errstate(invalid="ignore"):
+        want = orc.distill(host(s["logits"]), host(s["top_id"]), host(s["top_value"]), None if s.get("avail") is None else host(s["avail"]), scale, tail, host(s["grad_loss"]))
+    return loss, grad, want
+
+
+# What a teacher is sure of: log probabilities of its alternatives.
+SURE = {"1e-4": [-1e-4], "1e-6": [-1e-6], "1e-7": [-1e-7], "three": [float(np.log(0.97)), float(np.log(0.02)), float(np.log(0.009995))],
+        "two_halves": [float(np.log(0.5)) - 1e-6, float(np.log(0.5)) - 2e-6], "sure": [0.0]}
+
+
+@pytest.mark.parametrize("V", [40, 200, 600, 3000, 40000])
+@pytest.mark.parametrize("values", SURE)
+def test_the_small_remainder_of_a_sure_teacher(values, V):
+    """A student that is sure too (its other places hold e^-10 to e^-20) feels the remainder alone at all other places."""
+    values, R, g = SURE[values], 9, gen(V)
+    K = len(values)
+    s = dict(logits=randn(g, R, V), tail=True, grad_loss=randn(g, R), top_value=torch.tensor(values).expand(R, K).contiguous())
+    s["top_id"] = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(R)]).to(torch.int32)
+    s["logits"].scatter_(1, s["top_id"].long(), 20.0)
+    loss, grad, want = distill(s, 1.0, K)
+    near(grad, want["grad"], f32, TERMS, "grad", floor=want["grad_size"])
+    near(loss, want["loss"], f32, 4 * 1.25 * 2.0 ** -18, "loss", floor=np.maximum(1.0, np.abs(want["loss"])))
