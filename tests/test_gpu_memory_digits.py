@@ -168,3 +168,21 @@ def test_the_small_remainder_of_a_sure_teacher(values, V):
     loss, grad, want = distill(s, 1.0, K)
     near(grad, want["grad"], f32, TERMS, "grad", floor=want["grad_size"])
     near(loss, want["loss"], f32, 4 * 1.25 * 2.0 ** -18, "loss", floor=np.maximum(1.0, np.abs(want["loss"])))
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("R,V,K", [(9, 40, 5), (7, 257, 20), (6, 2048, 64), (5, 2049, 20), (4, 8192, 50), (3, 8193, 1), (2, 50021, 20), (1, 140001, 64)])
+def test_every_gradient_of_a_row(R, V, K, dtype, tail):
+    """Against the size of its own terms, so that none of the many small ones of a long row could be left out."""
+    g = gen(R + V + K)
+    s = dict(logits=randn(g, R, V, dtype=DT[dtype]), tail=tail, avail=None, grad_loss=(0.5 + torch.rand(R, generator=g)) * (4096.0 if dtype == "fp16" else 1.0))
+    s["top_id"] = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(R)]).to(torch.int32)
+    s["top_value"] = torch.log(0.8 * torch.softmax(randn(g, R, K), 1))
+    if V % 2:
+        s["avail"] = (torch.rand(R, V, generator=g) < 0.7).to(torch.uint8)
+    _, grad, want = distill(s, 0.8, K)
+    near(grad, want["grad"], DT[dtype], TERMS, "grad", floor=want["grad_size"])
+    there = want["grad_size"] > 0
+    step = torch.finfo(DT[dtype]).smallest_normal * torch.finfo(DT[dtype]).eps
+    assert (np.abs(want["grad"])[there] > 2 * (TERMS * want["grad_size"][there] + step)).mean() > 0.999
