@@ -186,3 +186,57 @@ def test_every_gradient_of_a_row(R, V, K, dtype, tail):
     there = want["grad_size"] > 0
     step = torch.finfo(DT[dtype]).smallest_normal * torch.finfo(DT[dtype]).eps
     assert (np.abs(want["grad"])[there] > 2 * (TERMS * want["grad_size"][there] + step)).mean() > 0.999
+
+
+# ------------------------------------------------------------------------------------------------ at the same time
+def side_by_side(calls):
+    """Every call alone, then all of them on streams of their own, over and over without a wait: the outputs of both."""
+    alone = []
+    for call, outs in calls:
+        call()
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in outs])
+        for t in outs:
+            t.fill_(7)
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(6):
+        for stream, (call, _) in zip(streams, calls):
+            with torch.cuda.stream(stream):
+                call()
+    torch.cuda.synchronize()
+    for (_, outs), want in zip(calls, alone):
+        for got, w in zip(outs, want):
+            assert torch.equal(got, w)
+
+
+@pytest.mark.parametrize("size", [(4, 300, 1, 2, 64, 64, "bf16"), (8, 200, 2, 2, 16, 16, "fp32"), (2, 300, 1, 4, 128, 128, "bf16")])
+def test_scans_at_the_same_time(size):
+    sets = [random_scan(*size, 50 + i) for i in range(2)]
+
+    def call(s):
+        s.forward()
+        s.backward()
+
+    side_by_side([(lambda s=s: call(s), [s.o, s.s_last, *s.grads]) for s in sets])
+
+
+@pytest.mark.parametrize("R,V", [(300, 40), (40, 30001)])
+def test_distillations_at_the_same_time(R, V):
+    calls, K = [], 9
+    for i in range(2):
+        g = gen(60 + i)
+        logits = randn(g, R, V).cuda()
+        ids = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(R)]).to(torch.int32).cuda()
+        values, upstream = torch.log(0.9 * torch.softmax(randn(g, R, K), 1)).cuda(), randn(g, R).cuda()
+        loss, log_sum, rest, grad = new(R), new(R), new(R), new(R, V)
+        bytes_ = binding.marl_distill_workspace_bytes(R, V, K)
+        assert (bytes_ > 0) == (V > 2048)
+        ws = room(bytes_)
+
+        def call(logits=logits, ids=ids, values=values, upstream=upstream, loss=loss, log_sum=log_sum, rest=rest, grad=grad, ws=ws):
+            binding.marl_distill(logits, ids, values, None, 1.0, True, loss, log_sum, rest, ws)
+            binding.marl_distill_grad(logits, ids, values, None, 1.0, True, log_sum, rest, upstream, grad)
+
+        calls.append((call, [loss, log_sum, rest, grad]))
+    side_by_side(calls)
