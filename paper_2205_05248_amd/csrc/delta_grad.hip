@@ -409,11 +409,12 @@ __device__ __forceinline__ Acc careful_rows(Acc c, const Plane *a, int tile, con
 //   dq = dN K + scale f dO S'      dk = dN' Q + X K - f dV S' + t U D'
 // The log decay of a step has a part in everything that is handed on across it, and its gradient is the sum of that:
 //   dg_i = sum_(m >= i > j) F_mj + sum_(m >= i) (q_m.(scale f dO S')_m - k_m.(f dV S')_m) + sum_(j < i) k_j.(t U D')_j + f_63 <D, S>
-// with F_mj = dM_mj k_m.k_j + dN_mj q_m.k_j.  (The differences of neighbours, sum_j F_ij - sum_j F_ji and so on, are cheaper to form, but hold what does not
-// cross i too, which has to cancel: at a decay of e^-12 a tenth of the gradient was rounding.)  Value columns come 32 or 64 at a time through shared memory.  Products with rows and columns of steps are split over the waves by
+// with F_mj = dM_mj k_m.k_j + dN_mj q_m.k_j.  (A running sum of the differences of neighbours, sum_j F_ij - sum_j F_ji and so on, holds what does not cross i
+// too, which has to cancel: at a decay of e^-12 a tenth of the gradient was rounding.)
+// Value columns come 32 or 64 at a time through shared memory.  Products with rows and columns of steps are split over the waves by
 // rows, those with key columns by columns (16 w on), so that every entry of S and D is split into planes once.
 // Waves of a workgroup: with 128 keys eight, of which four form dP and four dA, else four that form both (1.64 -> 1.21 ms of 4 x 8192 x 16 heads x 128 x
-// 128 bf16).  There it reads 2.8 GB and writes 0.4, and waits 65 % of its waves' cycles: a workgroup of 512 threads with 256 registers each fills a
+// 128 bf16).  There it reads 2.9 GB and writes 0.4 in 1.16 ms, and waits 62 % of its waves' cycles: a workgroup of 512 threads with 256 registers each fills a
 // compute unit, so that nothing else works while it waits for a block of columns.
 constexpr int grad_waves(int DK) { return DK == 128 ? 8 : 4; }
 constexpr int grad_columns(int DK) { return DK == 128 ? 64 : 32; }       // at a time: more do not fit the registers of four waves

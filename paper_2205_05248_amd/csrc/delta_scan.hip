@@ -134,9 +134,10 @@ __device__ __forceinline__ void write_square(const float *from, int ld, Frag *to
 }
 
 // A workgroup per key head and chunk: K and Q as fragments, and N and P of every value head that shares them, four at a time.  Bound by what it
-// writes, 31 to 74 KB for the squares of a head and three or four matrices of its keys: 0.8 GB of 4 x 8192 x 16 heads x 128 x 128 bf16 with what the backward
-// pass needs in 207 us, 4.0 TB/s (253 us with two workgroups a compute unit, which is what shared memory had room for before N and A took that of K
-// and Q; 222 with three; with 128 registers some 25 are spilled, which costs fp32 rows, three planes each, more than the fourth workgroup gives).
+// writes, 37 or 74 KB for the squares of a head and three or four matrices of its keys: 0.87 GB of 4 x 8192 x 16 heads x 128 x 128 bf16 with what the backward
+// pass needs in 215 us, 4.0 TB/s (with a plane of P less 207 us, 253 with two workgroups a compute unit, which is what shared memory had room for before
+// N and A took that of K and Q, 222 with three; with 128 registers some 25 are spilled, which costs fp32 rows, three planes each, more than the fourth
+// workgroup gives).
 template <typename E, int DK>
 __global__ __launch_bounds__(kDeltaThreads, kExact<E> == 1 ? 4 : 3) void chunk_kernel(DeltaArgs p)
 {
@@ -297,11 +298,11 @@ __global__ __launch_bounds__(kDeltaThreads, kExact<E> == 1 ? 4 : 3) void chunk_k
 // rows 16 w on of the chunk, and rows w DK / 4 on of the state, which stays in its accumulators; the others read it as planes from shared memory.
 // What a phase needs from memory is asked for where the same phase of the chunk before has used its registers, a whole chunk ahead, and
 // whether there is another chunk or not: behind a branch the compiler would wait for it at the next wait of any kind.
-// Bound by the chain of a chunk: three barriers, between them products that wait for the splitting of what the other waves made, some 830 vector and
-// 90 matrix instructions a wave; at 128 keys and columns a chunk takes 2.2 us with 16 columns (20011 steps, 16 heads, bf16: 700 us, 128 workgroups on
-// 256 compute units) and 5.0 with 32 (4 x 8192, with keep: 644 us, waves wait 31 % of their cycles, the matrix pipe is busy for 12 %).  Everything at
-// hand a chunk ahead takes 1.4 times the registers that a third workgroup on a compute unit would leave: with 168 they spill, 88 -> 196 us of the 320 x
-// 120 batch with 4 heads of 16.  fp16 with 128 keys spills with 256 too, and has a compute unit for a workgroup: 450 -> 293 us of 4096 steps, 16 heads with keep.
+// Bound by the chain of a chunk: three barriers, between them products that wait for the splitting of what the other waves made; at 128 keys and columns a
+// chunk takes 2.5 us with 16 columns (20011 steps, 16 heads, bf16: 775 us, 128 workgroups on 256 compute units; 360 vector and 54 matrix instructions a
+// wave) and 5.4 with 32 (4 x 8192, with keep: 697 us, 900 and 108 instructions, waves wait 33 % of their cycles, the matrix pipe is busy for 13 %).  Everything
+// at hand a chunk ahead takes 1.4 times the registers that a third workgroup on a compute unit would leave: with 168 they spill, 88 -> 196 us of the 320 x 120
+// batch with 4 heads of 16.  fp16 with 128 keys spills with 256 too, and has a compute unit for a workgroup: 450 -> 293 us of 4096 steps, 16 heads with keep.
 template <typename E, int DK, int NT, bool KEEP>
 __global__ __launch_bounds__(kDeltaThreads, (NT == 1 ? kExact<E> * DK <= 192 : DK == 32) ? 2 : 1) void scan_kernel(DeltaArgs p)
 {

@@ -1,8 +1,8 @@
 // Divergence of a student's logits from a teacher's kept alternatives, and the logits' gradient.  The alternatives' places are left out of
 // the sum over the row and added at the end, so that the probability of all others is a sum of its own and not one minus a number next to
-// one.  Forward and backward are bound by the bytes of the logits where rows are long: 8191 x 50021 fp16 with 20 alternatives 212 us forward (3.9
-// TB/s) and 326 backward (5.0 TB/s).  Short rows by their instructions: 409600 x 40 fp32 with a mask and five alternatives 44 and 43 us (1.9 and 3.5
-// TB/s).  Few rows by the chain of loads and sums: 16 x 131072 bf16 with 50 alternatives 5 us, and 7.5 of a wave a row that joins the parts.
+// one.  Forward and backward are bound by the bytes of the logits where rows are long: 8191 x 50021 fp16 with 20 alternatives 205 us forward (4.0
+// TB/s) and 321 backward (5.1 TB/s).  Short rows by their instructions: 409600 x 40 fp32 with a mask and five alternatives 41 and 42 us (2.0 and 3.5
+// TB/s).  Few rows by the chain of loads and sums: 16 x 131072 bf16 with 50 alternatives 5 us, and 7.8 of a wave a row that joins the parts.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

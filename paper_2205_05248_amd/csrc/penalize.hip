@@ -266,8 +266,9 @@ int marl_penalize(int32_t dtype, int32_t R, int32_t V, const void *logits, int64
     return with_dtype(dtype, [&](auto e) {
         // Pieces are counted from the line that the row's result begins in: up to 127 bytes before it.  Every piece reads the history, but with
         // four of 8192 places on a compute unit some pass logits while others count: 777 rows of 50021 in fp16 with 4096 tokens on
-        // average, 64 biases and a mask take 61 us (25 without any of them, a copy 22; 65 with stores through the caches), with pieces of 16384
-        // and 1024 threads 82, with 4096 and 256 threads 64.  Rows of one wave up to 960: 24 x 40 with 120 tokens take 6.4 us, most of it the launch.
+        // average, 64 biases and a mask take 61 us (24 without any of them, a copy 22: reading the tokens and looking for their places in every piece
+        // takes 15 of the rest, counting them and the edit of what they touch 7, listing the biases, by one wave before the pass, 7 to 15; 65 with
+        // stores through the caches), with pieces of 16384 and 1024 threads 82, with 4096 and 256 threads 64.  Rows of one wave up to 960: 24 x 40 with 120 tokens take 6.4 us, most of it the launch.
         const auto go = [&](auto kernel, int threads, int piece) {
             const size_t lds = piece * sizeof(unsigned) + (1 + 2 * (size_t)M) * sizeof(int);       // 40 KB at most
             p.pieces = (int)(((int64_t)V + 63 + piece - 1) / piece);
